@@ -217,6 +217,127 @@ loom_status loom_attn_decode_noalloc(const void* q, const void* k_cache, const v
                                      void* stream);
 
 /*
+ * Attention's backward pass: the gradients of loom_attn_fwd's result with respect to q, k and v.
+ * The paper has no counterpart (it evaluates inference).  With P = exp(scale q.k - lse), 0 where
+ * masked, and delta = dout . o - dlse per query row:
+ *     dS = P (dout . v - delta),  dq = scale dS k,  dk = scale dS^T q,  dv = P^T dout,
+ * dk and dv summed over the query heads of a kv head.
+ *   dout   [B, Hq, Sq, D]   bf16, read: the gradient of o
+ *   q, k, v, o, lse          read: the arguments and results of loom_attn_fwd (lse is required);
+ *                            a row with lse = -inf gives and gets no gradient
+ *   dlse   [B, Hq, Sq]      fp32, read: the gradient of lse; NULL where none is wanted
+ *   dq     [B, Hq, Sq, D]   bf16, written
+ *   dk, dv [B, Hkv, Skv, D] bf16, written
+ *   workspace  device scratch of at least loom_attn_bwd_workspace_bytes(...) bytes, whose contents
+ *          on entry do not matter (row statistics, 8 bytes per query of a head in tiles of 128, and
+ *          256 bytes of counters); a workspace serves one call at a time.
+ *   causal, scale as loom_attn_fwd.  The gradients must not overlap the inputs.
+ * Scores, probabilities and sums are fp32; P and dS are rounded to bf16 before they meet dout, q
+ * and k on the tensor cores, and each gradient once when it is stored.  Every sum has a fixed
+ * order: the same inputs give the same bits.
+ * Errors: INVALID_ARG (as loom_attn_fwd; a NULL pointer other than dlse), UNSUPPORTED (D; more
+ * than 2^30 tiles of 128 rows), MISALIGNED (dlse, lse: 4 bytes; the others 16), WORKSPACE, CUDA.
+ */
+loom_status loom_attn_bwd(const void* dout, const void* q, const void* k, const void* v, const void* o,
+                          const float* lse, const float* dlse, void* dq, void* dk, void* dv,
+                          void* workspace, size_t workspace_bytes, int B, int Hq, int Hkv, int Sq,
+                          int Skv, int D, int causal, float scale, void* stream);
+/* Workspace bytes of loom_attn_bwd; 0 on invalid or unsupported sizes. */
+size_t loom_attn_bwd_workspace_bytes(int B, int Hq, int Hkv, int Sq, int Skv, int D);
+
+/*
+ * The same over a ragged batch packed token-major: the gradients of loom_attn_fwd_varlen.
+ *   dout, o, dq  [total_q, Hq, D];  k, v, dk, dv  [total_k, Hkv, D];  lse, dlse  [Hq, total_q]
+ *   cu_seqlens_q, cu_seqlens_k  as loom_attn_fwd_varlen
+ *   max_seqlen_q, max_seqlen_k  upper bounds of the lengths (they only size the launch)
+ * No row of one sequence reaches another's gradients, whatever it holds.  total_q = 0 or total_k =
+ * 0 writes zeros; pointers to tensors without elements may be NULL.
+ * Errors: as loom_attn_bwd; cu_seqlens must be 4-byte aligned.
+ */
+loom_status loom_attn_bwd_varlen(const void* dout, const void* q, const void* k, const void* v,
+                                 const void* o, const float* lse, const float* dlse, void* dq, void* dk,
+                                 void* dv, const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_k,
+                                 void* workspace, size_t workspace_bytes, int B, int Hq, int Hkv,
+                                 int total_q, int total_k, int max_seqlen_q, int max_seqlen_k, int D,
+                                 int causal, float scale, void* stream);
+/* Workspace bytes of loom_attn_bwd_varlen; 0 on invalid or unsupported sizes. */
+size_t loom_attn_bwd_varlen_workspace_bytes(int B, int Hq, int Hkv, int total_q, int total_k, int D);
+
+/*
+ * From a packed QKV projection (loom_gemm_bf16 with the three weights side by side) to what
+ * attention takes: an RMS norm of every query and key head, the position rotation, and the split.
+ * The paper has no counterpart.  Per query or key head x of a token, with that tensor's norm
+ * weight w and the token's row (c, s) of the tables:
+ *     z = x w / sqrt(mean(x^2) + eps),   y_a = z_a c_i - z_b s_i,   y_b = z_b c_i + z_a s_i
+ * for the pairs i < rotary_dim / 2: (a, b) = (i, i + rotary_dim / 2), or interleaved (2i, 2i + 1);
+ * y = z past rotary_dim.  Value heads are copied.
+ *   qkv        [T, (Hq + 2 Hkv) D] bf16, read: a token's query, key and value heads; rows
+ *              qkv_stride elements apart (a multiple of 8, at least the row)
+ *   q_weight, k_weight  [D], read: bf16 or fp32 (weight_type)
+ *   cos, sin   [table_rows, rotary_dim / 2] fp32, read
+ *   positions  [T] int32 on the device: the tables' row of each token, clamped to the tables;
+ *              NULL: token t has position t, or t % seq_len with seq_len > 0
+ *   q, k, v    bf16, written.  seq_len = 0: packed [T, Hq, D] and [T, Hkv, D] (as
+ *              loom_attn_fwd_varlen takes them); seq_len > 0: T / seq_len sequences,
+ *              [T / seq_len, Hq or Hkv, seq_len, D] (as loom_attn_fwd takes them).  They must not
+ *              overlap qkv.
+ * Arithmetic is fp32; each value is rounded once, when it is stored.
+ * Errors: INVALID_ARG (NULL pointer, a size <= 0, T < 0, T % seq_len, qkv_stride below a row, eps
+ * not finite or <= 0, weight_type or interleaved not one of theirs), UNSUPPORTED (D not 64 or 128;
+ * rotary_dim not a multiple of 16 from 16 to D), MISALIGNED (positions: 4 bytes; the others 16;
+ * qkv_stride % 8), CUDA.  T = 0 returns LOOM_OK at once.
+ */
+enum { LOOM_BF16 = 0, LOOM_FP32 = 1 }; /* weight_type */
+loom_status loom_qkv_norm_rope(const void* qkv, int64_t qkv_stride, const void* q_weight,
+                               const void* k_weight, int weight_type, const float* cos,
+                               const float* sin, int table_rows, int rotary_dim, int interleaved,
+                               const int32_t* positions, void* q, void* k, void* v, int T, int seq_len,
+                               int Hq, int Hkv, int D, float eps, void* stream);
+
+/*
+ * Its serving form: q [T, Hq, D] is written, and k and v go to their rows of the caches that
+ * loom_attn_decode and loom_attn_decode_paged read.
+ *   positions  [T] int32 on the device (required)
+ *   slots      [T] int32 on the device (required): token t's row, page slots[t] / page_size, row
+ *              slots[t] % page_size of it; a slot outside [0, num_pages page_size) is not written
+ *              (padding).  Two tokens of a call must not share a slot.
+ *   k_cache, v_cache  bf16, written at those rows: kv_layout 0 (NHD) [num_pages, page_size, Hkv,
+ *              D], 1 (HND) [num_pages, Hkv, page_size, D].  A contiguous cache [B, Hkv, Skv, D] is
+ *              layout 1 with num_pages = B, page_size = Skv and slots b Skv + position.
+ * Any page_size; everything else as loom_qkv_norm_rope.
+ * Errors: as loom_qkv_norm_rope; kv_layout not 0 or 1: INVALID_ARG; more than 2^31 - 1 rows:
+ * UNSUPPORTED; slots: 4-byte aligned.
+ */
+loom_status loom_qkv_norm_rope_cache(const void* qkv, int64_t qkv_stride, const void* q_weight,
+                                     const void* k_weight, int weight_type, const float* cos,
+                                     const float* sin, int table_rows, int rotary_dim, int interleaved,
+                                     const int32_t* positions, const int32_t* slots, void* q,
+                                     void* k_cache, void* v_cache, int num_pages, int page_size,
+                                     int kv_layout, int T, int Hq, int Hkv, int D, float eps,
+                                     void* stream);
+
+/*
+ * The gradients of loom_qkv_norm_rope: of the projection, and of the two norm weights.
+ *   dq, dk, dv  bf16, read: the gradients of q, k and v, laid out like them (seq_len)
+ *   qkv, weights, tables, positions  as the forward call had them (the norms are recomputed)
+ *   dqkv       [T, (Hq + 2 Hkv) D] bf16, written; rows dqkv_stride elements apart (a multiple of 8;
+ *              what lies between the rows is left alone)
+ *   dq_weight, dk_weight  [D] fp32, written: summed over all tokens and heads in a fixed order
+ *   workspace  device scratch of at least loom_qkv_norm_rope_bwd_workspace_bytes(D) bytes, whose
+ *              contents on entry do not matter; it serves one call at a time.
+ * Errors: as loom_qkv_norm_rope, WORKSPACE.  T = 0 writes zeros to dq_weight and dk_weight.
+ */
+loom_status loom_qkv_norm_rope_bwd(const void* dq, const void* dk, const void* dv, const void* qkv,
+                                   int64_t qkv_stride, const void* q_weight, const void* k_weight,
+                                   int weight_type, const float* cos, const float* sin, int table_rows,
+                                   int rotary_dim, int interleaved, const int32_t* positions, void* dqkv,
+                                   int64_t dqkv_stride, float* dq_weight, float* dk_weight,
+                                   void* workspace, size_t workspace_bytes, int T, int seq_len, int Hq,
+                                   int Hkv, int D, float eps, void* stream);
+/* Workspace bytes of loom_qkv_norm_rope_bwd; 0 on an unsupported D. */
+size_t loom_qkv_norm_rope_bwd_workspace_bytes(int D);
+
+/*
  * Analytic schedule model (paper Sec. 2.6: HEG latency, Eq. 5-7, and the constrained
  * selection of Eq. 8-9, solved by enumeration) with the GB300 architecture description
  * of Sec. 2.7.  The kernels are compiled with the plan these functions report.
@@ -340,7 +461,8 @@ const char* loom_status_string(loom_status status);
  *   internal wait of the kernels (default 2e9).  0 restores the default.
  * loom_debug_inject: 0 = off; 1 = the decode split kernel's loader skips the copy of
  *   its second stage; 2 = the prefill kernel's loader skips its second K tile; 3 = the
- *   GEMM loader skips its third stage (of each CTA's K range).  The
+ *   GEMM loader skips its third stage (of each CTA's K range); 4 = the attention backward
+ *   kernel's loader stops before its second query tile.  The
  *   waits on the skipped data then expire, the kernel unwinds and the next
  *   loom_attn_check_error returns LOOM_ERR_TIMEOUT.  Host-side switch; no fault.
  */

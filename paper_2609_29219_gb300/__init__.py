@@ -32,6 +32,8 @@ __all__ = [
     "loom_model_decode_persistent_time_us", "loom_model_decode_tc_time_us", "DECODE_SPLIT_MERGE", "DECODE_PERSISTENT", "DECODE_CLUSTER",
     "loom_debug_prefill_slots", "loom_debug_decode_stage_plan", "loom_debug_gemm_stages",
     "loom_debug_gemm_order", "loom_debug_decode_tensor_cores", "loom_attn_fwd_cluster",
+    "loom_attn_bwd", "loom_attn_bwd_workspace_bytes", "loom_attn_bwd_varlen", "loom_attn_bwd_varlen_workspace_bytes",
+    "loom_qkv_norm_rope", "loom_qkv_norm_rope_cache", "loom_qkv_norm_rope_bwd", "loom_qkv_norm_rope_bwd_workspace_bytes",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -160,6 +162,24 @@ def capi() -> ctypes.CDLL:
             lib.loom_debug_gemm_order.restype = None
             lib.loom_debug_decode_tensor_cores.argtypes = [i32]
             lib.loom_debug_decode_tensor_cores.restype = None
+            i64 = ctypes.c_int64
+            lib.loom_attn_bwd.argtypes = [vp] * 11 + [sz] + [i32] * 7 + [f32, vp]
+            lib.loom_attn_bwd.restype = i32
+            lib.loom_attn_bwd_workspace_bytes.argtypes = [i32] * 6
+            lib.loom_attn_bwd_workspace_bytes.restype = sz
+            lib.loom_attn_bwd_varlen.argtypes = [vp] * 13 + [sz] + [i32] * 9 + [f32, vp]
+            lib.loom_attn_bwd_varlen.restype = i32
+            lib.loom_attn_bwd_varlen_workspace_bytes.argtypes = [i32] * 6
+            lib.loom_attn_bwd_varlen_workspace_bytes.restype = sz
+            norm = [vp, vp, i32, vp, vp, i32, i32, i32, vp]  # the weights, the tables and the positions
+            lib.loom_qkv_norm_rope.argtypes = [vp, i64] + norm + [vp] * 3 + [i32] * 5 + [f32, vp]
+            lib.loom_qkv_norm_rope.restype = i32
+            lib.loom_qkv_norm_rope_cache.argtypes = [vp, i64] + norm + [vp] * 4 + [i32] * 7 + [f32, vp]
+            lib.loom_qkv_norm_rope_cache.restype = i32
+            lib.loom_qkv_norm_rope_bwd.argtypes = [vp] * 4 + [i64] + norm + [vp, i64, vp, vp, vp, sz] + [i32] * 5 + [f32, vp]
+            lib.loom_qkv_norm_rope_bwd.restype = i32
+            lib.loom_qkv_norm_rope_bwd_workspace_bytes.argtypes = [i32]
+            lib.loom_qkv_norm_rope_bwd_workspace_bytes.restype = sz
             _lib = lib
     return _lib
 
@@ -448,6 +468,246 @@ def loom_attn_decode_paged(q, k_cache, v_cache, block_table, seqlens_k, o=None, 
         max_pages, 0 if layout == "nhd" else 1, D, float(scale), int(num_splits), _stream_of(stream, q))
     _check(st, "loom_attn_decode_paged")
     return (o, lse) if (return_lse or lse is not None) else o
+
+
+def loom_attn_bwd_workspace_bytes(B, Hq, Hkv, Sq, Skv, D) -> int:
+    return int(capi().loom_attn_bwd_workspace_bytes(B, Hq, Hkv, Sq, Skv, D))
+
+
+def loom_attn_bwd_varlen_workspace_bytes(B, Hq, Hkv, total_q, total_k, D) -> int:
+    return int(capi().loom_attn_bwd_varlen_workspace_bytes(B, Hq, Hkv, total_q, total_k, D))
+
+
+def _scratch(workspace, need, t):
+    """Pointer and size of the workspace, one of ``need`` bytes made here if None is given (and the
+    tensor, which has to live until the call has been queued)."""
+    if workspace is None:
+        workspace = _new((max(need, 16),), (1,), _torch_mod.uint8, t)
+    return _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(), workspace
+
+
+def _bwd_operands(do, q, k, v, o, lse, dlse, dq, dk, dv, ndim):
+    """Pointers of the backward entry points' tensor arguments, and the gradients."""
+    bf16 = _torch().bfloat16
+    qp, kp, vp_ = _ptr(q, "q", bf16, ndim), _ptr(k, "k", bf16, ndim), _ptr(v, "v", bf16, ndim)
+    if v.shape != k.shape or k.shape[-1] != q.shape[-1]:
+        raise ValueError("q/k/v shapes disagree")
+    for t, name in ((do, "do"), (o, "o")):
+        if t.shape != q.shape:
+            raise ValueError(f"{name} must have q's shape")
+    dop, op = _ptr(do, "do", bf16, ndim), _ptr(o, "o", bf16, ndim)
+    f32 = _torch_mod.float32
+    if lse is None:
+        raise TypeError("lse is needed: call the forward pass with return_lse=True")
+    lp = _dev_ptr(lse, "lse", f32)
+    dlp = None
+    if dlse is not None:
+        if dlse.shape != lse.shape:
+            raise ValueError("dlse must have lse's shape")
+        dlp = _dev_ptr(dlse, "dlse", f32)
+    if dq is None:
+        dq = _new(tuple(q.shape), q.stride(), bf16, q, True)
+    if dk is None:
+        dk = _new(tuple(k.shape), k.stride(), bf16, k, True)
+    if dv is None:
+        dv = _new(tuple(v.shape), v.stride(), bf16, v, True)
+    for t, like, name in ((dq, q, "dq"), (dk, k, "dk"), (dv, v, "dv")):
+        if t.shape != like.shape:
+            raise ValueError(f"{name} must have {name[1]}'s shape")
+    grads = (_ptr(dq, "dq", bf16, ndim), _ptr(dk, "dk", bf16, ndim), _ptr(dv, "dv", bf16, ndim))
+    return (dop, qp, kp, vp_, op, lp, dlp, *grads), (dq, dk, dv)
+
+
+def loom_attn_bwd(do, q, k, v, o, lse, dq=None, dk=None, dv=None, workspace=None, *, causal=False, scale=None, dlse=None,
+                  stream=None):
+    """Gradients of ``loom_attn_fwd``.  do and o [B,Hq,Sq,D], q, k, v as the forward call had them,
+    lse [B,Hq,Sq] as it returned it; dlse: the gradient of lse, or None.
+
+    ``workspace`` is a CUDA uint8 tensor of at least ``loom_attn_bwd_workspace_bytes`` bytes
+    (allocated here if None).  Writes and returns ``dq, dk, dv`` (allocated if None)."""
+    ptrs, grads = _bwd_operands(do, q, k, v, o, lse, dlse, dq, dk, dv, 4)
+    B, Hq, Sq, D = q.shape
+    Bk, Hkv, Skv, _ = k.shape
+    if Bk != B:
+        raise ValueError("q/k/v shapes disagree")
+    if tuple(lse.shape) != (B, Hq, Sq):
+        raise ValueError("lse must be [B, Hq, Sq]")
+    lib = _lib or capi()
+    need = 0 if workspace is not None else lib.loom_attn_bwd_workspace_bytes(B, Hq, Hkv, Sq, Skv, D)
+    wp, wbytes, workspace = _scratch(workspace, need, q)
+    if scale is None:
+        scale = D ** -0.5
+    st = lib.loom_attn_bwd(*ptrs, wp, wbytes, B, Hq, Hkv, Sq, Skv, D, int(bool(causal)), float(scale), _stream_of(stream, q))
+    _check(st, "loom_attn_bwd")
+    return grads
+
+
+def loom_attn_bwd_varlen(do, q, k, v, o, lse, cu_seqlens_q, cu_seqlens_k, max_seqlen_q, max_seqlen_k, dq=None, dk=None,
+                         dv=None, workspace=None, *, causal=False, scale=None, dlse=None, stream=None):
+    """Gradients of ``loom_attn_fwd_varlen``.  do, o and q [total_q, Hq, D], k and v [total_k, Hkv, D],
+    lse (and dlse) [Hq, total_q]; cu_seqlens_q / cu_seqlens_k [B + 1] int32 on the device; the
+    longest lengths as ints.  Writes and returns ``dq, dk, dv`` (allocated if None)."""
+    ptrs, grads = _bwd_operands(do, q, k, v, o, lse, dlse, dq, dk, dv, 3)
+    total_q, Hq, D = q.shape
+    total_k, Hkv, _ = k.shape
+    if lse.numel() != Hq * total_q:
+        raise ValueError("lse must hold Hq*total_q values")
+    i32 = _torch_mod.int32
+    cqp, ckp = _ptr(cu_seqlens_q, "cu_seqlens_q", i32, 1), _ptr(cu_seqlens_k, "cu_seqlens_k", i32, 1)
+    if cu_seqlens_q.numel() != cu_seqlens_k.numel() or cu_seqlens_q.numel() < 2:
+        raise ValueError("cu_seqlens_q and cu_seqlens_k must both be [B + 1]")
+    B = cu_seqlens_q.numel() - 1
+    lib = _lib or capi()
+    need = 0 if workspace is not None else lib.loom_attn_bwd_varlen_workspace_bytes(B, Hq, Hkv, total_q, total_k, D)
+    wp, wbytes, workspace = _scratch(workspace, need, q)
+    if scale is None:
+        scale = D ** -0.5
+    st = lib.loom_attn_bwd_varlen(*ptrs, cqp, ckp, wp, wbytes, B, Hq, Hkv, total_q, total_k, int(max_seqlen_q),
+                                  int(max_seqlen_k), D, int(bool(causal)), float(scale), _stream_of(stream, q))
+    _check(st, "loom_attn_bwd_varlen")
+    return grads
+
+
+def _row_matrix(t, name, width):
+    """Pointer and row distance of a bf16 CUDA matrix whose rows are contiguous."""
+    torch = _torch()
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if t.dtype is not torch.bfloat16:
+        raise TypeError(f"{name} must be {torch.bfloat16}, got {t.dtype}")
+    if t.dim() != 2 or t.shape[1] != width or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be [T, {width}] with contiguous rows, got shape {tuple(t.shape)}")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else width
+
+
+def _norm_operands(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, positions, interleaved):
+    """What the norm-and-rotation entry points share: (qkv pointer, its row distance), the weights',
+    tables' and positions' arguments, T and D."""
+    torch = _torch()
+    wt = q_weight.dtype
+    if wt not in (torch.bfloat16, torch.float32):
+        raise TypeError(f"q_weight must be {torch.bfloat16} or {torch.float32}, got {wt}")
+    qwp, kwp = _ptr(q_weight, "q_weight", wt, 1), _ptr(k_weight, "k_weight", wt, 1)
+    D = q_weight.shape[0]
+    if k_weight.shape[0] != D:
+        raise ValueError("q_weight and k_weight must both be [D]")
+    f32 = torch.float32
+    cp, sp = _ptr(cos, "cos", f32, 2), _ptr(sin, "sin", f32, 2)
+    if cos.shape != sin.shape:
+        raise ValueError("cos and sin must both be [positions, rotary_dim / 2]")
+    xp, stride = _row_matrix(qkv, "qkv", (num_heads + 2 * num_kv_heads) * D)
+    pp = None
+    if positions is not None:
+        pp = _ptr(positions, "positions", torch.int32, 1)
+        if positions.shape[0] != qkv.shape[0]:
+            raise ValueError("positions must be [T]")
+    return (xp, stride), (qwp, kwp, int(wt is f32), cp, sp, cos.shape[0], 2 * cos.shape[1], int(bool(interleaved)), pp), \
+        qkv.shape[0], D
+
+
+def loom_qkv_norm_rope(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, positions=None, q=None, k=None, v=None, *,
+                       seq_len=0, eps=1e-6, interleaved=False, stream=None):
+    """RMS norm of each query and key head, the position rotation, and the split of a packed projection.
+
+    qkv [T, (num_heads + 2 num_kv_heads) D] bf16 (its rows may lie further apart); q_weight, k_weight
+    [D] bf16 or fp32; cos, sin [positions, rotary_dim / 2] fp32; positions [T] int32 (None: t, or t %
+    seq_len).  Writes and returns ``q, k, v`` (allocated if None): [T, H, D], or with ``seq_len``
+    [T / seq_len, H, seq_len, D], as the ragged and the dense prefill take them."""
+    x, norm, T, D = _norm_operands(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, positions, interleaved)
+    if seq_len < 0 or (seq_len and T % seq_len):
+        raise ValueError("T must be a multiple of seq_len")
+    bf16 = _torch_mod.bfloat16
+    outs = []
+    for t, name, H in ((q, "q", num_heads), (k, "k", num_kv_heads), (v, "v", num_kv_heads)):
+        shape = (T // seq_len, H, seq_len, D) if seq_len else (T, H, D)
+        if t is None:
+            t = _new(shape, (H * seq_len * D, seq_len * D, D, 1) if seq_len else (H * D, D, 1), bf16, qkv)
+        elif tuple(t.shape) != shape:
+            raise ValueError(f"{name} must be {list(shape)}")
+        outs.append(t)
+    ptrs = [_ptr(t, n, bf16, t.dim()) for t, n in zip(outs, "qkv")]
+    st = (_lib or capi()).loom_qkv_norm_rope(*x, *norm, *ptrs, T, int(seq_len), num_heads, num_kv_heads, D, float(eps),
+                                             _stream_of(stream, qkv))
+    _check(st, "loom_qkv_norm_rope")
+    return tuple(outs)
+
+
+def loom_qkv_norm_rope_cache(qkv, q_weight, k_weight, cos, sin, positions, slots, k_cache, v_cache, num_heads, q=None, *,
+                             layout="nhd", eps=1e-6, interleaved=False, stream=None):
+    """``loom_qkv_norm_rope`` for serving: k and v go to their rows of the caches, q is returned.
+
+    positions and slots [T] int32: token t's row is slots[t] % page_size of page slots[t] //
+    page_size (a slot outside the cache, such as -1, is not written).  k_cache, v_cache [num_pages,
+    page_size, Hkv, D] (layout "nhd") or [num_pages, Hkv, page_size, D] ("hnd"; also a contiguous
+    cache [B, Hkv, capacity, D], whose slots are b * capacity + position).  Returns q [T, num_heads, D]."""
+    if layout not in ("nhd", "hnd"):
+        raise ValueError("layout is 'nhd' or 'hnd'")
+    bf16 = _torch().bfloat16
+    kp, vp_ = _ptr(k_cache, "k_cache", bf16, 4), _ptr(v_cache, "v_cache", bf16, 4)
+    pages, a, b, Dk = k_cache.shape
+    page_size, Hkv = (a, b) if layout == "nhd" else (b, a)
+    if positions is None or slots is None:
+        raise TypeError("positions and slots are needed")
+    x, norm, T, D = _norm_operands(qkv, q_weight, k_weight, cos, sin, num_heads, Hkv, positions, interleaved)
+    if v_cache.shape != k_cache.shape or Dk != D:
+        raise ValueError("the caches must have one shape, and D the weights'")
+    slp = _ptr(slots, "slots", _torch_mod.int32, 1)
+    if slots.shape[0] != T:
+        raise ValueError("slots must be [T]")
+    if q is None:
+        q = _new((T, num_heads, D), (num_heads * D, D, 1), bf16, qkv)
+    elif tuple(q.shape) != (T, num_heads, D):
+        raise ValueError(f"q must be {[T, num_heads, D]}")
+    st = (_lib or capi()).loom_qkv_norm_rope_cache(*x, *norm, slp, _ptr(q, "q", bf16, 3), kp, vp_, pages, page_size,
+                                                   0 if layout == "nhd" else 1, T, num_heads, Hkv, D, float(eps),
+                                                   _stream_of(stream, qkv))
+    _check(st, "loom_qkv_norm_rope_cache")
+    return q
+
+
+def loom_qkv_norm_rope_bwd_workspace_bytes(D) -> int:
+    return int(capi().loom_qkv_norm_rope_bwd_workspace_bytes(D))
+
+
+def loom_qkv_norm_rope_bwd(dq, dk, dv, qkv, q_weight, k_weight, cos, sin, positions=None, dqkv=None, dq_weight=None,
+                           dk_weight=None, workspace=None, *, eps=1e-6, interleaved=False, stream=None):
+    """Gradients of ``loom_qkv_norm_rope``: dq, dk, dv laid out as it returned q, k, v ([T, H, D] or
+    [B, H, seq_len, D]), the rest as the forward call had it.  Writes and returns ``dqkv`` (like qkv;
+    its rows may lie further apart), ``dq_weight`` and ``dk_weight`` ([D] fp32), allocated if None.
+    ``workspace``: a CUDA uint8 tensor of ``loom_qkv_norm_rope_bwd_workspace_bytes(D)`` bytes."""
+    torch = _torch()
+    bf16, f32 = torch.bfloat16, torch.float32
+    ndim = dq.dim()
+    if ndim not in (3, 4):
+        raise ValueError("dq must be [T, H, D] or [B, H, seq_len, D]")
+    ptrs = [_ptr(t, n, bf16, ndim) for t, n in ((dq, "dq"), (dk, "dk"), (dv, "dv"))]
+    Hq, Hkv = dq.shape[1], dk.shape[1]
+    x, norm, T, D = _norm_operands(qkv, q_weight, k_weight, cos, sin, Hq, Hkv, positions, interleaved)
+    seq_len = dq.shape[2] if ndim == 4 else 0
+    shape = (lambda H: (dq.shape[0], H, seq_len, D)) if ndim == 4 else (lambda H: (T, H, D))
+    if (tuple(dq.shape) != shape(Hq) or tuple(dk.shape) != shape(Hkv) or dv.shape != dk.shape
+            or (ndim == 4 and dq.shape[0] * seq_len != T)):
+        raise ValueError("dq, dk and dv must be laid out as q, k and v of the forward call")
+    width = (Hq + 2 * Hkv) * D
+    if dqkv is None:
+        dqkv = _new((T, width), (width, 1), bf16, qkv)
+    elif tuple(dqkv.shape) != (T, width):
+        raise ValueError(f"dqkv must be {[T, width]}")
+    if dq_weight is None:
+        dq_weight = _new((D,), (1,), f32, qkv)
+    if dk_weight is None:
+        dk_weight = _new((D,), (1,), f32, qkv)
+    if tuple(dq_weight.shape) != (D,) or tuple(dk_weight.shape) != (D,):
+        raise ValueError("dq_weight and dk_weight must be [D]")
+    lib = _lib or capi()
+    wp, wbytes, workspace = _scratch(workspace, lib.loom_qkv_norm_rope_bwd_workspace_bytes(D), qkv)
+    st = lib.loom_qkv_norm_rope_bwd(*ptrs, *x, *norm, *_row_matrix(dqkv, "dqkv", width), _ptr(dq_weight, "dq_weight", f32, 1),
+                                    _ptr(dk_weight, "dk_weight", f32, 1), wp, wbytes, T, int(seq_len), Hq, Hkv, D, float(eps),
+                                    _stream_of(stream, qkv))
+    _check(st, "loom_qkv_norm_rope_bwd")
+    return dqkv, dq_weight, dk_weight
 
 
 def loom_attn_check_error(stream=None, device=None):

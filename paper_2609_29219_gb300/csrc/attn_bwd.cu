@@ -1,0 +1,983 @@
+// Attention's backward pass for GB300 (sm_103a): TMA + mbarrier rings, tcgen05 MMAs with TMEM
+// accumulators, warp-specialised loader / MMA / elementwise roles.
+//
+// With S = scale Q K^T, P = exp(S - LSE) (0 where masked), dP = dO V^T and, per query row,
+// delta = dO . O - dLSE,
+//     dS = P o (dP - delta),   dV = P^T dO,   dK = scale dS^T Q,   dQ = scale dS K
+// (dK and dV summed over the query heads of a kv head).  P is recomputed from LSE, which the
+// forward pass returns, so no score leaves the chip.
+//
+// Two launches:
+//   attn_bwd_rows_kernel  delta and LSE of every query row, negated and in base 2, into the
+//                         workspace in tiles of 128 rows, and the item counters zeroed
+//   attn_bwd_kernel       persistent CTAs.  First the items (kv tile of 128 keys of a kv head):
+//                         dK and dV stay in TMEM while the CTA walks the query tiles of every
+//                         head of the group.  Then the items (query tile of 128 rows of a head):
+//                         dQ stays in TMEM while the CTA walks the keys.
+// Every gradient is summed in one CTA in a fixed order: no atomics on values, no fp32 copies of
+// the gradients in memory, the same bits each time.  The price is that S and dP are computed in
+// both walks: seven products of 128 x 128 x D per pair of tiles instead of five.
+// Items are taken from a counter, long ones first, so CTAs that finish the kv items early start on
+// the query items.
+#include <cuda.h>
+#include <cuda_bf16.h>
+
+#include <cmath>
+#include <cstring>
+#include <mutex>
+
+#include "bwd.h"
+#include "kernels.h"
+#include "ptx.cuh"
+
+namespace loom {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kTile = 128;   // queries and keys per tile
+constexpr int kThreads = 320;  // 8 elementwise warps, loader, MMA
+constexpr int kStat = 2 * kTile;  // floats of a query tile's row statistics: -LSE (base 2), then -delta
+
+template <int D>
+struct BwdCfg {
+  static constexpr int NBOX = D / 64;  // 128-byte-swizzled boxes of 64 columns per tile
+  static constexpr uint32_t BOX_BYTES = kTile * 128;
+  static constexpr uint32_t TILE_BYTES = NBOX * BOX_BYTES;
+  // kv items: K, V, then rings of Q and dO tiles and of row statistics
+  static constexpr int NQ = D == 128 ? 2 : 4;
+  static constexpr uint32_t K_OFF = 0, V_OFF = TILE_BYTES;
+  static constexpr uint32_t QR_OFF = 2 * TILE_BYTES, DOR_OFF = QR_OFF + NQ * TILE_BYTES;
+  static constexpr uint32_t ST_OFF = DOR_OFF + NQ * TILE_BYTES;
+  static constexpr uint32_t KV_END = ST_OFF + NQ * kStat * 4;
+  // query items: Q, dO, then rings of K and V tiles
+  static constexpr int NK = D == 128 ? 3 : 5, NV = D == 128 ? 2 : 4;
+  static constexpr uint32_t Q_OFF = 0, DO_OFF = TILE_BYTES;
+  static constexpr uint32_t KR_OFF = 2 * TILE_BYTES, VR_OFF = KR_OFF + NK * TILE_BYTES;
+  static constexpr uint32_t Q_END = VR_OFF + NV * TILE_BYTES;
+  static constexpr uint32_t ITEM_OFF = KV_END > Q_END ? KV_END : Q_END;  // two item records
+  static constexpr uint32_t BAR_OFF = ITEM_OFF + 2 * 64;
+  static constexpr int NBAR = 72;
+  static constexpr uint32_t TMEM_PTR_OFF = BAR_OFF + NBAR * 8;
+  static constexpr uint32_t ABORT_OFF = TMEM_PTR_OFF + 8;
+  static constexpr uint32_t BYTES = ABORT_OFF + 16 + 1024;  // + alignment slack
+  static_assert(BYTES <= 227 * 1024, "shared memory budget");
+  // TMEM: S / P at 0, dP / dS at 128; kv items dV at 256, dK at 256 + D; query items dQ at 256,
+  // two buffers of dS at 384 and 448
+  static constexpr uint32_t S_COL = 0, DP_COL = 128, DV_COL = 256, DK_COL = 256 + D, DQ_COL = 256, DS_COL = 384;
+};
+
+struct BwdParams {
+  __nv_bfloat16 *dq, *dk, *dv;
+  const float* stats;       // [planes][tiles][2][128]
+  unsigned int* counters;   // [0] kv items, [1] query items
+  int B, Hq, Hkv, Sq, Skv, causal;
+  float c;                  // scale * log2(e)
+  float scale;
+  int q_tiles, kv_tiles;    // dense: tiles per plane
+  int stat_tiles;           // tiles of row statistics per plane
+  int q_items, kv_items;    // dense: items
+  int q_block, kv_block;    // planes whose tiles are dealt together (see item order)
+  const int32_t *cu_q, *cu_k;
+  int total_q, total_k;
+  KernelCtl ctl;
+};
+
+// One item as the roles see it.  Rows are counted within the sequence; a tile's rows r of head h
+// start at row `qb + r` of plane h (ragged) or at row r of plane b * H + h (dense).
+struct Item {
+  int n;          // inner steps in all (0: gradients are zero); -1: no item is left
+  int row0;       // first row of the item's own tile (keys / queries)
+  int plane;      // kv items: kv plane; query items: query plane
+  int other;      // kv items: first query plane of the group; query items: kv plane
+  int t0, nt;     // inner tiles per plane: t0 .. t0 + nt - 1
+  int sq, skv;    // lengths
+  int qb, kb;     // first query and key row of the sequence (0 for dense)
+  int stat0;      // first tile of the sequence within a plane's row statistics
+};
+static_assert(sizeof(Item) <= 64, "item record");
+
+// ---------------------------------------------------------------- item order
+// Dense: blocks of `block` planes; within a block tile by tile over the planes, the longest
+// tiles first.  Planes in flight together share what they walk in L2.
+struct DenseItem {
+  int tile, plane;
+};
+__device__ __forceinline__ DenseItem dense_item(int idx, int tiles, int planes, int block) {
+  const int per = block * tiles, blk = idx / per, in = idx - blk * per;
+  const int p0 = blk * block, nb = min(block, planes - p0);
+  return {in / nb, p0 + in % nb};
+}
+
+// Ragged: sequences in order; a cursor that only moves forward (a CTA's indices grow).
+struct Cursor {
+  int b;
+  long long first;  // index of sequence b's first item
+  int tiles;        // its tiles per plane
+};
+__device__ __forceinline__ int seq_tiles(const int32_t* cu, int b) {
+  const int n = cu[b + 1] - cu[b];
+  return n > 0 ? (n + kTile - 1) / kTile : 0;
+}
+__device__ __forceinline__ bool cursor_to(Cursor& cur, const int32_t* cu, int B, int planes, long long idx) {
+  if (cur.b < 0) cur = {0, 0, seq_tiles(cu, 0)};
+  while (cur.b < B && idx >= cur.first + static_cast<long long>(cur.tiles) * planes) {
+    cur.first += static_cast<long long>(cur.tiles) * planes;
+    ++cur.b;
+    cur.tiles = cur.b < B ? seq_tiles(cu, cur.b) : 0;
+  }
+  return cur.b < B;
+}
+// First tile of sequence b in a plane's row statistics: tiles of different sequences never meet.
+__device__ __forceinline__ int ragged_stat0(const int32_t* cu_q, int b) { return cu_q[b] / kTile + b; }
+
+// KV: item idx of the kv items, else of the query items.
+template <bool KV, bool VARLEN>
+__device__ __forceinline__ Item make_item(const BwdParams& p, long long idx, Cursor& cur) {
+  Item it;
+  it.n = -1;
+  int tile, b;
+  const int G = p.Hq / p.Hkv;
+  if constexpr (VARLEN) {
+    const int planes = KV ? p.Hkv : p.Hq;
+    const int32_t* cu = KV ? p.cu_k : p.cu_q;
+    if (!cursor_to(cur, cu, p.B, planes, idx)) return it;
+    b = cur.b;
+    const int in = static_cast<int>(idx - cur.first);
+    tile = in / planes;
+    it.plane = in % planes;
+    it.other = KV ? it.plane * G : it.plane / G;
+    it.qb = p.cu_q[b];
+    it.kb = p.cu_k[b];
+    it.sq = p.cu_q[b + 1] - it.qb;
+    it.skv = p.cu_k[b + 1] - it.kb;
+    it.stat0 = ragged_stat0(p.cu_q, b);
+    // (causal query tiles are longest at the sequence's end)
+    if (!KV && p.causal) tile = cur.tiles - 1 - tile;
+  } else {
+    if (idx >= (KV ? p.kv_items : p.q_items)) return it;
+    const DenseItem d = KV ? dense_item(static_cast<int>(idx), p.kv_tiles, p.B * p.Hkv, p.kv_block)
+                           : dense_item(static_cast<int>(idx), p.q_tiles, p.B * p.Hq, p.q_block);
+    it.plane = d.plane;
+    if constexpr (KV) {
+      b = d.plane / p.Hkv;
+      it.other = b * p.Hq + (d.plane - b * p.Hkv) * G;
+    } else {
+      b = d.plane / p.Hq;
+      it.other = b * p.Hkv + (d.plane - b * p.Hq) / G;
+    }
+    tile = !KV && p.causal ? p.q_tiles - 1 - d.tile : d.tile;
+    it.qb = it.kb = it.stat0 = 0;
+    it.sq = p.Sq;
+    it.skv = p.Skv;
+  }
+  it.row0 = tile * kTile;
+  const int off = it.skv - it.sq;  // query i sees keys <= i + off
+  if constexpr (KV) {
+    const int tiles = (it.sq + kTile - 1) / kTile;
+    it.t0 = p.causal ? min(tiles, max(0, it.row0 - off) / kTile) : 0;
+    it.nt = tiles - it.t0;
+    it.n = it.nt * G;
+  } else {
+    const int seen = p.causal ? min(it.skv, it.row0 + kTile + off) : it.skv;
+    it.t0 = 0;
+    it.nt = it.n = seen > 0 ? (seen + kTile - 1) / kTile : 0;
+  }
+  return it;
+}
+
+// ---------------------------------------------------------------- shared pieces
+// Items pass from the loader to the other roles through two records.
+struct ItemRing {
+  uint32_t full, empty;  // two barriers each
+  Item* rec;
+};
+__device__ __forceinline__ bool ring_put(const ItemRing& r, int i, const Item& it, const KernelCtl& ctl, const Abort& ab) {
+  if (i >= 2 && !mbar_wait(r.empty + 8 * (i & 1), ((i >> 1) - 1) & 1, ctl, ab)) return false;
+  r.rec[i & 1] = it;
+  mbar_arrive(r.full + 8 * (i & 1));
+  return true;
+}
+// The i-th item, read by a whole warp.
+__device__ __forceinline__ bool ring_get(const ItemRing& r, int i, Item& it, const KernelCtl& ctl, const Abort& ab) {
+  if (!mbar_wait_warp(r.full + 8 * (i & 1), (i >> 1) & 1, ctl, ab)) return false;
+  it = r.rec[i & 1];
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) mbar_arrive(r.empty + 8 * (i & 1));
+  return true;
+}
+constexpr int kItemReaders = 9;  // the MMA warp and the elementwise warps
+
+template <int D, bool VARLEN>
+__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, int plane, int row, uint32_t bar) {
+  using C = BwdCfg<D>;
+#pragma unroll
+  for (int x = 0; x < C::NBOX; ++x)
+    tma_load_3d(dst + x * C::BOX_BYTES, map, x * 64, VARLEN ? plane : row, VARLEN ? row : plane, bar);
+}
+
+// Rows [n, 128) of a tile become zeros (ragged batches: they are the next sequence's, and a NaN
+// or an infinity there times a zero probability would reach this sequence's gradients).  By a
+// whole warp, after the tile has arrived and before an MMA reads it.
+template <int D>
+__device__ __forceinline__ void zero_rows(uint32_t tile, int n) {
+  using C = BwdCfg<D>;
+  for (int x = 0; x < C::NBOX; ++x)
+    for (uint32_t o = n * 128 + (threadIdx.x & 31) * 16; o < C::BOX_BYTES; o += 512)
+      st_shared_v4(tile + x * C::BOX_BYTES + o, 0, 0, 0, 0);
+}
+
+// The MMAs of one pair of tiles.  D[128 x 128] = A B^T, both K-major in shared memory.
+template <int D>
+__device__ __forceinline__ void issue_scores(uint32_t d_tmem, uint32_t a, uint32_t b) {
+  using C = BwdCfg<D>;
+  constexpr uint32_t idesc = idesc_bf16(kTile, kTile, 0, 0);
+  const uint64_t da = sdesc_sw128(a, 16, 1024), db = sdesc_sw128(b, 16, 1024);
+#pragma unroll
+  for (int x = 0; x < C::NBOX; ++x)
+    mma_ss_k64_el(d_tmem, da + x * (C::BOX_BYTES >> 4), db + x * (C::BOX_BYTES >> 4), idesc, x > 0);
+}
+// D[128 x D] += A B over 64 of the tile's rows: A in TMEM (packed bf16), B's rows 64 h .. 64 h + 63.
+template <int D>
+__device__ __forceinline__ void issue_grad_half(uint32_t d_tmem, uint32_t a_tmem, uint32_t b, int h, bool acc) {
+  using C = BwdCfg<D>;
+  constexpr uint32_t idesc = idesc_bf16(kTile, D, 0, 1);
+  mma_ts_k64_el(d_tmem, a_tmem, sdesc_sw128(b, C::BOX_BYTES, 1024) + h * 64 * (128 >> 4), idesc, acc ? 1u : 0u);
+}
+
+// 64 TMEM columns of this thread's lane.
+__device__ __forceinline__ void ld64(uint32_t tm, uint32_t* r) {
+  tmem_ld32(tm, r);
+  tmem_ld32(tm + 32, r + 32);
+  tmem_wait_ld();
+  reg_fence32(r);
+  reg_fence32(r + 32);
+}
+
+// A gradient row's COLS values from TMEM, scaled, as bf16 to global memory.
+template <int COLS>
+__device__ __forceinline__ void store_row(uint32_t tm, float scale, __nv_bfloat16* dst, bool store) {
+  const uint64_t s2 = f2(scale, scale);
+#pragma unroll 1
+  for (int c = 0; c < COLS; c += 32) {
+    uint32_t r[32];
+    tmem_ld32(tm + c, r);
+    tmem_wait_ld();
+    reg_fence32(r);
+    if (store) {
+      uint4* d = reinterpret_cast<uint4*>(dst + c);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint64_t x = mul2(f2(__uint_as_float(r[8 * i + 2 * j]), __uint_as_float(r[8 * i + 2 * j + 1])), s2);
+          w[j] = pack_bf16x2(f2lo(x), f2hi(x));
+        }
+        d[i] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+  }
+}
+template <int COLS>
+__device__ __forceinline__ void store_zeros(__nv_bfloat16* dst) {
+#pragma unroll
+  for (int c = 0; c < COLS; c += 8) *reinterpret_cast<uint4*>(dst + c) = make_uint4(0, 0, 0, 0);
+}
+
+struct Shared {
+  uint32_t base, bars, tmem;
+  ItemRing items;
+  Abort ab, drain_ab;
+};
+
+// ---------------------------------------------------------------- kv items: dK and dV
+// Per step n (one query tile of one head):
+//   MMA warp     S^T = K Q^T | dP^T = V dO^T, and once the elementwise warps have written P^T and
+//                dS^T (bf16, over S^T and dP^T):  dV += P^T dO,  dK += dS^T Q.  Issue order
+//                dV_n, S_n+1 | dK_n, dP_n+1: the tensor pipe has the products of one step's P
+//                while dS is computed, and those of dS while the next P is.
+//   elementwise  a thread has key row = TMEM lane, 64 of the tile's 128 queries (warps 0-3 the
+//                first half, 4-7 the second).
+template <int D, bool VARLEN>
+__device__ __forceinline__ void kv_items(const BwdParams& p, const Shared& sh, const CUtensorMap* tm_q,
+                                         const CUtensorMap* tm_do, const CUtensorMap* tm_k, const CUtensorMap* tm_v) {
+  using C = BwdCfg<D>;
+  constexpr int NQ = C::NQ;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const KernelCtl& ctl = p.ctl;
+  const Abort& ab = sh.ab;
+  const uint32_t bar_k = sh.bars, bar_v = bar_k + 8, bar_ke = bar_v + 8, bar_ve = bar_ke + 8;
+  const uint32_t bar_q = bar_ve + 8, bar_qe = bar_q + 8 * NQ, bar_do = bar_qe + 8 * NQ, bar_doe = bar_do + 8 * NQ;
+  const uint32_t bar_s = bar_doe + 8 * NQ, bar_dp = bar_s + 8, bar_p = bar_dp + 8, bar_ds = bar_p + 16;
+  const uint32_t bar_acc = bar_ds + 16, bar_acce = bar_acc + 8, bar_drain = bar_acce + 8;
+  const uint32_t sb = sh.base;
+
+  if (warp == 8) {
+    if (lane == 0) {
+      int n = 0, filled = 0;  // steps and items with steps so far
+      int in_flight_q = 0, in_flight_do = 0;
+      bool ok = true;
+      Cursor cur{-1, 0, 0};
+      for (int i = 0; ok; ++i) {
+        const Item it = make_item<true, VARLEN>(p, atomicAdd(p.counters, 1u), cur);
+        if (!(ok = ring_put(sh.items, i, it, ctl, ab)) || it.n < 0) break;
+        for (int j = 0; j < it.n; ++j, ++n) {
+          const int slot = n % NQ, ph = n / NQ;
+          const int g = j / it.nt, t = it.t0 + j - g * it.nt;
+          if (j == 0) {
+            if (filled > 0 && !(ok = mbar_wait(bar_ke, (filled - 1) & 1, ctl, ab))) break;
+            mbar_expect_tx(bar_k, C::TILE_BYTES);
+            load_tile<D, VARLEN>(sb + C::K_OFF, tm_k, it.plane, it.kb + it.row0, bar_k);
+          }
+          if (ph > 0 && !(ok = mbar_wait(bar_qe + 8 * slot, (ph - 1) & 1, ctl, ab))) break;
+          if (ctl.inject == 4 && n == 1) break;  // test hook: never load this tile
+          mbar_expect_tx(bar_q + 8 * slot, C::TILE_BYTES + kStat * 4);
+          load_tile<D, VARLEN>(sb + C::QR_OFF + slot * C::TILE_BYTES, tm_q, it.other + g, it.qb + t * kTile, bar_q + 8 * slot);
+          bulk_g2s(sb + C::ST_OFF + slot * (kStat * 4),
+                   p.stats + (static_cast<size_t>(it.other + g) * p.stat_tiles + it.stat0 + t) * kStat, kStat * 4,
+                   bar_q + 8 * slot);
+          in_flight_q = n + 1;
+          if (j == 0) {
+            if (filled > 0 && !(ok = mbar_wait(bar_ve, (filled - 1) & 1, ctl, ab))) break;
+            mbar_expect_tx(bar_v, C::TILE_BYTES);
+            load_tile<D, VARLEN>(sb + C::V_OFF, tm_v, it.plane, it.kb + it.row0, bar_v);
+            ++filled;
+          }
+          if (ph > 0 && !(ok = mbar_wait(bar_doe + 8 * slot, (ph - 1) & 1, ctl, ab))) break;
+          mbar_expect_tx(bar_do + 8 * slot, C::TILE_BYTES);
+          load_tile<D, VARLEN>(sb + C::DOR_OFF + slot * C::TILE_BYTES, tm_do, it.other + g, it.qb + t * kTile, bar_do + 8 * slot);
+          in_flight_do = n + 1;
+        }
+        if (ctl.inject == 4 && n == 1) break;
+      }
+      // copies still in flight must land before the shared memory is used for anything else
+      if (filled > 0) {
+        mbar_wait(bar_k, (filled - 1) & 1, ctl, sh.drain_ab);
+        mbar_wait(bar_v, (filled - 1) & 1, ctl, sh.drain_ab);
+      }
+      for (int m = max(0, in_flight_q - NQ); m < in_flight_q; ++m) mbar_wait(bar_q + 8 * (m % NQ), (m / NQ) & 1, ctl, sh.drain_ab);
+      for (int m = max(0, in_flight_do - NQ); m < in_flight_do; ++m)
+        mbar_wait(bar_do + 8 * (m % NQ), (m / NQ) & 1, ctl, sh.drain_ab);
+    }
+    __syncwarp();
+  } else if (warp == 9) {
+    const uint32_t tm = sh.tmem;
+    int n = 0, filled = 0;
+    bool ok = true;
+    Item it;
+    for (int i = 0; ok; ++i) {
+      if (!(ok = ring_get(sh.items, i, it, ctl, ab)) || it.n < 0) break;
+      if (it.n == 0) continue;
+      // rows of the step's query tile that belong to the sequence
+      auto rows_of = [&](int j) { return it.sq - (it.t0 + j % it.nt) * kTile; };
+      auto scores = [&](int j) -> bool {
+        const int slot = (n + j) % NQ;
+        const uint32_t q = sb + C::QR_OFF + slot * C::TILE_BYTES;
+        if (!mbar_wait_warp(bar_q + 8 * slot, ((n + j) / NQ) & 1, ctl, ab)) return false;
+        if (VARLEN && rows_of(j) < kTile) {
+          zero_rows<D>(q, rows_of(j));
+          fence_proxy_async_smem();
+          __syncwarp();
+        }
+        tc_fence_after();
+        issue_scores<D>(tm + C::S_COL, sb + C::K_OFF, q);
+        tc_commit_el(bar_s);
+        if (j + 1 == it.n) tc_commit_el(bar_ke);
+        return true;
+      };
+      auto dprobs = [&](int j) -> bool {
+        const int slot = (n + j) % NQ;
+        const uint32_t d = sb + C::DOR_OFF + slot * C::TILE_BYTES;
+        if (!mbar_wait_warp(bar_do + 8 * slot, ((n + j) / NQ) & 1, ctl, ab)) return false;
+        if (VARLEN && rows_of(j) < kTile) {
+          zero_rows<D>(d, rows_of(j));
+          fence_proxy_async_smem();
+          __syncwarp();
+        }
+        tc_fence_after();
+        issue_scores<D>(tm + C::DP_COL, sb + C::V_OFF, d);
+        tc_commit_el(bar_dp);
+        if (j + 1 == it.n) tc_commit_el(bar_ve);
+        return true;
+      };
+      if (!(ok = mbar_wait_warp(bar_k, filled & 1, ctl, ab) && scores(0))) break;
+      if (!(ok = mbar_wait_warp(bar_v, filled & 1, ctl, ab) && dprobs(0))) break;
+      for (int j = 0; j < it.n; ++j) {
+        const int m = n + j, slot = m % NQ;
+        const uint32_t q = sb + C::QR_OFF + slot * C::TILE_BYTES, d = sb + C::DOR_OFF + slot * C::TILE_BYTES;
+        // the gradients of the item before must have been read out
+        if (j == 0 && filled > 0 && !(ok = mbar_wait_warp(bar_acce, (filled - 1) & 1, ctl, ab))) break;
+        for (int h = 0; ok && h < 2; ++h) {
+          if (!(ok = mbar_wait_warp(bar_p + 8 * h, m & 1, ctl, ab))) break;
+          tc_fence_after();
+          issue_grad_half<D>(tm + C::DV_COL, tm + C::S_COL + 64 * h, d, h, j > 0 || h > 0);
+        }
+        if (!ok) break;
+        tc_commit_el(bar_doe + 8 * slot);
+        if (j + 1 < it.n && !(ok = scores(j + 1))) break;
+        for (int h = 0; ok && h < 2; ++h) {
+          if (!(ok = mbar_wait_warp(bar_ds + 8 * h, m & 1, ctl, ab))) break;
+          tc_fence_after();
+          issue_grad_half<D>(tm + C::DK_COL, tm + C::DP_COL + 64 * h, q, h, j > 0 || h > 0);
+        }
+        if (!ok) break;
+        tc_commit_el(bar_qe + 8 * slot);
+        if (j + 1 < it.n && !(ok = dprobs(j + 1))) break;
+      }
+      if (!ok) break;
+      tc_commit_el(bar_acc);
+      n += it.n;
+      ++filled;
+    }
+    // every MMA issued above is done before TMEM or shared memory is used for anything else
+    tc_commit_el(bar_drain);
+    mbar_wait_warp(bar_drain, 0, ctl, sh.drain_ab);
+  } else {
+    const int half = warp >> 2, r = (warp & 3) * 32 + lane;
+    const uint32_t tm = sh.tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+    const uint32_t s_tm = tm + C::S_COL + 64 * half, dp_tm = tm + C::DP_COL + 64 * half;
+    const uint64_t c2 = f2(p.c, p.c);
+    int n = 0, filled = 0;
+    bool ok = true;
+    Item it;
+    for (int i = 0; ok; ++i) {
+      if (!(ok = ring_get(sh.items, i, it, ctl, ab)) || it.n < 0) break;
+      const int off = it.skv - it.sq, key = it.row0 + r;
+      for (int j = 0; j < it.n; ++j, ++n) {
+        const int slot = n % NQ;
+        const uint32_t st = sb + C::ST_OFF + slot * (kStat * 4) + 256 * half;
+        const int q0 = (it.t0 + j % it.nt) * kTile + 64 * half;
+        // (the statistics came with the query tile)
+        if (!(ok = mbar_wait_warp(bar_q + 8 * slot, (n / NQ) & 1, ctl, ab))) break;
+        if (!(ok = mbar_wait_warp(bar_s, n & 1, ctl, ab))) break;
+        tc_fence_after();
+        uint32_t s[64];
+        ld64(s_tm, s);
+        if (p.causal && q0 + off < it.row0 + kTile - 1) {
+          // queries from key - off on see this key
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            const int hid = key - off - q0 - 32 * g;  // hidden queries of this word
+            const uint32_t hidden = hid >= 32 ? 0xffffffffu : hid <= 0 ? 0u : (1u << hid) - 1u;
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (hidden & (1u << e)) s[32 * g + e] = __float_as_uint(-INFINITY);
+          }
+        }
+        uint32_t pk[32];
+#pragma unroll
+        for (int e = 0; e < 64; e += 4) {
+          const uint4 l4 = ld_shared_v4(st + 4 * e);
+          const uint64_t x0 = fma2(f2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), c2,
+                                   f2(__uint_as_float(l4.x), __uint_as_float(l4.y)));
+          const uint64_t x1 = fma2(f2(__uint_as_float(s[e + 2]), __uint_as_float(s[e + 3])), c2,
+                                   f2(__uint_as_float(l4.z), __uint_as_float(l4.w)));
+          const float p0 = ex2(f2lo(x0)), p1 = ex2(f2hi(x0)), p2 = ex2(f2lo(x1)), p3 = ex2(f2hi(x1));
+          s[e] = __float_as_uint(p0);
+          s[e + 1] = __float_as_uint(p1);
+          s[e + 2] = __float_as_uint(p2);
+          s[e + 3] = __float_as_uint(p3);
+          pk[e / 2] = pack_bf16x2(p0, p1);
+          pk[e / 2 + 1] = pack_bf16x2(p2, p3);
+        }
+        tmem_st32(s_tm, pk);
+        tmem_wait_st();
+        tc_fence_before();
+        mbar_arrive(bar_p + 8 * half);
+
+        if (!(ok = mbar_wait_warp(bar_dp, n & 1, ctl, ab))) break;
+        tc_fence_after();
+        uint32_t d[64];
+        ld64(dp_tm, d);
+#pragma unroll
+        for (int e = 0; e < 64; e += 4) {
+          const uint4 l4 = ld_shared_v4(st + kTile * 4 + 4 * e);
+          const uint64_t x0 = mul2(add2(f2(__uint_as_float(d[e]), __uint_as_float(d[e + 1])),
+                                        f2(__uint_as_float(l4.x), __uint_as_float(l4.y))),
+                                   f2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])));
+          const uint64_t x1 = mul2(add2(f2(__uint_as_float(d[e + 2]), __uint_as_float(d[e + 3])),
+                                        f2(__uint_as_float(l4.z), __uint_as_float(l4.w))),
+                                   f2(__uint_as_float(s[e + 2]), __uint_as_float(s[e + 3])));
+          pk[e / 2] = pack_bf16x2(f2lo(x0), f2hi(x0));
+          pk[e / 2 + 1] = pack_bf16x2(f2lo(x1), f2hi(x1));
+        }
+        tmem_st32(dp_tm, pk);
+        tmem_wait_st();
+        tc_fence_before();
+        mbar_arrive(bar_ds + 8 * half);
+      }
+      if (!ok) break;
+      // warps 0-3 store dV, warps 4-7 dK
+      const bool store = key < it.skv;
+      const long long row = VARLEN ? static_cast<long long>(it.kb + key) * p.Hkv + it.plane
+                                   : static_cast<long long>(it.plane) * p.Skv + key;
+      __nv_bfloat16* dst = (half ? p.dk : p.dv) + (store ? row : 0) * D;
+      if (it.n == 0) {
+        if (store) store_zeros<D>(dst);
+        continue;
+      }
+      if (!(ok = mbar_wait_warp(bar_acc, filled & 1, ctl, ab))) break;
+      tc_fence_after();
+      store_row<D>(tm + (half ? C::DK_COL : C::DV_COL), half ? p.scale : 1.f, dst, store);
+      tc_fence_before();
+      mbar_arrive(bar_acce);
+      ++filled;
+    }
+  }
+}
+
+// ---------------------------------------------------------------- query items: dQ
+// Per step n (one kv tile):  S = Q K^T,  dP = dO V^T,  dQ += dS K.  P never leaves the registers;
+// dS has two TMEM buffers of its own, so S and dP of the next step are issued as soon as the
+// elementwise warps have loaded this step's.  They may therefore finish the next dS before the MMA
+// warp has looked at this one: each buffer has barriers of its own (those of one buffer are two
+// steps apart, and S of step n + 2 is issued behind dQ of step n).
+template <int D, bool VARLEN>
+__device__ __forceinline__ void q_items(const BwdParams& p, const Shared& sh, const CUtensorMap* tm_q,
+                                        const CUtensorMap* tm_do, const CUtensorMap* tm_k, const CUtensorMap* tm_v) {
+  using C = BwdCfg<D>;
+  constexpr int NK = C::NK, NV = C::NV;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const KernelCtl& ctl = p.ctl;
+  const Abort& ab = sh.ab;
+  const uint32_t bar_q = sh.bars, bar_do = bar_q + 8, bar_qe = bar_do + 8, bar_doe = bar_qe + 8;
+  const uint32_t bar_k = bar_doe + 8, bar_ke = bar_k + 8 * NK, bar_v = bar_ke + 8 * NK, bar_ve = bar_v + 8 * NV;
+  const uint32_t bar_s = bar_ve + 8 * NV, bar_dp = bar_s + 8, bar_sf = bar_dp + 8, bar_dpf = bar_sf + 8;
+  const uint32_t bar_ds = bar_dpf + 8, bar_acc = bar_ds + 32, bar_acce = bar_acc + 8, bar_drain = bar_acce + 8;
+  const uint32_t sb = sh.base;
+
+  if (warp == 8) {
+    if (lane == 0) {
+      int n = 0, filled = 0;
+      int in_flight_k = 0, in_flight_v = 0;
+      bool ok = true;
+      Cursor cur{-1, 0, 0};
+      for (int i = 0; ok; ++i) {
+        const Item it = make_item<false, VARLEN>(p, atomicAdd(p.counters + 1, 1u), cur);
+        if (!(ok = ring_put(sh.items, i, it, ctl, ab)) || it.n < 0) break;
+        for (int j = 0; j < it.n; ++j, ++n) {
+          if (j == 0) {
+            if (filled > 0 && !(ok = mbar_wait(bar_qe, (filled - 1) & 1, ctl, ab))) break;
+            mbar_expect_tx(bar_q, C::TILE_BYTES);
+            load_tile<D, VARLEN>(sb + C::Q_OFF, tm_q, it.plane, it.qb + it.row0, bar_q);
+          }
+          const int ks = n % NK, kp = n / NK, vs = n % NV, vp = n / NV;
+          if (kp > 0 && !(ok = mbar_wait(bar_ke + 8 * ks, (kp - 1) & 1, ctl, ab))) break;
+          mbar_expect_tx(bar_k + 8 * ks, C::TILE_BYTES);
+          load_tile<D, VARLEN>(sb + C::KR_OFF + ks * C::TILE_BYTES, tm_k, it.other, it.kb + j * kTile, bar_k + 8 * ks);
+          in_flight_k = n + 1;
+          if (j == 0) {
+            if (filled > 0 && !(ok = mbar_wait(bar_doe, (filled - 1) & 1, ctl, ab))) break;
+            mbar_expect_tx(bar_do, C::TILE_BYTES);
+            load_tile<D, VARLEN>(sb + C::DO_OFF, tm_do, it.plane, it.qb + it.row0, bar_do);
+            ++filled;
+          }
+          if (vp > 0 && !(ok = mbar_wait(bar_ve + 8 * vs, (vp - 1) & 1, ctl, ab))) break;
+          mbar_expect_tx(bar_v + 8 * vs, C::TILE_BYTES);
+          load_tile<D, VARLEN>(sb + C::VR_OFF + vs * C::TILE_BYTES, tm_v, it.other, it.kb + j * kTile, bar_v + 8 * vs);
+          in_flight_v = n + 1;
+        }
+      }
+      if (filled > 0) {
+        mbar_wait(bar_q, (filled - 1) & 1, ctl, sh.drain_ab);
+        mbar_wait(bar_do, (filled - 1) & 1, ctl, sh.drain_ab);
+      }
+      for (int m = max(0, in_flight_k - NK); m < in_flight_k; ++m) mbar_wait(bar_k + 8 * (m % NK), (m / NK) & 1, ctl, sh.drain_ab);
+      for (int m = max(0, in_flight_v - NV); m < in_flight_v; ++m) mbar_wait(bar_v + 8 * (m % NV), (m / NV) & 1, ctl, sh.drain_ab);
+    }
+    __syncwarp();
+  } else if (warp == 9) {
+    const uint32_t tm = sh.tmem;
+    int n = 0, filled = 0;
+    bool ok = true;
+    Item it;
+    for (int i = 0; ok; ++i) {
+      if (!(ok = ring_get(sh.items, i, it, ctl, ab)) || it.n < 0) break;
+      if (it.n == 0) continue;
+      auto scores = [&](int j) -> bool {
+        const int m = n + j, slot = m % NK;
+        const uint32_t k = sb + C::KR_OFF + slot * C::TILE_BYTES;
+        if (m > 0 && !mbar_wait_warp(bar_sf, (m - 1) & 1, ctl, ab)) return false;  // S is in registers
+        if (!mbar_wait_warp(bar_k + 8 * slot, (m / NK) & 1, ctl, ab)) return false;
+        if (VARLEN && it.skv - j * kTile < kTile) {
+          zero_rows<D>(k, it.skv - j * kTile);
+          fence_proxy_async_smem();
+          __syncwarp();
+        }
+        tc_fence_after();
+        issue_scores<D>(tm + C::S_COL, sb + C::Q_OFF, k);
+        tc_commit_el(bar_s);
+        if (j + 1 == it.n) tc_commit_el(bar_qe);
+        return true;
+      };
+      auto dprobs = [&](int j) -> bool {
+        const int m = n + j, slot = m % NV;
+        const uint32_t v = sb + C::VR_OFF + slot * C::TILE_BYTES;
+        if (m > 0 && !mbar_wait_warp(bar_dpf, (m - 1) & 1, ctl, ab)) return false;
+        if (!mbar_wait_warp(bar_v + 8 * slot, (m / NV) & 1, ctl, ab)) return false;
+        if (VARLEN && it.skv - j * kTile < kTile) {
+          zero_rows<D>(v, it.skv - j * kTile);
+          fence_proxy_async_smem();
+          __syncwarp();
+        }
+        tc_fence_after();
+        issue_scores<D>(tm + C::DP_COL, sb + C::DO_OFF, v);
+        tc_commit_el(bar_dp);
+        tc_commit_el(bar_ve + 8 * slot);
+        if (j + 1 == it.n) tc_commit_el(bar_doe);
+        return true;
+      };
+      if (!(ok = mbar_wait_warp(bar_q, filled & 1, ctl, ab) && scores(0))) break;
+      if (!(ok = mbar_wait_warp(bar_do, filled & 1, ctl, ab) && dprobs(0))) break;
+      for (int j = 0; j < it.n; ++j) {
+        const int m = n + j, slot = m % NK;
+        if (j + 1 < it.n && !(ok = scores(j + 1) && dprobs(j + 1))) break;
+        if (j == 0 && filled > 0 && !(ok = mbar_wait_warp(bar_acce, (filled - 1) & 1, ctl, ab))) break;
+        for (int h = 0; ok && h < 2; ++h) {
+          if (!(ok = mbar_wait_warp(bar_ds + 16 * (m & 1) + 8 * h, (m >> 1) & 1, ctl, ab))) break;
+          tc_fence_after();
+          issue_grad_half<D>(tm + C::DQ_COL, tm + C::DS_COL + 64 * (m & 1) + 32 * h, sb + C::KR_OFF + slot * C::TILE_BYTES, h,
+                             j > 0 || h > 0);
+        }
+        if (!ok) break;
+        tc_commit_el(bar_ke + 8 * slot);
+      }
+      if (!ok) break;
+      tc_commit_el(bar_acc);
+      n += it.n;
+      ++filled;
+    }
+    tc_commit_el(bar_drain);
+    mbar_wait_warp(bar_drain, 0, ctl, sh.drain_ab);
+  } else {
+    const int half = warp >> 2, r = (warp & 3) * 32 + lane;
+    const uint32_t tm = sh.tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+    const uint64_t c2 = f2(p.c, p.c);
+    int n = 0, filled = 0;
+    bool ok = true;
+    Item it;
+    for (int i = 0; ok; ++i) {
+      if (!(ok = ring_get(sh.items, i, it, ctl, ab)) || it.n < 0) break;
+      const int q = it.row0 + r;
+      const float* st = p.stats + (static_cast<size_t>(it.plane) * p.stat_tiles + it.stat0 + it.row0 / kTile) * kStat + r;
+      const float nl = __ldg(st), nd = __ldg(st + kTile);
+      const uint64_t nl2 = f2(nl, nl), nd2 = f2(nd, nd);
+      const int limit = p.causal ? min(it.skv, q + it.skv - it.sq + 1) : it.skv;  // keys [0, limit) are seen
+      for (int j = 0; j < it.n; ++j, ++n) {
+        const int k0 = j * kTile + 64 * half;
+        if (!(ok = mbar_wait_warp(bar_s, n & 1, ctl, ab))) break;
+        tc_fence_after();
+        uint32_t s[64];
+        ld64(tm + C::S_COL + 64 * half, s);
+        tc_fence_before();
+        mbar_arrive(bar_sf);
+        if (k0 + 64 > limit) {
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            const int vis = limit - k0 - 32 * g;
+            const uint32_t visible = vis >= 32 ? 0xffffffffu : vis <= 0 ? 0u : (1u << vis) - 1u;
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (!(visible & (1u << e))) s[32 * g + e] = __float_as_uint(-INFINITY);
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 64; e += 2) {
+          const uint64_t x = fma2(f2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), c2, nl2);
+          s[e] = __float_as_uint(ex2(f2lo(x)));
+          s[e + 1] = __float_as_uint(ex2(f2hi(x)));
+        }
+        if (!(ok = mbar_wait_warp(bar_dp, n & 1, ctl, ab))) break;
+        tc_fence_after();
+        uint32_t d[64], pk[32];
+        ld64(tm + C::DP_COL + 64 * half, d);
+        tc_fence_before();
+        mbar_arrive(bar_dpf);
+#pragma unroll
+        for (int e = 0; e < 64; e += 2) {
+          const uint64_t x = mul2(add2(f2(__uint_as_float(d[e]), __uint_as_float(d[e + 1])), nd2),
+                                  f2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])));
+          pk[e / 2] = pack_bf16x2(f2lo(x), f2hi(x));
+        }
+        // (dQ of two steps before, which read this buffer, was issued before this step's S)
+        tmem_st32(tm + C::DS_COL + 64 * (n & 1) + 32 * half, pk);
+        tmem_wait_st();
+        tc_fence_before();
+        mbar_arrive(bar_ds + 16 * (n & 1) + 8 * half);
+      }
+      if (!ok) break;
+      const bool store = q < it.sq;
+      const long long row = VARLEN ? static_cast<long long>(it.qb + q) * p.Hq + it.plane
+                                   : static_cast<long long>(it.plane) * p.Sq + q;
+      __nv_bfloat16* dst = p.dq + (store ? row : 0) * D + half * (D / 2);
+      if (it.n == 0) {
+        if (store) store_zeros<D / 2>(dst);
+        continue;
+      }
+      if (!(ok = mbar_wait_warp(bar_acc, filled & 1, ctl, ab))) break;
+      tc_fence_after();
+      store_row<D / 2>(tm + C::DQ_COL + half * (D / 2), p.scale, dst, store);
+      tc_fence_before();
+      mbar_arrive(bar_acce);
+      ++filled;
+    }
+  }
+}
+
+template <int D, bool VARLEN>
+__global__ void __launch_bounds__(kThreads, 1)
+    attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_do,
+                    const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const BwdParams p) {
+  using C = BwdCfg<D>;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw_base = smem_u32(smem_raw);
+  const uint32_t sbase = (raw_base + 1023u) & ~1023u;  // 128B-swizzled tiles
+  uint8_t* smem = smem_raw + (sbase - raw_base);
+  const int warp = threadIdx.x >> 5;
+  uint32_t* tmem_ptr = reinterpret_cast<uint32_t*>(smem + C::TMEM_PTR_OFF);
+  volatile int* flags = reinterpret_cast<volatile int*>(smem + C::ABORT_OFF);
+
+  // Barriers of the kv items and of the query items: [0, kv) and [kv, ..), each with an item ring.
+  constexpr int kKvBars = 4 + 4 * C::NQ + 2 + 4 + 3, kQBars = 4 + 2 * C::NK + 2 * C::NV + 4 + 4 + 3;
+  static_assert(kKvBars + kQBars + 8 <= C::NBAR, "barrier space");
+  const uint32_t bars = sbase + C::BAR_OFF;
+  const uint32_t kv_bars = bars, q_bars = bars + 8 * kKvBars, ring_bars = q_bars + 8 * kQBars;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kKvBars + kQBars; ++i) mbar_init(bars + 8 * i, 1);
+    // elementwise threads arrive on these
+    const uint32_t bar_p = kv_bars + 8 * (4 + 4 * C::NQ + 2);
+    for (int i = 0; i < 4; ++i) mbar_init(bar_p + 8 * i, 128);  // p[2], ds[2]
+    mbar_init(bar_p + 8 * 5, 256);                              // acc_empty
+    const uint32_t bar_sf = q_bars + 8 * (4 + 2 * C::NK + 2 * C::NV + 2);
+    mbar_init(bar_sf, 256);
+    mbar_init(bar_sf + 8, 256);    // dP free
+    for (int i = 2; i < 6; ++i) mbar_init(bar_sf + 8 * i, 128);  // ds[2][2]
+    mbar_init(bar_sf + 56, 256);   // acc_empty
+    for (int i = 0; i < 2; ++i) {  // two rings: full[2], empty[2]
+      mbar_init(ring_bars + 32 * i, 1);
+      mbar_init(ring_bars + 32 * i + 8, 1);
+      mbar_init(ring_bars + 32 * i + 16, kItemReaders);
+      mbar_init(ring_bars + 32 * i + 24, kItemReaders);
+    }
+    flags[0] = 0;
+    flags[1] = 0;
+    fence_barrier_init();
+  }
+  if (warp == 9) tmem_alloc(smem_u32(tmem_ptr), 512);
+  if (threadIdx.x == 256) {
+    prefetch_tensormap(&tm_q);
+    prefetch_tensormap(&tm_do);
+    prefetch_tensormap(&tm_k);
+    prefetch_tensormap(&tm_v);
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  // the row statistics and the zeroed counters come from the kernel before this one
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;");
+  Item* rec = reinterpret_cast<Item*>(smem + C::ITEM_OFF);
+  static_assert(sizeof(Item) * 2 <= 128, "item records");
+  Shared sh{sbase, kv_bars, *tmem_ptr, {ring_bars, ring_bars + 16, rec}, {flags}, {flags + 1}};
+  kv_items<D, VARLEN>(p, sh, &tm_q, &tm_do, &tm_k, &tm_v);
+  // The rings' shared memory and TMEM change hands: every role is done, its copies have landed
+  // and its MMAs are complete.
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (flags[0] == 0 && flags[1] == 0) {
+    sh.bars = q_bars;
+    sh.items.full = ring_bars + 32;
+    sh.items.empty = ring_bars + 48;
+    q_items<D, VARLEN>(p, sh, &tm_q, &tm_do, &tm_k, &tm_v);
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 9) {
+    tc_fence_after();
+    tmem_dealloc(*tmem_ptr, 512);
+  }
+}
+
+// ---------------------------------------------------------------- row statistics
+// One block per tile of 128 query rows of a head: -LSE log2(e) and dLSE - dO . O for each row.
+// Rows past the end, and rows whose LSE is -inf (no key is seen), get -inf and P = 0.  Bound by
+// reading dO and O once; D / 8 lanes of 16 bytes take a row.
+template <int D, bool VARLEN>
+__global__ void __launch_bounds__(256)
+    attn_bwd_rows_kernel(const __nv_bfloat16* dout, const __nv_bfloat16* o, const float* lse, const float* dlse, float* stats,
+                         unsigned int* counters, int B, int H, int Sq, int stat_tiles, const int32_t* cu_q) {
+  constexpr int LPR = D / 8, RPP = 256 / LPR;  // lanes per row, rows per pass of the block
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;");
+  if (blockIdx.x == 0 && threadIdx.x < 2) counters[threadIdx.x] = 0;
+  const int plane = static_cast<int>(blockIdx.x) / stat_tiles, tile = static_cast<int>(blockIdx.x) % stat_tiles;
+  int row0 = tile * kTile, n = Sq, qb = 0;
+  if constexpr (VARLEN) {
+    int lo = 0, hi = B - 1;  // the last sequence that starts at this tile or before it
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (ragged_stat0(cu_q, mid) <= tile)
+        lo = mid;
+      else
+        hi = mid - 1;
+    }
+    qb = cu_q[lo];
+    n = cu_q[lo + 1] - qb;
+    row0 = (tile - ragged_stat0(cu_q, lo)) * kTile;
+    if (row0 < 0 || row0 >= n) return;  // a tile of no sequence
+  }
+  const int l = threadIdx.x % LPR;
+  float* st = stats + static_cast<size_t>(blockIdx.x) * kStat;
+#pragma unroll 4
+  for (int r = threadIdx.x / LPR; r < kTile; r += RPP) {
+    const int row = row0 + r;
+    const bool in = row < n;
+    const long long at = VARLEN ? static_cast<long long>(qb + row) * H + plane : static_cast<long long>(plane) * Sq + row;
+    float a = 0.f;
+    if (in) {
+      const uint4 x = *reinterpret_cast<const uint4*>(dout + at * D + 8 * l);
+      const uint4 y = *reinterpret_cast<const uint4*>(o + at * D + 8 * l);
+      const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a = fmaf(bf16hi(xw[i]), bf16hi(yw[i]), fmaf(bf16lo(xw[i]), bf16lo(yw[i]), a));
+    }
+#pragma unroll
+    for (int m = LPR / 2; m > 0; m >>= 1) a += __shfl_xor_sync(0xffffffffu, a, m);
+    if (l == 0) {
+      float nl = -INFINITY, nd = 0.f;
+      if (in) {
+        const long long i = VARLEN ? static_cast<long long>(plane) * Sq + qb + row : at;
+        const float s = lse[i];
+        nl = s == -INFINITY ? -INFINITY : -s * kLog2e;
+        nd = (dlse ? dlse[i] : 0.f) - a;
+      }
+      st[r] = nl;
+      st[kTile + r] = nd;
+    }
+  }
+}
+
+// ---------------------------------------------------------------- host side
+using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiledFn encode_fn() {
+  static EncodeTiledFn fn = nullptr;
+  static std::once_flag once;
+  std::call_once(once, [] {
+    void* ptr = nullptr;
+    cudaDriverEntryPointQueryResult qres;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &ptr, 12000, cudaEnableDefault, &qres) == cudaSuccess &&
+        qres == cudaDriverEntryPointSuccess)
+      fn = reinterpret_cast<EncodeTiledFn>(ptr);
+  });
+  return fn;
+}
+
+// 64-column x 128-row boxes of dense planes [planes, rows, D] (innermost first D, rows, planes), or
+// of packed tokens [rows, H, D] (D, H, rows).
+bool make_map(CUtensorMap* map, const void* base, int D, long long rows, long long planes, bool tokens) {
+  EncodeTiledFn enc = encode_fn();
+  if (!enc) return false;
+  const cuuint64_t row = static_cast<cuuint64_t>(D) * 2;
+  cuuint64_t dims[3] = {static_cast<cuuint64_t>(D), static_cast<cuuint64_t>(tokens ? planes : rows),
+                        static_cast<cuuint64_t>(tokens ? rows : planes)};
+  cuuint64_t strides[2] = {row, row * dims[1]};
+  cuuint32_t box[3] = {64, tokens ? 1u : static_cast<cuuint32_t>(kTile), tokens ? static_cast<cuuint32_t>(kTile) : 1u};
+  cuuint32_t estr[3] = {1, 1, 1};
+  return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <class Kernel, class... Args>
+cudaError_t launch(Kernel kernel, int grid, int threads, uint32_t smem, cudaStream_t stream, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(grid));
+  cfg.blockDim = dim3(static_cast<unsigned>(threads));
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+template <int D, bool VARLEN>
+cudaError_t launch_d(const BwdArgs& a, const KernelCtl& ctl, cudaStream_t stream) {
+  using C = BwdCfg<D>;
+  static PerDeviceOnce configured;
+  int dev = 0, sms = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e != cudaSuccess) return e;
+  const auto kernel = attn_bwd_kernel<D, VARLEN>;
+  if (!configured.run(dev, [&] {
+        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::BYTES) == cudaSuccess;
+      }))
+    return cudaErrorInvalidValue;
+  CUtensorMap mq, mdo, mk, mv;
+  const long long q_planes = VARLEN ? a.Hq : static_cast<long long>(a.B) * a.Hq;
+  const long long kv_planes = VARLEN ? a.Hkv : static_cast<long long>(a.B) * a.Hkv;
+  if (!make_map(&mq, a.q, D, a.Sq, q_planes, VARLEN) || !make_map(&mdo, a.dout, D, a.Sq, q_planes, VARLEN) ||
+      !make_map(&mk, a.k, D, a.Skv, kv_planes, VARLEN) || !make_map(&mv, a.v, D, a.Skv, kv_planes, VARLEN))
+    return cudaErrorInvalidValue;
+  const int stat_tiles = static_cast<int>(bwd_stat_tiles(a.B, a.Sq, VARLEN));
+  unsigned int* counters = static_cast<unsigned int*>(a.workspace);
+  float* stats = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + 256);
+  e = launch(attn_bwd_rows_kernel<D, VARLEN>, static_cast<int>(q_planes * stat_tiles), 256, 0, stream,
+             static_cast<const __nv_bfloat16*>(a.dout), static_cast<const __nv_bfloat16*>(a.o), a.lse, a.dlse, stats, counters,
+             a.B, a.Hq, a.Sq, stat_tiles, a.cu_q);
+  if (e != cudaSuccess) return e;
+  BwdParams p;
+  memset(&p, 0, sizeof(p));
+  p.dq = static_cast<__nv_bfloat16*>(a.dq);
+  p.dk = static_cast<__nv_bfloat16*>(a.dk);
+  p.dv = static_cast<__nv_bfloat16*>(a.dv);
+  p.stats = stats;
+  p.counters = counters;
+  p.B = a.B;
+  p.Hq = a.Hq;
+  p.Hkv = a.Hkv;
+  p.Sq = a.Sq;
+  p.Skv = a.Skv;
+  p.causal = a.causal;
+  p.c = a.scale * kLog2e;
+  p.scale = a.scale;
+  p.stat_tiles = stat_tiles;
+  p.cu_q = a.cu_q;
+  p.cu_k = a.cu_k;
+  p.ctl = ctl;
+  long long items;
+  if constexpr (VARLEN) {
+    p.total_q = a.Sq;
+    p.total_k = a.Skv;
+    items = static_cast<long long>(a.B) * (static_cast<long long>(a.Hkv) * ((a.max_k + kTile - 1) / kTile) +
+                                           static_cast<long long>(a.Hq) * ((a.max_q + kTile - 1) / kTile));
+  } else {
+    p.q_tiles = (a.Sq + kTile - 1) / kTile;
+    p.kv_tiles = (a.Skv + kTile - 1) / kTile;
+    p.q_items = static_cast<int>(q_planes * p.q_tiles);
+    p.kv_items = static_cast<int>(kv_planes * p.kv_tiles);
+    p.q_block = (sms + p.q_tiles - 1) / p.q_tiles;
+    p.kv_block = (sms + p.kv_tiles - 1) / p.kv_tiles;
+    items = static_cast<long long>(p.q_items) + p.kv_items;
+  }
+  const int grid = static_cast<int>(items > 0 && items < sms ? items : sms);
+  return launch(kernel, grid, kThreads, C::BYTES, stream, mq, mdo, mk, mv, p);
+}
+
+}  // namespace
+
+cudaError_t launch_attn_bwd(const BwdArgs& a, const KernelCtl& ctl, cudaStream_t stream) {
+  if (a.cu_q) return a.D == 128 ? launch_d<128, true>(a, ctl, stream) : launch_d<64, true>(a, ctl, stream);
+  return a.D == 128 ? launch_d<128, false>(a, ctl, stream) : launch_d<64, false>(a, ctl, stream);
+}
+
+}  // namespace loom

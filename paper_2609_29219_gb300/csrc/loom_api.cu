@@ -9,11 +9,13 @@
 #include <vector>
 
 #include "../../include/loom_attn.h"
+#include "bwd.h"
 #include "gemm.h"
 #include "gemm_model.h"
 #include "kernels.h"
 #include "model.h"
 #include "paged.h"
+#include "qkv.h"
 #include "varlen.h"
 
 namespace loom {
@@ -325,6 +327,208 @@ loom_status loom_attn_decode_paged(const void* q, const void* k_cache, const voi
   PagedKV pk{block_table, num_pages, page_size, max_pages, kv_layout};
   return launch_decode_paged(a, pk, ctl, static_cast<cudaStream_t>(stream)) == cudaSuccess ? LOOM_OK
                                                                                           : LOOM_ERR_CUDA;
+}
+
+namespace {
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+// Sizes of a backward call that have a workspace: items and row statistics within 32 bits.
+bool bwd_sizes_fit(int B, int Hq, int Hkv, long long Sq, long long Skv, bool ragged) {
+  const long long q_planes = ragged ? Hq : static_cast<long long>(B) * Hq;
+  const long long kv_planes = ragged ? Hkv : static_cast<long long>(B) * Hkv;
+  return q_planes <= 0x7fffffffLL && q_planes * bwd_stat_tiles(B, Sq, ragged) <= 0x3fffffffLL &&
+         kv_planes * (Skv / 128 + (ragged ? B : 1)) <= 0x3fffffffLL;
+}
+
+loom_status bwd_call(const BwdArgs& a, size_t workspace_bytes, void* stream) {
+  const bool ragged = a.cu_q != nullptr;
+  if (a.Hq % a.Hkv != 0) return LOOM_ERR_INVALID_ARG;
+  if (!std::isfinite(a.scale) || a.scale <= 0.f) return LOOM_ERR_INVALID_ARG;
+  if (a.D != 64 && a.D != 128) return LOOM_ERR_UNSUPPORTED;
+  if (!bwd_sizes_fit(a.B, a.Hq, a.Hkv, a.Sq, a.Skv, ragged)) return LOOM_ERR_UNSUPPORTED;
+  for (const void* p : {a.dout, a.q, a.k, a.v, a.o, static_cast<const void*>(a.dq), static_cast<const void*>(a.dk),
+                        static_cast<const void*>(a.dv)})
+    if (!aligned16(p)) return LOOM_ERR_MISALIGNED;
+  if (!aligned4(a.lse) || !aligned4(a.dlse) || !aligned4(a.cu_q) || !aligned4(a.cu_k)) return LOOM_ERR_MISALIGNED;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (a.Sq == 0 || a.Skv == 0) {  // ragged: no queries or no keys at all, so no gradient
+    const size_t row = static_cast<size_t>(a.D) * 2;
+    cudaError_t e = cudaSuccess;
+    if (a.Sq > 0) e = cudaMemsetAsync(a.dq, 0, row * a.Hq * a.Sq, s);
+    if (e == cudaSuccess && a.Skv > 0) e = cudaMemsetAsync(a.dk, 0, row * a.Hkv * a.Skv, s);
+    if (e == cudaSuccess && a.Skv > 0) e = cudaMemsetAsync(a.dv, 0, row * a.Hkv * a.Skv, s);
+    return e == cudaSuccess ? LOOM_OK : LOOM_ERR_CUDA;
+  }
+  if (!a.workspace || workspace_bytes < bwd_workspace_bytes(a.B, a.Hq, a.Sq, ragged)) return LOOM_ERR_WORKSPACE;
+  if (!aligned16(a.workspace)) return LOOM_ERR_MISALIGNED;
+  KernelCtl ctl;
+  if (!make_ctl(&ctl)) return LOOM_ERR_CUDA;
+  return launch_attn_bwd(a, ctl, s) == cudaSuccess ? LOOM_OK : LOOM_ERR_CUDA;
+}
+}  // namespace
+
+size_t loom_attn_bwd_workspace_bytes(int B, int Hq, int Hkv, int Sq, int Skv, int D) {
+  if (B <= 0 || Hq <= 0 || Hkv <= 0 || Sq <= 0 || Skv <= 0 || Hq % Hkv || (D != 64 && D != 128)) return 0;
+  return bwd_sizes_fit(B, Hq, Hkv, Sq, Skv, false) ? bwd_workspace_bytes(B, Hq, Sq, false) : 0;
+}
+
+size_t loom_attn_bwd_varlen_workspace_bytes(int B, int Hq, int Hkv, int total_q, int total_k, int D) {
+  if (B <= 0 || Hq <= 0 || Hkv <= 0 || total_q < 0 || total_k < 0 || Hq % Hkv || (D != 64 && D != 128)) return 0;
+  return bwd_sizes_fit(B, Hq, Hkv, total_q, total_k, true) ? bwd_workspace_bytes(B, Hq, total_q, true) : 0;
+}
+
+loom_status loom_attn_bwd(const void* dout, const void* q, const void* k, const void* v, const void* o, const float* lse,
+                          const float* dlse, void* dq, void* dk, void* dv, void* workspace, size_t workspace_bytes, int B,
+                          int Hq, int Hkv, int Sq, int Skv, int D, int causal, float scale, void* stream) {
+  if (!dout || !q || !k || !v || !o || !lse || !dq || !dk || !dv) return LOOM_ERR_INVALID_ARG;
+  if (B <= 0 || Hq <= 0 || Hkv <= 0 || Sq <= 0 || Skv <= 0 || D <= 0) return LOOM_ERR_INVALID_ARG;
+  if ((causal != 0 && causal != 1) || (causal && Sq > Skv)) return LOOM_ERR_INVALID_ARG;
+  const BwdArgs a{dout, q, k, v, o, lse, dlse, dq, dk, dv, workspace, B, Hq, Hkv, Sq, Skv, D, causal, scale,
+                  nullptr, nullptr, 0, 0};
+  return bwd_call(a, workspace_bytes, stream);
+}
+
+loom_status loom_attn_bwd_varlen(const void* dout, const void* q, const void* k, const void* v, const void* o,
+                                 const float* lse, const float* dlse, void* dq, void* dk, void* dv,
+                                 const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_k, void* workspace,
+                                 size_t workspace_bytes, int B, int Hq, int Hkv, int total_q, int total_k, int max_seqlen_q,
+                                 int max_seqlen_k, int D, int causal, float scale, void* stream) {
+  if (!cu_seqlens_q || !cu_seqlens_k) return LOOM_ERR_INVALID_ARG;
+  if (B <= 0 || Hq <= 0 || Hkv <= 0 || total_q < 0 || total_k < 0 || max_seqlen_q < 0 || max_seqlen_k < 0 || D <= 0)
+    return LOOM_ERR_INVALID_ARG;
+  if (total_q > 0 && (!dout || !q || !o || !lse || !dq)) return LOOM_ERR_INVALID_ARG;
+  if (total_k > 0 && (!k || !v || !dk || !dv)) return LOOM_ERR_INVALID_ARG;
+  if (causal != 0 && causal != 1) return LOOM_ERR_INVALID_ARG;
+  const BwdArgs a{dout, q, k, v, o, lse, dlse, dq, dk, dv, workspace, B, Hq, Hkv, total_q, total_k, D, causal, scale,
+                  cu_seqlens_q, cu_seqlens_k, max_seqlen_q, max_seqlen_k};
+  return bwd_call(a, workspace_bytes, stream);
+}
+
+namespace {
+// The arguments that the three norm-and-rotation entry points share, checked; *a is filled in.
+loom_status qkv_common(QkvArgs* a, const void* qkv, int64_t qkv_stride, const void* q_weight, const void* k_weight,
+                       int weight_type, const float* cos, const float* sin, int table_rows, int rotary_dim, int interleaved,
+                       const int32_t* positions, int T, int Hq, int Hkv, int D, float eps) {
+  if (T < 0 || Hq <= 0 || Hkv <= 0 || D <= 0 || table_rows <= 0) return LOOM_ERR_INVALID_ARG;
+  if (!q_weight || !k_weight || !cos || !sin || (T > 0 && !qkv)) return LOOM_ERR_INVALID_ARG;
+  if (weight_type != LOOM_BF16 && weight_type != LOOM_FP32) return LOOM_ERR_INVALID_ARG;
+  if (interleaved != 0 && interleaved != 1) return LOOM_ERR_INVALID_ARG;
+  if (!std::isfinite(eps) || eps <= 0.f) return LOOM_ERR_INVALID_ARG;
+  if (D != 64 && D != 128) return LOOM_ERR_UNSUPPORTED;
+  if (rotary_dim < 16 || rotary_dim > D || rotary_dim % 16) return LOOM_ERR_UNSUPPORTED;
+  const long long heads = static_cast<long long>(Hq) + 2ll * Hkv;
+  if (heads * D > 0x3fffffffLL) return LOOM_ERR_UNSUPPORTED;
+  if (qkv_stride < heads * D) return LOOM_ERR_INVALID_ARG;
+  if (qkv_stride % 8) return LOOM_ERR_MISALIGNED;
+  if (!aligned16(qkv) || !aligned16(q_weight) || !aligned16(k_weight) || !aligned16(cos) || !aligned16(sin))
+    return LOOM_ERR_MISALIGNED;
+  if (!aligned4(positions)) return LOOM_ERR_MISALIGNED;
+  a->qkv = qkv;
+  a->row_elems = qkv_stride;
+  a->q_weight = q_weight;
+  a->k_weight = k_weight;
+  a->weights_f32 = weight_type == LOOM_FP32;
+  a->cos = cos;
+  a->sin = sin;
+  a->positions = positions;
+  a->T = T;
+  a->Hq = Hq;
+  a->Hkv = Hkv;
+  a->D = D;
+  a->R = rotary_dim;
+  a->P = table_rows;
+  a->interleaved = interleaved;
+  a->eps = eps;
+  return LOOM_OK;
+}
+}  // namespace
+
+loom_status loom_qkv_norm_rope(const void* qkv, int64_t qkv_stride, const void* q_weight, const void* k_weight,
+                               int weight_type, const float* cos, const float* sin, int table_rows, int rotary_dim,
+                               int interleaved, const int32_t* positions, void* q, void* k, void* v, int T, int seq_len,
+                               int Hq, int Hkv, int D, float eps, void* stream) {
+  QkvArgs a{};
+  const loom_status st = qkv_common(&a, qkv, qkv_stride, q_weight, k_weight, weight_type, cos, sin, table_rows, rotary_dim,
+                                    interleaved, positions, T, Hq, Hkv, D, eps);
+  if (st != LOOM_OK) return st;
+  if (seq_len < 0 || (seq_len > 0 && T % seq_len) || (T > 0 && (!q || !k || !v))) return LOOM_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v)) return LOOM_ERR_MISALIGNED;
+  if (T == 0) return LOOM_OK;
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.q_at.S = a.kv_at.S = seq_len;
+  a.q_at.H = Hq;
+  a.kv_at.H = Hkv;
+  return launch_qkv_norm_rope(a, static_cast<cudaStream_t>(stream)) == cudaSuccess ? LOOM_OK : LOOM_ERR_CUDA;
+}
+
+loom_status loom_qkv_norm_rope_cache(const void* qkv, int64_t qkv_stride, const void* q_weight, const void* k_weight,
+                                     int weight_type, const float* cos, const float* sin, int table_rows, int rotary_dim,
+                                     int interleaved, const int32_t* positions, const int32_t* slots, void* q, void* k_cache,
+                                     void* v_cache, int num_pages, int page_size, int kv_layout, int T, int Hq, int Hkv,
+                                     int D, float eps, void* stream) {
+  QkvArgs a{};
+  const loom_status st = qkv_common(&a, qkv, qkv_stride, q_weight, k_weight, weight_type, cos, sin, table_rows, rotary_dim,
+                                    interleaved, positions, T, Hq, Hkv, D, eps);
+  if (st != LOOM_OK) return st;
+  if (num_pages <= 0 || page_size <= 0 || (kv_layout != kPagedNHD && kv_layout != kPagedHND)) return LOOM_ERR_INVALID_ARG;
+  if (!k_cache || !v_cache || (T > 0 && (!q || !positions || !slots))) return LOOM_ERR_INVALID_ARG;
+  if (static_cast<long long>(num_pages) * page_size > 0x7fffffffLL) return LOOM_ERR_UNSUPPORTED;
+  if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned4(slots)) return LOOM_ERR_MISALIGNED;
+  if (T == 0) return LOOM_OK;
+  a.q = q;
+  a.k = k_cache;
+  a.v = v_cache;
+  a.q_at.H = Hq;
+  a.kv_at.H = Hkv;
+  a.kv_at.slots = slots;
+  a.kv_at.page = page_size;
+  a.kv_at.n_slots = num_pages * page_size;
+  a.kv_at.page_elems = static_cast<long long>(page_size) * Hkv * D;
+  a.kv_at.row_elems = kv_layout == kPagedNHD ? static_cast<long long>(Hkv) * D : D;
+  a.kv_at.head_elems = kv_layout == kPagedNHD ? D : static_cast<long long>(page_size) * D;
+  return launch_qkv_norm_rope(a, static_cast<cudaStream_t>(stream)) == cudaSuccess ? LOOM_OK : LOOM_ERR_CUDA;
+}
+
+size_t loom_qkv_norm_rope_bwd_workspace_bytes(int D) { return D == 64 || D == 128 ? qkv_bwd_workspace_bytes(D) : 0; }
+
+loom_status loom_qkv_norm_rope_bwd(const void* dq, const void* dk, const void* dv, const void* qkv, int64_t qkv_stride,
+                                   const void* q_weight, const void* k_weight, int weight_type, const float* cos,
+                                   const float* sin, int table_rows, int rotary_dim, int interleaved,
+                                   const int32_t* positions, void* dqkv, int64_t dqkv_stride, float* dq_weight,
+                                   float* dk_weight, void* workspace, size_t workspace_bytes, int T, int seq_len, int Hq,
+                                   int Hkv, int D, float eps, void* stream) {
+  QkvArgs a{};
+  const loom_status st = qkv_common(&a, qkv, qkv_stride, q_weight, k_weight, weight_type, cos, sin, table_rows, rotary_dim,
+                                    interleaved, positions, T, Hq, Hkv, D, eps);
+  if (st != LOOM_OK) return st;
+  if (seq_len < 0 || (seq_len > 0 && T % seq_len) || (T > 0 && (!dq || !dk || !dv || !dqkv))) return LOOM_ERR_INVALID_ARG;
+  if (!dq_weight || !dk_weight) return LOOM_ERR_INVALID_ARG;
+  if (dqkv_stride < (static_cast<int64_t>(Hq) + 2ll * Hkv) * D) return LOOM_ERR_INVALID_ARG;
+  if (dqkv_stride % 8 || !aligned16(dq) || !aligned16(dk) || !aligned16(dv) || !aligned16(dqkv) || !aligned4(dq_weight) ||
+      !aligned4(dk_weight))
+    return LOOM_ERR_MISALIGNED;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (T == 0) {
+    const bool ok = cudaMemsetAsync(dq_weight, 0, D * sizeof(float), s) == cudaSuccess &&
+                    cudaMemsetAsync(dk_weight, 0, D * sizeof(float), s) == cudaSuccess;
+    return ok ? LOOM_OK : LOOM_ERR_CUDA;
+  }
+  if (!workspace || workspace_bytes < qkv_bwd_workspace_bytes(D)) return LOOM_ERR_WORKSPACE;
+  if (!aligned16(workspace)) return LOOM_ERR_MISALIGNED;
+  a.q = const_cast<void*>(dq);
+  a.k = const_cast<void*>(dk);
+  a.v = const_cast<void*>(dv);
+  a.q_at.S = a.kv_at.S = seq_len;
+  a.q_at.H = Hq;
+  a.kv_at.H = Hkv;
+  a.dqkv = dqkv;
+  a.drow_elems = dqkv_stride;
+  a.dq_weight = dq_weight;
+  a.dk_weight = dk_weight;
+  a.partial = static_cast<float*>(workspace);
+  return launch_qkv_norm_rope_bwd(a, s) == cudaSuccess ? LOOM_OK : LOOM_ERR_CUDA;
 }
 
 namespace {
