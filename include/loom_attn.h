@@ -229,7 +229,7 @@ loom_status loom_attn_decode_noalloc(const void* q, const void* k_cache, const v
  *   dq     [B, Hq, Sq, D]   bf16, written
  *   dk, dv [B, Hkv, Skv, D] bf16, written
  *   workspace  device scratch of at least loom_attn_bwd_workspace_bytes(...) bytes, whose contents
- *          on entry do not matter (row statistics, 8 bytes per query of a head in tiles of 128, and
+ *          on entry do not matter (row statistics, 8 bytes per query of a head in tiles of 128 rows, and
  *          256 bytes of counters); a workspace serves one call at a time.
  *   causal, scale as loom_attn_fwd.  The gradients must not overlap the inputs.
  * Scores, probabilities and sums are fp32; P and dS are rounded to bf16 before they meet dout, q

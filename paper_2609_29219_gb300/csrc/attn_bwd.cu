@@ -35,7 +35,9 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kTile = 128;   // queries and keys per tile
-constexpr int kThreads = 320;  // 8 elementwise warps, loader, MMA
+constexpr int kEltWarps = 8;  // elementwise warps: four for each half of a tile's columns
+constexpr int kLoader = kEltWarps, kMma0 = kEltWarps + 1, kMma1 = kEltWarps + 2;
+constexpr int kThreads = (kMma1 + 1) * 32;
 constexpr int kStat = 2 * kTile;  // floats of a query tile's row statistics: -LSE (base 2), then -delta
 
 template <int D>
@@ -44,11 +46,11 @@ struct BwdCfg {
   static constexpr uint32_t BOX_BYTES = kTile * 128;
   static constexpr uint32_t TILE_BYTES = NBOX * BOX_BYTES;
   // kv items: K, V, then rings of Q and dO tiles and of row statistics
-  static constexpr int NQ = D == 128 ? 2 : 4;
+  static constexpr int NQ = D == 128 ? 3 : 4, ND = D == 128 ? 2 : 4;
   static constexpr uint32_t K_OFF = 0, V_OFF = TILE_BYTES;
   static constexpr uint32_t QR_OFF = 2 * TILE_BYTES, DOR_OFF = QR_OFF + NQ * TILE_BYTES;
-  static constexpr uint32_t ST_OFF = DOR_OFF + NQ * TILE_BYTES;
-  static constexpr uint32_t KV_END = ST_OFF + NQ * kStat * 4;
+  static constexpr uint32_t ST_OFF = DOR_OFF + ND * TILE_BYTES;
+  static constexpr uint32_t KV_END = ST_OFF + ND * kStat * 4;
   // query items: Q, dO, then rings of K and V tiles
   static constexpr int NK = D == 128 ? 3 : 5, NV = D == 128 ? 2 : 4;
   static constexpr uint32_t Q_OFF = 0, DO_OFF = TILE_BYTES;
@@ -56,10 +58,10 @@ struct BwdCfg {
   static constexpr uint32_t Q_END = VR_OFF + NV * TILE_BYTES;
   static constexpr uint32_t ITEM_OFF = KV_END > Q_END ? KV_END : Q_END;  // two item records
   static constexpr uint32_t BAR_OFF = ITEM_OFF + 2 * 64;
-  static constexpr int NBAR = 72;
+  static constexpr int NBAR = 4 + 2 * NQ + ND + 11 + 4 + 2 * NK + 2 * NV + 8 + 8;
   static constexpr uint32_t TMEM_PTR_OFF = BAR_OFF + NBAR * 8;
   static constexpr uint32_t ABORT_OFF = TMEM_PTR_OFF + 8;
-  static constexpr uint32_t BYTES = ABORT_OFF + 16 + 1024;  // + alignment slack
+  static constexpr uint32_t BYTES = ABORT_OFF + 16;  // from a 1024-byte boundary
   static_assert(BYTES <= 227 * 1024, "shared memory budget");
   // TMEM: S / P at 0, dP / dS at 128; kv items dV at 256, dK at 256 + D; query items dQ at 256,
   // two buffers of dS at 384 and 448
@@ -71,6 +73,7 @@ struct BwdParams {
   const float* stats;       // [planes][tiles][2][128]
   unsigned int* counters;   // [0] kv items, [1] query items
   int B, Hq, Hkv, Sq, Skv, causal;
+  int lg;                   // a query plane's rows are those of 2^lg heads of one kv head
   float c;                  // scale * log2(e)
   float scale;
   int q_tiles, kv_tiles;    // dense: tiles per plane
@@ -82,15 +85,19 @@ struct BwdParams {
   KernelCtl ctl;
 };
 
-// One item as the roles see it.  Rows are counted within the sequence; a tile's rows r of head h
-// start at row `qb + r` of plane h (ragged) or at row r of plane b * H + h (dense).
+// Query planes.  The rows of a plane are the rows of 2^lg query heads of one kv head, ordered by
+// query: row i is query i >> lg of the plane's head i mod 2^lg.  A tile of 128 rows then has 128 >> lg
+// queries of each, so that few or odd numbers of queries still fill tiles (chunk of 515 queries, 4
+// heads per kv head: 17 tiles instead of 20; one query of 8 heads: one tile instead of 8).
+//
+// One item as the roles see it.  Rows are counted within the sequence's plane.
 struct Item {
   int n;          // inner steps in all (0: gradients are zero); -1: no item is left
   int row0;       // first row of the item's own tile (keys / queries)
   int plane;      // kv items: kv plane; query items: query plane
   int other;      // kv items: first query plane of the group; query items: kv plane
   int t0, nt;     // inner tiles per plane: t0 .. t0 + nt - 1
-  int sq, skv;    // lengths
+  int sq, skv;    // lengths in queries and keys
   int qb, kb;     // first query and key row of the sequence (0 for dense)
   int stat0;      // first tile of the sequence within a plane's row statistics
 };
@@ -114,21 +121,23 @@ struct Cursor {
   long long first;  // index of sequence b's first item
   int tiles;        // its tiles per plane
 };
-__device__ __forceinline__ int seq_tiles(const int32_t* cu, int b) {
+__device__ __forceinline__ int seq_tiles(const int32_t* cu, int b, int lg) {
   const int n = cu[b + 1] - cu[b];
-  return n > 0 ? (n + kTile - 1) / kTile : 0;
+  return n > 0 ? ((n << lg) + kTile - 1) / kTile : 0;
 }
-__device__ __forceinline__ bool cursor_to(Cursor& cur, const int32_t* cu, int B, int planes, long long idx) {
-  if (cur.b < 0) cur = {0, 0, seq_tiles(cu, 0)};
+__device__ __forceinline__ bool cursor_to(Cursor& cur, const int32_t* cu, int lg, int B, int planes, long long idx) {
+  if (cur.b < 0) cur = {0, 0, seq_tiles(cu, 0, lg)};
   while (cur.b < B && idx >= cur.first + static_cast<long long>(cur.tiles) * planes) {
     cur.first += static_cast<long long>(cur.tiles) * planes;
     ++cur.b;
-    cur.tiles = cur.b < B ? seq_tiles(cu, cur.b) : 0;
+    cur.tiles = cur.b < B ? seq_tiles(cu, cur.b, lg) : 0;
   }
   return cur.b < B;
 }
 // First tile of sequence b in a plane's row statistics: tiles of different sequences never meet.
-__device__ __forceinline__ int ragged_stat0(const int32_t* cu_q, int b) { return cu_q[b] / kTile + b; }
+__device__ __forceinline__ int ragged_stat0(const int32_t* cu_q, int b, int lg) {
+  return static_cast<int>((static_cast<long long>(cu_q[b]) << lg) / kTile) + b;
+}
 
 // KV: item idx of the kv items, else of the query items.
 template <bool KV, bool VARLEN>
@@ -136,11 +145,11 @@ __device__ __forceinline__ Item make_item(const BwdParams& p, long long idx, Cur
   Item it;
   it.n = -1;
   int tile, b;
-  const int G = p.Hq / p.Hkv;
+  const int G = p.Hq / p.Hkv >> p.lg, HP = p.Hq >> p.lg;  // query planes of a kv head, of a sequence
   if constexpr (VARLEN) {
-    const int planes = KV ? p.Hkv : p.Hq;
+    const int planes = KV ? p.Hkv : HP;
     const int32_t* cu = KV ? p.cu_k : p.cu_q;
-    if (!cursor_to(cur, cu, p.B, planes, idx)) return it;
+    if (!cursor_to(cur, cu, KV ? 0 : p.lg, p.B, planes, idx)) return it;
     b = cur.b;
     const int in = static_cast<int>(idx - cur.first);
     tile = in / planes;
@@ -150,20 +159,20 @@ __device__ __forceinline__ Item make_item(const BwdParams& p, long long idx, Cur
     it.kb = p.cu_k[b];
     it.sq = p.cu_q[b + 1] - it.qb;
     it.skv = p.cu_k[b + 1] - it.kb;
-    it.stat0 = ragged_stat0(p.cu_q, b);
+    it.stat0 = ragged_stat0(p.cu_q, b, p.lg);
     // (causal query tiles are longest at the sequence's end)
     if (!KV && p.causal) tile = cur.tiles - 1 - tile;
   } else {
     if (idx >= (KV ? p.kv_items : p.q_items)) return it;
     const DenseItem d = KV ? dense_item(static_cast<int>(idx), p.kv_tiles, p.B * p.Hkv, p.kv_block)
-                           : dense_item(static_cast<int>(idx), p.q_tiles, p.B * p.Hq, p.q_block);
+                           : dense_item(static_cast<int>(idx), p.q_tiles, p.B * HP, p.q_block);
     it.plane = d.plane;
     if constexpr (KV) {
       b = d.plane / p.Hkv;
-      it.other = b * p.Hq + (d.plane - b * p.Hkv) * G;
+      it.other = b * HP + (d.plane - b * p.Hkv) * G;
     } else {
-      b = d.plane / p.Hq;
-      it.other = b * p.Hkv + (d.plane - b * p.Hq) / G;
+      b = d.plane / HP;
+      it.other = b * p.Hkv + (d.plane - b * HP) / G;
     }
     tile = !KV && p.causal ? p.q_tiles - 1 - d.tile : d.tile;
     it.qb = it.kb = it.stat0 = 0;
@@ -173,12 +182,12 @@ __device__ __forceinline__ Item make_item(const BwdParams& p, long long idx, Cur
   it.row0 = tile * kTile;
   const int off = it.skv - it.sq;  // query i sees keys <= i + off
   if constexpr (KV) {
-    const int tiles = (it.sq + kTile - 1) / kTile;
-    it.t0 = p.causal ? min(tiles, max(0, it.row0 - off) / kTile) : 0;
+    const int tiles = ((it.sq << p.lg) + kTile - 1) / kTile;
+    it.t0 = p.causal ? min(tiles, (max(0, min(it.sq, it.row0 - off)) << p.lg) / kTile) : 0;
     it.nt = tiles - it.t0;
     it.n = it.nt * G;
   } else {
-    const int seen = p.causal ? min(it.skv, it.row0 + kTile + off) : it.skv;
+    const int seen = p.causal ? min(it.skv, ((it.row0 + kTile) >> p.lg) + off) : it.skv;
     it.t0 = 0;
     it.nt = it.n = seen > 0 ? (seen + kTile - 1) / kTile : 0;
   }
@@ -205,8 +214,36 @@ __device__ __forceinline__ bool ring_get(const ItemRing& r, int i, Item& it, con
   if ((threadIdx.x & 31) == 0) mbar_arrive(r.empty + 8 * (i & 1));
   return true;
 }
-constexpr int kItemReaders = 9;  // the MMA warp and the elementwise warps
+// A whole warp's wait for two barriers at once, by different lanes: a wait costs the MMA warp some
+// 150 clocks even if the phase is over, and it has no time to spare.
+__device__ __forceinline__ bool wait_two(uint32_t bar0, uint32_t par0, uint32_t bar1, uint32_t par1, const KernelCtl& ctl,
+                                         const Abort& ab) {
+  const bool odd = threadIdx.x & 1;
+  return mbar_wait_warp(odd ? bar1 : bar0, odd ? par1 : par0, ctl, ab);
+}
+__device__ __forceinline__ bool wait_three(uint32_t bar0, uint32_t par0, uint32_t bar1, uint32_t par1, uint32_t bar2,
+                                           uint32_t par2, const KernelCtl& ctl, const Abort& ab) {
+  const int i = threadIdx.x & 3;
+  return mbar_wait_warp(i == 0 ? bar0 : i == 1 ? bar1 : bar2, i == 0 ? par0 : i == 1 ? par1 : par2, ctl, ab);
+}
+// One arrival for a warp whose lanes are all done with what the barrier guards.
+__device__ __forceinline__ void warp_arrive(uint32_t bar) {
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) mbar_arrive(bar);
+}
+constexpr int kItemReaders = kEltWarps + 2;  // the elementwise warps and the MMA warps
 
+// A tile of a query plane: 128 >> lg queries of 2^lg heads, from row `row` of the plane of a sequence
+// that starts at query qb.
+template <int D, bool VARLEN>
+__device__ __forceinline__ void load_q_tile(uint32_t dst, const CUtensorMap* map, int plane, int qb, int row, int lg,
+                                            uint32_t bar) {
+  using C = BwdCfg<D>;
+  const int query = qb + (row >> lg);
+#pragma unroll
+  for (int x = 0; x < C::NBOX; ++x)
+    tma_load_4d(dst + x * C::BOX_BYTES, map, x * 64, 0, VARLEN ? plane : query, VARLEN ? query : plane, bar);
+}
 template <int D, bool VARLEN>
 __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, int plane, int row, uint32_t bar) {
   using C = BwdCfg<D>;
@@ -242,6 +279,15 @@ __device__ __forceinline__ void issue_grad_half(uint32_t d_tmem, uint32_t a_tmem
   using C = BwdCfg<D>;
   constexpr uint32_t idesc = idesc_bf16(kTile, D, 0, 1);
   mma_ts_k64_el(d_tmem, a_tmem, sdesc_sw128(b, C::BOX_BYTES, 1024) + h * 64 * (128 >> 4), idesc, acc ? 1u : 0u);
+}
+// The same over chunk c (32 rows) of each half of the tile: A's halves are 64 columns apart.
+template <int D>
+__device__ __forceinline__ void issue_grad_chunks(uint32_t d_tmem, uint32_t a_tmem, uint32_t b, int c, bool acc) {
+  using C = BwdCfg<D>;
+  constexpr uint32_t idesc = idesc_bf16(kTile, D, 0, 1);
+  const uint64_t db = sdesc_sw128(b, C::BOX_BYTES, 1024) + c * 32 * (128 >> 4);
+  mma_ts_k32_el(d_tmem, a_tmem + 16 * c, db, idesc, acc ? 1u : 0u);
+  mma_ts_k32_el(d_tmem, a_tmem + 64 + 16 * c, db + 64 * (128 >> 4), idesc, 1u);
 }
 
 // 64 TMEM columns of this thread's lane.
@@ -290,29 +336,62 @@ struct Shared {
   Abort ab, drain_ab;
 };
 
+// P^T of 64 queries (this thread's key row) from S^T in s, left in s as fp32, and as bf16 over S^T in
+// TMEM in two chunks of 32 queries, each handed to the MMA warp as it is written.  nl: -LSE of the
+// queries in shared memory.
+__device__ __forceinline__ void probs_t(uint32_t* s, uint32_t s_tm, uint32_t nl, uint64_t c2, uint32_t bar_p) {
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    uint32_t pk[16];
+#pragma unroll
+    for (int i = 0; i < 32; i += 4) {
+      const int e = 32 * c + i;
+      const uint4 l4 = ld_shared_v4(nl + 4 * e);
+      const uint64_t x0 = fma2(f2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), c2,
+                               f2(__uint_as_float(l4.x), __uint_as_float(l4.y)));
+      const uint64_t x1 = fma2(f2(__uint_as_float(s[e + 2]), __uint_as_float(s[e + 3])), c2,
+                               f2(__uint_as_float(l4.z), __uint_as_float(l4.w)));
+      const float p0 = ex2(f2lo(x0)), p1 = ex2(f2hi(x0)), p2 = ex2(f2lo(x1)), p3 = ex2(f2hi(x1));
+      s[e] = __float_as_uint(p0);
+      s[e + 1] = __float_as_uint(p1);
+      s[e + 2] = __float_as_uint(p2);
+      s[e + 3] = __float_as_uint(p3);
+      pk[i / 2] = pack_bf16x2(p0, p1);
+      pk[i / 2 + 1] = pack_bf16x2(p2, p3);
+    }
+    tmem_st16(s_tm + 16 * c, pk);
+    tmem_wait_st();
+    tc_fence_before();
+    warp_arrive(bar_p + 8 * c);
+    if (c == 0) reg_fence32(s + 32);  // keeps the second chunk's arithmetic behind the first's hand-over
+  }
+}
+
 // ---------------------------------------------------------------- kv items: dK and dV
 // Per step n (one query tile of one head):
-//   MMA warp     S^T = K Q^T | dP^T = V dO^T, and once the elementwise warps have written P^T and
-//                dS^T (bf16, over S^T and dP^T):  dV += P^T dO,  dK += dS^T Q.  Issue order
-//                dV_n, S_n+1 | dK_n, dP_n+1: the tensor pipe has the products of one step's P
-//                while dS is computed, and those of dS while the next P is.
+//   MMA warps    S^T = K Q^T | dP^T = V dO^T, and once the elementwise warps have written P^T and
+//                dS^T (bf16, over S^T and dP^T):  dV += P^T dO,  dK += dS^T Q.  One warp issues
+//                dV_n, S_n+1, the other dK_n, dP_n+1: the tensor pipe has the products of one
+//                step's P while dS is computed, and those of dS while the next P is; and while
+//                one warp waits (150 to 240 clocks a wait, done or not), the other issues.
 //   elementwise  a thread has key row = TMEM lane, 64 of the tile's 128 queries (warps 0-3 the
 //                first half, 4-7 the second).
 template <int D, bool VARLEN>
 __device__ __forceinline__ void kv_items(const BwdParams& p, const Shared& sh, const CUtensorMap* tm_q,
                                          const CUtensorMap* tm_do, const CUtensorMap* tm_k, const CUtensorMap* tm_v) {
   using C = BwdCfg<D>;
-  constexpr int NQ = C::NQ;
+  constexpr int NQ = C::NQ, ND = C::ND;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const KernelCtl& ctl = p.ctl;
   const Abort& ab = sh.ab;
   const uint32_t bar_k = sh.bars, bar_v = bar_k + 8, bar_ke = bar_v + 8, bar_ve = bar_ke + 8;
-  const uint32_t bar_q = bar_ve + 8, bar_qe = bar_q + 8 * NQ, bar_do = bar_qe + 8 * NQ, bar_doe = bar_do + 8 * NQ;
-  const uint32_t bar_s = bar_doe + 8 * NQ, bar_dp = bar_s + 8, bar_p = bar_dp + 8, bar_ds = bar_p + 16;
+  const uint32_t bar_q = bar_ve + 8, bar_qe = bar_q + 8 * NQ, bar_do = bar_qe + 8 * NQ;
+  const uint32_t bar_s = bar_do + 8 * C::ND, bar_dp = bar_s + 8, bar_p = bar_dp + 8, bar_ds = bar_p + 16;
   const uint32_t bar_acc = bar_ds + 16, bar_acce = bar_acc + 8, bar_drain = bar_acce + 8;
+  const uint32_t bar_si = bar_drain + 8;  // [step % 2] the next step's S has been issued
   const uint32_t sb = sh.base;
 
-  if (warp == 8) {
+  if (warp == kLoader) {
     if (lane == 0) {
       int n = 0, filled = 0;  // steps and items with steps so far
       int in_flight_q = 0, in_flight_do = 0;
@@ -322,20 +401,17 @@ __device__ __forceinline__ void kv_items(const BwdParams& p, const Shared& sh, c
         const Item it = make_item<true, VARLEN>(p, atomicAdd(p.counters, 1u), cur);
         if (!(ok = ring_put(sh.items, i, it, ctl, ab)) || it.n < 0) break;
         for (int j = 0; j < it.n; ++j, ++n) {
-          const int slot = n % NQ, ph = n / NQ;
+          const int qs = n % NQ, ds = n % ND;
           const int g = j / it.nt, t = it.t0 + j - g * it.nt;
           if (j == 0) {
             if (filled > 0 && !(ok = mbar_wait(bar_ke, (filled - 1) & 1, ctl, ab))) break;
             mbar_expect_tx(bar_k, C::TILE_BYTES);
             load_tile<D, VARLEN>(sb + C::K_OFF, tm_k, it.plane, it.kb + it.row0, bar_k);
           }
-          if (ph > 0 && !(ok = mbar_wait(bar_qe + 8 * slot, (ph - 1) & 1, ctl, ab))) break;
+          if (n >= NQ && !(ok = mbar_wait(bar_qe + 8 * qs, (n / NQ - 1) & 1, ctl, ab))) break;
           if (ctl.inject == 4 && n == 1) break;  // test hook: never load this tile
-          mbar_expect_tx(bar_q + 8 * slot, C::TILE_BYTES + kStat * 4);
-          load_tile<D, VARLEN>(sb + C::QR_OFF + slot * C::TILE_BYTES, tm_q, it.other + g, it.qb + t * kTile, bar_q + 8 * slot);
-          bulk_g2s(sb + C::ST_OFF + slot * (kStat * 4),
-                   p.stats + (static_cast<size_t>(it.other + g) * p.stat_tiles + it.stat0 + t) * kStat, kStat * 4,
-                   bar_q + 8 * slot);
+          mbar_expect_tx(bar_q + 8 * qs, C::TILE_BYTES);
+          load_q_tile<D, VARLEN>(sb + C::QR_OFF + qs * C::TILE_BYTES, tm_q, it.other + g, it.qb, t * kTile, p.lg, bar_q + 8 * qs);
           in_flight_q = n + 1;
           if (j == 0) {
             if (filled > 0 && !(ok = mbar_wait(bar_ve, (filled - 1) & 1, ctl, ab))) break;
@@ -343,9 +419,14 @@ __device__ __forceinline__ void kv_items(const BwdParams& p, const Shared& sh, c
             load_tile<D, VARLEN>(sb + C::V_OFF, tm_v, it.plane, it.kb + it.row0, bar_v);
             ++filled;
           }
-          if (ph > 0 && !(ok = mbar_wait(bar_doe + 8 * slot, (ph - 1) & 1, ctl, ab))) break;
-          mbar_expect_tx(bar_do + 8 * slot, C::TILE_BYTES);
-          load_tile<D, VARLEN>(sb + C::DOR_OFF + slot * C::TILE_BYTES, tm_do, it.other + g, it.qb + t * kTile, bar_do + 8 * slot);
+          // dV and dK of step n - ND are done, and so are dP, issued before dK, and the reading of the
+          // step's row statistics
+          if (n >= ND && !(ok = mbar_wait(bar_qe + 8 * ((n - ND) % NQ), (n - ND) / NQ & 1, ctl, ab))) break;
+          mbar_expect_tx(bar_do + 8 * ds, C::TILE_BYTES + kStat * 4);
+          load_q_tile<D, VARLEN>(sb + C::DOR_OFF + ds * C::TILE_BYTES, tm_do, it.other + g, it.qb, t * kTile, p.lg, bar_do + 8 * ds);
+          bulk_g2s(sb + C::ST_OFF + ds * (kStat * 4),
+                   p.stats + (static_cast<size_t>(it.other + g) * p.stat_tiles + it.stat0 + t) * kStat, kStat * 4,
+                   bar_do + 8 * ds);
           in_flight_do = n + 1;
         }
         if (ctl.inject == 4 && n == 1) break;
@@ -356,11 +437,12 @@ __device__ __forceinline__ void kv_items(const BwdParams& p, const Shared& sh, c
         mbar_wait(bar_v, (filled - 1) & 1, ctl, sh.drain_ab);
       }
       for (int m = max(0, in_flight_q - NQ); m < in_flight_q; ++m) mbar_wait(bar_q + 8 * (m % NQ), (m / NQ) & 1, ctl, sh.drain_ab);
-      for (int m = max(0, in_flight_do - NQ); m < in_flight_do; ++m)
-        mbar_wait(bar_do + 8 * (m % NQ), (m / NQ) & 1, ctl, sh.drain_ab);
+      for (int m = max(0, in_flight_do - ND); m < in_flight_do; ++m)
+        mbar_wait(bar_do + 8 * (m % ND), (m / ND) & 1, ctl, sh.drain_ab);
     }
     __syncwarp();
-  } else if (warp == 9) {
+  } else if (warp >= kMma0) {
+    const bool first = warp == kMma0;  // S and dV, or dP and dK
     const uint32_t tm = sh.tmem;
     int n = 0, filled = 0;
     bool ok = true;
@@ -368,61 +450,69 @@ __device__ __forceinline__ void kv_items(const BwdParams& p, const Shared& sh, c
     for (int i = 0; ok; ++i) {
       if (!(ok = ring_get(sh.items, i, it, ctl, ab)) || it.n < 0) break;
       if (it.n == 0) continue;
-      // rows of the step's query tile that belong to the sequence
-      auto rows_of = [&](int j) { return it.sq - (it.t0 + j % it.nt) * kTile; };
-      auto scores = [&](int j) -> bool {
-        const int slot = (n + j) % NQ;
-        const uint32_t q = sb + C::QR_OFF + slot * C::TILE_BYTES;
-        if (!mbar_wait_warp(bar_q + 8 * slot, ((n + j) / NQ) & 1, ctl, ab)) return false;
-        if (VARLEN && rows_of(j) < kTile) {
-          zero_rows<D>(q, rows_of(j));
+      auto zero_past_end = [&](uint32_t tile, int j) {
+        const int rows = (it.sq << p.lg) - (it.t0 + j % it.nt) * kTile;  // of the step's query tile, within the sequence
+        if (VARLEN && rows < kTile) {
+          zero_rows<D>(tile, rows);
           fence_proxy_async_smem();
           __syncwarp();
         }
-        tc_fence_after();
-        issue_scores<D>(tm + C::S_COL, sb + C::K_OFF, q);
-        tc_commit_el(bar_s);
-        if (j + 1 == it.n) tc_commit_el(bar_ke);
-        return true;
       };
-      auto dprobs = [&](int j) -> bool {
-        const int slot = (n + j) % NQ;
-        const uint32_t d = sb + C::DOR_OFF + slot * C::TILE_BYTES;
-        if (!mbar_wait_warp(bar_do + 8 * slot, ((n + j) / NQ) & 1, ctl, ab)) return false;
-        if (VARLEN && rows_of(j) < kTile) {
-          zero_rows<D>(d, rows_of(j));
-          fence_proxy_async_smem();
-          __syncwarp();
-        }
-        tc_fence_after();
-        issue_scores<D>(tm + C::DP_COL, sb + C::V_OFF, d);
-        tc_commit_el(bar_dp);
-        if (j + 1 == it.n) tc_commit_el(bar_ve);
-        return true;
-      };
-      if (!(ok = mbar_wait_warp(bar_k, filled & 1, ctl, ab) && scores(0))) break;
-      if (!(ok = mbar_wait_warp(bar_v, filled & 1, ctl, ab) && dprobs(0))) break;
-      for (int j = 0; j < it.n; ++j) {
-        const int m = n + j, slot = m % NQ;
-        const uint32_t q = sb + C::QR_OFF + slot * C::TILE_BYTES, d = sb + C::DOR_OFF + slot * C::TILE_BYTES;
+      auto q_tile = [&](int j) { return sb + C::QR_OFF + (n + j) % NQ * C::TILE_BYTES; };
+      auto do_tile = [&](int j) { return sb + C::DOR_OFF + (n + j) % ND * C::TILE_BYTES; };
+      if (first) {
+        auto scores = [&](int j) {
+          zero_past_end(q_tile(j), j);
+          issue_scores<D>(tm + C::S_COL, sb + C::K_OFF, q_tile(j));
+          tc_commit_el(bar_s);
+          if (j + 1 == it.n) tc_commit_el(bar_ke);
+        };
+        if (!(ok = wait_two(bar_k, filled & 1, bar_q + 8 * (n % NQ), n / NQ & 1, ctl, ab))) break;
+        scores(0);
         // the gradients of the item before must have been read out
-        if (j == 0 && filled > 0 && !(ok = mbar_wait_warp(bar_acce, (filled - 1) & 1, ctl, ab))) break;
-        for (int h = 0; ok && h < 2; ++h) {
-          if (!(ok = mbar_wait_warp(bar_p + 8 * h, m & 1, ctl, ab))) break;
+        if (filled > 0 && !(ok = mbar_wait_warp(bar_acce, (filled - 1) & 1, ctl, ab))) break;
+        for (int j = 0; j < it.n; ++j) {
+          const int m = n + j;
+          const uint32_t par = m & 1;
+          const bool more = j + 1 < it.n;
+          if (!(ok = wait_two(bar_p, par, more ? bar_q + 8 * ((m + 1) % NQ) : bar_p, more ? (m + 1) / NQ & 1 : par, ctl, ab))) break;
+          zero_past_end(do_tile(j), j);  // (the elementwise warps have seen this tile arrive)
           tc_fence_after();
-          issue_grad_half<D>(tm + C::DV_COL, tm + C::S_COL + 64 * h, d, h, j > 0 || h > 0);
-        }
-        if (!ok) break;
-        tc_commit_el(bar_doe + 8 * slot);
-        if (j + 1 < it.n && !(ok = scores(j + 1))) break;
-        for (int h = 0; ok && h < 2; ++h) {
-          if (!(ok = mbar_wait_warp(bar_ds + 8 * h, m & 1, ctl, ab))) break;
+          issue_grad_chunks<D>(tm + C::DV_COL, tm + C::S_COL, do_tile(j), 0, j > 0);
+          if (!(ok = mbar_wait_warp(bar_p + 8, par, ctl, ab))) break;
           tc_fence_after();
-          issue_grad_half<D>(tm + C::DK_COL, tm + C::DP_COL + 64 * h, q, h, j > 0 || h > 0);
+          issue_grad_chunks<D>(tm + C::DV_COL, tm + C::S_COL, do_tile(j), 1, true);
+          if (more) scores(j + 1);
+          if (lane == 0) mbar_arrive(bar_si + 8 * (m & 1));
+          __syncwarp();
+          tc_commit_el(bar_qe + 8 * (m % NQ));
         }
-        if (!ok) break;
-        tc_commit_el(bar_qe + 8 * slot);
-        if (j + 1 < it.n && !(ok = dprobs(j + 1))) break;
+      } else {
+        auto dprobs = [&](int j) {
+          zero_past_end(do_tile(j), j);
+          issue_scores<D>(tm + C::DP_COL, sb + C::V_OFF, do_tile(j));
+          tc_commit_el(bar_dp);
+          if (j + 1 == it.n) tc_commit_el(bar_ve);
+        };
+        if (!(ok = wait_two(bar_v, filled & 1, bar_do + 8 * (n % ND), n / ND & 1, ctl, ab))) break;
+        dprobs(0);
+        if (filled > 0 && !(ok = mbar_wait_warp(bar_acce, (filled - 1) & 1, ctl, ab))) break;
+        for (int j = 0; j < it.n; ++j) {
+          const int m = n + j;
+          const uint32_t par = m & 1;
+          const bool more = j + 1 < it.n;
+          // dK goes behind the next S in the tensor pipe: the next P waits for that S
+          if (!(ok = wait_three(bar_ds, par, bar_si + 8 * (m & 1), m >> 1 & 1, more ? bar_do + 8 * ((m + 1) % ND) : bar_ds,
+                                more ? (m + 1) / ND & 1 : par, ctl, ab)))
+            break;
+          tc_fence_after();
+          issue_grad_chunks<D>(tm + C::DK_COL, tm + C::DP_COL, q_tile(j), 0, j > 0);
+          if (!(ok = mbar_wait_warp(bar_ds + 8, par, ctl, ab))) break;
+          tc_fence_after();
+          issue_grad_chunks<D>(tm + C::DK_COL, tm + C::DP_COL, q_tile(j), 1, true);
+          tc_commit_el(bar_qe + 8 * (m % NQ));
+          if (more) dprobs(j + 1);
+        }
       }
       if (!ok) break;
       tc_commit_el(bar_acc);
@@ -444,67 +534,52 @@ __device__ __forceinline__ void kv_items(const BwdParams& p, const Shared& sh, c
       if (!(ok = ring_get(sh.items, i, it, ctl, ab)) || it.n < 0) break;
       const int off = it.skv - it.sq, key = it.row0 + r;
       for (int j = 0; j < it.n; ++j, ++n) {
-        const int slot = n % NQ;
+        const int slot = n % ND;
         const uint32_t st = sb + C::ST_OFF + slot * (kStat * 4) + 256 * half;
         const int q0 = (it.t0 + j % it.nt) * kTile + 64 * half;
-        // (the statistics came with the query tile)
-        if (!(ok = mbar_wait_warp(bar_q + 8 * slot, (n / NQ) & 1, ctl, ab))) break;
-        if (!(ok = mbar_wait_warp(bar_s, n & 1, ctl, ab))) break;
+        // (the statistics come with the dO tile)
+        if (!(ok = wait_two(bar_s, n & 1, bar_do + 8 * slot, n / ND & 1, ctl, ab))) break;
         tc_fence_after();
         uint32_t s[64];
         ld64(s_tm, s);
-        if (p.causal && q0 + off < it.row0 + kTile - 1) {
+        if (p.causal && (q0 >> p.lg) + off < it.row0 + kTile - 1) {
           // queries from key - off on see this key
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
-            const int hid = key - off - q0 - 32 * g;  // hidden queries of this word
+            const int hid = (max(0, min(it.sq, key - off)) << p.lg) - q0 - 32 * g;  // hidden rows of this word
             const uint32_t hidden = hid >= 32 ? 0xffffffffu : hid <= 0 ? 0u : (1u << hid) - 1u;
 #pragma unroll
             for (int e = 0; e < 32; ++e)
               if (hidden & (1u << e)) s[32 * g + e] = __float_as_uint(-INFINITY);
           }
         }
-        uint32_t pk[32];
-#pragma unroll
-        for (int e = 0; e < 64; e += 4) {
-          const uint4 l4 = ld_shared_v4(st + 4 * e);
-          const uint64_t x0 = fma2(f2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), c2,
-                                   f2(__uint_as_float(l4.x), __uint_as_float(l4.y)));
-          const uint64_t x1 = fma2(f2(__uint_as_float(s[e + 2]), __uint_as_float(s[e + 3])), c2,
-                                   f2(__uint_as_float(l4.z), __uint_as_float(l4.w)));
-          const float p0 = ex2(f2lo(x0)), p1 = ex2(f2hi(x0)), p2 = ex2(f2lo(x1)), p3 = ex2(f2hi(x1));
-          s[e] = __float_as_uint(p0);
-          s[e + 1] = __float_as_uint(p1);
-          s[e + 2] = __float_as_uint(p2);
-          s[e + 3] = __float_as_uint(p3);
-          pk[e / 2] = pack_bf16x2(p0, p1);
-          pk[e / 2 + 1] = pack_bf16x2(p2, p3);
-        }
-        tmem_st32(s_tm, pk);
-        tmem_wait_st();
-        tc_fence_before();
-        mbar_arrive(bar_p + 8 * half);
-
+        probs_t(s, s_tm, st, c2, bar_p);
         if (!(ok = mbar_wait_warp(bar_dp, n & 1, ctl, ab))) break;
         tc_fence_after();
         uint32_t d[64];
         ld64(dp_tm, d);
 #pragma unroll
-        for (int e = 0; e < 64; e += 4) {
-          const uint4 l4 = ld_shared_v4(st + kTile * 4 + 4 * e);
-          const uint64_t x0 = mul2(add2(f2(__uint_as_float(d[e]), __uint_as_float(d[e + 1])),
-                                        f2(__uint_as_float(l4.x), __uint_as_float(l4.y))),
-                                   f2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])));
-          const uint64_t x1 = mul2(add2(f2(__uint_as_float(d[e + 2]), __uint_as_float(d[e + 3])),
-                                        f2(__uint_as_float(l4.z), __uint_as_float(l4.w))),
-                                   f2(__uint_as_float(s[e + 2]), __uint_as_float(s[e + 3])));
-          pk[e / 2] = pack_bf16x2(f2lo(x0), f2hi(x0));
-          pk[e / 2 + 1] = pack_bf16x2(f2lo(x1), f2hi(x1));
+        for (int c = 0; c < 2; ++c) {
+          uint32_t pk[16];
+#pragma unroll
+          for (int i = 0; i < 32; i += 4) {
+            const int e = 32 * c + i;
+            const uint4 l4 = ld_shared_v4(st + kTile * 4 + 4 * e);
+            const uint64_t x0 = mul2(add2(f2(__uint_as_float(d[e]), __uint_as_float(d[e + 1])),
+                                          f2(__uint_as_float(l4.x), __uint_as_float(l4.y))),
+                                     f2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])));
+            const uint64_t x1 = mul2(add2(f2(__uint_as_float(d[e + 2]), __uint_as_float(d[e + 3])),
+                                          f2(__uint_as_float(l4.z), __uint_as_float(l4.w))),
+                                     f2(__uint_as_float(s[e + 2]), __uint_as_float(s[e + 3])));
+            pk[i / 2] = pack_bf16x2(f2lo(x0), f2hi(x0));
+            pk[i / 2 + 1] = pack_bf16x2(f2lo(x1), f2hi(x1));
+          }
+          tmem_st16(dp_tm + 16 * c, pk);
+          tmem_wait_st();
+          tc_fence_before();
+          warp_arrive(bar_ds + 8 * c);
+          if (c == 0) reg_fence32(d + 32);
         }
-        tmem_st32(dp_tm, pk);
-        tmem_wait_st();
-        tc_fence_before();
-        mbar_arrive(bar_ds + 8 * half);
       }
       if (!ok) break;
       // warps 0-3 store dV, warps 4-7 dK
@@ -520,7 +595,7 @@ __device__ __forceinline__ void kv_items(const BwdParams& p, const Shared& sh, c
       tc_fence_after();
       store_row<D>(tm + (half ? C::DK_COL : C::DV_COL), half ? p.scale : 1.f, dst, store);
       tc_fence_before();
-      mbar_arrive(bar_acce);
+      warp_arrive(bar_acce);
       ++filled;
     }
   }
@@ -530,8 +605,8 @@ __device__ __forceinline__ void kv_items(const BwdParams& p, const Shared& sh, c
 // Per step n (one kv tile):  S = Q K^T,  dP = dO V^T,  dQ += dS K.  P never leaves the registers;
 // dS has two TMEM buffers of its own, so S and dP of the next step are issued as soon as the
 // elementwise warps have loaded this step's.  They may therefore finish the next dS before the MMA
-// warp has looked at this one: each buffer has barriers of its own (those of one buffer are two
-// steps apart, and S of step n + 2 is issued behind dQ of step n).
+// warp has looked at this one: each buffer has barriers of its own, and is written again once dQ of
+// two steps before is done.
 template <int D, bool VARLEN>
 __device__ __forceinline__ void q_items(const BwdParams& p, const Shared& sh, const CUtensorMap* tm_q,
                                         const CUtensorMap* tm_do, const CUtensorMap* tm_k, const CUtensorMap* tm_v) {
@@ -541,12 +616,13 @@ __device__ __forceinline__ void q_items(const BwdParams& p, const Shared& sh, co
   const KernelCtl& ctl = p.ctl;
   const Abort& ab = sh.ab;
   const uint32_t bar_q = sh.bars, bar_do = bar_q + 8, bar_qe = bar_do + 8, bar_doe = bar_qe + 8;
-  const uint32_t bar_k = bar_doe + 8, bar_ke = bar_k + 8 * NK, bar_v = bar_ke + 8 * NK, bar_ve = bar_v + 8 * NV;
-  const uint32_t bar_s = bar_ve + 8 * NV, bar_dp = bar_s + 8, bar_sf = bar_dp + 8, bar_dpf = bar_sf + 8;
-  const uint32_t bar_ds = bar_dpf + 8, bar_acc = bar_ds + 32, bar_acce = bar_acc + 8, bar_drain = bar_acce + 8;
+  const uint32_t bar_k = bar_doe + 8, bar_ke = bar_k + 8 * NK, bar_v = bar_ke + 8 * NK;
+  // bar_dpf[step % NV]: dP is in registers, and so V's slot is free
+  const uint32_t bar_s = bar_v + 8 * NV, bar_dp = bar_s + 8, bar_sf = bar_dp + 8, bar_dpf = bar_sf + 8;
+  const uint32_t bar_ds = bar_dpf + 8 * NV, bar_acc = bar_ds + 16, bar_acce = bar_acc + 8, bar_drain = bar_acce + 8;
   const uint32_t sb = sh.base;
 
-  if (warp == 8) {
+  if (warp == kLoader) {
     if (lane == 0) {
       int n = 0, filled = 0;
       int in_flight_k = 0, in_flight_v = 0;
@@ -559,7 +635,7 @@ __device__ __forceinline__ void q_items(const BwdParams& p, const Shared& sh, co
           if (j == 0) {
             if (filled > 0 && !(ok = mbar_wait(bar_qe, (filled - 1) & 1, ctl, ab))) break;
             mbar_expect_tx(bar_q, C::TILE_BYTES);
-            load_tile<D, VARLEN>(sb + C::Q_OFF, tm_q, it.plane, it.qb + it.row0, bar_q);
+            load_q_tile<D, VARLEN>(sb + C::Q_OFF, tm_q, it.plane, it.qb, it.row0, p.lg, bar_q);
           }
           const int ks = n % NK, kp = n / NK, vs = n % NV, vp = n / NV;
           if (kp > 0 && !(ok = mbar_wait(bar_ke + 8 * ks, (kp - 1) & 1, ctl, ab))) break;
@@ -569,10 +645,10 @@ __device__ __forceinline__ void q_items(const BwdParams& p, const Shared& sh, co
           if (j == 0) {
             if (filled > 0 && !(ok = mbar_wait(bar_doe, (filled - 1) & 1, ctl, ab))) break;
             mbar_expect_tx(bar_do, C::TILE_BYTES);
-            load_tile<D, VARLEN>(sb + C::DO_OFF, tm_do, it.plane, it.qb + it.row0, bar_do);
+            load_q_tile<D, VARLEN>(sb + C::DO_OFF, tm_do, it.plane, it.qb, it.row0, p.lg, bar_do);
             ++filled;
           }
-          if (vp > 0 && !(ok = mbar_wait(bar_ve + 8 * vs, (vp - 1) & 1, ctl, ab))) break;
+          if (vp > 0 && !(ok = mbar_wait(bar_dpf + 8 * vs, (vp - 1) & 1, ctl, ab))) break;
           mbar_expect_tx(bar_v + 8 * vs, C::TILE_BYTES);
           load_tile<D, VARLEN>(sb + C::VR_OFF + vs * C::TILE_BYTES, tm_v, it.other, it.kb + j * kTile, bar_v + 8 * vs);
           in_flight_v = n + 1;
@@ -586,7 +662,8 @@ __device__ __forceinline__ void q_items(const BwdParams& p, const Shared& sh, co
       for (int m = max(0, in_flight_v - NV); m < in_flight_v; ++m) mbar_wait(bar_v + 8 * (m % NV), (m / NV) & 1, ctl, sh.drain_ab);
     }
     __syncwarp();
-  } else if (warp == 9) {
+  } else if (warp >= kMma0) {
+    const bool first = warp == kMma0;  // S and dP, or dQ
     const uint32_t tm = sh.tmem;
     int n = 0, filled = 0;
     bool ok = true;
@@ -594,56 +671,49 @@ __device__ __forceinline__ void q_items(const BwdParams& p, const Shared& sh, co
     for (int i = 0; ok; ++i) {
       if (!(ok = ring_get(sh.items, i, it, ctl, ab)) || it.n < 0) break;
       if (it.n == 0) continue;
-      auto scores = [&](int j) -> bool {
-        const int m = n + j, slot = m % NK;
-        const uint32_t k = sb + C::KR_OFF + slot * C::TILE_BYTES;
-        if (m > 0 && !mbar_wait_warp(bar_sf, (m - 1) & 1, ctl, ab)) return false;  // S is in registers
-        if (!mbar_wait_warp(bar_k + 8 * slot, (m / NK) & 1, ctl, ab)) return false;
-        if (VARLEN && it.skv - j * kTile < kTile) {
-          zero_rows<D>(k, it.skv - j * kTile);
-          fence_proxy_async_smem();
-          __syncwarp();
-        }
-        tc_fence_after();
-        issue_scores<D>(tm + C::S_COL, sb + C::Q_OFF, k);
-        tc_commit_el(bar_s);
-        if (j + 1 == it.n) tc_commit_el(bar_qe);
-        return true;
-      };
-      auto dprobs = [&](int j) -> bool {
-        const int m = n + j, slot = m % NV;
-        const uint32_t v = sb + C::VR_OFF + slot * C::TILE_BYTES;
-        if (m > 0 && !mbar_wait_warp(bar_dpf, (m - 1) & 1, ctl, ab)) return false;
-        if (!mbar_wait_warp(bar_v + 8 * slot, (m / NV) & 1, ctl, ab)) return false;
-        if (VARLEN && it.skv - j * kTile < kTile) {
-          zero_rows<D>(v, it.skv - j * kTile);
-          fence_proxy_async_smem();
-          __syncwarp();
-        }
-        tc_fence_after();
-        issue_scores<D>(tm + C::DP_COL, sb + C::DO_OFF, v);
-        tc_commit_el(bar_dp);
-        tc_commit_el(bar_ve + 8 * slot);
-        if (j + 1 == it.n) tc_commit_el(bar_doe);
-        return true;
-      };
-      if (!(ok = mbar_wait_warp(bar_q, filled & 1, ctl, ab) && scores(0))) break;
-      if (!(ok = mbar_wait_warp(bar_do, filled & 1, ctl, ab) && dprobs(0))) break;
-      for (int j = 0; j < it.n; ++j) {
-        const int m = n + j, slot = m % NK;
-        if (j + 1 < it.n && !(ok = scores(j + 1) && dprobs(j + 1))) break;
-        if (j == 0 && filled > 0 && !(ok = mbar_wait_warp(bar_acce, (filled - 1) & 1, ctl, ab))) break;
-        for (int h = 0; ok && h < 2; ++h) {
-          if (!(ok = mbar_wait_warp(bar_ds + 16 * (m & 1) + 8 * h, (m >> 1) & 1, ctl, ab))) break;
+      auto k_tile = [&](int j) { return sb + C::KR_OFF + (n + j) % NK * C::TILE_BYTES; };
+      if (first) {
+        auto zero_past_end = [&](uint32_t tile, int j) {
+          if (VARLEN && it.skv - j * kTile < kTile) {
+            zero_rows<D>(tile, it.skv - j * kTile);
+            fence_proxy_async_smem();
+            __syncwarp();
+          }
+        };
+        for (int j = 0; j < it.n; ++j) {
+          const int m = n + j, ks = m % NK, vs = m % NV;
+          const uint32_t bk = bar_k + 8 * ks, pk = m / NK & 1, bv = bar_v + 8 * vs, pv = m / NV & 1;
+          const uint32_t v = sb + C::VR_OFF + vs * C::TILE_BYTES;
+          // the tiles, and S and dP of the step before in registers
+          if (j == 0 && !(ok = mbar_wait_warp(bar_q, filled & 1, ctl, ab))) break;
+          if (!(ok = wait_two(bk, pk, m > 0 ? bar_sf : bk, m > 0 ? (m - 1) & 1 : pk, ctl, ab))) break;
+          zero_past_end(k_tile(j), j);
           tc_fence_after();
-          issue_grad_half<D>(tm + C::DQ_COL, tm + C::DS_COL + 64 * (m & 1) + 32 * h, sb + C::KR_OFF + slot * C::TILE_BYTES, h,
-                             j > 0 || h > 0);
+          issue_scores<D>(tm + C::S_COL, sb + C::Q_OFF, k_tile(j));
+          tc_commit_el(bar_s);
+          if (j + 1 == it.n) tc_commit_el(bar_qe);
+          if (j == 0 && !(ok = mbar_wait_warp(bar_do, filled & 1, ctl, ab))) break;
+          if (!(ok = wait_two(bv, pv, m > 0 ? bar_dpf + 8 * ((m - 1) % NV) : bv, m > 0 ? (m - 1) / NV & 1 : pv, ctl, ab))) break;
+          zero_past_end(v, j);
+          tc_fence_after();
+          issue_scores<D>(tm + C::DP_COL, sb + C::DO_OFF, v);
+          tc_commit_el(bar_dp);
+          if (j + 1 == it.n) tc_commit_el(bar_doe);
         }
-        if (!ok) break;
-        tc_commit_el(bar_ke + 8 * slot);
+      } else {
+        // the gradient of the item before must have been read out
+        if (filled > 0 && !(ok = mbar_wait_warp(bar_acce, (filled - 1) & 1, ctl, ab))) break;
+        for (int j = 0; j < it.n; ++j) {
+          const int m = n + j;
+          if (!(ok = mbar_wait_warp(bar_ds + 8 * (m & 1), m >> 1 & 1, ctl, ab))) break;
+          tc_fence_after();
+          for (int h = 0; h < 2; ++h)
+            issue_grad_half<D>(tm + C::DQ_COL, tm + C::DS_COL + 64 * (m & 1) + 32 * h, k_tile(j), h, j > 0 || h > 0);
+          tc_commit_el(bar_ke + 8 * (m % NK));
+        }
+        if (ok) tc_commit_el(bar_acc);
       }
       if (!ok) break;
-      tc_commit_el(bar_acc);
       n += it.n;
       ++filled;
     }
@@ -658,7 +728,7 @@ __device__ __forceinline__ void q_items(const BwdParams& p, const Shared& sh, co
     Item it;
     for (int i = 0; ok; ++i) {
       if (!(ok = ring_get(sh.items, i, it, ctl, ab)) || it.n < 0) break;
-      const int q = it.row0 + r;
+      const int q = (it.row0 + r) >> p.lg;
       const float* st = p.stats + (static_cast<size_t>(it.plane) * p.stat_tiles + it.stat0 + it.row0 / kTile) * kStat + r;
       const float nl = __ldg(st), nd = __ldg(st + kTile);
       const uint64_t nl2 = f2(nl, nl), nd2 = f2(nd, nd);
@@ -670,7 +740,7 @@ __device__ __forceinline__ void q_items(const BwdParams& p, const Shared& sh, co
         uint32_t s[64];
         ld64(tm + C::S_COL + 64 * half, s);
         tc_fence_before();
-        mbar_arrive(bar_sf);
+        warp_arrive(bar_sf);
         if (k0 + 64 > limit) {
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
@@ -687,28 +757,29 @@ __device__ __forceinline__ void q_items(const BwdParams& p, const Shared& sh, co
           s[e] = __float_as_uint(ex2(f2lo(x)));
           s[e + 1] = __float_as_uint(ex2(f2hi(x)));
         }
-        if (!(ok = mbar_wait_warp(bar_dp, n & 1, ctl, ab))) break;
+        // ... and dQ of two steps before is done with this step's buffer of dS
+        const int m2 = n - 2;
+        if (!(ok = wait_two(bar_dp, n & 1, m2 >= 0 ? bar_ke + 8 * (m2 % NK) : bar_dp, m2 >= 0 ? m2 / NK & 1 : n & 1, ctl, ab))) break;
         tc_fence_after();
         uint32_t d[64], pk[32];
         ld64(tm + C::DP_COL + 64 * half, d);
         tc_fence_before();
-        mbar_arrive(bar_dpf);
+        warp_arrive(bar_dpf + 8 * (n % NV));
 #pragma unroll
         for (int e = 0; e < 64; e += 2) {
           const uint64_t x = mul2(add2(f2(__uint_as_float(d[e]), __uint_as_float(d[e + 1])), nd2),
                                   f2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])));
           pk[e / 2] = pack_bf16x2(f2lo(x), f2hi(x));
         }
-        // (dQ of two steps before, which read this buffer, was issued before this step's S)
         tmem_st32(tm + C::DS_COL + 64 * (n & 1) + 32 * half, pk);
         tmem_wait_st();
         tc_fence_before();
-        mbar_arrive(bar_ds + 16 * (n & 1) + 8 * half);
+        warp_arrive(bar_ds + 8 * (n & 1));
       }
       if (!ok) break;
       const bool store = q < it.sq;
-      const long long row = VARLEN ? static_cast<long long>(it.qb + q) * p.Hq + it.plane
-                                   : static_cast<long long>(it.plane) * p.Sq + q;
+      const long long head = (static_cast<long long>(it.plane) << p.lg) + ((it.row0 + r) & ((1 << p.lg) - 1));
+      const long long row = VARLEN ? static_cast<long long>(it.qb + q) * p.Hq + head : head * p.Sq + q;
       __nv_bfloat16* dst = p.dq + (store ? row : 0) * D + half * (D / 2);
       if (it.n == 0) {
         if (store) store_zeros<D / 2>(dst);
@@ -718,7 +789,7 @@ __device__ __forceinline__ void q_items(const BwdParams& p, const Shared& sh, co
       tc_fence_after();
       store_row<D / 2>(tm + C::DQ_COL + half * (D / 2), p.scale, dst, store);
       tc_fence_before();
-      mbar_arrive(bar_acce);
+      warp_arrive(bar_acce);
       ++filled;
     }
   }
@@ -729,30 +800,38 @@ __global__ void __launch_bounds__(kThreads, 1)
     attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_do,
                     const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const BwdParams p) {
   using C = BwdCfg<D>;
-  extern __shared__ uint8_t smem_raw[];
-  const uint32_t raw_base = smem_u32(smem_raw);
-  const uint32_t sbase = (raw_base + 1023u) & ~1023u;  // 128B-swizzled tiles
-  uint8_t* smem = smem_raw + (sbase - raw_base);
+  // 128-byte-swizzled tiles start at 1024-byte boundaries.  The tiles leave no room to round the
+  // base up (D = 128): it is aligned by declaration, and a launch where it is not does nothing but
+  // say so.
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const uint32_t sbase = smem_u32(smem);
+  if (sbase & 1023u) {
+    if (threadIdx.x == 0) atomicOr(p.ctl.err, kErrTimeout);
+    return;
+  }
   const int warp = threadIdx.x >> 5;
   uint32_t* tmem_ptr = reinterpret_cast<uint32_t*>(smem + C::TMEM_PTR_OFF);
   volatile int* flags = reinterpret_cast<volatile int*>(smem + C::ABORT_OFF);
 
   // Barriers of the kv items and of the query items: [0, kv) and [kv, ..), each with an item ring.
-  constexpr int kKvBars = 4 + 4 * C::NQ + 2 + 4 + 3, kQBars = 4 + 2 * C::NK + 2 * C::NV + 4 + 4 + 3;
+  constexpr int kKvBars = 4 + 2 * C::NQ + C::ND + 2 + 4 + 3 + 2, kQBars = 4 + 2 * C::NK + C::NV + 3 + C::NV + 2 + 3;
   static_assert(kKvBars + kQBars + 8 <= C::NBAR, "barrier space");
   const uint32_t bars = sbase + C::BAR_OFF;
   const uint32_t kv_bars = bars, q_bars = bars + 8 * kKvBars, ring_bars = q_bars + 8 * kQBars;
   if (threadIdx.x == 0) {
     for (int i = 0; i < kKvBars + kQBars; ++i) mbar_init(bars + 8 * i, 1);
-    // elementwise threads arrive on these
-    const uint32_t bar_p = kv_bars + 8 * (4 + 4 * C::NQ + 2);
-    for (int i = 0; i < 4; ++i) mbar_init(bar_p + 8 * i, 128);  // p[2], ds[2]
-    mbar_init(bar_p + 8 * 5, 256);                              // acc_empty
-    const uint32_t bar_sf = q_bars + 8 * (4 + 2 * C::NK + 2 * C::NV + 2);
-    mbar_init(bar_sf, 256);
-    mbar_init(bar_sf + 8, 256);    // dP free
-    for (int i = 2; i < 6; ++i) mbar_init(bar_sf + 8 * i, 128);  // ds[2][2]
-    mbar_init(bar_sf + 56, 256);   // acc_empty
+    // the elementwise warps arrive on these
+    const uint32_t bar_p = kv_bars + 8 * (4 + 2 * C::NQ + C::ND + 2);
+    for (int i = 0; i < 4; ++i) mbar_init(bar_p + 8 * i, kEltWarps);  // p[2], ds[2]
+    mbar_init(bar_p + 8 * 4, 2);                                      // acc: both MMA warps
+    mbar_init(bar_p + 8 * 5, kEltWarps);                              // acc_empty
+    mbar_init(bar_p + 8 * 6, 2);                                      // drain: both MMA warps
+    for (int i = 0; i < C::NQ; ++i) mbar_init(kv_bars + 8 * (4 + C::NQ + i), 2);  // q_empty: dV and dK
+    const uint32_t bar_sf = q_bars + 8 * (4 + 2 * C::NK + C::NV + 2);
+    for (int i = 0; i < 1 + C::NV + 2; ++i) mbar_init(bar_sf + 8 * i, kEltWarps);  // S free, dP free[NV], ds[2]
+    const uint32_t bar_qacce = bar_sf + 8 * (1 + C::NV + 3);
+    mbar_init(bar_qacce, kEltWarps);
+    mbar_init(bar_qacce + 8, 2);  // drain: both MMA warps
     for (int i = 0; i < 2; ++i) {  // two rings: full[2], empty[2]
       mbar_init(ring_bars + 32 * i, 1);
       mbar_init(ring_bars + 32 * i + 8, 1);
@@ -763,8 +842,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     flags[1] = 0;
     fence_barrier_init();
   }
-  if (warp == 9) tmem_alloc(smem_u32(tmem_ptr), 512);
-  if (threadIdx.x == 256) {
+  if (warp == kMma0) tmem_alloc(smem_u32(tmem_ptr), 512);
+  if (threadIdx.x == kLoader * 32) {
     prefetch_tensormap(&tm_q);
     prefetch_tensormap(&tm_do);
     prefetch_tensormap(&tm_k);
@@ -795,20 +874,20 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncwarp();
   tc_fence_before();
   __syncthreads();
-  if (warp == 9) {
+  if (warp == kMma0) {
     tc_fence_after();
     tmem_dealloc(*tmem_ptr, 512);
   }
 }
 
 // ---------------------------------------------------------------- row statistics
-// One block per tile of 128 query rows of a head: -LSE log2(e) and dLSE - dO . O for each row.
+// One block per tile of 128 rows of a query plane: -LSE log2(e) and dLSE - dO . O for each row.
 // Rows past the end, and rows whose LSE is -inf (no key is seen), get -inf and P = 0.  Bound by
 // reading dO and O once; D / 8 lanes of 16 bytes take a row.
 template <int D, bool VARLEN>
 __global__ void __launch_bounds__(256)
     attn_bwd_rows_kernel(const __nv_bfloat16* dout, const __nv_bfloat16* o, const float* lse, const float* dlse, float* stats,
-                         unsigned int* counters, int B, int H, int Sq, int stat_tiles, const int32_t* cu_q) {
+                         unsigned int* counters, int B, int H, int Sq, int lg, int stat_tiles, const int32_t* cu_q) {
   constexpr int LPR = D / 8, RPP = 256 / LPR;  // lanes per row, rows per pass of the block
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;");
@@ -819,23 +898,24 @@ __global__ void __launch_bounds__(256)
     int lo = 0, hi = B - 1;  // the last sequence that starts at this tile or before it
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
-      if (ragged_stat0(cu_q, mid) <= tile)
+      if (ragged_stat0(cu_q, mid, lg) <= tile)
         lo = mid;
       else
         hi = mid - 1;
     }
     qb = cu_q[lo];
     n = cu_q[lo + 1] - qb;
-    row0 = (tile - ragged_stat0(cu_q, lo)) * kTile;
-    if (row0 < 0 || row0 >= n) return;  // a tile of no sequence
+    row0 = (tile - ragged_stat0(cu_q, lo, lg)) * kTile;
+    if (row0 < 0 || row0 >= n << lg) return;  // a tile of no sequence
   }
   const int l = threadIdx.x % LPR;
   float* st = stats + static_cast<size_t>(blockIdx.x) * kStat;
 #pragma unroll 4
   for (int r = threadIdx.x / LPR; r < kTile; r += RPP) {
-    const int row = row0 + r;
-    const bool in = row < n;
-    const long long at = VARLEN ? static_cast<long long>(qb + row) * H + plane : static_cast<long long>(plane) * Sq + row;
+    const int query = (row0 + r) >> lg;
+    const long long head = (static_cast<long long>(plane) << lg) + ((row0 + r) & ((1 << lg) - 1));
+    const bool in = query < n;
+    const long long at = VARLEN ? static_cast<long long>(qb + query) * H + head : head * Sq + query;
     float a = 0.f;
     if (in) {
       const uint4 x = *reinterpret_cast<const uint4*>(dout + at * D + 8 * l);
@@ -849,7 +929,7 @@ __global__ void __launch_bounds__(256)
     if (l == 0) {
       float nl = -INFINITY, nd = 0.f;
       if (in) {
-        const long long i = VARLEN ? static_cast<long long>(plane) * Sq + qb + row : at;
+        const long long i = VARLEN ? head * Sq + qb + query : at;
         const float s = lse[i];
         nl = s == -INFINITY ? -INFINITY : -s * kLog2e;
         nd = (dlse ? dlse[i] : 0.f) - a;
@@ -894,6 +974,31 @@ bool make_map(CUtensorMap* map, const void* base, int D, long long rows, long lo
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Tiles of query planes of 2^lg heads: dense [planes, queries, heads, D] (innermost first D, heads,
+// queries, planes), packed tokens [queries, planes, heads, D] (D, heads, planes, queries).
+bool make_q_map(CUtensorMap* map, const void* base, int D, long long queries, long long planes, int lg, bool tokens) {
+  EncodeTiledFn enc = encode_fn();
+  if (!enc) return false;
+  const cuuint64_t row = static_cast<cuuint64_t>(D) * 2, nq = static_cast<cuuint64_t>(queries);
+  const cuuint64_t np = static_cast<cuuint64_t>(planes), heads = 1ull << lg;
+  cuuint64_t dims[4] = {static_cast<cuuint64_t>(D), heads, tokens ? np : nq, tokens ? nq : np};
+  cuuint64_t strides[3] = {tokens ? row : row * nq, tokens ? row << lg : row, tokens ? (row << lg) * np : (row << lg) * nq};
+  const cuuint32_t q = static_cast<cuuint32_t>(kTile >> lg);
+  cuuint32_t box[4] = {64, 1u << lg, tokens ? 1u : q, tokens ? q : 1u};
+  cuuint32_t estr[4] = {1, 1, 1, 1};
+  return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Planes whose tiles are dealt together: as many as have what they walk (bytes a plane) in L2 at
+// once, since the longest tiles of them all go first, but at least a round of CTAs.
+int planes_per_block(double bytes, int tiles, int sms, long long planes) {
+  const double fit = 48e6 / bytes;
+  const long long n = fit > planes ? planes : static_cast<long long>(fit), round = (sms + tiles - 1) / tiles;
+  return static_cast<int>(n < round ? round : n);
+}
+
 template <class Kernel, class... Args>
 cudaError_t launch(Kernel kernel, int grid, int threads, uint32_t smem, cudaStream_t stream, Args... args) {
   cudaLaunchConfig_t cfg = {};
@@ -923,17 +1028,18 @@ cudaError_t launch_d(const BwdArgs& a, const KernelCtl& ctl, cudaStream_t stream
       }))
     return cudaErrorInvalidValue;
   CUtensorMap mq, mdo, mk, mv;
-  const long long q_planes = VARLEN ? a.Hq : static_cast<long long>(a.B) * a.Hq;
+  const int lg = bwd_pack_log2(a.Hq / a.Hkv);
+  const long long q_planes = (VARLEN ? a.Hq : static_cast<long long>(a.B) * a.Hq) >> lg;
   const long long kv_planes = VARLEN ? a.Hkv : static_cast<long long>(a.B) * a.Hkv;
-  if (!make_map(&mq, a.q, D, a.Sq, q_planes, VARLEN) || !make_map(&mdo, a.dout, D, a.Sq, q_planes, VARLEN) ||
+  if (!make_q_map(&mq, a.q, D, a.Sq, q_planes, lg, VARLEN) || !make_q_map(&mdo, a.dout, D, a.Sq, q_planes, lg, VARLEN) ||
       !make_map(&mk, a.k, D, a.Skv, kv_planes, VARLEN) || !make_map(&mv, a.v, D, a.Skv, kv_planes, VARLEN))
     return cudaErrorInvalidValue;
-  const int stat_tiles = static_cast<int>(bwd_stat_tiles(a.B, a.Sq, VARLEN));
+  const int stat_tiles = static_cast<int>(bwd_stat_tiles(a.B, a.Sq, lg, VARLEN));
   unsigned int* counters = static_cast<unsigned int*>(a.workspace);
   float* stats = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + 256);
   e = launch(attn_bwd_rows_kernel<D, VARLEN>, static_cast<int>(q_planes * stat_tiles), 256, 0, stream,
              static_cast<const __nv_bfloat16*>(a.dout), static_cast<const __nv_bfloat16*>(a.o), a.lse, a.dlse, stats, counters,
-             a.B, a.Hq, a.Sq, stat_tiles, a.cu_q);
+             a.B, a.Hq, a.Sq, lg, stat_tiles, a.cu_q);
   if (e != cudaSuccess) return e;
   BwdParams p;
   memset(&p, 0, sizeof(p));
@@ -948,6 +1054,7 @@ cudaError_t launch_d(const BwdArgs& a, const KernelCtl& ctl, cudaStream_t stream
   p.Sq = a.Sq;
   p.Skv = a.Skv;
   p.causal = a.causal;
+  p.lg = lg;
   p.c = a.scale * kLog2e;
   p.scale = a.scale;
   p.stat_tiles = stat_tiles;
@@ -959,14 +1066,15 @@ cudaError_t launch_d(const BwdArgs& a, const KernelCtl& ctl, cudaStream_t stream
     p.total_q = a.Sq;
     p.total_k = a.Skv;
     items = static_cast<long long>(a.B) * (static_cast<long long>(a.Hkv) * ((a.max_k + kTile - 1) / kTile) +
-                                           static_cast<long long>(a.Hq) * ((a.max_q + kTile - 1) / kTile));
+                                           q_planes * (((static_cast<long long>(a.max_q) << lg) + kTile - 1) / kTile));
   } else {
-    p.q_tiles = (a.Sq + kTile - 1) / kTile;
+    p.q_tiles = static_cast<int>(((static_cast<long long>(a.Sq) << lg) + kTile - 1) / kTile);
     p.kv_tiles = (a.Skv + kTile - 1) / kTile;
     p.q_items = static_cast<int>(q_planes * p.q_tiles);
     p.kv_items = static_cast<int>(kv_planes * p.kv_tiles);
-    p.q_block = (sms + p.q_tiles - 1) / p.q_tiles;
-    p.kv_block = (sms + p.kv_tiles - 1) / p.kv_tiles;
+    const double row = 4.0 * D;  // a query's dO and Q, a key's K and V
+    p.kv_block = planes_per_block(row * a.Sq * (1 << lg), p.kv_tiles, sms, kv_planes);
+    p.q_block = planes_per_block(row * a.Skv / (a.Hq / a.Hkv >> lg), p.q_tiles, sms, q_planes);
     items = static_cast<long long>(p.q_items) + p.kv_items;
   }
   const int grid = static_cast<int>(items > 0 && items < sms ? items : sms);

@@ -21,14 +21,22 @@ struct BwdArgs {
   int max_q, max_k;            // ragged: they only bound the launch
 };
 
-// Rows of 128 queries per head that the workspace's row statistics have.
-inline long long bwd_stat_tiles(int B, long long Sq, bool ragged) {
-  return ragged ? Sq / 128 + B : (Sq + 127) / 128;
+// Query heads of a kv head whose rows make one plane, as a power of two: the largest that divides
+// the group, up to 32.
+inline int bwd_pack_log2(int G) {
+  int lg = 0;
+  while (lg < 5 && (G >> lg) % 2 == 0) ++lg;
+  return lg;
 }
-// Workspace: 256 bytes of counters, then 2 x 128 floats for each tile of 128 queries of each head.
-inline size_t bwd_workspace_bytes(int B, int Hq, long long Sq, bool ragged) {
-  const size_t planes = ragged ? static_cast<size_t>(Hq) : static_cast<size_t>(B) * Hq;
-  return 256 + planes * static_cast<size_t>(bwd_stat_tiles(B, Sq, ragged)) * 1024;
+// Tiles of 128 rows that a plane of 2^lg heads has in the workspace's row statistics.
+inline long long bwd_stat_tiles(int B, long long Sq, int lg, bool ragged) {
+  return ragged ? (Sq << lg) / 128 + B : ((Sq << lg) + 127) / 128;
+}
+// Workspace: 256 bytes of counters, then 2 x 128 floats for each tile of 128 rows of each plane.
+inline size_t bwd_workspace_bytes(int B, int Hq, int Hkv, long long Sq, bool ragged) {
+  const int lg = bwd_pack_log2(Hq / Hkv);
+  const size_t planes = (ragged ? static_cast<size_t>(Hq) : static_cast<size_t>(B) * Hq) >> lg;
+  return 256 + planes * static_cast<size_t>(bwd_stat_tiles(B, Sq, lg, ragged)) * 1024;
 }
 
 cudaError_t launch_attn_bwd(const BwdArgs& a, const KernelCtl& ctl, cudaStream_t stream);

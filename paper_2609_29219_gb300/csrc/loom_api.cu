@@ -334,9 +334,11 @@ bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0
 
 // Sizes of a backward call that have a workspace: items and row statistics within 32 bits.
 bool bwd_sizes_fit(int B, int Hq, int Hkv, long long Sq, long long Skv, bool ragged) {
-  const long long q_planes = ragged ? Hq : static_cast<long long>(B) * Hq;
+  const int lg = bwd_pack_log2(Hq / Hkv);
+  const long long heads = ragged ? Hq : static_cast<long long>(B) * Hq;
   const long long kv_planes = ragged ? Hkv : static_cast<long long>(B) * Hkv;
-  return q_planes <= 0x7fffffffLL && q_planes * bwd_stat_tiles(B, Sq, ragged) <= 0x3fffffffLL &&
+  return heads <= 0x7fffffffLL && Sq << lg <= 0x3fffffffLL && Skv <= 0x3fffffffLL &&
+         (heads >> lg) * bwd_stat_tiles(B, Sq, lg, ragged) <= 0x3fffffffLL &&
          kv_planes * (Skv / 128 + (ragged ? B : 1)) <= 0x3fffffffLL;
 }
 
@@ -359,7 +361,7 @@ loom_status bwd_call(const BwdArgs& a, size_t workspace_bytes, void* stream) {
     if (e == cudaSuccess && a.Skv > 0) e = cudaMemsetAsync(a.dv, 0, row * a.Hkv * a.Skv, s);
     return e == cudaSuccess ? LOOM_OK : LOOM_ERR_CUDA;
   }
-  if (!a.workspace || workspace_bytes < bwd_workspace_bytes(a.B, a.Hq, a.Sq, ragged)) return LOOM_ERR_WORKSPACE;
+  if (!a.workspace || workspace_bytes < bwd_workspace_bytes(a.B, a.Hq, a.Hkv, a.Sq, ragged)) return LOOM_ERR_WORKSPACE;
   if (!aligned16(a.workspace)) return LOOM_ERR_MISALIGNED;
   KernelCtl ctl;
   if (!make_ctl(&ctl)) return LOOM_ERR_CUDA;
@@ -369,12 +371,12 @@ loom_status bwd_call(const BwdArgs& a, size_t workspace_bytes, void* stream) {
 
 size_t loom_attn_bwd_workspace_bytes(int B, int Hq, int Hkv, int Sq, int Skv, int D) {
   if (B <= 0 || Hq <= 0 || Hkv <= 0 || Sq <= 0 || Skv <= 0 || Hq % Hkv || (D != 64 && D != 128)) return 0;
-  return bwd_sizes_fit(B, Hq, Hkv, Sq, Skv, false) ? bwd_workspace_bytes(B, Hq, Sq, false) : 0;
+  return bwd_sizes_fit(B, Hq, Hkv, Sq, Skv, false) ? bwd_workspace_bytes(B, Hq, Hkv, Sq, false) : 0;
 }
 
 size_t loom_attn_bwd_varlen_workspace_bytes(int B, int Hq, int Hkv, int total_q, int total_k, int D) {
   if (B <= 0 || Hq <= 0 || Hkv <= 0 || total_q < 0 || total_k < 0 || Hq % Hkv || (D != 64 && D != 128)) return 0;
-  return bwd_sizes_fit(B, Hq, Hkv, total_q, total_k, true) ? bwd_workspace_bytes(B, Hq, total_q, true) : 0;
+  return bwd_sizes_fit(B, Hq, Hkv, total_q, total_k, true) ? bwd_workspace_bytes(B, Hq, Hkv, total_q, true) : 0;
 }
 
 loom_status loom_attn_bwd(const void* dout, const void* q, const void* k, const void* v, const void* o, const float* lse,
