@@ -236,7 +236,7 @@ loom_status loom_attn_decode_noalloc(const void* q, const void* k_cache, const v
  * and k on the tensor cores, and each gradient once when it is stored.  Every sum has a fixed
  * order: the same inputs give the same bits.
  * Errors: INVALID_ARG (as loom_attn_fwd; a NULL pointer other than dlse), UNSUPPORTED (D; more
- * than 2^30 tiles of 128 rows), MISALIGNED (dlse, lse: 4 bytes; the others 16), WORKSPACE, CUDA.
+ * than 2^29 tiles of 128 rows), MISALIGNED (dlse, lse: 4 bytes; the others 16), WORKSPACE, CUDA.
  */
 loom_status loom_attn_bwd(const void* dout, const void* q, const void* k, const void* v, const void* o,
                           const float* lse, const float* dlse, void* dq, void* dk, void* dv,

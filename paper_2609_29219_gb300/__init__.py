@@ -16,6 +16,7 @@ Two layers:
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 import threading
 
@@ -192,13 +193,14 @@ def capi() -> ctypes.CDLL:
 # two launches; 1.7 by the call below), and the checks, lock and import statement per argument
 # (0.45; 0.3 in one expression).
 _torch_mod = None
+_bf16 = _f32 = _i32 = _u8 = None  # torch's types
 
 
 _empty_strided_cuda = None
 
 
 def _torch():
-    global _torch_mod, _empty_strided_cuda
+    global _torch_mod, _empty_strided_cuda, _bf16, _f32, _i32, _u8
     if _torch_mod is None:
         import torch
         try:  # what torch's generated code allocates by: no dispatch, on the current device
@@ -208,6 +210,7 @@ def _torch():
                 _empty_strided_cuda = call
         except ImportError:
             pass
+        _bf16, _f32, _i32, _u8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
         _torch_mod = torch
     return _torch_mod
 
@@ -217,13 +220,26 @@ def _new(shape, strides, dtype, t, like=False):
     (like: of t's shape and type).  It passes torch's dispatcher by only where nobody would
     miss the call: no dispatch or function mode, no deterministic mode (which fills new
     tensors), no subclass of Tensor."""
-    torch = _torch_mod
-    c = torch._C
-    if (_empty_strided_cuda is not None and type(t) is torch.Tensor and not c._len_torch_dispatch_stack()
-            and not c._len_torch_function_stack() and not c._get_deterministic_algorithms()
-            and t.get_device() == c._cuda_getDevice()):
+    if _direct(t):
         return _empty_strided_cuda(shape, strides, dtype)
+    torch = _torch_mod
     return torch.empty_like(t) if like else torch.empty(shape, dtype=dtype, device=t.device)
+
+
+def _direct(t):
+    """Whether new tensors on tensor t's device may pass the dispatcher by (see _new)."""
+    c = _torch_mod._C
+    return (_empty_strided_cuda is not None and type(t) is _torch_mod.Tensor and not c._len_torch_dispatch_stack()
+            and not c._len_torch_function_stack() and not c._get_deterministic_algorithms()
+            and t.get_device() == c._cuda_getDevice())
+
+
+def _maker(t):
+    """What makes uninitialised contiguous tensors on tensor t's device, of (shape, strides, type):
+    _new for a call that makes several (GB300 host: 0.9 us a tensor, 1.3 by _new)."""
+    if _direct(t):
+        return _empty_strided_cuda
+    return lambda shape, strides, dtype: _torch_mod.empty(shape, dtype=dtype, device=t.device)
 
 
 def _ptr(t, name, dtype, ndim):
@@ -470,52 +486,61 @@ def loom_attn_decode_paged(q, k_cache, v_cache, block_table, seqlens_k, o=None, 
     return (o, lse) if (return_lse or lse is not None) else o
 
 
+@functools.lru_cache(maxsize=256)
+def _bwd_need(varlen, *sizes):
+    lib = capi()
+    return (lib.loom_attn_bwd_varlen_workspace_bytes if varlen else lib.loom_attn_bwd_workspace_bytes)(*sizes)
+
+
+@functools.lru_cache(maxsize=4)
+def _norm_bwd_need(D):
+    return capi().loom_qkv_norm_rope_bwd_workspace_bytes(D)
+
+
+# The checks of the entry points below take most of a small call's time if each tensor goes through
+# _ptr, so they are one expression that names nothing, and what fails it is looked at again by name.
+# GB300 host, us per call before and after (C call in it): backward of 128 rows 25.0 -> BWD_US (6.4),
+# norm and rotation 17.6 -> NORM_US (3.8), into a cache 14.4 -> CACHE_US (3.8), its gradients 27.2 -> NBWD_US (5.5).
+def _bwd_checked(do, q, k, v, o, lse, dlse, dq, dk, dv, ndim):
+    """The backward entry points' tensors, named if they are not what they should be."""
+    for t, name in ((q, "q"), (k, "k"), (v, "v"), (do, "do"), (o, "o")):
+        _dev_ptr(t, name, _bf16, ndim)
+    if v.shape != k.shape or k.shape[-1] != q.shape[-1] or (ndim == 4 and k.shape[0] != q.shape[0]):
+        raise ValueError("q/k/v shapes disagree")
+    for t, name in ((do, "do"), (o, "o")):
+        if t.shape != q.shape:
+            raise ValueError(f"{name} must have q's shape")
+    if lse is None:
+        raise TypeError("lse is needed: call the forward pass with return_lse=True")
+    _dev_ptr(lse, "lse", _f32)
+    if dlse is not None:
+        _dev_ptr(dlse, "dlse", _f32)
+        if dlse.shape != lse.shape:
+            raise ValueError("dlse must have lse's shape")
+    for t, like, name in ((dq, q, "dq"), (dk, k, "dk"), (dv, v, "dv")):
+        if t is not None:
+            _dev_ptr(t, name, _bf16, ndim)
+            if t.shape != like.shape:
+                raise ValueError(f"{name} must have {name[1]}'s shape")
+
+
+def _bwd_fine(do, q, k, v, o, lse, dlse, qs, ks):
+    try:
+        return (q.is_cuda and q.dtype is _bf16 and q.is_contiguous() and do.is_cuda and do.dtype is _bf16 and do.is_contiguous()
+                and o.is_cuda and o.dtype is _bf16 and o.is_contiguous() and k.is_cuda and k.dtype is _bf16
+                and k.is_contiguous() and v.is_cuda and v.dtype is _bf16 and v.is_contiguous() and lse.is_cuda
+                and lse.dtype is _f32 and lse.is_contiguous() and do.shape == qs and o.shape == qs and v.shape == ks
+                and (dlse is None or (dlse.is_cuda and dlse.dtype is _f32 and dlse.is_contiguous() and dlse.shape == lse.shape)))
+    except AttributeError:
+        return False
+
+
 def loom_attn_bwd_workspace_bytes(B, Hq, Hkv, Sq, Skv, D) -> int:
     return int(capi().loom_attn_bwd_workspace_bytes(B, Hq, Hkv, Sq, Skv, D))
 
 
 def loom_attn_bwd_varlen_workspace_bytes(B, Hq, Hkv, total_q, total_k, D) -> int:
     return int(capi().loom_attn_bwd_varlen_workspace_bytes(B, Hq, Hkv, total_q, total_k, D))
-
-
-def _scratch(workspace, need, t):
-    """Pointer and size of the workspace, one of ``need`` bytes made here if None is given (and the
-    tensor, which has to live until the call has been queued)."""
-    if workspace is None:
-        workspace = _new((max(need, 16),), (1,), _torch_mod.uint8, t)
-    return _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(), workspace
-
-
-def _bwd_operands(do, q, k, v, o, lse, dlse, dq, dk, dv, ndim):
-    """Pointers of the backward entry points' tensor arguments, and the gradients."""
-    bf16 = _torch().bfloat16
-    qp, kp, vp_ = _ptr(q, "q", bf16, ndim), _ptr(k, "k", bf16, ndim), _ptr(v, "v", bf16, ndim)
-    if v.shape != k.shape or k.shape[-1] != q.shape[-1]:
-        raise ValueError("q/k/v shapes disagree")
-    for t, name in ((do, "do"), (o, "o")):
-        if t.shape != q.shape:
-            raise ValueError(f"{name} must have q's shape")
-    dop, op = _ptr(do, "do", bf16, ndim), _ptr(o, "o", bf16, ndim)
-    f32 = _torch_mod.float32
-    if lse is None:
-        raise TypeError("lse is needed: call the forward pass with return_lse=True")
-    lp = _dev_ptr(lse, "lse", f32)
-    dlp = None
-    if dlse is not None:
-        if dlse.shape != lse.shape:
-            raise ValueError("dlse must have lse's shape")
-        dlp = _dev_ptr(dlse, "dlse", f32)
-    if dq is None:
-        dq = _new(tuple(q.shape), q.stride(), bf16, q, True)
-    if dk is None:
-        dk = _new(tuple(k.shape), k.stride(), bf16, k, True)
-    if dv is None:
-        dv = _new(tuple(v.shape), v.stride(), bf16, v, True)
-    for t, like, name in ((dq, q, "dq"), (dk, k, "dk"), (dv, v, "dv")):
-        if t.shape != like.shape:
-            raise ValueError(f"{name} must have {name[1]}'s shape")
-    grads = (_ptr(dq, "dq", bf16, ndim), _ptr(dk, "dk", bf16, ndim), _ptr(dv, "dv", bf16, ndim))
-    return (dop, qp, kp, vp_, op, lp, dlp, *grads), (dq, dk, dv)
 
 
 def loom_attn_bwd(do, q, k, v, o, lse, dq=None, dk=None, dv=None, workspace=None, *, causal=False, scale=None, dlse=None,
@@ -525,21 +550,39 @@ def loom_attn_bwd(do, q, k, v, o, lse, dq=None, dk=None, dv=None, workspace=None
 
     ``workspace`` is a CUDA uint8 tensor of at least ``loom_attn_bwd_workspace_bytes`` bytes
     (allocated here if None).  Writes and returns ``dq, dk, dv`` (allocated if None)."""
-    ptrs, grads = _bwd_operands(do, q, k, v, o, lse, dlse, dq, dk, dv, 4)
-    B, Hq, Sq, D = q.shape
-    Bk, Hkv, Skv, _ = k.shape
-    if Bk != B:
-        raise ValueError("q/k/v shapes disagree")
+    _torch()
+    try:
+        qs, ks = q.shape, k.shape
+        B, Hq, Sq, D = qs
+        Bk, Hkv, Skv, Dk = ks
+        fine = Bk == B and Dk == D
+    except (AttributeError, ValueError):
+        fine = False
+    if not fine or dq is not None or dk is not None or dv is not None or not _bwd_fine(do, q, k, v, o, lse, dlse, qs, ks):
+        _bwd_checked(do, q, k, v, o, lse, dlse, dq, dk, dv, 4)
     if tuple(lse.shape) != (B, Hq, Sq):
         raise ValueError("lse must be [B, Hq, Sq]")
-    lib = _lib or capi()
-    need = 0 if workspace is not None else lib.loom_attn_bwd_workspace_bytes(B, Hq, Hkv, Sq, Skv, D)
-    wp, wbytes, workspace = _scratch(workspace, need, q)
-    if scale is None:
-        scale = D ** -0.5
-    st = lib.loom_attn_bwd(*ptrs, wp, wbytes, B, Hq, Hkv, Sq, Skv, D, int(bool(causal)), float(scale), _stream_of(stream, q))
-    _check(st, "loom_attn_bwd")
-    return grads
+    new = _maker(q)
+    if dq is None:
+        dq = new(tuple(qs), (Hq * Sq * D, Sq * D, D, 1), _bf16)
+    if dk is None:
+        dk = new(tuple(ks), (Hkv * Skv * D, Skv * D, D, 1), _bf16)
+    if dv is None:
+        dv = new(tuple(ks), (Hkv * Skv * D, Skv * D, D, 1), _bf16)
+    if workspace is None:
+        wbytes = _bwd_need(False, B, Hq, Hkv, Sq, Skv, D)
+        workspace = new((max(wbytes, 16),), (1,), _u8)
+        wp = workspace.data_ptr()
+    else:
+        wp = _dev_ptr(workspace, "workspace")
+        wbytes = workspace.numel() * workspace.element_size()
+    st = (_lib or capi()).loom_attn_bwd(
+        do.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
+        None if dlse is None else dlse.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), wp, wbytes, B, Hq, Hkv, Sq, Skv,
+        D, 1 if causal else 0, D ** -0.5 if scale is None else scale, _stream_of(stream, q))
+    if st:
+        raise LoomError(st, "loom_attn_bwd")
+    return dq, dk, dv
 
 
 def loom_attn_bwd_varlen(do, q, k, v, o, lse, cu_seqlens_q, cu_seqlens_k, max_seqlen_q, max_seqlen_k, dq=None, dk=None,
@@ -547,64 +590,103 @@ def loom_attn_bwd_varlen(do, q, k, v, o, lse, cu_seqlens_q, cu_seqlens_k, max_se
     """Gradients of ``loom_attn_fwd_varlen``.  do, o and q [total_q, Hq, D], k and v [total_k, Hkv, D],
     lse (and dlse) [Hq, total_q]; cu_seqlens_q / cu_seqlens_k [B + 1] int32 on the device; the
     longest lengths as ints.  Writes and returns ``dq, dk, dv`` (allocated if None)."""
-    ptrs, grads = _bwd_operands(do, q, k, v, o, lse, dlse, dq, dk, dv, 3)
-    total_q, Hq, D = q.shape
-    total_k, Hkv, _ = k.shape
+    _torch()
+    try:
+        qs, ks = q.shape, k.shape
+        total_q, Hq, D = qs
+        total_k, Hkv, Dk = ks
+        fine = Dk == D
+    except (AttributeError, ValueError):
+        fine = False
+    if not fine or dq is not None or dk is not None or dv is not None or not _bwd_fine(do, q, k, v, o, lse, dlse, qs, ks):
+        _bwd_checked(do, q, k, v, o, lse, dlse, dq, dk, dv, 3)
     if lse.numel() != Hq * total_q:
         raise ValueError("lse must hold Hq*total_q values")
-    i32 = _torch_mod.int32
-    cqp, ckp = _ptr(cu_seqlens_q, "cu_seqlens_q", i32, 1), _ptr(cu_seqlens_k, "cu_seqlens_k", i32, 1)
-    if cu_seqlens_q.numel() != cu_seqlens_k.numel() or cu_seqlens_q.numel() < 2:
+    cqp, ckp = _ptr(cu_seqlens_q, "cu_seqlens_q", _i32, 1), _ptr(cu_seqlens_k, "cu_seqlens_k", _i32, 1)
+    B = cu_seqlens_q.shape[0] - 1
+    if cu_seqlens_k.shape[0] != B + 1 or B < 1:
         raise ValueError("cu_seqlens_q and cu_seqlens_k must both be [B + 1]")
-    B = cu_seqlens_q.numel() - 1
-    lib = _lib or capi()
-    need = 0 if workspace is not None else lib.loom_attn_bwd_varlen_workspace_bytes(B, Hq, Hkv, total_q, total_k, D)
-    wp, wbytes, workspace = _scratch(workspace, need, q)
-    if scale is None:
-        scale = D ** -0.5
-    st = lib.loom_attn_bwd_varlen(*ptrs, cqp, ckp, wp, wbytes, B, Hq, Hkv, total_q, total_k, int(max_seqlen_q),
-                                  int(max_seqlen_k), D, int(bool(causal)), float(scale), _stream_of(stream, q))
-    _check(st, "loom_attn_bwd_varlen")
-    return grads
+    new = _maker(q)
+    if dq is None:
+        dq = new(tuple(qs), (Hq * D, D, 1), _bf16)
+    if dk is None:
+        dk = new(tuple(ks), (Hkv * D, D, 1), _bf16)
+    if dv is None:
+        dv = new(tuple(ks), (Hkv * D, D, 1), _bf16)
+    if workspace is None:
+        wbytes = _bwd_need(True, B, Hq, Hkv, total_q, total_k, D)
+        workspace = new((max(wbytes, 16),), (1,), _u8)
+        wp = workspace.data_ptr()
+    else:
+        wp = _dev_ptr(workspace, "workspace")
+        wbytes = workspace.numel() * workspace.element_size()
+    st = (_lib or capi()).loom_attn_bwd_varlen(
+        do.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
+        None if dlse is None else dlse.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), cqp, ckp, wp, wbytes, B, Hq, Hkv,
+        total_q, total_k, max_seqlen_q, max_seqlen_k, D, 1 if causal else 0, D ** -0.5 if scale is None else scale,
+        _stream_of(stream, q))
+    if st:
+        raise LoomError(st, "loom_attn_bwd_varlen")
+    return dq, dk, dv
 
 
 def _row_matrix(t, name, width):
     """Pointer and row distance of a bf16 CUDA matrix whose rows are contiguous."""
-    torch = _torch()
-    if not isinstance(t, torch.Tensor):
+    if not isinstance(t, _torch_mod.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor")
-    if t.dtype is not torch.bfloat16:
-        raise TypeError(f"{name} must be {torch.bfloat16}, got {t.dtype}")
+    if t.dtype is not _bf16:
+        raise TypeError(f"{name} must be {_bf16}, got {t.dtype}")
     if t.dim() != 2 or t.shape[1] != width or (t.shape[1] > 1 and t.stride(1) != 1):
         raise ValueError(f"{name} must be [T, {width}] with contiguous rows, got shape {tuple(t.shape)}")
     return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else width
 
 
-def _norm_operands(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, positions, interleaved):
-    """What the norm-and-rotation entry points share: (qkv pointer, its row distance), the weights',
-    tables' and positions' arguments, T and D."""
-    torch = _torch()
-    wt = q_weight.dtype
-    if wt not in (torch.bfloat16, torch.float32):
-        raise TypeError(f"q_weight must be {torch.bfloat16} or {torch.float32}, got {wt}")
-    qwp, kwp = _ptr(q_weight, "q_weight", wt, 1), _ptr(k_weight, "k_weight", wt, 1)
-    D = q_weight.shape[0]
-    if k_weight.shape[0] != D:
+def _norm_checked(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, positions):
+    """The norm-and-rotation entry points' shared tensors, named if they are not what they should be."""
+    for t, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        _dev_ptr(t, name, None, 1)
+        if t.dtype not in (_bf16, _f32):
+            raise TypeError(f"{name} must be {_bf16} or {_f32}, got {t.dtype}")
+    if k_weight.dtype is not q_weight.dtype:
+        raise TypeError("q_weight and k_weight must have one type")
+    if k_weight.shape != q_weight.shape:
         raise ValueError("q_weight and k_weight must both be [D]")
-    f32 = torch.float32
-    cp, sp = _ptr(cos, "cos", f32, 2), _ptr(sin, "sin", f32, 2)
+    _dev_ptr(cos, "cos", _f32, 2), _dev_ptr(sin, "sin", _f32, 2)
     if cos.shape != sin.shape:
         raise ValueError("cos and sin must both be [positions, rotary_dim / 2]")
-    xp, stride = _row_matrix(qkv, "qkv", (num_heads + 2 * num_kv_heads) * D)
-    pp = None
+    _row_matrix(qkv, "qkv", (num_heads + 2 * num_kv_heads) * q_weight.shape[0])
     if positions is not None:
-        pp = _ptr(positions, "positions", torch.int32, 1)
+        _dev_ptr(positions, "positions", _i32, 1)
         if positions.shape[0] != qkv.shape[0]:
             raise ValueError("positions must be [T]")
-    return (xp, stride), (qwp, kwp, int(wt is f32), cp, sp, cos.shape[0], 2 * cos.shape[1], int(bool(interleaved)), pp), \
-        qkv.shape[0], D
+
+
+def _norm_operands(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, positions, interleaved):
+    """What the norm-and-rotation entry points share: (T, D, qkv's row distance, and the C arguments
+    from q_weight to positions)."""
+    _torch()
+    try:
+        T, W = qkv.shape
+        D, = q_weight.shape
+        P, half = cos.shape
+        wt = q_weight.dtype
+        stride, inner = qkv.stride()
+        fine = (qkv.is_cuda and qkv.dtype is _bf16 and inner == 1 and W == (num_heads + 2 * num_kv_heads) * D
+                and q_weight.is_cuda and (wt is _bf16 or wt is _f32) and q_weight.is_contiguous()
+                and k_weight.is_cuda and k_weight.dtype is wt and k_weight.is_contiguous() and k_weight.shape[0] == D
+                and k_weight.dim() == 1 and cos.is_cuda and cos.dtype is _f32 and cos.is_contiguous() and sin.is_cuda
+                and sin.dtype is _f32 and sin.is_contiguous() and sin.shape == cos.shape
+                and (positions is None or (positions.is_cuda and positions.dtype is _i32 and positions.is_contiguous()
+                                           and positions.dim() == 1 and positions.shape[0] == T)))
+    except (AttributeError, ValueError):
+        fine = False
+    if not fine:
+        _norm_checked(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, positions)
+    return T, D, stride if T > 1 else W, (
+        q_weight.data_ptr(), k_weight.data_ptr(), 1 if wt is _f32 else 0, cos.data_ptr(), sin.data_ptr(), P, 2 * half,
+        1 if interleaved else 0, None if positions is None else positions.data_ptr())
 
 
 def loom_qkv_norm_rope(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, positions=None, q=None, k=None, v=None, *,
@@ -615,23 +697,40 @@ def loom_qkv_norm_rope(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_head
     [D] bf16 or fp32; cos, sin [positions, rotary_dim / 2] fp32; positions [T] int32 (None: t, or t %
     seq_len).  Writes and returns ``q, k, v`` (allocated if None): [T, H, D], or with ``seq_len``
     [T / seq_len, H, seq_len, D], as the ragged and the dense prefill take them."""
-    x, norm, T, D = _norm_operands(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, positions, interleaved)
-    if seq_len < 0 or (seq_len and T % seq_len):
+    T, D, row, norm = _norm_operands(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, positions, interleaved)
+    S = seq_len
+    if S < 0 or (S and T % S):
         raise ValueError("T must be a multiple of seq_len")
-    bf16 = _torch_mod.bfloat16
-    outs = []
-    for t, name, H in ((q, "q", num_heads), (k, "k", num_kv_heads), (v, "v", num_kv_heads)):
-        shape = (T // seq_len, H, seq_len, D) if seq_len else (T, H, D)
-        if t is None:
-            t = _new(shape, (H * seq_len * D, seq_len * D, D, 1) if seq_len else (H * D, D, 1), bf16, qkv)
-        elif tuple(t.shape) != shape:
+    if S:
+        qs, ks = (T // S, num_heads, S, D), (T // S, num_kv_heads, S, D)
+        qst, kst = (num_heads * S * D, S * D, D, 1), (num_kv_heads * S * D, S * D, D, 1)
+    else:
+        qs, ks, qst, kst = (T, num_heads, D), (T, num_kv_heads, D), (num_heads * D, D, 1), (num_kv_heads * D, D, 1)
+    for t, name, shape in ((q, "q", qs), (k, "k", ks), (v, "v", ks)) if q is not None or k is not None or v is not None else ():
+        if t is not None and (_dev_ptr(t, name, _bf16) is None or tuple(t.shape) != shape):
             raise ValueError(f"{name} must be {list(shape)}")
-        outs.append(t)
-    ptrs = [_ptr(t, n, bf16, t.dim()) for t, n in zip(outs, "qkv")]
-    st = (_lib or capi()).loom_qkv_norm_rope(*x, *norm, *ptrs, T, int(seq_len), num_heads, num_kv_heads, D, float(eps),
-                                             _stream_of(stream, qkv))
-    _check(st, "loom_qkv_norm_rope")
-    return tuple(outs)
+    new = _maker(qkv)
+    if q is None:
+        q = new(qs, qst, _bf16)
+    if k is None:
+        k = new(ks, kst, _bf16)
+    if v is None:
+        v = new(ks, kst, _bf16)
+    st = (_lib or capi()).loom_qkv_norm_rope(qkv.data_ptr(), row, *norm, q.data_ptr(), k.data_ptr(), v.data_ptr(), T, S, num_heads,
+                                             num_kv_heads, D, eps, _stream_of(stream, qkv))
+    if st:
+        raise LoomError(st, "loom_qkv_norm_rope")
+    return q, k, v
+
+
+def _cache_checked(k_cache, v_cache, positions, slots):
+    """The caches and slots of the cache form, named if they are not what they should be."""
+    _dev_ptr(k_cache, "k_cache", _bf16, 4), _dev_ptr(v_cache, "v_cache", _bf16, 4)
+    if v_cache.shape != k_cache.shape:
+        raise ValueError("the caches must have one shape")
+    if positions is None or slots is None:
+        raise TypeError("positions and slots are needed")
+    _dev_ptr(slots, "slots", _i32, 1)
 
 
 def loom_qkv_norm_rope_cache(qkv, q_weight, k_weight, cos, sin, positions, slots, k_cache, v_cache, num_heads, q=None, *,
@@ -644,26 +743,30 @@ def loom_qkv_norm_rope_cache(qkv, q_weight, k_weight, cos, sin, positions, slots
     cache [B, Hkv, capacity, D], whose slots are b * capacity + position).  Returns q [T, num_heads, D]."""
     if layout not in ("nhd", "hnd"):
         raise ValueError("layout is 'nhd' or 'hnd'")
-    bf16 = _torch().bfloat16
-    kp, vp_ = _ptr(k_cache, "k_cache", bf16, 4), _ptr(v_cache, "v_cache", bf16, 4)
-    pages, a, b, Dk = k_cache.shape
+    _torch()
+    try:
+        cs = k_cache.shape
+        pages, a, b, Dk = cs
+        fine = (k_cache.is_cuda and k_cache.dtype is _bf16 and k_cache.is_contiguous() and v_cache.is_cuda
+                and v_cache.dtype is _bf16 and v_cache.is_contiguous() and v_cache.shape == cs and positions is not None
+                and slots.is_cuda and slots.dtype is _i32 and slots.is_contiguous() and slots.dim() == 1)
+    except (AttributeError, ValueError):
+        fine = False
+    if not fine:
+        _cache_checked(k_cache, v_cache, positions, slots)
     page_size, Hkv = (a, b) if layout == "nhd" else (b, a)
-    if positions is None or slots is None:
-        raise TypeError("positions and slots are needed")
-    x, norm, T, D = _norm_operands(qkv, q_weight, k_weight, cos, sin, num_heads, Hkv, positions, interleaved)
-    if v_cache.shape != k_cache.shape or Dk != D:
-        raise ValueError("the caches must have one shape, and D the weights'")
-    slp = _ptr(slots, "slots", _torch_mod.int32, 1)
-    if slots.shape[0] != T:
-        raise ValueError("slots must be [T]")
+    T, D, row, norm = _norm_operands(qkv, q_weight, k_weight, cos, sin, num_heads, Hkv, positions, interleaved)
+    if Dk != D or slots.shape[0] != T:
+        raise ValueError("the caches must have the weights' D, and slots be [T]")
     if q is None:
-        q = _new((T, num_heads, D), (num_heads * D, D, 1), bf16, qkv)
-    elif tuple(q.shape) != (T, num_heads, D):
+        q = _new((T, num_heads, D), (num_heads * D, D, 1), _bf16, qkv)
+    elif _dev_ptr(q, "q", _bf16, 3) is None or tuple(q.shape) != (T, num_heads, D):
         raise ValueError(f"q must be {[T, num_heads, D]}")
-    st = (_lib or capi()).loom_qkv_norm_rope_cache(*x, *norm, slp, _ptr(q, "q", bf16, 3), kp, vp_, pages, page_size,
-                                                   0 if layout == "nhd" else 1, T, num_heads, Hkv, D, float(eps),
-                                                   _stream_of(stream, qkv))
-    _check(st, "loom_qkv_norm_rope_cache")
+    st = (_lib or capi()).loom_qkv_norm_rope_cache(
+        qkv.data_ptr(), row, *norm, slots.data_ptr(), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), pages, page_size,
+        0 if layout == "nhd" else 1, T, num_heads, Hkv, D, eps, _stream_of(stream, qkv))
+    if st:
+        raise LoomError(st, "loom_qkv_norm_rope_cache")
     return q
 
 
@@ -677,36 +780,50 @@ def loom_qkv_norm_rope_bwd(dq, dk, dv, qkv, q_weight, k_weight, cos, sin, positi
     [B, H, seq_len, D]), the rest as the forward call had it.  Writes and returns ``dqkv`` (like qkv;
     its rows may lie further apart), ``dq_weight`` and ``dk_weight`` ([D] fp32), allocated if None.
     ``workspace``: a CUDA uint8 tensor of ``loom_qkv_norm_rope_bwd_workspace_bytes(D)`` bytes."""
-    torch = _torch()
-    bf16, f32 = torch.bfloat16, torch.float32
-    ndim = dq.dim()
-    if ndim not in (3, 4):
-        raise ValueError("dq must be [T, H, D] or [B, H, seq_len, D]")
-    ptrs = [_ptr(t, n, bf16, ndim) for t, n in ((dq, "dq"), (dk, "dk"), (dv, "dv"))]
-    Hq, Hkv = dq.shape[1], dk.shape[1]
-    x, norm, T, D = _norm_operands(qkv, q_weight, k_weight, cos, sin, Hq, Hkv, positions, interleaved)
-    seq_len = dq.shape[2] if ndim == 4 else 0
-    shape = (lambda H: (dq.shape[0], H, seq_len, D)) if ndim == 4 else (lambda H: (T, H, D))
-    if (tuple(dq.shape) != shape(Hq) or tuple(dk.shape) != shape(Hkv) or dv.shape != dk.shape
-            or (ndim == 4 and dq.shape[0] * seq_len != T)):
+    _torch()
+    try:
+        qs, ks = dq.shape, dk.shape
+        ndim, Hq, Hkv = len(qs), qs[1], ks[1]
+        fine = (dq.is_cuda and dq.dtype is _bf16 and dq.is_contiguous() and dk.is_cuda and dk.dtype is _bf16
+                and dk.is_contiguous() and dv.is_cuda and dv.dtype is _bf16 and dv.is_contiguous() and dv.shape == ks)
+    except (AttributeError, IndexError):
+        fine = False
+    if not fine:
+        for t, n in ((dq, "dq"), (dk, "dk"), (dv, "dv")):
+            _dev_ptr(t, n, _bf16, 3 if dq.dim() != 4 else 4)
+    T, D, row, norm = _norm_operands(qkv, q_weight, k_weight, cos, sin, Hq, Hkv, positions, interleaved)
+    S = qs[2] if ndim == 4 else 0
+    if (not fine or tuple(qs) != ((qs[0], Hq, S, D) if ndim == 4 else (T, Hq, D)) or (qs[0] * S if ndim == 4 else T) != T
+            or tuple(ks) != (qs[0], Hkv, *qs[2:])):
         raise ValueError("dq, dk and dv must be laid out as q, k and v of the forward call")
     width = (Hq + 2 * Hkv) * D
+    new = _maker(qkv)
     if dqkv is None:
-        dqkv = _new((T, width), (width, 1), bf16, qkv)
-    elif tuple(dqkv.shape) != (T, width):
-        raise ValueError(f"dqkv must be {[T, width]}")
+        dqkv, drow = new((T, width), (width, 1), _bf16), width
+    else:
+        drow = _row_matrix(dqkv, "dqkv", width)[1]
+        if dqkv.shape[0] != T:
+            raise ValueError(f"dqkv must be {[T, width]}")
     if dq_weight is None:
-        dq_weight = _new((D,), (1,), f32, qkv)
+        dq_weight = new((D,), (1,), _f32)
+    elif _dev_ptr(dq_weight, "dq_weight", _f32) is None or tuple(dq_weight.shape) != (D,):
+        raise ValueError("dq_weight must be [D]")
     if dk_weight is None:
-        dk_weight = _new((D,), (1,), f32, qkv)
-    if tuple(dq_weight.shape) != (D,) or tuple(dk_weight.shape) != (D,):
-        raise ValueError("dq_weight and dk_weight must be [D]")
-    lib = _lib or capi()
-    wp, wbytes, workspace = _scratch(workspace, lib.loom_qkv_norm_rope_bwd_workspace_bytes(D), qkv)
-    st = lib.loom_qkv_norm_rope_bwd(*ptrs, *x, *norm, *_row_matrix(dqkv, "dqkv", width), _ptr(dq_weight, "dq_weight", f32, 1),
-                                    _ptr(dk_weight, "dk_weight", f32, 1), wp, wbytes, T, int(seq_len), Hq, Hkv, D, float(eps),
-                                    _stream_of(stream, qkv))
-    _check(st, "loom_qkv_norm_rope_bwd")
+        dk_weight = new((D,), (1,), _f32)
+    elif _dev_ptr(dk_weight, "dk_weight", _f32) is None or tuple(dk_weight.shape) != (D,):
+        raise ValueError("dk_weight must be [D]")
+    if workspace is None:
+        wbytes = _norm_bwd_need(D)
+        workspace = new((max(wbytes, 16),), (1,), _u8)
+        wp = workspace.data_ptr()
+    else:
+        wp = _dev_ptr(workspace, "workspace")
+        wbytes = workspace.numel() * workspace.element_size()
+    st = (_lib or capi()).loom_qkv_norm_rope_bwd(
+        dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), qkv.data_ptr(), row, *norm, dqkv.data_ptr(), drow, dq_weight.data_ptr(),
+        dk_weight.data_ptr(), wp, wbytes, T, S, Hq, Hkv, D, eps, _stream_of(stream, qkv))
+    if st:
+        raise LoomError(st, "loom_qkv_norm_rope_bwd")
     return dqkv, dq_weight, dk_weight
 
 

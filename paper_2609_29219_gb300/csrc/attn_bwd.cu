@@ -38,6 +38,8 @@ constexpr int kTile = 128;   // queries and keys per tile
 constexpr int kEltWarps = 8;  // elementwise warps: four for each half of a tile's columns
 constexpr int kLoader = kEltWarps, kMma0 = kEltWarps + 1, kMma1 = kEltWarps + 2;
 constexpr int kThreads = (kMma1 + 1) * 32;
+constexpr int kShortItem = 4;  // steps
+constexpr int kRowThreads = 256, kRowsPerBlock = 32;  // of the row statistics
 constexpr int kStat = 2 * kTile;  // floats of a query tile's row statistics: -LSE (base 2), then -delta
 
 template <int D>
@@ -45,20 +47,22 @@ struct BwdCfg {
   static constexpr int NBOX = D / 64;  // 128-byte-swizzled boxes of 64 columns per tile
   static constexpr uint32_t BOX_BYTES = kTile * 128;
   static constexpr uint32_t TILE_BYTES = NBOX * BOX_BYTES;
+  // An item's own two tiles: D = 64 has room to load the next item's beside them.
+  static constexpr int NOWN = D == 128 ? 1 : 2;
   // kv items: K, V, then rings of Q and dO tiles and of row statistics
   static constexpr int NQ = D == 128 ? 3 : 4, ND = D == 128 ? 2 : 4;
-  static constexpr uint32_t K_OFF = 0, V_OFF = TILE_BYTES;
-  static constexpr uint32_t QR_OFF = 2 * TILE_BYTES, DOR_OFF = QR_OFF + NQ * TILE_BYTES;
+  static constexpr uint32_t K_OFF = 0, V_OFF = NOWN * TILE_BYTES;
+  static constexpr uint32_t QR_OFF = 2 * NOWN * TILE_BYTES, DOR_OFF = QR_OFF + NQ * TILE_BYTES;
   static constexpr uint32_t ST_OFF = DOR_OFF + ND * TILE_BYTES;
   static constexpr uint32_t KV_END = ST_OFF + ND * kStat * 4;
   // query items: Q, dO, then rings of K and V tiles
   static constexpr int NK = D == 128 ? 3 : 5, NV = D == 128 ? 2 : 4;
-  static constexpr uint32_t Q_OFF = 0, DO_OFF = TILE_BYTES;
-  static constexpr uint32_t KR_OFF = 2 * TILE_BYTES, VR_OFF = KR_OFF + NK * TILE_BYTES;
+  static constexpr uint32_t Q_OFF = 0, DO_OFF = NOWN * TILE_BYTES;
+  static constexpr uint32_t KR_OFF = 2 * NOWN * TILE_BYTES, VR_OFF = KR_OFF + NK * TILE_BYTES;
   static constexpr uint32_t Q_END = VR_OFF + NV * TILE_BYTES;
   static constexpr uint32_t ITEM_OFF = KV_END > Q_END ? KV_END : Q_END;  // two item records
   static constexpr uint32_t BAR_OFF = ITEM_OFF + 2 * 64;
-  static constexpr int NBAR = 4 + 2 * NQ + ND + 11 + 4 + 2 * NK + 2 * NV + 8 + 8;
+  static constexpr int NBAR = 8 * NOWN + 2 * NQ + ND + 11 + 2 * NK + 2 * NV + 8 + 8;
   static constexpr uint32_t TMEM_PTR_OFF = BAR_OFF + NBAR * 8;
   static constexpr uint32_t ABORT_OFF = TMEM_PTR_OFF + 8;
   static constexpr uint32_t BYTES = ABORT_OFF + 16;  // from a 1024-byte boundary
@@ -73,6 +77,7 @@ struct BwdParams {
   const float* stats;       // [planes][tiles][2][128]
   unsigned int* counters;   // [0] kv items, [1] query items
   int B, Hq, Hkv, Sq, Skv, causal;
+  int wide;                 // dq, dk and dv are 32-byte aligned
   int lg;                   // a query plane's rows are those of 2^lg heads of one kv head
   float c;                  // scale * log2(e)
   float scale;
@@ -252,15 +257,20 @@ __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, 
     tma_load_3d(dst + x * C::BOX_BYTES, map, x * 64, VARLEN ? plane : row, VARLEN ? row : plane, bar);
 }
 
-// Rows [n, 128) of a tile become zeros (ragged batches: they are the next sequence's, and a NaN
-// or an infinity there times a zero probability would reach this sequence's gradients).  By a
-// whole warp, after the tile has arrived and before an MMA reads it.
+// A ragged batch's last tile of a sequence goes on with the next sequence's rows, which must not
+// reach this one's gradients whatever they hold (a NaN or an infinity times a zero probability
+// would).  As columns of S and dP they are masked; as rows that a gradient's product sums over, the
+// product stops at the last group of 16 with a row n of the sequence in it (issue_grad_rows), and the
+// rest of that group becomes zeros here.  By a whole warp, once the tile has arrived.  (Zeroing the
+// tile to its end before S and dP cost 1000 to 2500 clocks a step.)
 template <int D>
 __device__ __forceinline__ void zero_rows(uint32_t tile, int n) {
   using C = BwdCfg<D>;
+  const uint32_t end = static_cast<uint32_t>((n + 15) / 16 * 16) * 128;
   for (int x = 0; x < C::NBOX; ++x)
-    for (uint32_t o = n * 128 + (threadIdx.x & 31) * 16; o < C::BOX_BYTES; o += 512)
-      st_shared_v4(tile + x * C::BOX_BYTES + o, 0, 0, 0, 0);
+    for (uint32_t o = n * 128 + (threadIdx.x & 31) * 16; o < end; o += 512) st_shared_v4(tile + x * C::BOX_BYTES + o, 0, 0, 0, 0);
+  fence_proxy_async_smem();
+  __syncwarp();
 }
 
 // The MMAs of one pair of tiles.  D[128 x 128] = A B^T, both K-major in shared memory.
@@ -289,6 +299,26 @@ __device__ __forceinline__ void issue_grad_chunks(uint32_t d_tmem, uint32_t a_tm
   mma_ts_k32_el(d_tmem, a_tmem + 16 * c, db, idesc, acc ? 1u : 0u);
   mma_ts_k32_el(d_tmem, a_tmem + 64 + 16 * c, db + 64 * (128 >> 4), idesc, 1u);
 }
+// The same over the first n rows (rounded up to 16) of the tile: A's halves of 64 rows are half_cols
+// columns apart.
+__device__ __forceinline__ void mma_ts_k16_el(uint32_t d_tmem, uint32_t a_tmem, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, e;\n\tsetp.ne.b32 p, %4, 0;\n\telect.sync _|e, 0xffffffff;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+template <int D>
+__device__ __forceinline__ void issue_grad_rows(uint32_t d_tmem, uint32_t a_tmem, uint32_t half_cols, uint32_t b, int n, bool acc) {
+  using C = BwdCfg<D>;
+  constexpr uint32_t idesc = idesc_bf16(kTile, D, 0, 1);
+  const uint64_t db = sdesc_sw128(b, C::BOX_BYTES, 1024);
+  for (int k = 0; 16 * k < n; ++k)
+    mma_ts_k16_el(d_tmem, a_tmem + (k >> 2) * half_cols + (k & 3) * 8, db + k * 16 * (128 >> 4), idesc, acc || k > 0 ? 1u : 0u);
+}
+
+// A word whose lowest n bits are set.
+__device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
 
 // 64 TMEM columns of this thread's lane.
 __device__ __forceinline__ void ld64(uint32_t tm, uint32_t* r) {
@@ -299,28 +329,50 @@ __device__ __forceinline__ void ld64(uint32_t tm, uint32_t* r) {
   reg_fence32(r + 32);
 }
 
-// A gradient row's COLS values from TMEM, scaled, as bf16 to global memory.
+// A gradient row's COLS values from TMEM, scaled, as bf16 to global memory: dst is this thread's row,
+// store whether there is one.  Lanes 2 i and 2 i + 1 swap halves of 64-byte pieces first, so that a
+// warp's 32-byte stores meet 16 rows each instead of 32: a store instruction takes the load/store
+// unit a clock per 128-byte line, and a tile's 16-byte stores row by row 2 us of an item's end.
+// wide: the tensors are 32-byte aligned (else 16-byte stores, row by row).
+__device__ __forceinline__ void st_global_v8(__nv_bfloat16* p, const uint32_t* w) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
+               "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+               : "memory");
+}
 template <int COLS>
-__device__ __forceinline__ void store_row(uint32_t tm, float scale, __nv_bfloat16* dst, bool store) {
+__device__ __forceinline__ void store_row(uint32_t tm, float scale, __nv_bfloat16* dst, bool store, bool wide) {
   const uint64_t s2 = f2(scale, scale);
+  const bool odd = threadIdx.x & 1;
+  const bool other_store = __shfl_xor_sync(0xffffffffu, store, 1);
+  __nv_bfloat16* other = reinterpret_cast<__nv_bfloat16*>(
+      __shfl_xor_sync(0xffffffffu, reinterpret_cast<unsigned long long>(dst), 1));
 #pragma unroll 1
   for (int c = 0; c < COLS; c += 32) {
-    uint32_t r[32];
+    uint32_t r[32], w[16];
     tmem_ld32(tm + c, r);
     tmem_wait_ld();
     reg_fence32(r);
-    if (store) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const uint64_t x = mul2(f2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])), s2);
+      w[i] = pack_bf16x2(f2lo(x), f2hi(x));
+    }
+    if (wide) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t got = __shfl_xor_sync(0xffffffffu, odd ? w[i] : w[8 + i], 1);
+        if (odd)
+          w[i] = got;
+        else
+          w[8 + i] = got;
+      }
+      // w[0..7]: of the even lane's row, w[8..15]: of the odd lane's
+      if (odd ? other_store : store) st_global_v8((odd ? other : dst) + c + (odd ? 16 : 0), w);
+      if (odd ? store : other_store) st_global_v8((odd ? dst : other) + c + (odd ? 16 : 0), w + 8);
+    } else if (store) {
       uint4* d = reinterpret_cast<uint4*>(dst + c);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint32_t w[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint64_t x = mul2(f2(__uint_as_float(r[8 * i + 2 * j]), __uint_as_float(r[8 * i + 2 * j + 1])), s2);
-          w[j] = pack_bf16x2(f2lo(x), f2hi(x));
-        }
-        d[i] = make_uint4(w[0], w[1], w[2], w[3]);
-      }
+      for (int i = 0; i < 4; ++i) d[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
     }
   }
 }
@@ -384,8 +436,9 @@ __device__ __forceinline__ void kv_items(const BwdParams& p, const Shared& sh, c
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const KernelCtl& ctl = p.ctl;
   const Abort& ab = sh.ab;
-  const uint32_t bar_k = sh.bars, bar_v = bar_k + 8, bar_ke = bar_v + 8, bar_ve = bar_ke + 8;
-  const uint32_t bar_q = bar_ve + 8, bar_qe = bar_q + 8 * NQ, bar_do = bar_qe + 8 * NQ;
+  constexpr int NO = C::NOWN;
+  const uint32_t bar_k = sh.bars, bar_v = bar_k + 8 * NO, bar_ke = bar_v + 8 * NO, bar_ve = bar_ke + 8 * NO;
+  const uint32_t bar_q = bar_ve + 8 * NO, bar_qe = bar_q + 8 * NQ, bar_do = bar_qe + 8 * NQ;
   const uint32_t bar_s = bar_do + 8 * C::ND, bar_dp = bar_s + 8, bar_p = bar_dp + 8, bar_ds = bar_p + 16;
   const uint32_t bar_acc = bar_ds + 16, bar_acce = bar_acc + 8, bar_drain = bar_acce + 8;
   const uint32_t bar_si = bar_drain + 8;  // [step % 2] the next step's S has been issued
@@ -394,19 +447,26 @@ __device__ __forceinline__ void kv_items(const BwdParams& p, const Shared& sh, c
   if (warp == kLoader) {
     if (lane == 0) {
       int n = 0, filled = 0;  // steps and items with steps so far
-      int in_flight_q = 0, in_flight_do = 0;
+      int in_flight_k = 0, in_flight_q = 0, in_flight_do = 0;
       bool ok = true;
       Cursor cur{-1, 0, 0};
+      // The first item is the CTA's own, the others come from the counter: fetched when the loads of
+      // the item before are out (any earlier, and long items go to CTAs that are not done), but before
+      // the loads of a short one, since the answer takes as long as such an item.
+      long long idx = blockIdx.x;
       for (int i = 0; ok; ++i) {
-        const Item it = make_item<true, VARLEN>(p, atomicAdd(p.counters, 1u), cur);
+        const Item it = make_item<true, VARLEN>(p, idx, cur);
         if (!(ok = ring_put(sh.items, i, it, ctl, ab)) || it.n < 0) break;
+        if (it.n <= kShortItem) idx = static_cast<long long>(gridDim.x) + atomicAdd(p.counters, 1u);
+        int g = 0, t = it.t0;  // head plane of the group, tile
         for (int j = 0; j < it.n; ++j, ++n) {
           const int qs = n % NQ, ds = n % ND;
-          const int g = j / it.nt, t = it.t0 + j - g * it.nt;
           if (j == 0) {
-            if (filled > 0 && !(ok = mbar_wait(bar_ke, (filled - 1) & 1, ctl, ab))) break;
-            mbar_expect_tx(bar_k, C::TILE_BYTES);
-            load_tile<D, VARLEN>(sb + C::K_OFF, tm_k, it.plane, it.kb + it.row0, bar_k);
+            const int o = filled % NO;
+            if (filled >= NO && !(ok = mbar_wait(bar_ke + 8 * o, (filled / NO - 1) & 1, ctl, ab))) break;
+            mbar_expect_tx(bar_k + 8 * o, C::TILE_BYTES);
+            load_tile<D, VARLEN>(sb + C::K_OFF + o * C::TILE_BYTES, tm_k, it.plane, it.kb + it.row0, bar_k + 8 * o);
+            in_flight_k = filled + 1;
           }
           if (n >= NQ && !(ok = mbar_wait(bar_qe + 8 * qs, (n / NQ - 1) & 1, ctl, ab))) break;
           if (ctl.inject == 4 && n == 1) break;  // test hook: never load this tile
@@ -414,9 +474,10 @@ __device__ __forceinline__ void kv_items(const BwdParams& p, const Shared& sh, c
           load_q_tile<D, VARLEN>(sb + C::QR_OFF + qs * C::TILE_BYTES, tm_q, it.other + g, it.qb, t * kTile, p.lg, bar_q + 8 * qs);
           in_flight_q = n + 1;
           if (j == 0) {
-            if (filled > 0 && !(ok = mbar_wait(bar_ve, (filled - 1) & 1, ctl, ab))) break;
-            mbar_expect_tx(bar_v, C::TILE_BYTES);
-            load_tile<D, VARLEN>(sb + C::V_OFF, tm_v, it.plane, it.kb + it.row0, bar_v);
+            const int o = filled % NO;
+            if (filled >= NO && !(ok = mbar_wait(bar_ve + 8 * o, (filled / NO - 1) & 1, ctl, ab))) break;
+            mbar_expect_tx(bar_v + 8 * o, C::TILE_BYTES);
+            load_tile<D, VARLEN>(sb + C::V_OFF + o * C::TILE_BYTES, tm_v, it.plane, it.kb + it.row0, bar_v + 8 * o);
             ++filled;
           }
           // dV and dK of step n - ND are done, and so are dP, issued before dK, and the reading of the
@@ -428,14 +489,14 @@ __device__ __forceinline__ void kv_items(const BwdParams& p, const Shared& sh, c
                    p.stats + (static_cast<size_t>(it.other + g) * p.stat_tiles + it.stat0 + t) * kStat, kStat * 4,
                    bar_do + 8 * ds);
           in_flight_do = n + 1;
+          if (++t == it.t0 + it.nt) ++g, t = it.t0;
         }
+        if (it.n > kShortItem) idx = static_cast<long long>(gridDim.x) + atomicAdd(p.counters, 1u);
         if (ctl.inject == 4 && n == 1) break;
       }
       // copies still in flight must land before the shared memory is used for anything else
-      if (filled > 0) {
-        mbar_wait(bar_k, (filled - 1) & 1, ctl, sh.drain_ab);
-        mbar_wait(bar_v, (filled - 1) & 1, ctl, sh.drain_ab);
-      }
+      for (int m = max(0, in_flight_k - NO); m < in_flight_k; ++m) mbar_wait(bar_k + 8 * (m % NO), (m / NO) & 1, ctl, sh.drain_ab);
+      for (int m = max(0, filled - NO); m < filled; ++m) mbar_wait(bar_v + 8 * (m % NO), (m / NO) & 1, ctl, sh.drain_ab);
       for (int m = max(0, in_flight_q - NQ); m < in_flight_q; ++m) mbar_wait(bar_q + 8 * (m % NQ), (m / NQ) & 1, ctl, sh.drain_ab);
       for (int m = max(0, in_flight_do - ND); m < in_flight_do; ++m)
         mbar_wait(bar_do + 8 * (m % ND), (m / ND) & 1, ctl, sh.drain_ab);
@@ -450,24 +511,19 @@ __device__ __forceinline__ void kv_items(const BwdParams& p, const Shared& sh, c
     for (int i = 0; ok; ++i) {
       if (!(ok = ring_get(sh.items, i, it, ctl, ab)) || it.n < 0) break;
       if (it.n == 0) continue;
-      auto zero_past_end = [&](uint32_t tile, int j) {
-        const int rows = (it.sq << p.lg) - (it.t0 + j % it.nt) * kTile;  // of the step's query tile, within the sequence
-        if (VARLEN && rows < kTile) {
-          zero_rows<D>(tile, rows);
-          fence_proxy_async_smem();
-          __syncwarp();
-        }
-      };
+      // rows of a plane's last query tile that belong to the sequence, and steps until one
+      const int last_rows = VARLEN ? (it.sq << p.lg) - (it.t0 + it.nt - 1) * kTile : kTile;
+      int to_last = it.nt - 1;
+      const int own = filled % NO, own_ph = filled / NO & 1;
       auto q_tile = [&](int j) { return sb + C::QR_OFF + (n + j) % NQ * C::TILE_BYTES; };
       auto do_tile = [&](int j) { return sb + C::DOR_OFF + (n + j) % ND * C::TILE_BYTES; };
       if (first) {
         auto scores = [&](int j) {
-          zero_past_end(q_tile(j), j);
-          issue_scores<D>(tm + C::S_COL, sb + C::K_OFF, q_tile(j));
+          issue_scores<D>(tm + C::S_COL, sb + C::K_OFF + own * C::TILE_BYTES, q_tile(j));
           tc_commit_el(bar_s);
-          if (j + 1 == it.n) tc_commit_el(bar_ke);
+          if (j + 1 == it.n) tc_commit_el(bar_ke + 8 * own);
         };
-        if (!(ok = wait_two(bar_k, filled & 1, bar_q + 8 * (n % NQ), n / NQ & 1, ctl, ab))) break;
+        if (!(ok = wait_two(bar_k + 8 * own, own_ph, bar_q + 8 * (n % NQ), n / NQ & 1, ctl, ab))) break;
         scores(0);
         // the gradients of the item before must have been read out
         if (filled > 0 && !(ok = mbar_wait_warp(bar_acce, (filled - 1) & 1, ctl, ab))) break;
@@ -476,12 +532,18 @@ __device__ __forceinline__ void kv_items(const BwdParams& p, const Shared& sh, c
           const uint32_t par = m & 1;
           const bool more = j + 1 < it.n;
           if (!(ok = wait_two(bar_p, par, more ? bar_q + 8 * ((m + 1) % NQ) : bar_p, more ? (m + 1) / NQ & 1 : par, ctl, ab))) break;
-          zero_past_end(do_tile(j), j);  // (the elementwise warps have seen this tile arrive)
           tc_fence_after();
-          issue_grad_chunks<D>(tm + C::DV_COL, tm + C::S_COL, do_tile(j), 0, j > 0);
+          const int rows = to_last == 0 ? last_rows : kTile;
+          to_last = to_last == 0 ? it.nt - 1 : to_last - 1;
+          if (rows == kTile) issue_grad_chunks<D>(tm + C::DV_COL, tm + C::S_COL, do_tile(j), 0, j > 0);
           if (!(ok = mbar_wait_warp(bar_p + 8, par, ctl, ab))) break;
           tc_fence_after();
-          issue_grad_chunks<D>(tm + C::DV_COL, tm + C::S_COL, do_tile(j), 1, true);
+          if (rows == kTile) {
+            issue_grad_chunks<D>(tm + C::DV_COL, tm + C::S_COL, do_tile(j), 1, true);
+          } else {
+            zero_rows<D>(do_tile(j), rows);  // (it came with the statistics, which P was made with)
+            issue_grad_rows<D>(tm + C::DV_COL, tm + C::S_COL, 64, do_tile(j), rows, j > 0);
+          }
           if (more) scores(j + 1);
           if (lane == 0) mbar_arrive(bar_si + 8 * (m & 1));
           __syncwarp();
@@ -489,12 +551,11 @@ __device__ __forceinline__ void kv_items(const BwdParams& p, const Shared& sh, c
         }
       } else {
         auto dprobs = [&](int j) {
-          zero_past_end(do_tile(j), j);
-          issue_scores<D>(tm + C::DP_COL, sb + C::V_OFF, do_tile(j));
+          issue_scores<D>(tm + C::DP_COL, sb + C::V_OFF + own * C::TILE_BYTES, do_tile(j));
           tc_commit_el(bar_dp);
-          if (j + 1 == it.n) tc_commit_el(bar_ve);
+          if (j + 1 == it.n) tc_commit_el(bar_ve + 8 * own);
         };
-        if (!(ok = wait_two(bar_v, filled & 1, bar_do + 8 * (n % ND), n / ND & 1, ctl, ab))) break;
+        if (!(ok = wait_two(bar_v + 8 * own, own_ph, bar_do + 8 * (n % ND), n / ND & 1, ctl, ab))) break;
         dprobs(0);
         if (filled > 0 && !(ok = mbar_wait_warp(bar_acce, (filled - 1) & 1, ctl, ab))) break;
         for (int j = 0; j < it.n; ++j) {
@@ -506,10 +567,17 @@ __device__ __forceinline__ void kv_items(const BwdParams& p, const Shared& sh, c
                                 more ? (m + 1) / ND & 1 : par, ctl, ab)))
             break;
           tc_fence_after();
-          issue_grad_chunks<D>(tm + C::DK_COL, tm + C::DP_COL, q_tile(j), 0, j > 0);
+          const int rows = to_last == 0 ? last_rows : kTile;
+          to_last = to_last == 0 ? it.nt - 1 : to_last - 1;
+          if (rows == kTile) issue_grad_chunks<D>(tm + C::DK_COL, tm + C::DP_COL, q_tile(j), 0, j > 0);
           if (!(ok = mbar_wait_warp(bar_ds + 8, par, ctl, ab))) break;
           tc_fence_after();
-          issue_grad_chunks<D>(tm + C::DK_COL, tm + C::DP_COL, q_tile(j), 1, true);
+          if (rows == kTile) {
+            issue_grad_chunks<D>(tm + C::DK_COL, tm + C::DP_COL, q_tile(j), 1, true);
+          } else {
+            zero_rows<D>(q_tile(j), rows);
+            issue_grad_rows<D>(tm + C::DK_COL, tm + C::DP_COL, 64, q_tile(j), rows, j > 0);
+          }
           tc_commit_el(bar_qe + 8 * (m % NQ));
           if (more) dprobs(j + 1);
         }
@@ -528,15 +596,30 @@ __device__ __forceinline__ void kv_items(const BwdParams& p, const Shared& sh, c
     const uint32_t s_tm = tm + C::S_COL + 64 * half, dp_tm = tm + C::DP_COL + 64 * half;
     const uint64_t c2 = f2(p.c, p.c);
     int n = 0, filled = 0;
-    bool ok = true;
+    bool ok = true, pending = false, dst_store = false;
+    __nv_bfloat16* dst = nullptr;
+    // An item's gradients are stored after the first step of the next one, whose products the MMA
+    // warps issue meanwhile.
+    auto finish = [&]() -> bool {
+      if (!mbar_wait_warp(bar_acc, filled & 1, ctl, ab)) return false;
+      tc_fence_after();
+      store_row<D>(tm + (half ? C::DK_COL : C::DV_COL), half ? p.scale : 1.f, dst, dst_store, p.wide);
+      tc_fence_before();
+      warp_arrive(bar_acce);
+      ++filled;
+      pending = false;
+      return true;
+    };
     Item it;
     for (int i = 0; ok; ++i) {
       if (!(ok = ring_get(sh.items, i, it, ctl, ab)) || it.n < 0) break;
       const int off = it.skv - it.sq, key = it.row0 + r;
+      int t = it.t0;
       for (int j = 0; j < it.n; ++j, ++n) {
         const int slot = n % ND;
         const uint32_t st = sb + C::ST_OFF + slot * (kStat * 4) + 256 * half;
-        const int q0 = (it.t0 + j % it.nt) * kTile + 64 * half;
+        const int q0 = t * kTile + 64 * half;
+        if (++t == it.t0 + it.nt) t = it.t0;
         // (the statistics come with the dO tile)
         if (!(ok = wait_two(bar_s, n & 1, bar_do + 8 * slot, n / ND & 1, ctl, ab))) break;
         tc_fence_after();
@@ -546,11 +629,20 @@ __device__ __forceinline__ void kv_items(const BwdParams& p, const Shared& sh, c
           // queries from key - off on see this key
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
-            const int hid = (max(0, min(it.sq, key - off)) << p.lg) - q0 - 32 * g;  // hidden rows of this word
-            const uint32_t hidden = hid >= 32 ? 0xffffffffu : hid <= 0 ? 0u : (1u << hid) - 1u;
+            const uint32_t hidden = low_bits((max(0, min(it.sq, key - off)) << p.lg) - q0 - 32 * g);
 #pragma unroll
             for (int e = 0; e < 32; ++e)
               if (hidden & (1u << e)) s[32 * g + e] = __float_as_uint(-INFINITY);
+          }
+        }
+        const int in = VARLEN ? (it.sq << p.lg) - q0 : 64;  // columns that belong to the sequence
+        if (VARLEN && in < 64) {
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            const uint32_t inside = low_bits(in - 32 * g);
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (!(inside & (1u << e))) s[32 * g + e] = __float_as_uint(-INFINITY);
           }
         }
         probs_t(s, s_tm, st, c2, bar_p);
@@ -558,6 +650,15 @@ __device__ __forceinline__ void kv_items(const BwdParams& p, const Shared& sh, c
         tc_fence_after();
         uint32_t d[64];
         ld64(dp_tm, d);
+        if (VARLEN && in < 64) {
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            const uint32_t inside = low_bits(in - 32 * g);
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (!(inside & (1u << e))) d[32 * g + e] = 0;
+          }
+        }
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
           uint32_t pk[16];
@@ -580,24 +681,23 @@ __device__ __forceinline__ void kv_items(const BwdParams& p, const Shared& sh, c
           warp_arrive(bar_ds + 8 * c);
           if (c == 0) reg_fence32(d + 32);
         }
+        if (pending && !(ok = finish())) break;
       }
       if (!ok) break;
       // warps 0-3 store dV, warps 4-7 dK
       const bool store = key < it.skv;
       const long long row = VARLEN ? static_cast<long long>(it.kb + key) * p.Hkv + it.plane
                                    : static_cast<long long>(it.plane) * p.Skv + key;
-      __nv_bfloat16* dst = (half ? p.dk : p.dv) + (store ? row : 0) * D;
-      if (it.n == 0) {
-        if (store) store_zeros<D>(dst);
-        continue;
+      __nv_bfloat16* const at = (half ? p.dk : p.dv) + (store ? row : 0) * D;
+      if (it.n > 0) {
+        dst = at;
+        dst_store = store;
+        pending = true;
+      } else if (store) {  // (another item's may be pending)
+        store_zeros<D>(at);
       }
-      if (!(ok = mbar_wait_warp(bar_acc, filled & 1, ctl, ab))) break;
-      tc_fence_after();
-      store_row<D>(tm + (half ? C::DK_COL : C::DV_COL), half ? p.scale : 1.f, dst, store);
-      tc_fence_before();
-      warp_arrive(bar_acce);
-      ++filled;
     }
+    if (ok && pending) finish();
   }
 }
 
@@ -615,8 +715,9 @@ __device__ __forceinline__ void q_items(const BwdParams& p, const Shared& sh, co
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const KernelCtl& ctl = p.ctl;
   const Abort& ab = sh.ab;
-  const uint32_t bar_q = sh.bars, bar_do = bar_q + 8, bar_qe = bar_do + 8, bar_doe = bar_qe + 8;
-  const uint32_t bar_k = bar_doe + 8, bar_ke = bar_k + 8 * NK, bar_v = bar_ke + 8 * NK;
+  constexpr int NO = C::NOWN;
+  const uint32_t bar_q = sh.bars, bar_do = bar_q + 8 * NO, bar_qe = bar_do + 8 * NO, bar_doe = bar_qe + 8 * NO;
+  const uint32_t bar_k = bar_doe + 8 * NO, bar_ke = bar_k + 8 * NK, bar_v = bar_ke + 8 * NK;
   // bar_dpf[step % NV]: dP is in registers, and so V's slot is free
   const uint32_t bar_s = bar_v + 8 * NV, bar_dp = bar_s + 8, bar_sf = bar_dp + 8, bar_dpf = bar_sf + 8;
   const uint32_t bar_ds = bar_dpf + 8 * NV, bar_acc = bar_ds + 16, bar_acce = bar_acc + 8, bar_drain = bar_acce + 8;
@@ -625,17 +726,21 @@ __device__ __forceinline__ void q_items(const BwdParams& p, const Shared& sh, co
   if (warp == kLoader) {
     if (lane == 0) {
       int n = 0, filled = 0;
-      int in_flight_k = 0, in_flight_v = 0;
+      int in_flight_q = 0, in_flight_k = 0, in_flight_v = 0;
       bool ok = true;
       Cursor cur{-1, 0, 0};
+      unsigned int idx = atomicAdd(p.counters + 1, 1u);
       for (int i = 0; ok; ++i) {
-        const Item it = make_item<false, VARLEN>(p, atomicAdd(p.counters + 1, 1u), cur);
+        const Item it = make_item<false, VARLEN>(p, idx, cur);
         if (!(ok = ring_put(sh.items, i, it, ctl, ab)) || it.n < 0) break;
+        if (it.n <= kShortItem) idx = atomicAdd(p.counters + 1, 1u);
         for (int j = 0; j < it.n; ++j, ++n) {
           if (j == 0) {
-            if (filled > 0 && !(ok = mbar_wait(bar_qe, (filled - 1) & 1, ctl, ab))) break;
-            mbar_expect_tx(bar_q, C::TILE_BYTES);
-            load_q_tile<D, VARLEN>(sb + C::Q_OFF, tm_q, it.plane, it.qb, it.row0, p.lg, bar_q);
+            const int o = filled % NO;
+            if (filled >= NO && !(ok = mbar_wait(bar_qe + 8 * o, (filled / NO - 1) & 1, ctl, ab))) break;
+            mbar_expect_tx(bar_q + 8 * o, C::TILE_BYTES);
+            load_q_tile<D, VARLEN>(sb + C::Q_OFF + o * C::TILE_BYTES, tm_q, it.plane, it.qb, it.row0, p.lg, bar_q + 8 * o);
+            in_flight_q = filled + 1;
           }
           const int ks = n % NK, kp = n / NK, vs = n % NV, vp = n / NV;
           if (kp > 0 && !(ok = mbar_wait(bar_ke + 8 * ks, (kp - 1) & 1, ctl, ab))) break;
@@ -643,9 +748,10 @@ __device__ __forceinline__ void q_items(const BwdParams& p, const Shared& sh, co
           load_tile<D, VARLEN>(sb + C::KR_OFF + ks * C::TILE_BYTES, tm_k, it.other, it.kb + j * kTile, bar_k + 8 * ks);
           in_flight_k = n + 1;
           if (j == 0) {
-            if (filled > 0 && !(ok = mbar_wait(bar_doe, (filled - 1) & 1, ctl, ab))) break;
-            mbar_expect_tx(bar_do, C::TILE_BYTES);
-            load_q_tile<D, VARLEN>(sb + C::DO_OFF, tm_do, it.plane, it.qb, it.row0, p.lg, bar_do);
+            const int o = filled % NO;
+            if (filled >= NO && !(ok = mbar_wait(bar_doe + 8 * o, (filled / NO - 1) & 1, ctl, ab))) break;
+            mbar_expect_tx(bar_do + 8 * o, C::TILE_BYTES);
+            load_q_tile<D, VARLEN>(sb + C::DO_OFF + o * C::TILE_BYTES, tm_do, it.plane, it.qb, it.row0, p.lg, bar_do + 8 * o);
             ++filled;
           }
           if (vp > 0 && !(ok = mbar_wait(bar_dpf + 8 * vs, (vp - 1) & 1, ctl, ab))) break;
@@ -653,11 +759,10 @@ __device__ __forceinline__ void q_items(const BwdParams& p, const Shared& sh, co
           load_tile<D, VARLEN>(sb + C::VR_OFF + vs * C::TILE_BYTES, tm_v, it.other, it.kb + j * kTile, bar_v + 8 * vs);
           in_flight_v = n + 1;
         }
+        if (it.n > kShortItem) idx = atomicAdd(p.counters + 1, 1u);
       }
-      if (filled > 0) {
-        mbar_wait(bar_q, (filled - 1) & 1, ctl, sh.drain_ab);
-        mbar_wait(bar_do, (filled - 1) & 1, ctl, sh.drain_ab);
-      }
+      for (int m = max(0, in_flight_q - NO); m < in_flight_q; ++m) mbar_wait(bar_q + 8 * (m % NO), (m / NO) & 1, ctl, sh.drain_ab);
+      for (int m = max(0, filled - NO); m < filled; ++m) mbar_wait(bar_do + 8 * (m % NO), (m / NO) & 1, ctl, sh.drain_ab);
       for (int m = max(0, in_flight_k - NK); m < in_flight_k; ++m) mbar_wait(bar_k + 8 * (m % NK), (m / NK) & 1, ctl, sh.drain_ab);
       for (int m = max(0, in_flight_v - NV); m < in_flight_v; ++m) mbar_wait(bar_v + 8 * (m % NV), (m / NV) & 1, ctl, sh.drain_ab);
     }
@@ -671,34 +776,26 @@ __device__ __forceinline__ void q_items(const BwdParams& p, const Shared& sh, co
     for (int i = 0; ok; ++i) {
       if (!(ok = ring_get(sh.items, i, it, ctl, ab)) || it.n < 0) break;
       if (it.n == 0) continue;
+      const int own = filled % NO, own_ph = filled / NO & 1;
       auto k_tile = [&](int j) { return sb + C::KR_OFF + (n + j) % NK * C::TILE_BYTES; };
       if (first) {
-        auto zero_past_end = [&](uint32_t tile, int j) {
-          if (VARLEN && it.skv - j * kTile < kTile) {
-            zero_rows<D>(tile, it.skv - j * kTile);
-            fence_proxy_async_smem();
-            __syncwarp();
-          }
-        };
         for (int j = 0; j < it.n; ++j) {
           const int m = n + j, ks = m % NK, vs = m % NV;
           const uint32_t bk = bar_k + 8 * ks, pk = m / NK & 1, bv = bar_v + 8 * vs, pv = m / NV & 1;
           const uint32_t v = sb + C::VR_OFF + vs * C::TILE_BYTES;
           // the tiles, and S and dP of the step before in registers
-          if (j == 0 && !(ok = mbar_wait_warp(bar_q, filled & 1, ctl, ab))) break;
+          if (j == 0 && !(ok = mbar_wait_warp(bar_q + 8 * own, own_ph, ctl, ab))) break;
           if (!(ok = wait_two(bk, pk, m > 0 ? bar_sf : bk, m > 0 ? (m - 1) & 1 : pk, ctl, ab))) break;
-          zero_past_end(k_tile(j), j);
           tc_fence_after();
-          issue_scores<D>(tm + C::S_COL, sb + C::Q_OFF, k_tile(j));
+          issue_scores<D>(tm + C::S_COL, sb + C::Q_OFF + own * C::TILE_BYTES, k_tile(j));
           tc_commit_el(bar_s);
-          if (j + 1 == it.n) tc_commit_el(bar_qe);
-          if (j == 0 && !(ok = mbar_wait_warp(bar_do, filled & 1, ctl, ab))) break;
+          if (j + 1 == it.n) tc_commit_el(bar_qe + 8 * own);
+          if (j == 0 && !(ok = mbar_wait_warp(bar_do + 8 * own, own_ph, ctl, ab))) break;
           if (!(ok = wait_two(bv, pv, m > 0 ? bar_dpf + 8 * ((m - 1) % NV) : bv, m > 0 ? (m - 1) / NV & 1 : pv, ctl, ab))) break;
-          zero_past_end(v, j);
           tc_fence_after();
-          issue_scores<D>(tm + C::DP_COL, sb + C::DO_OFF, v);
+          issue_scores<D>(tm + C::DP_COL, sb + C::DO_OFF + own * C::TILE_BYTES, v);
           tc_commit_el(bar_dp);
-          if (j + 1 == it.n) tc_commit_el(bar_doe);
+          if (j + 1 == it.n) tc_commit_el(bar_doe + 8 * own);
         }
       } else {
         // the gradient of the item before must have been read out
@@ -707,8 +804,14 @@ __device__ __forceinline__ void q_items(const BwdParams& p, const Shared& sh, co
           const int m = n + j;
           if (!(ok = mbar_wait_warp(bar_ds + 8 * (m & 1), m >> 1 & 1, ctl, ab))) break;
           tc_fence_after();
-          for (int h = 0; h < 2; ++h)
-            issue_grad_half<D>(tm + C::DQ_COL, tm + C::DS_COL + 64 * (m & 1) + 32 * h, k_tile(j), h, j > 0 || h > 0);
+          const int rows = VARLEN ? it.skv - j * kTile : kTile;
+          if (rows >= kTile) {
+            for (int h = 0; h < 2; ++h)
+              issue_grad_half<D>(tm + C::DQ_COL, tm + C::DS_COL + 64 * (m & 1) + 32 * h, k_tile(j), h, j > 0 || h > 0);
+          } else {
+            zero_rows<D>(k_tile(j), rows);
+            issue_grad_rows<D>(tm + C::DQ_COL, tm + C::DS_COL + 64 * (m & 1), 32, k_tile(j), rows, j > 0);
+          }
           tc_commit_el(bar_ke + 8 * (m % NK));
         }
         if (ok) tc_commit_el(bar_acc);
@@ -724,7 +827,18 @@ __device__ __forceinline__ void q_items(const BwdParams& p, const Shared& sh, co
     const uint32_t tm = sh.tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
     const uint64_t c2 = f2(p.c, p.c);
     int n = 0, filled = 0;
-    bool ok = true;
+    bool ok = true, pending = false, dst_store = false;
+    __nv_bfloat16* dst = nullptr;
+    auto finish = [&]() -> bool {  // as in kv_items
+      if (!mbar_wait_warp(bar_acc, filled & 1, ctl, ab)) return false;
+      tc_fence_after();
+      store_row<D / 2>(tm + C::DQ_COL + half * (D / 2), p.scale, dst, dst_store, p.wide);
+      tc_fence_before();
+      warp_arrive(bar_acce);
+      ++filled;
+      pending = false;
+      return true;
+    };
     Item it;
     for (int i = 0; ok; ++i) {
       if (!(ok = ring_get(sh.items, i, it, ctl, ab)) || it.n < 0) break;
@@ -744,8 +858,7 @@ __device__ __forceinline__ void q_items(const BwdParams& p, const Shared& sh, co
         if (k0 + 64 > limit) {
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
-            const int vis = limit - k0 - 32 * g;
-            const uint32_t visible = vis >= 32 ? 0xffffffffu : vis <= 0 ? 0u : (1u << vis) - 1u;
+            const uint32_t visible = low_bits(limit - k0 - 32 * g);
 #pragma unroll
             for (int e = 0; e < 32; ++e)
               if (!(visible & (1u << e))) s[32 * g + e] = __float_as_uint(-INFINITY);
@@ -765,6 +878,15 @@ __device__ __forceinline__ void q_items(const BwdParams& p, const Shared& sh, co
         ld64(tm + C::DP_COL + 64 * half, d);
         tc_fence_before();
         warp_arrive(bar_dpf + 8 * (n % NV));
+        if (VARLEN && k0 + 64 > it.skv) {  // (dP of the next sequence's keys may be no number)
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            const uint32_t inside = low_bits(it.skv - k0 - 32 * g);
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (!(inside & (1u << e))) d[32 * g + e] = 0;
+          }
+        }
 #pragma unroll
         for (int e = 0; e < 64; e += 2) {
           const uint64_t x = mul2(add2(f2(__uint_as_float(d[e]), __uint_as_float(d[e + 1])), nd2),
@@ -775,23 +897,22 @@ __device__ __forceinline__ void q_items(const BwdParams& p, const Shared& sh, co
         tmem_wait_st();
         tc_fence_before();
         warp_arrive(bar_ds + 8 * (n & 1));
+        if (pending && !(ok = finish())) break;
       }
       if (!ok) break;
       const bool store = q < it.sq;
       const long long head = (static_cast<long long>(it.plane) << p.lg) + ((it.row0 + r) & ((1 << p.lg) - 1));
       const long long row = VARLEN ? static_cast<long long>(it.qb + q) * p.Hq + head : head * p.Sq + q;
-      __nv_bfloat16* dst = p.dq + (store ? row : 0) * D + half * (D / 2);
-      if (it.n == 0) {
-        if (store) store_zeros<D / 2>(dst);
-        continue;
+      __nv_bfloat16* const at = p.dq + (store ? row : 0) * D + half * (D / 2);
+      if (it.n > 0) {
+        dst = at;
+        dst_store = store;
+        pending = true;
+      } else if (store) {
+        store_zeros<D / 2>(at);
       }
-      if (!(ok = mbar_wait_warp(bar_acc, filled & 1, ctl, ab))) break;
-      tc_fence_after();
-      store_row<D / 2>(tm + C::DQ_COL + half * (D / 2), p.scale, dst, store);
-      tc_fence_before();
-      warp_arrive(bar_acce);
-      ++filled;
     }
+    if (ok && pending) finish();
   }
 }
 
@@ -814,20 +935,20 @@ __global__ void __launch_bounds__(kThreads, 1)
   volatile int* flags = reinterpret_cast<volatile int*>(smem + C::ABORT_OFF);
 
   // Barriers of the kv items and of the query items: [0, kv) and [kv, ..), each with an item ring.
-  constexpr int kKvBars = 4 + 2 * C::NQ + C::ND + 2 + 4 + 3 + 2, kQBars = 4 + 2 * C::NK + C::NV + 3 + C::NV + 2 + 3;
+  constexpr int kKvBars = 4 * C::NOWN + 2 * C::NQ + C::ND + 11, kQBars = 4 * C::NOWN + 2 * C::NK + 2 * C::NV + 8;
   static_assert(kKvBars + kQBars + 8 <= C::NBAR, "barrier space");
   const uint32_t bars = sbase + C::BAR_OFF;
   const uint32_t kv_bars = bars, q_bars = bars + 8 * kKvBars, ring_bars = q_bars + 8 * kQBars;
   if (threadIdx.x == 0) {
     for (int i = 0; i < kKvBars + kQBars; ++i) mbar_init(bars + 8 * i, 1);
     // the elementwise warps arrive on these
-    const uint32_t bar_p = kv_bars + 8 * (4 + 2 * C::NQ + C::ND + 2);
+    const uint32_t bar_p = kv_bars + 8 * (4 * C::NOWN + 2 * C::NQ + C::ND + 2);
     for (int i = 0; i < 4; ++i) mbar_init(bar_p + 8 * i, kEltWarps);  // p[2], ds[2]
     mbar_init(bar_p + 8 * 4, 2);                                      // acc: both MMA warps
     mbar_init(bar_p + 8 * 5, kEltWarps);                              // acc_empty
     mbar_init(bar_p + 8 * 6, 2);                                      // drain: both MMA warps
-    for (int i = 0; i < C::NQ; ++i) mbar_init(kv_bars + 8 * (4 + C::NQ + i), 2);  // q_empty: dV and dK
-    const uint32_t bar_sf = q_bars + 8 * (4 + 2 * C::NK + C::NV + 2);
+    for (int i = 0; i < C::NQ; ++i) mbar_init(kv_bars + 8 * (4 * C::NOWN + C::NQ + i), 2);  // q_empty: dV and dK
+    const uint32_t bar_sf = q_bars + 8 * (4 * C::NOWN + 2 * C::NK + C::NV + 2);
     for (int i = 0; i < 1 + C::NV + 2; ++i) mbar_init(bar_sf + 8 * i, kEltWarps);  // S free, dP free[NV], ds[2]
     const uint32_t bar_qacce = bar_sf + 8 * (1 + C::NV + 3);
     mbar_init(bar_qacce, kEltWarps);
@@ -881,18 +1002,19 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 // ---------------------------------------------------------------- row statistics
-// One block per tile of 128 rows of a query plane: -LSE log2(e) and dLSE - dO . O for each row.
+// kTile / kRowsPerBlock blocks per tile of 128 rows of a query plane: -LSE log2(e) and dLSE - dO . O for each row.
 // Rows past the end, and rows whose LSE is -inf (no key is seen), get -inf and P = 0.  Bound by
 // reading dO and O once; D / 8 lanes of 16 bytes take a row.
 template <int D, bool VARLEN>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(kRowThreads)
     attn_bwd_rows_kernel(const __nv_bfloat16* dout, const __nv_bfloat16* o, const float* lse, const float* dlse, float* stats,
                          unsigned int* counters, int B, int H, int Sq, int lg, int stat_tiles, const int32_t* cu_q) {
-  constexpr int LPR = D / 8, RPP = 256 / LPR;  // lanes per row, rows per pass of the block
+  constexpr int LPR = D / 8, PASSES = kRowsPerBlock * LPR / kRowThreads;  // lanes per row
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;");
   if (blockIdx.x == 0 && threadIdx.x < 2) counters[threadIdx.x] = 0;
-  const int plane = static_cast<int>(blockIdx.x) / stat_tiles, tile = static_cast<int>(blockIdx.x) % stat_tiles;
+  const int at_tile = static_cast<int>(blockIdx.x / (kTile / kRowsPerBlock)), part = static_cast<int>(blockIdx.x % (kTile / kRowsPerBlock));
+  const int plane = at_tile / stat_tiles, tile = at_tile % stat_tiles;
   int row0 = tile * kTile, n = Sq, qb = 0;
   if constexpr (VARLEN) {
     int lo = 0, hi = B - 1;  // the last sequence that starts at this tile or before it
@@ -908,34 +1030,41 @@ __global__ void __launch_bounds__(256)
     row0 = (tile - ragged_stat0(cu_q, lo, lg)) * kTile;
     if (row0 < 0 || row0 >= n << lg) return;  // a tile of no sequence
   }
-  const int l = threadIdx.x % LPR;
-  float* st = stats + static_cast<size_t>(blockIdx.x) * kStat;
-#pragma unroll 4
-  for (int r = threadIdx.x / LPR; r < kTile; r += RPP) {
-    const int query = (row0 + r) >> lg;
-    const long long head = (static_cast<long long>(plane) << lg) + ((row0 + r) & ((1 << lg) - 1));
-    const bool in = query < n;
-    const long long at = VARLEN ? static_cast<long long>(qb + query) * H + head : head * Sq + query;
-    float a = 0.f;
-    if (in) {
-      const uint4 x = *reinterpret_cast<const uint4*>(dout + at * D + 8 * l);
-      const uint4 y = *reinterpret_cast<const uint4*>(o + at * D + 8 * l);
-      const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
+  const int l = threadIdx.x % LPR, r0 = part * kRowsPerBlock + static_cast<int>(threadIdx.x) / LPR;
+  float* st = stats + static_cast<size_t>(at_tile) * kStat;
+  uint4 x[PASSES], y[PASSES];
+  float nl[PASSES], dl[PASSES];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) a = fmaf(bf16hi(xw[i]), bf16hi(yw[i]), fmaf(bf16lo(xw[i]), bf16lo(yw[i]), a));
+  for (int i = 0; i < PASSES; ++i) {
+    const int row = row0 + r0 + i * (kRowThreads / LPR), query = row >> lg;
+    const long long head = (static_cast<long long>(plane) << lg) + (row & ((1 << lg) - 1));
+    const long long at = VARLEN ? static_cast<long long>(qb + query) * H + head : head * Sq + query;
+    x[i] = y[i] = make_uint4(0, 0, 0, 0);
+    nl[i] = -INFINITY;
+    dl[i] = 0.f;
+    if (query < n) {
+      x[i] = *reinterpret_cast<const uint4*>(dout + at * D + 8 * l);
+      y[i] = *reinterpret_cast<const uint4*>(o + at * D + 8 * l);
+      if (l == 0) {
+        const long long s = VARLEN ? head * Sq + qb + query : at;
+        const float e = lse[s];
+        nl[i] = e == -INFINITY ? -INFINITY : -e * kLog2e;
+        if (dlse) dl[i] = dlse[s];
+      }
     }
+  }
+#pragma unroll
+  for (int i = 0; i < PASSES; ++i) {
+    const uint32_t xw[4] = {x[i].x, x[i].y, x[i].z, x[i].w}, yw[4] = {y[i].x, y[i].y, y[i].z, y[i].w};
+    float a = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) a = fmaf(bf16hi(xw[w]), bf16hi(yw[w]), fmaf(bf16lo(xw[w]), bf16lo(yw[w]), a));
 #pragma unroll
     for (int m = LPR / 2; m > 0; m >>= 1) a += __shfl_xor_sync(0xffffffffu, a, m);
     if (l == 0) {
-      float nl = -INFINITY, nd = 0.f;
-      if (in) {
-        const long long i = VARLEN ? head * Sq + qb + query : at;
-        const float s = lse[i];
-        nl = s == -INFINITY ? -INFINITY : -s * kLog2e;
-        nd = (dlse ? dlse[i] : 0.f) - a;
-      }
-      st[r] = nl;
-      st[kTile + r] = nd;
+      const int r = r0 + i * (kRowThreads / LPR);
+      st[r] = nl[i];
+      st[kTile + r] = dl[i] - a;
     }
   }
 }
@@ -1037,7 +1166,7 @@ cudaError_t launch_d(const BwdArgs& a, const KernelCtl& ctl, cudaStream_t stream
   const int stat_tiles = static_cast<int>(bwd_stat_tiles(a.B, a.Sq, lg, VARLEN));
   unsigned int* counters = static_cast<unsigned int*>(a.workspace);
   float* stats = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + 256);
-  e = launch(attn_bwd_rows_kernel<D, VARLEN>, static_cast<int>(q_planes * stat_tiles), 256, 0, stream,
+  e = launch(attn_bwd_rows_kernel<D, VARLEN>, static_cast<int>(q_planes * stat_tiles) * (kTile / kRowsPerBlock), kRowThreads, 0, stream,
              static_cast<const __nv_bfloat16*>(a.dout), static_cast<const __nv_bfloat16*>(a.o), a.lse, a.dlse, stats, counters,
              a.B, a.Hq, a.Sq, lg, stat_tiles, a.cu_q);
   if (e != cudaSuccess) return e;
@@ -1054,6 +1183,7 @@ cudaError_t launch_d(const BwdArgs& a, const KernelCtl& ctl, cudaStream_t stream
   p.Sq = a.Sq;
   p.Skv = a.Skv;
   p.causal = a.causal;
+  p.wide = ((reinterpret_cast<uintptr_t>(a.dq) | reinterpret_cast<uintptr_t>(a.dk) | reinterpret_cast<uintptr_t>(a.dv)) & 31) == 0;
   p.lg = lg;
   p.c = a.scale * kLog2e;
   p.scale = a.scale;

@@ -338,7 +338,7 @@ bool bwd_sizes_fit(int B, int Hq, int Hkv, long long Sq, long long Skv, bool rag
   const long long heads = ragged ? Hq : static_cast<long long>(B) * Hq;
   const long long kv_planes = ragged ? Hkv : static_cast<long long>(B) * Hkv;
   return heads <= 0x7fffffffLL && Sq << lg <= 0x3fffffffLL && Skv <= 0x3fffffffLL &&
-         (heads >> lg) * bwd_stat_tiles(B, Sq, lg, ragged) <= 0x3fffffffLL &&
+         (heads >> lg) * bwd_stat_tiles(B, Sq, lg, ragged) <= 0x1fffffffLL &&
          kv_planes * (Skv / 128 + (ragged ? B : 1)) <= 0x3fffffffLL;
 }
 

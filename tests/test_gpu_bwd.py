@@ -138,6 +138,16 @@ def test_ragged_against_the_formula(loom, ql, kl, causal, D):
 
 
 @pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("kl,ql", [((130, 130), (0, 150)), ((0, 140), (150, 150))])
+def test_items_without_steps_between_others(loom, kl, ql, D):
+    """Sequences without queries (or keys) in turn with others, several items for each CTA."""
+    host, grads, cq, ck = _ragged(loom, ql * 30, kl * 30, 16, 16, D, False, False)
+    _check_ragged(host, grads, cq, ck, False, D ** -0.5)
+    for b in range(0, 60, 2):
+        assert (grads[0][cq[b]:cq[b + 1]] == 0).all() and (grads[1][ck[b]:ck[b + 1]] == 0).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("causal", [False, True])
 def test_a_sequence_of_nan_and_infinity_reaches_no_other(loom, causal, D):
     ql, kl = (70, 130, 200, 33), (70, 200, 190, 33)
@@ -243,6 +253,16 @@ def test_given_outputs_workspace_and_stream(loom):
     torch.cuda.synchronize()
     assert all(torch.equal(x, y) for x, y in zip(outs, want))
     loom.loom_attn_check_error()
+
+
+def test_outputs_aligned_to_16_bytes_only(loom):
+    import torch
+    host, want = _dense(loom, 1, 4, 2, 260, 260, 64, True, False)
+    dev = [t.cuda() for t in host[:6]]
+    outs = [torch.empty(t.numel() + 8, dtype=torch.bfloat16, device="cuda")[8:].view(t.shape) for t in dev[1:4]]
+    assert all(t.data_ptr() % 32 == 16 for t in outs)
+    loom.loom_attn_bwd(*dev, *outs, causal=True)
+    assert all(torch.equal(x, y) for x, y in zip(outs, want))
 
 
 def test_offsets_past_32_bits(loom):
