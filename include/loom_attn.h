@@ -229,8 +229,9 @@ loom_status loom_attn_decode_noalloc(const void* q, const void* k_cache, const v
  *   dq     [B, Hq, Sq, D]   bf16, written
  *   dk, dv [B, Hkv, Skv, D] bf16, written
  *   workspace  device scratch of at least loom_attn_bwd_workspace_bytes(...) bytes, whose contents
- *          on entry do not matter (row statistics, 8 bytes per query of a head in tiles of 128 rows, and
- *          256 bytes of counters); a workspace serves one call at a time.
+ *          on entry do not matter (row statistics, 8 bytes per query of a head in tiles of 128 rows,
+ *          counters, and where the tiles are few and their sums long, partial sums); a workspace
+ *          serves one call at a time.
  *   causal, scale as loom_attn_fwd.  The gradients must not overlap the inputs.
  * Scores, probabilities and sums are fp32; P and dS are rounded to bf16 before they meet dout, q
  * and k on the tensor cores, and each gradient once when it is stored.  Every sum has a fixed

@@ -79,6 +79,21 @@ def test_many_items_and_a_scale_of_ones_own(loom, causal):
     _check_dense(host, grads, causal, 0.25)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("B,Hq,Hkv,Sq,Skv", [(1, 8, 1, 700, 700), (1, 2, 2, 1100, 1500), (1, 3, 1, 130, 2000), (2, 4, 1, 1000, 1000)])
+def test_few_long_items_are_split(loom, B, Hq, Hkv, Sq, Skv, D, causal):
+    """Few tiles with many steps, whose sums are split and joined (the workspace shows that they are);
+    the same bits each time."""
+    import torch
+    host, grads = _dense(loom, B, Hq, Hkv, Sq, Skv, D, causal, False)
+    stats = B * Hq * Sq * 8
+    assert loom.loom_attn_bwd_workspace_bytes(B, Hq, Hkv, Sq, Skv, D) > 4 * stats
+    _check_dense(host, grads, causal, D ** -0.5)
+    again = _dense(loom, B, Hq, Hkv, Sq, Skv, D, causal, False)[1]
+    assert all(torch.equal(x, y) for x, y in zip(grads, again))
+
+
 def _ragged(loom, ql, kl, Hq, Hkv, D, causal, dlse, seed=0, spoil=None):
     import torch
     gen = torch.Generator().manual_seed(seed)
@@ -126,6 +141,8 @@ RAGGED = [
     ((5, 200, 130), (260, 40, 130)),               # more queries than keys: rows that see nothing
     ((0, 150, 64, 10), (90, 0, 300, 7)),           # queries without keys, keys without queries
     ((3,) * 40, None),                             # many short ones
+    ((1, 900, 700), None),                         # few long ones: split sums, shares without steps
+    ((2, 5, 1200), (900, 1500, 3)),                # ... and rows that see nothing
 ]
 
 
