@@ -11,11 +11,15 @@
 // Value heads are copied.  All arithmetic is fp32; a value is rounded once, when it is stored.
 //
 // What bounds it: the projection is read once and written once, and no value meets another
-// outside its head, so it is the memory's bandwidth.  A head is D / 8 lanes of 16 bytes; a warp
-// takes a token and UNR steps of 256 / D heads, all of whose loads are issued before the first
-// is used, so that the token's angles and the weights are loaded once for all of them and enough
-// bytes are in flight.  The norm's sum is shuffled within the head's lanes, and so is the pair's
-// partner of the half-split form, which lies R / 16 lanes away.
+// outside its head, so it is the memory's bandwidth, and after that the instructions per value:
+// at 100 instructions for 16 bytes of a lane they took as long as the memory (8192 tokens, H32/8,
+// D 128: 49 us; 35 with what follows).  So the norm's factor is applied last, and weight and angle
+// are multiplied once for all of a token's heads:
+//     y_i = r (x_i A_i + x_partner(i) B_i),   A_i = w_i c_i,   B_i = w_partner(i) (+-) s_i;
+// the arithmetic is on pairs of floats, and the partner's values are shuffled as packed bf16.
+// A head is D / 8 lanes of 16 bytes; a warp takes a unit, up to UNR steps of 256 / D heads of one
+// kind (query, key or value) of a token, and issues the loads of all of them before it uses the
+// first.
 #include <cuda_bf16.h>
 
 #include "kernels.h"
@@ -26,17 +30,25 @@ namespace loom {
 namespace {
 
 constexpr int kWarps = 8;             // per block
-constexpr int kMaxBwdBlocks = 152 * 4;  // partial sums of the weights' gradients
+constexpr int kMaxBwdBlocks = 152 * 2;  // as many as are resident; partial sums of the weights' gradients
+// Steps of a unit: four, or one where the call is over as soon as its longest warp.  GB300, device
+// us with one / two / four / eight steps: 8192 tokens H32/8 D 128 - / 58 / 34.7 / 35.5 (two: before
+// the heads' kinds were kept apart), 579 tokens into a cache 5.9 / 5.2 / 4.4 / -, one token 2.1 / 2.3
+// / 2.4 / -; backward, 8192 tokens 84 with two, 61 with four (at two blocks on an SM; three spill: 79),
+// 96 with eight.
+constexpr int kSteps = 4, kFewSteps = 1;
+constexpr long long kManyValues = 1 << 18;
 
 struct QkvParams {
   const __nv_bfloat16* x;
   long long row_elems;
   const void *wq, *wk;
+  int w_f32;
   const float *cos, *sin;
   const int32_t* pos;
   int T, Hq, Hkv, R, P;
-  int chunks;        // warps' shares of a token
-  long long units;   // T * chunks
+  int q_units, kv_units;  // units of a token's query heads, of its key heads (and of its value heads)
+  long long units;        // of all tokens
   float eps;
   QkvPlace q_at, kv_at;
   __nv_bfloat16 *q, *k, *v;
@@ -44,6 +56,23 @@ struct QkvParams {
   long long drow_elems;
   float* partial;
 };
+
+// Unit `unit`: which token's heads of which kind, from head h0 on (counted within the kind).
+enum Kind { kQuery, kKey, kValue };
+struct Unit {
+  int t, kind, h0, heads;  // heads: of the kind
+};
+template <int D, int UNR>
+__device__ __forceinline__ Unit unit_of(const QkvParams& p, long long unit) {
+  const int per = p.q_units + 2 * p.kv_units;
+  const long long token = unit / per;
+  const int t = token < p.T ? static_cast<int>(token) : p.T;
+  int u = static_cast<int>(unit - token * per);
+  if (u < p.q_units) return {t, kQuery, u * (256 / D * UNR), p.Hq};
+  u -= p.q_units;
+  const int kind = u < p.kv_units ? kKey : kValue;
+  return {t, kind, (u - (kind == kValue ? p.kv_units : 0)) * (256 / D * UNR), p.Hkv};
+}
 
 __device__ __forceinline__ uint4 ld_stream(const __nv_bfloat16* p) {
   return __ldcs(reinterpret_cast<const uint4*>(p));
@@ -61,36 +90,44 @@ __device__ __forceinline__ long long place_token(const QkvPlace& at, int t, long
   return static_cast<long long>(t) * at.H * D;
 }
 
-__device__ __forceinline__ void unpack8(const uint4& u, float* f) {
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    f[2 * i] = bf16lo(w[i]);
-    f[2 * i + 1] = bf16hi(w[i]);
-  }
+// Eight packed bf16 as four pairs of floats, and back.
+__device__ __forceinline__ void unpack8(const uint4& u, uint64_t* f) {
+  f[0] = f2(bf16lo(u.x), bf16hi(u.x));
+  f[1] = f2(bf16lo(u.y), bf16hi(u.y));
+  f[2] = f2(bf16lo(u.z), bf16hi(u.z));
+  f[3] = f2(bf16lo(u.w), bf16hi(u.w));
 }
-__device__ __forceinline__ uint4 pack8(const float* f) {
-  return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
+__device__ __forceinline__ uint4 pack8(const uint64_t* f) {
+  return make_uint4(pack_bf16x2(f2lo(f[0]), f2hi(f[0])), pack_bf16x2(f2lo(f[1]), f2hi(f[1])), pack_bf16x2(f2lo(f[2]), f2hi(f[2])),
+                    pack_bf16x2(f2lo(f[3]), f2hi(f[3])));
 }
 
-template <bool W_F32>
-__device__ __forceinline__ void load_weight(const void* w, int i0, float* f) {
-  if constexpr (W_F32) {
-    const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(w) + i0);
-    const float4 a = __ldg(p), b = __ldg(p + 1);
+// Eight weights from i0 on.
+__device__ __forceinline__ void load_weight(const QkvParams& p, int kind, int i0, float* f) {
+  const void* w = kind == kQuery ? p.wq : p.wk;
+  if (p.w_f32) {
+    const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(w) + i0);
+    const float4 a = __ldg(q), b = __ldg(q + 1);
     f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
   } else {
-    unpack8(__ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(w) + i0)), f);
+    const uint4 u = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(w) + i0));
+    f[0] = bf16lo(u.x), f[1] = bf16hi(u.x), f[2] = bf16lo(u.y), f[3] = bf16hi(u.y);
+    f[4] = bf16lo(u.z), f[5] = bf16hi(u.z), f[6] = bf16lo(u.w), f[7] = bf16hi(u.w);
   }
 }
 
-// This lane's angles: y_i = z_i c_i + partner(z)_i s_i, with the pair's sign in s (BWD: of the
-// transposed rotation).  src: the lane that holds the partners (half-split).
+// The lane whose values are the partners of this lane's (half-split pairs; else this lane).
+template <int D, bool INTER>
+__device__ __forceinline__ int partner_lane(const QkvParams& p, int lane) {
+  const int i0 = 8 * (lane % (D / 8)), half = p.R / 2;
+  return INTER || i0 >= p.R ? lane : i0 < half ? lane + half / 8 : lane - half / 8;
+}
+
+// This lane's angles at token t: y_i = z_i c_i + partner(z)_i s_i, with the pair's sign in s (BWD: of
+// the transposed rotation).
 template <int D, bool INTER, bool BWD>
-__device__ __forceinline__ void load_angles(const QkvParams& p, int t, int lane, float* c, float* s, int& src) {
-  constexpr int LPH = D / 8;
-  const int l = lane % LPH, i0 = 8 * l;
-  src = lane;
+__device__ __forceinline__ void load_angles(const QkvParams& p, int t, int lane, float* c, float* s) {
+  const int i0 = 8 * (lane % (D / 8));
 #pragma unroll
   for (int i = 0; i < 8; ++i) c[i] = 1.f, s[i] = 0.f;
   if (i0 >= p.R) return;
@@ -111,7 +148,6 @@ __device__ __forceinline__ void load_angles(const QkvParams& p, int t, int lane,
   } else {
     const bool first = i0 < half;
     const int at = first ? i0 : i0 - half;
-    src = first ? lane + half / 8 : lane - half / 8;
     const float sign = first == BWD ? 1.f : -1.f;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -123,15 +159,21 @@ __device__ __forceinline__ void load_angles(const QkvParams& p, int t, int lane,
   }
 }
 
+// The partners of eight packed values.
 template <bool INTER>
-__device__ __forceinline__ void rotate8(const float* z, const float* c, const float* s, int src, float* y) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float other = INTER ? z[i ^ 1] : __shfl_sync(0xffffffffu, z[i], src);
-    y[i] = fmaf(other, s[i], z[i] * c[i]);
-  }
+__device__ __forceinline__ uint4 partners(const uint4& u, int src) {
+  if constexpr (INTER)
+    return make_uint4(__funnelshift_l(u.x, u.x, 16), __funnelshift_l(u.y, u.y, 16), __funnelshift_l(u.z, u.z, 16),
+                      __funnelshift_l(u.w, u.w, 16));
+  else
+    return make_uint4(__shfl_sync(0xffffffffu, u.x, src), __shfl_sync(0xffffffffu, u.y, src), __shfl_sync(0xffffffffu, u.z, src),
+                      __shfl_sync(0xffffffffu, u.w, src));
 }
 
+__device__ __forceinline__ float sum8(const uint64_t* a, const uint64_t* b) {
+  const uint64_t s = add2(fma2(a[1], b[1], mul2(a[0], b[0])), fma2(a[3], b[3], mul2(a[2], b[2])));
+  return f2lo(s) + f2hi(s);
+}
 // Sum over the LPH lanes of a head.
 template <int LPH>
 __device__ __forceinline__ float head_sum(float a) {
@@ -140,151 +182,159 @@ __device__ __forceinline__ float head_sum(float a) {
   return a;
 }
 
-template <int D, bool INTER, bool W_F32, int UNR>
+// Value 0 of token t's head 0 of a kind where it is written (backward: read), and the distance
+// between heads; a token whose cache slot lies outside the cache has no such place.
+template <int D>
+__device__ __forceinline__ __nv_bfloat16* place(const QkvParams& p, const Unit& u, long long& head) {
+  __nv_bfloat16* base = u.kind == kQuery ? p.q : u.kind == kKey ? p.k : p.v;
+  const QkvPlace& at = u.kind == kQuery ? p.q_at : p.kv_at;
+  if (u.kind == kQuery || !at.slots) return base + place_token<D>(at, u.t, head);
+  const int slot = __ldg(at.slots + u.t);
+  head = at.head_elems;
+  if (slot < 0 || slot >= at.n_slots) return nullptr;
+  const int page = slot / at.page;
+  return base + page * at.page_elems + static_cast<long long>(slot - page * at.page) * at.row_elems;
+}
+
+template <int D, bool INTER, int UNR>
 __global__ void __launch_bounds__(kWarps * 32) qkv_norm_rope_kernel(const QkvParams p) {
   constexpr int LPH = D / 8, RPW = 32 / LPH;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;");
   const long long unit = static_cast<long long>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
   if (unit >= p.units) return;
-  const int lane = threadIdx.x & 31, i0 = 8 * (lane % LPH);
-  const int t = static_cast<int>(unit / p.chunks);
-  const int row0 = static_cast<int>(unit - static_cast<long long>(t) * p.chunks) * (RPW * UNR) + lane / LPH;
-  const int heads = p.Hq + 2 * p.Hkv;
+  const Unit u = unit_of<D, UNR>(p, unit);
+  const int lane = threadIdx.x & 31, i0 = 8 * (lane % LPH), h0 = u.h0 + lane / LPH;
+  const int first = u.kind == kQuery ? 0 : u.kind == kKey ? p.Hq : p.Hq + p.Hkv;
+  const __nv_bfloat16* x = p.x + static_cast<long long>(u.t) * p.row_elems + static_cast<long long>(first + h0) * D + i0;
   uint4 raw[UNR];
-  const __nv_bfloat16* x = p.x + static_cast<long long>(t) * p.row_elems + i0;
 #pragma unroll
-  for (int u = 0; u < UNR; ++u) {
-    const int h = row0 + u * RPW;
-    raw[u] = h < heads ? ld_stream(x + static_cast<long long>(h) * D) : make_uint4(0, 0, 0, 0);
+  for (int s = 0; s < UNR; ++s)
+    raw[s] = h0 + s * RPW < u.heads ? ld_stream(x + s * RPW * D) : make_uint4(0, 0, 0, 0);
+  long long head;
+  __nv_bfloat16* dst = place<D>(p, u, head);
+  if (!dst) return;
+  dst += h0 * head + i0;
+  if (u.kind == kValue) {
+#pragma unroll
+    for (int s = 0; s < UNR; ++s)
+      if (h0 + s * RPW < u.heads) __stcs(reinterpret_cast<uint4*>(dst + s * RPW * head), raw[s]);
+    return;
   }
-  float c[8], s[8], wq[8], wk[8];
-  int src;
-  load_angles<D, INTER, false>(p, t, lane, c, s, src);
-  load_weight<W_F32>(p.wq, i0, wq);
-  load_weight<W_F32>(p.wk, i0, wk);
-  long long q_head, kv_head;
-  const long long q_tok = place_token<D>(p.q_at, t, q_head);
-  long long kv_tok;
-  bool kv_ok = true;
-  if (p.kv_at.slots) {
-    const int slot = __ldg(p.kv_at.slots + t);
-    kv_ok = slot >= 0 && slot < p.kv_at.n_slots;
-    const int page = kv_ok ? slot / p.kv_at.page : 0;
-    kv_tok = page * p.kv_at.page_elems + static_cast<long long>(slot - page * p.kv_at.page) * p.kv_at.row_elems;
-    kv_head = p.kv_at.head_elems;
-  } else {
-    kv_tok = place_token<D>(p.kv_at, t, kv_head);
-  }
+  const int src = partner_lane<D, INTER>(p, lane);
+  uint64_t a[4], b[4];
+  {
+    float c[8], s[8], w[8], wp[8];
+    load_angles<D, INTER, false>(p, u.t, lane, c, s);
+    load_weight(p, u.kind, i0, w);
+    load_weight(p, u.kind, 8 * (src % LPH), wp);
 #pragma unroll
-  for (int u = 0; u < UNR; ++u) {
-    const int h = row0 + u * RPW;
-    const bool is_q = h < p.Hq, is_v = h >= p.Hq + p.Hkv;
-    float z[8], y[8];
-    unpack8(raw[u], z);
-    float ss = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) ss = fmaf(z[i], z[i], ss);
-    const float r = rsqrtf(head_sum<LPH>(ss) * (1.f / D) + p.eps);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) z[i] = z[i] * r * (is_q ? wq[i] : wk[i]);
-    rotate8<INTER>(z, c, s, src, y);
-    const uint4 out = is_v ? raw[u] : pack8(y);
-    if (h < heads && (is_q || kv_ok)) {
-      __nv_bfloat16* dst = is_q ? p.q + q_tok + h * q_head
-                           : is_v ? p.v + kv_tok + (h - p.Hq - p.Hkv) * kv_head
-                                  : p.k + kv_tok + (h - p.Hq) * kv_head;
-      *reinterpret_cast<uint4*>(dst + i0) = out;
+    for (int i = 0; i < 4; ++i) {
+      a[i] = f2(w[2 * i] * c[2 * i], w[2 * i + 1] * c[2 * i + 1]);
+      b[i] = INTER ? f2(wp[2 * i + 1] * s[2 * i], wp[2 * i] * s[2 * i + 1]) : f2(wp[2 * i] * s[2 * i], wp[2 * i + 1] * s[2 * i + 1]);
     }
+  }
+#pragma unroll
+  for (int s = 0; s < UNR; ++s) {
+    uint64_t z[4], o[4];
+    unpack8(raw[s], z);
+    unpack8(partners<INTER>(raw[s], src), o);
+    const float r = rsqrtf(head_sum<LPH>(sum8(z, z)) * (1.f / D) + p.eps);
+    const uint64_t r2 = f2(r, r);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) z[i] = mul2(fma2(o[i], b[i], mul2(z[i], a[i])), r2);
+    if (h0 + s * RPW < u.heads) __stcs(reinterpret_cast<uint4*>(dst + s * RPW * head), pack8(z));
   }
 }
 
-// The gradients.  Blocks walk the (token, share) units in a fixed order, each lane adding up what
-// its eight values give to the weights' gradients; a block's sum goes to the workspace, where
-// qkv_weight_grad_kernel adds the blocks' in their order: no atomics, the same bits each time.
-template <int D, bool INTER, bool W_F32, int UNR>
-__global__ void __launch_bounds__(kWarps * 32) qkv_norm_rope_bwd_kernel(const QkvParams p) {
+// The gradients.  With g the rotation transposed of dy and u = g w:  dx = r u - x r^3 mean(u x) and
+// dw += r g x.  A warp takes the same heads of every so many tokens (the grid's warps are a multiple
+// of a token's units), each lane adding up what its eight values give to the weight's gradient; a
+// block's sum goes to the workspace, where qkv_weight_grad_kernel adds the blocks' in their order: no
+// atomics, the same bits each time.
+template <int D, bool INTER, int UNR>
+__global__ void __launch_bounds__(kWarps * 32, 2) qkv_norm_rope_bwd_kernel(const QkvParams p) {
   constexpr int LPH = D / 8, RPW = 32 / LPH;
   __shared__ float sums[kWarps][2 * D];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, i0 = 8 * (lane % LPH);
-  const int heads = p.Hq + 2 * p.Hkv;
-  float wq[8], wk[8], gq[8], gk[8];
-  load_weight<W_F32>(p.wq, i0, wq);
-  load_weight<W_F32>(p.wk, i0, wk);
+  const int src = partner_lane<D, INTER>(p, lane);
+  Unit u = unit_of<D, UNR>(p, static_cast<long long>(blockIdx.x) * kWarps + warp);
+  const int tokens = static_cast<int>(gridDim.x) * kWarps / (p.q_units + 2 * p.kv_units);  // from one to the next
+  const int h0 = u.h0 + lane / LPH;
+  const int first = u.kind == kQuery ? 0 : u.kind == kKey ? p.Hq : p.Hq + p.Hkv;
+  const long long at = static_cast<long long>(first + h0) * D + i0;
+  uint64_t w[4], gw[4];
+  {
+    float wf[8];
+    load_weight(p, u.kind, i0, wf);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) gq[i] = gk[i] = 0.f;
-  const long long step = static_cast<long long>(gridDim.x) * kWarps;
-  for (long long unit = static_cast<long long>(blockIdx.x) * kWarps + warp; unit < p.units; unit += step) {
-    const int t = static_cast<int>(unit / p.chunks);
-    const int row0 = static_cast<int>(unit - static_cast<long long>(t) * p.chunks) * (RPW * UNR) + lane / LPH;
-    long long q_head, kv_head;
-    const long long q_tok = place_token<D>(p.q_at, t, q_head), kv_tok = place_token<D>(p.kv_at, t, kv_head);
-    const __nv_bfloat16* x = p.x + static_cast<long long>(t) * p.row_elems + i0;
+    for (int i = 0; i < 4; ++i) {
+      w[i] = f2(wf[2 * i], wf[2 * i + 1]);
+      gw[i] = f2(0.f, 0.f);
+    }
+  }
+  for (; u.t < p.T; u.t = p.T - u.t > tokens ? u.t + tokens : p.T) {
+    const __nv_bfloat16* x = p.x + static_cast<long long>(u.t) * p.row_elems + at;
+    __nv_bfloat16* dx = p.dx + static_cast<long long>(u.t) * p.drow_elems + at;
+    long long head;
+    const __nv_bfloat16* dy = place<D>(p, u, head) + i0;
+    dy += h0 * head;
     uint4 rdy[UNR], rx[UNR];
 #pragma unroll
-    for (int u = 0; u < UNR; ++u) {
-      const int h = row0 + u * RPW;
-      const bool is_q = h < p.Hq, is_v = h >= p.Hq + p.Hkv;
-      rdy[u] = rx[u] = make_uint4(0, 0, 0, 0);
-      if (h < heads) {
-        const __nv_bfloat16* dy = is_q ? p.q + q_tok + h * q_head
-                                  : is_v ? p.v + kv_tok + (h - p.Hq - p.Hkv) * kv_head
-                                         : p.k + kv_tok + (h - p.Hq) * kv_head;
-        rdy[u] = ld_stream(dy + i0);
-        if (!is_v) rx[u] = ld_stream(x + static_cast<long long>(h) * D);
+    for (int s = 0; s < UNR; ++s) {
+      const bool in = h0 + s * RPW < u.heads;
+      rdy[s] = in ? ld_stream(dy + s * RPW * head) : make_uint4(0, 0, 0, 0);
+      rx[s] = in && u.kind != kValue ? ld_stream(x + s * RPW * D) : make_uint4(0, 0, 0, 0);
+    }
+    if (u.kind == kValue) {
+#pragma unroll
+      for (int s = 0; s < UNR; ++s)
+        if (h0 + s * RPW < u.heads) __stcs(reinterpret_cast<uint4*>(dx + s * RPW * D), rdy[s]);
+      continue;
+    }
+    uint64_t c[4], s[4];
+    {
+      float cf[8], sf[8];
+      load_angles<D, INTER, true>(p, u.t, lane, cf, sf);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        c[i] = f2(cf[2 * i], cf[2 * i + 1]);
+        s[i] = f2(sf[2 * i], sf[2 * i + 1]);
       }
     }
-    float c[8], s[8];
-    int src;
-    load_angles<D, INTER, true>(p, t, lane, c, s, src);
 #pragma unroll
-    for (int u = 0; u < UNR; ++u) {
-      const int h = row0 + u * RPW;
-      const bool is_q = h < p.Hq, is_v = h >= p.Hq + p.Hkv;
-      float n[8], dy[8], g[8];
-      unpack8(rx[u], n);
-      unpack8(rdy[u], dy);
-      rotate8<INTER>(dy, c, s, src, g);
-      float ss = 0.f;
+    for (int k = 0; k < UNR; ++k) {
+      uint64_t z[4], g[4], o[4];
+      unpack8(rx[k], z);
+      unpack8(rdy[k], g);
+      unpack8(partners<INTER>(rdy[k], src), o);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) ss = fmaf(n[i], n[i], ss);
-      const float r = rsqrtf(head_sum<LPH>(ss) * (1.f / D) + p.eps);
-      float dot = 0.f;
+      for (int i = 0; i < 4; ++i) g[i] = fma2(o[i], s[i], mul2(g[i], c[i]));
+      const float r = rsqrtf(head_sum<LPH>(sum8(z, z)) * (1.f / D) + p.eps);
+      const uint64_t r2 = f2(r, r);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        n[i] *= r;
-        const float gn = is_v ? 0.f : g[i] * n[i];
-        if (is_q)
-          gq[i] += gn;
-        else
-          gk[i] += gn;
-        g[i] *= is_q ? wq[i] : wk[i];
-        dot = fmaf(g[i], n[i], dot);
+      for (int i = 0; i < 4; ++i) {
+        gw[i] = fma2(mul2(g[i], z[i]), r2, gw[i]);
+        g[i] = mul2(g[i], w[i]);
       }
-      dot = head_sum<LPH>(dot) * (1.f / D);
+      const float m = -(r * r) * (head_sum<LPH>(sum8(g, z)) * (1.f / D));
+      const uint64_t m2 = f2(m, m);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) g[i] = r * fmaf(-dot, n[i], g[i]);
-      if (h < heads)
-        *reinterpret_cast<uint4*>(p.dx + static_cast<long long>(t) * p.drow_elems + static_cast<long long>(h) * D + i0) =
-            is_v ? rdy[u] : pack8(g);
+      for (int i = 0; i < 4; ++i) g[i] = mul2(fma2(z[i], m2, g[i]), r2);
+      if (h0 + k * RPW < u.heads) __stcs(reinterpret_cast<uint4*>(dx + k * RPW * D), pack8(g));
     }
   }
   // the warp's head groups, then the block's warps
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
+    float a = i & 1 ? f2hi(gw[i / 2]) : f2lo(gw[i / 2]);
 #pragma unroll
-    for (int m = LPH; m < 32; m <<= 1) {
-      gq[i] += __shfl_xor_sync(0xffffffffu, gq[i], m);
-      gk[i] += __shfl_xor_sync(0xffffffffu, gk[i], m);
-    }
-  }
-  if (lane < LPH) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      sums[warp][i0 + i] = gq[i];
-      sums[warp][D + i0 + i] = gk[i];
+    for (int m = LPH; m < 32; m <<= 1) a += __shfl_xor_sync(0xffffffffu, a, m);
+    if (lane < LPH) {
+      sums[warp][i0 + i] = u.kind == kQuery ? a : 0.f;
+      sums[warp][D + i0 + i] = u.kind == kKey ? a : 0.f;
     }
   }
   __syncthreads();
@@ -296,22 +346,27 @@ __global__ void __launch_bounds__(kWarps * 32) qkv_norm_rope_bwd_kernel(const Qk
   }
 }
 
-// Adds the blocks' partial sums [n][2 D] in a fixed order: a block takes 32 of the 2 D columns.
+// Adds the blocks' partial sums [n][2 D] in a fixed order: a block takes 8 of the 2 D columns, 128
+// threads each.
 __global__ void __launch_bounds__(1024) qkv_weight_grad_kernel(const float* partial, int n, int D, float* dwq, float* dwk) {
-  __shared__ float sums[32][33];
+  __shared__ float sums[128][9], parts[4][8];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;");
-  const int x = threadIdx.x & 31, y = threadIdx.x >> 5, col = blockIdx.x * 32 + x;
+  const int x = threadIdx.x & 7, y = threadIdx.x >> 3;
   float a = 0.f;
-  for (int i = y; i < n; i += 32) a += partial[static_cast<size_t>(i) * (2 * D) + col];
+#pragma unroll 4
+  for (int i = y; i < n; i += 128) a += partial[static_cast<size_t>(i) * (2 * D) + blockIdx.x * 8 + x];
   sums[y][x] = a;
   __syncthreads();
-  a = sums[x][y];  // column y's sum over the rows that thread row x took
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;  // warp: column warp % 8, rows 32 (warp / 8) ..
+  a = sums[(warp >> 3) * 32 + lane][warp & 7];
 #pragma unroll
   for (int m = 16; m > 0; m >>= 1) a += __shfl_xor_sync(0xffffffffu, a, m);
-  if (x == 0) {
-    const int i = blockIdx.x * 32 + y;
-    (i < D ? dwq[i] : dwk[i - D]) = a;
+  if (lane == 0) parts[warp >> 3][warp & 7] = a;
+  __syncthreads();
+  if (threadIdx.x < 8) {
+    const int i = blockIdx.x * 8 + x;
+    (i < D ? dwq[i] : dwk[i - D]) = (parts[0][x] + parts[1][x]) + (parts[2][x] + parts[3][x]);
   }
 }
 
@@ -337,6 +392,7 @@ QkvParams params_of(const QkvArgs& a, int unroll) {
   p.row_elems = a.row_elems;
   p.wq = a.q_weight;
   p.wk = a.k_weight;
+  p.w_f32 = a.weights_f32;
   p.cos = a.cos;
   p.sin = a.sin;
   p.pos = a.positions;
@@ -345,9 +401,10 @@ QkvParams params_of(const QkvArgs& a, int unroll) {
   p.Hkv = a.Hkv;
   p.R = a.R;
   p.P = a.P;
-  const int rows = 256 / a.D * unroll;  // heads that a warp takes
-  p.chunks = (a.Hq + 2 * a.Hkv + rows - 1) / rows;
-  p.units = static_cast<long long>(a.T) * p.chunks;
+  const int heads = 256 / a.D * unroll;  // of a unit
+  p.q_units = (a.Hq + heads - 1) / heads;
+  p.kv_units = (a.Hkv + heads - 1) / heads;
+  p.units = static_cast<long long>(a.T) * (p.q_units + 2 * p.kv_units);
   p.eps = a.eps;
   p.q_at = a.q_at;
   p.kv_at = a.kv_at;
@@ -366,32 +423,30 @@ cudaError_t launch_fwd_u(const QkvArgs& a, cudaStream_t stream) {
   const long long blocks = (p.units + kWarps - 1) / kWarps;
   if (blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
   const int g = static_cast<int>(blocks);
-  if (a.interleaved)
-    return a.weights_f32 ? launch(qkv_norm_rope_kernel<D, true, true, UNR>, g, kWarps * 32, stream, p)
-                         : launch(qkv_norm_rope_kernel<D, true, false, UNR>, g, kWarps * 32, stream, p);
-  return a.weights_f32 ? launch(qkv_norm_rope_kernel<D, false, true, UNR>, g, kWarps * 32, stream, p)
-                       : launch(qkv_norm_rope_kernel<D, false, false, UNR>, g, kWarps * 32, stream, p);
+  return a.interleaved ? launch(qkv_norm_rope_kernel<D, true, UNR>, g, kWarps * 32, stream, p)
+                       : launch(qkv_norm_rope_kernel<D, false, UNR>, g, kWarps * 32, stream, p);
 }
 
 template <int D>
 cudaError_t launch_fwd_d(const QkvArgs& a, cudaStream_t stream) {
-  return launch_fwd_u<D, 4>(a, stream);
+  return static_cast<long long>(a.T) * (a.Hq + 2 * a.Hkv) * D >= kManyValues ? launch_fwd_u<D, kSteps>(a, stream)
+                                                                           : launch_fwd_u<D, kFewSteps>(a, stream);
 }
 
-template <int D, int UNR>
-cudaError_t launch_bwd_u(const QkvArgs& a, cudaStream_t stream) {
-  const QkvParams p = params_of(a, UNR);
-  const long long blocks = (p.units + kWarps - 1) / kWarps;
-  const int g = static_cast<int>(blocks < kMaxBwdBlocks ? blocks : kMaxBwdBlocks);
-  cudaError_t e;
-  if (a.interleaved)
-    e = a.weights_f32 ? launch(qkv_norm_rope_bwd_kernel<D, true, true, UNR>, g, kWarps * 32, stream, p)
-                      : launch(qkv_norm_rope_bwd_kernel<D, true, false, UNR>, g, kWarps * 32, stream, p);
-  else
-    e = a.weights_f32 ? launch(qkv_norm_rope_bwd_kernel<D, false, true, UNR>, g, kWarps * 32, stream, p)
-                      : launch(qkv_norm_rope_bwd_kernel<D, false, false, UNR>, g, kWarps * 32, stream, p);
+template <int D>
+cudaError_t launch_bwd_d(const QkvArgs& a, cudaStream_t stream) {
+  const QkvParams p = params_of(a, kSteps);
+  // blocks whose warps are a multiple of a token's units, as many as there is room for or need of
+  const int per = p.q_units + 2 * p.kv_units;
+  int unit = 1;
+  while (unit * kWarps % per) ++unit;
+  if (unit > kMaxBwdBlocks) return cudaErrorInvalidConfiguration;
+  const long long need = (p.units + static_cast<long long>(unit) * kWarps - 1) / (static_cast<long long>(unit) * kWarps);
+  const int most = kMaxBwdBlocks / unit, g = static_cast<int>(need < most ? need : most) * unit;
+  const cudaError_t e = a.interleaved ? launch(qkv_norm_rope_bwd_kernel<D, true, kSteps>, g, kWarps * 32, stream, p)
+                                      : launch(qkv_norm_rope_bwd_kernel<D, false, kSteps>, g, kWarps * 32, stream, p);
   if (e != cudaSuccess) return e;
-  return launch(qkv_weight_grad_kernel, 2 * D / 32, 1024, stream, static_cast<const float*>(p.partial), g, D, a.dq_weight,
+  return launch(qkv_weight_grad_kernel, 2 * D / 8, 1024, stream, static_cast<const float*>(p.partial), g, D, a.dq_weight,
                 a.dk_weight);
 }
 
@@ -402,7 +457,7 @@ cudaError_t launch_qkv_norm_rope(const QkvArgs& a, cudaStream_t stream) {
 }
 
 cudaError_t launch_qkv_norm_rope_bwd(const QkvArgs& a, cudaStream_t stream) {
-  return a.D == 128 ? launch_bwd_u<128, 4>(a, stream) : launch_bwd_u<64, 4>(a, stream);
+  return a.D == 128 ? launch_bwd_d<128>(a, stream) : launch_bwd_d<64>(a, stream);
 }
 
 size_t qkv_bwd_workspace_bytes(int D) { return static_cast<size_t>(kMaxBwdBlocks) * 2 * D * sizeof(float); }
