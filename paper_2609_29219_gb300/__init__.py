@@ -197,10 +197,11 @@ _bf16 = _f32 = _i32 = _u8 = None  # torch's types
 
 
 _empty_strided_cuda = None
+_fast = None  # the compiled binding, where it can be used
 
 
 def _torch():
-    global _torch_mod, _empty_strided_cuda, _bf16, _f32, _i32, _u8
+    global _torch_mod, _empty_strided_cuda, _bf16, _f32, _i32, _u8, _fast
     if _torch_mod is None:
         import torch
         try:  # what torch's generated code allocates by: no dispatch, on the current device
@@ -212,7 +213,36 @@ def _torch():
             pass
         _bf16, _f32, _i32, _u8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
         _torch_mod = torch
+        _fast = _compiled_binding(torch)
     return _torch_mod
+
+
+def _compiled_binding(torch):
+    """The compiled binding (csrc/binding.cpp), or None where it was not built or torch lacks what it
+    calls."""
+    c = torch._C
+    if _empty_strided_cuda is None or not hasattr(c, "_cuda_getCurrentRawStream"):
+        return None
+    try:
+        from . import _binding
+    except ImportError:
+        return None
+    lib = capi()
+    _binding.set_up(
+        (torch.Tensor, torch.nn.Parameter, _bf16, _f32, _i32, _u8, _empty_strided_cuda, c._cuda_getCurrentRawStream,
+         c._len_torch_dispatch_stack, c._len_torch_function_stack, c._get_deterministic_algorithms, c._cuda_getDevice),
+        tuple(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in (
+            "loom_attn_bwd", "loom_attn_bwd_workspace_bytes", "loom_attn_bwd_varlen", "loom_attn_bwd_varlen_workspace_bytes",
+            "loom_qkv_norm_rope", "loom_qkv_norm_rope_cache", "loom_qkv_norm_rope_bwd",
+            "loom_qkv_norm_rope_bwd_workspace_bytes")))
+    return _binding
+
+
+def _fast_result(r, where):
+    """The compiled binding's outputs; it returned a status where the C call refused."""
+    if type(r) is tuple:
+        return r
+    raise LoomError(r, where)
 
 
 def _new(shape, strides, dtype, t, like=False):
@@ -498,9 +528,11 @@ def _norm_bwd_need(D):
 
 
 # The checks of the entry points below take most of a small call's time if each tensor goes through
-# _ptr, so they are one expression that names nothing, and what fails it is looked at again by name.
-# GB300 host, us per call before and after (C call in it): backward of 128 rows 25.0 -> BWD_US (6.4),
-# norm and rotation 17.6 -> NORM_US (3.8), into a cache 14.4 -> CACHE_US (3.8), its gradients 27.2 -> NBWD_US (5.5).
+# _ptr, so they are one expression that names nothing, and what fails it is looked at again by name;
+# and the common case goes through the compiled binding.  GB300 host, us per call with _ptr / one
+# expression / compiled (the C call in it): backward of 128 rows 25.0 / 19.9 / 16.5 (4), norm and
+# rotation 17.6 / 14.7 / 11.6 (2), into a cache 14.4 / 12.9 / 9.1 (2), its gradients 27.2 / 22.1 /
+# 17.0 (3).  Each output takes 0.9 of it.
 def _bwd_checked(do, q, k, v, o, lse, dlse, dq, dk, dv, ndim):
     """The backward entry points' tensors, named if they are not what they should be."""
     for t, name in ((q, "q"), (k, "k"), (v, "v"), (do, "do"), (o, "o")):
@@ -551,6 +583,10 @@ def loom_attn_bwd(do, q, k, v, o, lse, dq=None, dk=None, dv=None, workspace=None
     ``workspace`` is a CUDA uint8 tensor of at least ``loom_attn_bwd_workspace_bytes`` bytes
     (allocated here if None).  Writes and returns ``dq, dk, dv`` (allocated if None)."""
     _torch()
+    if _fast is not None and dq is None and dk is None and dv is None and workspace is None and stream is None:
+        r = _fast.attn_bwd(do, q, k, v, o, lse, dlse, causal, scale)
+        if r is not None:
+            return _fast_result(r, "loom_attn_bwd")
     try:
         qs, ks = q.shape, k.shape
         B, Hq, Sq, D = qs
@@ -591,6 +627,10 @@ def loom_attn_bwd_varlen(do, q, k, v, o, lse, cu_seqlens_q, cu_seqlens_k, max_se
     lse (and dlse) [Hq, total_q]; cu_seqlens_q / cu_seqlens_k [B + 1] int32 on the device; the
     longest lengths as ints.  Writes and returns ``dq, dk, dv`` (allocated if None)."""
     _torch()
+    if _fast is not None and dq is None and dk is None and dv is None and workspace is None and stream is None:
+        r = _fast.attn_bwd_varlen(do, q, k, v, o, lse, dlse, causal, scale, cu_seqlens_q, cu_seqlens_k, max_seqlen_q, max_seqlen_k)
+        if r is not None:
+            return _fast_result(r, "loom_attn_bwd_varlen")
     try:
         qs, ks = q.shape, k.shape
         total_q, Hq, D = qs
@@ -697,6 +737,11 @@ def loom_qkv_norm_rope(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_head
     [D] bf16 or fp32; cos, sin [positions, rotary_dim / 2] fp32; positions [T] int32 (None: t, or t %
     seq_len).  Writes and returns ``q, k, v`` (allocated if None): [T, H, D], or with ``seq_len``
     [T / seq_len, H, seq_len, D], as the ragged and the dense prefill take them."""
+    _torch()
+    if _fast is not None and q is None and k is None and v is None and stream is None:
+        r = _fast.norm_rope(qkv, q_weight, k_weight, cos, sin, positions, interleaved, eps, num_heads, num_kv_heads, seq_len)
+        if r is not None:
+            return _fast_result(r, "loom_qkv_norm_rope")
     T, D, row, norm = _norm_operands(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, positions, interleaved)
     S = seq_len
     if S < 0 or (S and T % S):
@@ -744,6 +789,11 @@ def loom_qkv_norm_rope_cache(qkv, q_weight, k_weight, cos, sin, positions, slots
     if layout not in ("nhd", "hnd"):
         raise ValueError("layout is 'nhd' or 'hnd'")
     _torch()
+    if _fast is not None and q is None and stream is None:
+        r = _fast.norm_rope_cache(qkv, q_weight, k_weight, cos, sin, positions, interleaved, eps, num_heads, slots, k_cache,
+                                  v_cache, layout == "hnd")
+        if r is not None:
+            return _fast_result(r, "loom_qkv_norm_rope_cache")[0]
     try:
         cs = k_cache.shape
         pages, a, b, Dk = cs
@@ -781,6 +831,10 @@ def loom_qkv_norm_rope_bwd(dq, dk, dv, qkv, q_weight, k_weight, cos, sin, positi
     its rows may lie further apart), ``dq_weight`` and ``dk_weight`` ([D] fp32), allocated if None.
     ``workspace``: a CUDA uint8 tensor of ``loom_qkv_norm_rope_bwd_workspace_bytes(D)`` bytes."""
     _torch()
+    if _fast is not None and dqkv is None and dq_weight is None and dk_weight is None and workspace is None and stream is None:
+        r = _fast.norm_rope_bwd(qkv, q_weight, k_weight, cos, sin, positions, interleaved, eps, dq, dk, dv)
+        if r is not None:
+            return _fast_result(r, "loom_qkv_norm_rope_bwd")
     try:
         qs, ks = dq.shape, dk.shape
         ndim, Hq, Hkv = len(qs), qs[1], ks[1]

@@ -1,19 +1,24 @@
 """Build the CUDA library ``libloomattn.so`` in-tree for sm_103a (GB300).
 
 Each translation unit is compiled by nvcc in parallel, then linked into one shared
-library next to this file.  No CMake, no torch extension machinery.
+library next to this file.  No CMake, no torch extension machinery.  Beside it
+``_binding.so``, the short way from Python to the entry points around training and serving
+(plain CPython API; where the interpreter's headers are missing it is left out, and the
+package's Python code does the same).
 """
 from __future__ import annotations
 
 import os
 import shutil
 import subprocess
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libloomattn.so")
+BINDING = os.path.join(HERE, "_binding.so")
 SOURCES = ["loom_api.cu", "attn_fwd.cu", "attn_decode.cu", "loom_noalloc.cu", "gemm.cu",
            "attn_bwd.cu", "qkv_rope.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
@@ -62,6 +67,12 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) 
         if verbose or ptxas_info:
             print(r.stdout + r.stderr)
 
+    src, include = os.path.join(CSRC, "binding.cpp"), sysconfig.get_paths()["include"]
+    if os.path.exists(os.path.join(include, "Python.h")) and (
+            force or _stale(BINDING, [src, os.path.join(os.path.dirname(HERE), "include", "loom_attn.h")])):
+        tmp = BINDING + f".tmp{os.getpid()}"
+        run(["g++", "-O2", "-std=c++17", "-Wall", "-fPIC", "-shared", f"-I{include}", src, "-o", tmp])
+        os.replace(tmp, BINDING)
     if jobs:
         with ThreadPoolExecutor(max_workers=len(jobs)) as ex:
             list(ex.map(run, jobs))
