@@ -218,19 +218,15 @@ def _torch():
 
 
 def _compiled_binding(torch):
-    """The compiled binding (csrc/binding.cpp), or None where it was not built or torch lacks what it
-    calls."""
-    c = torch._C
-    if _empty_strided_cuda is None or not hasattr(c, "_cuda_getCurrentRawStream"):
-        return None
+    """The compiled binding (csrc/binding.cpp), or None where it was not built, or for another torch."""
     try:
         from . import _binding
     except ImportError:
         return None
+    if not torch.__version__.startswith(_binding.torch_version):
+        return None
     lib = capi()
     _binding.set_up(
-        (torch.Tensor, torch.nn.Parameter, _bf16, _f32, _i32, _u8, _empty_strided_cuda, c._cuda_getCurrentRawStream,
-         c._len_torch_dispatch_stack, c._len_torch_function_stack, c._get_deterministic_algorithms, c._cuda_getDevice),
         tuple(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in (
             "loom_attn_bwd", "loom_attn_bwd_workspace_bytes", "loom_attn_bwd_varlen", "loom_attn_bwd_varlen_workspace_bytes",
             "loom_qkv_norm_rope", "loom_qkv_norm_rope_cache", "loom_qkv_norm_rope_bwd",
@@ -530,9 +526,9 @@ def _norm_bwd_need(D):
 # The checks of the entry points below take most of a small call's time if each tensor goes through
 # _ptr, so they are one expression that names nothing, and what fails it is looked at again by name;
 # and the common case goes through the compiled binding.  GB300 host, us per call with _ptr / one
-# expression / compiled (the C call in it): backward of 128 rows 25.0 / 19.9 / 16.5 (4), norm and
-# rotation 17.6 / 14.7 / 11.6 (2), into a cache 14.4 / 12.9 / 9.1 (2), its gradients 27.2 / 22.1 /
-# 17.0 (3).  Each output takes 0.9 of it.
+# expression / compiled (the C call in it): backward of 128 rows 25.0 / 19.9 / 9.5 (4), norm and
+# rotation 17.6 / 14.7 / 5.5 (2), into a cache 14.4 / 12.9 / 3.9 (2), its gradients 27.2 / 22.1 /
+# 8.4 (3).
 def _bwd_checked(do, q, k, v, o, lse, dlse, dq, dk, dv, ndim):
     """The backward entry points' tensors, named if they are not what they should be."""
     for t, name in ((q, "q"), (k, "k"), (v, "v"), (do, "do"), (o, "o")):

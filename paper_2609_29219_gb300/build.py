@@ -3,11 +3,12 @@
 Each translation unit is compiled by nvcc in parallel, then linked into one shared
 library next to this file.  No CMake, no torch extension machinery.  Beside it
 ``_binding.so``, the short way from Python to the entry points around training and serving
-(plain CPython API; where the interpreter's headers are missing it is left out, and the
-package's Python code does the same).
+(it looks at tensors through torch's C++ interface; where the interpreter's or torch's headers
+are missing it is left out, and the package's Python code does the same).
 """
 from __future__ import annotations
 
+import importlib.util
 import os
 import shutil
 import subprocess
@@ -45,6 +46,24 @@ def _stale(target: str, deps) -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def _binding_job(force: bool):
+    """The command that compiles the binding, and the file it writes; None where there is nothing to do."""
+    src, python = os.path.join(CSRC, "binding.cpp"), sysconfig.get_paths()["include"]
+    spec = importlib.util.find_spec("torch")
+    torch = os.path.dirname(spec.origin) if spec and spec.origin else ""
+    needs = [os.path.join(python, "Python.h"), os.path.join(torch, "include", "torch", "csrc", "autograd", "python_variable.h"),
+             os.path.join(torch, "lib", "libtorch_python.so")]
+    deps = [src, os.path.join(os.path.dirname(HERE), "include", "loom_attn.h"), os.path.join(torch, "version.py")]
+    if not all(map(os.path.exists, needs)) or not (force or _stale(BINDING, deps)):
+        return None
+    cuda = os.path.dirname(os.path.dirname(_nvcc()))
+    tmp = BINDING + f".tmp{os.getpid()}"
+    return ["g++", "-O2", "-std=c++17", "-Wall", "-fPIC", "-shared", f"-I{python}", "-isystem", os.path.join(torch, "include"),
+            "-isystem", os.path.join(torch, "include", "torch", "csrc", "api", "include"),
+            "-isystem", os.path.join(cuda, "include"), src, "-o", tmp, f"-L{os.path.join(torch, 'lib')}",
+            "-ltorch_python", "-ltorch_cuda", "-lc10_cuda", "-ltorch_cpu", "-lc10"], tmp
+
+
 def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) -> str:
     """Compile (if needed) and return the path of ``libloomattn.so``."""
     os.makedirs(BUILD, exist_ok=True)
@@ -60,23 +79,23 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) 
             extra = ["-Xptxas", "-v"] if ptxas_info else []
             jobs.append([nvcc, *FLAGS, *extra, "-c", s, "-o", o])
 
+    binding = _binding_job(force)
+    if binding:
+        jobs.append(binding[0])
+
     def run(cmd):
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:
-            raise RuntimeError(f"nvcc failed ({' '.join(cmd)}):\n{r.stdout}\n{r.stderr}")
+            raise RuntimeError(f"{os.path.basename(cmd[0])} failed ({' '.join(cmd)}):\n{r.stdout}\n{r.stderr}")
         if verbose or ptxas_info:
             print(r.stdout + r.stderr)
 
-    src, include = os.path.join(CSRC, "binding.cpp"), sysconfig.get_paths()["include"]
-    if os.path.exists(os.path.join(include, "Python.h")) and (
-            force or _stale(BINDING, [src, os.path.join(os.path.dirname(HERE), "include", "loom_attn.h")])):
-        tmp = BINDING + f".tmp{os.getpid()}"
-        run(["g++", "-O2", "-std=c++17", "-Wall", "-fPIC", "-shared", f"-I{include}", src, "-o", tmp])
-        os.replace(tmp, BINDING)
     if jobs:
         with ThreadPoolExecutor(max_workers=len(jobs)) as ex:
             list(ex.map(run, jobs))
-    if force or jobs or _stale(LIB, objs):
+    if binding:
+        os.replace(binding[1], BINDING)
+    if force or _stale(LIB, objs):
         tmp = LIB + f".tmp{os.getpid()}"
         run([nvcc, *ARCH, "-shared", "-o", tmp, *objs])
         os.replace(tmp, LIB)

@@ -122,3 +122,36 @@ def test_errors_are_the_same(loom, monkeypatch):
         if way == "compiled":
             first = kinds
     assert first == kinds
+
+
+def test_out_of_memory_is_torchs_error(loom, monkeypatch):
+    """Where an output cannot be allocated both ways raise what torch raises, and the next call works."""
+    import torch
+    x = torch.randn((4096, 8 * 128), device="cuda").bfloat16()
+    w, cos = torch.ones(128, device="cuda").bfloat16(), torch.rand((4096, 32), device="cuda")
+    call = lambda: loom.loom_qkv_norm_rope(x, w, w, cos, cos, 4, 2)  # noqa: E731
+    want = [t.clone() for t in call()]
+    for way in ("compiled", "python"):
+        if way == "python":
+            monkeypatch.setattr(loom, "_fast", None)
+        torch.cuda.synchronize()
+        torch.cuda.empty_cache()
+        torch.cuda.set_per_process_memory_fraction(1e-6)
+        try:
+            with pytest.raises(torch.OutOfMemoryError):
+                hold = [call() for _ in range(64)]  # noqa: F841
+        finally:
+            torch.cuda.set_per_process_memory_fraction(1.0)
+        assert all(torch.equal(a, b) for a, b in zip(want, call()))
+
+
+def test_a_function_transform_is_refused_both_ways(loom, monkeypatch):
+    """A batched tensor of torch.func has no memory of its own: the call names that, it reads nothing."""
+    import torch
+    w, cos = torch.ones(64, device="cuda").bfloat16(), torch.rand((8, 32), device="cuda")
+    x = torch.randn((3, 8, 4 * 64), device="cuda").bfloat16()
+    for way in ("compiled", "python"):
+        if way == "python":
+            monkeypatch.setattr(loom, "_fast", None)
+        with pytest.raises(Exception):
+            torch.func.vmap(lambda t: loom.loom_qkv_norm_rope(t, w, w, cos, cos, 2, 1)[0])(x)
