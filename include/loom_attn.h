@@ -326,7 +326,8 @@ loom_status loom_qkv_norm_rope_cache(const void* qkv, int64_t qkv_stride, const 
  *   dq_weight, dk_weight  [D] fp32, written: summed over all tokens and heads in a fixed order
  *   workspace  device scratch of at least loom_qkv_norm_rope_bwd_workspace_bytes(D) bytes, whose
  *              contents on entry do not matter; it serves one call at a time.
- * Errors: as loom_qkv_norm_rope, WORKSPACE.  T = 0 writes zeros to dq_weight and dk_weight.
+ * Errors: as loom_qkv_norm_rope; WORKSPACE; more than 16384 heads (Hq + 2 Hkv): UNSUPPORTED.  T = 0
+ * writes zeros to dq_weight and dk_weight.
  */
 loom_status loom_qkv_norm_rope_bwd(const void* dq, const void* dk, const void* dv, const void* qkv,
                                    int64_t qkv_stride, const void* q_weight, const void* k_weight,

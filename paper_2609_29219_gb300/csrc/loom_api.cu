@@ -509,6 +509,7 @@ loom_status loom_qkv_norm_rope_bwd(const void* dq, const void* dk, const void* d
   if (seq_len < 0 || (seq_len > 0 && T % seq_len) || (T > 0 && (!dq || !dk || !dv || !dqkv))) return LOOM_ERR_INVALID_ARG;
   if (!dq_weight || !dk_weight) return LOOM_ERR_INVALID_ARG;
   if (dqkv_stride < (static_cast<int64_t>(Hq) + 2ll * Hkv) * D) return LOOM_ERR_INVALID_ARG;
+  if (Hq + 2ll * Hkv > kMaxBwdHeads) return LOOM_ERR_UNSUPPORTED;
   if (dqkv_stride % 8 || !aligned16(dq) || !aligned16(dk) || !aligned16(dv) || !aligned16(dqkv) || !aligned4(dq_weight) ||
       !aligned4(dk_weight))
     return LOOM_ERR_MISALIGNED;

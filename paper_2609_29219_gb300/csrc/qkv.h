@@ -39,6 +39,9 @@ struct QkvArgs {
   float* partial;        // [blocks][2][D] (workspace)
 };
 
+// Heads (Hq + 2 Hkv) of a token at most in the backward pass.
+constexpr int kMaxBwdHeads = 16384;
+
 cudaError_t launch_qkv_norm_rope(const QkvArgs& a, cudaStream_t stream);
 cudaError_t launch_qkv_norm_rope_bwd(const QkvArgs& a, cudaStream_t stream);
 // Bytes of workspace of the backward pass: a partial sum of the weights' gradients per block.

@@ -22,6 +22,8 @@
 // first.
 #include <cuda_bf16.h>
 
+#include <type_traits>
+
 #include "kernels.h"
 #include "ptx.cuh"
 #include "qkv.h"
@@ -30,13 +32,15 @@ namespace loom {
 namespace {
 
 constexpr int kWarps = 8;             // per block
-constexpr int kMaxBwdBlocks = 152 * 2;  // as many as are resident; partial sums of the weights' gradients
-// Steps of a unit: four, or one where the call is over as soon as its longest warp.  GB300, device
-// us with one / two / four / eight steps: 8192 tokens H32/8 D 128 - / 58 / 34.7 / 35.5 (two: before
-// the heads' kinds were kept apart), 579 tokens into a cache 5.9 / 5.2 / 4.4 / -, one token 2.1 / 2.3
-// / 2.4 / -; backward, 8192 tokens 84 with two, 61 with four (at two blocks on an SM; three spill: 79),
-// 96 with eight.
-constexpr int kSteps = 4, kFewSteps = 1;
+constexpr int kBwdBlocksPerSm = 2, kBwdStages = 2;
+constexpr int kMaxBwdBlocks = 152 * kBwdBlocksPerSm;  // as many as are resident; partial sums of the weights' gradients
+// Steps of a unit: one where the call is over as soon as its longest warp, else four, or two where
+// four would leave a third of the steps without heads (units of two steps fewer than 3/2 of those of
+// four).  GB300, device us with one / two / four steps, forward and backward: 30 tokens H32/8 D 128
+// (184320 values) backward 4.0 / 4.1 / 4.6; 200 tokens (1228800) 6.3 / 6.1 / 5.2; 20000 tokens 137 /
+// 95 / 80 and 264 / 160 / 122; H9/3 (units 9 / 5 / 4) 52 / 39 / 42 and 95 / 66 / 66; H4/4 (6 / 3 / 3)
+// 34 / 25 / 31 and 60 / 40 / 49; H28/4 (18 / 9 / 6) 107 / 75 / 70 and 207 / 126 / 108.  Eight steps:
+// forward of 8192 tokens H32/8 35.5 (four: 34.7).
 constexpr long long kManyValues = 1 << 18;
 
 struct QkvParams {
@@ -123,21 +127,21 @@ __device__ __forceinline__ int partner_lane(const QkvParams& p, int lane) {
   return INTER || i0 >= p.R ? lane : i0 < half ? lane + half / 8 : lane - half / 8;
 }
 
-// This lane's angles at token t: y_i = z_i c_i + partner(z)_i s_i, with the pair's sign in s (BWD: of
-// the transposed rotation).
-template <int D, bool INTER, bool BWD>
-__device__ __forceinline__ void load_angles(const QkvParams& p, int t, int lane, float* c, float* s) {
-  const int i0 = 8 * (lane % (D / 8));
+// The position whose angles token t takes.
+__device__ __forceinline__ int position(const QkvParams& p, int t) {
+  const int pos = p.pos ? __ldg(p.pos + t) : p.q_at.S > 0 ? t % p.q_at.S : t;
+  return min(max(pos, 0), p.P - 1);
+}
+
+// The angles of the eight values from i0 on, from their position's R / 2 = half cosines and sines:
+// y_i = z_i c_i + partner(z)_i s_i, with the pair's sign in s (BWD: of the transposed rotation).
+template <bool INTER, bool BWD>
+__device__ __forceinline__ void angles(const float* cos, const float* sin, int i0, int half, float* c, float* s) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) c[i] = 1.f, s[i] = 0.f;
-  if (i0 >= p.R) return;
-  int pos = p.pos ? __ldg(p.pos + t) : p.q_at.S > 0 ? t % p.q_at.S : t;
-  pos = min(max(pos, 0), p.P - 1);
-  const int half = p.R / 2;
-  const long long row = static_cast<long long>(pos) * half;
+  if (i0 >= 2 * half) return;
   if constexpr (INTER) {
-    const float4 a = __ldg(reinterpret_cast<const float4*>(p.cos + row + i0 / 2));
-    const float4 b = __ldg(reinterpret_cast<const float4*>(p.sin + row + i0 / 2));
+    const float4 a = *reinterpret_cast<const float4*>(cos + i0 / 2), b = *reinterpret_cast<const float4*>(sin + i0 / 2);
     const float cc[4] = {a.x, a.y, a.z, a.w}, ss[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -151,8 +155,7 @@ __device__ __forceinline__ void load_angles(const QkvParams& p, int t, int lane,
     const float sign = first == BWD ? 1.f : -1.f;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const float4 a = __ldg(reinterpret_cast<const float4*>(p.cos + row + at) + h);
-      const float4 b = __ldg(reinterpret_cast<const float4*>(p.sin + row + at) + h);
+      const float4 a = *(reinterpret_cast<const float4*>(cos + at) + h), b = *(reinterpret_cast<const float4*>(sin + at) + h);
       c[4 * h] = a.x, c[4 * h + 1] = a.y, c[4 * h + 2] = a.z, c[4 * h + 3] = a.w;
       s[4 * h] = sign * b.x, s[4 * h + 1] = sign * b.y, s[4 * h + 2] = sign * b.z, s[4 * h + 3] = sign * b.w;
     }
@@ -225,7 +228,8 @@ __global__ void __launch_bounds__(kWarps * 32) qkv_norm_rope_kernel(const QkvPar
   uint64_t a[4], b[4];
   {
     float c[8], s[8], w[8], wp[8];
-    load_angles<D, INTER, false>(p, u.t, lane, c, s);
+    const long long row = static_cast<long long>(position(p, u.t)) * (p.R / 2);
+    angles<INTER, false>(p.cos + row, p.sin + row, i0, p.R / 2, c, s);
     load_weight(p, u.kind, i0, w);
     load_weight(p, u.kind, 8 * (src % LPH), wp);
 #pragma unroll
@@ -249,22 +253,38 @@ __global__ void __launch_bounds__(kWarps * 32) qkv_norm_rope_kernel(const QkvPar
 
 // The gradients.  With g the rotation transposed of dy and u = g w:  dx = r u - x r^3 mean(u x) and
 // dw += r g x.  A warp takes the same heads of every so many tokens (the grid's warps are a multiple
-// of a token's units), each lane adding up what its eight values give to the weight's gradient; a
+// of a token's units, or the last few have nothing to do), each lane adding up what its eight values give to the weight's gradient; a
 // block's sum goes to the workspace, where qkv_weight_grad_kernel adds the blocks' in their order: no
-// atomics, the same bits each time.
+// atomics, the same bits each time.  While a warp works on a token the next one's dy, x and angles are
+// on their way to its part of shared memory (held in registers they were requested only after the
+// last token's use: 8192 tokens H32/8 D 128 59 us, here 49.6; with three stages 53.6, with three blocks
+// on an SM 53.6).
+template <int UNR>
+struct BwdStage {  // of a warp
+  uint4 dy[UNR][32], x[UNR][32];  // each lane's own
+  float cos[64], sin[64];         // of the token; R / 2 of them
+};
+
+__device__ __forceinline__ void copy16(void* dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+}
+
 template <int D, bool INTER, int UNR>
-__global__ void __launch_bounds__(kWarps * 32, 2) qkv_norm_rope_bwd_kernel(const QkvParams p) {
+__global__ void __launch_bounds__(kWarps * 32, kBwdBlocksPerSm) qkv_norm_rope_bwd_kernel(const QkvParams p) {
   constexpr int LPH = D / 8, RPW = 32 / LPH;
-  __shared__ float sums[kWarps][2 * D];
+  extern __shared__ __align__(16) uint8_t bwd_smem[];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, i0 = 8 * (lane % LPH);
   const int src = partner_lane<D, INTER>(p, lane);
   Unit u = unit_of<D, UNR>(p, static_cast<long long>(blockIdx.x) * kWarps + warp);
   const int tokens = static_cast<int>(gridDim.x) * kWarps / (p.q_units + 2 * p.kv_units);  // from one to the next
+  if (u.t >= tokens) u.t = p.T;
   const int h0 = u.h0 + lane / LPH;
   const int first = u.kind == kQuery ? 0 : u.kind == kKey ? p.Hq : p.Hq + p.Hkv;
   const long long at = static_cast<long long>(first + h0) * D + i0;
+  const int half = p.R / 2;
+  BwdStage<UNR>* stages = reinterpret_cast<BwdStage<UNR>*>(bwd_smem) + kBwdStages * warp;
   uint64_t w[4], gw[4];
   {
     float wf[8];
@@ -275,29 +295,55 @@ __global__ void __launch_bounds__(kWarps * 32, 2) qkv_norm_rope_bwd_kernel(const
       gw[i] = f2(0.f, 0.f);
     }
   }
-  for (; u.t < p.T; u.t = p.T - u.t > tokens ? u.t + tokens : p.T) {
-    const __nv_bfloat16* x = p.x + static_cast<long long>(u.t) * p.row_elems + at;
-    __nv_bfloat16* dx = p.dx + static_cast<long long>(u.t) * p.drow_elems + at;
+  const auto after = [&](int t) { return p.T - t > tokens ? t + tokens : p.T; };
+  // requests token t, whose position is pos
+  const auto request = [&](BwdStage<UNR>& st, int t, int pos) {
+    Unit v = u;
+    v.t = t;
     long long head;
-    const __nv_bfloat16* dy = place<D>(p, u, head) + i0;
+    const __nv_bfloat16* dy = place<D>(p, v, head) + i0;
     dy += h0 * head;
-    uint4 rdy[UNR], rx[UNR];
+    const __nv_bfloat16* x = p.x + static_cast<long long>(t) * p.row_elems + at;
 #pragma unroll
-    for (int s = 0; s < UNR; ++s) {
-      const bool in = h0 + s * RPW < u.heads;
-      rdy[s] = in ? ld_stream(dy + s * RPW * head) : make_uint4(0, 0, 0, 0);
-      rx[s] = in && u.kind != kValue ? ld_stream(x + s * RPW * D) : make_uint4(0, 0, 0, 0);
+    for (int s = 0; s < UNR; ++s)
+      if (h0 + s * RPW < u.heads) {
+        copy16(&st.dy[s][lane], dy + s * RPW * head);
+        if (u.kind != kValue) copy16(&st.x[s][lane], x + s * RPW * D);
+      }
+    if (u.kind != kValue && 4 * (lane & 15) < half) {
+      const float* from = (lane < 16 ? p.cos : p.sin) + static_cast<long long>(pos) * half + 4 * (lane & 15);
+      copy16((lane < 16 ? st.cos : st.sin) + 4 * (lane & 15), from);
     }
+  };
+  int to = u.t, ahead = 0, now = 0, free = 0;  // the token requested next, its position; stages
+  const auto request_next = [&] {
+    if (to < p.T) {
+      request(stages[free], to, ahead);
+      to = after(to);
+      if (to < p.T) ahead = position(p, to);
+    }
+    free = free + 1 < kBwdStages ? free + 1 : 0;
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  if (to < p.T) ahead = position(p, to);
+#pragma unroll
+  for (int i = 0; i + 1 < kBwdStages; ++i) request_next();
+  for (; u.t < p.T; u.t = after(u.t), now = now + 1 < kBwdStages ? now + 1 : 0) {
+    request_next();
+    asm volatile("cp.async.wait_group %0;" ::"n"(kBwdStages - 1) : "memory");
+    __syncwarp();
+    const BwdStage<UNR>& st = stages[now];
+    __nv_bfloat16* dx = p.dx + static_cast<long long>(u.t) * p.drow_elems + at;
     if (u.kind == kValue) {
 #pragma unroll
       for (int s = 0; s < UNR; ++s)
-        if (h0 + s * RPW < u.heads) __stcs(reinterpret_cast<uint4*>(dx + s * RPW * D), rdy[s]);
+        if (h0 + s * RPW < u.heads) __stcs(reinterpret_cast<uint4*>(dx + s * RPW * D), st.dy[s][lane]);
       continue;
     }
     uint64_t c[4], s[4];
     {
       float cf[8], sf[8];
-      load_angles<D, INTER, true>(p, u.t, lane, cf, sf);
+      angles<INTER, true>(st.cos, st.sin, i0, half, cf, sf);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         c[i] = f2(cf[2 * i], cf[2 * i + 1]);
@@ -306,10 +352,12 @@ __global__ void __launch_bounds__(kWarps * 32, 2) qkv_norm_rope_bwd_kernel(const
     }
 #pragma unroll
     for (int k = 0; k < UNR; ++k) {
+      const bool in = h0 + k * RPW < u.heads;
+      const uint4 rdy = in ? st.dy[k][lane] : make_uint4(0, 0, 0, 0), rx = in ? st.x[k][lane] : make_uint4(0, 0, 0, 0);
       uint64_t z[4], g[4], o[4];
-      unpack8(rx[k], z);
-      unpack8(rdy[k], g);
-      unpack8(partners<INTER>(rdy[k], src), o);
+      unpack8(rx, z);
+      unpack8(rdy, g);
+      unpack8(partners<INTER>(rdy, src), o);
 #pragma unroll
       for (int i = 0; i < 4; ++i) g[i] = fma2(o[i], s[i], mul2(g[i], c[i]));
       const float r = rsqrtf(head_sum<LPH>(sum8(z, z)) * (1.f / D) + p.eps);
@@ -323,9 +371,12 @@ __global__ void __launch_bounds__(kWarps * 32, 2) qkv_norm_rope_bwd_kernel(const
       const uint64_t m2 = f2(m, m);
 #pragma unroll
       for (int i = 0; i < 4; ++i) g[i] = mul2(fma2(z[i], m2, g[i]), r2);
-      if (h0 + k * RPW < u.heads) __stcs(reinterpret_cast<uint4*>(dx + k * RPW * D), pack8(g));
+      if (in) __stcs(reinterpret_cast<uint4*>(dx + k * RPW * D), pack8(g));
     }
+    __syncwarp();  // every lane has read the angles before the next request
   }
+  __syncthreads();  // the stages become the warps' sums
+  float(*sums)[2 * D] = reinterpret_cast<float(*)[2 * D]>(bwd_smem);
   // the warp's head groups, then the block's warps
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -373,10 +424,11 @@ __global__ void __launch_bounds__(1024) qkv_weight_grad_kernel(const float* part
 // A launch as a programmatic dependent of the kernel before it in the stream: every kernel here
 // waits for that one (griddepcontrol.wait) before its first access to memory.
 template <class Kernel, class... Args>
-cudaError_t launch(Kernel kernel, int grid, int threads, cudaStream_t stream, Args... args) {
+cudaError_t launch(Kernel kernel, int grid, int threads, size_t smem, cudaStream_t stream, Args... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(grid));
   cfg.blockDim = dim3(static_cast<unsigned>(threads));
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -423,31 +475,55 @@ cudaError_t launch_fwd_u(const QkvArgs& a, cudaStream_t stream) {
   const long long blocks = (p.units + kWarps - 1) / kWarps;
   if (blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
   const int g = static_cast<int>(blocks);
-  return a.interleaved ? launch(qkv_norm_rope_kernel<D, true, UNR>, g, kWarps * 32, stream, p)
-                       : launch(qkv_norm_rope_kernel<D, false, UNR>, g, kWarps * 32, stream, p);
+  return a.interleaved ? launch(qkv_norm_rope_kernel<D, true, UNR>, g, kWarps * 32, 0, stream, p)
+                       : launch(qkv_norm_rope_kernel<D, false, UNR>, g, kWarps * 32, 0, stream, p);
+}
+
+template <int D, int UNR>
+cudaError_t launch_bwd_u(const QkvArgs& a, cudaStream_t stream) {
+  const QkvParams p = params_of(a, UNR);
+  // blocks whose warps are a multiple of a token's units (unless that is more than there is room for),
+  // as many as there is room for or need of
+  const int per = p.q_units + 2 * p.kv_units;
+  static_assert(kMaxBwdHeads / (256 / D * 4) + 3 <= kMaxBwdBlocks * kWarps, "a token's units have a warp each");
+  int unit = 1;
+  while (unit < kMaxBwdBlocks && unit * kWarps % per) ++unit;
+  const long long need = (p.units + static_cast<long long>(unit) * kWarps - 1) / (static_cast<long long>(unit) * kWarps);
+  const int most = kMaxBwdBlocks / unit, g = static_cast<int>(need < most ? need : most) * unit;
+  constexpr size_t smem = kBwdStages * kWarps * sizeof(BwdStage<UNR>);
+  static_assert(smem >= kWarps * 2 * D * sizeof(float), "the stages hold the sums");
+  const auto inter = qkv_norm_rope_bwd_kernel<D, true, UNR>, split = qkv_norm_rope_bwd_kernel<D, false, UNR>;
+  static PerDeviceOnce configured;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (!configured.run(dev, [&] {
+        return cudaFuncSetAttribute(inter, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) == cudaSuccess &&
+               cudaFuncSetAttribute(split, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) == cudaSuccess;
+      }))
+    return cudaErrorInvalidValue;
+  e = launch(a.interleaved ? inter : split, g, kWarps * 32, smem, stream, p);
+  if (e != cudaSuccess) return e;
+  return launch(qkv_weight_grad_kernel, 2 * D / 8, 1024, 0, stream, static_cast<const float*>(p.partial), g, D, a.dq_weight,
+                a.dk_weight);
+}
+
+// Calls f(std::integral_constant<int, steps>) with the steps of a unit.
+template <class F>
+cudaError_t with_steps(const QkvArgs& a, F f) {
+  if (static_cast<long long>(a.T) * (a.Hq + 2 * a.Hkv) * a.D < kManyValues) return f(std::integral_constant<int, 1>());
+  const int heads = 256 / a.D;  // of a step
+  const auto units = [&](int n) { return (a.Hq + heads * n - 1) / (heads * n) + 2 * ((a.Hkv + heads * n - 1) / (heads * n)); };
+  return 2 * units(2) < 3 * units(4) ? f(std::integral_constant<int, 2>()) : f(std::integral_constant<int, 4>());
 }
 
 template <int D>
 cudaError_t launch_fwd_d(const QkvArgs& a, cudaStream_t stream) {
-  return static_cast<long long>(a.T) * (a.Hq + 2 * a.Hkv) * D >= kManyValues ? launch_fwd_u<D, kSteps>(a, stream)
-                                                                           : launch_fwd_u<D, kFewSteps>(a, stream);
+  return with_steps(a, [&](auto n) { return launch_fwd_u<D, decltype(n)::value>(a, stream); });
 }
-
 template <int D>
 cudaError_t launch_bwd_d(const QkvArgs& a, cudaStream_t stream) {
-  const QkvParams p = params_of(a, kSteps);
-  // blocks whose warps are a multiple of a token's units, as many as there is room for or need of
-  const int per = p.q_units + 2 * p.kv_units;
-  int unit = 1;
-  while (unit * kWarps % per) ++unit;
-  if (unit > kMaxBwdBlocks) return cudaErrorInvalidConfiguration;
-  const long long need = (p.units + static_cast<long long>(unit) * kWarps - 1) / (static_cast<long long>(unit) * kWarps);
-  const int most = kMaxBwdBlocks / unit, g = static_cast<int>(need < most ? need : most) * unit;
-  const cudaError_t e = a.interleaved ? launch(qkv_norm_rope_bwd_kernel<D, true, kSteps>, g, kWarps * 32, stream, p)
-                                      : launch(qkv_norm_rope_bwd_kernel<D, false, kSteps>, g, kWarps * 32, stream, p);
-  if (e != cudaSuccess) return e;
-  return launch(qkv_weight_grad_kernel, 2 * D / 8, 1024, stream, static_cast<const float*>(p.partial), g, D, a.dq_weight,
-                a.dk_weight);
+  return with_steps(a, [&](auto n) { return launch_bwd_u<D, decltype(n)::value>(a, stream); });
 }
 
 }  // namespace

@@ -101,3 +101,8 @@ def test_nothing_to_do(lib):
     assert _caller(lib.loom_qkv_norm_rope, FWD)(T=0, S=0) == 0
     assert _caller(lib.loom_qkv_norm_rope_cache, CACHE)(T=0) == 0
     assert lib.loom_qkv_norm_rope_bwd_workspace_bytes(96) == 0
+
+
+def test_norm_backward_heads(lib):
+    """More heads than the gradient's warps can be dealt to, by their rows' length."""
+    assert _caller(lib.loom_qkv_norm_rope_bwd, NBWD)(Hq=16384, Hkv=1, stride=16386 * 64, dstride=16386 * 64) == 2

@@ -203,6 +203,13 @@ def test_rows_between_are_left_alone_and_empty_calls(loom):
     assert not dqw.any() and not dkw.any()
 
 
+@pytest.mark.parametrize("T,Hq,Hkv,D", [(2, 2433, 3, 128), (9, 2433, 3, 128), (1, 16382, 1, 64), (2, 9000, 1, 128)])
+def test_heads_that_do_not_divide_the_warps(loom, T, Hq, Hkv, D):
+    """A token's units (307 of the first two, prime) are no divisor of the grid's warps."""
+    test_forward(loom, T, Hq, Hkv, D, 32, 0, True, False)
+    test_backward(loom, T, Hq, Hkv, D, 32, 0, True, False)
+
+
 def test_the_same_inputs_give_the_same_bits_on_any_stream(loom):
     import torch
     c = Case(5000, 16, 4, 64, 64, seed=5)
