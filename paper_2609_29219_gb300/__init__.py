@@ -3,7 +3,8 @@
 Every function here only marshals arguments (tensor data pointers, sizes, the current
 CUDA stream) into the C ABI declared in ``include/loom_attn.h``; all computation runs
 in the library's CUDA kernels.  There is no fallback: if the compiled library is
-missing, every call raises.
+missing, every call raises.  (Where ``_binding.so`` was built, the training and serving
+entry points marshal their common case there.)
 
 Two layers:
 
