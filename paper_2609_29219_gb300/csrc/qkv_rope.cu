@@ -13,7 +13,7 @@
 // What bounds it: the projection is read once and written once, and no value meets another
 // outside its head, so it is the memory's bandwidth, and after that the instructions per value:
 // at 100 instructions for 16 bytes of a lane they took as long as the memory (8192 tokens, H32/8,
-// D 128: 49 us; 35 with what follows).  So the norm's factor is applied last, and weight and angle
+// D 128: 49 us; 33 with what follows).  So the norm's factor is applied last, and weight and angle
 // are multiplied once for all of a token's heads:
 //     y_i = r (x_i A_i + x_partner(i) B_i),   A_i = w_i c_i,   B_i = w_partner(i) (+-) s_i;
 // the arithmetic is on pairs of floats, and the partner's values are shuffled as packed bf16.
@@ -31,7 +31,7 @@
 namespace loom {
 namespace {
 
-constexpr int kWarps = 8;             // per block
+constexpr int kWarps = 8;  // per block (the forward's: at most)
 constexpr int kBwdBlocksPerSm = 2, kBwdStages = 2;
 constexpr int kMaxBwdBlocks = 152 * kBwdBlocksPerSm;  // as many as are resident; partial sums of the weights' gradients
 // Steps of a unit: one where the call is over as soon as its longest warp, else four, or two where
@@ -40,7 +40,7 @@ constexpr int kMaxBwdBlocks = 152 * kBwdBlocksPerSm;  // as many as are resident
 // (184320 values) backward 4.0 / 4.1 / 4.6; 200 tokens (1228800) 6.3 / 6.1 / 5.2; 20000 tokens 137 /
 // 95 / 80 and 264 / 160 / 122; H9/3 (units 9 / 5 / 4) 52 / 39 / 42 and 95 / 66 / 66; H4/4 (6 / 3 / 3)
 // 34 / 25 / 31 and 60 / 40 / 49; H28/4 (18 / 9 / 6) 107 / 75 / 70 and 207 / 126 / 108.  Eight steps:
-// forward of 8192 tokens H32/8 35.5 (four: 34.7).
+// forward of 8192 tokens H32/8 35.5 (four: 34.7; both in blocks of eight warps).
 constexpr long long kManyValues = 1 << 18;
 
 struct QkvParams {
@@ -204,7 +204,7 @@ __global__ void __launch_bounds__(kWarps * 32) qkv_norm_rope_kernel(const QkvPar
   constexpr int LPH = D / 8, RPW = 32 / LPH;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;");
-  const long long unit = static_cast<long long>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
+  const long long unit = static_cast<long long>(blockIdx.x) * (blockDim.x >> 5) + (threadIdx.x >> 5);
   if (unit >= p.units) return;
   const Unit u = unit_of<D, UNR>(p, unit);
   const int lane = threadIdx.x & 31, i0 = 8 * (lane % LPH), h0 = u.h0 + lane / LPH;
@@ -469,14 +469,19 @@ QkvParams params_of(const QkvArgs& a, int unroll) {
   return p;
 }
 
+// Blocks of four warps, whose places are free again sooner, where there are more warps than are
+// resident (64 registers: 32 an SM); else of eight, of which there are fewer to start.  GB300, device us
+// with eight / four / two warps: 8192 tokens H32/8 D 128 35.2 / 33.0 / 32.7, 30000 tokens 118 / 111 / 111,
+// H16/2 D 64 41.9 / 40.0 / 60.9; 579 tokens H32/8 4.0 / 4.3 / 4.2.
 template <int D, int UNR>
 cudaError_t launch_fwd_u(const QkvArgs& a, cudaStream_t stream) {
   const QkvParams p = params_of(a, UNR);
-  const long long blocks = (p.units + kWarps - 1) / kWarps;
+  const int warps = p.units > 152 * 32 ? kWarps / 2 : kWarps;
+  const long long blocks = (p.units + warps - 1) / warps;
   if (blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
   const int g = static_cast<int>(blocks);
-  return a.interleaved ? launch(qkv_norm_rope_kernel<D, true, UNR>, g, kWarps * 32, 0, stream, p)
-                       : launch(qkv_norm_rope_kernel<D, false, UNR>, g, kWarps * 32, 0, stream, p);
+  return a.interleaved ? launch(qkv_norm_rope_kernel<D, true, UNR>, g, warps * 32, 0, stream, p)
+                       : launch(qkv_norm_rope_kernel<D, false, UNR>, g, warps * 32, 0, stream, p);
 }
 
 template <int D, int UNR>
