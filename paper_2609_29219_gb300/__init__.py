@@ -527,9 +527,9 @@ def _norm_bwd_need(D):
 # The checks of the entry points below take most of a small call's time if each tensor goes through
 # _ptr, so they are one expression that names nothing, and what fails it is looked at again by name;
 # and the common case goes through the compiled binding.  GB300 host, us per call with _ptr / one
-# expression / compiled (the C call in it): backward of 128 rows 25.0 / 19.9 / 9.5 (4), norm and
-# rotation 17.6 / 14.7 / 5.5 (2), into a cache 14.4 / 12.9 / 3.9 (2), its gradients 27.2 / 22.1 /
-# 8.4 (3).
+# expression / compiled (the C call in it): backward of 128 rows 25.0 / 19.9 / 9 (4), norm and
+# rotation 17.6 / 14.7 / 5.4 (2), into a cache 14.4 / 12.9 / 3.8 (2), its gradients 27.2 / 22.1 /
+# 8 (3).
 def _bwd_checked(do, q, k, v, o, lse, dlse, dq, dk, dv, ndim):
     """The backward entry points' tensors, named if they are not what they should be."""
     for t, name in ((q, "q"), (k, "k"), (v, "v"), (do, "do"), (o, "o")):

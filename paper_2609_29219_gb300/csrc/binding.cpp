@@ -4,8 +4,8 @@
 // tuple; or None, having done nothing, where anything is not as the common case has it -- the caller's
 // Python code then does the call or names what is wrong; or the status, an int, where the C call
 // refuses.  Tensors are looked at and made through torch's C++ interface: GB300 host, us a call, by their
-// Python attributes / here: backward of 128 rows 16.5 / 9.5, norm and rotation 11.6 / 5.5, into a
-// cache 9.1 / 3.9, its gradients 17.0 / 8.4.
+// Python attributes / here: backward of 128 rows 16.5 / 9, norm and rotation 11.6 / 5.4, into a
+// cache 9.1 / 3.8, its gradients 17.0 / 8.
 // It does not link against the library: set_up() gets the C functions' addresses.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
@@ -14,6 +14,7 @@
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -48,7 +49,7 @@ struct Ref {  // owned
   }
 };
 
-constexpr at::ScalarType kBf16 = at::kBFloat16, kF32 = at::kFloat, kI32 = at::kInt, kU8 = at::kByte;
+constexpr at::ScalarType kBf16 = at::kBFloat16, kF32 = at::kFloat, kI32 = at::kInt;
 
 struct Tensor {
   const at::Tensor* t = nullptr;
@@ -111,10 +112,8 @@ PyObject* make(long long device, int dims, const long long* size, at::ScalarType
 PyObject* make_like(long long device, const Tensor& t, at::ScalarType type, void** ptr) {
   return make(device, t.dims, t.size, type, ptr);
 }
-PyObject* make_bytes(long long device, size_t bytes, void** ptr) {
-  const long long n = bytes < 16 ? 16 : static_cast<long long>(bytes);
-  return make(device, 1, &n, kU8, ptr);
-}
+// Scratch on the current device for a call on its current stream (no tensor: nobody sees it).
+c10::DataPtr scratch(size_t bytes) { return c10::cuda::CUDACachingAllocator::get()->allocate(bytes < 16 ? 16 : bytes); }
 
 PyObject* status(loom_status st) { return PyLong_FromLong(st); }
 
@@ -169,22 +168,21 @@ PyObject* bwd(PyObject* const* a, bool varlen) {
   const int iB = static_cast<int>(B), iHq = static_cast<int>(Hq), iHkv = static_cast<int>(Hkv), iSq = static_cast<int>(Sq),
             iSkv = static_cast<int>(Skv), iD = static_cast<int>(D);
   const size_t need = varlen ? F.attn_bwd_varlen_bytes(iB, iHq, iHkv, iSq, iSkv, iD) : F.attn_bwd_bytes(iB, iHq, iHkv, iSq, iSkv, iD);
-  void *dqp, *dkp, *dvp, *wp;
+  void *dqp, *dkp, *dvp;
   Ref dq(make_like(dev, q, bf16, &dqp));
   if (!dq.p) return nullptr;
   Ref dk(make_like(dev, k, bf16, &dkp));
   if (!dk.p) return nullptr;
   Ref dv(make_like(dev, v, bf16, &dvp));
   if (!dv.p) return nullptr;
-  Ref ws(make_bytes(dev, need, &wp));
-  if (!ws.p) return nullptr;
+  const c10::DataPtr ws = scratch(need);
   void* s = stream_of(dev);
   const float *l = static_cast<const float*>(lse.ptr), *dl = static_cast<const float*>(dlse.ptr);
   const loom_status st =
       varlen ? F.attn_bwd_varlen(d.ptr, q.ptr, k.ptr, v.ptr, o.ptr, l, dl, dqp, dkp, dvp, static_cast<const int32_t*>(cq.ptr),
-                                 static_cast<const int32_t*>(ck.ptr), wp, need, iB, iHq, iHkv, iSq, iSkv,
+                                 static_cast<const int32_t*>(ck.ptr), ws.get(), need, iB, iHq, iHkv, iSq, iSkv,
                                  static_cast<int>(max_q), static_cast<int>(max_k), iD, causal, scale, s)
-             : F.attn_bwd(d.ptr, q.ptr, k.ptr, v.ptr, o.ptr, l, dl, dqp, dkp, dvp, wp, need, iB, iHq, iHkv, iSq, iSkv, iD, causal,
+             : F.attn_bwd(d.ptr, q.ptr, k.ptr, v.ptr, o.ptr, l, dl, dqp, dkp, dvp, ws.get(), need, iB, iHq, iHkv, iSq, iSkv, iD, causal,
                           scale, s);
   if (st != LOOM_OK) return status(st);
   return PyTuple_Pack(3, dq.p, dk.p, dv.p);
@@ -295,19 +293,18 @@ PyObject* norm_rope_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const long long dev = device_of(m.x);
   if (dev < 0) Py_RETURN_NONE;
   const size_t need = F.norm_rope_bwd_bytes(static_cast<int>(m.D));
-  void *xp, *qp, *kp, *wp;
+  void *xp, *qp, *kp;
   Ref dx(make(dev, 2, m.x.size, kBf16, &xp));
   if (!dx.p) return nullptr;
   Ref dqw(make(dev, 1, m.qw.size, kF32, &qp));
   if (!dqw.p) return nullptr;
   Ref dkw(make(dev, 1, m.qw.size, kF32, &kp));
   if (!dkw.p) return nullptr;
-  Ref ws(make_bytes(dev, need, &wp));
-  if (!ws.p) return nullptr;
+  const c10::DataPtr ws = scratch(need);
   const loom_status st = F.norm_rope_bwd(
       dq.ptr, dk.ptr, dv.ptr, m.x.ptr, m.row, m.qw.ptr, m.kw.ptr, m.type, static_cast<const float*>(m.cos.ptr),
       static_cast<const float*>(m.sin.ptr), m.P, m.R, m.interleaved, m.positions(), xp, m.x.size[1], static_cast<float*>(qp),
-      static_cast<float*>(kp), wp, need, static_cast<int>(m.T), static_cast<int>(S), static_cast<int>(Hq), static_cast<int>(Hkv),
+      static_cast<float*>(kp), ws.get(), need, static_cast<int>(m.T), static_cast<int>(S), static_cast<int>(Hq), static_cast<int>(Hkv),
       static_cast<int>(m.D), m.eps, stream_of(dev));
   if (st != LOOM_OK) return status(st);
   return PyTuple_Pack(3, dx.p, dqw.p, dkw.p);
