@@ -19,6 +19,13 @@
 // both walks: seven products of 128 x 128 x D per pair of tiles instead of five.
 // Items are taken from a counter, long ones first, so CTAs that finish the kv items early start on
 // the query items.
+//
+// What bounds it: the tensor pipe and the hand-overs around it.  A step of a kv item (D = 128) is four
+// products, 2048 clocks of the pipe, and takes 2940: the score products read both operands from
+// shared memory, at all of its bandwidth, so that dK and the next dP take 1440 to 1600 clocks
+// together, dV and the next S 1250 to 1380; a query item's step takes 2110 for its three (1536).
+// GB300: B4 H32 S2048 D128 causal 356 us (966 TFLOP/s of the five products that the gradients need, 1352
+// of the seven), B1 H32/8 S8192 1114 us (1234, 1727; under the power limit).
 #include <cuda.h>
 #include <cuda_bf16.h>
 
