@@ -25,7 +25,7 @@
 // shared memory, at all of its bandwidth, so that dK and the next dP take 1440 to 1600 clocks
 // together, dV and the next S 1250 to 1380; a query item's step takes 2110 for its three (1536).
 // GB300: B4 H32 S2048 D128 causal 356 us (966 TFLOP/s of the five products that the gradients need, 1352
-// of the seven), B1 H32/8 S8192 1114 us (1234, 1727; under the power limit).
+// of the seven), B1 H32/8 S8192 1078 us (1275, 1785; under the power limit).
 #include <cuda.h>
 #include <cuda_bf16.h>
 
@@ -1247,7 +1247,7 @@ cudaError_t launch_d(const BwdArgs& a, const KernelCtl& ctl, cudaStream_t stream
       !make_map(&mk, a.k, D, a.Skv, kv_planes, VARLEN) || !make_map(&mv, a.v, D, a.Skv, kv_planes, VARLEN))
     return cudaErrorInvalidValue;
   const int stat_tiles = static_cast<int>(bwd_stat_tiles(a.B, a.Sq, lg, VARLEN));
-  const BwdPlan plan = bwd_plan(a.B, a.Hq, a.Hkv, a.Sq, a.Skv, D, VARLEN, sms);
+  const BwdPlan plan = bwd_plan(a.B, a.Hq, a.Hkv, a.Sq, a.Skv, D, VARLEN, a.causal != 0, sms);
   unsigned int* counters = static_cast<unsigned int*>(a.workspace);
   float* stats = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + plan.stats_at);
   e = launch(attn_bwd_rows_kernel<D, VARLEN>, static_cast<int>(q_planes * stat_tiles) * (kTile / kRowsPerBlock), kRowThreads, 0, stream,

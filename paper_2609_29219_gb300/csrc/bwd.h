@@ -42,31 +42,41 @@ struct BwdPlan {
   int counters;                 // 64, then one for each elementwise warp of each item where items are split
   size_t stats_at, partial_at, bytes;
 };
-inline BwdPlan bwd_plan(int B, int Hq, int Hkv, long long Sq, long long Skv, int D, bool ragged, int sms) {
+inline BwdPlan bwd_plan(int B, int Hq, int Hkv, long long Sq, long long Skv, int D, bool ragged, bool causal, int sms) {
   const int lg = bwd_pack_log2(Hq / Hkv), G = Hq / Hkv >> lg;
   const long long seqs = ragged ? 1 : B;
   const long long q_planes = seqs * (Hq >> lg), kv_planes = seqs * Hkv, stat_tiles = bwd_stat_tiles(B, Sq, lg, ragged);
   BwdPlan p{};
   p.kv_items = kv_planes * (ragged ? Skv / 128 + B : (Skv + 127) / 128);
   p.q_items = q_planes * stat_tiles;
-  // Steps of an item (ragged: of a sequence of average length), a kv item's of about 1.4 us and a
-  // query item's of 1.2 (D = 128).  The splits are those of the least estimate: the time of all
-  // steps spread over the SMs, 4 us for each share (its partial sums), and half the longest share,
-  // but no less than one share of each kind one after the other.  GB300, us, unsplit / split: B1 H8/1
-  // S2000 causal 158 / 49, B2 H16/2 S512 causal 50 / 31, B1 H8/1 S300 causal 32 / 24; a chunk of 515 at 3001,
-  // H32/8, has an item for each SM and stays whole (70; 97 in two and four shares).
-  const double rows = static_cast<double>(Sq) / (ragged ? B : 1) * (1 << lg), keys = static_cast<double>(Skv) / (ragged ? B : 1);
-  const double kv_us = 1.4 * G * (rows < 128 ? 1 : rows / 128), q_us = 1.2 * (keys < 128 ? 1 : keys / 128);
-  const double all = (p.kv_items * kv_us + p.q_items * q_us) / sms;
+  // The splits of the least estimate (us, ragged: as if all sequences had the average length): all of
+  // the work spread over the SMs and part of the longest share of each kind, or the longest share if
+  // that takes longer.  A share of a split item writes and reads its partial sums, and the last one
+  // to arrive adds the others'.  The constants are those that choose best among 1 to 16 shares of kv items
+  // and 1 to 8 of query items over 7000 random shapes (1 to 96 heads, 32 to 8000 queries and keys): its
+  // choices take 1.8 % longer than the best ones on average, no splits 16 %.  GB300, us, unsplit / split: B1 H8/1 S2000
+  // causal 158 / 47, B1 H32/8 S2048 causal 136 / 100; B1 H16/16 S2048 causal, an item for each SM and more,
+  // 52 / 73.
+  const auto tiles = [&](long long rows) {
+    return ragged ? static_cast<double>(rows) / B / 128 + 0.5 : static_cast<double>((rows + 127) / 128);
+  };
+  const double kv_steps = G * tiles(Sq << lg), q_steps = tiles(Skv);
+  const double seen = causal ? 1 - 0.5 * static_cast<double>(Sq < Skv ? Sq : Skv) / static_cast<double>(Skv > 0 ? Skv : 1) : 1;
+  const double kv_step = D == 128 ? 1.1 : 1.5, q_step = D == 128 ? 0.67 : 0.95, kv_part = D == 128 ? 6 : 7, q_part = 2;
   double best = 1e300;
-  for (int a = 1; a <= 16 && (a == 1 || kv_us / a >= 2.8); a *= 2)
-    for (int b = 1; b <= 16 && (b == 1 || q_us / b >= 2.4); b *= 2) {
+  // (items of many steps that keep less than a third of the SMs busy always have two shares or more)
+  const int least = kv_steps >= 8 && p.kv_items + p.q_items <= sms / 3 ? 2 : 1;
+  for (int a = least; a <= 16 && (a == 1 || a <= kv_steps); a *= 2)
+    for (int b = 1; b <= 8 && (b == 1 || b <= q_steps); b *= 2) {
       // (a quarter of a gigabyte of partial sums of each kind at most)
       if (a > 1 && p.kv_items * a * 1024.0 * D > 2.7e8) continue;
       if (b > 1 && p.q_items * b * 512.0 * D > 2.7e8) continue;
-      const double k = kv_us / a, q = q_us / b, shares = (a > 1 ? p.kv_items * a : 0) + (b > 1 ? p.q_items * b : 0);
-      const double spread = all + 4.0 * shares / sms + 0.5 * (k > q ? k : q), chain = k + q + (a > 1 ? 4 : 0) + (b > 1 ? 4 : 0);
-      const double us = spread > chain ? spread : chain;
+      const double k_all = kv_steps * seen * kv_step + 2.5 + (a > 1 ? a * kv_part : 0);
+      const double q_all = q_steps * seen * q_step + 2.1 + (b > 1 ? b * q_part : 0);
+      const double k_long = kv_steps * kv_step / a + 2.5 + (a > 1 ? 4.3 + 1.1 * a : 0);
+      const double q_long = q_steps * q_step / b + 2.1 + (b > 1 ? 0.35 * b : 0);
+      const double spread = (p.kv_items * k_all + p.q_items * q_all) / sms + 0.42 * k_long + 0.16 * q_long;
+      const double longest = k_long > q_long ? k_long : q_long, us = spread > longest ? spread : longest;
       if (us < best) best = us, p.kv_split = a, p.q_split = b;
     }
   const bool any = p.kv_split > 1 || p.q_split > 1;
@@ -76,6 +86,12 @@ inline BwdPlan bwd_plan(int B, int Hq, int Hkv, long long Sq, long long Skv, int
   p.bytes = p.partial_at + (p.kv_split > 1 ? static_cast<size_t>(p.kv_items) * p.kv_split * 1024 * D : 0) +
             (p.q_split > 1 ? static_cast<size_t>(p.q_items) * p.q_split * 512 * D : 0);
   return p;
+}
+
+// The workspace of a call, causal or not.
+inline size_t bwd_workspace(int B, int Hq, int Hkv, long long Sq, long long Skv, int D, bool ragged, int sms) {
+  const size_t full = bwd_plan(B, Hq, Hkv, Sq, Skv, D, ragged, false, sms).bytes, causal = bwd_plan(B, Hq, Hkv, Sq, Skv, D, ragged, true, sms).bytes;
+  return full > causal ? full : causal;
 }
 
 cudaError_t launch_attn_bwd(const BwdArgs& a, const KernelCtl& ctl, cudaStream_t stream);

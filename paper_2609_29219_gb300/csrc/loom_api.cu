@@ -361,7 +361,7 @@ loom_status bwd_call(const BwdArgs& a, size_t workspace_bytes, void* stream) {
     if (e == cudaSuccess && a.Skv > 0) e = cudaMemsetAsync(a.dv, 0, row * a.Hkv * a.Skv, s);
     return e == cudaSuccess ? LOOM_OK : LOOM_ERR_CUDA;
   }
-  if (!a.workspace || workspace_bytes < bwd_plan(a.B, a.Hq, a.Hkv, a.Sq, a.Skv, a.D, ragged, sms_or_model()).bytes)
+  if (!a.workspace || workspace_bytes < bwd_workspace(a.B, a.Hq, a.Hkv, a.Sq, a.Skv, a.D, ragged, sms_or_model()))
     return LOOM_ERR_WORKSPACE;
   if (!aligned16(a.workspace)) return LOOM_ERR_MISALIGNED;
   KernelCtl ctl;
@@ -372,12 +372,12 @@ loom_status bwd_call(const BwdArgs& a, size_t workspace_bytes, void* stream) {
 
 size_t loom_attn_bwd_workspace_bytes(int B, int Hq, int Hkv, int Sq, int Skv, int D) {
   if (B <= 0 || Hq <= 0 || Hkv <= 0 || Sq <= 0 || Skv <= 0 || Hq % Hkv || (D != 64 && D != 128)) return 0;
-  return bwd_sizes_fit(B, Hq, Hkv, Sq, Skv, false) ? bwd_plan(B, Hq, Hkv, Sq, Skv, D, false, sms_or_model()).bytes : 0;
+  return bwd_sizes_fit(B, Hq, Hkv, Sq, Skv, false) ? bwd_workspace(B, Hq, Hkv, Sq, Skv, D, false, sms_or_model()) : 0;
 }
 
 size_t loom_attn_bwd_varlen_workspace_bytes(int B, int Hq, int Hkv, int total_q, int total_k, int D) {
   if (B <= 0 || Hq <= 0 || Hkv <= 0 || total_q < 0 || total_k < 0 || Hq % Hkv || (D != 64 && D != 128)) return 0;
-  return bwd_sizes_fit(B, Hq, Hkv, total_q, total_k, true) ? bwd_plan(B, Hq, Hkv, total_q, total_k, D, true, sms_or_model()).bytes : 0;
+  return bwd_sizes_fit(B, Hq, Hkv, total_q, total_k, true) ? bwd_workspace(B, Hq, Hkv, total_q, total_k, D, true, sms_or_model()) : 0;
 }
 
 loom_status loom_attn_bwd(const void* dout, const void* q, const void* k, const void* v, const void* o, const float* lse,
