@@ -51,10 +51,11 @@ inline BwdPlan bwd_plan(int B, int Hq, int Hkv, long long Sq, long long Skv, int
   p.q_items = q_planes * stat_tiles;
   // The splits of the least estimate (us, ragged: as if all sequences had the average length): all of
   // the work spread over the SMs and part of the longest share of each kind, or the longest share if
-  // that takes longer.  A share of a split item writes and reads its partial sums, and the last one
-  // to arrive adds the others'.  The constants are those that choose best among 1 to 16 shares of kv items
+  // that takes longer, query items' after the kv items' full rounds.  A share of a split item writes
+  // and reads its partial sums, and the last one to arrive adds the others'; the kernel that can split
+  // takes longer over whole kv items too.  The constants are those that choose best among 1 to 16 shares of kv items
   // and 1 to 8 of query items over 7000 random shapes (1 to 96 heads, 32 to 8000 queries and keys): its
-  // choices take 1.8 % longer than the best ones on average, no splits 16 %.  GB300, us, unsplit / split: B1 H8/1 S2000
+  // choices take 1.7 % longer than the best ones on average, no splits 16 %.  GB300, us, unsplit / split: B1 H8/1 S2000
   // causal 158 / 47, B1 H32/8 S2048 causal 136 / 100; B1 H16/16 S2048 causal, an item for each SM and more,
   // 52 / 73.
   const auto tiles = [&](long long rows) {
@@ -71,12 +72,13 @@ inline BwdPlan bwd_plan(int B, int Hq, int Hkv, long long Sq, long long Skv, int
       // (a quarter of a gigabyte of partial sums of each kind at most)
       if (a > 1 && p.kv_items * a * 1024.0 * D > 2.7e8) continue;
       if (b > 1 && p.q_items * b * 512.0 * D > 2.7e8) continue;
-      const double k_all = kv_steps * seen * kv_step + 2.5 + (a > 1 ? a * kv_part : 0);
+      const double k_all = kv_steps * seen * kv_step + 2.5 + (a > 1 ? a * kv_part : b > 1 ? 0.9 : 0);
       const double q_all = q_steps * seen * q_step + 2.1 + (b > 1 ? b * q_part : 0);
       const double k_long = kv_steps * kv_step / a + 2.5 + (a > 1 ? 4.3 + 1.1 * a : 0);
       const double q_long = q_steps * q_step / b + 2.1 + (b > 1 ? 0.35 * b : 0);
       const double spread = (p.kv_items * k_all + p.q_items * q_all) / sms + 0.42 * k_long + 0.16 * q_long;
-      const double longest = k_long > q_long ? k_long : q_long, us = spread > longest ? spread : longest;
+      const double rounds = static_cast<double>(p.kv_items * a / sms) * (k_all / a), q_end = 0.85 * rounds + q_long;
+      const double longest = k_long > q_end ? k_long : q_end, us = spread > longest ? spread : longest;
       if (us < best) best = us, p.kv_split = a, p.q_split = b;
     }
   const bool any = p.kv_split > 1 || p.q_split > 1;
@@ -90,7 +92,8 @@ inline BwdPlan bwd_plan(int B, int Hq, int Hkv, long long Sq, long long Skv, int
 
 // The workspace of a call, causal or not.
 inline size_t bwd_workspace(int B, int Hq, int Hkv, long long Sq, long long Skv, int D, bool ragged, int sms) {
-  const size_t full = bwd_plan(B, Hq, Hkv, Sq, Skv, D, ragged, false, sms).bytes, causal = bwd_plan(B, Hq, Hkv, Sq, Skv, D, ragged, true, sms).bytes;
+  const size_t full = bwd_plan(B, Hq, Hkv, Sq, Skv, D, ragged, false, sms).bytes;
+  const size_t causal = bwd_plan(B, Hq, Hkv, Sq, Skv, D, ragged, true, sms).bytes;
   return full > causal ? full : causal;
 }
 
