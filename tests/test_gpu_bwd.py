@@ -320,6 +320,47 @@ def test_a_skipped_copy_times_out_and_the_next_call_is_right(loom):
     _check_dense(host, grads, False, 128 ** -0.5)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("ragged", [False, True])
+@pytest.mark.parametrize("Hq,Hkv", [(16, 16), (8, 1)])
+def test_a_skipped_copy_times_out_in_every_form(loom, Hq, Hkv, ragged, D):
+    """Whole and split items (8 heads of one kv head)."""
+    def call():
+        if ragged:
+            return _ragged(loom, (130, 900, 513), (130, 900, 513), Hq, Hkv, D, False, False)
+        return _dense(loom, 1, Hq, Hkv, 700, 700, D, False, False)
+
+    loom.loom_attn_check_error()
+    loom.loom_debug_set_timeout_ns(50_000_000)
+    loom.loom_debug_inject(4)
+    try:
+        with pytest.raises(loom.LoomError) as e:
+            call()
+        assert e.value.status == 6
+    finally:
+        loom.loom_debug_inject(0)
+        loom.loom_debug_set_timeout_ns(0)
+    out = call()
+    if ragged:
+        _check_ragged(*out, False, D ** -0.5)
+    else:
+        _check_dense(*out, False, D ** -0.5)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("ql,kl", [((1, 900, 700), (1, 900, 700)), ((2, 5, 1200), (900, 1500, 1300)), ((40, 64), (2500, 1900))])
+def test_few_long_ragged_items_are_split(loom, ql, kl, causal, D):
+    """Few tiles with many steps, whose sums are split and joined (the workspace shows that they are);
+    the same bits each time."""
+    host, grads, cq, ck = _ragged(loom, ql, kl, 8, 1, D, causal, True)
+    stats = 8 * (sum(ql) + 128 * len(ql)) * 8
+    assert loom.loom_attn_bwd_varlen_workspace_bytes(len(ql), 8, 1, sum(ql), sum(kl), D) > 2 * stats
+    _check_ragged(host, grads, cq, ck, causal, D ** -0.5)
+    again = _ragged(loom, ql, kl, 8, 1, D, causal, True)[1]
+    assert all((a == b).all() for a, b in zip(grads, again))
+
+
 def test_refusals_of_the_binding(loom):
     import torch
     host, _ = _dense(loom, 1, 4, 2, 20, 20, 64, False, False)
