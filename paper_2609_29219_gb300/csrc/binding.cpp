@@ -105,7 +105,8 @@ void* stream_of(long long device) {
 PyObject* make(long long device, int dims, const long long* size, at::ScalarType type, void** ptr) {
   int64_t n[4];
   for (int i = 0; i < dims; ++i) n[i] = size[i];
-  at::Tensor t(at::detail::empty_cuda(at::IntArrayRef(n, static_cast<size_t>(dims)), type, at::Device(at::kCUDA, static_cast<c10::DeviceIndex>(device)), std::nullopt));
+  const at::Device cuda(at::kCUDA, static_cast<c10::DeviceIndex>(device));
+  at::Tensor t(at::detail::empty_cuda(at::IntArrayRef(n, static_cast<size_t>(dims)), type, cuda, std::nullopt));
   *ptr = t.data_ptr();
   return THPVariable_Wrap(std::move(t));
 }
