@@ -224,7 +224,7 @@ loom_status loom_attn_decode_noalloc(const void* q, const void* k_cache, const v
  * dk and dv summed over the query heads of a kv head.
  *   dout   [B, Hq, Sq, D]   bf16, read: the gradient of o
  *   q, k, v, o, lse          read: the arguments and results of loom_attn_fwd (lse is required);
- *                            a row with lse = -inf gives and gets no gradient
+ *                            a row with lse = -inf gives and gets no gradient, whatever o and dlse hold
  *   dlse   [B, Hq, Sq]      fp32, read: the gradient of lse; NULL where none is wanted
  *   dq     [B, Hq, Sq, D]   bf16, written
  *   dk, dv [B, Hkv, Skv, D] bf16, written
@@ -251,8 +251,9 @@ size_t loom_attn_bwd_workspace_bytes(int B, int Hq, int Hkv, int Sq, int Skv, in
  *   dout, o, dq  [total_q, Hq, D];  k, v, dk, dv  [total_k, Hkv, D];  lse, dlse  [Hq, total_q]
  *   cu_seqlens_q, cu_seqlens_k  as loom_attn_fwd_varlen
  *   max_seqlen_q, max_seqlen_k  upper bounds of the lengths (they only size the launch)
- * No row of one sequence reaches another's gradients, whatever it holds.  total_q = 0 or total_k =
- * 0 writes zeros; pointers to tensors without elements may be NULL.
+ * No row of one sequence reaches another's gradients, whatever it holds, nor does a query that sees
+ * no key (causal, more queries than keys) reach any gradient.  total_q = 0 or total_k = 0 writes
+ * zeros; pointers to tensors without elements may be NULL.
  * Errors: as loom_attn_bwd; cu_seqlens must be 4-byte aligned.
  */
 loom_status loom_attn_bwd_varlen(const void* dout, const void* q, const void* k, const void* v,

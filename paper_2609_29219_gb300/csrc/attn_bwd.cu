@@ -118,8 +118,8 @@ struct Item {
   int g, t;       // the share's first step: plane of the group (kv items), tile
   int shares;     // shares of the item that have steps
   int id, share;  // the item, and which of its shares this is
-  int sq, skv;    // lengths in queries and keys
-  int qb, kb;     // first query and key row of the sequence (0 for dense)
+  int sq, skv;    // lengths in queries (that see a key) and keys
+  int qb, kb;     // first query (that sees a key) and key row of the sequence (0 for dense)
   int stat0;      // first tile of the sequence within a plane's row statistics
 };
 static_assert(sizeof(Item) <= 64, "item record");
@@ -155,6 +155,10 @@ __device__ __forceinline__ bool cursor_to(Cursor& cur, const int32_t* cu, int lg
   }
   return cur.b < B;
 }
+// Queries at a ragged sequence's start that see no key (causal, more queries than keys).  The walks
+// begin behind them: masked by a probability of zero alone, a NaN or an infinity of theirs would reach
+// the others' gradients.
+__device__ __forceinline__ int unseen_queries(int sq, int skv, int causal) { return causal ? max(0, sq - skv) : 0; }
 // First tile of sequence b in a plane's row statistics: tiles of different sequences never meet.
 __device__ __forceinline__ int ragged_stat0(const int32_t* cu_q, int b, int lg) {
   return static_cast<int>((static_cast<long long>(cu_q[b]) << lg) / kTile) + b;
@@ -188,6 +192,9 @@ __device__ __forceinline__ Item make_item(const BwdParams& p, long long idx, Cur
     it.kb = p.cu_k[b];
     it.sq = p.cu_q[b + 1] - it.qb;
     it.skv = p.cu_k[b + 1] - it.kb;
+    const int unseen = unseen_queries(it.sq, it.skv, p.causal);
+    it.qb += unseen;
+    it.sq -= unseen;
     it.stat0 = ragged_stat0(p.cu_q, b, p.lg);
     // (causal query tiles are longest at the sequence's end)
     if (!KV && p.causal) tile = cur.tiles - 1 - tile;
@@ -227,7 +234,8 @@ __device__ __forceinline__ Item make_item(const BwdParams& p, long long idx, Cur
     }
   } else {
     const int seen = p.causal ? min(it.skv, ((it.row0 + kTile) >> p.lg) + off) : it.skv;
-    const int steps = seen > 0 ? (seen + kTile - 1) / kTile : 0;
+    // (ragged: the sequence has a tile for the unseen queries too)
+    const int steps = seen > 0 && (!VARLEN || it.row0 < it.sq << p.lg) ? (seen + kTile - 1) / kTile : 0;
     it.n = steps;
     it.t = 0;
     if constexpr (SPLIT) {
@@ -1082,13 +1090,14 @@ __global__ void __launch_bounds__(kThreads<VARLEN>, 1)
 
 // ---------------------------------------------------------------- row statistics
 // kTile / kRowsPerBlock blocks per tile of 128 rows of a query plane: -LSE log2(e) and dLSE - dO . O for each row.
-// Rows past the end, and rows whose LSE is -inf (no key is seen), get -inf and P = 0.  Bound by
-// reading dO and O once; D / 8 lanes of 16 bytes take a row.
+// Rows past the end, and rows whose LSE is -inf, get -inf and 0, so P = 0 and dS = 0 whatever their dLSE
+// and O are.  A ragged sequence's rows are counted from its first query that sees a key; dQ of those before it
+// becomes zeros here.  Bound by reading dO and O once; D / 8 lanes of 16 bytes take a row.
 template <int D, bool VARLEN>
 __global__ void __launch_bounds__(kRowThreads)
     attn_bwd_rows_kernel(const __nv_bfloat16* dout, const __nv_bfloat16* o, const float* lse, const float* dlse, float* stats,
                          unsigned int* counters, int n_counters, int B, int H, int Sq, int lg, int stat_tiles,
-                         const int32_t* cu_q) {
+                         const int32_t* cu_q, const int32_t* cu_k, int causal, __nv_bfloat16* dq) {
   constexpr int LPR = D / 8, PASSES = kRowsPerBlock * LPR / kRowThreads;  // lanes per row
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;");
@@ -1097,7 +1106,7 @@ __global__ void __launch_bounds__(kRowThreads)
     counters[i] = 0;
   const int at_tile = static_cast<int>(blockIdx.x / (kTile / kRowsPerBlock)), part = static_cast<int>(blockIdx.x % (kTile / kRowsPerBlock));
   const int plane = at_tile / stat_tiles, tile = at_tile % stat_tiles;
-  int row0 = tile * kTile, n = Sq, qb = 0;
+  int row0 = tile * kTile, n = Sq, qb = 0, unseen = 0;
   if constexpr (VARLEN) {
     int lo = 0, hi = B - 1;  // the last sequence that starts at this tile or before it
     while (lo < hi) {
@@ -1111,6 +1120,8 @@ __global__ void __launch_bounds__(kRowThreads)
     n = cu_q[lo + 1] - qb;
     row0 = (tile - ragged_stat0(cu_q, lo, lg)) * kTile;
     if (row0 < 0 || row0 >= n << lg) return;  // a tile of no sequence
+    unseen = unseen_queries(n, cu_k[lo + 1] - cu_k[lo], causal);
+    n -= unseen;
   }
   const int l = threadIdx.x % LPR, r0 = part * kRowsPerBlock + static_cast<int>(threadIdx.x) / LPR;
   float* st = stats + static_cast<size_t>(at_tile) * kStat;
@@ -1120,7 +1131,9 @@ __global__ void __launch_bounds__(kRowThreads)
   for (int i = 0; i < PASSES; ++i) {
     const int row = row0 + r0 + i * (kRowThreads / LPR), query = row >> lg;
     const long long head = (static_cast<long long>(plane) << lg) + (row & ((1 << lg) - 1));
-    const long long at = VARLEN ? static_cast<long long>(qb + query) * H + head : head * Sq + query;
+    const long long at = VARLEN ? static_cast<long long>(qb + unseen + query) * H + head : head * Sq + query;
+    if (VARLEN && query < unseen)
+      *reinterpret_cast<uint4*>(dq + (static_cast<long long>(qb + query) * H + head) * D + 8 * l) = make_uint4(0, 0, 0, 0);
     x[i] = y[i] = make_uint4(0, 0, 0, 0);
     nl[i] = -INFINITY;
     dl[i] = 0.f;
@@ -1128,7 +1141,7 @@ __global__ void __launch_bounds__(kRowThreads)
       x[i] = *reinterpret_cast<const uint4*>(dout + at * D + 8 * l);
       y[i] = *reinterpret_cast<const uint4*>(o + at * D + 8 * l);
       if (l == 0) {
-        const long long s = VARLEN ? head * Sq + qb + query : at;
+        const long long s = VARLEN ? head * Sq + qb + unseen + query : at;
         const float e = lse[s];
         nl[i] = e == -INFINITY ? -INFINITY : -e * kLog2e;
         if (dlse) dl[i] = dlse[s];
@@ -1146,7 +1159,7 @@ __global__ void __launch_bounds__(kRowThreads)
     if (l == 0) {
       const int r = r0 + i * (kRowThreads / LPR);
       st[r] = nl[i];
-      st[kTile + r] = dl[i] - a;
+      st[kTile + r] = nl[i] == -INFINITY ? 0.f : dl[i] - a;
     }
   }
 }
@@ -1252,7 +1265,7 @@ cudaError_t launch_d(const BwdArgs& a, const KernelCtl& ctl, cudaStream_t stream
   float* stats = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + plan.stats_at);
   e = launch(attn_bwd_rows_kernel<D, VARLEN>, static_cast<int>(q_planes * stat_tiles) * (kTile / kRowsPerBlock), kRowThreads, 0, stream,
              static_cast<const __nv_bfloat16*>(a.dout), static_cast<const __nv_bfloat16*>(a.o), a.lse, a.dlse, stats, counters,
-             plan.counters, a.B, a.Hq, a.Sq, lg, stat_tiles, a.cu_q);
+             plan.counters, a.B, a.Hq, a.Sq, lg, stat_tiles, a.cu_q, a.cu_k, a.causal, static_cast<__nv_bfloat16*>(a.dq));
   if (e != cudaSuccess) return e;
   BwdParams p;
   memset(&p, 0, sizeof(p));
