@@ -5,10 +5,12 @@
 
 Each function saves its inputs (attention also O and LSE) and calls the entry points of the
 package; a gradient of LSE is taken into account.  ``linear`` is the BF16 GEMM with its gradients.
+The kernels have first gradients only: differentiating a gradient raises.
 """
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 import paper_2609_29219_gb300 as loom
 
@@ -23,6 +25,7 @@ class _Attention(torch.autograd.Function):
         return o, lse
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, do, dlse):
         q, k, v, o, lse = ctx.saved_tensors
         do = torch.zeros_like(o) if do is None else do.contiguous()
@@ -46,6 +49,7 @@ class _AttentionVarlen(torch.autograd.Function):
         return o, lse
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, do, dlse):
         q, k, v, o, lse, cu_q, cu_k = ctx.saved_tensors
         max_q, max_k, causal, scale = ctx.rest
@@ -70,6 +74,7 @@ class _QkvNormRope(torch.autograd.Function):
                                        **ctx.rest)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dq, dk, dv):
         qkv, q_weight, k_weight, cos, sin, positions = ctx.saved_tensors
         dqkv, dqw, dkw = loom.loom_qkv_norm_rope_bwd(dq.contiguous(), dk.contiguous(), dv.contiguous(), qkv, q_weight, k_weight,
@@ -90,6 +95,7 @@ class _Linear(torch.autograd.Function):
         return loom.loom_gemm_bf16(x, weight, b_transposed=True)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         x, weight = ctx.saved_tensors
         dy = dy.contiguous()
