@@ -84,7 +84,10 @@ class _QkvNormRope(torch.autograd.Function):
 
 def qkv_norm_rope(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, positions=None, *, seq_len=0, eps=1e-6,
                   interleaved=False):
-    """``loom_qkv_norm_rope`` with gradients of qkv and the two norm weights: (q, k, v)."""
+    """``loom_qkv_norm_rope`` with gradients of qkv and the two norm weights: (q, k, v).  The tables have none."""
+    for t, name in ((cos, "cos"), (sin, "sin")):
+        if t.requires_grad and torch.is_grad_enabled():
+            raise ValueError(f"{name} requires a gradient, which qkv_norm_rope does not have: detach it")
     return _QkvNormRope.apply(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, positions, seq_len, eps, interleaved)
 
 

@@ -91,3 +91,13 @@ def test_a_second_differentiation_is_refused(autograd, i):
     first = torch.autograd.grad(out.square().sum(), args[0], create_graph=True)[0]
     with pytest.raises(RuntimeError):
         (out.sum() + first.square().sum()).backward()
+
+
+@pytest.mark.parametrize("which", ["cos", "sin"])
+def test_tables_that_want_a_gradient_are_refused(autograd, which):
+    tables = {n: _rand(6, 4, grad=n == which) for n in ("cos", "sin")}
+    args = (_rand(6, 32), _rand(8), _rand(8), tables["cos"], tables["sin"], 2, 1)
+    with pytest.raises(ValueError, match=which):
+        autograd.qkv_norm_rope(*args)
+    with torch.no_grad():  # nothing is differentiated here
+        assert autograd.qkv_norm_rope(*args)[0].shape == (6, 2, 8)
