@@ -242,15 +242,40 @@ def _fast_result(r, where):
     raise LoomError(r, where)
 
 
-def _new(shape, strides, dtype, t, like=False):
+def _new(shape, strides, dtype, t, like=False, stream=None):
     """An uninitialised contiguous tensor (strides: its strides) on CUDA tensor t's device
-    (like: of t's shape and type).  It passes torch's dispatcher by only where nobody would
-    miss the call: no dispatch or function mode, no deterministic mode (which fills new
-    tensors), no subclass of Tensor."""
+    (like: of t's shape and type), for a call on the stream.  It passes torch's dispatcher by
+    only where nobody would miss the call: no dispatch or function mode, no deterministic mode
+    (which fills new tensors), no subclass of Tensor."""
+    if stream is not None and not _is_current(stream, t):
+        return _new_on(stream, shape, dtype, t, like)
     if _direct(t):
         return _empty_strided_cuda(shape, strides, dtype)
     torch = _torch_mod
     return torch.empty_like(t) if like else torch.empty(shape, dtype=dtype, device=t.device)
+
+
+def _is_current(stream, t):
+    """Whether the stream given is the current one of tensor t's device."""
+    return _stream_ptr(stream, t.device) == _stream_of(None, t)
+
+
+def _new_on(stream, shape, dtype, t, like=False):
+    """_new for a call on a stream given.  The allocator must know that the tensor is that stream's:
+    memory of the current stream may still be in use by what is queued there, and is handed out again there
+    as soon as the tensor is gone (scratch: when the call returns), whatever this stream does.  It is noted as
+    used on the current stream too, where a program that waits for this one may read it."""
+    torch = _torch_mod
+    if not isinstance(stream, torch.cuda.Stream):
+        handle = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+        # (0 and 1: the default stream's handles)
+        stream = torch.cuda.ExternalStream(handle, t.device) if handle > 1 else torch.cuda.default_stream(t.device)
+    if stream.device != t.device:
+        raise ValueError(f"the stream is of {stream.device}, the tensors are on {t.device}")
+    with torch.cuda.stream(stream):
+        new = torch.empty_like(t) if like else torch.empty(shape, dtype=dtype, device=t.device)
+    new.record_stream(torch.cuda.current_stream(t.device))
+    return new
 
 
 def _direct(t):
@@ -261,12 +286,21 @@ def _direct(t):
             and t.get_device() == c._cuda_getDevice())
 
 
-def _maker(t):
+def _maker(t, stream):
     """What makes uninitialised contiguous tensors on tensor t's device, of (shape, strides, type):
     _new for a call that makes several (GB300 host: 0.9 us a tensor, 1.3 by _new)."""
+    if stream is not None and not _is_current(stream, t):
+        return lambda shape, strides, dtype: _new_on(stream, shape, dtype, t)
     if _direct(t):
         return _empty_strided_cuda
     return lambda shape, strides, dtype: _torch_mod.empty(shape, dtype=dtype, device=t.device)
+
+
+def _workspace(need, t, stream):
+    """Scratch of a decode call."""
+    if stream is not None and not _is_current(stream, t):
+        return _new_on(stream, (max(need, 16),), _u8, t)
+    return _torch_mod.empty(max(need, 16), dtype=_u8, device=t.device)
 
 
 def _ptr(t, name, dtype, ndim):
@@ -314,6 +348,8 @@ def _check(status: int, where: str):
 
 
 # ------------------------------------------------------------------ C-ABI functions
+# stream: None (the current one), a torch stream or a handle.  Outputs and scratch that a call on
+# a stream given allocates belong to that stream, as under torch.cuda.stream.
 def loom_attn_fwd(q, k, v, o=None, lse=None, *, causal=False, scale=None, stream=None,
                   return_lse=False):
     """Prefill attention.  q [B,Hq,Sq,D], k/v [B,Hkv,Skv,D] bf16 CUDA tensors.
@@ -331,12 +367,12 @@ def loom_attn_fwd(q, k, v, o=None, lse=None, *, causal=False, scale=None, stream
     if v.shape != k.shape or Bk != B or Dk != D:
         raise ValueError("q/k/v shapes disagree")
     if o is None:
-        o = _new((B, Hq, Sq, D), (Hq * Sq * D, Sq * D, D, 1), bf16, q, True)
+        o = _new((B, Hq, Sq, D), (Hq * Sq * D, Sq * D, D, 1), bf16, q, True, stream)
     if o.shape != q.shape:
         raise ValueError("o must have q's shape")
     op = _ptr(o, "o", bf16, 4)
     if lse is None and return_lse:
-        lse = _new((B, Hq, Sq), (Hq * Sq, Sq, 1), torch.float32, q)
+        lse = _new((B, Hq, Sq), (Hq * Sq, Sq, 1), torch.float32, q, stream=stream)
     lp = None
     if lse is not None:
         if tuple(lse.shape) != (B, Hq, Sq):
@@ -358,7 +394,7 @@ def loom_attn_decode_workspace_bytes(B, Hq, Hkv, Skv, D, num_splits=0) -> int:
     return int(capi().loom_attn_decode_workspace_bytes(B, Hq, Hkv, Skv, D, num_splits))
 
 
-def _decode_operands(q, k_cache, v_cache, seqlens_k, o, lse, return_lse):
+def _decode_operands(q, k_cache, v_cache, seqlens_k, o, lse, return_lse, stream):
     """Pointers and sizes of the contiguous decode entry points' tensor arguments."""
     torch = _torch()
     bf16 = torch.bfloat16
@@ -375,10 +411,10 @@ def _decode_operands(q, k_cache, v_cache, seqlens_k, o, lse, return_lse):
             raise ValueError("seqlens_k must be [B]")
         sp = _ptr(seqlens_k, "seqlens_k", torch.int32, 1)
     if o is None:
-        o = _new((B, Hq, 1, D), (Hq * D, D, D, 1), bf16, q, True)
+        o = _new((B, Hq, 1, D), (Hq * D, D, D, 1), bf16, q, True, stream)
     op = _ptr(o, "o", bf16, 4)
     if lse is None and return_lse:
-        lse = _new((B, Hq), (Hq, 1), torch.float32, q)
+        lse = _new((B, Hq), (Hq, 1), torch.float32, q, stream=stream)
     lp = None
     if lse is not None:
         if lse.numel() != B * Hq:
@@ -396,10 +432,10 @@ def loom_attn_decode(q, k_cache, v_cache, seqlens_k=None, o=None, lse=None, work
     """
     torch = _torch()
     (qp, kp, vp_, sp, op, lp), (B, Hq, Hkv, Skv, D), o, lse = _decode_operands(
-        q, k_cache, v_cache, seqlens_k, o, lse, return_lse)
+        q, k_cache, v_cache, seqlens_k, o, lse, return_lse, stream)
     if workspace is None:
         need = loom_attn_decode_workspace_bytes(B, Hq, Hkv, Skv, D, num_splits)
-        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
+        workspace = _workspace(need, q, stream)
     wp = _dev_ptr(workspace, "workspace")
     if scale is None:
         scale = D ** -0.5
@@ -415,7 +451,7 @@ def loom_attn_decode_noalloc(q, k_cache, v_cache, seqlens_k=None, o=None, lse=No
     workspace argument, no device allocation by the library).  Arguments and results as
     ``loom_attn_decode``; problems whose partials exceed the array raise LOOM_ERR_WORKSPACE."""
     (qp, kp, vp_, sp, op, lp), (B, Hq, Hkv, Skv, D), o, lse = _decode_operands(
-        q, k_cache, v_cache, seqlens_k, o, lse, return_lse)
+        q, k_cache, v_cache, seqlens_k, o, lse, return_lse, stream)
     if scale is None:
         scale = D ** -0.5
     st = (_lib or capi()).loom_attn_decode_noalloc(qp, kp, vp_, sp, op, lp, B, Hq, Hkv, Skv, D, float(scale),
@@ -444,10 +480,10 @@ def loom_attn_fwd_varlen(q, k, v, cu_seqlens_q, cu_seqlens_k, max_seqlen_q, o=No
         raise ValueError("cu_seqlens_q and cu_seqlens_k must both be [B + 1]")
     B = cu_seqlens_q.numel() - 1
     if o is None:
-        o = _new((total_q, Hq, D), (Hq * D, D, 1), bf16, q, True)
+        o = _new((total_q, Hq, D), (Hq * D, D, 1), bf16, q, True, stream)
     op = _ptr(o, "o", bf16, 3)
     if lse is None and return_lse:
-        lse = _new((Hq, total_q), (total_q, 1), torch.float32, q)
+        lse = _new((Hq, total_q), (total_q, 1), torch.float32, q, stream=stream)
     lp = None
     if lse is not None:
         if lse.numel() != Hq * total_q:
@@ -490,10 +526,10 @@ def loom_attn_decode_paged(q, k_cache, v_cache, block_table, seqlens_k, o=None, 
         raise ValueError("seqlens_k must be [B]")
     sp = _ptr(seqlens_k, "seqlens_k", torch.int32, 1)
     if o is None:
-        o = _new((B, Hq, 1, D), (Hq * D, D, D, 1), bf16, q, True)
+        o = _new((B, Hq, 1, D), (Hq * D, D, D, 1), bf16, q, True, stream)
     op = _ptr(o, "o", bf16, 4)
     if lse is None and return_lse:
-        lse = _new((B, Hq), (Hq, 1), torch.float32, q)
+        lse = _new((B, Hq), (Hq, 1), torch.float32, q, stream=stream)
     lp = None
     if lse is not None:
         if lse.numel() != B * Hq:
@@ -502,7 +538,7 @@ def loom_attn_decode_paged(q, k_cache, v_cache, block_table, seqlens_k, o=None, 
     Skv = max_pages * page_size
     if workspace is None:
         need = loom_attn_decode_workspace_bytes(B, Hq, Hkv, Skv, D, num_splits)
-        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
+        workspace = _workspace(need, q, stream)
     wp = _dev_ptr(workspace, "workspace")
     if scale is None:
         scale = D ** -0.5
@@ -595,7 +631,7 @@ def loom_attn_bwd(do, q, k, v, o, lse, dq=None, dk=None, dv=None, workspace=None
         _bwd_checked(do, q, k, v, o, lse, dlse, dq, dk, dv, 4)
     if tuple(lse.shape) != (B, Hq, Sq):
         raise ValueError("lse must be [B, Hq, Sq]")
-    new = _maker(q)
+    new = _maker(q, stream)
     if dq is None:
         dq = new(tuple(qs), (Hq * Sq * D, Sq * D, D, 1), _bf16)
     if dk is None:
@@ -643,7 +679,7 @@ def loom_attn_bwd_varlen(do, q, k, v, o, lse, cu_seqlens_q, cu_seqlens_k, max_se
     B = cu_seqlens_q.shape[0] - 1
     if cu_seqlens_k.shape[0] != B + 1 or B < 1:
         raise ValueError("cu_seqlens_q and cu_seqlens_k must both be [B + 1]")
-    new = _maker(q)
+    new = _maker(q, stream)
     if dq is None:
         dq = new(tuple(qs), (Hq * D, D, 1), _bf16)
     if dk is None:
@@ -751,7 +787,7 @@ def loom_qkv_norm_rope(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_head
     for t, name, shape in ((q, "q", qs), (k, "k", ks), (v, "v", ks)) if q is not None or k is not None or v is not None else ():
         if t is not None and (_dev_ptr(t, name, _bf16) is None or tuple(t.shape) != shape):
             raise ValueError(f"{name} must be {list(shape)}")
-    new = _maker(qkv)
+    new = _maker(qkv, stream)
     if q is None:
         q = new(qs, qst, _bf16)
     if k is None:
@@ -806,7 +842,7 @@ def loom_qkv_norm_rope_cache(qkv, q_weight, k_weight, cos, sin, positions, slots
     if Dk != D or slots.shape[0] != T:
         raise ValueError("the caches must have the weights' D, and slots be [T]")
     if q is None:
-        q = _new((T, num_heads, D), (num_heads * D, D, 1), _bf16, qkv)
+        q = _new((T, num_heads, D), (num_heads * D, D, 1), _bf16, qkv, stream=stream)
     elif _dev_ptr(q, "q", _bf16, 3) is None or tuple(q.shape) != (T, num_heads, D):
         raise ValueError(f"q must be {[T, num_heads, D]}")
     st = (_lib or capi()).loom_qkv_norm_rope_cache(
@@ -848,7 +884,7 @@ def loom_qkv_norm_rope_bwd(dq, dk, dv, qkv, q_weight, k_weight, cos, sin, positi
             or tuple(ks) != (qs[0], Hkv, *qs[2:])):
         raise ValueError("dq, dk and dv must be laid out as q, k and v of the forward call")
     width = (Hq + 2 * Hkv) * D
-    new = _maker(qkv)
+    new = _maker(qkv, stream)
     if dqkv is None:
         dqkv, drow = new((T, width), (width, 1), _bf16), width
     else:
@@ -936,7 +972,7 @@ def loom_gemm_bf16(a, b, c=None, *, stream=None, b_transposed=False):
     if K2 != K:
         raise ValueError(f"a is [M, {K}] but b has {K2} along K")
     if c is None:
-        c = _new((M, N), (N, 1), bf16, a)
+        c = _new((M, N), (N, 1), bf16, a, stream=stream)
     cp = _ptr(c, "c", bf16, 2)
     if tuple(c.shape) != (M, N):
         raise ValueError("c must be [M, N]")
