@@ -278,14 +278,16 @@ size_t loom_attn_bwd_varlen_workspace_bytes(int B, int Hq, int Hkv, int total_q,
  *   q_weight, k_weight  [D], read: bf16 or fp32 (weight_type)
  *   cos, sin   [table_rows, rotary_dim / 2] fp32, read
  *   positions  [T] int32 on the device: the tables' row of each token, clamped to the tables;
- *              NULL: token t has position t, or t % seq_len with seq_len > 0
+ *              NULL: token t has position t, or t % seq_len with seq_len > 0, and the tables must
+ *              have a row for each
  *   q, k, v    bf16, written.  seq_len = 0: packed [T, Hq, D] and [T, Hkv, D] (as
  *              loom_attn_fwd_varlen takes them); seq_len > 0: T / seq_len sequences,
  *              [T / seq_len, Hq or Hkv, seq_len, D] (as loom_attn_fwd takes them).  They must not
  *              overlap qkv.
  * Arithmetic is fp32; each value is rounded once, when it is stored.
  * Errors: INVALID_ARG (NULL pointer, a size <= 0, T < 0, T % seq_len, qkv_stride below a row, eps
- * not finite or <= 0, weight_type or interleaved not one of theirs), UNSUPPORTED (D not 64 or 128;
+ * not finite or <= 0, weight_type or interleaved not one of theirs, tables shorter than the positions
+ * that NULL implies), UNSUPPORTED (D not 64 or 128;
  * rotary_dim not a multiple of 16 from 16 to D), MISALIGNED (positions: 4 bytes; the others 16;
  * qkv_stride % 8), CUDA.  T = 0 returns LOOM_OK at once.
  */

@@ -762,6 +762,12 @@ def _norm_operands(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, p
         1 if interleaved else 0, None if positions is None else positions.data_ptr())
 
 
+def _check_tables(T, seq_len, cos, positions):
+    """Without positions, the tables must have a row for each that is implied."""
+    if positions is None and T and (seq_len or T) > cos.shape[0]:
+        raise ValueError(f"cos and sin have {cos.shape[0]} rows, positions go up to {(seq_len or T) - 1}")
+
+
 def loom_qkv_norm_rope(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, positions=None, q=None, k=None, v=None, *,
                        seq_len=0, eps=1e-6, interleaved=False, stream=None):
     """RMS norm of each query and key head, the position rotation, and the split of a packed projection.
@@ -779,6 +785,7 @@ def loom_qkv_norm_rope(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_head
     S = seq_len
     if S < 0 or (S and T % S):
         raise ValueError("T must be a multiple of seq_len")
+    _check_tables(T, S, cos, positions)
     if S:
         qs, ks = (T // S, num_heads, S, D), (T // S, num_kv_heads, S, D)
         qst, kst = (num_heads * S * D, S * D, D, 1), (num_kv_heads * S * D, S * D, D, 1)
@@ -883,6 +890,7 @@ def loom_qkv_norm_rope_bwd(dq, dk, dv, qkv, q_weight, k_weight, cos, sin, positi
     if (not fine or tuple(qs) != ((qs[0], Hq, S, D) if ndim == 4 else (T, Hq, D)) or (qs[0] * S if ndim == 4 else T) != T
             or tuple(ks) != (qs[0], Hkv, *qs[2:])):
         raise ValueError("dq, dk and dv must be laid out as q, k and v of the forward call")
+    _check_tables(T, S, cos, positions)
     width = (Hq + 2 * Hkv) * D
     new = _maker(qkv, stream)
     if dqkv is None:

@@ -204,6 +204,8 @@ struct Norm {
   int type, P, R, interleaved;
   float eps;
   const int32_t* positions() const { return static_cast<const int32_t*>(pos.ptr); }
+  // the tables have the rows that no positions given imply
+  bool tables_reach(long long S) const { return pos.t || (S > 0 ? S : T) <= P; }
 };
 bool norm_args(PyObject* const* a, long long heads, Norm* m) {
   if (!view(a[0], kBf16, &m->x, true) || m->x.dims != 2 || !small(m->x)) return false;
@@ -230,7 +232,7 @@ PyObject* norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
   long long Hq, Hkv, S;
   Norm m;
   if (n != 11 || !as_int(a[8], &Hq) || !as_int(a[9], &Hkv) || !as_int(a[10], &S) || Hq <= 0 || Hkv <= 0 ||
-      !norm_args(a, Hq + 2 * Hkv, &m) || (S > 0 && m.T % S))
+      !norm_args(a, Hq + 2 * Hkv, &m) || (S > 0 && m.T % S) || !m.tables_reach(S))
     Py_RETURN_NONE;
   const long long dev = device_of(m.x);
   if (dev < 0) Py_RETURN_NONE;
@@ -289,7 +291,8 @@ PyObject* norm_rope_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Py_RETURN_NONE;
   const long long Hq = dq.size[1], Hkv = dk.size[1], S = dq.dims == 4 ? dq.size[2] : 0;
   if (!norm_args(a, Hq + 2 * Hkv, &m) || dq.size[0] != dk.size[0] || dq.size[2] != dk.size[2] || dq.size[dq.dims - 1] != m.D ||
-      dk.size[dk.dims - 1] != m.D || (S ? dq.size[0] * S : dq.size[0]) != m.T || (dq.dims == 4 && S == 0))
+      dk.size[dk.dims - 1] != m.D || (S ? dq.size[0] * S : dq.size[0]) != m.T || (dq.dims == 4 && S == 0) ||
+      !m.tables_reach(S))
     Py_RETURN_NONE;
   const long long dev = device_of(m.x);
   if (dev < 0) Py_RETURN_NONE;

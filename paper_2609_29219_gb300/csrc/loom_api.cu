@@ -444,6 +444,11 @@ loom_status qkv_common(QkvArgs* a, const void* qkv, int64_t qkv_stride, const vo
   a->eps = eps;
   return LOOM_OK;
 }
+
+// Whether the tables have a row for each position that no positions given imply.
+bool tables_reach(const int32_t* positions, int T, int seq_len, int table_rows) {
+  return positions || T == 0 || (seq_len > 0 ? seq_len : T) <= table_rows;
+}
 }  // namespace
 
 loom_status loom_qkv_norm_rope(const void* qkv, int64_t qkv_stride, const void* q_weight, const void* k_weight,
@@ -455,6 +460,7 @@ loom_status loom_qkv_norm_rope(const void* qkv, int64_t qkv_stride, const void* 
                                     interleaved, positions, T, Hq, Hkv, D, eps);
   if (st != LOOM_OK) return st;
   if (seq_len < 0 || (seq_len > 0 && T % seq_len) || (T > 0 && (!q || !k || !v))) return LOOM_ERR_INVALID_ARG;
+  if (!tables_reach(positions, T, seq_len, table_rows)) return LOOM_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(k) || !aligned16(v)) return LOOM_ERR_MISALIGNED;
   if (T == 0) return LOOM_OK;
   a.q = q;
@@ -508,6 +514,7 @@ loom_status loom_qkv_norm_rope_bwd(const void* dq, const void* dk, const void* d
   if (st != LOOM_OK) return st;
   if (seq_len < 0 || (seq_len > 0 && T % seq_len) || (T > 0 && (!dq || !dk || !dv || !dqkv))) return LOOM_ERR_INVALID_ARG;
   if (!dq_weight || !dk_weight) return LOOM_ERR_INVALID_ARG;
+  if (!tables_reach(positions, T, seq_len, table_rows)) return LOOM_ERR_INVALID_ARG;
   if (dqkv_stride < (static_cast<int64_t>(Hq) + 2ll * Hkv) * D) return LOOM_ERR_INVALID_ARG;
   if (Hq + 2ll * Hkv > kMaxBwdHeads) return LOOM_ERR_UNSUPPORTED;
   if (dqkv_stride % 8 || !aligned16(dq) || !aligned16(dk) || !aligned16(dv) || !aligned16(dqkv) || !aligned4(dq_weight) ||
