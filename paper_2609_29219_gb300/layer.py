@@ -23,20 +23,25 @@ def rope_tables(positions, rotary_dim, base=10000.0, device="cuda"):
 
 
 class PagedCache:
-    """K and V pages [num_pages, page, Hkv, D] and the pages of each sequence, given out in order."""
+    """K and V pages [num_pages, page, Hkv, D] and the pages of each sequence, given out in order.
+    Every sequence has `used` tokens (on the host; `lens` on the device) of `capacity`, whole pages."""
 
     def __init__(self, sequences, capacity, Hkv, D, page=16, device="cuda"):
         per = -(-capacity // page)
         self.page, self.device = page, device
+        self.capacity, self.used = per * page, 0
         self.k, self.v = (torch.zeros((sequences * per, page, Hkv, D), dtype=torch.bfloat16, device=device) for _ in range(2))
         self.table = torch.randperm(sequences * per, device=device).to(torch.int32).view(sequences, per)
         self.lens = torch.zeros(sequences, dtype=torch.int32, device=device)
 
     def take(self, count):
         """Positions and slots of each sequence's next `count` tokens, token-major by sequence."""
+        if not 0 <= count <= self.capacity - self.used:
+            raise ValueError(f"the cache has room for {self.capacity - self.used} more tokens a sequence, not {count}")
         pos = self.lens[:, None] + torch.arange(count, dtype=torch.int32, device=self.device)
         slots = self.table.gather(1, (pos // self.page).long()) * self.page + pos % self.page
         self.lens += count
+        self.used += count
         return pos.reshape(-1), slots.reshape(-1)
 
 
