@@ -70,6 +70,8 @@ class AttentionLayer:
     @torch.no_grad()
     def step(self, x, cache):
         """One token of each sequence, x [B, model]: its k and v go into the cache, its query reads it."""
+        if cache.used >= self.cos.shape[0]:
+            raise ValueError(f"the rotation tables have no position {cache.used}")
         pos, slots = cache.take(1)
         qkv = loom.loom_gemm_bf16(x, self.w_qkv, b_transposed=True)
         q = loom.loom_qkv_norm_rope_cache(qkv, self.q_norm, self.k_norm, self.cos, self.sin, pos, slots, cache.k, cache.v, self.Hq)

@@ -18,3 +18,12 @@ def test_a_full_cache_is_refused():
         cache.take(1)
     with pytest.raises(ValueError):
         cache.take(-1)
+
+
+def test_a_step_past_the_rotation_tables_is_refused():
+    layer = layer_mod.AttentionLayer(model=64, Hq=2, Hkv=1, D=64, positions=5, device="cpu")
+    cache = layer_mod.PagedCache(2, 16, 1, 64, device="cpu")
+    cache.take(5)
+    with pytest.raises(ValueError, match="position 5"):
+        layer.step(torch.zeros((2, 64), dtype=torch.bfloat16), cache)
+    assert cache.used == 5 and cache.lens.tolist() == [5, 5]
