@@ -199,10 +199,14 @@ _bf16 = _f32 = _i32 = _u8 = None  # torch's types
 
 _empty_strided_cuda = None
 _fast = None  # the compiled binding, where it can be used
+_current_device = None  # torch's: the index of the current device
+# Whether there is more than one: with one GPU every CUDA tensor is on it, and devices are not
+# compared (GB300 host: 0.1 us a tensor).
+_several = False
 
 
 def _torch():
-    global _torch_mod, _empty_strided_cuda, _bf16, _f32, _i32, _u8, _fast
+    global _torch_mod, _empty_strided_cuda, _bf16, _f32, _i32, _u8, _fast, _current_device, _several
     if _torch_mod is None:
         import torch
         try:  # what torch's generated code allocates by: no dispatch, on the current device
@@ -213,6 +217,8 @@ def _torch():
         except ImportError:
             pass
         _bf16, _f32, _i32, _u8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
+        _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        _several = torch.cuda.device_count() > 1
         _torch_mod = torch
         _fast = _compiled_binding(torch)
     return _torch_mod
@@ -279,11 +285,11 @@ def _new_on(stream, shape, dtype, t, like=False):
 
 
 def _direct(t):
-    """Whether new tensors on tensor t's device may pass the dispatcher by (see _new)."""
+    """Whether new tensors on tensor t's device may pass the dispatcher by (see _new).  t is a call's first
+    tensor, which is on the current device."""
     c = _torch_mod._C
     return (_empty_strided_cuda is not None and type(t) is _torch_mod.Tensor and not c._len_torch_dispatch_stack()
-            and not c._len_torch_function_stack() and not c._get_deterministic_algorithms()
-            and t.get_device() == c._cuda_getDevice())
+            and not c._len_torch_function_stack() and not c._get_deterministic_algorithms())
 
 
 def _maker(t, stream):
@@ -303,15 +309,30 @@ def _workspace(need, t, stream):
     return _torch_mod.empty(max(need, 16), dtype=_u8, device=t.device)
 
 
-def _ptr(t, name, dtype, ndim):
+def _on_current(t, name):
+    """The device index of a call's first tensor: where the kernels run, so it must be the current one."""
+    d = t.get_device()
+    if d != _current_device():
+        raise ValueError(f"{name} is on cuda:{d}, which is not the current device")
+    return d
+
+
+def _together(first, *others):
+    """Whether a call's tensors (those that there are) are on the first's device."""
+    d = first.get_device()
+    return all(t is None or t.get_device() == d for t in others)
+
+
+def _ptr(t, name, dtype, ndim, dev=None):
     """_dev_ptr of a tensor that passes its checks, in one expression (it names what fails)."""
     if (isinstance(t, _torch_mod.Tensor) and t.is_cuda and t.dtype is dtype and t.dim() == ndim
-            and t.is_contiguous()):
+            and t.is_contiguous() and (dev is None or t.get_device() == dev)):
         return t.data_ptr()
-    return _dev_ptr(t, name, dtype, ndim)
+    return _dev_ptr(t, name, dtype, ndim, dev)
 
 
-def _dev_ptr(t, name, dtype=None, ndim=None):
+def _dev_ptr(t, name, dtype=None, ndim=None, dev=None):
+    """Pointer of a contiguous CUDA tensor (dev: on that device), or what it is not."""
     torch = _torch()
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
@@ -323,6 +344,8 @@ def _dev_ptr(t, name, dtype=None, ndim=None):
         raise ValueError(f"{name} must have {ndim} dims, got shape {tuple(t.shape)}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
+    if dev is not None and t.get_device() != dev:
+        raise ValueError(f"{name} is on cuda:{t.get_device()}, the call's first tensor on cuda:{dev}")
     return t.data_ptr()
 
 
@@ -360,8 +383,9 @@ def loom_attn_fwd(q, k, v, o=None, lse=None, *, causal=False, scale=None, stream
     torch = _torch()
     bf16 = torch.bfloat16
     qp = _ptr(q, "q", bf16, 4)
-    kp = _ptr(k, "k", bf16, 4)
-    vp_ = _ptr(v, "v", bf16, 4)
+    dev = _on_current(q, "q") if _several else None
+    kp = _ptr(k, "k", bf16, 4, dev)
+    vp_ = _ptr(v, "v", bf16, 4, dev)
     B, Hq, Sq, D = q.shape
     Bk, Hkv, Skv, Dk = k.shape
     if v.shape != k.shape or Bk != B or Dk != D:
@@ -370,14 +394,14 @@ def loom_attn_fwd(q, k, v, o=None, lse=None, *, causal=False, scale=None, stream
         o = _new((B, Hq, Sq, D), (Hq * Sq * D, Sq * D, D, 1), bf16, q, True, stream)
     if o.shape != q.shape:
         raise ValueError("o must have q's shape")
-    op = _ptr(o, "o", bf16, 4)
+    op = _ptr(o, "o", bf16, 4, dev)
     if lse is None and return_lse:
         lse = _new((B, Hq, Sq), (Hq * Sq, Sq, 1), torch.float32, q, stream=stream)
     lp = None
     if lse is not None:
         if tuple(lse.shape) != (B, Hq, Sq):
             raise ValueError("lse must be [B, Hq, Sq]")
-        lp = _dev_ptr(lse, "lse", torch.float32)
+        lp = _dev_ptr(lse, "lse", torch.float32, None, dev)
     if scale is None:
         scale = D ** -0.5
     st = (_lib or capi()).loom_attn_fwd(qp, kp, vp_, op, lp, B, Hq, Hkv, Sq, Skv, D, int(bool(causal)), float(scale),
@@ -395,12 +419,13 @@ def loom_attn_decode_workspace_bytes(B, Hq, Hkv, Skv, D, num_splits=0) -> int:
 
 
 def _decode_operands(q, k_cache, v_cache, seqlens_k, o, lse, return_lse, stream):
-    """Pointers and sizes of the contiguous decode entry points' tensor arguments."""
+    """Pointers and sizes of the contiguous decode entry points' tensor arguments, outputs, and the device."""
     torch = _torch()
     bf16 = torch.bfloat16
     qp = _ptr(q, "q", bf16, 4)
-    kp = _ptr(k_cache, "k_cache", bf16, 4)
-    vp_ = _ptr(v_cache, "v_cache", bf16, 4)
+    dev = _on_current(q, "q") if _several else None
+    kp = _ptr(k_cache, "k_cache", bf16, 4, dev)
+    vp_ = _ptr(v_cache, "v_cache", bf16, 4, dev)
     B, Hq, Sq, D = q.shape
     Bk, Hkv, Skv, Dk = k_cache.shape
     if Sq != 1 or v_cache.shape != k_cache.shape or Bk != B or Dk != D:
@@ -409,18 +434,18 @@ def _decode_operands(q, k_cache, v_cache, seqlens_k, o, lse, return_lse, stream)
     if seqlens_k is not None:
         if tuple(seqlens_k.shape) != (B,):
             raise ValueError("seqlens_k must be [B]")
-        sp = _ptr(seqlens_k, "seqlens_k", torch.int32, 1)
+        sp = _ptr(seqlens_k, "seqlens_k", torch.int32, 1, dev)
     if o is None:
         o = _new((B, Hq, 1, D), (Hq * D, D, D, 1), bf16, q, True, stream)
-    op = _ptr(o, "o", bf16, 4)
+    op = _ptr(o, "o", bf16, 4, dev)
     if lse is None and return_lse:
         lse = _new((B, Hq), (Hq, 1), torch.float32, q, stream=stream)
     lp = None
     if lse is not None:
         if lse.numel() != B * Hq:
             raise ValueError("lse must hold B*Hq values")
-        lp = _dev_ptr(lse, "lse", torch.float32)
-    return (qp, kp, vp_, sp, op, lp), (B, Hq, Hkv, Skv, D), o, lse
+        lp = _dev_ptr(lse, "lse", torch.float32, None, dev)
+    return (qp, kp, vp_, sp, op, lp), (B, Hq, Hkv, Skv, D), o, lse, dev
 
 
 def loom_attn_decode(q, k_cache, v_cache, seqlens_k=None, o=None, lse=None, workspace=None, *,
@@ -431,12 +456,12 @@ def loom_attn_decode(q, k_cache, v_cache, seqlens_k=None, o=None, lse=None, work
     bytes (allocated here if None).  Returns ``o`` or ``(o, lse)``.
     """
     torch = _torch()
-    (qp, kp, vp_, sp, op, lp), (B, Hq, Hkv, Skv, D), o, lse = _decode_operands(
+    (qp, kp, vp_, sp, op, lp), (B, Hq, Hkv, Skv, D), o, lse, dev = _decode_operands(
         q, k_cache, v_cache, seqlens_k, o, lse, return_lse, stream)
     if workspace is None:
         need = loom_attn_decode_workspace_bytes(B, Hq, Hkv, Skv, D, num_splits)
         workspace = _workspace(need, q, stream)
-    wp = _dev_ptr(workspace, "workspace")
+    wp = _dev_ptr(workspace, "workspace", None, None, dev)
     if scale is None:
         scale = D ** -0.5
     st = (_lib or capi()).loom_attn_decode(qp, kp, vp_, sp, op, lp, wp, workspace.numel() * workspace.element_size(),
@@ -450,7 +475,7 @@ def loom_attn_decode_noalloc(q, k_cache, v_cache, seqlens_k=None, o=None, lse=No
     """Flash Decode with the partials in the library's built-in scratch array (no
     workspace argument, no device allocation by the library).  Arguments and results as
     ``loom_attn_decode``; problems whose partials exceed the array raise LOOM_ERR_WORKSPACE."""
-    (qp, kp, vp_, sp, op, lp), (B, Hq, Hkv, Skv, D), o, lse = _decode_operands(
+    (qp, kp, vp_, sp, op, lp), (B, Hq, Hkv, Skv, D), o, lse, _ = _decode_operands(
         q, k_cache, v_cache, seqlens_k, o, lse, return_lse, stream)
     if scale is None:
         scale = D ** -0.5
@@ -468,27 +493,28 @@ def loom_attn_fwd_varlen(q, k, v, cu_seqlens_q, cu_seqlens_k, max_seqlen_q, o=No
     torch = _torch()
     bf16 = torch.bfloat16
     qp = _ptr(q, "q", bf16, 3)
-    kp = _ptr(k, "k", bf16, 3)
-    vp_ = _ptr(v, "v", bf16, 3)
+    dev = _on_current(q, "q") if _several else None
+    kp = _ptr(k, "k", bf16, 3, dev)
+    vp_ = _ptr(v, "v", bf16, 3, dev)
     total_q, Hq, D = q.shape
     total_k, Hkv, Dk = k.shape
     if v.shape != k.shape or Dk != D:
         raise ValueError("varlen prefill takes q [total_q, Hq, D] and k/v [total_k, Hkv, D]")
-    cqp = _ptr(cu_seqlens_q, "cu_seqlens_q", torch.int32, 1)
-    ckp = _ptr(cu_seqlens_k, "cu_seqlens_k", torch.int32, 1)
+    cqp = _ptr(cu_seqlens_q, "cu_seqlens_q", torch.int32, 1, dev)
+    ckp = _ptr(cu_seqlens_k, "cu_seqlens_k", torch.int32, 1, dev)
     if cu_seqlens_q.numel() != cu_seqlens_k.numel() or cu_seqlens_q.numel() < 2:
         raise ValueError("cu_seqlens_q and cu_seqlens_k must both be [B + 1]")
     B = cu_seqlens_q.numel() - 1
     if o is None:
         o = _new((total_q, Hq, D), (Hq * D, D, 1), bf16, q, True, stream)
-    op = _ptr(o, "o", bf16, 3)
+    op = _ptr(o, "o", bf16, 3, dev)
     if lse is None and return_lse:
         lse = _new((Hq, total_q), (total_q, 1), torch.float32, q, stream=stream)
     lp = None
     if lse is not None:
         if lse.numel() != Hq * total_q:
             raise ValueError("lse must hold Hq*total_q values")
-        lp = _dev_ptr(lse, "lse", torch.float32)
+        lp = _dev_ptr(lse, "lse", torch.float32, None, dev)
     if scale is None:
         scale = D ** -0.5
     st = (_lib or capi()).loom_attn_fwd_varlen(qp, kp, vp_, op, lp, cqp, ckp, B, Hq, Hkv, total_q, total_k,
@@ -507,8 +533,9 @@ def loom_attn_decode_paged(q, k_cache, v_cache, block_table, seqlens_k, o=None, 
     torch = _torch()
     bf16 = torch.bfloat16
     qp = _ptr(q, "q", bf16, 4)
-    kp = _ptr(k_cache, "k_cache", bf16, 4)
-    vp_ = _ptr(v_cache, "v_cache", bf16, 4)
+    dev = _on_current(q, "q") if _several else None
+    kp = _ptr(k_cache, "k_cache", bf16, 4, dev)
+    vp_ = _ptr(v_cache, "v_cache", bf16, 4, dev)
     B, Hq, Sq, D = q.shape
     if layout not in ("nhd", "hnd"):
         raise ValueError("layout is 'nhd' or 'hnd'")
@@ -521,25 +548,25 @@ def loom_attn_decode_paged(q, k_cache, v_cache, block_table, seqlens_k, o=None, 
     if block_table.dim() != 2 or block_table.shape[0] != B:
         raise ValueError("block_table must be [B, max_pages]")
     max_pages = block_table.shape[1]
-    tp = _ptr(block_table, "block_table", torch.int32, 2)
+    tp = _ptr(block_table, "block_table", torch.int32, 2, dev)
     if tuple(seqlens_k.shape) != (B,):
         raise ValueError("seqlens_k must be [B]")
-    sp = _ptr(seqlens_k, "seqlens_k", torch.int32, 1)
+    sp = _ptr(seqlens_k, "seqlens_k", torch.int32, 1, dev)
     if o is None:
         o = _new((B, Hq, 1, D), (Hq * D, D, D, 1), bf16, q, True, stream)
-    op = _ptr(o, "o", bf16, 4)
+    op = _ptr(o, "o", bf16, 4, dev)
     if lse is None and return_lse:
         lse = _new((B, Hq), (Hq, 1), torch.float32, q, stream=stream)
     lp = None
     if lse is not None:
         if lse.numel() != B * Hq:
             raise ValueError("lse must hold B*Hq values")
-        lp = _dev_ptr(lse, "lse", torch.float32)
+        lp = _dev_ptr(lse, "lse", torch.float32, None, dev)
     Skv = max_pages * page_size
     if workspace is None:
         need = loom_attn_decode_workspace_bytes(B, Hq, Hkv, Skv, D, num_splits)
         workspace = _workspace(need, q, stream)
-    wp = _dev_ptr(workspace, "workspace")
+    wp = _dev_ptr(workspace, "workspace", None, None, dev)
     if scale is None:
         scale = D ** -0.5
     st = (_lib or capi()).loom_attn_decode_paged(
@@ -568,8 +595,10 @@ def _norm_bwd_need(D):
 # 8 (3).
 def _bwd_checked(do, q, k, v, o, lse, dlse, dq, dk, dv, ndim):
     """The backward entry points' tensors, named if they are not what they should be."""
-    for t, name in ((q, "q"), (k, "k"), (v, "v"), (do, "do"), (o, "o")):
-        _dev_ptr(t, name, _bf16, ndim)
+    _dev_ptr(q, "q", _bf16, ndim)
+    dev = q.get_device()
+    for t, name in ((k, "k"), (v, "v"), (do, "do"), (o, "o")):
+        _dev_ptr(t, name, _bf16, ndim, dev)
     if v.shape != k.shape or k.shape[-1] != q.shape[-1] or (ndim == 4 and k.shape[0] != q.shape[0]):
         raise ValueError("q/k/v shapes disagree")
     for t, name in ((do, "do"), (o, "o")):
@@ -577,14 +606,14 @@ def _bwd_checked(do, q, k, v, o, lse, dlse, dq, dk, dv, ndim):
             raise ValueError(f"{name} must have q's shape")
     if lse is None:
         raise TypeError("lse is needed: call the forward pass with return_lse=True")
-    _dev_ptr(lse, "lse", _f32)
+    _dev_ptr(lse, "lse", _f32, None, dev)
     if dlse is not None:
-        _dev_ptr(dlse, "dlse", _f32)
+        _dev_ptr(dlse, "dlse", _f32, None, dev)
         if dlse.shape != lse.shape:
             raise ValueError("dlse must have lse's shape")
     for t, like, name in ((dq, q, "dq"), (dk, k, "dk"), (dv, v, "dv")):
         if t is not None:
-            _dev_ptr(t, name, _bf16, ndim)
+            _dev_ptr(t, name, _bf16, ndim, dev)
             if t.shape != like.shape:
                 raise ValueError(f"{name} must have {name[1]}'s shape")
 
@@ -595,7 +624,8 @@ def _bwd_fine(do, q, k, v, o, lse, dlse, qs, ks):
                 and o.is_cuda and o.dtype is _bf16 and o.is_contiguous() and k.is_cuda and k.dtype is _bf16
                 and k.is_contiguous() and v.is_cuda and v.dtype is _bf16 and v.is_contiguous() and lse.is_cuda
                 and lse.dtype is _f32 and lse.is_contiguous() and do.shape == qs and o.shape == qs and v.shape == ks
-                and (dlse is None or (dlse.is_cuda and dlse.dtype is _f32 and dlse.is_contiguous() and dlse.shape == lse.shape)))
+                and (dlse is None or (dlse.is_cuda and dlse.dtype is _f32 and dlse.is_contiguous() and dlse.shape == lse.shape))
+                and (not _several or _together(q, do, k, v, o, lse, dlse)))
     except AttributeError:
         return False
 
@@ -631,6 +661,7 @@ def loom_attn_bwd(do, q, k, v, o, lse, dq=None, dk=None, dv=None, workspace=None
         _bwd_checked(do, q, k, v, o, lse, dlse, dq, dk, dv, 4)
     if tuple(lse.shape) != (B, Hq, Sq):
         raise ValueError("lse must be [B, Hq, Sq]")
+    dev = _on_current(q, "q") if _several else None
     new = _maker(q, stream)
     if dq is None:
         dq = new(tuple(qs), (Hq * Sq * D, Sq * D, D, 1), _bf16)
@@ -643,7 +674,7 @@ def loom_attn_bwd(do, q, k, v, o, lse, dq=None, dk=None, dv=None, workspace=None
         workspace = new((max(wbytes, 16),), (1,), _u8)
         wp = workspace.data_ptr()
     else:
-        wp = _dev_ptr(workspace, "workspace")
+        wp = _dev_ptr(workspace, "workspace", None, None, dev)
         wbytes = workspace.numel() * workspace.element_size()
     st = (_lib or capi()).loom_attn_bwd(
         do.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
@@ -675,7 +706,8 @@ def loom_attn_bwd_varlen(do, q, k, v, o, lse, cu_seqlens_q, cu_seqlens_k, max_se
         _bwd_checked(do, q, k, v, o, lse, dlse, dq, dk, dv, 3)
     if lse.numel() != Hq * total_q:
         raise ValueError("lse must hold Hq*total_q values")
-    cqp, ckp = _ptr(cu_seqlens_q, "cu_seqlens_q", _i32, 1), _ptr(cu_seqlens_k, "cu_seqlens_k", _i32, 1)
+    dev = _on_current(q, "q") if _several else None
+    cqp, ckp = _ptr(cu_seqlens_q, "cu_seqlens_q", _i32, 1, dev), _ptr(cu_seqlens_k, "cu_seqlens_k", _i32, 1, dev)
     B = cu_seqlens_q.shape[0] - 1
     if cu_seqlens_k.shape[0] != B + 1 or B < 1:
         raise ValueError("cu_seqlens_q and cu_seqlens_k must both be [B + 1]")
@@ -691,7 +723,7 @@ def loom_attn_bwd_varlen(do, q, k, v, o, lse, cu_seqlens_q, cu_seqlens_k, max_se
         workspace = new((max(wbytes, 16),), (1,), _u8)
         wp = workspace.data_ptr()
     else:
-        wp = _dev_ptr(workspace, "workspace")
+        wp = _dev_ptr(workspace, "workspace", None, None, dev)
         wbytes = workspace.numel() * workspace.element_size()
     st = (_lib or capi()).loom_attn_bwd_varlen(
         do.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
@@ -703,8 +735,8 @@ def loom_attn_bwd_varlen(do, q, k, v, o, lse, cu_seqlens_q, cu_seqlens_k, max_se
     return dq, dk, dv
 
 
-def _row_matrix(t, name, width):
-    """Pointer and row distance of a bf16 CUDA matrix whose rows are contiguous."""
+def _row_matrix(t, name, width, dev=None):
+    """Pointer and row distance of a bf16 CUDA matrix whose rows are contiguous (dev: on that device)."""
     if not isinstance(t, _torch_mod.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if not t.is_cuda:
@@ -713,32 +745,35 @@ def _row_matrix(t, name, width):
         raise TypeError(f"{name} must be {_bf16}, got {t.dtype}")
     if t.dim() != 2 or t.shape[1] != width or (t.shape[1] > 1 and t.stride(1) != 1):
         raise ValueError(f"{name} must be [T, {width}] with contiguous rows, got shape {tuple(t.shape)}")
+    if dev is not None and t.get_device() != dev:
+        raise ValueError(f"{name} is on cuda:{t.get_device()}, the call's first tensor on cuda:{dev}")
     return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else width
 
 
 def _norm_checked(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, positions):
     """The norm-and-rotation entry points' shared tensors, named if they are not what they should be."""
+    dev = qkv.get_device() if isinstance(qkv, _torch_mod.Tensor) and qkv.is_cuda else None
     for t, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-        _dev_ptr(t, name, None, 1)
+        _dev_ptr(t, name, None, 1, dev)
         if t.dtype not in (_bf16, _f32):
             raise TypeError(f"{name} must be {_bf16} or {_f32}, got {t.dtype}")
     if k_weight.dtype is not q_weight.dtype:
         raise TypeError("q_weight and k_weight must have one type")
     if k_weight.shape != q_weight.shape:
         raise ValueError("q_weight and k_weight must both be [D]")
-    _dev_ptr(cos, "cos", _f32, 2), _dev_ptr(sin, "sin", _f32, 2)
+    _dev_ptr(cos, "cos", _f32, 2, dev), _dev_ptr(sin, "sin", _f32, 2, dev)
     if cos.shape != sin.shape:
         raise ValueError("cos and sin must both be [positions, rotary_dim / 2]")
     _row_matrix(qkv, "qkv", (num_heads + 2 * num_kv_heads) * q_weight.shape[0])
     if positions is not None:
-        _dev_ptr(positions, "positions", _i32, 1)
+        _dev_ptr(positions, "positions", _i32, 1, dev)
         if positions.shape[0] != qkv.shape[0]:
             raise ValueError("positions must be [T]")
 
 
 def _norm_operands(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, positions, interleaved):
-    """What the norm-and-rotation entry points share: (T, D, qkv's row distance, and the C arguments
-    from q_weight to positions)."""
+    """What the norm-and-rotation entry points share: (T, D, the device's index, qkv's row distance, and
+    the C arguments from q_weight to positions)."""
     _torch()
     try:
         T, W = qkv.shape
@@ -752,12 +787,13 @@ def _norm_operands(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, p
                 and k_weight.dim() == 1 and cos.is_cuda and cos.dtype is _f32 and cos.is_contiguous() and sin.is_cuda
                 and sin.dtype is _f32 and sin.is_contiguous() and sin.shape == cos.shape
                 and (positions is None or (positions.is_cuda and positions.dtype is _i32 and positions.is_contiguous()
-                                           and positions.dim() == 1 and positions.shape[0] == T)))
+                                           and positions.dim() == 1 and positions.shape[0] == T))
+                and (not _several or _together(qkv, q_weight, k_weight, cos, sin, positions)))
     except (AttributeError, ValueError):
         fine = False
     if not fine:
         _norm_checked(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, positions)
-    return T, D, stride if T > 1 else W, (
+    return T, D, _on_current(qkv, "qkv") if _several else None, stride if T > 1 else W, (
         q_weight.data_ptr(), k_weight.data_ptr(), 1 if wt is _f32 else 0, cos.data_ptr(), sin.data_ptr(), P, 2 * half,
         1 if interleaved else 0, None if positions is None else positions.data_ptr())
 
@@ -781,7 +817,7 @@ def loom_qkv_norm_rope(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_head
         r = _fast.norm_rope(qkv, q_weight, k_weight, cos, sin, positions, interleaved, eps, num_heads, num_kv_heads, seq_len)
         if r is not None:
             return _fast_result(r, "loom_qkv_norm_rope")
-    T, D, row, norm = _norm_operands(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, positions, interleaved)
+    T, D, dev, row, norm = _norm_operands(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, positions, interleaved)
     S = seq_len
     if S < 0 or (S and T % S):
         raise ValueError("T must be a multiple of seq_len")
@@ -792,7 +828,7 @@ def loom_qkv_norm_rope(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_head
     else:
         qs, ks, qst, kst = (T, num_heads, D), (T, num_kv_heads, D), (num_heads * D, D, 1), (num_kv_heads * D, D, 1)
     for t, name, shape in ((q, "q", qs), (k, "k", ks), (v, "v", ks)) if q is not None or k is not None or v is not None else ():
-        if t is not None and (_dev_ptr(t, name, _bf16) is None or tuple(t.shape) != shape):
+        if t is not None and (_dev_ptr(t, name, _bf16, None, dev) is None or tuple(t.shape) != shape):
             raise ValueError(f"{name} must be {list(shape)}")
     new = _maker(qkv, stream)
     if q is None:
@@ -845,12 +881,15 @@ def loom_qkv_norm_rope_cache(qkv, q_weight, k_weight, cos, sin, positions, slots
     if not fine:
         _cache_checked(k_cache, v_cache, positions, slots)
     page_size, Hkv = (a, b) if layout == "nhd" else (b, a)
-    T, D, row, norm = _norm_operands(qkv, q_weight, k_weight, cos, sin, num_heads, Hkv, positions, interleaved)
+    T, D, dev, row, norm = _norm_operands(qkv, q_weight, k_weight, cos, sin, num_heads, Hkv, positions, interleaved)
+    if _several and not _together(qkv, k_cache, v_cache, slots):
+        for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache"), (slots, "slots")):
+            _dev_ptr(t, name, dev=dev)
     if Dk != D or slots.shape[0] != T:
         raise ValueError("the caches must have the weights' D, and slots be [T]")
     if q is None:
         q = _new((T, num_heads, D), (num_heads * D, D, 1), _bf16, qkv, stream=stream)
-    elif _dev_ptr(q, "q", _bf16, 3) is None or tuple(q.shape) != (T, num_heads, D):
+    elif _dev_ptr(q, "q", _bf16, 3, dev) is None or tuple(q.shape) != (T, num_heads, D):
         raise ValueError(f"q must be {[T, num_heads, D]}")
     st = (_lib or capi()).loom_qkv_norm_rope_cache(
         qkv.data_ptr(), row, *norm, slots.data_ptr(), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), pages, page_size,
@@ -885,34 +924,37 @@ def loom_qkv_norm_rope_bwd(dq, dk, dv, qkv, q_weight, k_weight, cos, sin, positi
     if not fine:
         for t, n in ((dq, "dq"), (dk, "dk"), (dv, "dv")):
             _dev_ptr(t, n, _bf16, 3 if dq.dim() != 4 else 4)
-    T, D, row, norm = _norm_operands(qkv, q_weight, k_weight, cos, sin, Hq, Hkv, positions, interleaved)
+    T, D, dev, row, norm = _norm_operands(qkv, q_weight, k_weight, cos, sin, Hq, Hkv, positions, interleaved)
     S = qs[2] if ndim == 4 else 0
     if (not fine or tuple(qs) != ((qs[0], Hq, S, D) if ndim == 4 else (T, Hq, D)) or (qs[0] * S if ndim == 4 else T) != T
             or tuple(ks) != (qs[0], Hkv, *qs[2:])):
         raise ValueError("dq, dk and dv must be laid out as q, k and v of the forward call")
     _check_tables(T, S, cos, positions)
+    if _several and not _together(qkv, dq, dk, dv):
+        for t, name in ((dq, "dq"), (dk, "dk"), (dv, "dv")):
+            _dev_ptr(t, name, dev=dev)
     width = (Hq + 2 * Hkv) * D
     new = _maker(qkv, stream)
     if dqkv is None:
         dqkv, drow = new((T, width), (width, 1), _bf16), width
     else:
-        drow = _row_matrix(dqkv, "dqkv", width)[1]
+        drow = _row_matrix(dqkv, "dqkv", width, dev)[1]
         if dqkv.shape[0] != T:
             raise ValueError(f"dqkv must be {[T, width]}")
     if dq_weight is None:
         dq_weight = new((D,), (1,), _f32)
-    elif _dev_ptr(dq_weight, "dq_weight", _f32) is None or tuple(dq_weight.shape) != (D,):
+    elif _dev_ptr(dq_weight, "dq_weight", _f32, None, dev) is None or tuple(dq_weight.shape) != (D,):
         raise ValueError("dq_weight must be [D]")
     if dk_weight is None:
         dk_weight = new((D,), (1,), _f32)
-    elif _dev_ptr(dk_weight, "dk_weight", _f32) is None or tuple(dk_weight.shape) != (D,):
+    elif _dev_ptr(dk_weight, "dk_weight", _f32, None, dev) is None or tuple(dk_weight.shape) != (D,):
         raise ValueError("dk_weight must be [D]")
     if workspace is None:
         wbytes = _norm_bwd_need(D)
         workspace = new((max(wbytes, 16),), (1,), _u8)
         wp = workspace.data_ptr()
     else:
-        wp = _dev_ptr(workspace, "workspace")
+        wp = _dev_ptr(workspace, "workspace", None, None, dev)
         wbytes = workspace.numel() * workspace.element_size()
     st = (_lib or capi()).loom_qkv_norm_rope_bwd(
         dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), qkv.data_ptr(), row, *norm, dqkv.data_ptr(), drow, dq_weight.data_ptr(),
@@ -971,7 +1013,8 @@ def loom_gemm_bf16(a, b, c=None, *, stream=None, b_transposed=False):
     torch = _torch()
     bf16 = torch.bfloat16
     ap = _ptr(a, "a", bf16, 2)
-    bp = _ptr(b, "b", bf16, 2)
+    dev = _on_current(a, "a") if _several else None
+    bp = _ptr(b, "b", bf16, 2, dev)
     M, K = a.shape
     if b_transposed:
         N, K2 = b.shape
@@ -981,7 +1024,7 @@ def loom_gemm_bf16(a, b, c=None, *, stream=None, b_transposed=False):
         raise ValueError(f"a is [M, {K}] but b has {K2} along K")
     if c is None:
         c = _new((M, N), (N, 1), bf16, a, stream=stream)
-    cp = _ptr(c, "c", bf16, 2)
+    cp = _ptr(c, "c", bf16, 2, dev)
     if tuple(c.shape) != (M, N):
         raise ValueError("c must be [M, N]")
     lib = _lib or capi()

@@ -21,6 +21,8 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/version.h>
 
+#include <initializer_list>
+
 #include "../../include/loom_attn.h"
 
 namespace {
@@ -84,6 +86,13 @@ bool same(const Tensor& a, const Tensor& b) {
 bool small(const Tensor& a) {
   for (int i = 0; i < a.dims; ++i)
     if (a.size[i] < 0 || a.size[i] > 0x7fffffffLL) return false;
+  return true;
+}
+
+// The others (those that there are) are on the first's device.
+bool together(const Tensor& first, std::initializer_list<const Tensor*> others) {
+  for (const Tensor* t : others)
+    if (t->t && t->t->get_device() != first.t->get_device()) return false;
   return true;
 }
 
@@ -165,7 +174,7 @@ PyObject* bwd(PyObject* const* a, bool varlen) {
     B = cq.size[0] - 1;
   }
   const long long dev = device_of(q);
-  if (dev < 0) Py_RETURN_NONE;
+  if (dev < 0 || !together(q, {&d, &k, &v, &o, &lse, &dlse, &cq, &ck})) Py_RETURN_NONE;
   const int iB = static_cast<int>(B), iHq = static_cast<int>(Hq), iHkv = static_cast<int>(Hkv), iSq = static_cast<int>(Sq),
             iSkv = static_cast<int>(Skv), iD = static_cast<int>(D);
   const size_t need = varlen ? F.attn_bwd_varlen_bytes(iB, iHq, iHkv, iSq, iSkv, iD) : F.attn_bwd_bytes(iB, iHq, iHkv, iSq, iSkv, iD);
@@ -220,6 +229,7 @@ bool norm_args(PyObject* const* a, long long heads, Norm* m) {
   m->row = m->T > 1 ? m->x.t->stride(0) : m->x.size[1];
   if (m->x.t->stride(1) != 1) return false;
   if (a[5] != Py_None && (!view(a[5], kI32, &m->pos) || m->pos.dims != 1 || m->pos.size[0] != m->T)) return false;
+  if (!together(m->x, {&m->qw, &m->kw, &m->cos, &m->sin, &m->pos})) return false;
   m->type = f32 ? LOOM_FP32 : LOOM_BF16;
   m->P = static_cast<int>(m->cos.size[0]);
   m->R = m->cos.size[1] > 1024 ? 0 : static_cast<int>(2 * m->cos.size[1]);
@@ -265,7 +275,7 @@ PyObject* norm_rope_cache(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const int hnd = PyObject_IsTrue(a[12]) > 0;
   const long long Hkv = kc.size[hnd ? 1 : 2], page = kc.size[hnd ? 2 : 1];
   if (!norm_args(a, Hq + 2 * Hkv, &m) || kc.size[3] != m.D || !view(a[9], kI32, &slots) || slots.dims != 1 ||
-      slots.size[0] != m.T)
+      slots.size[0] != m.T || !together(m.x, {&slots, &kc, &vc}))
     Py_RETURN_NONE;
   const long long dev = device_of(m.x);
   if (dev < 0) Py_RETURN_NONE;
@@ -292,7 +302,7 @@ PyObject* norm_rope_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const long long Hq = dq.size[1], Hkv = dk.size[1], S = dq.dims == 4 ? dq.size[2] : 0;
   if (!norm_args(a, Hq + 2 * Hkv, &m) || dq.size[0] != dk.size[0] || dq.size[2] != dk.size[2] || dq.size[dq.dims - 1] != m.D ||
       dk.size[dk.dims - 1] != m.D || (S ? dq.size[0] * S : dq.size[0]) != m.T || (dq.dims == 4 && S == 0) ||
-      !m.tables_reach(S))
+      !m.tables_reach(S) || !together(m.x, {&dq, &dk, &dv}))
     Py_RETURN_NONE;
   const long long dev = device_of(m.x);
   if (dev < 0) Py_RETURN_NONE;
