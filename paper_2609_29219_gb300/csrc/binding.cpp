@@ -233,7 +233,11 @@ bool norm_args(PyObject* const* a, long long heads, Norm* m) {
   m->type = f32 ? LOOM_FP32 : LOOM_BF16;
   m->P = static_cast<int>(m->cos.size[0]);
   m->R = m->cos.size[1] > 1024 ? 0 : static_cast<int>(2 * m->cos.size[1]);
-  m->interleaved = PyObject_IsTrue(a[6]) > 0;
+  m->interleaved = PyObject_IsTrue(a[6]);
+  if (m->interleaved < 0) {  // (the Python code meets it again)
+    PyErr_Clear();
+    return false;
+  }
   return as_float(a[7], &m->eps);
 }
 
@@ -272,7 +276,7 @@ PyObject* norm_rope_cache(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (n != 13 || !as_int(a[8], &Hq) || Hq <= 0 || !view(a[10], kBf16, &kc) || kc.dims != 4 || !small(kc) ||
       !view(a[11], kBf16, &vc) || !same(kc, vc) || a[5] == Py_None)
     Py_RETURN_NONE;
-  const int hnd = PyObject_IsTrue(a[12]) > 0;
+  const int hnd = a[12] == Py_True;
   const long long Hkv = kc.size[hnd ? 1 : 2], page = kc.size[hnd ? 2 : 1];
   if (!norm_args(a, Hq + 2 * Hkv, &m) || kc.size[3] != m.D || !view(a[9], kI32, &slots) || slots.dims != 1 ||
       slots.size[0] != m.T || !together(m.x, {&slots, &kc, &vc}))
