@@ -4,7 +4,7 @@ Each translation unit is compiled by nvcc in parallel, then linked into one shar
 library next to this file.  No CMake, no torch extension machinery.  Beside it
 ``_binding.so``, the short way from Python to the entry points around training and serving
 (it looks at tensors through torch's C++ interface; where the interpreter's or torch's headers
-are missing it is left out, and the package's Python code does the same).
+are missing, or it does not compile with them, it is left out, and the package's Python code does the same).
 """
 from __future__ import annotations
 
@@ -12,6 +12,7 @@ import importlib.util
 import os
 import shutil
 import subprocess
+import sys
 import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
@@ -79,10 +80,6 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) 
             extra = ["-Xptxas", "-v"] if ptxas_info else []
             jobs.append([nvcc, *FLAGS, *extra, "-c", s, "-o", o])
 
-    binding = _binding_job(force)
-    if binding:
-        jobs.append(binding[0])
-
     def run(cmd):
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:
@@ -90,11 +87,23 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) 
         if verbose or ptxas_info:
             print(r.stdout + r.stderr)
 
-    if jobs:
-        with ThreadPoolExecutor(max_workers=len(jobs)) as ex:
+    def run_binding(cmd, made):
+        try:
+            run(cmd)
+        except (OSError, RuntimeError) as e:
+            if os.path.exists(BINDING):  # of another source or torch
+                os.remove(BINDING)
+            print(f"_binding.so is left out, the Python code takes its place: {e}", file=sys.stderr)
+        else:
+            os.replace(made, BINDING)
+
+    binding = _binding_job(force)
+    if jobs or binding:
+        with ThreadPoolExecutor(max_workers=len(jobs) + 1) as ex:
+            optional = ex.submit(run_binding, *binding) if binding else None
             list(ex.map(run, jobs))
-    if binding:
-        os.replace(binding[1], BINDING)
+            if optional:
+                optional.result()
     if force or _stale(LIB, objs):
         tmp = LIB + f".tmp{os.getpid()}"
         run([nvcc, *ARCH, "-shared", "-o", tmp, *objs])
