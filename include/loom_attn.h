@@ -266,6 +266,16 @@ loom_status loom_attn_bwd_varlen(const void* dout, const void* q, const void* k,
 size_t loom_attn_bwd_varlen_workspace_bytes(int B, int Hq, int Hkv, int total_q, int total_k, int D);
 
 /*
+ * How the backward pass deals its work (ragged = 0: loom_attn_bwd; 1: loom_attn_bwd_varlen, Sq and Skv
+ * the totals).  plan [4], written: shares that the sums of an item of 128 keys, and of one of 128
+ * query rows, are dealt to (1: none; more: fp32 partial sums in the workspace, added in the shares'
+ * order); planes of kv heads, and of query heads, whose items are dealt together (ragged: 0).
+ * Errors: INVALID_ARG, UNSUPPORTED, as the calls.
+ */
+loom_status loom_attn_bwd_plan(int B, int Hq, int Hkv, int Sq, int Skv, int D, int causal, int ragged,
+                               int* plan);
+
+/*
  * From a packed QKV projection (loom_gemm_bf16 with the three weights side by side) to what
  * attention takes: an RMS norm of every query and key head, the position rotation, and the split.
  * The paper has no counterpart.  Per query or key head x of a token, with that tensor's norm

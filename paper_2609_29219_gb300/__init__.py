@@ -35,7 +35,7 @@ __all__ = [
     "loom_debug_prefill_slots", "loom_debug_decode_stage_plan", "loom_debug_gemm_stages",
     "loom_debug_gemm_order", "loom_debug_decode_tensor_cores", "loom_attn_fwd_cluster",
     "loom_attn_bwd", "loom_attn_bwd_workspace_bytes", "loom_attn_bwd_varlen", "loom_attn_bwd_varlen_workspace_bytes",
-    "loom_qkv_norm_rope", "loom_qkv_norm_rope_cache", "loom_qkv_norm_rope_bwd", "loom_qkv_norm_rope_bwd_workspace_bytes",
+    "loom_attn_bwd_plan", "loom_qkv_norm_rope", "loom_qkv_norm_rope_cache", "loom_qkv_norm_rope_bwd", "loom_qkv_norm_rope_bwd_workspace_bytes",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -173,6 +173,8 @@ def capi() -> ctypes.CDLL:
             lib.loom_attn_bwd_varlen.restype = i32
             lib.loom_attn_bwd_varlen_workspace_bytes.argtypes = [i32] * 6
             lib.loom_attn_bwd_varlen_workspace_bytes.restype = sz
+            lib.loom_attn_bwd_plan.argtypes = [i32] * 8 + [vp]
+            lib.loom_attn_bwd_plan.restype = i32
             norm = [vp, vp, i32, vp, vp, i32, i32, i32, vp]  # the weights, the tables and the positions
             lib.loom_qkv_norm_rope.argtypes = [vp, i64] + norm + [vp] * 3 + [i32] * 5 + [f32, vp]
             lib.loom_qkv_norm_rope.restype = i32
@@ -636,6 +638,15 @@ def loom_attn_bwd_workspace_bytes(B, Hq, Hkv, Sq, Skv, D) -> int:
 
 def loom_attn_bwd_varlen_workspace_bytes(B, Hq, Hkv, total_q, total_k, D) -> int:
     return int(capi().loom_attn_bwd_varlen_workspace_bytes(B, Hq, Hkv, total_q, total_k, D))
+
+
+def loom_attn_bwd_plan(B, Hq, Hkv, Sq, Skv, D, causal=False, ragged=False) -> dict:
+    """How ``loom_attn_bwd`` (ragged: ``loom_attn_bwd_varlen``, Sq and Skv the totals) deals its work: the
+    shares of the items of 128 keys and of 128 query rows, and the planes of kv and of query heads whose
+    items are dealt together (0: ragged)."""
+    plan = (ctypes.c_int * 4)()
+    _check(capi().loom_attn_bwd_plan(B, Hq, Hkv, Sq, Skv, D, int(bool(causal)), int(bool(ragged)), plan), "loom_attn_bwd_plan")
+    return dict(zip(("kv_shares", "q_shares", "kv_block", "q_block"), plan))
 
 
 def loom_attn_bwd(do, q, k, v, o, lse, dq=None, dk=None, dv=None, workspace=None, *, causal=False, scale=None, dlse=None,

@@ -1215,14 +1215,6 @@ bool make_q_map(CUtensorMap* map, const void* base, int D, long long queries, lo
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Planes whose tiles are dealt together: as many as have what they walk (bytes a plane) in L2 at
-// once, since the longest tiles of them all go first, but at least a round of CTAs.
-int planes_per_block(double bytes, int tiles, int sms, long long planes) {
-  const double fit = 48e6 / bytes;
-  const long long n = fit > planes ? planes : static_cast<long long>(fit), round = (sms + tiles - 1) / tiles;
-  return static_cast<int>(n < round ? round : n);
-}
-
 template <class Kernel, class... Args>
 cudaError_t launch(Kernel kernel, int grid, int threads, uint32_t smem, cudaStream_t stream, Args... args) {
   cudaLaunchConfig_t cfg = {};
@@ -1304,9 +1296,8 @@ cudaError_t launch_d(const BwdArgs& a, const KernelCtl& ctl, cudaStream_t stream
     p.kv_tiles = (a.Skv + kTile - 1) / kTile;
     p.q_items = static_cast<int>(q_planes * p.q_tiles);
     p.kv_items = static_cast<int>(kv_planes * p.kv_tiles);
-    const double row = 4.0 * D;  // a query's dO and Q, a key's K and V
-    p.kv_block = planes_per_block(row * a.Sq * (1 << lg), p.kv_tiles, sms, kv_planes);
-    p.q_block = planes_per_block(row * a.Skv / (a.Hq / a.Hkv >> lg), p.q_tiles, sms, q_planes);
+    p.kv_block = plan.kv_block;
+    p.q_block = plan.q_block;
     items = static_cast<long long>(p.q_items) * p.q_split + static_cast<long long>(p.kv_items) * p.kv_split;
   }
   const int grid = static_cast<int>(items > 0 && items < sms ? items : sms);

@@ -38,10 +38,18 @@ inline long long bwd_stat_tiles(int B, long long Sq, int lg, bool ragged) {
 // item's steps are split into shares (with partial sums in fp32 in the workspace).
 struct BwdPlan {
   int kv_split, q_split;        // shares of an item, powers of two
+  int kv_block, q_block;        // dense: planes whose tiles are dealt together
   long long kv_items, q_items;  // (ragged: at most)
   int counters;                 // 64, then one for each elementwise warp of each item where items are split
   size_t stats_at, partial_at, bytes;
 };
+// Planes whose tiles are dealt together: as many as have what they walk (bytes a plane) in L2 at
+// once, since the longest tiles of them all go first, but at least a round of CTAs.
+inline int bwd_planes_per_block(double bytes, long long tiles, int sms, long long planes) {
+  const double fit = 48e6 / bytes;
+  const long long n = fit > planes ? planes : static_cast<long long>(fit), round = (sms + tiles - 1) / tiles;
+  return static_cast<int>(n < round ? round : n);
+}
 inline BwdPlan bwd_plan(int B, int Hq, int Hkv, long long Sq, long long Skv, int D, bool ragged, bool causal, int sms) {
   const int lg = bwd_pack_log2(Hq / Hkv), G = Hq / Hkv >> lg;
   const long long seqs = ragged ? 1 : B;
@@ -81,6 +89,11 @@ inline BwdPlan bwd_plan(int B, int Hq, int Hkv, long long Sq, long long Skv, int
       const double longest = k_long > q_end ? k_long : q_end, us = spread > longest ? spread : longest;
       if (us < best) best = us, p.kv_split = a, p.q_split = b;
     }
+  if (!ragged) {
+    const double row = 4.0 * D;  // a query's dO and Q, a key's K and V
+    p.kv_block = bwd_planes_per_block(row * Sq * (1 << lg), (Skv + 127) / 128, sms, kv_planes);
+    p.q_block = bwd_planes_per_block(row * Skv / G, stat_tiles, sms, q_planes);
+  }
   const bool any = p.kv_split > 1 || p.q_split > 1;
   p.counters = 64 + (any ? static_cast<int>((p.kv_items + p.q_items) * 8) : 0);
   p.stats_at = (static_cast<size_t>(p.counters) * 4 + 255) / 256 * 256;

@@ -380,6 +380,19 @@ size_t loom_attn_bwd_varlen_workspace_bytes(int B, int Hq, int Hkv, int total_q,
   return bwd_sizes_fit(B, Hq, Hkv, total_q, total_k, true) ? bwd_workspace(B, Hq, Hkv, total_q, total_k, D, true, sms_or_model()) : 0;
 }
 
+loom_status loom_attn_bwd_plan(int B, int Hq, int Hkv, int Sq, int Skv, int D, int causal, int ragged, int* plan) {
+  if (!plan || B <= 0 || Hq <= 0 || Hkv <= 0 || Sq < !ragged || Skv < !ragged || D <= 0) return LOOM_ERR_INVALID_ARG;
+  if (Hq % Hkv || (causal != 0 && causal != 1) || (ragged != 0 && ragged != 1) || (!ragged && causal && Sq > Skv))
+    return LOOM_ERR_INVALID_ARG;
+  if ((D != 64 && D != 128) || !bwd_sizes_fit(B, Hq, Hkv, Sq, Skv, ragged != 0)) return LOOM_ERR_UNSUPPORTED;
+  const BwdPlan p = bwd_plan(B, Hq, Hkv, Sq, Skv, D, ragged != 0, causal != 0, sms_or_model());
+  plan[0] = p.kv_split;
+  plan[1] = p.q_split;
+  plan[2] = p.kv_block;
+  plan[3] = p.q_block;
+  return LOOM_OK;
+}
+
 loom_status loom_attn_bwd(const void* dout, const void* q, const void* k, const void* v, const void* o, const float* lse,
                           const float* dlse, void* dq, void* dk, void* dv, void* workspace, size_t workspace_bytes, int B,
                           int Hq, int Hkv, int Sq, int Skv, int D, int causal, float scale, void* stream) {
