@@ -690,7 +690,7 @@ def loom_attn_bwd(do, q, k, v, o, lse, dq=None, dk=None, dv=None, workspace=None
     st = (_lib or capi()).loom_attn_bwd(
         do.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
         None if dlse is None else dlse.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), wp, wbytes, B, Hq, Hkv, Sq, Skv,
-        D, 1 if causal else 0, D ** -0.5 if scale is None else scale, _stream_of(stream, q))
+        D, 1 if causal else 0, D ** -0.5 if scale is None else float(scale), _stream_of(stream, q))
     if st:
         raise LoomError(st, "loom_attn_bwd")
     return dq, dk, dv
@@ -739,7 +739,7 @@ def loom_attn_bwd_varlen(do, q, k, v, o, lse, cu_seqlens_q, cu_seqlens_k, max_se
     st = (_lib or capi()).loom_attn_bwd_varlen(
         do.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
         None if dlse is None else dlse.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), cqp, ckp, wp, wbytes, B, Hq, Hkv,
-        total_q, total_k, max_seqlen_q, max_seqlen_k, D, 1 if causal else 0, D ** -0.5 if scale is None else scale,
+        total_q, total_k, int(max_seqlen_q), int(max_seqlen_k), D, 1 if causal else 0, D ** -0.5 if scale is None else float(scale),
         _stream_of(stream, q))
     if st:
         raise LoomError(st, "loom_attn_bwd_varlen")
@@ -828,6 +828,7 @@ def loom_qkv_norm_rope(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_head
         r = _fast.norm_rope(qkv, q_weight, k_weight, cos, sin, positions, interleaved, eps, num_heads, num_kv_heads, seq_len)
         if r is not None:
             return _fast_result(r, "loom_qkv_norm_rope")
+    num_heads, num_kv_heads, seq_len = int(num_heads), int(num_kv_heads), int(seq_len)
     T, D, dev, row, norm = _norm_operands(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, positions, interleaved)
     S = seq_len
     if S < 0 or (S and T % S):
@@ -849,7 +850,7 @@ def loom_qkv_norm_rope(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_head
     if v is None:
         v = new(ks, kst, _bf16)
     st = (_lib or capi()).loom_qkv_norm_rope(qkv.data_ptr(), row, *norm, q.data_ptr(), k.data_ptr(), v.data_ptr(), T, S, num_heads,
-                                             num_kv_heads, D, eps, _stream_of(stream, qkv))
+                                             num_kv_heads, D, float(eps), _stream_of(stream, qkv))
     if st:
         raise LoomError(st, "loom_qkv_norm_rope")
     return q, k, v
@@ -891,6 +892,7 @@ def loom_qkv_norm_rope_cache(qkv, q_weight, k_weight, cos, sin, positions, slots
         fine = False
     if not fine:
         _cache_checked(k_cache, v_cache, positions, slots)
+    num_heads = int(num_heads)
     page_size, Hkv = (a, b) if layout == "nhd" else (b, a)
     T, D, dev, row, norm = _norm_operands(qkv, q_weight, k_weight, cos, sin, num_heads, Hkv, positions, interleaved)
     if _several and not _together(qkv, k_cache, v_cache, slots):
@@ -904,7 +906,7 @@ def loom_qkv_norm_rope_cache(qkv, q_weight, k_weight, cos, sin, positions, slots
         raise ValueError(f"q must be {[T, num_heads, D]}")
     st = (_lib or capi()).loom_qkv_norm_rope_cache(
         qkv.data_ptr(), row, *norm, slots.data_ptr(), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), pages, page_size,
-        0 if layout == "nhd" else 1, T, num_heads, Hkv, D, eps, _stream_of(stream, qkv))
+        0 if layout == "nhd" else 1, T, num_heads, Hkv, D, float(eps), _stream_of(stream, qkv))
     if st:
         raise LoomError(st, "loom_qkv_norm_rope_cache")
     return q
@@ -969,7 +971,7 @@ def loom_qkv_norm_rope_bwd(dq, dk, dv, qkv, q_weight, k_weight, cos, sin, positi
         wbytes = workspace.numel() * workspace.element_size()
     st = (_lib or capi()).loom_qkv_norm_rope_bwd(
         dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), qkv.data_ptr(), row, *norm, dqkv.data_ptr(), drow, dq_weight.data_ptr(),
-        dk_weight.data_ptr(), wp, wbytes, T, S, Hq, Hkv, D, eps, _stream_of(stream, qkv))
+        dk_weight.data_ptr(), wp, wbytes, T, S, Hq, Hkv, D, float(eps), _stream_of(stream, qkv))
     if st:
         raise LoomError(st, "loom_qkv_norm_rope_bwd")
     return dqkv, dq_weight, dk_weight
