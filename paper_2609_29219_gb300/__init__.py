@@ -935,8 +935,9 @@ def loom_qkv_norm_rope_bwd(dq, dk, dv, qkv, q_weight, k_weight, cos, sin, positi
     except (AttributeError, IndexError):
         fine = False
     if not fine:
+        dims = 4 if isinstance(dq, _torch_mod.Tensor) and dq.dim() == 4 else 3
         for t, n in ((dq, "dq"), (dk, "dk"), (dv, "dv")):
-            _dev_ptr(t, n, _bf16, 3 if dq.dim() != 4 else 4)
+            _dev_ptr(t, n, _bf16, dims)
     T, D, dev, row, norm = _norm_operands(qkv, q_weight, k_weight, cos, sin, Hq, Hkv, positions, interleaved)
     S = qs[2] if ndim == 4 else 0
     if (not fine or tuple(qs) != ((qs[0], Hq, S, D) if ndim == 4 else (T, Hq, D)) or (qs[0] * S if ndim == 4 else T) != T

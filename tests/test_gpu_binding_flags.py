@@ -30,3 +30,17 @@ def test_a_flag_that_raises(loom, monkeypatch, way):  # noqa: F811
         with pytest.raises(KeyError, match="no truth value"):
             f()
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("way", ["compiled", "python"])
+def test_gradients_that_are_no_tensors_are_named(loom, monkeypatch, way):  # noqa: F811
+    import torch
+    if way == "python":
+        monkeypatch.setattr(loom, "_fast", None)
+    z = lambda *s: torch.zeros(s, device="cuda", dtype=torch.bfloat16)  # noqa: E731
+    w, t = z(64), torch.zeros((8, 32), device="cuda")
+    grads = {"dq": z(8, 2, 64), "dk": z(8, 1, 64), "dv": z(8, 1, 64)}
+    for name in grads:
+        for bad in (None, [1.0]):
+            with pytest.raises(TypeError, match=name):
+                loom.loom_qkv_norm_rope_bwd(*{**grads, name: bad}.values(), z(8, 256), w, w, t, t)
