@@ -9,23 +9,33 @@
 //
 // Two launches:
 //   attn_bwd_rows_kernel  delta and LSE of every query row, negated and in base 2, into the
-//                         workspace in tiles of 128 rows, and the item counters zeroed
+//                         workspace in tiles of 128 rows; the item counters, and dQ of ragged queries
+//                         that see no key, zeroed
 //   attn_bwd_kernel       persistent CTAs.  First the items (kv tile of 128 keys of a kv head):
 //                         dK and dV stay in TMEM while the CTA walks the query tiles of every
 //                         head of the group.  Then the items (query tile of 128 rows of a head):
 //                         dQ stays in TMEM while the CTA walks the keys.
-// Every gradient is summed in one CTA in a fixed order: no atomics on values, no fp32 copies of
-// the gradients in memory, the same bits each time.  The price is that S and dP are computed in
-// both walks: seven products of 128 x 128 x D per pair of tiles instead of five.
+// A gradient's sum stays in TMEM over a whole item, or a share of one, in a fixed order: no atomics on
+// values, the same bits each time.  The price is that S and dP are computed in both walks: seven
+// products of 128 x 128 x D per pair of tiles instead of five.  What it saves is fp32 sums of dQ in
+// memory, 512 D bytes for every pair of tiles, added in an order that would have to be kept.  What the plan
+// deals in shares (bwd.h; 512 items of H32/8 S8192 too) does pass through memory in fp32: one partial sum
+// a share.
 // Items are taken from a counter, long ones first, so CTAs that finish the kv items early start on
 // the query items.
+//
+// P and dS are rounded to bf16 where they become operands of dV, dK and dQ, as the forward rounds P:
+// in 32 bits they would take a slower kind of product, twice the TMEM, and operands Q, K and dO of
+// that type.  A gradient's error against 64 bits is 0.0024 of its norm; 0.0017 with one rounding, at the end.
 //
 // What bounds it: the tensor pipe and the hand-overs around it.  A step of a kv item (D = 128) is four
 // products, 2048 clocks of the pipe, and takes 2940: the score products read both operands from
 // shared memory, at all of its bandwidth, so that dK and the next dP take 1440 to 1600 clocks
 // together, dV and the next S 1250 to 1380; a query item's step takes 2110 for its three (1536).
-// GB300: B4 H32 S2048 D128 causal 356 us (966 TFLOP/s of the five products that the gradients need, 1352
-// of the seven), B1 H32/8 S8192 1078 us (1275, 1785; under the power limit).
+// GB300, on the device alone (graph replays): B4 H32 S2048 D128 causal 355 to 359 us (958 to 968 TFLOP/s
+// of the five products that the gradients need, 1.4 times that of the seven), B1 H32/8 S8192 1073 to 1093
+// (1257 to 1281; under the power limit), D64 H64/16 S8192 1650 to 1657 (829 to 833; not traced).  Call after
+// call: 371 to 388, 1166 to 1256.
 #include <cuda.h>
 #include <cuda_bf16.h>
 
@@ -165,7 +175,7 @@ __device__ __forceinline__ int ragged_stat0(const int32_t* cu_q, int b, int lg) 
 }
 
 // KV: item idx of the kv items, else of the query items.
-// An item whose steps are many and whose like are few is split: its shares accumulate a run of its
+// An item is split where the plan deals its steps in shares: these accumulate a run of its
 // steps each, write what they have in fp32, and the last one to arrive adds them up in their order.
 template <bool KV, bool VARLEN, bool SPLIT>
 __device__ __forceinline__ Item make_item(const BwdParams& p, long long idx, Cursor& cur) {
@@ -1257,7 +1267,8 @@ cudaError_t launch_d(const BwdArgs& a, const KernelCtl& ctl, cudaStream_t stream
   float* stats = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + plan.stats_at);
   e = launch(attn_bwd_rows_kernel<D, VARLEN>, static_cast<int>(q_planes * stat_tiles) * (kTile / kRowsPerBlock), kRowThreads, 0, stream,
              static_cast<const __nv_bfloat16*>(a.dout), static_cast<const __nv_bfloat16*>(a.o), a.lse, a.dlse, stats, counters,
-             plan.counters, a.B, a.Hq, a.Sq, lg, stat_tiles, a.cu_q, a.cu_k, a.causal, static_cast<__nv_bfloat16*>(a.dq));
+             plan.counters, a.B, a.Hq, a.Sq, lg, stat_tiles, a.cu_q, a.cu_k, a.causal,
+             static_cast<__nv_bfloat16*>(a.dq));
   if (e != cudaSuccess) return e;
   BwdParams p;
   memset(&p, 0, sizeof(p));

@@ -34,8 +34,9 @@ inline long long bwd_stat_tiles(int B, long long Sq, int lg, bool ragged) {
 }
 // How a call's work is dealt, and its workspace.  The kernel has two kinds of items: a tile of 128
 // keys of a kv head, whose steps are the query tiles of the group's heads that see it, and a tile of
-// 128 rows of a query plane, whose steps are the kv tiles it sees.  Where items are few and long, an
-// item's steps are split into shares (with partial sums in fp32 in the workspace).
+// 128 rows of a query plane, whose steps are the kv tiles it sees.  Where whole items would leave SMs
+// idle at the end, an item's steps are split into shares (with partial sums in fp32 in the workspace): few
+// and long items, but also the 512 of H32/8 S8192 causal, in two.
 struct BwdPlan {
   int kv_split, q_split;        // shares of an item, powers of two
   int kv_block, q_block;        // dense: planes whose tiles are dealt together
@@ -43,8 +44,12 @@ struct BwdPlan {
   int counters;                 // 64, then one for each elementwise warp of each item where items are split
   size_t stats_at, partial_at, bytes;
 };
-// Planes whose tiles are dealt together: as many as have what they walk (bytes a plane) in L2 at
-// once, since the longest tiles of them all go first, but at least a round of CTAs.
+// Planes whose tiles are dealt together: as many as have what their items walk at a time (bytes a plane)
+// in L2 at once, since the longest tiles of them all go first, but at least a round of CTAs.  A kv plane
+// walks the query planes of its group one after another, and one of them is counted.  With all of the
+// group's (another choice only where a group is no power of two), GB300, us, one / all: B8 H28/4 S2048 causal
+// 607 / 590, B2 S16384 7756 / 7716, B4 H28/4 S8192 4008 / 4030, D64 2974 / 3023, B2 H15/5 S8192 993 / 1010;
+// ten shapes 0.2 % apart on average.
 inline int bwd_planes_per_block(double bytes, long long tiles, int sms, long long planes) {
   const double fit = 48e6 / bytes;
   const long long n = fit > planes ? planes : static_cast<long long>(fit), round = (sms + tiles - 1) / tiles;
@@ -57,13 +62,15 @@ inline BwdPlan bwd_plan(int B, int Hq, int Hkv, long long Sq, long long Skv, int
   BwdPlan p{};
   p.kv_items = kv_planes * (ragged ? Skv / 128 + B : (Skv + 127) / 128);
   p.q_items = q_planes * stat_tiles;
-  // The splits of the least estimate (us, ragged: as if all sequences had the average length): all of
-  // the work spread over the SMs and part of the longest share of each kind, or the longest share if
-  // that takes longer, query items' after the kv items' full rounds.  A share of a split item writes
-  // and reads its partial sums, and the last one to arrive adds the others'; the kernel that can split
-  // takes longer over whole kv items too.  The constants are those that choose best among 1 to 16 shares of kv items
-  // and 1 to 8 of query items over 7000 random shapes (1 to 96 heads, 32 to 8000 queries and keys): its
-  // choices take 1.7 % longer than the best ones on average, no splits 16 %.  GB300, us, unsplit / split: B1 H8/1 S2000
+  // The splits of the least score: all of the work spread over the SMs and part of the longest share of
+  // each kind, or the longest share if that is more, query items' after the kv items' full rounds.  A
+  // share of a split item writes and reads its partial sums, and the last one to arrive adds the others';
+  // the kernel that can split takes longer over whole kv items too.  The constants are fitted: they choose
+  // best among 1 to 16 shares of kv items and 1 to 8 of query items over 7000 random dense shapes (1 to 96
+  // heads, 32 to 8000 queries and keys), where the choices take 1.7 % longer than the best ones on average,
+  // no splits 16 %.  They are about microseconds, but no step times (those at D = 128 are 1.6 and 1.1, not
+  // 1.1 and 0.67; at D = 64 steps are shorter, not longer), and not tried outside those shapes: a ragged
+  // batch enters as if all its sequences had the average length.  GB300, us, unsplit / split: B1 H8/1 S2000
   // causal 158 / 47, B1 H32/8 S2048 causal 136 / 100; B1 H16/16 S2048 causal, an item for each SM and more,
   // 52 / 73.
   const auto tiles = [&](long long rows) {
@@ -73,7 +80,10 @@ inline BwdPlan bwd_plan(int B, int Hq, int Hkv, long long Sq, long long Skv, int
   const double seen = causal ? 1 - 0.5 * static_cast<double>(Sq < Skv ? Sq : Skv) / static_cast<double>(Skv > 0 ? Skv : 1) : 1;
   const double kv_step = D == 128 ? 1.1 : 1.5, q_step = D == 128 ? 0.67 : 0.95, kv_part = D == 128 ? 6 : 7, q_part = 2;
   double best = 1e300;
-  // (items of many steps that keep less than a third of the SMs busy always have two shares or more)
+  // Items of eight steps and more that keep less than a third of the SMs busy always have two shares or
+  // more.  By the score alone 1.5 % of random shapes of 1 to 32 heads would have whole items instead: 37 of
+  // those, 16 to 21 us, take 0.96 to 1.13 times as long in shares, 1.04 on average, so the rule gains
+  // nothing; it keeps few long items in the form that they are tested in.
   const int least = kv_steps >= 8 && p.kv_items + p.q_items <= sms / 3 ? 2 : 1;
   for (int a = least; a <= 16 && (a == 1 || a <= kv_steps); a *= 2)
     for (int b = 1; b <= 8 && (b == 1 || b <= q_steps); b *= 2) {
@@ -86,8 +96,8 @@ inline BwdPlan bwd_plan(int B, int Hq, int Hkv, long long Sq, long long Skv, int
       const double q_long = q_steps * q_step / b + 2.1 + (b > 1 ? 0.35 * b : 0);
       const double spread = (p.kv_items * k_all + p.q_items * q_all) / sms + 0.42 * k_long + 0.16 * q_long;
       const double rounds = static_cast<double>(p.kv_items * a / sms) * (k_all / a), q_end = 0.85 * rounds + q_long;
-      const double longest = k_long > q_end ? k_long : q_end, us = spread > longest ? spread : longest;
-      if (us < best) best = us, p.kv_split = a, p.q_split = b;
+      const double longest = k_long > q_end ? k_long : q_end, score = spread > longest ? spread : longest;
+      if (score < best) best = score, p.kv_split = a, p.q_split = b;
     }
   if (!ragged) {
     const double row = 4.0 * D;  // a query's dO and Q, a key's K and V
