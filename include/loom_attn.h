@@ -189,6 +189,76 @@ loom_status loom_attn_decode_paged(const void* q, const void* k_cache, const voi
                                    int D, float scale, int num_splits, void* stream);
 
 /*
+ * Attention of a chunk of new tokens per sequence over the paged cache that loom_attn_decode_paged
+ * reads: a prompt's next chunk, drafted tokens, single tokens, or any mixture of them in one call.
+ * The paper has no counterpart.  The keys and values of the new tokens are in the cache already
+ * (loom_qkv_norm_rope_cache).
+ *   q            [total_q, Hq, D]  bf16, read: the new tokens, packed by sequence
+ *   k_cache, v_cache, block_table, num_pages, page_size, max_pages, kv_layout
+ *                as loom_attn_decode_paged; block_table [B, max_pages]
+ *   cu_seqlens_q [B + 1] int32 on the device: sequence b has the query tokens cu_seqlens_q[b] ..
+ *                cu_seqlens_q[b + 1] - 1; it starts at 0, never decreases and ends at total_q at most.
+ *                Tokens from cu_seqlens_q[B] on are padding: their rows of o and lse are left alone
+ *   seqlens_k    [B] int32 on the device: keys of each sequence, the new tokens among them; clamped
+ *                to 0 .. max_pages * page_size
+ *   o            [total_q, Hq, D]  bf16, written
+ *   lse          [Hq, total_q]     fp32, written (natural log); may be NULL
+ *   workspace    device scratch of at least loom_attn_chunk_paged_workspace_bytes(...) bytes, whose
+ *                contents on entry do not matter; it serves one call at a time
+ *   causal       1: query i of a sequence's n sees the keys j <= i + (keys - n); 0: all of them
+ * A query that sees no key gets O = 0 and LSE = -inf.  What the cache holds past a sequence's keys
+ * reaches no output, whatever it is; a NaN or infinity in the value of one of a sequence's keys may
+ * reach all its queries.  Sums have a fixed order: the same inputs give the same bits.
+ * Errors: INVALID_ARG (NULL pointer, a size <= 0, total_q < 0, Hq % Hkv, scale, kv_layout, causal),
+ * UNSUPPORTED (as loom_attn_decode_paged; more than 2^31 - 1 query rows total_q Hq), MISALIGNED (q,
+ * caches, o, workspace: 16 bytes; the others 4), WORKSPACE, CUDA.  total_q = 0 returns LOOM_OK at once.
+ */
+loom_status loom_attn_chunk_paged(const void* q, const void* k_cache, const void* v_cache,
+                                  const int32_t* block_table, const int32_t* cu_seqlens_q,
+                                  const int32_t* seqlens_k, void* o, float* lse, void* workspace,
+                                  size_t workspace_bytes, int B, int Hq, int Hkv, int total_q,
+                                  int num_pages, int page_size, int max_pages, int kv_layout, int D,
+                                  int causal, float scale, void* stream);
+/* Workspace bytes of loom_attn_chunk_paged; 0 on invalid or unsupported sizes.  At most 41 MB. */
+size_t loom_attn_chunk_paged_workspace_bytes(int B, int Hq, int Hkv, int total_q, int D);
+
+/*
+ * The bookkeeping of a serving step on the device: from the requests' lengths, the block tables,
+ * positions, slots and offsets that loom_qkv_norm_rope_cache, loom_attn_chunk_paged and
+ * loom_attn_decode_paged take, with pages from a free list and back to it.  The paper has no counterpart.
+ *   new_lens     [B] int32, read: tokens that request b brings to this step, in the order of the
+ *                requests; negative: the request is over, and the pages of its lens[b] tokens go back
+ *   lens         [B] int32, read: tokens that it has in the cache (clamped to 0 .. max_pages page_size)
+ *   block_table  [B, max_pages] int32, read and written: the first ceil(lens[b] / page_size) entries of
+ *                a row are its pages; the entries of pages that it takes are written after them,
+ *                and nothing else is
+ *   free_pages   [num_pages] int32, read and written: the free pages, *free_count of them, the last one
+ *                taken first.  Pages given back are appended (by request, in the table's order)
+ *                before any is taken; a list longer than num_pages (a page given back twice) is cut there
+ *   free_count   [1] int32, read;  free_count_out [1] int32, written
+ *   cu_seqlens   [B + 1] int32, written: the offsets of the requests' tokens, T at most
+ *   seqlens_k    [B] int32, written: lens[b] + new_lens[b]; lens[b] for a request that is refused, 0
+ *                for one that is over
+ *   positions, slots  [T] int32, written: a token's position and its row of the cache (page
+ *                page_size + row in it); a token of a refused request, one past the last request's, and
+ *                one whose page lies outside 0 .. num_pages - 1 have slot -1 (position 0 but for the last)
+ *   granted      [B] int32, written: the tokens of request b that the step has room for, new_lens[b] or 0
+ * A request is refused whole: where its row of the table or the T tokens have no room for it, or
+ * where the free pages do not reach it in the order of the requests (one that needs no new page is never
+ * refused for that).  It takes no page, and its tokens keep their place in the step.
+ * seqlens_k may be lens, and free_count_out free_count; the call can then be captured and replayed
+ * step by step.  No other buffers may overlap.
+ * Errors: INVALID_ARG (NULL pointer; positions and slots may be NULL with T = 0; B, num_pages,
+ * page_size or max_pages <= 0, T < 0), UNSUPPORTED (B > 8192; more than 2^31 - 1 rows in the cache or of
+ * a request, or entries of the table), MISALIGNED (4 bytes), CUDA.
+ */
+loom_status loom_paged_plan(const int32_t* new_lens, const int32_t* lens, int32_t* block_table,
+                            int32_t* free_pages, const int32_t* free_count, int32_t* free_count_out,
+                            int32_t* cu_seqlens, int32_t* seqlens_k, int32_t* positions, int32_t* slots,
+                            int32_t* granted, int B, int T, int num_pages, int page_size,
+                            int max_pages, void* stream);
+
+/*
  * Flash Decode without any allocation and without a workspace argument.  The paper has
  * no counterpart; this entry point exists for callers that cannot obtain device scratch
  * memory for a call -- serving engines that reserve all device memory at start-up and
@@ -354,6 +424,41 @@ loom_status loom_qkv_norm_rope_bwd(const void* dq, const void* dk, const void* d
                                    int Hkv, int D, float eps, void* stream);
 /* Workspace bytes of loom_qkv_norm_rope_bwd; 0 on an unsupported D. */
 size_t loom_qkv_norm_rope_bwd_workspace_bytes(int D);
+
+/*
+ * The three calls with positions on several axes (time, height and width of image and video tokens):
+ * pair i of a head's rotary_dim / 2 turns by the row of its axis' position, column i of the tables.
+ *   positions  [n_axes, T] int32 on the device (required), rows positions_stride elements apart
+ *              (at least T); each clamped to the tables
+ *   n_axes     1 to 4
+ *   pair_axis  [rotary_dim / 2] int on the host, read during the call: the axis of each pair
+ * Everything else as the call without axes.
+ * Errors: as that call; NULL pair_axis, an axis outside 0 .. n_axes - 1, n_axes < 1, positions_stride
+ * below T: INVALID_ARG; n_axes > 4: UNSUPPORTED.
+ */
+loom_status loom_qkv_norm_rope_axes(const void* qkv, int64_t qkv_stride, const void* q_weight,
+                                    const void* k_weight, int weight_type, const float* cos,
+                                    const float* sin, int table_rows, int rotary_dim, int interleaved,
+                                    const int32_t* positions, int64_t positions_stride, int n_axes,
+                                    const int* pair_axis, void* q, void* k, void* v, int T, int seq_len,
+                                    int Hq, int Hkv, int D, float eps, void* stream);
+loom_status loom_qkv_norm_rope_axes_cache(const void* qkv, int64_t qkv_stride, const void* q_weight,
+                                          const void* k_weight, int weight_type, const float* cos,
+                                          const float* sin, int table_rows, int rotary_dim,
+                                          int interleaved, const int32_t* positions,
+                                          int64_t positions_stride, int n_axes, const int* pair_axis,
+                                          const int32_t* slots, void* q, void* k_cache, void* v_cache,
+                                          int num_pages, int page_size, int kv_layout, int T, int Hq,
+                                          int Hkv, int D, float eps, void* stream);
+loom_status loom_qkv_norm_rope_axes_bwd(const void* dq, const void* dk, const void* dv, const void* qkv,
+                                        int64_t qkv_stride, const void* q_weight, const void* k_weight,
+                                        int weight_type, const float* cos, const float* sin,
+                                        int table_rows, int rotary_dim, int interleaved,
+                                        const int32_t* positions, int64_t positions_stride, int n_axes,
+                                        const int* pair_axis, void* dqkv, int64_t dqkv_stride,
+                                        float* dq_weight, float* dk_weight, void* workspace,
+                                        size_t workspace_bytes, int T, int seq_len, int Hq, int Hkv,
+                                        int D, float eps, void* stream);
 
 /*
  * Analytic schedule model (paper Sec. 2.6: HEG latency, Eq. 5-7, and the constrained

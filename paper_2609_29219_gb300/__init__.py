@@ -36,6 +36,7 @@ __all__ = [
     "loom_debug_gemm_order", "loom_debug_decode_tensor_cores", "loom_attn_fwd_cluster",
     "loom_attn_bwd", "loom_attn_bwd_workspace_bytes", "loom_attn_bwd_varlen", "loom_attn_bwd_varlen_workspace_bytes",
     "loom_attn_bwd_plan", "loom_qkv_norm_rope", "loom_qkv_norm_rope_cache", "loom_qkv_norm_rope_bwd", "loom_qkv_norm_rope_bwd_workspace_bytes",
+    "loom_attn_chunk_paged", "loom_attn_chunk_paged_workspace_bytes", "loom_paged_plan",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -182,6 +183,19 @@ def capi() -> ctypes.CDLL:
             lib.loom_qkv_norm_rope_cache.restype = i32
             lib.loom_qkv_norm_rope_bwd.argtypes = [vp] * 4 + [i64] + norm + [vp, i64, vp, vp, vp, sz] + [i32] * 5 + [f32, vp]
             lib.loom_qkv_norm_rope_bwd.restype = i32
+            axes = norm + [i64, i32, vp]  # and the axes of the positions
+            lib.loom_qkv_norm_rope_axes.argtypes = [vp, i64] + axes + [vp] * 3 + [i32] * 5 + [f32, vp]
+            lib.loom_qkv_norm_rope_axes.restype = i32
+            lib.loom_qkv_norm_rope_axes_cache.argtypes = [vp, i64] + axes + [vp] * 4 + [i32] * 7 + [f32, vp]
+            lib.loom_qkv_norm_rope_axes_cache.restype = i32
+            lib.loom_qkv_norm_rope_axes_bwd.argtypes = [vp] * 4 + [i64] + axes + [vp, i64, vp, vp, vp, sz] + [i32] * 5 + [f32, vp]
+            lib.loom_qkv_norm_rope_axes_bwd.restype = i32
+            lib.loom_attn_chunk_paged.argtypes = [vp] * 9 + [sz] + [i32] * 10 + [f32, vp]
+            lib.loom_attn_chunk_paged.restype = i32
+            lib.loom_attn_chunk_paged_workspace_bytes.argtypes = [i32] * 5
+            lib.loom_attn_chunk_paged_workspace_bytes.restype = sz
+            lib.loom_paged_plan.argtypes = [vp] * 11 + [i32] * 5 + [vp]
+            lib.loom_paged_plan.restype = i32
             lib.loom_qkv_norm_rope_bwd_workspace_bytes.argtypes = [i32]
             lib.loom_qkv_norm_rope_bwd_workspace_bytes.restype = sz
             _lib = lib
@@ -578,6 +592,111 @@ def loom_attn_decode_paged(q, k_cache, v_cache, block_table, seqlens_k, o=None, 
     return (o, lse) if (return_lse or lse is not None) else o
 
 
+def loom_attn_chunk_paged_workspace_bytes(B, Hq, Hkv, total_q, D) -> int:
+    return int(capi().loom_attn_chunk_paged_workspace_bytes(B, Hq, Hkv, total_q, D))
+
+
+@functools.lru_cache(maxsize=256)
+def _chunk_need(device, *sizes):  # (the devices' SMs may differ)
+    return capi().loom_attn_chunk_paged_workspace_bytes(*sizes)
+
+
+def loom_attn_chunk_paged(q, k_cache, v_cache, block_table, cu_seqlens_q, seqlens_k, o=None, lse=None, workspace=None, *,
+                          causal=True, scale=None, stream=None, return_lse=False, layout="nhd"):
+    """Attention of each sequence's new tokens over its keys in a paged cache (theirs among them).
+
+    q [total_q, Hq, D]: the new tokens, packed; k_cache/v_cache bf16, [num_pages, page_size, Hkv, D]
+    (layout "nhd") or [num_pages, Hkv, page_size, D] ("hnd"); block_table [B, max_pages], cu_seqlens_q
+    [B + 1] and seqlens_k [B] int32, all on the device.  Tokens from cu_seqlens_q[B] on are padding, whose
+    rows are left as they were.  ``workspace``: a CUDA uint8 tensor of at least
+    ``loom_attn_chunk_paged_workspace_bytes`` bytes (allocated here if None).  Returns ``o``
+    ([total_q, Hq, D]) or ``(o, lse)`` with lse [Hq, total_q]."""
+    _torch()
+    if layout not in ("nhd", "hnd"):
+        raise ValueError("layout is 'nhd' or 'hnd'")
+    qp = _ptr(q, "q", _bf16, 3)
+    dev = _on_current(q, "q") if _several else None
+    kp = _ptr(k_cache, "k_cache", _bf16, 4, dev)
+    vp_ = _ptr(v_cache, "v_cache", _bf16, 4, dev)
+    total_q, Hq, D = q.shape
+    if layout == "nhd":
+        num_pages, page_size, Hkv, Dk = k_cache.shape
+    else:
+        num_pages, Hkv, page_size, Dk = k_cache.shape
+    if v_cache.shape != k_cache.shape or Dk != D:
+        raise ValueError("the chunk's attention takes q [total_q, Hq, D] and two caches of one shape")
+    tp = _ptr(block_table, "block_table", _i32, 2, dev)
+    cp = _ptr(cu_seqlens_q, "cu_seqlens_q", _i32, 1, dev)
+    sp = _ptr(seqlens_k, "seqlens_k", _i32, 1, dev)
+    B, max_pages = block_table.shape
+    if cu_seqlens_q.shape[0] != B + 1 or seqlens_k.shape[0] != B:
+        raise ValueError("block_table, cu_seqlens_q and seqlens_k must be [B, max_pages], [B + 1] and [B]")
+    if o is None:
+        o = _new((total_q, Hq, D), (Hq * D, D, 1), _bf16, q, True, stream)
+    elif o.shape != q.shape:
+        raise ValueError("o must have q's shape")
+    op = _ptr(o, "o", _bf16, 3, dev)
+    if lse is None and return_lse:
+        lse = _new((Hq, total_q), (total_q, 1), _f32, q, stream=stream)
+    lp = None
+    if lse is not None:
+        lp = _ptr(lse, "lse", _f32, 2, dev)
+        if tuple(lse.shape) != (Hq, total_q):
+            raise ValueError("lse must be [Hq, total_q]")
+    if workspace is None:
+        wbytes = _chunk_need(q.get_device(), B, Hq, Hkv, total_q, D)
+        workspace = _new((max(wbytes, 16),), (1,), _u8, q, stream=stream)
+        wp = workspace.data_ptr()
+    else:
+        wp = _dev_ptr(workspace, "workspace", None, None, dev)
+        wbytes = workspace.numel() * workspace.element_size()
+    st = (_lib or capi()).loom_attn_chunk_paged(
+        qp, kp, vp_, tp, cp, sp, op, lp, wp, wbytes, B, Hq, Hkv, total_q, num_pages, page_size, max_pages,
+        0 if layout == "nhd" else 1, D, 1 if causal else 0, D ** -0.5 if scale is None else float(scale), _stream_of(stream, q))
+    _check(st, "loom_attn_chunk_paged")
+    return (o, lse) if lse is not None else o
+
+
+def loom_paged_plan(new_lens, lens, block_table, free_pages, free_count, num_tokens, page_size, seqlens_k=None,
+                    free_count_out=None, cu_seqlens=None, positions=None, slots=None, granted=None, *, stream=None):
+    """A serving step's bookkeeping on the device, from the requests' lengths.
+
+    new_lens and lens [B] int32: the tokens that each request brings to the step (negative: it is over,
+    and its pages go back to the list) and those that it has in the cache; block_table [B, max_pages]
+    int32, updated with the pages taken; free_pages [num_pages] int32 with free_count [1] int32 of
+    them free; num_tokens: the tokens that the step has room for (those past the last request's are padding).
+    A request that the table, the tokens or the free pages have no room for is refused whole.
+
+    Writes and returns ``cu_seqlens`` [B + 1], ``seqlens_k`` [B] (may be lens), ``positions`` and ``slots``
+    [num_tokens] and ``granted`` [B] (allocated if None); the free pages that are left go to
+    ``free_count_out`` (None: to free_count)."""
+    _torch()
+    np_ = _ptr(new_lens, "new_lens", _i32, 1)
+    dev = _on_current(new_lens, "new_lens") if _several else None
+    B, T = new_lens.shape[0], int(num_tokens)
+    lp, tp = _ptr(lens, "lens", _i32, 1, dev), _ptr(block_table, "block_table", _i32, 2, dev)
+    fp, cp = _ptr(free_pages, "free_pages", _i32, 1, dev), _ptr(free_count, "free_count", _i32, 1, dev)
+    if lens.shape[0] != B or block_table.shape[0] != B or free_count.shape[0] != 1:
+        raise ValueError("new_lens, lens, block_table and free_count must be [B], [B], [B, max_pages] and [1]")
+    if T < 0:
+        raise ValueError("num_tokens must not be negative")
+    if free_count_out is None:
+        free_count_out = free_count
+    outs = []
+    for t, name, n in ((free_count_out, "free_count_out", 1), (cu_seqlens, "cu_seqlens", B + 1), (seqlens_k, "seqlens_k", B),
+                       (positions, "positions", T), (slots, "slots", T), (granted, "granted", B)):
+        if t is None:
+            t = _new((n,), (1,), _i32, new_lens, stream=stream)
+        elif _ptr(t, name, _i32, 1, dev) is None or t.shape[0] != n:
+            raise ValueError(f"{name} must be [{n}]")
+        outs.append(t)
+    st = (_lib or capi()).loom_paged_plan(
+        np_, lp, tp, fp, cp, *(t.data_ptr() for t in outs), B, T, free_pages.shape[0], int(page_size), block_table.shape[1],
+        _stream_of(stream, new_lens))
+    _check(st, "loom_paged_plan")
+    return tuple(outs[1:])
+
+
 @functools.lru_cache(maxsize=256)
 def _bwd_need(varlen, *sizes):
     lib = capi()
@@ -782,10 +901,33 @@ def _norm_checked(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, po
             raise ValueError("positions must be [T]")
 
 
-def _norm_operands(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, positions, interleaved):
+@functools.lru_cache(maxsize=64)
+def _axis_array(pair_axis):
+    return (ctypes.c_int * len(pair_axis))(*pair_axis)
+
+
+def _axes_operands(qkv, cos, positions, pair_axis):
+    """The C arguments of positions on several axes, from positions on."""
+    if positions is None:
+        raise TypeError("positions are needed with pair_axis")
+    _dev_ptr(positions, "positions", _i32, 2, qkv.get_device())
+    if positions.shape[1] != qkv.shape[0]:
+        raise ValueError("positions must be [axes, T] with pair_axis")
+    axes = _axis_array(tuple(map(int, pair_axis)))
+    if len(axes) != cos.shape[1]:
+        raise ValueError(f"pair_axis must name an axis for each of the {cos.shape[1]} pairs that the tables have")
+    if not all(0 <= a < positions.shape[0] for a in axes):
+        raise ValueError(f"pair_axis names an axis that positions do not have ({positions.shape[0]} axes)")
+    return positions.data_ptr(), positions.shape[1], positions.shape[0], axes
+
+
+def _norm_operands(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, positions, interleaved, pair_axis=None):
     """What the norm-and-rotation entry points share: (T, D, the device's index, qkv's row distance, and
-    the C arguments from q_weight to positions)."""
+    the C arguments from q_weight to positions, or to pair_axis)."""
     _torch()
+    if pair_axis is not None:
+        T, D, dev, row, norm = _norm_operands(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, None, interleaved)
+        return T, D, dev, row, norm[:-1] + _axes_operands(qkv, cos, positions, pair_axis)
     try:
         T, W = qkv.shape
         D, = q_weight.shape
@@ -816,20 +958,24 @@ def _check_tables(T, seq_len, cos, positions):
 
 
 def loom_qkv_norm_rope(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, positions=None, q=None, k=None, v=None, *,
-                       seq_len=0, eps=1e-6, interleaved=False, stream=None):
+                       seq_len=0, eps=1e-6, interleaved=False, pair_axis=None, stream=None):
     """RMS norm of each query and key head, the position rotation, and the split of a packed projection.
 
     qkv [T, (num_heads + 2 num_kv_heads) D] bf16 (its rows may lie further apart); q_weight, k_weight
     [D] bf16 or fp32; cos, sin [positions, rotary_dim / 2] fp32; positions [T] int32 (None: t, or t %
     seq_len).  Writes and returns ``q, k, v`` (allocated if None): [T, H, D], or with ``seq_len``
-    [T / seq_len, H, seq_len, D], as the ragged and the dense prefill take them."""
+    [T / seq_len, H, seq_len, D], as the ragged and the dense prefill take them.
+
+    ``pair_axis``, a sequence of rotary_dim / 2 whole numbers: positions are [axes, T] (at most four axes)
+    and pair i of a head turns by its token's position on axis pair_axis[i]."""
     _torch()
-    if _fast is not None and q is None and k is None and v is None and stream is None:
+    if _fast is not None and q is None and k is None and v is None and stream is None and pair_axis is None:
         r = _fast.norm_rope(qkv, q_weight, k_weight, cos, sin, positions, interleaved, eps, num_heads, num_kv_heads, seq_len)
         if r is not None:
             return _fast_result(r, "loom_qkv_norm_rope")
     num_heads, num_kv_heads, seq_len = int(num_heads), int(num_kv_heads), int(seq_len)
-    T, D, dev, row, norm = _norm_operands(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, positions, interleaved)
+    T, D, dev, row, norm = _norm_operands(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, positions, interleaved,
+                                          pair_axis)
     S = seq_len
     if S < 0 or (S and T % S):
         raise ValueError("T must be a multiple of seq_len")
@@ -849,7 +995,8 @@ def loom_qkv_norm_rope(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_head
         k = new(ks, kst, _bf16)
     if v is None:
         v = new(ks, kst, _bf16)
-    st = (_lib or capi()).loom_qkv_norm_rope(qkv.data_ptr(), row, *norm, q.data_ptr(), k.data_ptr(), v.data_ptr(), T, S, num_heads,
+    lib = _lib or capi()
+    st = (lib.loom_qkv_norm_rope if pair_axis is None else lib.loom_qkv_norm_rope_axes)(qkv.data_ptr(), row, *norm, q.data_ptr(), k.data_ptr(), v.data_ptr(), T, S, num_heads,
                                              num_kv_heads, D, float(eps), _stream_of(stream, qkv))
     if st:
         raise LoomError(st, "loom_qkv_norm_rope")
@@ -867,17 +1014,18 @@ def _cache_checked(k_cache, v_cache, positions, slots):
 
 
 def loom_qkv_norm_rope_cache(qkv, q_weight, k_weight, cos, sin, positions, slots, k_cache, v_cache, num_heads, q=None, *,
-                             layout="nhd", eps=1e-6, interleaved=False, stream=None):
+                             layout="nhd", eps=1e-6, interleaved=False, pair_axis=None, stream=None):
     """``loom_qkv_norm_rope`` for serving: k and v go to their rows of the caches, q is returned.
 
     positions and slots [T] int32: token t's row is slots[t] % page_size of page slots[t] //
     page_size (a slot outside the cache, such as -1, is not written).  k_cache, v_cache [num_pages,
     page_size, Hkv, D] (layout "nhd") or [num_pages, Hkv, page_size, D] ("hnd"; also a contiguous
-    cache [B, Hkv, capacity, D], whose slots are b * capacity + position).  Returns q [T, num_heads, D]."""
+    cache [B, Hkv, capacity, D], whose slots are b * capacity + position).  Returns q [T, num_heads, D].
+    ``pair_axis``: positions on several axes, as ``loom_qkv_norm_rope``."""
     if layout not in ("nhd", "hnd"):
         raise ValueError("layout is 'nhd' or 'hnd'")
     _torch()
-    if _fast is not None and q is None and stream is None:
+    if _fast is not None and q is None and stream is None and pair_axis is None:
         r = _fast.norm_rope_cache(qkv, q_weight, k_weight, cos, sin, positions, interleaved, eps, num_heads, slots, k_cache,
                                   v_cache, layout == "hnd")
         if r is not None:
@@ -894,7 +1042,7 @@ def loom_qkv_norm_rope_cache(qkv, q_weight, k_weight, cos, sin, positions, slots
         _cache_checked(k_cache, v_cache, positions, slots)
     num_heads = int(num_heads)
     page_size, Hkv = (a, b) if layout == "nhd" else (b, a)
-    T, D, dev, row, norm = _norm_operands(qkv, q_weight, k_weight, cos, sin, num_heads, Hkv, positions, interleaved)
+    T, D, dev, row, norm = _norm_operands(qkv, q_weight, k_weight, cos, sin, num_heads, Hkv, positions, interleaved, pair_axis)
     if _several and not _together(qkv, k_cache, v_cache, slots):
         for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache"), (slots, "slots")):
             _dev_ptr(t, name, dev=dev)
@@ -904,7 +1052,8 @@ def loom_qkv_norm_rope_cache(qkv, q_weight, k_weight, cos, sin, positions, slots
         q = _new((T, num_heads, D), (num_heads * D, D, 1), _bf16, qkv, stream=stream)
     elif _dev_ptr(q, "q", _bf16, 3, dev) is None or tuple(q.shape) != (T, num_heads, D):
         raise ValueError(f"q must be {[T, num_heads, D]}")
-    st = (_lib or capi()).loom_qkv_norm_rope_cache(
+    lib = _lib or capi()
+    st = (lib.loom_qkv_norm_rope_cache if pair_axis is None else lib.loom_qkv_norm_rope_axes_cache)(
         qkv.data_ptr(), row, *norm, slots.data_ptr(), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), pages, page_size,
         0 if layout == "nhd" else 1, T, num_heads, Hkv, D, float(eps), _stream_of(stream, qkv))
     if st:
@@ -917,13 +1066,14 @@ def loom_qkv_norm_rope_bwd_workspace_bytes(D) -> int:
 
 
 def loom_qkv_norm_rope_bwd(dq, dk, dv, qkv, q_weight, k_weight, cos, sin, positions=None, dqkv=None, dq_weight=None,
-                           dk_weight=None, workspace=None, *, eps=1e-6, interleaved=False, stream=None):
+                           dk_weight=None, workspace=None, *, eps=1e-6, interleaved=False, pair_axis=None, stream=None):
     """Gradients of ``loom_qkv_norm_rope``: dq, dk, dv laid out as it returned q, k, v ([T, H, D] or
     [B, H, seq_len, D]), the rest as the forward call had it.  Writes and returns ``dqkv`` (like qkv;
     its rows may lie further apart), ``dq_weight`` and ``dk_weight`` ([D] fp32), allocated if None.
     ``workspace``: a CUDA uint8 tensor of ``loom_qkv_norm_rope_bwd_workspace_bytes(D)`` bytes."""
     _torch()
-    if _fast is not None and dqkv is None and dq_weight is None and dk_weight is None and workspace is None and stream is None:
+    if (_fast is not None and dqkv is None and dq_weight is None and dk_weight is None and workspace is None and stream is None
+            and pair_axis is None):
         r = _fast.norm_rope_bwd(qkv, q_weight, k_weight, cos, sin, positions, interleaved, eps, dq, dk, dv)
         if r is not None:
             return _fast_result(r, "loom_qkv_norm_rope_bwd")
@@ -938,7 +1088,7 @@ def loom_qkv_norm_rope_bwd(dq, dk, dv, qkv, q_weight, k_weight, cos, sin, positi
         dims = 4 if isinstance(dq, _torch_mod.Tensor) and dq.dim() == 4 else 3
         for t, n in ((dq, "dq"), (dk, "dk"), (dv, "dv")):
             _dev_ptr(t, n, _bf16, dims)
-    T, D, dev, row, norm = _norm_operands(qkv, q_weight, k_weight, cos, sin, Hq, Hkv, positions, interleaved)
+    T, D, dev, row, norm = _norm_operands(qkv, q_weight, k_weight, cos, sin, Hq, Hkv, positions, interleaved, pair_axis)
     S = qs[2] if ndim == 4 else 0
     if (not fine or tuple(qs) != ((qs[0], Hq, S, D) if ndim == 4 else (T, Hq, D)) or (qs[0] * S if ndim == 4 else T) != T
             or tuple(ks) != (qs[0], Hkv, *qs[2:])):
@@ -970,7 +1120,8 @@ def loom_qkv_norm_rope_bwd(dq, dk, dv, qkv, q_weight, k_weight, cos, sin, positi
     else:
         wp = _dev_ptr(workspace, "workspace", None, None, dev)
         wbytes = workspace.numel() * workspace.element_size()
-    st = (_lib or capi()).loom_qkv_norm_rope_bwd(
+    lib = _lib or capi()
+    st = (lib.loom_qkv_norm_rope_bwd if pair_axis is None else lib.loom_qkv_norm_rope_axes_bwd)(
         dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), qkv.data_ptr(), row, *norm, dqkv.data_ptr(), drow, dq_weight.data_ptr(),
         dk_weight.data_ptr(), wp, wbytes, T, S, Hq, Hkv, D, float(eps), _stream_of(stream, qkv))
     if st:

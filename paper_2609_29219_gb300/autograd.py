@@ -66,10 +66,10 @@ def attention_varlen(q, k, v, cu_seqlens_q, cu_seqlens_k, max_seqlen_q, max_seql
 
 class _QkvNormRope(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, positions, seq_len, eps, interleaved):
+    def forward(ctx, qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, positions, seq_len, eps, interleaved, pair_axis):
         ctx.save_for_backward(qkv, q_weight, k_weight, cos, sin, positions)
         ctx.shapes = (num_heads, num_kv_heads, seq_len)
-        ctx.rest = {"eps": eps, "interleaved": interleaved}
+        ctx.rest = {"eps": eps, "interleaved": interleaved, "pair_axis": pair_axis}
         return loom.loom_qkv_norm_rope(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, positions, seq_len=seq_len,
                                        **ctx.rest)
 
@@ -79,16 +79,17 @@ class _QkvNormRope(torch.autograd.Function):
         qkv, q_weight, k_weight, cos, sin, positions = ctx.saved_tensors
         dqkv, dqw, dkw = loom.loom_qkv_norm_rope_bwd(dq.contiguous(), dk.contiguous(), dv.contiguous(), qkv, q_weight, k_weight,
                                                      cos, sin, positions, **ctx.rest)
-        return (dqkv, dqw.to(q_weight.dtype), dkw.to(k_weight.dtype), *(None,) * 8)
+        return (dqkv, dqw.to(q_weight.dtype), dkw.to(k_weight.dtype), *(None,) * 9)
 
 
 def qkv_norm_rope(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, positions=None, *, seq_len=0, eps=1e-6,
-                  interleaved=False):
+                  interleaved=False, pair_axis=None):
     """``loom_qkv_norm_rope`` with gradients of qkv and the two norm weights: (q, k, v).  The tables have none."""
     for t, name in ((cos, "cos"), (sin, "sin")):
         if t.requires_grad and torch.is_grad_enabled():
             raise ValueError(f"{name} requires a gradient, which qkv_norm_rope does not have: detach it")
-    return _QkvNormRope.apply(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, positions, seq_len, eps, interleaved)
+    return _QkvNormRope.apply(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, positions, seq_len, eps, interleaved,
+                              None if pair_axis is None else tuple(pair_axis))
 
 
 class _Linear(torch.autograd.Function):

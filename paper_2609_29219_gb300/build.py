@@ -22,7 +22,7 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libloomattn.so")
 BINDING = os.path.join(HERE, "_binding.so")
 SOURCES = ["loom_api.cu", "attn_fwd.cu", "attn_decode.cu", "loom_noalloc.cu", "gemm.cu",
-           "attn_bwd.cu", "qkv_rope.cu"]
+           "attn_bwd.cu", "qkv_rope.cu", "attn_chunk.cu", "paged_plan.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ARCH + ["-O3", "-lineinfo", "-std=c++17", "--expt-relaxed-constexpr",
                 "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall"]

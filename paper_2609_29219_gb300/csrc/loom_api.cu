@@ -10,6 +10,7 @@
 
 #include "../../include/loom_attn.h"
 #include "bwd.h"
+#include "chunk.h"
 #include "gemm.h"
 #include "gemm_model.h"
 #include "kernels.h"
@@ -421,6 +422,71 @@ loom_status loom_attn_bwd_varlen(const void* dout, const void* q, const void* k,
 }
 
 namespace {
+// Sizes of a chunk call that there is a kernel for.
+bool chunk_sizes_ok(int B, int Hq, int Hkv, int total_q, int D) {
+  return (D == 64 || D == 128) && static_cast<long long>(total_q) * Hq <= 0x7fffffffLL;
+}
+}  // namespace
+
+size_t loom_attn_chunk_paged_workspace_bytes(int B, int Hq, int Hkv, int total_q, int D) {
+  if (B <= 0 || Hq <= 0 || Hkv <= 0 || total_q < 0 || Hq % Hkv != 0 || !chunk_sizes_ok(B, Hq, Hkv, total_q, D)) return 0;
+  return chunk_workspace_bytes(Hq, Hkv, total_q, D, sms_or_model());
+}
+
+loom_status loom_attn_chunk_paged(const void* q, const void* k_cache, const void* v_cache, const int32_t* block_table,
+                                  const int32_t* cu_seqlens_q, const int32_t* seqlens_k, void* o, float* lse,
+                                  void* workspace, size_t workspace_bytes, int B, int Hq, int Hkv, int total_q,
+                                  int num_pages, int page_size, int max_pages, int kv_layout, int D, int causal,
+                                  float scale, void* stream) {
+  if (B <= 0 || Hq <= 0 || Hkv <= 0 || num_pages <= 0 || page_size <= 0 || max_pages <= 0 || D <= 0 || total_q < 0)
+    return LOOM_ERR_INVALID_ARG;
+  if (!k_cache || !v_cache || !block_table || !cu_seqlens_q || !seqlens_k || (total_q > 0 && (!q || !o)))
+    return LOOM_ERR_INVALID_ARG;
+  if (Hq % Hkv != 0) return LOOM_ERR_INVALID_ARG;
+  if (causal != 0 && causal != 1) return LOOM_ERR_INVALID_ARG;
+  if (!std::isfinite(scale) || scale <= 0.f) return LOOM_ERR_INVALID_ARG;
+  if (kv_layout != kPagedNHD && kv_layout != kPagedHND) return LOOM_ERR_INVALID_ARG;
+  if (!chunk_sizes_ok(B, Hq, Hkv, total_q, D) || !paged_page_size_ok(page_size)) return LOOM_ERR_UNSUPPORTED;
+  if (static_cast<long long>(num_pages) * page_size > 0x7fffffffLL ||
+      static_cast<long long>(num_pages) * Hkv > 0x7fffffffLL ||
+      static_cast<long long>(max_pages) * page_size > 0x7fffffffLL ||
+      static_cast<long long>(B) * max_pages > 0x7fffffffLL)
+    return LOOM_ERR_UNSUPPORTED;
+  if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(o)) return LOOM_ERR_MISALIGNED;
+  if (!aligned4(block_table) || !aligned4(cu_seqlens_q) || !aligned4(seqlens_k) || !aligned4(lse)) return LOOM_ERR_MISALIGNED;
+  if (total_q == 0) return LOOM_OK;
+  if (!workspace || workspace_bytes < chunk_workspace_bytes(Hq, Hkv, total_q, D, sms_or_model())) return LOOM_ERR_WORKSPACE;
+  if (!aligned16(workspace)) return LOOM_ERR_MISALIGNED;
+  KernelCtl ctl;
+  if (!make_ctl(&ctl)) return LOOM_ERR_CUDA;
+  const ChunkArgs a{q, k_cache, v_cache, cu_seqlens_q, seqlens_k, o, lse, workspace, B, Hq, Hkv, total_q, D, causal, scale,
+                    PagedKV{block_table, num_pages, page_size, max_pages, kv_layout}};
+  return launch_chunk_paged(a, ctl, static_cast<cudaStream_t>(stream)) == cudaSuccess ? LOOM_OK : LOOM_ERR_CUDA;
+}
+
+loom_status loom_paged_plan(const int32_t* new_lens, const int32_t* lens, int32_t* block_table, int32_t* free_pages,
+                            const int32_t* free_count, int32_t* free_count_out, int32_t* cu_seqlens, int32_t* seqlens_k,
+                            int32_t* positions, int32_t* slots, int32_t* granted, int B, int T, int num_pages,
+                            int page_size, int max_pages, void* stream) {
+  if (B <= 0 || T < 0 || num_pages <= 0 || page_size <= 0 || max_pages <= 0) return LOOM_ERR_INVALID_ARG;
+  if (!new_lens || !lens || !block_table || !free_pages || !free_count || !free_count_out || !cu_seqlens || !seqlens_k ||
+      !granted || (T > 0 && (!positions || !slots)))
+    return LOOM_ERR_INVALID_ARG;
+  if (B > kMaxPlanB || static_cast<long long>(num_pages) * page_size > 0x7fffffffLL ||
+      static_cast<long long>(max_pages) * page_size > 0x7fffffffLL || static_cast<long long>(B) * max_pages > 0x7fffffffLL)
+    return LOOM_ERR_UNSUPPORTED;
+  for (const void* p : {static_cast<const void*>(new_lens), static_cast<const void*>(lens), static_cast<const void*>(block_table),
+                        static_cast<const void*>(free_pages), static_cast<const void*>(free_count),
+                        static_cast<const void*>(free_count_out), static_cast<const void*>(cu_seqlens),
+                        static_cast<const void*>(seqlens_k), static_cast<const void*>(positions),
+                        static_cast<const void*>(slots), static_cast<const void*>(granted)})
+    if (!aligned4(p)) return LOOM_ERR_MISALIGNED;
+  const PlanArgs a{new_lens, lens, block_table, free_pages, free_count, free_count_out, cu_seqlens, seqlens_k, positions, slots,
+                   granted, B, T, num_pages, page_size, max_pages};
+  return launch_paged_plan(a, static_cast<cudaStream_t>(stream)) == cudaSuccess ? LOOM_OK : LOOM_ERR_CUDA;
+}
+
+namespace {
 // The arguments that the three norm-and-rotation entry points share, checked; *a is filled in.
 loom_status qkv_common(QkvArgs* a, const void* qkv, int64_t qkv_stride, const void* q_weight, const void* k_weight,
                        int weight_type, const float* cos, const float* sin, int table_rows, int rotary_dim, int interleaved,
@@ -464,95 +530,162 @@ bool tables_reach(const int32_t* positions, int T, int seq_len, int table_rows) 
 }
 }  // namespace
 
-loom_status loom_qkv_norm_rope(const void* qkv, int64_t qkv_stride, const void* q_weight, const void* k_weight,
-                               int weight_type, const float* cos, const float* sin, int table_rows, int rotary_dim,
-                               int interleaved, const int32_t* positions, void* q, void* k, void* v, int T, int seq_len,
-                               int Hq, int Hkv, int D, float eps, void* stream) {
-  QkvArgs a{};
-  const loom_status st = qkv_common(&a, qkv, qkv_stride, q_weight, k_weight, weight_type, cos, sin, table_rows, rotary_dim,
-                                    interleaved, positions, T, Hq, Hkv, D, eps);
-  if (st != LOOM_OK) return st;
-  if (seq_len < 0 || (seq_len > 0 && T % seq_len) || (T > 0 && (!q || !k || !v))) return LOOM_ERR_INVALID_ARG;
-  if (!tables_reach(positions, T, seq_len, table_rows)) return LOOM_ERR_INVALID_ARG;
+namespace {
+// The positions of the calls with axes, checked; *a is filled in (after qkv_common).
+loom_status axes_args(QkvArgs* a, int64_t positions_stride, int n_axes, const int* pair_axis) {
+  if (n_axes < 1 || !pair_axis || positions_stride < a->T || (a->T > 0 && !a->positions)) return LOOM_ERR_INVALID_ARG;
+  if (n_axes > kMaxAxes) return LOOM_ERR_UNSUPPORTED;
+  for (int i = 0; i < a->R / 2; ++i) {
+    if (pair_axis[i] < 0 || pair_axis[i] >= n_axes) return LOOM_ERR_INVALID_ARG;
+    a->axis_of[i / 32] |= static_cast<unsigned long long>(pair_axis[i]) << (2 * (i % 32));
+  }
+  a->n_axes = n_axes;
+  a->pos_stride = positions_stride;
+  return LOOM_OK;
+}
+
+loom_status norm_rope_call(QkvArgs& a, void* q, void* k, void* v, int seq_len, void* stream) {
+  if (seq_len < 0 || (seq_len > 0 && a.T % seq_len) || (a.T > 0 && (!q || !k || !v))) return LOOM_ERR_INVALID_ARG;
+  if (!tables_reach(a.positions, a.T, seq_len, a.P)) return LOOM_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(k) || !aligned16(v)) return LOOM_ERR_MISALIGNED;
-  if (T == 0) return LOOM_OK;
+  if (a.T == 0) return LOOM_OK;
   a.q = q;
   a.k = k;
   a.v = v;
   a.q_at.S = a.kv_at.S = seq_len;
-  a.q_at.H = Hq;
-  a.kv_at.H = Hkv;
+  a.q_at.H = a.Hq;
+  a.kv_at.H = a.Hkv;
   return launch_qkv_norm_rope(a, static_cast<cudaStream_t>(stream)) == cudaSuccess ? LOOM_OK : LOOM_ERR_CUDA;
 }
 
-loom_status loom_qkv_norm_rope_cache(const void* qkv, int64_t qkv_stride, const void* q_weight, const void* k_weight,
-                                     int weight_type, const float* cos, const float* sin, int table_rows, int rotary_dim,
-                                     int interleaved, const int32_t* positions, const int32_t* slots, void* q, void* k_cache,
-                                     void* v_cache, int num_pages, int page_size, int kv_layout, int T, int Hq, int Hkv,
-                                     int D, float eps, void* stream) {
-  QkvArgs a{};
-  const loom_status st = qkv_common(&a, qkv, qkv_stride, q_weight, k_weight, weight_type, cos, sin, table_rows, rotary_dim,
-                                    interleaved, positions, T, Hq, Hkv, D, eps);
-  if (st != LOOM_OK) return st;
+loom_status norm_rope_cache_call(QkvArgs& a, const int32_t* slots, void* q, void* k_cache, void* v_cache, int num_pages,
+                                 int page_size, int kv_layout, void* stream) {
   if (num_pages <= 0 || page_size <= 0 || (kv_layout != kPagedNHD && kv_layout != kPagedHND)) return LOOM_ERR_INVALID_ARG;
-  if (!k_cache || !v_cache || (T > 0 && (!q || !positions || !slots))) return LOOM_ERR_INVALID_ARG;
+  if (!k_cache || !v_cache || (a.T > 0 && (!q || !a.positions || !slots))) return LOOM_ERR_INVALID_ARG;
   if (static_cast<long long>(num_pages) * page_size > 0x7fffffffLL) return LOOM_ERR_UNSUPPORTED;
   if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned4(slots)) return LOOM_ERR_MISALIGNED;
-  if (T == 0) return LOOM_OK;
+  if (a.T == 0) return LOOM_OK;
   a.q = q;
   a.k = k_cache;
   a.v = v_cache;
-  a.q_at.H = Hq;
-  a.kv_at.H = Hkv;
+  a.q_at.H = a.Hq;
+  a.kv_at.H = a.Hkv;
   a.kv_at.slots = slots;
   a.kv_at.page = page_size;
   a.kv_at.n_slots = num_pages * page_size;
-  a.kv_at.page_elems = static_cast<long long>(page_size) * Hkv * D;
-  a.kv_at.row_elems = kv_layout == kPagedNHD ? static_cast<long long>(Hkv) * D : D;
-  a.kv_at.head_elems = kv_layout == kPagedNHD ? D : static_cast<long long>(page_size) * D;
+  a.kv_at.page_elems = static_cast<long long>(page_size) * a.Hkv * a.D;
+  a.kv_at.row_elems = kv_layout == kPagedNHD ? static_cast<long long>(a.Hkv) * a.D : a.D;
+  a.kv_at.head_elems = kv_layout == kPagedNHD ? a.D : static_cast<long long>(page_size) * a.D;
   return launch_qkv_norm_rope(a, static_cast<cudaStream_t>(stream)) == cudaSuccess ? LOOM_OK : LOOM_ERR_CUDA;
 }
 
-size_t loom_qkv_norm_rope_bwd_workspace_bytes(int D) { return D == 64 || D == 128 ? qkv_bwd_workspace_bytes(D) : 0; }
-
-loom_status loom_qkv_norm_rope_bwd(const void* dq, const void* dk, const void* dv, const void* qkv, int64_t qkv_stride,
-                                   const void* q_weight, const void* k_weight, int weight_type, const float* cos,
-                                   const float* sin, int table_rows, int rotary_dim, int interleaved,
-                                   const int32_t* positions, void* dqkv, int64_t dqkv_stride, float* dq_weight,
-                                   float* dk_weight, void* workspace, size_t workspace_bytes, int T, int seq_len, int Hq,
-                                   int Hkv, int D, float eps, void* stream) {
-  QkvArgs a{};
-  const loom_status st = qkv_common(&a, qkv, qkv_stride, q_weight, k_weight, weight_type, cos, sin, table_rows, rotary_dim,
-                                    interleaved, positions, T, Hq, Hkv, D, eps);
-  if (st != LOOM_OK) return st;
-  if (seq_len < 0 || (seq_len > 0 && T % seq_len) || (T > 0 && (!dq || !dk || !dv || !dqkv))) return LOOM_ERR_INVALID_ARG;
+loom_status norm_rope_bwd_call(QkvArgs& a, const void* dq, const void* dk, const void* dv, void* dqkv, int64_t dqkv_stride,
+                               float* dq_weight, float* dk_weight, void* workspace, size_t workspace_bytes, int seq_len,
+                               void* stream) {
+  if (seq_len < 0 || (seq_len > 0 && a.T % seq_len) || (a.T > 0 && (!dq || !dk || !dv || !dqkv))) return LOOM_ERR_INVALID_ARG;
   if (!dq_weight || !dk_weight) return LOOM_ERR_INVALID_ARG;
-  if (!tables_reach(positions, T, seq_len, table_rows)) return LOOM_ERR_INVALID_ARG;
-  if (dqkv_stride < (static_cast<int64_t>(Hq) + 2ll * Hkv) * D) return LOOM_ERR_INVALID_ARG;
-  if (Hq + 2ll * Hkv > kMaxBwdHeads) return LOOM_ERR_UNSUPPORTED;
+  if (!tables_reach(a.positions, a.T, seq_len, a.P)) return LOOM_ERR_INVALID_ARG;
+  if (dqkv_stride < (static_cast<int64_t>(a.Hq) + 2ll * a.Hkv) * a.D) return LOOM_ERR_INVALID_ARG;
+  if (a.Hq + 2ll * a.Hkv > kMaxBwdHeads) return LOOM_ERR_UNSUPPORTED;
   if (dqkv_stride % 8 || !aligned16(dq) || !aligned16(dk) || !aligned16(dv) || !aligned16(dqkv) || !aligned4(dq_weight) ||
       !aligned4(dk_weight))
     return LOOM_ERR_MISALIGNED;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (T == 0) {
-    const bool ok = cudaMemsetAsync(dq_weight, 0, D * sizeof(float), s) == cudaSuccess &&
-                    cudaMemsetAsync(dk_weight, 0, D * sizeof(float), s) == cudaSuccess;
+  if (a.T == 0) {
+    const bool ok = cudaMemsetAsync(dq_weight, 0, a.D * sizeof(float), s) == cudaSuccess &&
+                    cudaMemsetAsync(dk_weight, 0, a.D * sizeof(float), s) == cudaSuccess;
     return ok ? LOOM_OK : LOOM_ERR_CUDA;
   }
-  if (!workspace || workspace_bytes < qkv_bwd_workspace_bytes(D)) return LOOM_ERR_WORKSPACE;
+  if (!workspace || workspace_bytes < qkv_bwd_workspace_bytes(a.D)) return LOOM_ERR_WORKSPACE;
   if (!aligned16(workspace)) return LOOM_ERR_MISALIGNED;
   a.q = const_cast<void*>(dq);
   a.k = const_cast<void*>(dk);
   a.v = const_cast<void*>(dv);
   a.q_at.S = a.kv_at.S = seq_len;
-  a.q_at.H = Hq;
-  a.kv_at.H = Hkv;
+  a.q_at.H = a.Hq;
+  a.kv_at.H = a.Hkv;
   a.dqkv = dqkv;
   a.drow_elems = dqkv_stride;
   a.dq_weight = dq_weight;
   a.dk_weight = dk_weight;
   a.partial = static_cast<float*>(workspace);
   return launch_qkv_norm_rope_bwd(a, s) == cudaSuccess ? LOOM_OK : LOOM_ERR_CUDA;
+}
+}  // namespace
+
+loom_status loom_qkv_norm_rope(const void* qkv, int64_t qkv_stride, const void* q_weight, const void* k_weight,
+                               int weight_type, const float* cos, const float* sin, int table_rows, int rotary_dim, int interleaved,
+                               const int32_t* positions,
+                               void* q, void* k, void* v, int T, int seq_len, int Hq, int Hkv, int D, float eps, void* stream) {
+  QkvArgs a{};
+  const loom_status st = qkv_common(&a, qkv, qkv_stride, q_weight, k_weight, weight_type, cos, sin, table_rows, rotary_dim, interleaved,
+                              positions, T, Hq, Hkv, D, eps);
+  return st != LOOM_OK ? st : norm_rope_call(a, q, k, v, seq_len, stream);
+}
+
+loom_status loom_qkv_norm_rope_cache(const void* qkv, int64_t qkv_stride, const void* q_weight, const void* k_weight,
+                                     int weight_type, const float* cos, const float* sin, int table_rows, int rotary_dim, int interleaved,
+                                     const int32_t* positions,
+                                     const int32_t* slots, void* q, void* k_cache, void* v_cache, int num_pages, int page_size,
+                                     int kv_layout, int T, int Hq, int Hkv, int D, float eps, void* stream) {
+  QkvArgs a{};
+  const loom_status st = qkv_common(&a, qkv, qkv_stride, q_weight, k_weight, weight_type, cos, sin, table_rows, rotary_dim, interleaved,
+                              positions, T, Hq, Hkv, D, eps);
+  return st != LOOM_OK ? st : norm_rope_cache_call(a, slots, q, k_cache, v_cache, num_pages, page_size, kv_layout, stream);
+}
+
+size_t loom_qkv_norm_rope_bwd_workspace_bytes(int D) { return D == 64 || D == 128 ? qkv_bwd_workspace_bytes(D) : 0; }
+
+loom_status loom_qkv_norm_rope_bwd(const void* dq, const void* dk, const void* dv, const void* qkv, int64_t qkv_stride,
+                                   const void* q_weight, const void* k_weight,
+                                   int weight_type, const float* cos, const float* sin, int table_rows, int rotary_dim, int interleaved,
+                                   const int32_t* positions,
+                                   void* dqkv, int64_t dqkv_stride, float* dq_weight, float* dk_weight, void* workspace,
+                                   size_t workspace_bytes, int T, int seq_len, int Hq, int Hkv, int D, float eps, void* stream) {
+  QkvArgs a{};
+  const loom_status st = qkv_common(&a, qkv, qkv_stride, q_weight, k_weight, weight_type, cos, sin, table_rows, rotary_dim, interleaved,
+                              positions, T, Hq, Hkv, D, eps);
+  return st != LOOM_OK ? st
+                       : norm_rope_bwd_call(a, dq, dk, dv, dqkv, dqkv_stride, dq_weight, dk_weight, workspace, workspace_bytes,
+                                            seq_len, stream);
+}
+
+loom_status loom_qkv_norm_rope_axes(const void* qkv, int64_t qkv_stride, const void* q_weight, const void* k_weight,
+                                    int weight_type, const float* cos, const float* sin, int table_rows, int rotary_dim, int interleaved,
+                                    const int32_t* positions, int64_t positions_stride, int n_axes, const int* pair_axis,
+                                    void* q, void* k, void* v, int T, int seq_len, int Hq, int Hkv, int D, float eps, void* stream) {
+  QkvArgs a{};
+  loom_status st = qkv_common(&a, qkv, qkv_stride, q_weight, k_weight, weight_type, cos, sin, table_rows, rotary_dim, interleaved,
+                              positions, T, Hq, Hkv, D, eps);
+  if (st == LOOM_OK) st = axes_args(&a, positions_stride, n_axes, pair_axis);
+  return st != LOOM_OK ? st : norm_rope_call(a, q, k, v, seq_len, stream);
+}
+
+loom_status loom_qkv_norm_rope_axes_cache(const void* qkv, int64_t qkv_stride, const void* q_weight, const void* k_weight,
+                                          int weight_type, const float* cos, const float* sin, int table_rows, int rotary_dim,
+                                          int interleaved, const int32_t* positions, int64_t positions_stride, int n_axes, const int* pair_axis,
+                                          const int32_t* slots, void* q, void* k_cache, void* v_cache, int num_pages, int page_size,
+                                          int kv_layout, int T, int Hq, int Hkv, int D, float eps, void* stream) {
+  QkvArgs a{};
+  loom_status st = qkv_common(&a, qkv, qkv_stride, q_weight, k_weight, weight_type, cos, sin, table_rows, rotary_dim, interleaved,
+                              positions, T, Hq, Hkv, D, eps);
+  if (st == LOOM_OK) st = axes_args(&a, positions_stride, n_axes, pair_axis);
+  return st != LOOM_OK ? st : norm_rope_cache_call(a, slots, q, k_cache, v_cache, num_pages, page_size, kv_layout, stream);
+}
+
+loom_status loom_qkv_norm_rope_axes_bwd(const void* dq, const void* dk, const void* dv, const void* qkv, int64_t qkv_stride,
+                                        const void* q_weight, const void* k_weight,
+                                        int weight_type, const float* cos, const float* sin, int table_rows, int rotary_dim, int interleaved,
+                                        const int32_t* positions, int64_t positions_stride, int n_axes, const int* pair_axis,
+                                        void* dqkv, int64_t dqkv_stride, float* dq_weight, float* dk_weight, void* workspace,
+                                        size_t workspace_bytes, int T, int seq_len, int Hq, int Hkv, int D, float eps, void* stream) {
+  QkvArgs a{};
+  loom_status st = qkv_common(&a, qkv, qkv_stride, q_weight, k_weight, weight_type, cos, sin, table_rows, rotary_dim, interleaved,
+                              positions, T, Hq, Hkv, D, eps);
+  if (st == LOOM_OK) st = axes_args(&a, positions_stride, n_axes, pair_axis);
+  return st != LOOM_OK ? st
+                       : norm_rope_bwd_call(a, dq, dk, dv, dqkv, dqkv_stride, dq_weight, dk_weight, workspace, workspace_bytes,
+                                            seq_len, stream);
 }
 
 namespace {

@@ -1,5 +1,5 @@
-// Paged KV cache for Flash Decode: the launch interface between the C ABI (loom_api.cu)
-// and the decode kernels (attn_decode.cu).
+// Paged KV cache: the launch interface between the C ABI (loom_api.cu) and the decode kernels
+// (attn_decode.cu), and a step's bookkeeping (paged_plan.cu).
 #pragma once
 
 #include <cstdint>
@@ -28,5 +28,23 @@ constexpr bool paged_page_size_ok(int p) { return p == 8 || p == 16 || p == 32 |
 
 // a.k / a.v are the caches, a.Skv = max_pages * page_size, a.seqlens is required.
 cudaError_t launch_decode_paged(const DecodeArgs& a, const PagedKV& pk, const KernelCtl& ctl, cudaStream_t stream);
+
+struct PlanArgs {
+  const int32_t* new_lens;    // [B]
+  const int32_t* lens;        // [B]
+  int32_t* block_table;       // [B, max_pages]
+  int32_t* free_pages;        // [num_pages]
+  const int32_t* free_count;  // [1]
+  int32_t* free_count_out;    // [1]
+  int32_t* cu;                // [B + 1]
+  int32_t* seqlens;           // [B]
+  int32_t* positions;         // [T]
+  int32_t* slots;             // [T]
+  int32_t* granted;           // [B]
+  int B, T, num_pages, page, max_pages;
+};
+constexpr int kMaxPlanB = 8192;  // requests whose prefix sums one block's shared memory holds
+
+cudaError_t launch_paged_plan(const PlanArgs& a, cudaStream_t stream);
 
 }  // namespace loom

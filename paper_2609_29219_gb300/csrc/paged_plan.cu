@@ -1,0 +1,194 @@
+// The bookkeeping of a serving step over a paged cache: offsets, positions, slots and new pages from
+// the requests' lengths.
+//
+// With n_b new tokens, len_b cached ones and pages of s rows:
+//     cu_b     = sum_{a<b} max(n_a, 0)
+//     need_b   = ceil((len_b + n_b) / s) - ceil(len_b / s)      (0 where the row or the step has no room)
+//     off_b    = sum_{a<b} need_a;   granted where need_b = 0 or off_b + need_b <= pages that are free
+// The demands granted are a prefix of all demands, so one prefix sum decides them: page k of the step is
+// the k-th from the end of the free list, request b's are off_b .. off_b + need_b - 1.
+//
+// What bounds it is a launch and the chain of latencies after it: lengths, prefix sums, the table's
+// entry, the stores.  So it is one launch of one cluster whose blocks all compute the prefix sums for
+// themselves (in shared memory) and share the tokens and pages; the one cluster barrier lies between the
+// last read of the lengths and the free count and the first write, so that those may be updated in place.
+#include "kernels.h"
+#include "paged.h"
+#include "ptx.cuh"
+
+namespace loom {
+namespace {
+
+constexpr int kThreads = 1024, kClusterBlocks = 8;
+// Requests and tokens that one block deals with alone.
+constexpr int kAloneTokens = 2048, kAloneRequests = 1024;
+
+// Exclusive prefix sums of a and b over the block, and their totals.
+struct Sums {
+  long long a, b, all_a, all_b;
+};
+__device__ __forceinline__ Sums scan(long long a, long long b, long long (*part)[2]) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  long long x = a, y = b;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const long long u = __shfl_up_sync(0xffffffffu, x, d), v = __shfl_up_sync(0xffffffffu, y, d);
+    if (lane >= d) x += u, y += v;
+  }
+  __syncthreads();  // the last call's sums have been read
+  if (lane == 31) part[warp][0] = x, part[warp][1] = y;
+  __syncthreads();
+  long long p = part[lane][0], q = part[lane][1];
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const long long u = __shfl_up_sync(0xffffffffu, p, d), v = __shfl_up_sync(0xffffffffu, q, d);
+    if (lane >= d) p += u, q += v;
+  }
+  const long long before_p = __shfl_sync(0xffffffffu, p, (warp + 31) & 31), before_q = __shfl_sync(0xffffffffu, q, (warp + 31) & 31);
+  return {(warp ? before_p : 0) + x - a, (warp ? before_q : 0) + y - b, __shfl_sync(0xffffffffu, p, 31),
+          __shfl_sync(0xffffffffu, q, 31)};
+}
+
+__device__ __forceinline__ int pages_of(long long rows, int page) { return static_cast<int>((rows + page - 1) / page); }
+
+// The largest b with at[b] <= x, of n + 1 values that never decrease, at[0] <= x < at[n].
+__device__ __forceinline__ int holder(const int* at, int n, int x) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (at[mid] <= x)
+      lo = mid;
+    else
+      hi = mid;
+  }
+  return lo;
+}
+
+enum : uint8_t { kGranted = 1, kOver = 2 };
+
+__global__ void __launch_bounds__(kThreads) paged_plan_kernel(const PlanArgs p) {
+  extern __shared__ int plan_smem[];
+  __shared__ long long part[32][2];
+  const int B = p.B;
+  int* cu = plan_smem;        // [B + 1] first token, p.T at most
+  int* off = cu + B + 1;      // [B + 1] pages that the requests before ask for (one more than there are, at most)
+  int* rel = off + B + 1;     // [B + 1] pages that the requests before give back, as many as there are at most
+  int* len = rel + B + 1;     // [B] cached tokens
+  uint8_t* state = reinterpret_cast<uint8_t*>(len + B);
+  const int blocks = static_cast<int>(cluster_nctarank()), rank = static_cast<int>(cluster_ctarank());
+  const int first = rank * kThreads + static_cast<int>(threadIdx.x), step = blocks * kThreads;
+  const long long rows = static_cast<long long>(p.max_pages) * p.page;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;");
+
+  const int listed = min(max(*p.free_count, 0), p.num_pages);
+  long long tokens = 0, given = 0, asked = 0;
+  for (int b0 = 0; b0 < B; b0 += kThreads) {
+    const int b = b0 + static_cast<int>(threadIdx.x);
+    int n = 0, l = 0;
+    if (b < B) {
+      n = p.new_lens[b];
+      l = static_cast<int>(min(max(static_cast<long long>(p.lens[b]), 0ll), rows));
+    }
+    const Sums s = scan(max(n, 0), n < 0 ? pages_of(l, p.page) : 0, part);
+    const long long end = tokens + s.a + max(n, 0);
+    const bool fits = n >= 0 && l + static_cast<long long>(n) <= rows && end <= p.T;
+    const int need = fits && n > 0 ? pages_of(l + static_cast<long long>(n), p.page) - pages_of(l, p.page) : 0;
+    const Sums t = scan(need, 0, part);
+    if (b < B) {
+      cu[b] = static_cast<int>(min(tokens + s.a, static_cast<long long>(p.T)));
+      rel[b] = static_cast<int>(min(given + s.b, static_cast<long long>(p.num_pages)));
+      off[b] = static_cast<int>(min(asked + t.a, static_cast<long long>(p.num_pages) + 1));
+      len[b] = l;
+      // (whether the pages reach it is known when all that are given back are)
+      state[b] = n < 0 ? kOver : fits ? (need == 0 || asked + t.a + need <= p.num_pages ? kGranted : 0) : 0;
+    }
+    tokens += s.all_a;
+    given += s.all_b;
+    asked += t.all_a;
+  }
+  if (threadIdx.x == 0) {
+    cu[B] = static_cast<int>(min(tokens, static_cast<long long>(p.T)));
+    rel[B] = static_cast<int>(min(given, static_cast<long long>(p.num_pages)));
+    off[B] = static_cast<int>(min(asked, static_cast<long long>(p.num_pages) + 1));
+  }
+  __syncthreads();
+  const int total = static_cast<int>(min(listed + given, static_cast<long long>(p.num_pages)));
+  // Where the demands pass the total: off is sorted, and every demand before the first that does is met.
+  int taken = off[B];
+  if (taken > total) taken = off[holder(off, B, total)];
+  cluster_sync_all();  // every block has read what may be updated in place
+
+  // entry i of the free list with the pages given back at its end
+  const auto listed_page = [&](int i) {
+    if (i < listed) return p.free_pages[i];
+    const int b = holder(rel, B, i - listed);
+    return p.block_table[static_cast<size_t>(b) * p.max_pages + (i - listed - rel[b])];
+  };
+  const auto fresh_page = [&](int k) { return listed_page(total - 1 - k); };
+  const auto is_granted = [&](int b) { return state[b] == kGranted && (off[b + 1] == off[b] || off[b + 1] <= total); };
+
+  for (int b = first; b < B; b += step) {
+    const bool g = is_granted(b);
+    const int n = cu[b + 1] - cu[b];
+    p.cu[b] = cu[b];
+    p.seqlens[b] = state[b] == kOver ? 0 : len[b] + (g ? n : 0);
+    p.granted[b] = g ? n : 0;
+  }
+  if (first == 0) {
+    p.cu[B] = cu[B];
+    *p.free_count_out = total - taken;
+  }
+  for (int k = first; k < taken; k += step) {
+    const int b = holder(off, B, k);
+    p.block_table[static_cast<size_t>(b) * p.max_pages + pages_of(len[b], p.page) + (k - off[b])] = fresh_page(k);
+  }
+  for (int i = listed + first; i < total - taken; i += step) p.free_pages[i] = listed_page(i);
+  for (int t = first; t < p.T; t += step) {
+    int pos = 0, slot = -1;
+    if (t < cu[B]) {
+      const int b = holder(cu, B, t);
+      if (is_granted(b)) {
+        pos = len[b] + (t - cu[b]);
+        const int j = pos / p.page, held = pages_of(len[b], p.page);
+        const int at = j < held ? p.block_table[static_cast<size_t>(b) * p.max_pages + j] : fresh_page(off[b] + j - held);
+        if (at >= 0 && at < p.num_pages) slot = at * p.page + pos % p.page;
+      }
+    }
+    p.positions[t] = pos;
+    p.slots[t] = slot;
+  }
+}
+
+}  // namespace
+
+cudaError_t launch_paged_plan(const PlanArgs& a, cudaStream_t stream) {
+  const size_t smem = (4 * static_cast<size_t>(a.B) + 3) * sizeof(int) + a.B;
+  static_assert((4 * kMaxPlanB + 3) * sizeof(int) + kMaxPlanB <= 200 * 1024, "prefix sums in shared memory");
+  static PerDeviceOnce configured;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (!configured.run(dev, [] {
+        return cudaFuncSetAttribute(paged_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                    (4 * kMaxPlanB + 3) * sizeof(int) + kMaxPlanB) == cudaSuccess;
+      }))
+    return cudaErrorInvalidValue;
+  cudaLaunchConfig_t cfg = {};
+  const int blocks = a.T <= kAloneTokens && a.B <= kAloneRequests ? 1 : kClusterBlocks;
+  cfg.gridDim = dim3(static_cast<unsigned>(blocks));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = static_cast<unsigned>(blocks);
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, paged_plan_kernel, a);
+}
+
+}  // namespace loom

@@ -27,7 +27,10 @@ struct QkvArgs {
   int weights_f32;       // the weights are fp32 (else bf16)
   const float* cos;      // [P, R / 2]
   const float* sin;      // [P, R / 2]
-  const int32_t* positions;  // [T], or null: t (S = 0) or t % S
+  const int32_t* positions;  // [T], or null: t (S = 0) or t % S; with axes [n_axes, T]
+  int n_axes;                // 0: one position a token; else pair i turns by that of its axis
+  long long pos_stride;      // axes: from one axis' positions to the next's
+  unsigned long long axis_of[2];  // axes: two bits for each pair of a head
   int T, Hq, Hkv, D, R, P, interleaved;
   float eps;
   QkvPlace q_at, kv_at;
@@ -38,6 +41,8 @@ struct QkvArgs {
   float *dq_weight, *dk_weight;  // [D]
   float* partial;        // [blocks][2][D] (workspace)
 };
+
+constexpr int kMaxAxes = 4;  // what two bits tell apart
 
 // Heads (Hq + 2 Hkv) of a token at most in the backward pass.
 constexpr int kMaxBwdHeads = 16384;

@@ -20,6 +20,9 @@
 // A head is D / 8 lanes of 16 bytes; a warp takes a unit, up to UNR steps of 256 / D heads of one
 // kind (query, key or value) of a token, and issues the loads of all of them before it uses the
 // first.
+//
+// With positions on several axes (AXES) pair i takes its angle from the row of its axis' position:
+// only where the angles come from differs.
 #include <cuda_bf16.h>
 
 #include <type_traits>
@@ -50,6 +53,9 @@ struct QkvParams {
   int w_f32;
   const float *cos, *sin;
   const int32_t* pos;
+  int n_axes;
+  long long pos_stride;
+  unsigned long long axis_of[2];
   int T, Hq, Hkv, R, P;
   int q_units, kv_units;  // units of a token's query heads, of its key heads (and of its value heads)
   long long units;        // of all tokens
@@ -133,6 +139,25 @@ __device__ __forceinline__ int position(const QkvParams& p, int t) {
   return min(max(pos, 0), p.P - 1);
 }
 
+// The positions of a token whose pairs turn on several axes.
+struct AxisPositions {
+  int at[kMaxAxes];
+};
+__device__ __forceinline__ AxisPositions axis_positions(const QkvParams& p, int t) {
+  AxisPositions a;
+#pragma unroll
+  for (int x = 0; x < kMaxAxes; ++x)
+    a.at[x] = x < p.n_axes ? min(max(__ldg(p.pos + x * p.pos_stride + t), 0), p.P - 1) : 0;
+  return a;
+}
+// The axis of pair i.
+__device__ __forceinline__ int axis_of(const QkvParams& p, int i) {
+  return static_cast<int>((i < 32 ? p.axis_of[0] : p.axis_of[1]) >> (2 * (i & 31))) & 3;
+}
+__device__ __forceinline__ int position_on(const AxisPositions& a, int axis) {
+  return axis & 2 ? (axis & 1 ? a.at[3] : a.at[2]) : (axis & 1 ? a.at[1] : a.at[0]);
+}
+
 // The angles of the eight values from i0 on, from their position's R / 2 = half cosines and sines:
 // y_i = z_i c_i + partner(z)_i s_i, with the pair's sign in s (BWD: of the transposed rotation).
 template <bool INTER, bool BWD>
@@ -159,6 +184,43 @@ __device__ __forceinline__ void angles(const float* cos, const float* sin, int i
       c[4 * h] = a.x, c[4 * h + 1] = a.y, c[4 * h + 2] = a.z, c[4 * h + 3] = a.w;
       s[4 * h] = sign * b.x, s[4 * h + 1] = sign * b.y, s[4 * h + 2] = sign * b.z, s[4 * h + 3] = sign * b.w;
     }
+  }
+}
+
+// angles<INTER, false> where the pairs turn on several axes.  A lane reads its pairs' columns from the
+// rows of those axes that it has, 16 bytes at a time, and keeps each pair's own.  GB300, 8192 tokens H32/8 D 128, three axes
+// in turns: AXES_VECTOR_US; a value at a time AXES_SCALAR_US.
+template <bool INTER>
+__device__ __forceinline__ void axis_angles(const QkvParams& p, const AxisPositions& at, int i0, float* c, float* s) {
+  constexpr int N = INTER ? 4 : 8;  // pairs
+  const int half = p.R / 2;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) c[i] = 1.f, s[i] = 0.f;
+  if (i0 >= p.R) return;
+  const bool low = INTER || i0 < half;
+  const int first = INTER ? i0 / 2 : low ? i0 : i0 - half;
+  const uint32_t axes = static_cast<uint32_t>((first < 32 ? p.axis_of[0] : p.axis_of[1]) >> (2 * (first & 31)));
+  float cc[N], ss[N];
+#pragma unroll
+  for (int x = 0; x < kMaxAxes; ++x) {
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < N; ++i) any |= (axes >> (2 * i) & 3) == x;
+    if (!any) continue;
+    const long long row = static_cast<long long>(at.at[x]) * half + first;
+#pragma unroll
+    for (int h = 0; h < N / 4; ++h) {
+      const float4 a = __ldg(reinterpret_cast<const float4*>(p.cos + row) + h), b = __ldg(reinterpret_cast<const float4*>(p.sin + row) + h);
+      const float av[4] = {a.x, a.y, a.z, a.w}, bv[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if ((axes >> (2 * (4 * h + i)) & 3) == x) cc[4 * h + i] = av[i], ss[4 * h + i] = bv[i];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    c[i] = cc[INTER ? i / 2 : i];
+    s[i] = INTER ? (i & 1 ? ss[i / 2] : -ss[i / 2]) : low ? -ss[i % N] : ss[i % N];
   }
 }
 
@@ -199,7 +261,7 @@ __device__ __forceinline__ __nv_bfloat16* place(const QkvParams& p, const Unit& 
   return base + page * at.page_elems + static_cast<long long>(slot - page * at.page) * at.row_elems;
 }
 
-template <int D, bool INTER, int UNR>
+template <int D, bool INTER, int UNR, bool AXES>
 __global__ void __launch_bounds__(kWarps * 32) qkv_norm_rope_kernel(const QkvParams p) {
   constexpr int LPH = D / 8, RPW = 32 / LPH;
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -228,8 +290,12 @@ __global__ void __launch_bounds__(kWarps * 32) qkv_norm_rope_kernel(const QkvPar
   uint64_t a[4], b[4];
   {
     float c[8], s[8], w[8], wp[8];
-    const long long row = static_cast<long long>(position(p, u.t)) * (p.R / 2);
-    angles<INTER, false>(p.cos + row, p.sin + row, i0, p.R / 2, c, s);
+    if constexpr (AXES) {
+      axis_angles<INTER>(p, axis_positions(p, u.t), i0, c, s);
+    } else {
+      const long long row = static_cast<long long>(position(p, u.t)) * (p.R / 2);
+      angles<INTER, false>(p.cos + row, p.sin + row, i0, p.R / 2, c, s);
+    }
     load_weight(p, u.kind, i0, w);
     load_weight(p, u.kind, 8 * (src % LPH), wp);
 #pragma unroll
@@ -269,7 +335,11 @@ __device__ __forceinline__ void copy16(void* dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
 }
 
-template <int D, bool INTER, int UNR>
+__device__ __forceinline__ void copy4(void* dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+}
+
+template <int D, bool INTER, int UNR, bool AXES>
 __global__ void __launch_bounds__(kWarps * 32, kBwdBlocksPerSm) qkv_norm_rope_bwd_kernel(const QkvParams p) {
   constexpr int LPH = D / 8, RPW = 32 / LPH;
   extern __shared__ __align__(16) uint8_t bwd_smem[];
@@ -296,8 +366,15 @@ __global__ void __launch_bounds__(kWarps * 32, kBwdBlocksPerSm) qkv_norm_rope_bw
     }
   }
   const auto after = [&](int t) { return p.T - t > tokens ? t + tokens : p.T; };
+  using Position = std::conditional_t<AXES, AxisPositions, int>;
+  const auto position_of = [&](int t) -> Position {
+    if constexpr (AXES)
+      return axis_positions(p, t);
+    else
+      return position(p, t);
+  };
   // requests token t, whose position is pos
-  const auto request = [&](BwdStage<UNR>& st, int t, int pos) {
+  const auto request = [&](BwdStage<UNR>& st, int t, const Position& pos) {
     Unit v = u;
     v.t = t;
     long long head;
@@ -311,21 +388,31 @@ __global__ void __launch_bounds__(kWarps * 32, kBwdBlocksPerSm) qkv_norm_rope_bw
         if (u.kind != kValue) copy16(&st.x[s][lane], x + s * RPW * D);
       }
     if (u.kind != kValue && 4 * (lane & 15) < half) {
-      const float* from = (lane < 16 ? p.cos : p.sin) + static_cast<long long>(pos) * half + 4 * (lane & 15);
-      copy16((lane < 16 ? st.cos : st.sin) + 4 * (lane & 15), from);
+      const float* table = lane < 16 ? p.cos : p.sin;
+      float* to = (lane < 16 ? st.cos : st.sin) + 4 * (lane & 15);
+      if constexpr (AXES) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int pair = 4 * (lane & 15) + i;
+          copy4(to + i, table + static_cast<long long>(position_on(pos, axis_of(p, pair))) * half + pair);
+        }
+      } else {
+        copy16(to, table + static_cast<long long>(pos) * half + 4 * (lane & 15));
+      }
     }
   };
-  int to = u.t, ahead = 0, now = 0, free = 0;  // the token requested next, its position; stages
+  int to = u.t, now = 0, free = 0;  // the token requested next; stages
+  Position ahead{};                 // its position
   const auto request_next = [&] {
     if (to < p.T) {
       request(stages[free], to, ahead);
       to = after(to);
-      if (to < p.T) ahead = position(p, to);
+      if (to < p.T) ahead = position_of(to);
     }
     free = free + 1 < kBwdStages ? free + 1 : 0;
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  if (to < p.T) ahead = position(p, to);
+  if (to < p.T) ahead = position_of(to);
 #pragma unroll
   for (int i = 0; i + 1 < kBwdStages; ++i) request_next();
   for (; u.t < p.T; u.t = after(u.t), now = now + 1 < kBwdStages ? now + 1 : 0) {
@@ -448,6 +535,10 @@ QkvParams params_of(const QkvArgs& a, int unroll) {
   p.cos = a.cos;
   p.sin = a.sin;
   p.pos = a.positions;
+  p.n_axes = a.n_axes;
+  p.pos_stride = a.pos_stride;
+  p.axis_of[0] = a.axis_of[0];
+  p.axis_of[1] = a.axis_of[1];
   p.T = a.T;
   p.Hq = a.Hq;
   p.Hkv = a.Hkv;
@@ -480,11 +571,12 @@ cudaError_t launch_fwd_u(const QkvArgs& a, cudaStream_t stream) {
   const long long blocks = (p.units + warps - 1) / warps;
   if (blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
   const int g = static_cast<int>(blocks);
-  return a.interleaved ? launch(qkv_norm_rope_kernel<D, true, UNR>, g, warps * 32, 0, stream, p)
-                       : launch(qkv_norm_rope_kernel<D, false, UNR>, g, warps * 32, 0, stream, p);
+  const auto kernel = a.n_axes ? (a.interleaved ? qkv_norm_rope_kernel<D, true, UNR, true> : qkv_norm_rope_kernel<D, false, UNR, true>)
+                               : (a.interleaved ? qkv_norm_rope_kernel<D, true, UNR, false> : qkv_norm_rope_kernel<D, false, UNR, false>);
+  return launch(kernel, g, warps * 32, 0, stream, p);
 }
 
-template <int D, int UNR>
+template <int D, int UNR, bool AXES>
 cudaError_t launch_bwd_u(const QkvArgs& a, cudaStream_t stream) {
   const QkvParams p = params_of(a, UNR);
   // blocks whose warps are a multiple of a token's units (unless that is more than there is room for),
@@ -497,7 +589,7 @@ cudaError_t launch_bwd_u(const QkvArgs& a, cudaStream_t stream) {
   const int most = kMaxBwdBlocks / unit, g = static_cast<int>(need < most ? need : most) * unit;
   constexpr size_t smem = kBwdStages * kWarps * sizeof(BwdStage<UNR>);
   static_assert(smem >= kWarps * 2 * D * sizeof(float), "the stages hold the sums");
-  const auto inter = qkv_norm_rope_bwd_kernel<D, true, UNR>, split = qkv_norm_rope_bwd_kernel<D, false, UNR>;
+  const auto inter = qkv_norm_rope_bwd_kernel<D, true, UNR, AXES>, split = qkv_norm_rope_bwd_kernel<D, false, UNR, AXES>;
   static PerDeviceOnce configured;
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
@@ -528,7 +620,9 @@ cudaError_t launch_fwd_d(const QkvArgs& a, cudaStream_t stream) {
 }
 template <int D>
 cudaError_t launch_bwd_d(const QkvArgs& a, cudaStream_t stream) {
-  return with_steps(a, [&](auto n) { return launch_bwd_u<D, decltype(n)::value>(a, stream); });
+  return with_steps(a, [&](auto n) {
+    return a.n_axes ? launch_bwd_u<D, decltype(n)::value, true>(a, stream) : launch_bwd_u<D, decltype(n)::value, false>(a, stream);
+  });
 }
 
 }  // namespace
