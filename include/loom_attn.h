@@ -585,7 +585,8 @@ const char* loom_status_string(loom_status status);
  * loom_debug_inject: 0 = off; 1 = the decode split kernel's loader skips the copy of
  *   its second stage; 2 = the prefill kernel's loader skips its second K tile; 3 = the
  *   GEMM loader skips its third stage (of each CTA's K range); 4 = the attention backward
- *   kernel's loader stops before its second query tile.  The
+ *   kernel's loader stops before its second query tile; 5 = the chunk attention's loader skips
+ *   its second K tile (of each CTA).  The
  *   waits on the skipped data then expire, the kernel unwinds and the next
  *   loom_attn_check_error returns LOOM_ERR_TIMEOUT.  Host-side switch; no fault.
  */
