@@ -11,14 +11,16 @@
 // i of a tile is token i / gt, head i % gt of the plane, TQ = 128 / gt tokens a tile, so that single tokens
 // and drafts fill as few tiles as they can and a key is read once for all of them.  A unit of work is a
 // pair of query tiles (256 rows; the second may be missing) of a plane of a sequence, against the keys
-// that it sees.
+// that it sees.  Two tiles alternate on the tensor pipe, each over all of the keys; a single tile's
+// even key tiles go one tile's way and its odd ones the other's, whose sums are joined in the end (O in
+// TMEM, m and l through shared memory), so that its steps overlap too.
 //
 // Dealing.  All units lie on one line, in order, each as long as its modelled cost: kUnitCost and a
 // weight per key.  CTA c of G takes the stretch [W c / G, W (c + 1) / G) of the line's W, cut to
 // whole key tiles of the units it starts and ends in.  So the CTAs finish together for any mixture of
-// prompts and single tokens, no list of items is made or stored, and nothing depends on timing: the
-// offsets' prefix sum and a binary search give each CTA its first unit.  A unit that lies in one stretch
-// is finished there.  The pieces of a cut one go to the workspace in 32 bits; the last warp to bring its
+// prompts and single tokens, no list of items is made in memory, and nothing depends on timing: the
+// sequences' prefix sum and a binary search give each CTA its first unit, and one warp walks on from there,
+// a few units ahead of the others.  A unit that lies in one stretch is finished there.  The pieces of a cut one go to the workspace in 32 bits; the last warp to bring its
 // rows' piece joins all of them in the pieces' order.
 //
 // What bounds it: many queries, the tensor cores, as the prefill kernel, whose step this one repeats
@@ -26,7 +28,6 @@
 #include <cuda.h>
 #include <cuda_bf16.h>
 
-#include <atomic>
 #include <chrono>
 #include <mutex>
 
@@ -46,20 +47,22 @@ constexpr int kKeyCost2 = 8, kKeyCost1 = 6, kUnitCost = 1024;
 template <int D>
 struct ChunkCfg {
   static constexpr int BM = 128, BN = 128;
-  static constexpr int NSLOT = D == 128 ? 4 : 10;   // K/V ring slots
-  static constexpr int NKE = NSLOT / 2;
-  static constexpr int THREADS = 320;               // 8 softmax warps, loader, MMA
+  static constexpr int NR = D == 128 ? 2 : 5;       // slots of the K ring, and of the V ring
+  static constexpr int THREADS = 384;               // 8 softmax warps, K loader, MMA, V loader, scheduler
+  static constexpr int NREC = 4;                    // units that the scheduler is ahead
   static constexpr int NBOX = D / 64;               // 128-byte swizzled boxes per row of a tile
   static constexpr uint32_t BOX_BYTES = BM * 128;
   static constexpr uint32_t TILE_BYTES = NBOX * BOX_BYTES;
   static constexpr uint32_t Q_OFF = 0;
   static constexpr uint32_t RING_OFF = 2 * TILE_BYTES;
-  static constexpr uint32_t STG_OFF = RING_OFF + NSLOT * TILE_BYTES;  // 4 KB for each softmax warp
-  static constexpr uint32_t BAR_OFF = STG_OFF + 8 * 4096;
-  // q[2], qe[2], full[NSLOT], empty[NKE], s[2], p[2][2], o[2], oe[2], drain
-  static constexpr int NBAR = 4 + NSLOT + NKE + 2 + 4 + 2 + 2 + 1;
-  static constexpr uint32_t START_OFF = BAR_OFF + NBAR * 8;  // where this CTA's stretch begins (Start)
-  static constexpr uint32_t SUM_OFF = START_OFF + 32;        // the scan's sums, one per warp
+  static constexpr uint32_t STG_OFF = RING_OFF + 2 * NR * TILE_BYTES;  // 4 KB for each softmax warp
+  static constexpr uint32_t ML_OFF = STG_OFF + 8 * 4096;               // [BM] (m, l): see bar_ml
+  static constexpr uint32_t BAR_OFF = ML_OFF + BM * 8;
+  // q[2], qe[2], full[2][NR], empty[2][NR], s[2], p[2][2], o[2], oe[2], ml, mle, drain, rec[NREC], rece[NREC]
+  static constexpr int NBAR = 4 + 4 * NR + 2 + 4 + 2 + 2 + 3 + 2 * NREC;
+  static constexpr uint32_t REC_OFF = (BAR_OFF + NBAR * 8 + 15) / 16 * 16;  // [NREC] Item
+  static constexpr uint32_t LINE_OFF = REC_OFF + NREC * 80;                 // Line, and the Walk to its start
+  static constexpr uint32_t SUM_OFF = LINE_OFF + 128;                       // the scan's sums, one per warp
   static constexpr uint32_t TMEM_PTR_OFF = SUM_OFF + 16 * 8;
   static constexpr uint32_t ABORT_OFF = TMEM_PTR_OFF + 8;
   static constexpr uint32_t BYTES = ABORT_OFF + 16 + 1024;  // + alignment slack
@@ -76,7 +79,7 @@ struct ChunkParams {
   float* part;                // [2 G][groups][D / 4][32] float4: the rows of cut units' pieces
   float2* part_ml;            // [2 G][groups][32]: their (m, l); l < 0: no keys, no row
   unsigned long long* count;  // [G][8]: pieces of a 32-row group that have come
-  unsigned long long tag;     // of this launch, in the upper 48 bits of a count
+  unsigned long long tag;     // of this process, in the upper 48 bits of a count
   int groups;                 // 32-row groups of a unit that the workspace has room for
   int B, Hq, total_q, causal;
   int gt, planes, planes_per_kv, tq;  // heads of a plane, planes of a token, tokens of a tile
@@ -86,6 +89,11 @@ struct ChunkParams {
 };
 
 // ---------------------------------------------------------------- the line of work
+// a / b of numbers that are not negative: nearly always below 2^32, where it takes a fifth of the time.
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+  if (((a | b) >> 32) == 0) return static_cast<unsigned>(a) / static_cast<unsigned>(b);
+  return a / b;
+}
 struct Seq {
   int qb, sq, skv, pairs;  // first token, tokens, keys, pairs of query tiles
 };
@@ -96,7 +104,7 @@ __device__ __forceinline__ Seq load_seq(const ChunkParams& p, int b) {
   s.sq = min(max(p.cu_q[b + 1], s.qb), p.total_q) - s.qb;
   const long long cap = static_cast<long long>(p.max_pages) * p.page;
   s.skv = static_cast<int>(min(max(static_cast<long long>(p.seqlens[b]), 0ll), cap));
-  s.pairs = static_cast<int>((static_cast<long long>(s.sq) + 2 * p.tq - 1) / (2 * p.tq));
+  s.pairs = static_cast<int>((static_cast<unsigned>(s.sq) + 2u * p.tq - 1) / (2u * p.tq));
   return s;
 }
 // Keys that the queries before token `end` of a sequence see.
@@ -116,7 +124,7 @@ __device__ __forceinline__ long long cost_before(const ChunkParams& p, const Seq
   if (p.causal) {
     // pair j sees off + step (j + 1) keys, from the first j where that is positive
     const long long step = 2ll * p.tq, off = static_cast<long long>(s.skv) - s.sq;
-    const long long j0 = off >= 0 ? 0 : -off / step;
+    const long long j0 = off >= 0 ? 0 : quotient(-off, step);
     const long long n = i - j0;
     keys = n > 0 ? n * off + step * ((j0 + 1 + i) * n / 2) : 0;
   }
@@ -125,38 +133,47 @@ __device__ __forceinline__ long long cost_before(const ChunkParams& p, const Seq
 __device__ __forceinline__ long long plane_cost(const ChunkParams& p, const Seq& s) {
   return s.pairs ? cost_before(p, s, s.pairs - 1) + unit_cost(p, s, s.pairs - 1) : 0;
 }
-// The line's place where CTA c of G begins.
-__device__ __forceinline__ long long bound_of(long long W, int G, int c) {
-  return W / G * c + static_cast<int>(W % G) * c / G;
-}
+// The line, W long and dealt to G CTAs, and this CTA's stretch of it.
+struct Line {
+  long long W, x0, x1;
+  long long each;  // W / G
+  int rest, G;     // W % G
+  __device__ __forceinline__ void set(long long length, int ctas) {
+    W = length;
+    G = ctas;
+    each = quotient(W, G);
+    rest = static_cast<int>(W - each * G);
+  }
+  // Where CTA c's stretch begins.
+  __device__ __forceinline__ long long bound(int c) const { return each * c + static_cast<unsigned>(rest * c) / static_cast<unsigned>(G); }
+};
 // Key tiles of a unit that lie before the place d > 0 behind its beginning.
 __device__ __forceinline__ int tiles_before(long long d, int key, int tiles) {
   d -= kUnitCost;
   if (d <= 0) return 0;
-  const long long t = (d + key * 128 - 1) / (key * 128);
+  const unsigned long long u = static_cast<unsigned long long>(d);
+  const long long t = key == kKeyCost2 ? (u + kKeyCost2 * 128 - 1) / (kKeyCost2 * 128) : (u + kKeyCost1 * 128 - 1) / (kKeyCost1 * 128);
   return t < tiles ? static_cast<int>(t) : tiles;
 }
 
-// What a CTA knows of its stretch.
-struct Line {
-  long long W, x0, x1;
-  int G;
-};
 // A place on the line: unit `pair` of a plane of sequence b, which begins at `at`.
 struct Walk {
   int b, plane, pair;
   long long at;
   Seq s;
 };
-// A unit, or the piece of it that this CTA has.
+// A unit, or the piece of it that this CTA has; shared memory's record of it is 80 bytes.
 struct Item {
   int b, plane, t0, qb, sq, skv;  // t0: its first token within the sequence
+  int lo, n;                      // first key tile and key tiles here (n < 0: there are no more items)
+  int n0, n1;                     // of these, the steps of S, P and O number 0 and number 1
+  int tiles;                      // all its key tiles
+  int two;                        // it has two query tiles
+  int key, pad;                   // a key's cost
   long long at, cost;             // its place on the line
-  int key, tiles;                 // a key's cost, all its key tiles
-  int lo, n0, n;                  // first key tile, key tiles of tile 0 and of tile 1 here
-  bool two;                       // it has a tile 0 (a single tile is tile 1)
   __device__ __forceinline__ bool cut() const { return n < tiles; }
 };
+static_assert(sizeof(Item) == 72, "fits its record");
 
 // The CTA's next piece, and the walk behind it; false past the stretch's end.
 __device__ __forceinline__ bool next_item(const ChunkParams& p, const Line& ln, Walk& w, Item& it) {
@@ -177,7 +194,8 @@ __device__ __forceinline__ bool next_item(const ChunkParams& p, const Line& ln, 
     it.lo = ln.x0 > it.at ? tiles_before(ln.x0 - it.at, it.key, it.tiles) : 0;
     const int hi = ln.x1 < it.at + it.cost ? tiles_before(ln.x1 - it.at, it.key, it.tiles) : it.tiles;
     it.n = hi - it.lo;
-    it.n0 = it.two ? max(0, min(hi, (keys_until(p, w.s, it.t0 + p.tq) + 127) / 128) - it.lo) : 0;
+    it.n0 = it.two ? max(0, min(hi, (keys_until(p, w.s, it.t0 + p.tq) + 127) / 128) - it.lo) : (it.n + 1) / 2;
+    it.n1 = it.two ? it.n : it.n / 2;
     w.at += it.cost;
     if (++w.pair == w.s.pairs) {
       w.pair = 0;
@@ -195,25 +213,64 @@ __device__ __forceinline__ bool next_item(const ChunkParams& p, const Line& ln, 
   return false;
 }
 
-// The pieces of a cut unit: calls f(slot) with each piece's place in the workspace, in order, and returns
-// the CTA that has the first.  The first piece is its CTA's last unit, the others' are their CTAs' first.
-template <class F>
-__device__ __forceinline__ int for_pieces(const Line& ln, const Item& it, F f) {
-  int c = min(ln.G - 1, static_cast<int>(static_cast<double>(it.at) / static_cast<double>(ln.W) * ln.G));
-  while (c > 0 && bound_of(ln.W, ln.G, c) > it.at) --c;
-  while (c + 1 < ln.G && bound_of(ln.W, ln.G, c + 1) <= it.at) ++c;
-  int first = -1;
-  for (int lo = 0; lo < it.tiles && c < ln.G; ++c) {
-    const long long end = c + 1 < ln.G ? bound_of(ln.W, ln.G, c + 1) : ln.W;
-    const int hi = end < it.at + it.cost ? tiles_before(end - it.at, it.key, it.tiles) : it.tiles;
-    if (hi > lo) {
-      f(lo == 0 ? 2 * c + 1 : 2 * c);
-      if (first < 0) first = c;
-    }
-    lo = hi;
+// The walk to this CTA's first unit: sequence b begins at `at`.
+__device__ __forceinline__ Walk walk_from(const ChunkParams& p, const Line& ln, int b, long long at) {
+  Walk w;
+  w.b = b;
+  w.s = load_seq(p, b);
+  const long long plane = plane_cost(p, w.s);
+  w.plane = static_cast<int>(quotient(ln.x0 - at, plane));
+  const long long r = ln.x0 - at - w.plane * plane;
+  int lo = 0, hi = w.s.pairs;  // the last pair that begins at r or before
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (cost_before(p, w.s, mid) <= r)
+      lo = mid;
+    else
+      hi = mid;
   }
-  return first;
+  w.pair = lo;
+  w.at = at + w.plane * plane + cost_before(p, w.s, lo);
+  return w;
 }
+
+// The pieces of a cut unit, found by a whole warp: the first CTA that has one (its last unit; the others' pieces
+// are their CTAs' first), and which of the 32 CTAs from `from` on have one.
+__device__ __forceinline__ int first_cta(const Line& ln, const Item& it) {
+  int c = min(ln.G - 1, static_cast<int>(static_cast<float>(it.at) / static_cast<float>(ln.W) * ln.G));
+  while (c > 0 && ln.bound(c) > it.at) --c;
+  while (c + 1 < ln.G && ln.bound(c + 1) <= it.at) ++c;
+  // (it may begin in a stretch that holds none of its key tiles)
+  while (c + 1 < ln.G && tiles_before(ln.bound(c + 1) - it.at, it.key, it.tiles) == 0) ++c;
+  return c;
+}
+__device__ __forceinline__ uint32_t piece_ctas(const Line& ln, const Item& it, int from) {
+  const int c = from + static_cast<int>(threadIdx.x & 31);
+  bool has = false;
+  if (c < ln.G) {
+    const long long begin = ln.bound(c) - it.at, end = (c + 1 < ln.G ? ln.bound(c + 1) : ln.W) - it.at;
+    const int lo = begin > 0 ? tiles_before(begin, it.key, it.tiles) : 0;
+    const int hi = end < it.cost ? tiles_before(end, it.key, it.tiles) : it.tiles;
+    has = end > 0 && begin < it.cost && lo < hi;
+  }
+  return __ballot_sync(0xffffffffu, has);
+}
+// The pieces' places in the workspace, one after another (-1 after the last); the whole warp asks.
+struct Pieces {
+  int first, from;
+  uint32_t ctas;  // of the 32 before `from` that are yet to come
+  __device__ __forceinline__ explicit Pieces(int first_cta) : first(first_cta), from(first_cta), ctas(0) {}
+  __device__ __forceinline__ int next(const Line& ln, const Item& it) {
+    while (!ctas) {
+      if (from >= ln.G || ln.bound(from) >= it.at + it.cost) return -1;
+      ctas = piece_ctas(ln, it, from);
+      from += 32;
+    }
+    const int c = from - 33 + __ffs(static_cast<int>(ctas));
+    ctas &= ctas - 1;
+    return c == first ? 2 * c + 1 : 2 * c;
+  }
+};
 
 // ---------------------------------------------------------------- softmax
 // One online-softmax step of one query row (this thread's TMEM lane) over a 128-key tile of S in TMEM at
@@ -301,6 +358,10 @@ __device__ __forceinline__ bool chunk_step(uint32_t s_tm, uint32_t o_tm, uint32_
   return true;
 }
 
+__device__ __forceinline__ void st_shared_f2(uint32_t addr, float a, float b) {
+  asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(addr), "f"(a), "f"(b) : "memory");
+}
+
 // 64 columns of this warp's 32 rows, packed bf16 pairs of each lane's own row in w, to the rows' places in O (my_at:
 // this row's first column, in elements; < 0: not a row): through the warp's 4 KB of shared memory, so that
 // a store writes whole 128-byte lines (from the lanes' own rows it would touch 32 lines).
@@ -322,115 +383,239 @@ __device__ __forceinline__ void store_rows(uint32_t stg, const uint32_t* w, long
 
 __device__ __forceinline__ float row_lse(float m, float l) { return l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2; }
 
-// Counts one more piece of a 32-row group: how many have come (tag: see ChunkParams; a count of another launch, or
-// whatever else the workspace held, counts as none).
+// Counts one more piece of a 32-row group: how many have come.  A count without the tag (see ChunkParams) is
+// whatever the workspace held before, and begins anew; a launch leaves its counts at zero.
 __device__ __forceinline__ int count_piece(unsigned long long* at, unsigned long long tag) {
-  unsigned long long seen = *reinterpret_cast<volatile unsigned long long*>(at), mine;
-  while (true) {
-    mine = ((seen ^ tag) >> 16 ? tag : seen) + 1;
-    const unsigned long long was = atomicCAS(at, seen, mine);
-    if (was == seen) return static_cast<int>(mine & 0xffff);
-    seen = was;
+  unsigned long long was = atomicAdd(at, 1ull);
+  while ((was ^ tag) >> 16) {
+    const unsigned long long seen = was + 1;
+    was = atomicCAS(at, seen, tag + 1);
+    if (was == seen) return 1;
+    if ((was ^ tag) >> 16)
+      --was;  // (another's count on top of what there was)
+    else
+      was = atomicAdd(at, 1ull);
   }
+  return static_cast<int>(was & 0xffff) + 1;
 }
 
-// What a cut unit's piece has to say of one query row (this thread's TMEM lane).
-struct PieceRow {
-  long long at;    // its place in O, in elements
-  float* lse_at;   // and in LSE, or null
-  float m, l;
-  bool has_tiles;  // this CTA walked key tiles of the row's tile
-  bool row, any;   // it is a row; the warp has one
+// What a unit, or a piece of it, has to say of one query row (this thread's TMEM lane): its place in O, in elements
+// (-1: not a row), and in LSE (or null), and its sums, O's in TMEM: weight 0 of that at o_tm, and with
+// `both` weight 1 of that at o_tm + D.
+struct RowSums {
+  long long at;
+  float* lse_at;
+  float m, l, w0, w1;
+  bool has, both;  // key tiles were walked here
+  bool any;        // the warp has a row
   bool alive;      // no wait has given up
 };
 
+// 32 columns of a row's O from column c on, weighted and summed.
+template <int D>
+__device__ __forceinline__ void load_o(uint32_t o_tm, int c, const RowSums& r, float scale, uint32_t* out) {
+  tmem_ld32(o_tm + c, out);
+  tmem_wait_ld();
+  reg_fence32(out);
+  const uint64_t a = f2(r.w0 * scale, r.w0 * scale);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const uint64_t x = mul2(f2(__uint_as_float(out[2 * i]), __uint_as_float(out[2 * i + 1])), a);
+    out[2 * i] = __float_as_uint(f2lo(x)), out[2 * i + 1] = __float_as_uint(f2hi(x));
+  }
+  if (r.both) {
+    uint32_t other[32];
+    tmem_ld32(o_tm + D + c, other);
+    tmem_wait_ld();
+    reg_fence32(other);
+    const uint64_t b = f2(r.w1 * scale, r.w1 * scale);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const uint64_t x = fma2(f2(__uint_as_float(other[2 * i]), __uint_as_float(other[2 * i + 1])), b,
+                              f2(__uint_as_float(out[2 * i]), __uint_as_float(out[2 * i + 1])));
+      out[2 * i] = __float_as_uint(f2lo(x)), out[2 * i + 1] = __float_as_uint(f2hi(x));
+    }
+  }
+}
+// O has been read out of TMEM: the next item's P.V may overwrite it.
+__device__ __forceinline__ void release_o(const RowSums& r, uint32_t bar_oe, uint32_t bar_oe1) {
+  tc_fence_before();
+  mbar_arrive(bar_oe);
+  if (r.both) mbar_arrive(bar_oe1);
+}
+
+// Joins the pieces of a warp's rows, N of them and U chunks of 16 bytes of a row at a time, all of whose loads are
+// on their way together: a round takes an access' latency, whatever it loads.
+template <int D, int U, int N>
+__device__ __forceinline__ void join_pieces(const ChunkParams& p, const Line& ln, const Item& it, int first, const float2* ml,
+                                            const float4* part, int rows, int lg, const RowSums& r) {
+  const int lane = threadIdx.x & 31, my = lane & ((1 << lg) - 1), parts = 32 >> lg;
+  const bool mine = my < rows;
+  const size_t ml_slot = static_cast<size_t>(p.groups) * 32, part_slot = ml_slot * (D / 4);
+  const long long at = __shfl_sync(0xffffffffu, r.at, my);
+#pragma unroll 1
+  for (int block = 0; block < D / 4; block += U * parts) {  // (of all lanes alike)
+    const int c0 = block + (lane >> lg);
+    float acc[4 * U], M = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4 * U; ++i) acc[i] = 0.f;
+    Pieces pieces(first);
+    bool more = true;
+#pragma unroll 1
+    while (more) {
+      int slots[N];
+#pragma unroll
+      for (int k = 0; k < N; ++k) slots[k] = -1;
+#pragma unroll 1
+      for (int k = 0; k < N && more; ++k) {
+        const int slot = pieces.next(ln, it);
+        more = slot >= 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) slots[i] = i == k ? slot : slots[i];
+      }
+      float2 x[N];
+      float4 v[N][U];
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        const bool there = mine && slots[k] >= 0;
+        const size_t slot = there ? slots[k] : 0;
+        x[k] = there ? __ldcg(ml + slot * ml_slot + my) : make_float2(-INFINITY, -1.f);
+        const float4* from = part + slot * part_slot + my;
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+          v[k][i] = there && c0 + i * parts < D / 4 ? __ldcg(from + (c0 + i * parts) * 32) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+      float M_new = M;
+#pragma unroll
+      for (int k = 0; k < N; ++k) M_new = fmaxf(M_new, x[k].x);
+      const float base = M_new == -INFINITY ? 0.f : M_new, alpha = ex2(M - base);
+      l *= alpha;
+#pragma unroll
+      for (int i = 0; i < 4 * U; ++i) acc[i] *= alpha;
+      M = M_new;
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        if (x[k].y < 0.f) continue;  // (no keys of the row's tile: nothing was written there)
+        const float w = ex2(x[k].x - base);
+        l = fmaf(w, x[k].y, l);
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+          acc[4 * i] = fmaf(w, v[k][i].x, acc[4 * i]);
+          acc[4 * i + 1] = fmaf(w, v[k][i].y, acc[4 * i + 1]);
+          acc[4 * i + 2] = fmaf(w, v[k][i].z, acc[4 * i + 2]);
+          acc[4 * i + 3] = fmaf(w, v[k][i].w, acc[4 * i + 3]);
+        }
+      }
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    if (mine)
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+        if (c0 + i * parts < D / 4)
+          *reinterpret_cast<uint2*>(p.o + at + (c0 + i * parts) * 4) =
+              make_uint2(pack_bf16x2(acc[4 * i] * inv, acc[4 * i + 1] * inv), pack_bf16x2(acc[4 * i + 2] * inv, acc[4 * i + 3] * inv));
+    // (every lane below `rows` has its own row)
+    if (block == 0 && r.lse_at) *r.lse_at = row_lse(M, l);
+  }
+}
+
+// Counts a piece of this warp's rows of a cut unit; true for the last to come.
+__device__ __forceinline__ bool last_piece(const ChunkParams& p, const Line& ln, const Item& it, int first, int warp) {
+  int pieces = 0, come = 0;
+  for (int from = first; from < ln.G; from += 32) {
+    if (ln.bound(from) >= it.at + it.cost) break;
+    pieces += __popc(piece_ctas(ln, it, from));
+  }
+  if ((threadIdx.x & 31) == 0) {
+    unsigned long long* count = p.count + static_cast<size_t>(first) * 8 + warp;
+    come = count_piece(count, p.tag);
+    if (come == pieces) *reinterpret_cast<volatile unsigned long long*>(count) = p.tag;
+  }
+  return __shfl_sync(0xffffffffu, come, 0) == pieces;
+}
+
+// A whole unit: this warp's 32 rows are stored.  (Not inlined, like the next: its registers would spill the softmax
+// loop's.)
+template <int D>
+__device__ __noinline__ void finish_unit(const ChunkParams& p, const RowSums r, uint32_t o_tm, uint32_t bar_oe, uint32_t bar_oe1,
+                                         uint32_t stg) {
+  const float inv = r.l == 0.f ? 0.f : 1.f / r.l;
+  uint32_t w[D / 2];
+  if (r.has) {
+#pragma unroll
+    for (int ch = 0; ch < D / 32; ++ch) {
+      uint32_t rr[32];
+      load_o<D>(o_tm, ch * 32, r, inv, rr);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) w[ch * 16 + i] = pack_bf16x2(__uint_as_float(rr[2 * i]), __uint_as_float(rr[2 * i + 1]));
+    }
+    release_o(r, bar_oe, bar_oe1);
+  } else {
+#pragma unroll
+    for (int i = 0; i < D / 2; ++i) w[i] = 0;
+  }
+#pragma unroll
+  for (int h = 0; h < D / 64; ++h) store_rows(stg, w + 32 * h, r.at < 0 ? r.at : r.at + 64 * h, p.o);
+  if (r.lse_at) *r.lse_at = row_lse(r.m, r.l);
+}
+
 // A piece of a cut unit: this warp's 32 rows go to the workspace, each 16 bytes of a row beside the other lanes'
 // (one store: 512 bytes in a row).  The last warp to bring its piece of the rows joins all of them, in the
-// pieces' order.  A CTA that gave up counts its pieces all the same, so that the counts are whole again at the
-// launch's end.  Not inlined: it is rare, and its registers would spill the softmax loop's.
+// pieces' order.  Not inlined: it is rare, and its registers would spill the softmax loop's.
 template <int D>
-__device__ __noinline__ void finish_piece(const ChunkParams& p, const Line& ln, const Item& it, const PieceRow r, uint32_t o_tm,
-                                          uint32_t bar_oe, uint32_t stg, int warp) {
+__device__ __noinline__ void finish_piece(const ChunkParams& p, const Line& ln, const Item& it, const RowSums r, uint32_t o_tm,
+                                          uint32_t bar_oe, uint32_t bar_oe1, int warp) {
   const int lane = threadIdx.x & 31, group = it.two ? warp : warp & 3;
-  const auto part_of = [&](int slot) {
-    return reinterpret_cast<float4*>(p.part) + (static_cast<size_t>(slot) * p.groups + group) * (D / 4) * 32 + lane;
-  };
-  const auto ml_of = [&](int slot) { return p.part_ml + (static_cast<size_t>(slot) * p.groups + group) * 32 + lane; };
+  const bool row = r.at >= 0;
   const int slot = it.lo == 0 ? 2 * static_cast<int>(blockIdx.x) + 1 : 2 * static_cast<int>(blockIdx.x);
   if (r.alive && r.any) {
-    float4* mine = part_of(slot);
-    if (r.has_tiles) {
+    float4* mine = reinterpret_cast<float4*>(p.part) + (static_cast<size_t>(slot) * p.groups + group) * (D / 4) * 32 + lane;
+    if (r.has) {
 #pragma unroll
       for (int ch = 0; ch < D / 32; ++ch) {
         uint32_t rr[32];
-        tmem_ld32(o_tm + ch * 32, rr);
-        tmem_wait_ld();
-        reg_fence32(rr);
-        if (r.row)
+        load_o<D>(o_tm, ch * 32, r, 1.f, rr);
+        if (row)
 #pragma unroll
           for (int u = 0; u < 8; ++u)
             mine[(ch * 8 + u) * 32] = make_float4(__uint_as_float(rr[4 * u]), __uint_as_float(rr[4 * u + 1]),
                                                   __uint_as_float(rr[4 * u + 2]), __uint_as_float(rr[4 * u + 3]));
       }
     }
-    if (r.row) *ml_of(slot) = make_float2(r.m, r.has_tiles ? r.l : -1.f);
+    if (row) p.part_ml[(static_cast<size_t>(slot) * p.groups + group) * 32 + lane] = make_float2(r.m, r.has ? r.l : -1.f);
   }
-  if (r.alive && r.has_tiles) {
-    tc_fence_before();
-    mbar_arrive(bar_oe);
-  }
+  if (r.alive && r.has) release_o(r, bar_oe, bar_oe1);
   if (!r.any) return;
-  int pieces = 0;
-  const int first = for_pieces(ln, it, [&](int) { ++pieces; });
-  unsigned long long* count = p.count + static_cast<size_t>(first) * 8 + warp;
+  const int first = first_cta(ln, it);
   __threadfence();
   __syncwarp();
-  int come = 0;
-  if (lane == 0) {
-    come = count_piece(count, p.tag);
-    if (come == pieces) *reinterpret_cast<volatile unsigned long long*>(count) = p.tag;
-  }
-  come = __shfl_sync(0xffffffffu, come, 0);
-  if (!r.alive || come != pieces) return;
+  if (!last_piece(p, ln, it, first, warp) || !r.alive) return;
   __syncwarp();
   __threadfence();
-  float M = -INFINITY, l = 0.f;
-  for_pieces(ln, it, [&](int s) {
-    if (r.row) M = fmaxf(M, __ldcg(ml_of(s)).x);
-  });
-  const float base = M == -INFINITY ? 0.f : M;
-  for_pieces(ln, it, [&](int s) {
-    if (!r.row) return;
-    const float2 ml = __ldcg(ml_of(s));
-    if (!(ml.y < 0.f)) l = fmaf(ex2(ml.x - base), ml.y, l);
-  });
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll 1
-  for (int h = 0; h < D / 64; ++h) {
-    float acc[64];
-#pragma unroll
-    for (int i = 0; i < 64; ++i) acc[i] = 0.f;
-    for_pieces(ln, it, [&](int s) {
-      if (!r.row) return;
-      const float2 ml = __ldcg(ml_of(s));
-      if (ml.y < 0.f) return;
-      const float weight = ex2(ml.x - base);
-      const float4* from = part_of(s) + h * 16 * 32;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float4 v = __ldcg(from + i * 32);
-        acc[4 * i] = fmaf(weight, v.x, acc[4 * i]);
-        acc[4 * i + 1] = fmaf(weight, v.y, acc[4 * i + 1]);
-        acc[4 * i + 2] = fmaf(weight, v.z, acc[4 * i + 2]);
-        acc[4 * i + 3] = fmaf(weight, v.w, acc[4 * i + 3]);
-      }
-    });
-    uint32_t w[32];
-#pragma unroll
-    for (int i = 0; i < 32; ++i) w[i] = pack_bf16x2(acc[2 * i] * inv, acc[2 * i + 1] * inv);
-    store_rows(stg, w, r.at < 0 ? r.at : r.at + 64 * h, p.o);
+  // The warp's rows (its first lanes') are spread over all lanes: 1 << lg of them side by side, each lane with
+  // every (32 >> lg)-th 16 bytes of its row.
+  const int rows = __popc(__ballot_sync(0xffffffffu, row));
+  const int lg = rows > 1 ? 32 - __clz(rows - 1) : 0;
+  const float2* ml = p.part_ml + group * 32;
+  const float4* part = reinterpret_cast<const float4*>(p.part) + static_cast<size_t>(group) * (D / 4) * 32;
+  if (lg <= 2)
+    join_pieces<D, 4, 6>(p, ln, it, first, ml, part, rows, lg, r);
+  else
+    join_pieces<D, 8, 3>(p, ln, it, first, ml, part, rows, lg, r);
+}
+
+// After a wait has given up, a softmax warp counts the pieces that it has not brought all the same, so that every
+// count is whole again at the launch's end: a captured launch may be replayed on this workspace.
+__device__ __noinline__ void count_rest(const ChunkParams& p, const Line& ln, int b, long long at, int warp, int counted) {
+  if (ln.x0 >= ln.x1) return;
+  Walk w = walk_from(p, ln, b, at);
+  Item it;
+  while (next_item(p, ln, w, it)) {
+    // the warp's first row, if it has rows: as the softmax role has it
+    const int i = (warp & 3) * 32, token = it.t0 + (it.two ? (warp >> 2) * p.tq : 0) + i / p.gt;
+    if (!it.cut() || (!it.two && warp >= 4) || i / p.gt >= p.tq || token >= it.sq) continue;
+    if (--counted < 0) last_piece(p, ln, it, first_cta(ln, it), warp);
   }
-  if (r.lse_at) *r.lse_at = row_lse(M, l);
 }
 
 template <int D>
@@ -446,13 +631,17 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
 
   const uint32_t bar_q = sbase + C::BAR_OFF;           // [2] Q_t loaded
   const uint32_t bar_qe = bar_q + 16;                  // [2] Q_t no longer read
-  const uint32_t bar_full = bar_qe + 16;               // [NSLOT]
-  const uint32_t bar_empty = bar_full + 8 * C::NSLOT;  // [NKE] K number n and the V before it are no longer read
-  const uint32_t bar_s = bar_empty + 8 * C::NKE;       // [2] S_t ready
+  const uint32_t bar_full = bar_qe + 16;               // [2][NR] slots of the K ring and of the V ring filled
+  const uint32_t bar_empty = bar_full + 16 * C::NR;    // [2][NR] and no longer read
+  const uint32_t bar_s = bar_empty + 16 * C::NR;       // [2] S_t ready
   const uint32_t bar_p = bar_s + 16;                   // [2][2] half h of P_t written (h = 0: and O_t rescaled)
   const uint32_t bar_o = bar_p + 32;                   // [2] O_t of the item complete
   const uint32_t bar_oe = bar_o + 16;                  // [2] O_t read out
-  const uint32_t bar_drain = bar_oe + 16;
+  const uint32_t bar_ml = bar_oe + 16;                 // m and l of a single tile's odd key tiles are there
+  const uint32_t bar_mle = bar_ml + 8;                 // and read
+  const uint32_t bar_drain = bar_mle + 8;
+  const uint32_t bar_rec = bar_drain + 8;              // [NREC] a record is written
+  const uint32_t bar_rece = bar_rec + 8 * C::NREC;     // [NREC] and read by the other roles' warps
   uint32_t* tmem_ptr = reinterpret_cast<uint32_t*>(smem + C::TMEM_PTR_OFF);
   Abort ab{reinterpret_cast<volatile int*>(smem + C::ABORT_OFF)};
 
@@ -466,9 +655,17 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
       mbar_init(bar_o + 8 * t, 1);
       mbar_init(bar_oe + 8 * t, C::BM);
     }
-    for (int s = 0; s < C::NSLOT; ++s) mbar_init(bar_full + 8 * s, 1);
-    for (int n = 0; n < C::NKE; ++n) mbar_init(bar_empty + 8 * n, 1);
+    for (int s = 0; s < 2 * C::NR; ++s) {
+      mbar_init(bar_full + 8 * s, 1);
+      mbar_init(bar_empty + 8 * s, 1);
+    }
+    mbar_init(bar_ml, C::BM);
+    mbar_init(bar_mle, C::BM);
     mbar_init(bar_drain, 1);
+    for (int i = 0; i < C::NREC; ++i) {
+      mbar_init(bar_rec + 8 * i, 1);
+      mbar_init(bar_rece + 8 * i, C::THREADS / 32 - 1);
+    }
     *ab.flag = 0;
     *(ab.flag + 1) = 0;
     fence_barrier_init();
@@ -486,14 +683,15 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
   asm volatile("griddepcontrol.launch_dependents;");
 
   // The line's length, and the sequence in which this CTA's stretch begins: a prefix sum over the sequences.
-  Line ln;
-  Walk walk;
+  Line& ln = *reinterpret_cast<Line*>(smem + C::LINE_OFF);
+  volatile long long* start = reinterpret_cast<volatile long long*>(smem + C::LINE_OFF + sizeof(Line));  // sequence, its place
+  static_assert(sizeof(Line) + 16 <= 128, "fits");
   {
     volatile long long* sums = reinterpret_cast<volatile long long*>(smem + C::SUM_OFF);
-    volatile long long* start = reinterpret_cast<volatile long long*>(smem + C::START_OFF);
     constexpr int kWarps = C::THREADS / 32;
-    ln.G = static_cast<int>(gridDim.x);
-    ln.W = ln.x0 = ln.x1 = 0;
+    Line l;
+    const int G = static_cast<int>(gridDim.x);
+    l.x0 = 0;
     const bool one = p.B <= C::THREADS;
     // (one round: the sum of all and this CTA's sequence from the same scan; else a round for each)
     for (int round = 0; round < (one ? 1 : 2); ++round) {
@@ -512,16 +710,17 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
         __syncthreads();
         long long all = 0;
         x += before - cost;
+#pragma unroll
         for (int i = 0; i < kWarps; ++i) {
           const long long y = sums[i];
           if (i < warp) x += y;
           all += y;
         }
         if (one) {
-          ln.W = all;
-          ln.x0 = bound_of(ln.W, ln.G, blockIdx.x);
+          l.set(all, G);
+          l.x0 = l.bound(blockIdx.x);
         }
-        if ((one || round == 1) && x <= ln.x0 && ln.x0 < x + cost) {
+        if ((one || round == 1) && x <= l.x0 && l.x0 < x + cost) {
           start[0] = b;
           start[1] = x;
         }
@@ -529,103 +728,118 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
         __syncthreads();
       }
       if (!one && round == 0) {
-        ln.W = before;
-        ln.x0 = bound_of(ln.W, ln.G, blockIdx.x);
+        l.set(before, G);
+        l.x0 = l.bound(blockIdx.x);
       }
     }
-    ln.x1 = static_cast<int>(blockIdx.x) + 1 < ln.G ? bound_of(ln.W, ln.G, blockIdx.x + 1) : ln.W;
-    walk.b = p.B;
-    if (ln.x0 < ln.x1) {
-      walk.b = static_cast<int>(start[0]);
-      walk.s = load_seq(p, walk.b);
-      const long long plane = plane_cost(p, walk.s), in = ln.x0 - start[1];
-      walk.plane = static_cast<int>(in / plane);
-      const long long r = in - walk.plane * plane;
-      int lo = 0, hi = walk.s.pairs;  // the last pair that begins at r or before
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (cost_before(p, walk.s, mid) <= r)
-          lo = mid;
-        else
-          hi = mid;
-      }
-      walk.pair = lo;
-      walk.at = start[1] + walk.plane * plane + cost_before(p, walk.s, lo);
-    }
+    l.x1 = static_cast<int>(blockIdx.x) + 1 < G ? l.bound(blockIdx.x + 1) : l.W;
+    if (threadIdx.x == 0) ln = l;
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_ptr;
-  Item it{};
 
-  if (warp == 8) {
-    // ------------------------------------------------------------------ loader (whole warp)
-    // Lane 0 waits and expects; a tile's pieces of min(page, 64) keys are looked up and copied by one lane each.
-    if (lane == 0) {
-      prefetch_tensormap(&tm_q);
-      prefetch_tensormap(&tm_k);
-      prefetch_tensormap(&tm_v);
+  // The items, for the other roles' warps: item number i, once its record is written (null where a wait gave up, or
+  // past the last one); a warp gives the record back when it needs no more of it.
+  int rec_n = 0, counted = 0;  // counted: (softmax warps) pieces of cut units that this warp has counted
+  const auto take_item = [&]() -> const Item* {
+    const int i = rec_n % C::NREC;
+    if (!mbar_wait_warp(bar_rec + 8 * i, (rec_n / C::NREC) & 1, p.ctl, ab)) return nullptr;
+    const Item* it = reinterpret_cast<const Item*>(smem + C::REC_OFF + i * 80);
+    return *reinterpret_cast<const volatile int*>(&it->n) < 0 ? nullptr : it;
+  };
+  const auto give_item = [&]() {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar_rece + 8 * (rec_n % C::NREC));
+    ++rec_n;
+  };
+
+  if (warp == 11) {
+    // ------------------------------------------------------------------ scheduler (whole warp, all lanes alike)
+    Walk walk;
+    walk.b = p.B;
+    const Line l = ln;
+    if (l.x0 < l.x1) walk = walk_from(p, l, static_cast<int>(start[0]), start[1]);
+    bool more = true;
+    for (int k = 0; more; ++k) {
+      Item it;
+      more = next_item(p, l, walk, it);
+      if (!more) it.n = -1;
+      const int i = k % C::NREC;
+      if (k >= C::NREC && !mbar_wait_warp(bar_rece + 8 * i, (k / C::NREC - 1) & 1, p.ctl, ab)) break;
+      if (lane == 0) {
+        *reinterpret_cast<Item*>(smem + C::REC_OFF + i * 80) = it;
+        mbar_arrive(bar_rec + 8 * i);
+      }
+      __syncwarp();
     }
+  } else if (warp == 8 || warp == 10) {
+    // ------------------------------------------------------------------ loaders (whole warps): Q and K, and V
+    // Lane 0 waits and expects; a tile's pieces of min(page, 64) keys are looked up and copied by one lane each.
+    const bool is_v = warp == 10;
+    const CUtensorMap* map = is_v ? &tm_v : &tm_k;
+    if (lane == 0) {
+      if (!is_v) prefetch_tensormap(&tm_q);
+      prefetch_tensormap(map);
+    }
+    const uint32_t full = bar_full + (is_v ? 8 * C::NR : 0), empty = bar_empty + (is_v ? 8 * C::NR : 0);
+    const uint32_t ring = sbase + C::RING_OFF + (is_v ? C::NR * C::TILE_BYTES : 0);
     int pos = 0, issued = 0, skipped = -1, q_issued[2] = {0, 0};
     bool ok = true;
-    const int rows = min(p.page, 64);
+    const int rows = min(p.page, 64), rows_lg = 31 - __clz(rows);  // (8, 16, 32 or 64)
     const uint32_t q_bytes = static_cast<uint32_t>(C::NBOX * p.tq * p.gt * 128);
-    const auto load_q = [&](int t) -> bool {
+    const auto load_q = [&](int t, int plane, int token) -> bool {
       const int n = q_issued[t];
       if (n > 0 && !mbar_wait_warp(bar_qe + 8 * t, (n - 1) & 1, p.ctl, ab)) return false;
       if (lane == 0) {
         mbar_expect_tx(bar_q + 8 * t, q_bytes);
-        const int token = it.qb + it.t0 + (it.two && t == 1 ? p.tq : 0);
         for (int x = 0; x < C::NBOX; ++x)
-          tma_load_4d(sbase + C::Q_OFF + t * C::TILE_BYTES + x * C::BOX_BYTES, &tm_q, x * 64, 0, it.plane, token, bar_q + 8 * t);
+          tma_load_4d(sbase + C::Q_OFF + t * C::TILE_BYTES + x * C::BOX_BYTES, &tm_q, x * 64, 0, plane, token, bar_q + 8 * t);
       }
       __syncwarp();
       q_issued[t] = n + 1;
       return true;
     };
-    while (ok && next_item(p, ln, walk, it)) {
-      if (it.n == 0) continue;  // no keys: nothing to load
-      const int32_t* table = p.table + static_cast<size_t>(it.b) * p.max_pages;
+    const Item* rec;
+    while (ok && (rec = take_item())) {
+      const int lo = rec->lo, end = lo + rec->n, skv = rec->skv, plane = rec->plane, token = rec->qb + rec->t0, n0 = rec->n0;
+      const bool two = rec->two;
+      const int32_t* table = p.table + static_cast<size_t>(rec->b) * p.max_pages;
+      give_item();
+      if (lo == end) continue;  // no keys: nothing to load
       // the page of this lane's piece of key tile j (none past the sequence's keys)
       const auto page_of = [&](int j) {
         const int key = j * C::BN + lane * rows;
-        return lane * rows < C::BN && key < it.skv ? table[key / p.page] : -1;
+        return lane * rows < C::BN && key < skv ? table[static_cast<unsigned>(key) / static_cast<unsigned>(p.page)] : -1;
       };
-      int page = page_of(it.lo);
-      if (!(ok = load_q(it.n0 > 0 ? 0 : 1))) break;
-      const int hk = it.plane / p.planes_per_kv;
-      for (int jj = 0; jj < 2 * it.n; ++jj, ++pos) {  // K_0, [Q_1], V_0, K_1, V_1, ...
-        if (jj == 1 && it.n0 > 0 && !(ok = load_q(1))) break;
-        const int slot = pos % C::NSLOT;
-        // the slot's last tile, at position pos - NSLOT, is released with K number n
-        if (pos >= C::NSLOT) {
-          const int n = (pos - C::NSLOT + 1) >> 1;
-          if (!(ok = mbar_wait_warp(bar_empty + 8 * (n % C::NKE), (n / C::NKE) & 1, p.ctl, ab))) break;
-        }
+      int page = page_of(lo);
+      if (!is_v && n0 > 0 && !(ok = load_q(0, plane, token))) break;
+      const int hk = plane / p.planes_per_kv;
+      for (int j = lo; j < end; ++j, ++pos) {
+        const int slot = pos % C::NR;
+        if (pos >= C::NR && !(ok = mbar_wait_warp(empty + 8 * slot, (pos / C::NR - 1) & 1, p.ctl, ab))) break;
         issued = pos + 1;
-        if (p.ctl.inject == 5 && pos == 2) {  // test hook: never load this tile
+        if (p.ctl.inject == 5 && !is_v && pos == 1) {  // test hook: never load this tile
           skipped = pos;
           continue;
         }
-        const int j = it.lo + (jj >> 1), key0 = j * C::BN;
-        const int pieces = (min(C::BN, it.skv - key0) + rows - 1) / rows;
-        if (lane == 0) mbar_expect_tx(bar_full + 8 * slot, static_cast<uint32_t>(C::NBOX * pieces * rows * 128));
+        const int pieces = (min(C::BN, skv - j * C::BN) + rows - 1) >> rows_lg;
+        if (lane == 0) mbar_expect_tx(full + 8 * slot, static_cast<uint32_t>(C::NBOX * pieces * rows * 128));
         __syncwarp();
         if (lane < pieces) {
           // NHD view [keys of all pages, Hkv, D]: (dim, kv head, key); HND view [pages x Hkv, page, D]:
           // (dim, row in page, page x Hkv + kv head).  A page that there is not: past the end, which reads as zeros.
-          const int key = key0 + lane * rows, in = key % p.page;
+          const int in = static_cast<int>(static_cast<unsigned>(j * C::BN + lane * rows) % static_cast<unsigned>(p.page));
           const bool bad = page < 0 || page >= p.num_pages;
           const int y = p.hnd ? in : hk;
           const int z = p.hnd ? (bad ? p.num_pages * p.Hkv : page * p.Hkv + hk) : (bad ? p.num_pages * p.page : page * p.page + in);
-          const CUtensorMap* map = (jj & 1) ? &tm_v : &tm_k;
 #pragma unroll
           for (int x = 0; x < C::NBOX; ++x)
-            tma_load_3d(sbase + C::RING_OFF + slot * C::TILE_BYTES + x * C::BOX_BYTES + lane * rows * 128, map, x * 64, y, z,
-                        bar_full + 8 * slot);
+            tma_load_3d(ring + slot * C::TILE_BYTES + x * C::BOX_BYTES + lane * rows * 128, map, x * 64, y, z, full + 8 * slot);
         }
-        if ((jj & 1) && j + 1 < it.lo + it.n) page = page_of(j + 1);
+        if (j == lo && !is_v && two && !(ok = load_q(1, plane, token + p.tq))) break;
+        if (j + 1 < end) page = page_of(j + 1);
       }
     }
     // drain copies still in flight before the CTA may exit
@@ -633,8 +847,8 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
       Abort no_abort{ab.flag + 1};
       for (int t = 0; t < 2; ++t)
         if (q_issued[t] > 0) mbar_wait(bar_q + 8 * t, (q_issued[t] - 1) & 1, p.ctl, no_abort);
-      for (int ps = max(0, issued - C::NSLOT); ps < issued; ++ps)
-        if (ps != skipped) mbar_wait(bar_full + 8 * (ps % C::NSLOT), (ps / C::NSLOT) & 1, p.ctl, no_abort);
+      for (int ps = max(0, issued - C::NR); ps < issued; ++ps)
+        if (ps != skipped) mbar_wait(full + 8 * (ps % C::NR), (ps / C::NR) & 1, p.ctl, no_abort);
     }
   } else if (warp == 9) {
     // ------------------------------------------------------------------ MMA issuer (whole warp, one lane elected)
@@ -642,89 +856,114 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
     constexpr uint32_t idesc_pv = idesc_bf16(C::BM, D, 0, 1);     // P from TMEM, V MN-major
     const uint64_t dq0 = sdesc_sw128(sbase + C::Q_OFF, 16, 1024);
     const uint64_t dk0 = sdesc_sw128(sbase + C::RING_OFF, 16, 1024);
-    const uint64_t dv0 = sdesc_sw128(sbase + C::RING_OFF, C::BOX_BYTES, 1024);
+    const uint64_t dv0 = sdesc_sw128(sbase + C::RING_OFF + C::NR * C::TILE_BYTES, C::BOX_BYTES, 1024);
     constexpr uint32_t kTile16 = C::TILE_BYTES >> 4, kBox16 = C::BOX_BYTES >> 4;
-    const auto wait_slot = [&](int ps) {
-      return mbar_wait_warp(bar_full + 8 * (ps % C::NSLOT), (ps / C::NSLOT) & 1, p.ctl, ab);
-    };
-    const auto issue_s = [&](int t, int kpos) {
-      const uint64_t a = dq0 + t * kTile16, b = dk0 + (kpos % C::NSLOT) * kTile16;
+    const auto wait_k = [&](int n) { return mbar_wait_warp(bar_full + 8 * (n % C::NR), (n / C::NR) & 1, p.ctl, ab); };
+    const auto wait_v = [&](int n) { return mbar_wait_warp(bar_full + 8 * (C::NR + n % C::NR), (n / C::NR) & 1, p.ctl, ab); };
+    const auto free_k = [&](int n) { tc_commit_el(bar_empty + 8 * (n % C::NR)); };
+    const auto free_v = [&](int n) { tc_commit_el(bar_empty + 8 * (C::NR + n % C::NR)); };
+    // S_t = Q K^T with the query tile q and K number n
+    const auto issue_s = [&](int t, int q, int n) {
+      const uint64_t a = dq0 + q * kTile16, b = dk0 + (n % C::NR) * kTile16;
 #pragma unroll
       for (int x = 0; x < C::NBOX; ++x)
         mma_ss_k64_el(tmem + C::S_COL + t * C::BN, a + x * kBox16, b + x * kBox16, idesc_s, x > 0);
+      tc_commit_el(bar_s + 8 * t);
     };
-    const auto issue_pv = [&](int t, int vpos, bool acc, int half) {
-      const uint64_t b = dv0 + (vpos % C::NSLOT) * kTile16 + half * 64 * (128 >> 4);
-      mma_ts_k64_el(tmem + C::O_COL + t * D, tmem + C::S_COL + t * C::BN + half * 32, b, idesc_pv, acc ? 1u : 0u);
-    };
-    int pos = 0, cnt0 = 0, cnt1 = 0;  // ring position of K_0; S/P uses so far per tile
-    int n0 = 0, n1 = 0;               // items so far that had a tile 0, a tile 1
-    bool ok = true;
-    while (ok && next_item(p, ln, walk, it)) {
-      const int nt0 = it.n0, nt = it.n;
-      if (nt == 0) continue;
-      if (nt0 > 0) {
-        if (!(ok = mbar_wait_warp(bar_q, n0 & 1, p.ctl, ab) && wait_slot(pos))) break;
+    int q1 = 0;                                       // items so far with two query tiles
+    // key tiles so far; steps of S, P and O number 0 and 1, items that had some (no arrays: number t is not
+    // always a constant, and they would go to local memory)
+    int pos = 0, cnt0 = 0, cnt1 = 0, items0 = 0, items1 = 0;
+    // O_t += P_t V with V number n, the half written first as soon as it is there; step j of the item's
+    const auto issue_pv = [&](int t, int n, int j) -> bool {
+      const uint64_t b = dv0 + (n % C::NR) * kTile16;
+      const int cnt = t ? cnt1 : cnt0, items = t ? items1 : items0;
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        if (!mbar_wait_warp(bar_p + 16 * t + 8 * half, (cnt + j) & 1, p.ctl, ab)) return false;
+        // O_t of the item before must have been read out
+        if (half == 0 && j == 0 && items > 0 && !mbar_wait_warp(bar_oe + 8 * t, (items - 1) & 1, p.ctl, ab)) return false;
         tc_fence_after();
-        issue_s(0, pos);
-        tc_commit_el(bar_s);
-        if (nt0 == 1) tc_commit_el(bar_qe);  // every S of tile 0 issued
+        mma_ts_k64_el(tmem + C::O_COL + t * D, tmem + C::S_COL + t * C::BN + half * 32, b + half * 64 * (128 >> 4), idesc_pv,
+                      j > 0 || half > 0 ? 1u : 0u);
       }
-      if (!(ok = mbar_wait_warp(bar_q + 8, n1 & 1, p.ctl, ab) && (nt0 > 0 || wait_slot(pos)))) break;
+      return true;
+    };
+    // Two query tiles: S0 S1 | PV0 S0' | PV1 S1' | ...: the tensor pipe works on one tile while the other's
+    // softmax runs.  Tile 0 stops at its own diagonal.
+    const auto two_tiles = [&](int n0, int n) -> bool {
+      if (n0 > 0) {
+        if (!mbar_wait_warp(bar_q, items0 & 1, p.ctl, ab) || !wait_k(pos)) return false;
+        tc_fence_after();
+        issue_s(0, 0, pos);
+        if (n0 == 1) tc_commit_el(bar_qe);  // every S of tile 0 issued
+      }
+      if (!mbar_wait_warp(bar_q + 8, q1 & 1, p.ctl, ab) || (n0 == 0 && !wait_k(pos))) return false;
       tc_fence_after();
-      issue_s(1, pos);
-      tc_commit_el(bar_s + 8);
-      tc_commit_el(bar_empty + 8 * ((pos >> 1) % C::NKE));
-      if (!(ok = wait_slot(pos + 1))) break;
-      if (nt == 1) tc_commit_el(bar_qe + 8);  // every S of tile 1 issued
-      for (int j = 0; j < nt; ++j) {
-        const int vpos = pos + 2 * j + 1, kpos = pos + 2 * j + 2;
-        const bool more = j + 1 < nt;
-        if (j < nt0) {  // query tile 0 stops at its own diagonal
-          if (!(ok = mbar_wait_warp(bar_p, (cnt0 + j) & 1, p.ctl, ab))) break;
-          // O_0 of the previous item must have been read out
-          if (j == 0 && n0 > 0 && !(ok = mbar_wait_warp(bar_oe, (n0 - 1) & 1, p.ctl, ab))) break;
-          tc_fence_after();
-          issue_pv(0, vpos, j > 0, 0);
-          if (!(ok = mbar_wait_warp(bar_p + 8, (cnt0 + j) & 1, p.ctl, ab))) break;
-          tc_fence_after();
-          issue_pv(0, vpos, true, 1);
-          if (j + 1 == nt0) tc_commit_el(bar_o);
+      issue_s(1, 1, pos);
+      free_k(pos);
+      if (n == 1) tc_commit_el(bar_qe + 8);
+      if (!wait_v(pos)) return false;
+      for (int j = 0; j < n; ++j) {
+        const bool more = j + 1 < n;
+        if (j < n0) {
+          if (!issue_pv(0, pos + j, j)) return false;
+          if (j + 1 == n0) tc_commit_el(bar_o);
         }
         if (more) {
-          if (!(ok = wait_slot(kpos))) break;
+          if (!wait_k(pos + j + 1)) return false;
           tc_fence_after();
-          if (j + 1 < nt0) {
-            issue_s(0, kpos);
-            tc_commit_el(bar_s);
-            if (j + 2 == nt0) tc_commit_el(bar_qe);  // tile 0's last S of the item
+          if (j + 1 < n0) {
+            issue_s(0, 0, pos + j + 1);
+            if (j + 2 == n0) tc_commit_el(bar_qe);
           }
         }
-        if (!(ok = mbar_wait_warp(bar_p + 16, (cnt1 + j) & 1, p.ctl, ab))) break;
-        if (j == 0 && n1 > 0 && !(ok = mbar_wait_warp(bar_oe + 8, (n1 - 1) & 1, p.ctl, ab))) break;
-        tc_fence_after();
-        issue_pv(1, vpos, j > 0, 0);
-        if (!(ok = mbar_wait_warp(bar_p + 24, (cnt1 + j) & 1, p.ctl, ab))) break;
-        tc_fence_after();
-        issue_pv(1, vpos, true, 1);
+        if (!issue_pv(1, pos + j, j)) return false;
+        free_v(pos + j);
         if (!more) {
           tc_commit_el(bar_o + 8);
         } else {
           // (the next V is awaited while P.V keeps the tensor pipe busy; at D = 64 that would hold S back)
-          if (D == 128 && !(ok = wait_slot(vpos + 2))) break;
-          issue_s(1, kpos);
-          tc_commit_el(bar_s + 8);
-          tc_commit_el(bar_empty + 8 * ((kpos >> 1) % C::NKE));
-          if (D != 128 && !(ok = wait_slot(vpos + 2))) break;
-          if (j + 2 == nt) tc_commit_el(bar_qe + 8);  // tile 1's last S of the item
+          if (D == 128 && !wait_v(pos + j + 1)) return false;
+          issue_s(1, 1, pos + j + 1);
+          free_k(pos + j + 1);
+          if (j + 2 == n) tc_commit_el(bar_qe + 8);
+          if (D != 128 && !wait_v(pos + j + 1)) return false;
         }
       }
-      if (!ok) break;
-      cnt0 += nt0;
-      cnt1 += nt;
-      pos += 2 * nt;
-      n0 += nt0 > 0;
-      ++n1;
+      return true;
+    };
+    // One query tile: key tile j goes the way of number j % 2.
+    const auto one_tile = [&](int n) -> bool {
+      const auto next_s = [&](int j) -> bool {
+        if (!wait_k(pos + j)) return false;
+        tc_fence_after();
+        issue_s(j & 1, 0, pos + j);
+        free_k(pos + j);
+        if (j + 1 == n) tc_commit_el(bar_qe);
+        return true;
+      };
+      if (!mbar_wait_warp(bar_q, items0 & 1, p.ctl, ab) || !next_s(0) || (n > 1 && !next_s(1))) return false;
+      for (int j = 0; j < n; ++j) {
+        if (!wait_v(pos + j) || !issue_pv(j & 1, pos + j, j >> 1)) return false;
+        free_v(pos + j);
+        if (j + 2 >= n) tc_commit_el(bar_o + 8 * (j & 1));
+        if (j + 2 < n && !next_s(j + 2)) return false;
+      }
+      return true;
+    };
+    while (const Item* rec = take_item()) {
+      const int n = rec->n, n0 = rec->n0, n1 = rec->n1;
+      const bool two = rec->two;
+      give_item();
+      if (n == 0) continue;
+      if (!(two ? two_tiles(n0, n) : one_tile(n))) break;
+      cnt0 += n0;
+      cnt1 += n1;
+      pos += n;
+      items0 += n0 > 0;
+      items1 += n1 > 0;
+      q1 += two;
     }
     // wait for every MMA issued above before TMEM may be released
     Abort no_abort{ab.flag + 1};
@@ -732,99 +971,103 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
     mbar_wait_warp(bar_drain, 0, p.ctl, no_abort);
   } else {
     // ------------------------------------------------------------------ softmax
-    const int t = warp >> 2;                         // query tile of this warpgroup
+    const int t = warp >> 2;                         // S, P and O number t are this warpgroup's
     const int row_in_tile = (warp & 3) * 32 + lane;  // == TMEM lane
     const uint32_t lane_addr = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t s_tm = tmem + lane_addr + C::S_COL + t * C::BN;
     const uint32_t o_tm = tmem + lane_addr + C::O_COL + t * D;
     const uint32_t my_s = bar_s + 8 * t, my_p = bar_p + 16 * t, my_o = bar_o + 8 * t, my_oe = bar_oe + 8 * t;
     const uint32_t stg = sbase + C::STG_OFF + warp * 4096;
+    const uint32_t ml = sbase + C::ML_OFF + row_in_tile * 8;
     const int row_token = row_in_tile / p.gt, row_head = row_in_tile - row_token * p.gt;
-    int cnt = 0, items = 0;  // S tiles of this query tile so far, items that had it
-    int pos = 0;             // ring position of the item's K_0
+    int cnt = 0, items = 0;  // this warpgroup's steps so far, items that had some
+    int pos = 0, shared = 0, items1 = 0;  // key tiles so far; single tiles that both had steps of; items of number 1
     bool alive = true;
-    while (next_item(p, ln, walk, it)) {
-      const int n = t == 0 ? it.n0 : it.n;
-      const int first_token = it.t0 + (it.two && t == 1 ? p.tq : 0);
-      const bool has_tile = t == 1 || it.two;
-      const int token = first_token + row_token;
-      const bool row = has_tile && row_token < p.tq && token < it.sq;
+    while (const Item* rec = alive ? take_item() : nullptr) {
+      const Item& it = *rec;
+      const int n = t == 0 ? it.n0 : it.n1;
+      const int token = it.t0 + (it.two ? t * p.tq : 0) + row_token;
+      const bool row = row_token < p.tq && token < it.sq;
       const bool any = __any_sync(0xffffffffu, row);
       const int query = min(token, it.sq - 1);  // (a row that is none: masked like the last)
       const int limit = (p.causal ? max(0, query + it.skv - it.sq + 1) : it.skv) - it.lo * C::BN;
       // The unit's last tile here, where it reaches past the sequence's keys: what V's rows hold there (other
       // keys, or nothing that was ever written) must not meet P = 0, so they are cleared, by the
-      // warps of tile 0 if it takes part in the step, which P.V of tile 1 follows.
+      // warps whose P.V comes first.
       const int over = it.skv - (it.lo + it.n - 1) * C::BN;  // keys of the last tile
-      const bool clears = over < C::BN && (t == 0 ? it.n0 == it.n : it.n0 < it.n);
+      const bool clears = over < C::BN && (it.two ? (t == 0 ? it.n0 == it.n : it.n0 < it.n) : t == ((it.n - 1) & 1));
       float m_run = -INFINITY, l_run = 0.f;
-      for (int j = 0; alive && j < n; ++j) {
+      for (int i = 0; alive && i < n; ++i) {
+        const int j = it.two ? i : 2 * i + t;  // key tile
         const auto before_p = [&]() -> bool {
           if (!clears || j + 1 < it.n) return true;
-          const int vpos = pos + 2 * j + 1, slot = vpos % C::NSLOT;
-          if (!mbar_wait_warp(bar_full + 8 * slot, (vpos / C::NSLOT) & 1, p.ctl, ab)) return false;
-          const uint32_t v = sbase + C::RING_OFF + slot * C::TILE_BYTES;
+          const int vn = pos + j, slot = vn % C::NR;
+          if (!mbar_wait_warp(bar_full + 8 * (C::NR + slot), (vn / C::NR) & 1, p.ctl, ab)) return false;
+          const uint32_t v = sbase + C::RING_OFF + (C::NR + slot) * C::TILE_BYTES;
           const int chunks = (C::BN - over) * 8;
-          for (int i = row_in_tile; i < C::NBOX * chunks; i += C::BM)
-            st_shared_v4(v + i / chunks * C::BOX_BYTES + over * 128 + i % chunks * 16, 0, 0, 0, 0);
+          for (int x = row_in_tile; x < C::NBOX * chunks; x += C::BM)
+            st_shared_v4(v + x / chunks * C::BOX_BYTES + over * 128 + x % chunks * 16, 0, 0, 0, 0);
           fence_proxy_async_smem();
           return true;
         };
         if (any) {
-          alive = chunk_step<D>(s_tm, o_tm, my_s, (cnt + j) & 1, my_p, j == 0, limit - j * C::BN, p.c, m_run, l_run, p.ctl, ab,
+          alive = chunk_step<D>(s_tm, o_tm, my_s, (cnt + i) & 1, my_p, i == 0, limit - j * C::BN, p.c, m_run, l_run, p.ctl, ab,
                                 before_p);
-        } else if (mbar_wait_warp(my_s, (cnt + j) & 1, p.ctl, ab) && before_p()) {  // a warp without rows keeps step
+        } else if (mbar_wait_warp(my_s, (cnt + i) & 1, p.ctl, ab) && before_p()) {  // a warp without rows keeps step
           mbar_arrive(my_p);
           mbar_arrive(my_p + 8);
         } else {
           alive = false;
         }
       }
-      alive = alive && (n == 0 || mbar_wait_warp(my_o, items & 1, p.ctl, ab));
-      tc_fence_after();
-      const int head = it.plane * p.gt + row_head;
-      const long long at = row ? (static_cast<long long>(it.qb + token) * p.Hq + head) * D : -1;
-      float* lse_at = row && p.lse ? p.lse + static_cast<size_t>(head) * p.total_q + it.qb + token : nullptr;
-      if (!it.cut()) {
-        if (alive && any) {
-          const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
-          const uint64_t inv2 = f2(inv, inv);
-          uint32_t w[D / 2];
-          if (n > 0) {
-#pragma unroll
-            for (int ch = 0; ch < D / 32; ch += 2) {
-              uint32_t rr[2][32];
-              tmem_ld32(o_tm + ch * 32, rr[0]);
-              tmem_ld32(o_tm + ch * 32 + 32, rr[1]);
-              tmem_wait_ld();
-              reg_fence32(rr[0]);
-              reg_fence32(rr[1]);
-#pragma unroll
-              for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                  const uint64_t x = mul2(f2(__uint_as_float(rr[u][2 * i]), __uint_as_float(rr[u][2 * i + 1])), inv2);
-                  w[(ch + u) * 16 + i] = pack_bf16x2(f2lo(x), f2hi(x));
-                }
-            }
-            tc_fence_before();
-            mbar_arrive(my_oe);  // O is in registers: the next item's P.V may overwrite it
-          } else {
-#pragma unroll
-            for (int i = 0; i < D / 2; ++i) w[i] = 0;
+      const bool both = !it.two && it.n1 > 0;
+      if (!it.two && t == 1) {
+        // the odd key tiles of a single tile: O stays in TMEM, m and l go to the even ones' warps
+        if (both) {
+          alive = alive && (shared == 0 || mbar_wait_warp(bar_mle, (shared - 1) & 1, p.ctl, ab));
+          if (alive) {
+            st_shared_f2(ml, m_run, l_run);
+            mbar_arrive(bar_ml);
+            alive = mbar_wait_warp(my_o, items & 1, p.ctl, ab);  // (a wait by parity may not miss a phase)
           }
-#pragma unroll
-          for (int h = 0; h < D / 64; ++h) store_rows(stg, w + 32 * h, at < 0 ? at : at + 64 * h, p.o);
-          if (lse_at) *lse_at = row_lse(m_run, l_run);
-        } else if (alive && n > 0) {
-          mbar_arrive(my_oe);
         }
       } else {
-        finish_piece<D>(p, ln, it, {at, lse_at, m_run, l_run, n > 0, row, any, alive}, o_tm, my_oe, stg, warp);
+        alive = alive && (n == 0 || mbar_wait_warp(my_o, items & 1, p.ctl, ab));
+        RowSums r{-1, nullptr, m_run, l_run, 1.f, 0.f, n > 0, both, any, alive};
+        if (both) {
+          alive = alive && mbar_wait_warp(bar_o + 8, items1 & 1, p.ctl, ab) && mbar_wait_warp(bar_ml, shared & 1, p.ctl, ab);
+          if (alive) {
+            const float2 other = ld_shared_f2(ml);
+            mbar_arrive(bar_mle);
+            r.m = fmaxf(m_run, other.x);
+            const float base = r.m == -INFINITY ? 0.f : r.m;
+            r.w0 = ex2(m_run - base);
+            r.w1 = ex2(other.x - base);
+            r.l = r.w0 * l_run + r.w1 * other.y;
+          }
+          r.alive = alive;
+        }
+        tc_fence_after();
+        if (row) {
+          const int head = it.plane * p.gt + row_head;
+          r.at = (static_cast<long long>(it.qb + token) * p.Hq + head) * D;
+          if (p.lse) r.lse_at = p.lse + static_cast<size_t>(head) * p.total_q + it.qb + token;
+        }
+        if (it.cut()) {
+          finish_piece<D>(p, ln, it, r, o_tm, my_oe, bar_oe + 8, warp);
+          counted += any;
+        } else if (alive && any) {
+          finish_unit<D>(p, r, o_tm, my_oe, bar_oe + 8, stg);
+        } else if (alive && n > 0) {
+          release_o(r, my_oe, bar_oe + 8);
+        }
       }
       cnt += n;
       items += n > 0;
-      pos += 2 * it.n;
+      pos += it.n;
+      shared += both;
+      items1 += it.n1 > 0;
+      give_item();
     }
   }
 
@@ -835,6 +1078,7 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
+  if (ab.raised() && warp < 8) count_rest(p, ln, static_cast<int>(start[0]), start[1], warp, counted);
 }
 
 // ---------------------------------------------------------------- host side
@@ -902,15 +1146,15 @@ int row_groups(int total_q, int gt) {
 
 constexpr size_t kCountBytes = 16384;  // counts of up to 256 CTAs
 
-// A launch's tag: 48 bits that no other launch of this process has and that memory holds by chance only.
-unsigned long long launch_tag() {
-  static std::atomic<unsigned long long> n{static_cast<unsigned long long>(
-      std::chrono::steady_clock::now().time_since_epoch().count())};
-  unsigned long long z = n.fetch_add(1) * 0x9E3779B97F4A7C15ull;
-  z ^= z >> 29;
-  z *= 0xBF58476D1CE4E5B9ull;
-  z ^= z >> 32;
-  return z << 16;
+// 48 bits that no other process has and that memory holds by chance only.
+unsigned long long process_tag() {
+  static const unsigned long long tag = [] {
+    unsigned long long z = static_cast<unsigned long long>(std::chrono::system_clock::now().time_since_epoch().count());
+    z = (z ^ z >> 31) * 0x9E3779B97F4A7C15ull;
+    z = (z ^ z >> 29) * 0xBF58476D1CE4E5B9ull;
+    return (z ^ z >> 32) << 16;
+  }();
+  return tag;
 }
 
 template <int D>
@@ -944,7 +1188,7 @@ cudaError_t launch_d(const ChunkArgs& a, const KernelCtl& ctl, cudaStream_t stre
   p.count = reinterpret_cast<unsigned long long*>(ws);
   p.part_ml = reinterpret_cast<float2*>(ws + kCountBytes);
   p.part = reinterpret_cast<float*>(ws + kCountBytes + static_cast<size_t>(2 * ctas) * p.groups * 32 * sizeof(float2));
-  p.tag = launch_tag();
+  p.tag = process_tag();
   p.B = a.B;
   p.Hq = a.Hq;
   p.Hkv = a.Hkv;
