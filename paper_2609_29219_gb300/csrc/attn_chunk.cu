@@ -42,7 +42,9 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kRescaleThreshold = 8.0f;  // base-2 units; P <= 2^8 between rescales
 
 // The line's units.  A key of a pair of tiles costs kKeyCost2, of a single tile kKeyCost1; a unit kUnitCost more.
-constexpr int kKeyCost2 = 8, kKeyCost1 = 6, kUnitCost = 1024;
+constexpr int kKeyCost2 = 8, kKeyCost1 = 4, kUnitCost = 3072;
+// The least that a CTA is given of units that are longer: they are not cut into shorter pieces.
+constexpr int kLeastStretch = 7168;
 
 template <int D>
 struct ChunkCfg {
@@ -62,8 +64,8 @@ struct ChunkCfg {
   static constexpr int NBAR = 4 + 4 * NR + 2 + 4 + 2 + 2 + 3 + 2 * NREC;
   static constexpr uint32_t REC_OFF = (BAR_OFF + NBAR * 8 + 15) / 16 * 16;  // [NREC] Item
   static constexpr uint32_t LINE_OFF = REC_OFF + NREC * 80;                 // Line, and the Walk to its start
-  static constexpr uint32_t SUM_OFF = LINE_OFF + 128;                       // the scan's sums, one per warp
-  static constexpr uint32_t TMEM_PTR_OFF = SUM_OFF + 16 * 8;
+  static constexpr uint32_t SUM_OFF = LINE_OFF + 96;  // the scan's sums, one per warp, and numbers of units
+  static constexpr uint32_t TMEM_PTR_OFF = SUM_OFF + THREADS / 32 * 12;
   static constexpr uint32_t ABORT_OFF = TMEM_PTR_OFF + 8;
   static constexpr uint32_t BYTES = ABORT_OFF + 16 + 1024;  // + alignment slack
   static constexpr uint32_t S_COL = 0;       // + t * BN
@@ -138,11 +140,14 @@ struct Line {
   long long W, x0, x1;
   long long each;  // W / G
   int rest, G;     // W % G
-  __device__ __forceinline__ void set(long long length, int ctas) {
+  __device__ __forceinline__ void set(long long length, int units, int ctas, int cta) {
     W = length;
     G = ctas;
+    if (units < ctas && W < static_cast<long long>(ctas) * kLeastStretch) G = max(max(1, units), static_cast<int>(W) / kLeastStretch);
     each = quotient(W, G);
     rest = static_cast<int>(W - each * G);
+    x0 = cta < G ? bound(cta) : W;
+    x1 = cta + 1 < G ? bound(cta + 1) : W;
   }
   // Where CTA c's stretch begins.
   __device__ __forceinline__ long long bound(int c) const { return each * c + static_cast<unsigned>(rest * c) / static_cast<unsigned>(G); }
@@ -213,11 +218,11 @@ __device__ __forceinline__ bool next_item(const ChunkParams& p, const Line& ln, 
   return false;
 }
 
-// The walk to this CTA's first unit: sequence b begins at `at`.
-__device__ __forceinline__ Walk walk_from(const ChunkParams& p, const Line& ln, int b, long long at) {
+// The walk to this CTA's first unit, from the sequence s, number b, that begins at `at`.
+__device__ __forceinline__ Walk walk_from(const ChunkParams& p, const Line& ln, int b, const Seq& s, long long at) {
   Walk w;
   w.b = b;
-  w.s = load_seq(p, b);
+  w.s = s;
   const long long plane = plane_cost(p, w.s);
   w.plane = static_cast<int>(quotient(ln.x0 - at, plane));
   const long long r = ln.x0 - at - w.plane * plane;
@@ -540,22 +545,21 @@ template <int D>
 __device__ __noinline__ void finish_unit(const ChunkParams& p, const RowSums r, uint32_t o_tm, uint32_t bar_oe, uint32_t bar_oe1,
                                          uint32_t stg) {
   const float inv = r.l == 0.f ? 0.f : 1.f / r.l;
-  uint32_t w[D / 2];
-  if (r.has) {
+#pragma unroll 1
+  for (int h = 0; h < D / 64; ++h) {  // (code that runs once a unit: the shorter, the sooner it is fetched)
+    uint32_t w[64];
+    if (r.has) {
+      load_o<D>(o_tm, 64 * h, r, inv, w);
+      load_o<D>(o_tm, 64 * h + 32, r, inv, w + 32);
 #pragma unroll
-    for (int ch = 0; ch < D / 32; ++ch) {
-      uint32_t rr[32];
-      load_o<D>(o_tm, ch * 32, r, inv, rr);
+      for (int i = 0; i < 32; ++i) w[i] = pack_bf16x2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+    } else {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) w[ch * 16 + i] = pack_bf16x2(__uint_as_float(rr[2 * i]), __uint_as_float(rr[2 * i + 1]));
+      for (int i = 0; i < 32; ++i) w[i] = 0;
     }
-    release_o(r, bar_oe, bar_oe1);
-  } else {
-#pragma unroll
-    for (int i = 0; i < D / 2; ++i) w[i] = 0;
+    if (r.has && h + 1 == D / 64) release_o(r, bar_oe, bar_oe1);
+    store_rows(stg, w, r.at < 0 ? r.at : r.at + 64 * h, p.o);
   }
-#pragma unroll
-  for (int h = 0; h < D / 64; ++h) store_rows(stg, w + 32 * h, r.at < 0 ? r.at : r.at + 64 * h, p.o);
   if (r.lse_at) *r.lse_at = row_lse(r.m, r.l);
 }
 
@@ -571,7 +575,7 @@ __device__ __noinline__ void finish_piece(const ChunkParams& p, const Line& ln, 
   if (r.alive && r.any) {
     float4* mine = reinterpret_cast<float4*>(p.part) + (static_cast<size_t>(slot) * p.groups + group) * (D / 4) * 32 + lane;
     if (r.has) {
-#pragma unroll
+#pragma unroll 1
       for (int ch = 0; ch < D / 32; ++ch) {
         uint32_t rr[32];
         load_o<D>(o_tm, ch * 32, r, 1.f, rr);
@@ -608,7 +612,7 @@ __device__ __noinline__ void finish_piece(const ChunkParams& p, const Line& ln, 
 // count is whole again at the launch's end: a captured launch may be replayed on this workspace.
 __device__ __noinline__ void count_rest(const ChunkParams& p, const Line& ln, int b, long long at, int warp, int counted) {
   if (ln.x0 >= ln.x1) return;
-  Walk w = walk_from(p, ln, b, at);
+  Walk w = walk_from(p, ln, b, load_seq(p, b), at);
   Item it;
   while (next_item(p, ln, w, it)) {
     // the warp's first row, if it has rows: as the softmax role has it
@@ -685,12 +689,15 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
   // The line's length, and the sequence in which this CTA's stretch begins: a prefix sum over the sequences.
   Line& ln = *reinterpret_cast<Line*>(smem + C::LINE_OFF);
   volatile long long* start = reinterpret_cast<volatile long long*>(smem + C::LINE_OFF + sizeof(Line));  // sequence, its place
-  static_assert(sizeof(Line) + 16 <= 128, "fits");
+  Seq& start_seq = *reinterpret_cast<Seq*>(smem + C::LINE_OFF + sizeof(Line) + 16);
+  static_assert(sizeof(Line) + 16 + sizeof(Seq) <= 96, "fits");
   {
     volatile long long* sums = reinterpret_cast<volatile long long*>(smem + C::SUM_OFF);
     constexpr int kWarps = C::THREADS / 32;
     Line l;
+    volatile int* unit_sums = reinterpret_cast<volatile int*>(smem + C::SUM_OFF + C::THREADS / 32 * 8);
     const int G = static_cast<int>(gridDim.x);
+    int units = 0;
     l.x0 = 0;
     const bool one = p.B <= C::THREADS;
     // (one round: the sum of all and this CTA's sequence from the same scan; else a round for each)
@@ -699,14 +706,21 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
       for (int b0 = 0; b0 < p.B; b0 += C::THREADS) {
         const int b = b0 + static_cast<int>(threadIdx.x);
         long long cost = 0;
-        if (b < p.B) cost = p.planes * plane_cost(p, load_seq(p, b));
+        int n = 0;
+        Seq s;
+        if (b < p.B) {
+          s = load_seq(p, b);
+          cost = p.planes * plane_cost(p, s);
+          n = min(s.pairs, 1 << 15) * min(p.planes, 1 << 10);  // (more than there are CTAs is enough)
+        }
+        n = __reduce_add_sync(0xffffffffu, min(n, 1 << 15));
         long long x = cost;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
           const long long y = __shfl_up_sync(0xffffffffu, x, d);
           if (lane >= d) x += y;
         }
-        if (lane == 31) sums[warp] = x;
+        if (lane == 31) sums[warp] = x, unit_sums[warp] = n;
         __syncthreads();
         long long all = 0;
         x += before - cost;
@@ -715,24 +729,23 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
           const long long y = sums[i];
           if (i < warp) x += y;
           all += y;
+          if (round == 0) units = min(units + unit_sums[i], 1 << 20);
         }
         if (one) {
-          l.set(all, G);
-          l.x0 = l.bound(blockIdx.x);
+          l.set(all, units, G, blockIdx.x);
         }
         if ((one || round == 1) && x <= l.x0 && l.x0 < x + cost) {
           start[0] = b;
           start[1] = x;
+          start_seq = s;
         }
         before += all;
         __syncthreads();
       }
       if (!one && round == 0) {
-        l.set(before, G);
-        l.x0 = l.bound(blockIdx.x);
+        l.set(before, units, G, blockIdx.x);
       }
     }
-    l.x1 = static_cast<int>(blockIdx.x) + 1 < G ? l.bound(blockIdx.x + 1) : l.W;
     if (threadIdx.x == 0) ln = l;
   }
   tc_fence_before();
@@ -760,7 +773,7 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
     Walk walk;
     walk.b = p.B;
     const Line l = ln;
-    if (l.x0 < l.x1) walk = walk_from(p, l, static_cast<int>(start[0]), start[1]);
+    if (l.x0 < l.x1) walk = walk_from(p, l, static_cast<int>(start[0]), start_seq, start[1]);
     bool more = true;
     for (int k = 0; more; ++k) {
       Item it;
@@ -785,12 +798,13 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
     }
     const uint32_t full = bar_full + (is_v ? 8 * C::NR : 0), empty = bar_empty + (is_v ? 8 * C::NR : 0);
     const uint32_t ring = sbase + C::RING_OFF + (is_v ? C::NR * C::TILE_BYTES : 0);
-    int pos = 0, issued = 0, skipped = -1, q_issued[2] = {0, 0};
+    int pos = 0, issued = 0, skipped = -1, q_issued0 = 0, q_issued1 = 0;
     bool ok = true;
     const int rows = min(p.page, 64), rows_lg = 31 - __clz(rows);  // (8, 16, 32 or 64)
     const uint32_t q_bytes = static_cast<uint32_t>(C::NBOX * p.tq * p.gt * 128);
+    int q_single = 0;  // the Q tile that the next single tile takes: they take turns
     const auto load_q = [&](int t, int plane, int token) -> bool {
-      const int n = q_issued[t];
+      const int n = t ? q_issued1 : q_issued0;
       if (n > 0 && !mbar_wait_warp(bar_qe + 8 * t, (n - 1) & 1, p.ctl, ab)) return false;
       if (lane == 0) {
         mbar_expect_tx(bar_q + 8 * t, q_bytes);
@@ -798,7 +812,7 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
           tma_load_4d(sbase + C::Q_OFF + t * C::TILE_BYTES + x * C::BOX_BYTES, &tm_q, x * 64, 0, plane, token, bar_q + 8 * t);
       }
       __syncwarp();
-      q_issued[t] = n + 1;
+      (t ? q_issued1 : q_issued0) = n + 1;
       return true;
     };
     const Item* rec;
@@ -814,7 +828,8 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
         return lane * rows < C::BN && key < skv ? table[static_cast<unsigned>(key) / static_cast<unsigned>(p.page)] : -1;
       };
       int page = page_of(lo);
-      if (!is_v && n0 > 0 && !(ok = load_q(0, plane, token))) break;
+      if (!is_v && n0 > 0 && !(ok = load_q(two ? 0 : q_single, plane, token))) break;
+      q_single ^= !two;
       const int hk = plane / p.planes_per_kv;
       for (int j = lo; j < end; ++j, ++pos) {
         const int slot = pos % C::NR;
@@ -845,8 +860,8 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
     // drain copies still in flight before the CTA may exit
     if (lane == 0) {
       Abort no_abort{ab.flag + 1};
-      for (int t = 0; t < 2; ++t)
-        if (q_issued[t] > 0) mbar_wait(bar_q + 8 * t, (q_issued[t] - 1) & 1, p.ctl, no_abort);
+      if (q_issued0 > 0) mbar_wait(bar_q, (q_issued0 - 1) & 1, p.ctl, no_abort);
+      if (q_issued1 > 0) mbar_wait(bar_q + 8, (q_issued1 - 1) & 1, p.ctl, no_abort);
       for (int ps = max(0, issued - C::NR); ps < issued; ++ps)
         if (ps != skipped) mbar_wait(full + 8 * (ps % C::NR), (ps / C::NR) & 1, p.ctl, no_abort);
     }
@@ -870,7 +885,7 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
         mma_ss_k64_el(tmem + C::S_COL + t * C::BN, a + x * kBox16, b + x * kBox16, idesc_s, x > 0);
       tc_commit_el(bar_s + 8 * t);
     };
-    int q1 = 0;                                       // items so far with two query tiles
+    int q0 = 0, q1 = 0, q_single = 0;  // loads so far of Q tile 0 and 1; the one that the next single tile takes
     // key tiles so far; steps of S, P and O number 0 and 1, items that had some (no arrays: number t is not
     // always a constant, and they would go to local memory)
     int pos = 0, cnt0 = 0, cnt1 = 0, items0 = 0, items1 = 0;
@@ -893,12 +908,12 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
     // softmax runs.  Tile 0 stops at its own diagonal.
     const auto two_tiles = [&](int n0, int n) -> bool {
       if (n0 > 0) {
-        if (!mbar_wait_warp(bar_q, items0 & 1, p.ctl, ab) || !wait_k(pos)) return false;
+        if (!mbar_wait_warp(bar_q, q0++ & 1, p.ctl, ab) || !wait_k(pos)) return false;
         tc_fence_after();
         issue_s(0, 0, pos);
         if (n0 == 1) tc_commit_el(bar_qe);  // every S of tile 0 issued
       }
-      if (!mbar_wait_warp(bar_q + 8, q1 & 1, p.ctl, ab) || (n0 == 0 && !wait_k(pos))) return false;
+      if (!mbar_wait_warp(bar_q + 8, q1++ & 1, p.ctl, ab) || (n0 == 0 && !wait_k(pos))) return false;
       tc_fence_after();
       issue_s(1, 1, pos);
       free_k(pos);
@@ -935,15 +950,17 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
     };
     // One query tile: key tile j goes the way of number j % 2.
     const auto one_tile = [&](int n) -> bool {
+      const int q = q_single, loads = q ? q1++ : q0++;
+      q_single ^= 1;
       const auto next_s = [&](int j) -> bool {
         if (!wait_k(pos + j)) return false;
         tc_fence_after();
-        issue_s(j & 1, 0, pos + j);
+        issue_s(j & 1, q, pos + j);
         free_k(pos + j);
-        if (j + 1 == n) tc_commit_el(bar_qe);
+        if (j + 1 == n) tc_commit_el(bar_qe + 8 * q);
         return true;
       };
-      if (!mbar_wait_warp(bar_q, items0 & 1, p.ctl, ab) || !next_s(0) || (n > 1 && !next_s(1))) return false;
+      if (!mbar_wait_warp(bar_q + 8 * q, loads & 1, p.ctl, ab) || !next_s(0) || (n > 1 && !next_s(1))) return false;
       for (int j = 0; j < n; ++j) {
         if (!wait_v(pos + j) || !issue_pv(j & 1, pos + j, j >> 1)) return false;
         free_v(pos + j);
@@ -963,7 +980,6 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
       pos += n;
       items0 += n0 > 0;
       items1 += n1 > 0;
-      q1 += two;
     }
     // wait for every MMA issued above before TMEM may be released
     Abort no_abort{ab.flag + 1};
