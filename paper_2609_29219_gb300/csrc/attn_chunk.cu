@@ -41,8 +41,8 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kRescaleThreshold = 8.0f;  // base-2 units; P <= 2^8 between rescales
 
-// The line's units.  A key of a pair of tiles costs kKeyCost2, of a single tile kKeyCost1; a unit kUnitCost more.
-constexpr int kKeyCost2 = 8, kKeyCost1 = 4, kUnitCost = 3072;
+// The line's units: a key of a pair of tiles costs 1 << kKeyLg2, of a single tile 1 << kKeyLg1; a unit kUnitCost more.
+constexpr int kKeyLg2 = 3, kKeyLg1 = 2, kUnitCost = 3072;
 // The least that a CTA is given of units that are longer: they are not cut into shorter pieces.
 constexpr int kLeastStretch = 7168;
 
@@ -114,11 +114,11 @@ __device__ __forceinline__ int keys_until(const ChunkParams& p, const Seq& s, lo
   if (!p.causal) return s.skv;
   return static_cast<int>(max(0ll, min(end, static_cast<long long>(s.sq)) + s.skv - s.sq));
 }
-__device__ __forceinline__ int key_cost(const ChunkParams& p, const Seq& s, int pair) {
-  return s.sq - 2ll * p.tq * pair > p.tq ? kKeyCost2 : kKeyCost1;
+__device__ __forceinline__ int key_lg(const ChunkParams& p, const Seq& s, int pair) {
+  return s.sq - 2ll * p.tq * pair > p.tq ? kKeyLg2 : kKeyLg1;
 }
 __device__ __forceinline__ long long unit_cost(const ChunkParams& p, const Seq& s, int pair) {
-  return kUnitCost + static_cast<long long>(key_cost(p, s, pair)) * keys_until(p, s, 2ll * p.tq * (pair + 1));
+  return kUnitCost + (static_cast<long long>(keys_until(p, s, 2ll * p.tq * (pair + 1))) << key_lg(p, s, pair));
 }
 // Cost of a plane's pairs before pair i < pairs (all of them of two tiles, none past the sequence's end).
 __device__ __forceinline__ long long cost_before(const ChunkParams& p, const Seq& s, int i) {
@@ -130,7 +130,7 @@ __device__ __forceinline__ long long cost_before(const ChunkParams& p, const Seq
     const long long n = i - j0;
     keys = n > 0 ? n * off + step * ((j0 + 1 + i) * n / 2) : 0;
   }
-  return static_cast<long long>(i) * kUnitCost + kKeyCost2 * keys;
+  return static_cast<long long>(i) * kUnitCost + (keys << kKeyLg2);
 }
 __device__ __forceinline__ long long plane_cost(const ChunkParams& p, const Seq& s) {
   return s.pairs ? cost_before(p, s, s.pairs - 1) + unit_cost(p, s, s.pairs - 1) : 0;
@@ -153,12 +153,9 @@ struct Line {
   __device__ __forceinline__ long long bound(int c) const { return each * c + static_cast<unsigned>(rest * c) / static_cast<unsigned>(G); }
 };
 // Key tiles of a unit that lie before the place d > 0 behind its beginning.
-__device__ __forceinline__ int tiles_before(long long d, int key, int tiles) {
-  d -= kUnitCost;
-  if (d <= 0) return 0;
-  const unsigned long long u = static_cast<unsigned long long>(d);
-  const long long t = key == kKeyCost2 ? (u + kKeyCost2 * 128 - 1) / (kKeyCost2 * 128) : (u + kKeyCost1 * 128 - 1) / (kKeyCost1 * 128);
-  return t < tiles ? static_cast<int>(t) : tiles;
+__device__ __forceinline__ int tiles_before(long long d, int key_lg, int tiles) {
+  const long long t = (d - kUnitCost + (128 << key_lg) - 1) >> (key_lg + 7);
+  return t < 0 ? 0 : t < tiles ? static_cast<int>(t) : tiles;
 }
 
 // A place on the line: unit `pair` of a plane of sequence b, which begins at `at`.
@@ -174,7 +171,7 @@ struct Item {
   int n0, n1;                     // of these, the steps of S, P and O number 0 and number 1
   int tiles;                      // all its key tiles
   int two;                        // it has two query tiles
-  int key, pad;                   // a key's cost
+  int key_lg, pad;                // a key's cost
   long long at, cost;             // its place on the line
   __device__ __forceinline__ bool cut() const { return n < tiles; }
 };
@@ -182,6 +179,7 @@ static_assert(sizeof(Item) == 72, "fits its record");
 
 // The CTA's next piece, and the walk behind it; false past the stretch's end.
 __device__ __forceinline__ bool next_item(const ChunkParams& p, const Line& ln, Walk& w, Item& it) {
+#pragma unroll 1
   while (w.b < p.B && w.at < ln.x1) {
     const long long step = 2ll * p.tq;
     it.b = w.b;
@@ -191,13 +189,13 @@ __device__ __forceinline__ bool next_item(const ChunkParams& p, const Line& ln, 
     it.skv = w.s.skv;
     it.t0 = static_cast<int>(step * w.pair);
     it.two = w.s.sq - it.t0 > p.tq;
-    it.key = it.two ? kKeyCost2 : kKeyCost1;
+    it.key_lg = it.two ? kKeyLg2 : kKeyLg1;
     const int keys = keys_until(p, w.s, step * (w.pair + 1));
     it.tiles = (keys + 127) / 128;
     it.at = w.at;
-    it.cost = kUnitCost + static_cast<long long>(it.key) * keys;
-    it.lo = ln.x0 > it.at ? tiles_before(ln.x0 - it.at, it.key, it.tiles) : 0;
-    const int hi = ln.x1 < it.at + it.cost ? tiles_before(ln.x1 - it.at, it.key, it.tiles) : it.tiles;
+    it.cost = kUnitCost + (static_cast<long long>(keys) << it.key_lg);
+    it.lo = ln.x0 > it.at ? tiles_before(ln.x0 - it.at, it.key_lg, it.tiles) : 0;
+    const int hi = ln.x1 < it.at + it.cost ? tiles_before(ln.x1 - it.at, it.key_lg, it.tiles) : it.tiles;
     it.n = hi - it.lo;
     it.n0 = it.two ? max(0, min(hi, (keys_until(p, w.s, it.t0 + p.tq) + 127) / 128) - it.lo) : (it.n + 1) / 2;
     it.n1 = it.two ? it.n : it.n / 2;
@@ -206,6 +204,7 @@ __device__ __forceinline__ bool next_item(const ChunkParams& p, const Line& ln, 
       w.pair = 0;
       if (++w.plane == p.planes) {
         w.plane = 0;
+#pragma unroll 1
         while (++w.b < p.B) {
           w.s = load_seq(p, w.b);
           if (w.s.pairs) break;
@@ -227,6 +226,7 @@ __device__ __forceinline__ Walk walk_from(const ChunkParams& p, const Line& ln, 
   w.plane = static_cast<int>(quotient(ln.x0 - at, plane));
   const long long r = ln.x0 - at - w.plane * plane;
   int lo = 0, hi = w.s.pairs;  // the last pair that begins at r or before
+#pragma unroll 1
   while (hi - lo > 1) {
     const int mid = (lo + hi) / 2;
     if (cost_before(p, w.s, mid) <= r)
@@ -243,10 +243,13 @@ __device__ __forceinline__ Walk walk_from(const ChunkParams& p, const Line& ln, 
 // are their CTAs' first), and which of the 32 CTAs from `from` on have one.
 __device__ __forceinline__ int first_cta(const Line& ln, const Item& it) {
   int c = min(ln.G - 1, static_cast<int>(static_cast<float>(it.at) / static_cast<float>(ln.W) * ln.G));
+#pragma unroll 1
   while (c > 0 && ln.bound(c) > it.at) --c;
+#pragma unroll 1
   while (c + 1 < ln.G && ln.bound(c + 1) <= it.at) ++c;
   // (it may begin in a stretch that holds none of its key tiles)
-  while (c + 1 < ln.G && tiles_before(ln.bound(c + 1) - it.at, it.key, it.tiles) == 0) ++c;
+#pragma unroll 1
+  while (c + 1 < ln.G && tiles_before(ln.bound(c + 1) - it.at, it.key_lg, it.tiles) == 0) ++c;
   return c;
 }
 __device__ __forceinline__ uint32_t piece_ctas(const Line& ln, const Item& it, int from) {
@@ -254,8 +257,8 @@ __device__ __forceinline__ uint32_t piece_ctas(const Line& ln, const Item& it, i
   bool has = false;
   if (c < ln.G) {
     const long long begin = ln.bound(c) - it.at, end = (c + 1 < ln.G ? ln.bound(c + 1) : ln.W) - it.at;
-    const int lo = begin > 0 ? tiles_before(begin, it.key, it.tiles) : 0;
-    const int hi = end < it.cost ? tiles_before(end, it.key, it.tiles) : it.tiles;
+    const int lo = begin > 0 ? tiles_before(begin, it.key_lg, it.tiles) : 0;
+    const int hi = end < it.cost ? tiles_before(end, it.key_lg, it.tiles) : it.tiles;
     has = end > 0 && begin < it.cost && lo < hi;
   }
   return __ballot_sync(0xffffffffu, has);
@@ -266,6 +269,7 @@ struct Pieces {
   uint32_t ctas;  // of the 32 before `from` that are yet to come
   __device__ __forceinline__ explicit Pieces(int first_cta) : first(first_cta), from(first_cta), ctas(0) {}
   __device__ __forceinline__ int next(const Line& ln, const Item& it) {
+#pragma unroll 1
     while (!ctas) {
       if (from >= ln.G || ln.bound(from) >= it.at + it.cost) return -1;
       ctas = piece_ctas(ln, it, from);
@@ -276,6 +280,15 @@ struct Pieces {
     return c == first ? 2 * c + 1 : 2 * c;
   }
 };
+
+// mbar_wait_warp as a call: in line at each of the roles' waits it made the kernel twice as long as the
+// instruction cache, and what runs once a unit was fetched anew each time.
+__device__ __noinline__ bool wait_long(uint32_t bar, uint32_t parity, const KernelCtl& ctl, const Abort& ab) {
+  return mbar_wait_warp(bar, parity, ctl, ab);
+}
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, const KernelCtl& ctl, const Abort& ab) {
+  return __all_sync(0xffffffffu, mbar_try_wait(bar, parity)) || wait_long(bar, parity, ctl, ab);
+}
 
 // ---------------------------------------------------------------- softmax
 // One online-softmax step of one query row (this thread's TMEM lane) over a 128-key tile of S in TMEM at
@@ -527,6 +540,7 @@ __device__ __forceinline__ void join_pieces(const ChunkParams& p, const Line& ln
 // Counts a piece of this warp's rows of a cut unit; true for the last to come.
 __device__ __forceinline__ bool last_piece(const ChunkParams& p, const Line& ln, const Item& it, int first, int warp) {
   int pieces = 0, come = 0;
+#pragma unroll 1
   for (int from = first; from < ln.G; from += 32) {
     if (ln.bound(from) >= it.at + it.cost) break;
     pieces += __popc(piece_ctas(ln, it, from));
@@ -602,10 +616,7 @@ __device__ __noinline__ void finish_piece(const ChunkParams& p, const Line& ln, 
   const int lg = rows > 1 ? 32 - __clz(rows - 1) : 0;
   const float2* ml = p.part_ml + group * 32;
   const float4* part = reinterpret_cast<const float4*>(p.part) + static_cast<size_t>(group) * (D / 4) * 32;
-  if (lg <= 2)
-    join_pieces<D, 4, 6>(p, ln, it, first, ml, part, rows, lg, r);
-  else
-    join_pieces<D, 8, 3>(p, ln, it, first, ml, part, rows, lg, r);
+  join_pieces<D, 8, 3>(p, ln, it, first, ml, part, rows, lg, r);
 }
 
 // After a wait has given up, a softmax warp counts the pieces that it has not brought all the same, so that every
@@ -677,6 +688,7 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
   // rows of the Q tiles that no load fills (a tile has tq gt rows): zeros, so that their scores are too
   {
     const int rows = p.tq * p.gt, n = (C::BM - rows) * 8;
+#pragma unroll 1
     for (int i = threadIdx.x; i < 2 * C::NBOX * n; i += C::THREADS)
       st_shared_v4(sbase + C::Q_OFF + i / n * C::BOX_BYTES + rows * 128 + i % n * 16, 0, 0, 0, 0);
     fence_proxy_async_smem();
@@ -701,8 +713,10 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
     l.x0 = 0;
     const bool one = p.B <= C::THREADS;
     // (one round: the sum of all and this CTA's sequence from the same scan; else a round for each)
+#pragma unroll 1
     for (int round = 0; round < (one ? 1 : 2); ++round) {
       long long before = 0;
+#pragma unroll 1
       for (int b0 = 0; b0 < p.B; b0 += C::THREADS) {
         const int b = b0 + static_cast<int>(threadIdx.x);
         long long cost = 0;
@@ -758,7 +772,7 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
   int rec_n = 0, counted = 0;  // counted: (softmax warps) pieces of cut units that this warp has counted
   const auto take_item = [&]() -> const Item* {
     const int i = rec_n % C::NREC;
-    if (!mbar_wait_warp(bar_rec + 8 * i, (rec_n / C::NREC) & 1, p.ctl, ab)) return nullptr;
+    if (!wait_warp(bar_rec + 8 * i, (rec_n / C::NREC) & 1, p.ctl, ab)) return nullptr;
     const Item* it = reinterpret_cast<const Item*>(smem + C::REC_OFF + i * 80);
     return *reinterpret_cast<const volatile int*>(&it->n) < 0 ? nullptr : it;
   };
@@ -775,12 +789,13 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
     const Line l = ln;
     if (l.x0 < l.x1) walk = walk_from(p, l, static_cast<int>(start[0]), start_seq, start[1]);
     bool more = true;
+#pragma unroll 1
     for (int k = 0; more; ++k) {
       Item it;
       more = next_item(p, l, walk, it);
       if (!more) it.n = -1;
       const int i = k % C::NREC;
-      if (k >= C::NREC && !mbar_wait_warp(bar_rece + 8 * i, (k / C::NREC - 1) & 1, p.ctl, ab)) break;
+      if (k >= C::NREC && !wait_warp(bar_rece + 8 * i, (k / C::NREC - 1) & 1, p.ctl, ab)) break;
       if (lane == 0) {
         *reinterpret_cast<Item*>(smem + C::REC_OFF + i * 80) = it;
         mbar_arrive(bar_rec + 8 * i);
@@ -805,7 +820,7 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
     int q_single = 0;  // the Q tile that the next single tile takes: they take turns
     const auto load_q = [&](int t, int plane, int token) -> bool {
       const int n = t ? q_issued1 : q_issued0;
-      if (n > 0 && !mbar_wait_warp(bar_qe + 8 * t, (n - 1) & 1, p.ctl, ab)) return false;
+      if (n > 0 && !wait_warp(bar_qe + 8 * t, (n - 1) & 1, p.ctl, ab)) return false;
       if (lane == 0) {
         mbar_expect_tx(bar_q + 8 * t, q_bytes);
         for (int x = 0; x < C::NBOX; ++x)
@@ -831,9 +846,10 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
       if (!is_v && n0 > 0 && !(ok = load_q(two ? 0 : q_single, plane, token))) break;
       q_single ^= !two;
       const int hk = plane / p.planes_per_kv;
+#pragma unroll 1
       for (int j = lo; j < end; ++j, ++pos) {
         const int slot = pos % C::NR;
-        if (pos >= C::NR && !(ok = mbar_wait_warp(empty + 8 * slot, (pos / C::NR - 1) & 1, p.ctl, ab))) break;
+        if (pos >= C::NR && !(ok = wait_warp(empty + 8 * slot, (pos / C::NR - 1) & 1, p.ctl, ab))) break;
         issued = pos + 1;
         if (p.ctl.inject == 5 && !is_v && pos == 1) {  // test hook: never load this tile
           skipped = pos;
@@ -873,10 +889,11 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
     const uint64_t dk0 = sdesc_sw128(sbase + C::RING_OFF, 16, 1024);
     const uint64_t dv0 = sdesc_sw128(sbase + C::RING_OFF + C::NR * C::TILE_BYTES, C::BOX_BYTES, 1024);
     constexpr uint32_t kTile16 = C::TILE_BYTES >> 4, kBox16 = C::BOX_BYTES >> 4;
-    const auto wait_k = [&](int n) { return mbar_wait_warp(bar_full + 8 * (n % C::NR), (n / C::NR) & 1, p.ctl, ab); };
-    const auto wait_v = [&](int n) { return mbar_wait_warp(bar_full + 8 * (C::NR + n % C::NR), (n / C::NR) & 1, p.ctl, ab); };
-    const auto free_k = [&](int n) { tc_commit_el(bar_empty + 8 * (n % C::NR)); };
-    const auto free_v = [&](int n) { tc_commit_el(bar_empty + 8 * (C::NR + n % C::NR)); };
+    const auto wait_k = [&](int n) { return wait_warp(bar_full + 8 * (n % C::NR), (n / C::NR) & 1, p.ctl, ab); };
+    const auto wait_v = [&](int n) { return wait_warp(bar_full + 8 * (C::NR + n % C::NR), (n / C::NR) & 1, p.ctl, ab); };
+    int q0 = 0, q1 = 0, q_single = 0;  // loads so far of Q tile 0 and 1; the one that the next single tile takes
+    int pos = 0;                       // key tiles so far
+    int cnt0 = 0, cnt1 = 0, items0 = 0, items1 = 0;  // steps of S, P and O number 0 and 1, items that had some
     // S_t = Q K^T with the query tile q and K number n
     const auto issue_s = [&](int t, int q, int n) {
       const uint64_t a = dq0 + q * kTile16, b = dk0 + (n % C::NR) * kTile16;
@@ -885,87 +902,70 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
         mma_ss_k64_el(tmem + C::S_COL + t * C::BN, a + x * kBox16, b + x * kBox16, idesc_s, x > 0);
       tc_commit_el(bar_s + 8 * t);
     };
-    int q0 = 0, q1 = 0, q_single = 0;  // loads so far of Q tile 0 and 1; the one that the next single tile takes
-    // key tiles so far; steps of S, P and O number 0 and 1, items that had some (no arrays: number t is not
-    // always a constant, and they would go to local memory)
-    int pos = 0, cnt0 = 0, cnt1 = 0, items0 = 0, items1 = 0;
-    // O_t += P_t V with V number n, the half written first as soon as it is there; step j of the item's
-    const auto issue_pv = [&](int t, int n, int j) -> bool {
+    // O_t += P_t V with V number n, the half written first as soon as it is there; step i of number t's
+    const auto issue_pv = [&](int t, int n, int i) -> bool {
       const uint64_t b = dv0 + (n % C::NR) * kTile16;
       const int cnt = t ? cnt1 : cnt0, items = t ? items1 : items0;
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        if (!mbar_wait_warp(bar_p + 16 * t + 8 * half, (cnt + j) & 1, p.ctl, ab)) return false;
+        if (!wait_warp(bar_p + 16 * t + 8 * half, (cnt + i) & 1, p.ctl, ab)) return false;
         // O_t of the item before must have been read out
-        if (half == 0 && j == 0 && items > 0 && !mbar_wait_warp(bar_oe + 8 * t, (items - 1) & 1, p.ctl, ab)) return false;
+        if (half == 0 && i == 0 && items > 0 && !wait_warp(bar_oe + 8 * t, (items - 1) & 1, p.ctl, ab)) return false;
         tc_fence_after();
         mma_ts_k64_el(tmem + C::O_COL + t * D, tmem + C::S_COL + t * C::BN + half * 32, b + half * 64 * (128 >> 4), idesc_pv,
-                      j > 0 || half > 0 ? 1u : 0u);
+                      i > 0 || half > 0 ? 1u : 0u);
       }
       return true;
     };
-    // Two query tiles: S0 S1 | PV0 S0' | PV1 S1' | ...: the tensor pipe works on one tile while the other's
-    // softmax runs.  Tile 0 stops at its own diagonal.
+    const auto free_slot = [&](int ring, int n) { tc_commit_el(bar_empty + 8 * (ring * C::NR + n % C::NR)); };
+    // The items' loops have one place each that issues a number's S and P.V (the MMAs take 36 instructions each,
+    // and a prologue and an end of their own doubled that); the first steps are only S.
+    // Two query tiles: S0 S1 | PV0 S0' | PV1 S1' | ...: the tensor pipe works on one tile while the other's softmax
+    // runs.  Tile 0 stops at its own diagonal.
     const auto two_tiles = [&](int n0, int n) -> bool {
-      if (n0 > 0) {
-        if (!mbar_wait_warp(bar_q, q0++ & 1, p.ctl, ab) || !wait_k(pos)) return false;
-        tc_fence_after();
-        issue_s(0, 0, pos);
-        if (n0 == 1) tc_commit_el(bar_qe);  // every S of tile 0 issued
-      }
-      if (!mbar_wait_warp(bar_q + 8, q1++ & 1, p.ctl, ab) || (n0 == 0 && !wait_k(pos))) return false;
-      tc_fence_after();
-      issue_s(1, 1, pos);
-      free_k(pos);
-      if (n == 1) tc_commit_el(bar_qe + 8);
-      if (!wait_v(pos)) return false;
-      for (int j = 0; j < n; ++j) {
-        const bool more = j + 1 < n;
-        if (j < n0) {
-          if (!issue_pv(0, pos + j, j)) return false;
-          if (j + 1 == n0) tc_commit_el(bar_o);
-        }
-        if (more) {
-          if (!wait_k(pos + j + 1)) return false;
-          tc_fence_after();
-          if (j + 1 < n0) {
-            issue_s(0, 0, pos + j + 1);
-            if (j + 2 == n0) tc_commit_el(bar_qe);
+#pragma unroll 1
+      for (int i = -1; i < n; ++i) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const int nt = t ? n : n0;
+          if (i >= 0 && i < nt) {
+            if (!issue_pv(t, pos + i, i)) return false;
+            if (i + 1 == nt) tc_commit_el(bar_o + 8 * t);
+            if (t == 1) free_slot(1, pos + i);
           }
-        }
-        if (!issue_pv(1, pos + j, j)) return false;
-        free_v(pos + j);
-        if (!more) {
-          tc_commit_el(bar_o + 8);
-        } else {
+          if (i + 1 >= nt) continue;
+          if (i < 0 && !wait_warp(bar_q + 8 * t, (t ? q1++ : q0++) & 1, p.ctl, ab)) return false;
+          if ((t == 0 || n0 <= i + 1) && !wait_k(pos + i + 1)) return false;
           // (the next V is awaited while P.V keeps the tensor pipe busy; at D = 64 that would hold S back)
-          if (D == 128 && !wait_v(pos + j + 1)) return false;
-          issue_s(1, 1, pos + j + 1);
-          free_k(pos + j + 1);
-          if (j + 2 == n) tc_commit_el(bar_qe + 8);
-          if (D != 128 && !wait_v(pos + j + 1)) return false;
+          if (D == 128 && t == 1 && i >= 0 && !wait_v(pos + i + 1)) return false;
+          tc_fence_after();
+          issue_s(t, t, pos + i + 1);
+          if (t == 1) free_slot(0, pos + i + 1);
+          if (i + 2 == nt) tc_commit_el(bar_qe + 8 * t);  // the Q tile's last S of the item
+          if (t == 1 && (D != 128 || i < 0) && !wait_v(pos + i + 1)) return false;
         }
       }
       return true;
     };
-    // One query tile: key tile j goes the way of number j % 2.
+    // One query tile: key tile x goes the way of number x % 2.
     const auto one_tile = [&](int n) -> bool {
-      const int q = q_single, loads = q ? q1++ : q0++;
+      const int q = q_single;
       q_single ^= 1;
-      const auto next_s = [&](int j) -> bool {
-        if (!wait_k(pos + j)) return false;
+#pragma unroll 1
+      for (int x = -2; x < n; ++x) {
+        const int t = x & 1, k = x + 2;
+        if (x >= 0) {
+          if (!wait_v(pos + x) || !issue_pv(t, pos + x, x >> 1)) return false;
+          free_slot(1, pos + x);
+          if (k >= n) tc_commit_el(bar_o + 8 * t);
+        }
+        if (k >= n) continue;
+        if (k == 0 && !wait_warp(bar_q + 8 * q, (q ? q1++ : q0++) & 1, p.ctl, ab)) return false;
+        if (!wait_k(pos + k)) return false;
         tc_fence_after();
-        issue_s(j & 1, q, pos + j);
-        free_k(pos + j);
-        if (j + 1 == n) tc_commit_el(bar_qe + 8 * q);
-        return true;
-      };
-      if (!mbar_wait_warp(bar_q + 8 * q, loads & 1, p.ctl, ab) || !next_s(0) || (n > 1 && !next_s(1))) return false;
-      for (int j = 0; j < n; ++j) {
-        if (!wait_v(pos + j) || !issue_pv(j & 1, pos + j, j >> 1)) return false;
-        free_v(pos + j);
-        if (j + 2 >= n) tc_commit_el(bar_o + 8 * (j & 1));
-        if (j + 2 < n && !next_s(j + 2)) return false;
+        issue_s(t, q, pos + k);
+        free_slot(0, pos + k);
+        if (k + 1 == n) tc_commit_el(bar_qe + 8 * q);
       }
       return true;
     };
@@ -984,7 +984,7 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
     // wait for every MMA issued above before TMEM may be released
     Abort no_abort{ab.flag + 1};
     tc_commit_el(bar_drain);
-    mbar_wait_warp(bar_drain, 0, p.ctl, no_abort);
+    wait_warp(bar_drain, 0, p.ctl, no_abort);
   } else {
     // ------------------------------------------------------------------ softmax
     const int t = warp >> 2;                         // S, P and O number t are this warpgroup's
@@ -1013,14 +1013,16 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
       const int over = it.skv - (it.lo + it.n - 1) * C::BN;  // keys of the last tile
       const bool clears = over < C::BN && (it.two ? (t == 0 ? it.n0 == it.n : it.n0 < it.n) : t == ((it.n - 1) & 1));
       float m_run = -INFINITY, l_run = 0.f;
+#pragma unroll 1
       for (int i = 0; alive && i < n; ++i) {
         const int j = it.two ? i : 2 * i + t;  // key tile
         const auto before_p = [&]() -> bool {
           if (!clears || j + 1 < it.n) return true;
           const int vn = pos + j, slot = vn % C::NR;
-          if (!mbar_wait_warp(bar_full + 8 * (C::NR + slot), (vn / C::NR) & 1, p.ctl, ab)) return false;
+          if (!wait_warp(bar_full + 8 * (C::NR + slot), (vn / C::NR) & 1, p.ctl, ab)) return false;
           const uint32_t v = sbase + C::RING_OFF + (C::NR + slot) * C::TILE_BYTES;
           const int chunks = (C::BN - over) * 8;
+#pragma unroll 1
           for (int x = row_in_tile; x < C::NBOX * chunks; x += C::BM)
             st_shared_v4(v + x / chunks * C::BOX_BYTES + over * 128 + x % chunks * 16, 0, 0, 0, 0);
           fence_proxy_async_smem();
@@ -1029,7 +1031,7 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
         if (any) {
           alive = chunk_step<D>(s_tm, o_tm, my_s, (cnt + i) & 1, my_p, i == 0, limit - j * C::BN, p.c, m_run, l_run, p.ctl, ab,
                                 before_p);
-        } else if (mbar_wait_warp(my_s, (cnt + i) & 1, p.ctl, ab) && before_p()) {  // a warp without rows keeps step
+        } else if (wait_warp(my_s, (cnt + i) & 1, p.ctl, ab) && before_p()) {  // a warp without rows keeps step
           mbar_arrive(my_p);
           mbar_arrive(my_p + 8);
         } else {
@@ -1040,18 +1042,18 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
       if (!it.two && t == 1) {
         // the odd key tiles of a single tile: O stays in TMEM, m and l go to the even ones' warps
         if (both) {
-          alive = alive && (shared == 0 || mbar_wait_warp(bar_mle, (shared - 1) & 1, p.ctl, ab));
+          alive = alive && (shared == 0 || wait_warp(bar_mle, (shared - 1) & 1, p.ctl, ab));
           if (alive) {
             st_shared_f2(ml, m_run, l_run);
             mbar_arrive(bar_ml);
-            alive = mbar_wait_warp(my_o, items & 1, p.ctl, ab);  // (a wait by parity may not miss a phase)
+            alive = wait_warp(my_o, items & 1, p.ctl, ab);  // (a wait by parity may not miss a phase)
           }
         }
       } else {
-        alive = alive && (n == 0 || mbar_wait_warp(my_o, items & 1, p.ctl, ab));
+        alive = alive && (n == 0 || wait_warp(my_o, items & 1, p.ctl, ab));
         RowSums r{-1, nullptr, m_run, l_run, 1.f, 0.f, n > 0, both, any, alive};
         if (both) {
-          alive = alive && mbar_wait_warp(bar_o + 8, items1 & 1, p.ctl, ab) && mbar_wait_warp(bar_ml, shared & 1, p.ctl, ab);
+          alive = alive && wait_warp(bar_o + 8, items1 & 1, p.ctl, ab) && wait_warp(bar_ml, shared & 1, p.ctl, ab);
           if (alive) {
             const float2 other = ld_shared_f2(ml);
             mbar_arrive(bar_mle);
