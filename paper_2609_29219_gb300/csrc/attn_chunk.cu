@@ -239,6 +239,15 @@ __device__ __forceinline__ Walk walk_from(const ChunkParams& p, const Line& ln, 
   return w;
 }
 
+__device__ __forceinline__ void st_shared_u32(uint32_t addr, uint32_t v) {
+  asm volatile("st.shared.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+__device__ __forceinline__ int ld_shared_i32(uint32_t addr) {
+  int v;
+  asm volatile("ld.shared.s32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return v;
+}
+
 // The pieces of a cut unit, found by a whole warp: the first CTA that has one (its last unit; the others' pieces
 // are their CTAs' first), and which of the 32 CTAs from `from` on have one.
 __device__ __forceinline__ int first_cta(const Line& ln, const Item& it) {
@@ -263,26 +272,25 @@ __device__ __forceinline__ uint32_t piece_ctas(const Line& ln, const Item& it, i
   }
   return __ballot_sync(0xffffffffu, has);
 }
-// The pieces' places in the workspace, one after another (-1 after the last); the whole warp asks.
-struct Pieces {
-  int first, from;
-  uint32_t ctas;  // of the 32 before `from` that are yet to come
-  __device__ __forceinline__ explicit Pieces(int first_cta) : first(first_cta), from(first_cta), ctas(0) {}
-  __device__ __forceinline__ int next(const Line& ln, const Item& it) {
+// The places of a cut unit's pieces in the workspace, in order, into the warp's list in shared memory (4 bytes each,
+// one for each CTA at most); how many there are.
+__device__ __forceinline__ int list_pieces(const Line& ln, const Item& it, int first, uint32_t list) {
+  const int lane = static_cast<int>(threadIdx.x & 31);
+  int n = 0;
 #pragma unroll 1
-    while (!ctas) {
-      if (from >= ln.G || ln.bound(from) >= it.at + it.cost) return -1;
-      ctas = piece_ctas(ln, it, from);
-      from += 32;
-    }
-    const int c = from - 33 + __ffs(static_cast<int>(ctas));
-    ctas &= ctas - 1;
-    return c == first ? 2 * c + 1 : 2 * c;
+  for (int from = first; from < ln.G; from += 32) {
+    if (ln.bound(from) >= it.at + it.cost) break;
+    const uint32_t ctas = piece_ctas(ln, it, from);
+    const int c = from + lane;
+    if (ctas >> lane & 1u) st_shared_u32(list + 4 * (n + __popc(ctas & ((1u << lane) - 1u))), c == first ? 2 * c + 1 : 2 * c);
+    n += __popc(ctas);
   }
-};
+  __syncwarp();
+  return n;
+}
 
-// mbar_wait_warp as a call: in line at each of the roles' waits it made the kernel twice as long as the
-// instruction cache, and what runs once a unit was fetched anew each time.
+// mbar_wait_warp as a call: in line at each of the roles' waits it made the kernel longer than the instruction
+// cache, and what runs once a unit was fetched anew each time.
 __device__ __noinline__ bool wait_long(uint32_t bar, uint32_t parity, const KernelCtl& ctl, const Abort& ab) {
   return mbar_wait_warp(bar, parity, ctl, ab);
 }
@@ -381,20 +389,19 @@ __device__ __forceinline__ void st_shared_f2(uint32_t addr, float a, float b) {
 }
 
 // 64 columns of this warp's 32 rows, packed bf16 pairs of each lane's own row in w, to the rows' places in O (my_at:
-// this row's first column, in elements; < 0: not a row): through the warp's 4 KB of shared memory, so that
+// this row's first column, in 16 bytes from o; < 0: not a row): through the warp's 4 KB of shared memory, so that
 // a store writes whole 128-byte lines (from the lanes' own rows it would touch 32 lines).
-__device__ __forceinline__ void store_rows(uint32_t stg, const uint32_t* w, long long my_at, __nv_bfloat16* o) {
-  const int lane = threadIdx.x & 31;
+__device__ __forceinline__ void store_rows(uint32_t stg, const uint32_t* w, int my_at, uint4* o) {
+  const int lane = threadIdx.x & 31, j = lane % 8;
 #pragma unroll
   for (int c = 0; c < 8; ++c)
     st_shared_v4(stg + lane * 128 + ((c ^ (lane & 7)) << 4), w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
   __syncwarp();
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
-    const int r = k * 4 + lane / 8, j = lane % 8;
-    const long long at = __shfl_sync(0xffffffffu, my_at, r);
+    const int r = k * 4 + lane / 8, at = __shfl_sync(0xffffffffu, my_at, r);
     const uint4 v = ld_shared_v4(stg + r * 128 + ((j ^ (r & 7)) << 4));
-    if (at >= 0) reinterpret_cast<uint4*>(o + at)[j] = v;
+    if (at >= 0) o[at + j] = v;
   }
   __syncwarp();
 }
@@ -417,11 +424,11 @@ __device__ __forceinline__ int count_piece(unsigned long long* at, unsigned long
   return static_cast<int>(was & 0xffff) + 1;
 }
 
-// What a unit, or a piece of it, has to say of one query row (this thread's TMEM lane): its place in O, in elements
-// (-1: not a row), and in LSE (or null), and its sums, O's in TMEM: weight 0 of that at o_tm, and with
+// What a unit, or a piece of it, has to say of one query row (this thread's TMEM lane): its place in O, in 16 bytes
+// from the unit's first token (-1: not a row), and in LSE (or null), and its sums, O's in TMEM: weight 0 of that at o_tm, and with
 // `both` weight 1 of that at o_tm + D.
 struct RowSums {
-  long long at;
+  int at;
   float* lse_at;
   float m, l, w0, w1;
   bool has, both;  // key tiles were walked here
@@ -465,38 +472,27 @@ __device__ __forceinline__ void release_o(const RowSums& r, uint32_t bar_oe, uin
 // Joins the pieces of a warp's rows, N of them and U chunks of 16 bytes of a row at a time, all of whose loads are
 // on their way together: a round takes an access' latency, whatever it loads.
 template <int D, int U, int N>
-__device__ __forceinline__ void join_pieces(const ChunkParams& p, const Line& ln, const Item& it, int first, const float2* ml,
-                                            const float4* part, int rows, int lg, const RowSums& r) {
+__device__ __forceinline__ void join_pieces(const ChunkParams& p, uint32_t list, int pieces, const float2* ml, const float4* part,
+                                            int rows, int lg, const RowSums& r, long long unit_at) {
   const int lane = threadIdx.x & 31, my = lane & ((1 << lg) - 1), parts = 32 >> lg;
   const bool mine = my < rows;
   const size_t ml_slot = static_cast<size_t>(p.groups) * 32, part_slot = ml_slot * (D / 4);
-  const long long at = __shfl_sync(0xffffffffu, r.at, my);
+  const int at = __shfl_sync(0xffffffffu, r.at, my);
+  __nv_bfloat16* o = p.o + unit_at + static_cast<long long>(at) * 8;
 #pragma unroll 1
   for (int block = 0; block < D / 4; block += U * parts) {  // (of all lanes alike)
     const int c0 = block + (lane >> lg);
     float acc[4 * U], M = -INFINITY, l = 0.f;
 #pragma unroll
     for (int i = 0; i < 4 * U; ++i) acc[i] = 0.f;
-    Pieces pieces(first);
-    bool more = true;
 #pragma unroll 1
-    while (more) {
-      int slots[N];
-#pragma unroll
-      for (int k = 0; k < N; ++k) slots[k] = -1;
-#pragma unroll 1
-      for (int k = 0; k < N && more; ++k) {
-        const int slot = pieces.next(ln, it);
-        more = slot >= 0;
-#pragma unroll
-        for (int i = 0; i < N; ++i) slots[i] = i == k ? slot : slots[i];
-      }
+    for (int k0 = 0; k0 < pieces; k0 += N) {
       float2 x[N];
       float4 v[N][U];
 #pragma unroll
       for (int k = 0; k < N; ++k) {
-        const bool there = mine && slots[k] >= 0;
-        const size_t slot = there ? slots[k] : 0;
+        const bool there = mine && k0 + k < pieces;
+        const size_t slot = there ? ld_shared_i32(list + 4 * (k0 + k)) : 0;
         x[k] = there ? __ldcg(ml + slot * ml_slot + my) : make_float2(-INFINITY, -1.f);
         const float4* from = part + slot * part_slot + my;
 #pragma unroll
@@ -530,21 +526,16 @@ __device__ __forceinline__ void join_pieces(const ChunkParams& p, const Line& ln
 #pragma unroll
       for (int i = 0; i < U; ++i)
         if (c0 + i * parts < D / 4)
-          *reinterpret_cast<uint2*>(p.o + at + (c0 + i * parts) * 4) =
+          *reinterpret_cast<uint2*>(o + (c0 + i * parts) * 4) =
               make_uint2(pack_bf16x2(acc[4 * i] * inv, acc[4 * i + 1] * inv), pack_bf16x2(acc[4 * i + 2] * inv, acc[4 * i + 3] * inv));
     // (every lane below `rows` has its own row)
     if (block == 0 && r.lse_at) *r.lse_at = row_lse(M, l);
   }
 }
 
-// Counts a piece of this warp's rows of a cut unit; true for the last to come.
-__device__ __forceinline__ bool last_piece(const ChunkParams& p, const Line& ln, const Item& it, int first, int warp) {
-  int pieces = 0, come = 0;
-#pragma unroll 1
-  for (int from = first; from < ln.G; from += 32) {
-    if (ln.bound(from) >= it.at + it.cost) break;
-    pieces += __popc(piece_ctas(ln, it, from));
-  }
+// Counts one of the pieces of this warp's rows of a cut unit; true for the last to come.
+__device__ __forceinline__ bool last_piece(const ChunkParams& p, int pieces, int first, int warp) {
+  int come = 0;
   if ((threadIdx.x & 31) == 0) {
     unsigned long long* count = p.count + static_cast<size_t>(first) * 8 + warp;
     come = count_piece(count, p.tag);
@@ -556,23 +547,36 @@ __device__ __forceinline__ bool last_piece(const ChunkParams& p, const Line& ln,
 // A whole unit: this warp's 32 rows are stored.  (Not inlined, like the next: its registers would spill the softmax
 // loop's.)
 template <int D>
-__device__ __noinline__ void finish_unit(const ChunkParams& p, const RowSums r, uint32_t o_tm, uint32_t bar_oe, uint32_t bar_oe1,
-                                         uint32_t stg) {
+__device__ __noinline__ void finish_unit(const ChunkParams& p, const RowSums r, long long unit_at, uint32_t o_tm, uint32_t bar_oe,
+                                         uint32_t bar_oe1, uint32_t stg) {
   const float inv = r.l == 0.f ? 0.f : 1.f / r.l;
+  const uint64_t inv2 = f2(inv * r.w0, inv * r.w0);
+  uint4* o = reinterpret_cast<uint4*>(p.o + unit_at);
 #pragma unroll 1
   for (int h = 0; h < D / 64; ++h) {  // (code that runs once a unit: the shorter, the sooner it is fetched)
     uint32_t w[64];
-    if (r.has) {
+    if (r.both) {
       load_o<D>(o_tm, 64 * h, r, inv, w);
       load_o<D>(o_tm, 64 * h + 32, r, inv, w + 32);
+    } else if (r.has) {
+      tmem_ld32(o_tm + 64 * h, w);
+      tmem_ld32(o_tm + 64 * h + 32, w + 32);
+      tmem_wait_ld();
+      reg_fence32(w);
+      reg_fence32(w + 32);
 #pragma unroll
-      for (int i = 0; i < 32; ++i) w[i] = pack_bf16x2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+      for (int i = 0; i < 32; ++i) {
+        const uint64_t x = mul2(f2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1])), inv2);
+        w[2 * i] = __float_as_uint(f2lo(x)), w[2 * i + 1] = __float_as_uint(f2hi(x));
+      }
     } else {
 #pragma unroll
-      for (int i = 0; i < 32; ++i) w[i] = 0;
+      for (int i = 0; i < 64; ++i) w[i] = 0;
     }
     if (r.has && h + 1 == D / 64) release_o(r, bar_oe, bar_oe1);
-    store_rows(stg, w, r.at < 0 ? r.at : r.at + 64 * h, p.o);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) w[i] = pack_bf16x2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+    store_rows(stg, w, r.at < 0 ? r.at : r.at + 8 * h, o);
   }
   if (r.lse_at) *r.lse_at = row_lse(r.m, r.l);
 }
@@ -581,8 +585,8 @@ __device__ __noinline__ void finish_unit(const ChunkParams& p, const RowSums r, 
 // (one store: 512 bytes in a row).  The last warp to bring its piece of the rows joins all of them, in the
 // pieces' order.  Not inlined: it is rare, and its registers would spill the softmax loop's.
 template <int D>
-__device__ __noinline__ void finish_piece(const ChunkParams& p, const Line& ln, const Item& it, const RowSums r, uint32_t o_tm,
-                                          uint32_t bar_oe, uint32_t bar_oe1, int warp) {
+__device__ __noinline__ void finish_piece(const ChunkParams& p, const Line& ln, const Item& it, const RowSums r, long long unit_at,
+                                          uint32_t o_tm, uint32_t bar_oe, uint32_t bar_oe1, uint32_t stg, int warp) {
   const int lane = threadIdx.x & 31, group = it.two ? warp : warp & 3;
   const bool row = r.at >= 0;
   const int slot = it.lo == 0 ? 2 * static_cast<int>(blockIdx.x) + 1 : 2 * static_cast<int>(blockIdx.x);
@@ -604,10 +608,10 @@ __device__ __noinline__ void finish_piece(const ChunkParams& p, const Line& ln, 
   }
   if (r.alive && r.has) release_o(r, bar_oe, bar_oe1);
   if (!r.any) return;
-  const int first = first_cta(ln, it);
+  const int first = first_cta(ln, it), pieces = list_pieces(ln, it, first, stg);  // (while the stores are on their way)
   __threadfence();
   __syncwarp();
-  if (!last_piece(p, ln, it, first, warp) || !r.alive) return;
+  if (!last_piece(p, pieces, first, warp) || !r.alive) return;
   __syncwarp();
   __threadfence();
   // The warp's rows (its first lanes') are spread over all lanes: 1 << lg of them side by side, each lane with
@@ -616,12 +620,14 @@ __device__ __noinline__ void finish_piece(const ChunkParams& p, const Line& ln, 
   const int lg = rows > 1 ? 32 - __clz(rows - 1) : 0;
   const float2* ml = p.part_ml + group * 32;
   const float4* part = reinterpret_cast<const float4*>(p.part) + static_cast<size_t>(group) * (D / 4) * 32;
-  join_pieces<D, 8, 3>(p, ln, it, first, ml, part, rows, lg, r);
+  join_pieces<D, 8, 3>(p, stg, pieces, ml, part, rows, lg, r, unit_at);
+  __syncwarp();  // the list has been read
 }
 
 // After a wait has given up, a softmax warp counts the pieces that it has not brought all the same, so that every
 // count is whole again at the launch's end: a captured launch may be replayed on this workspace.
-__device__ __noinline__ void count_rest(const ChunkParams& p, const Line& ln, int b, long long at, int warp, int counted) {
+__device__ __noinline__ void count_rest(const ChunkParams& p, const Line& ln, int b, long long at, uint32_t stg, int warp,
+                                        int counted) {
   if (ln.x0 >= ln.x1) return;
   Walk w = walk_from(p, ln, b, load_seq(p, b), at);
   Item it;
@@ -629,7 +635,9 @@ __device__ __noinline__ void count_rest(const ChunkParams& p, const Line& ln, in
     // the warp's first row, if it has rows: as the softmax role has it
     const int i = (warp & 3) * 32, token = it.t0 + (it.two ? (warp >> 2) * p.tq : 0) + i / p.gt;
     if (!it.cut() || (!it.two && warp >= 4) || i / p.gt >= p.tq || token >= it.sq) continue;
-    if (--counted < 0) last_piece(p, ln, it, first_cta(ln, it), warp);
+    if (--counted >= 0) continue;
+    const int first = first_cta(ln, it);
+    last_piece(p, list_pieces(ln, it, first, stg), first, warp);
   }
 }
 
@@ -1066,16 +1074,17 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
           r.alive = alive;
         }
         tc_fence_after();
+        const long long unit_at = static_cast<long long>(it.qb + it.t0) * p.Hq * D;  // its first token's place in O
         if (row) {
           const int head = it.plane * p.gt + row_head;
-          r.at = (static_cast<long long>(it.qb + token) * p.Hq + head) * D;
+          r.at = ((token - it.t0) * p.Hq + head) * (D / 8);
           if (p.lse) r.lse_at = p.lse + static_cast<size_t>(head) * p.total_q + it.qb + token;
         }
         if (it.cut()) {
-          finish_piece<D>(p, ln, it, r, o_tm, my_oe, bar_oe + 8, warp);
+          finish_piece<D>(p, ln, it, r, unit_at, o_tm, my_oe, bar_oe + 8, stg, warp);
           counted += any;
         } else if (alive && any) {
-          finish_unit<D>(p, r, o_tm, my_oe, bar_oe + 8, stg);
+          finish_unit<D>(p, r, unit_at, o_tm, my_oe, bar_oe + 8, stg);
         } else if (alive && n > 0) {
           release_o(r, my_oe, bar_oe + 8);
         }
@@ -1096,7 +1105,7 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
-  if (ab.raised() && warp < 8) count_rest(p, ln, static_cast<int>(start[0]), start[1], warp, counted);
+  if (ab.raised() && warp < 8) count_rest(p, ln, static_cast<int>(start[0]), start[1], sbase + C::STG_OFF + warp * 4096, warp, counted);
 }
 
 // ---------------------------------------------------------------- host side
