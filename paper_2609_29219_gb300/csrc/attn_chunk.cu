@@ -44,7 +44,7 @@ constexpr float kRescaleThreshold = 8.0f;  // base-2 units; P <= 2^8 between res
 // The line's units: a key of a pair of tiles costs 1 << kKeyLg2, of a single tile 1 << kKeyLg1; a unit kUnitCost more.
 constexpr int kKeyLg2 = 3, kKeyLg1 = 2, kUnitCost = 3072;
 // The least that a CTA is given of units that are longer: they are not cut into shorter pieces.
-constexpr int kLeastStretch = 7168;
+constexpr int kLeastStretch = 4608;
 
 template <int D>
 struct ChunkCfg {
@@ -171,11 +171,12 @@ struct Item {
   int n0, n1;                     // of these, the steps of S, P and O number 0 and number 1
   int tiles;                      // all its key tiles
   int two;                        // it has two query tiles
-  int key_lg, pad;                // a key's cost
+  int key_lg;                     // a key's cost
+  int first, pieces;              // cut: the first CTA that has a piece, and how many have
   long long at, cost;             // its place on the line
   __device__ __forceinline__ bool cut() const { return n < tiles; }
 };
-static_assert(sizeof(Item) == 72, "fits its record");
+static_assert(sizeof(Item) == 80, "fits its record");
 
 // The CTA's next piece, and the walk behind it; false past the stretch's end.
 __device__ __forceinline__ bool next_item(const ChunkParams& p, const Line& ln, Walk& w, Item& it) {
@@ -272,21 +273,25 @@ __device__ __forceinline__ uint32_t piece_ctas(const Line& ln, const Item& it, i
   }
   return __ballot_sync(0xffffffffu, has);
 }
-// The places of a cut unit's pieces in the workspace, in order, into the warp's list in shared memory (4 bytes each,
-// one for each CTA at most); how many there are.
-__device__ __forceinline__ int list_pieces(const Line& ln, const Item& it, int first, uint32_t list) {
+// How many pieces a cut unit has; and their places in the workspace, in order, into the warp's list in shared
+// memory (4 bytes each, one for each CTA at most).
+__device__ __forceinline__ int count_pieces(const Line& ln, const Item& it, int first) {
+  int n = 0;
+#pragma unroll 1
+  for (int from = first; from < ln.G && ln.bound(from) < it.at + it.cost; from += 32) n += __popc(piece_ctas(ln, it, from));
+  return n;
+}
+__device__ __forceinline__ void list_pieces(const Line& ln, const Item& it, int first, uint32_t list) {
   const int lane = static_cast<int>(threadIdx.x & 31);
   int n = 0;
 #pragma unroll 1
-  for (int from = first; from < ln.G; from += 32) {
-    if (ln.bound(from) >= it.at + it.cost) break;
+  for (int from = first; from < ln.G && ln.bound(from) < it.at + it.cost; from += 32) {
     const uint32_t ctas = piece_ctas(ln, it, from);
     const int c = from + lane;
     if (ctas >> lane & 1u) st_shared_u32(list + 4 * (n + __popc(ctas & ((1u << lane) - 1u))), c == first ? 2 * c + 1 : 2 * c);
     n += __popc(ctas);
   }
   __syncwarp();
-  return n;
 }
 
 // mbar_wait_warp as a call: in line at each of the roles' waits it made the kernel longer than the instruction
@@ -303,11 +308,11 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, const K
 // s_tm: mask keys >= limit, move the running max lazily, write P = 2^(S c - m) as bf16 over the first
 // half of S's columns in two halves (arriving on bar_p and bar_p + 8 after each), rescale O at o_tm where
 // the max moved, and add to the row's sum.  S is only ready after the tile's previous P.V (issued before it by
-// the same warp), so the rescale needs no wait.  before_p() runs before the first arrival.
-template <int D, class F>
+// the same warp), so the rescale needs no wait.
+template <int D>
 __device__ __forceinline__ bool chunk_step(uint32_t s_tm, uint32_t o_tm, uint32_t bar_s, uint32_t par_s, uint32_t bar_p,
                                            bool first, int limit, float c, float& m_run, float& l_run, const KernelCtl& ctl,
-                                           const Abort& ab, F before_p) {
+                                           const Abort& ab) {
   constexpr int BN = 128;
   if (!mbar_wait_warp(bar_s, par_s, ctl, ab)) return false;
   tc_fence_after();
@@ -375,7 +380,6 @@ __device__ __forceinline__ bool chunk_step(uint32_t s_tm, uint32_t o_tm, uint32_
       }
       tmem_wait_st();
     }
-    if (half == 0 && !before_p()) return false;
     tc_fence_before();
     mbar_arrive(bar_p + 8 * half);
   }
@@ -608,11 +612,10 @@ __device__ __noinline__ void finish_piece(const ChunkParams& p, const Line& ln, 
   }
   if (r.alive && r.has) release_o(r, bar_oe, bar_oe1);
   if (!r.any) return;
-  const int first = first_cta(ln, it), pieces = list_pieces(ln, it, first, stg);  // (while the stores are on their way)
   __threadfence();
   __syncwarp();
-  if (!last_piece(p, pieces, first, warp) || !r.alive) return;
-  __syncwarp();
+  if (!last_piece(p, it.pieces, it.first, warp) || !r.alive) return;
+  list_pieces(ln, it, it.first, stg);
   __threadfence();
   // The warp's rows (its first lanes') are spread over all lanes: 1 << lg of them side by side, each lane with
   // every (32 >> lg)-th 16 bytes of its row.
@@ -620,14 +623,13 @@ __device__ __noinline__ void finish_piece(const ChunkParams& p, const Line& ln, 
   const int lg = rows > 1 ? 32 - __clz(rows - 1) : 0;
   const float2* ml = p.part_ml + group * 32;
   const float4* part = reinterpret_cast<const float4*>(p.part) + static_cast<size_t>(group) * (D / 4) * 32;
-  join_pieces<D, 8, 3>(p, stg, pieces, ml, part, rows, lg, r, unit_at);
+  join_pieces<D, 8, 3>(p, stg, it.pieces, ml, part, rows, lg, r, unit_at);
   __syncwarp();  // the list has been read
 }
 
 // After a wait has given up, a softmax warp counts the pieces that it has not brought all the same, so that every
 // count is whole again at the launch's end: a captured launch may be replayed on this workspace.
-__device__ __noinline__ void count_rest(const ChunkParams& p, const Line& ln, int b, long long at, uint32_t stg, int warp,
-                                        int counted) {
+__device__ __noinline__ void count_rest(const ChunkParams& p, const Line& ln, int b, long long at, int warp, int counted) {
   if (ln.x0 >= ln.x1) return;
   Walk w = walk_from(p, ln, b, load_seq(p, b), at);
   Item it;
@@ -637,7 +639,7 @@ __device__ __noinline__ void count_rest(const ChunkParams& p, const Line& ln, in
     if (!it.cut() || (!it.two && warp >= 4) || i / p.gt >= p.tq || token >= it.sq) continue;
     if (--counted >= 0) continue;
     const int first = first_cta(ln, it);
-    last_piece(p, list_pieces(ln, it, first, stg), first, warp);
+    last_piece(p, count_pieces(ln, it, first), first, warp);
   }
 }
 
@@ -802,6 +804,10 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
       Item it;
       more = next_item(p, l, walk, it);
       if (!more) it.n = -1;
+      if (more && it.cut()) {
+        it.first = first_cta(l, it);
+        it.pieces = count_pieces(l, it, it.first);
+      }
       const int i = k % C::NREC;
       if (k >= C::NREC && !wait_warp(bar_rece + 8 * i, (k / C::NREC - 1) & 1, p.ctl, ab)) break;
       if (lane == 0) {
@@ -1024,26 +1030,24 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
 #pragma unroll 1
       for (int i = 0; alive && i < n; ++i) {
         const int j = it.two ? i : 2 * i + t;  // key tile
-        const auto before_p = [&]() -> bool {
-          if (!clears || j + 1 < it.n) return true;
+        if (clears && j + 1 == it.n) {
           const int vn = pos + j, slot = vn % C::NR;
-          if (!wait_warp(bar_full + 8 * (C::NR + slot), (vn / C::NR) & 1, p.ctl, ab)) return false;
+          // (S first: it is issued behind the P.V of the tile that had V's slot before, without which V's barrier
+          // could be two phases behind, which a wait by parity takes for done)
+          alive = wait_warp(my_s, (cnt + i) & 1, p.ctl, ab) && wait_warp(bar_full + 8 * (C::NR + slot), (vn / C::NR) & 1, p.ctl, ab);
+          if (!alive) break;
           const uint32_t v = sbase + C::RING_OFF + (C::NR + slot) * C::TILE_BYTES;
           const int chunks = (C::BN - over) * 8;
 #pragma unroll 1
           for (int x = row_in_tile; x < C::NBOX * chunks; x += C::BM)
             st_shared_v4(v + x / chunks * C::BOX_BYTES + over * 128 + x % chunks * 16, 0, 0, 0, 0);
           fence_proxy_async_smem();
-          return true;
-        };
+        }
         if (any) {
-          alive = chunk_step<D>(s_tm, o_tm, my_s, (cnt + i) & 1, my_p, i == 0, limit - j * C::BN, p.c, m_run, l_run, p.ctl, ab,
-                                before_p);
-        } else if (wait_warp(my_s, (cnt + i) & 1, p.ctl, ab) && before_p()) {  // a warp without rows keeps step
+          alive = chunk_step<D>(s_tm, o_tm, my_s, (cnt + i) & 1, my_p, i == 0, limit - j * C::BN, p.c, m_run, l_run, p.ctl, ab);
+        } else if ((alive = wait_warp(my_s, (cnt + i) & 1, p.ctl, ab))) {  // a warp without rows keeps step
           mbar_arrive(my_p);
           mbar_arrive(my_p + 8);
-        } else {
-          alive = false;
         }
       }
       const bool both = !it.two && it.n1 > 0;
@@ -1105,7 +1109,7 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
-  if (ab.raised() && warp < 8) count_rest(p, ln, static_cast<int>(start[0]), start[1], sbase + C::STG_OFF + warp * 4096, warp, counted);
+  if (ab.raised() && warp < 8) count_rest(p, ln, static_cast<int>(start[0]), start[1], warp, counted);
 }
 
 // ---------------------------------------------------------------- host side
