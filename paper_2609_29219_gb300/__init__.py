@@ -253,7 +253,8 @@ def _compiled_binding(torch):
         tuple(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in (
             "loom_attn_bwd", "loom_attn_bwd_workspace_bytes", "loom_attn_bwd_varlen", "loom_attn_bwd_varlen_workspace_bytes",
             "loom_qkv_norm_rope", "loom_qkv_norm_rope_cache", "loom_qkv_norm_rope_bwd",
-            "loom_qkv_norm_rope_bwd_workspace_bytes")))
+            "loom_qkv_norm_rope_bwd_workspace_bytes", "loom_qkv_norm_rope_axes", "loom_qkv_norm_rope_axes_cache",
+            "loom_qkv_norm_rope_axes_bwd", "loom_attn_chunk_paged", "loom_attn_chunk_paged_workspace_bytes", "loom_paged_plan")))
     return _binding
 
 
@@ -614,6 +615,11 @@ def loom_attn_chunk_paged(q, k_cache, v_cache, block_table, cu_seqlens_q, seqlen
     _torch()
     if layout not in ("nhd", "hnd"):
         raise ValueError("layout is 'nhd' or 'hnd'")
+    if _fast is not None and o is None and lse is None and workspace is None and stream is None:
+        r = _fast.chunk(q, k_cache, v_cache, block_table, cu_seqlens_q, seqlens_k, causal, scale, layout == "hnd", bool(return_lse))
+        if r is not None:
+            r = _fast_result(r, "loom_attn_chunk_paged")
+            return r if return_lse else r[0]
     qp = _ptr(q, "q", _bf16, 3)
     dev = _on_current(q, "q") if _several else None
     kp = _ptr(k_cache, "k_cache", _bf16, 4, dev)
@@ -671,6 +677,11 @@ def loom_paged_plan(new_lens, lens, block_table, free_pages, free_count, num_tok
     [num_tokens] and ``granted`` [B] (allocated if None); the free pages that are left go to
     ``free_count_out`` (None: to free_count)."""
     _torch()
+    if _fast is not None and cu_seqlens is None and positions is None and slots is None and granted is None and stream is None:
+        r = _fast.plan(new_lens, lens, block_table, free_pages, free_count, free_count if free_count_out is None else free_count_out,
+                       seqlens_k, num_tokens, page_size)
+        if r is not None:
+            return _fast_result(r, "loom_paged_plan")
     np_ = _ptr(new_lens, "new_lens", _i32, 1)
     dev = _on_current(new_lens, "new_lens") if _several else None
     B, T = new_lens.shape[0], int(num_tokens)
@@ -913,7 +924,7 @@ def _axes_operands(qkv, cos, positions, pair_axis):
     _dev_ptr(positions, "positions", _i32, 2, qkv.get_device())
     if positions.shape[1] != qkv.shape[0]:
         raise ValueError("positions must be [axes, T] with pair_axis")
-    axes = _axis_array(tuple(map(int, pair_axis)))
+    axes = _axis_array(pair_axis if type(pair_axis) is tuple else tuple(map(int, pair_axis)))
     if len(axes) != cos.shape[1]:
         raise ValueError(f"pair_axis must name an axis for each of the {cos.shape[1]} pairs that the tables have")
     if not all(0 <= a < positions.shape[0] for a in axes):
@@ -969,8 +980,9 @@ def loom_qkv_norm_rope(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_head
     ``pair_axis``, a sequence of rotary_dim / 2 whole numbers: positions are [axes, T] (at most four axes)
     and pair i of a head turns by its token's position on axis pair_axis[i]."""
     _torch()
-    if _fast is not None and q is None and k is None and v is None and stream is None and pair_axis is None:
-        r = _fast.norm_rope(qkv, q_weight, k_weight, cos, sin, positions, interleaved, eps, num_heads, num_kv_heads, seq_len)
+    if _fast is not None and q is None and k is None and v is None and stream is None:
+        r = _fast.norm_rope(qkv, q_weight, k_weight, cos, sin, positions, interleaved, eps, num_heads, num_kv_heads, seq_len,
+                            pair_axis)
         if r is not None:
             return _fast_result(r, "loom_qkv_norm_rope")
     num_heads, num_kv_heads, seq_len = int(num_heads), int(num_kv_heads), int(seq_len)
@@ -1025,9 +1037,9 @@ def loom_qkv_norm_rope_cache(qkv, q_weight, k_weight, cos, sin, positions, slots
     if layout not in ("nhd", "hnd"):
         raise ValueError("layout is 'nhd' or 'hnd'")
     _torch()
-    if _fast is not None and q is None and stream is None and pair_axis is None:
+    if _fast is not None and q is None and stream is None:
         r = _fast.norm_rope_cache(qkv, q_weight, k_weight, cos, sin, positions, interleaved, eps, num_heads, slots, k_cache,
-                                  v_cache, layout == "hnd")
+                                  v_cache, layout == "hnd", pair_axis)
         if r is not None:
             return _fast_result(r, "loom_qkv_norm_rope_cache")[0]
     try:
@@ -1072,9 +1084,8 @@ def loom_qkv_norm_rope_bwd(dq, dk, dv, qkv, q_weight, k_weight, cos, sin, positi
     its rows may lie further apart), ``dq_weight`` and ``dk_weight`` ([D] fp32), allocated if None.
     ``workspace``: a CUDA uint8 tensor of ``loom_qkv_norm_rope_bwd_workspace_bytes(D)`` bytes."""
     _torch()
-    if (_fast is not None and dqkv is None and dq_weight is None and dk_weight is None and workspace is None and stream is None
-            and pair_axis is None):
-        r = _fast.norm_rope_bwd(qkv, q_weight, k_weight, cos, sin, positions, interleaved, eps, dq, dk, dv)
+    if _fast is not None and dqkv is None and dq_weight is None and dk_weight is None and workspace is None and stream is None:
+        r = _fast.norm_rope_bwd(qkv, q_weight, k_weight, cos, sin, positions, interleaved, eps, dq, dk, dv, pair_axis)
         if r is not None:
             return _fast_result(r, "loom_qkv_norm_rope_bwd")
     try:

@@ -69,7 +69,7 @@ class _QkvNormRope(torch.autograd.Function):
     def forward(ctx, qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, positions, seq_len, eps, interleaved, pair_axis):
         ctx.save_for_backward(qkv, q_weight, k_weight, cos, sin, positions)
         ctx.shapes = (num_heads, num_kv_heads, seq_len)
-        ctx.rest = {"eps": eps, "interleaved": interleaved, "pair_axis": pair_axis}
+        ctx.rest = {"eps": eps, "interleaved": interleaved, **({} if pair_axis is None else {"pair_axis": pair_axis})}
         return loom.loom_qkv_norm_rope(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, positions, seq_len=seq_len,
                                        **ctx.rest)
 

@@ -36,6 +36,12 @@ struct Functions {
   decltype(&loom_qkv_norm_rope_cache) norm_rope_cache;
   decltype(&loom_qkv_norm_rope_bwd) norm_rope_bwd;
   decltype(&loom_qkv_norm_rope_bwd_workspace_bytes) norm_rope_bwd_bytes;
+  decltype(&loom_qkv_norm_rope_axes) norm_rope_axes;
+  decltype(&loom_qkv_norm_rope_axes_cache) norm_rope_axes_cache;
+  decltype(&loom_qkv_norm_rope_axes_bwd) norm_rope_axes_bwd;
+  decltype(&loom_attn_chunk_paged) chunk;
+  decltype(&loom_attn_chunk_paged_workspace_bytes) chunk_bytes;
+  decltype(&loom_paged_plan) plan;
 } F = {};
 
 struct Ref {  // owned
@@ -206,17 +212,21 @@ PyObject* attn_bwd_varlen(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return bwd(a, true);
 }
 
-// What the norm-and-rotation calls share: qkv, q_weight, k_weight, cos, sin, positions, interleaved, eps.
+constexpr int kMaxPairs = 64;  // pairs of a head of 128 values
+
+// What the norm-and-rotation calls share: qkv, q_weight, k_weight, cos, sin, positions, interleaved, eps; and last
+// pair_axis (None, or a tuple of ints).
 struct Norm {
   Tensor x, qw, kw, cos, sin, pos;
   long long T, D, row;
-  int type, P, R, interleaved;
+  int type, P, R, interleaved, axes;
+  int axis[kMaxPairs];
   float eps;
   const int32_t* positions() const { return static_cast<const int32_t*>(pos.ptr); }
   // the tables have the rows that no positions given imply
   bool tables_reach(long long S) const { return pos.t || (S > 0 ? S : T) <= P; }
 };
-bool norm_args(PyObject* const* a, long long heads, Norm* m) {
+bool norm_args(PyObject* const* a, long long heads, PyObject* pair_axis, Norm* m) {
   if (!view(a[0], kBf16, &m->x, true) || m->x.dims != 2 || !small(m->x)) return false;
   const bool f32 = view(a[1], kF32, &m->qw);
   if ((!f32 && !view(a[1], kBf16, &m->qw)) || m->qw.dims != 1) return false;
@@ -228,7 +238,20 @@ bool norm_args(PyObject* const* a, long long heads, Norm* m) {
   if (m->D <= 0 || m->D > 1024 || heads <= 0 || heads > 0x100000 || m->x.size[1] != heads * m->D) return false;
   m->row = m->T > 1 ? m->x.t->stride(0) : m->x.size[1];
   if (m->x.t->stride(1) != 1) return false;
-  if (a[5] != Py_None && (!view(a[5], kI32, &m->pos) || m->pos.dims != 1 || m->pos.size[0] != m->T)) return false;
+  m->axes = 0;
+  if (pair_axis != Py_None) {
+    if (!PyTuple_CheckExact(pair_axis) || PyTuple_GET_SIZE(pair_axis) != m->cos.size[1] || PyTuple_GET_SIZE(pair_axis) > kMaxPairs ||
+        !view(a[5], kI32, &m->pos) || m->pos.dims != 2 || m->pos.size[1] != m->T || m->pos.size[0] < 1 || m->pos.size[0] > 4)
+      return false;
+    m->axes = static_cast<int>(m->pos.size[0]);
+    for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(pair_axis); ++i) {
+      long long x;
+      if (!as_int(PyTuple_GET_ITEM(pair_axis, i), &x) || x >= m->axes) return false;
+      m->axis[i] = static_cast<int>(x);
+    }
+  } else if (a[5] != Py_None && (!view(a[5], kI32, &m->pos) || m->pos.dims != 1 || m->pos.size[0] != m->T)) {
+    return false;
+  }
   if (!together(m->x, {&m->qw, &m->kw, &m->cos, &m->sin, &m->pos})) return false;
   m->type = f32 ? LOOM_FP32 : LOOM_BF16;
   m->P = static_cast<int>(m->cos.size[0]);
@@ -241,12 +264,12 @@ bool norm_args(PyObject* const* a, long long heads, Norm* m) {
   return as_float(a[7], &m->eps);
 }
 
-// norm_rope(qkv, q_weight, k_weight, cos, sin, positions, interleaved, eps, num_heads, num_kv_heads, seq_len)
+// norm_rope(qkv, q_weight, k_weight, cos, sin, positions, interleaved, eps, num_heads, num_kv_heads, seq_len, pair_axis)
 PyObject* norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
   long long Hq, Hkv, S;
   Norm m;
-  if (n != 11 || !as_int(a[8], &Hq) || !as_int(a[9], &Hkv) || !as_int(a[10], &S) || Hq <= 0 || Hkv <= 0 ||
-      !norm_args(a, Hq + 2 * Hkv, &m) || (S > 0 && m.T % S) || !m.tables_reach(S))
+  if (n != 12 || !as_int(a[8], &Hq) || !as_int(a[9], &Hkv) || !as_int(a[10], &S) || Hq <= 0 || Hkv <= 0 ||
+      !norm_args(a, Hq + 2 * Hkv, a[11], &m) || (S > 0 && m.T % S) || !m.tables_reach(S))
     Py_RETURN_NONE;
   const long long dev = device_of(m.x);
   if (dev < 0) Py_RETURN_NONE;
@@ -259,26 +282,30 @@ PyObject* norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!k.p) return nullptr;
   Ref v(make(dev, dims, ks, kBf16, &vp));
   if (!v.p) return nullptr;
-  const loom_status st = F.norm_rope(m.x.ptr, m.row, m.qw.ptr, m.kw.ptr, m.type, static_cast<const float*>(m.cos.ptr),
-                                     static_cast<const float*>(m.sin.ptr), m.P, m.R, m.interleaved, m.positions(), qp, kp, vp,
-                                     static_cast<int>(m.T), static_cast<int>(S), static_cast<int>(Hq), static_cast<int>(Hkv),
-                                     static_cast<int>(m.D), m.eps, stream_of(dev));
+  const float *cos = static_cast<const float*>(m.cos.ptr), *sin = static_cast<const float*>(m.sin.ptr);
+  const int T = static_cast<int>(m.T), iS = static_cast<int>(S), iHq = static_cast<int>(Hq), iHkv = static_cast<int>(Hkv),
+            D = static_cast<int>(m.D);
+  const loom_status st =
+      m.axes ? F.norm_rope_axes(m.x.ptr, m.row, m.qw.ptr, m.kw.ptr, m.type, cos, sin, m.P, m.R, m.interleaved, m.positions(), m.T,
+                                m.axes, m.axis, qp, kp, vp, T, iS, iHq, iHkv, D, m.eps, stream_of(dev))
+             : F.norm_rope(m.x.ptr, m.row, m.qw.ptr, m.kw.ptr, m.type, cos, sin, m.P, m.R, m.interleaved, m.positions(), qp, kp, vp,
+                           T, iS, iHq, iHkv, D, m.eps, stream_of(dev));
   if (st != LOOM_OK) return status(st);
   return PyTuple_Pack(3, q.p, k.p, v.p);
 }
 
 // norm_rope_cache(qkv, q_weight, k_weight, cos, sin, positions, interleaved, eps, num_heads, slots, k_cache, v_cache,
-// head_major): (q,)
+// head_major, pair_axis): (q,)
 PyObject* norm_rope_cache(PyObject*, PyObject* const* a, Py_ssize_t n) {
   long long Hq;
   Norm m;
   Tensor slots, kc, vc;
-  if (n != 13 || !as_int(a[8], &Hq) || Hq <= 0 || !view(a[10], kBf16, &kc) || kc.dims != 4 || !small(kc) ||
+  if (n != 14 || !as_int(a[8], &Hq) || Hq <= 0 || !view(a[10], kBf16, &kc) || kc.dims != 4 || !small(kc) ||
       !view(a[11], kBf16, &vc) || !same(kc, vc) || a[5] == Py_None)
     Py_RETURN_NONE;
   const int hnd = a[12] == Py_True;
   const long long Hkv = kc.size[hnd ? 1 : 2], page = kc.size[hnd ? 2 : 1];
-  if (!norm_args(a, Hq + 2 * Hkv, &m) || kc.size[3] != m.D || !view(a[9], kI32, &slots) || slots.dims != 1 ||
+  if (!norm_args(a, Hq + 2 * Hkv, a[13], &m) || kc.size[3] != m.D || !view(a[9], kI32, &slots) || slots.dims != 1 ||
       slots.size[0] != m.T || !together(m.x, {&slots, &kc, &vc}))
     Py_RETURN_NONE;
   const long long dev = device_of(m.x);
@@ -287,24 +314,29 @@ PyObject* norm_rope_cache(PyObject*, PyObject* const* a, Py_ssize_t n) {
   void* qp;
   Ref q(make(dev, 3, qs, kBf16, &qp));
   if (!q.p) return nullptr;
-  const loom_status st = F.norm_rope_cache(
-      m.x.ptr, m.row, m.qw.ptr, m.kw.ptr, m.type, static_cast<const float*>(m.cos.ptr), static_cast<const float*>(m.sin.ptr), m.P,
-      m.R, m.interleaved, m.positions(), static_cast<const int32_t*>(slots.ptr), qp, kc.ptr, vc.ptr, static_cast<int>(kc.size[0]),
-      static_cast<int>(page), hnd, static_cast<int>(m.T), static_cast<int>(Hq), static_cast<int>(Hkv), static_cast<int>(m.D),
-      m.eps, stream_of(dev));
+  const float *cos = static_cast<const float*>(m.cos.ptr), *sin = static_cast<const float*>(m.sin.ptr);
+  const int32_t* sp = static_cast<const int32_t*>(slots.ptr);
+  const int T = static_cast<int>(m.T), iHq = static_cast<int>(Hq), iHkv = static_cast<int>(Hkv), D = static_cast<int>(m.D),
+            pages = static_cast<int>(kc.size[0]), rows = static_cast<int>(page);
+  const loom_status st =
+      m.axes ? F.norm_rope_axes_cache(m.x.ptr, m.row, m.qw.ptr, m.kw.ptr, m.type, cos, sin, m.P, m.R, m.interleaved, m.positions(),
+                                      m.T, m.axes, m.axis, sp, qp, kc.ptr, vc.ptr, pages, rows, hnd, T, iHq, iHkv, D, m.eps,
+                                      stream_of(dev))
+             : F.norm_rope_cache(m.x.ptr, m.row, m.qw.ptr, m.kw.ptr, m.type, cos, sin, m.P, m.R, m.interleaved, m.positions(), sp, qp,
+                                 kc.ptr, vc.ptr, pages, rows, hnd, T, iHq, iHkv, D, m.eps, stream_of(dev));
   if (st != LOOM_OK) return status(st);
   return PyTuple_Pack(1, q.p);
 }
 
-// norm_rope_bwd(qkv, q_weight, k_weight, cos, sin, positions, interleaved, eps, dq, dk, dv)
+// norm_rope_bwd(qkv, q_weight, k_weight, cos, sin, positions, interleaved, eps, dq, dk, dv, pair_axis)
 PyObject* norm_rope_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Norm m;
   Tensor dq, dk, dv;
-  if (n != 11 || !view(a[8], kBf16, &dq) || dq.dims < 3 || !view(a[9], kBf16, &dk) || dk.dims != dq.dims ||
+  if (n != 12 || !view(a[8], kBf16, &dq) || dq.dims < 3 || !view(a[9], kBf16, &dk) || dk.dims != dq.dims ||
       !view(a[10], kBf16, &dv) || !same(dv, dk) || !small(dq) || !small(dk))
     Py_RETURN_NONE;
   const long long Hq = dq.size[1], Hkv = dk.size[1], S = dq.dims == 4 ? dq.size[2] : 0;
-  if (!norm_args(a, Hq + 2 * Hkv, &m) || dq.size[0] != dk.size[0] || dq.size[2] != dk.size[2] || dq.size[dq.dims - 1] != m.D ||
+  if (!norm_args(a, Hq + 2 * Hkv, a[11], &m) || dq.size[0] != dk.size[0] || dq.size[2] != dk.size[2] || dq.size[dq.dims - 1] != m.D ||
       dk.size[dk.dims - 1] != m.D || (S ? dq.size[0] * S : dq.size[0]) != m.T || (dq.dims == 4 && S == 0) ||
       !m.tables_reach(S) || !together(m.x, {&dq, &dk, &dv}))
     Py_RETURN_NONE;
@@ -319,25 +351,106 @@ PyObject* norm_rope_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Ref dkw(make(dev, 1, m.qw.size, kF32, &kp));
   if (!dkw.p) return nullptr;
   const c10::DataPtr ws = scratch(need);
-  const loom_status st = F.norm_rope_bwd(
-      dq.ptr, dk.ptr, dv.ptr, m.x.ptr, m.row, m.qw.ptr, m.kw.ptr, m.type, static_cast<const float*>(m.cos.ptr),
-      static_cast<const float*>(m.sin.ptr), m.P, m.R, m.interleaved, m.positions(), xp, m.x.size[1], static_cast<float*>(qp),
-      static_cast<float*>(kp), ws.get(), need, static_cast<int>(m.T), static_cast<int>(S), static_cast<int>(Hq), static_cast<int>(Hkv),
-      static_cast<int>(m.D), m.eps, stream_of(dev));
+  const float *cos = static_cast<const float*>(m.cos.ptr), *sin = static_cast<const float*>(m.sin.ptr);
+  float *qg = static_cast<float*>(qp), *kg = static_cast<float*>(kp);
+  const int T = static_cast<int>(m.T), iS = static_cast<int>(S), iHq = static_cast<int>(Hq), iHkv = static_cast<int>(Hkv),
+            D = static_cast<int>(m.D);
+  const loom_status st =
+      m.axes ? F.norm_rope_axes_bwd(dq.ptr, dk.ptr, dv.ptr, m.x.ptr, m.row, m.qw.ptr, m.kw.ptr, m.type, cos, sin, m.P, m.R,
+                                    m.interleaved, m.positions(), m.T, m.axes, m.axis, xp, m.x.size[1], qg, kg, ws.get(), need, T, iS,
+                                    iHq, iHkv, D, m.eps, stream_of(dev))
+             : F.norm_rope_bwd(dq.ptr, dk.ptr, dv.ptr, m.x.ptr, m.row, m.qw.ptr, m.kw.ptr, m.type, cos, sin, m.P, m.R, m.interleaved,
+                               m.positions(), xp, m.x.size[1], qg, kg, ws.get(), need, T, iS, iHq, iHkv, D, m.eps, stream_of(dev));
   if (st != LOOM_OK) return status(st);
   return PyTuple_Pack(3, dx.p, dqw.p, dkw.p);
+}
+
+// chunk(q, k_cache, v_cache, block_table, cu_seqlens_q, seqlens_k, causal, scale, head_major, with_lse): (o,) or (o, lse)
+PyObject* chunk(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Tensor q, kc, vc, table, cu, lens;
+  if (n != 10 || !view(a[0], kBf16, &q) || q.dims != 3 || !view(a[1], kBf16, &kc) || kc.dims != 4 || !view(a[2], kBf16, &vc) ||
+      !same(kc, vc) || !view(a[3], kI32, &table) || table.dims != 2 || !view(a[4], kI32, &cu) || cu.dims != 1 ||
+      !view(a[5], kI32, &lens) || lens.dims != 1 || !small(q) || !small(kc) || !small(table))
+    Py_RETURN_NONE;
+  const int hnd = a[8] == Py_True;
+  const long long T = q.size[0], Hq = q.size[1], D = q.size[2], Hkv = kc.size[hnd ? 1 : 2], page = kc.size[hnd ? 2 : 1],
+                  B = table.size[0];
+  if (kc.size[3] != D || cu.size[0] != B + 1 || lens.size[0] != B) Py_RETURN_NONE;
+  const int causal = PyObject_IsTrue(a[6]);
+  if (causal < 0) return nullptr;
+  float scale = 0.f;
+  if (a[7] == Py_None)
+    scale = D == 64 ? 0.125f : 0.088388347648318440550f;  // D^-1/2 (other D are refused)
+  else if (!as_float(a[7], &scale))
+    Py_RETURN_NONE;
+  const long long dev = device_of(q);
+  if (dev < 0 || !together(q, {&kc, &vc, &table, &cu, &lens})) Py_RETURN_NONE;
+  const int iB = static_cast<int>(B), iHq = static_cast<int>(Hq), iHkv = static_cast<int>(Hkv), iT = static_cast<int>(T),
+            iD = static_cast<int>(D);
+  const size_t need = F.chunk_bytes(iB, iHq, iHkv, iT, iD);
+  const bool with_lse = a[9] == Py_True;
+  const long long ls[2] = {Hq, T};
+  void *op, *lp = nullptr;
+  Ref o(make_like(dev, q, kBf16, &op)), lse;
+  if (!o.p) return nullptr;
+  if (with_lse && !(lse.p = make(dev, 2, ls, kF32, &lp))) return nullptr;
+  const c10::DataPtr ws = scratch(need);
+  const loom_status st = F.chunk(q.ptr, kc.ptr, vc.ptr, static_cast<const int32_t*>(table.ptr), static_cast<const int32_t*>(cu.ptr),
+                                 static_cast<const int32_t*>(lens.ptr), op, static_cast<float*>(lp), ws.get(), need, iB, iHq, iHkv, iT,
+                                 static_cast<int>(kc.size[0]), static_cast<int>(page), static_cast<int>(table.size[1]), hnd, iD,
+                                 causal, scale, stream_of(dev));
+  if (st != LOOM_OK) return status(st);
+  return with_lse ? PyTuple_Pack(2, o.p, lse.p) : PyTuple_Pack(1, o.p);
+}
+
+// plan(new_lens, lens, block_table, free_pages, free_count, free_count_out, seqlens_k or None, num_tokens, page_size):
+// (cu_seqlens, seqlens_k, positions, slots, granted)
+PyObject* plan(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Tensor news, lens, table, list, count, out, seqlens;
+  long long T, page;
+  if (n != 9 || !view(a[0], kI32, &news) || news.dims != 1 || !view(a[1], kI32, &lens) || !same(lens, news) ||
+      !view(a[2], kI32, &table) || table.dims != 2 || table.size[0] != news.size[0] || !view(a[3], kI32, &list) || list.dims != 1 ||
+      !view(a[4], kI32, &count) || count.dims != 1 || count.size[0] != 1 || !view(a[5], kI32, &out) || !same(out, count) ||
+      (a[6] != Py_None && (!view(a[6], kI32, &seqlens) || !same(seqlens, news))) || !as_int(a[7], &T) || !as_int(a[8], &page) ||
+      !small(table) || !small(list))
+    Py_RETURN_NONE;
+  const long long dev = device_of(news), B = news.size[0], B1 = B + 1;
+  if (dev < 0 || !together(news, {&lens, &table, &list, &count, &out, &seqlens})) Py_RETURN_NONE;
+  void *cp, *sp = seqlens.ptr, *pp, *lp, *gp;
+  Ref cu(make(dev, 1, &B1, kI32, &cp)), lengths;
+  if (!cu.p) return nullptr;
+  if (a[6] == Py_None) {
+    lengths.p = make(dev, 1, &B, kI32, &sp);
+    if (!lengths.p) return nullptr;
+  } else {
+    Py_INCREF(a[6]);
+    lengths.p = a[6];
+  }
+  Ref positions(make(dev, 1, &T, kI32, &pp));
+  if (!positions.p) return nullptr;
+  Ref slots(make(dev, 1, &T, kI32, &lp));
+  if (!slots.p) return nullptr;
+  Ref granted(make(dev, 1, &B, kI32, &gp));
+  if (!granted.p) return nullptr;
+  const auto i32 = [](void* x) { return static_cast<int32_t*>(x); };
+  const loom_status st = F.plan(i32(news.ptr), i32(lens.ptr), i32(table.ptr), i32(list.ptr), i32(count.ptr), i32(out.ptr), i32(cp),
+                                i32(sp), i32(pp), i32(lp), i32(gp), static_cast<int>(B), static_cast<int>(T),
+                                static_cast<int>(list.size[0]), static_cast<int>(page), static_cast<int>(table.size[1]), stream_of(dev));
+  if (st != LOOM_OK) return status(st);
+  return PyTuple_Pack(5, cu.p, lengths.p, positions.p, slots.p, granted.p);
 }
 
 // set_up((addresses ...)): the C functions.
 PyObject* set_up(PyObject*, PyObject* args) {
   PyObject* addresses;
   if (!PyArg_ParseTuple(args, "O!", &PyTuple_Type, &addresses)) return nullptr;
-  if (PyTuple_GET_SIZE(addresses) != 8) {
-    PyErr_SetString(PyExc_ValueError, "set_up takes 8 addresses");
+  constexpr int kFunctions = 14;
+  if (PyTuple_GET_SIZE(addresses) != kFunctions) {
+    PyErr_SetString(PyExc_ValueError, "set_up takes 14 addresses");
     return nullptr;
   }
-  void* at[8];
-  for (int i = 0; i < 8; ++i) {
+  void* at[kFunctions];
+  for (int i = 0; i < kFunctions; ++i) {
     at[i] = PyLong_AsVoidPtr(PyTuple_GET_ITEM(addresses, i));
     if (!at[i]) {
       if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "a null address");
@@ -352,6 +465,12 @@ PyObject* set_up(PyObject*, PyObject* args) {
   F.norm_rope_cache = reinterpret_cast<decltype(F.norm_rope_cache)>(at[5]);
   F.norm_rope_bwd = reinterpret_cast<decltype(F.norm_rope_bwd)>(at[6]);
   F.norm_rope_bwd_bytes = reinterpret_cast<decltype(F.norm_rope_bwd_bytes)>(at[7]);
+  F.norm_rope_axes = reinterpret_cast<decltype(F.norm_rope_axes)>(at[8]);
+  F.norm_rope_axes_cache = reinterpret_cast<decltype(F.norm_rope_axes_cache)>(at[9]);
+  F.norm_rope_axes_bwd = reinterpret_cast<decltype(F.norm_rope_axes_bwd)>(at[10]);
+  F.chunk = reinterpret_cast<decltype(F.chunk)>(at[11]);
+  F.chunk_bytes = reinterpret_cast<decltype(F.chunk_bytes)>(at[12]);
+  F.plan = reinterpret_cast<decltype(F.plan)>(at[13]);
   Py_RETURN_NONE;
 }
 
@@ -372,6 +491,8 @@ PyMethodDef methods[] = {{"set_up", set_up, METH_VARARGS, nullptr},
                          {"norm_rope", fast<norm_rope>(), METH_FASTCALL, nullptr},
                          {"norm_rope_cache", fast<norm_rope_cache>(), METH_FASTCALL, nullptr},
                          {"norm_rope_bwd", fast<norm_rope_bwd>(), METH_FASTCALL, nullptr},
+                         {"chunk", fast<chunk>(), METH_FASTCALL, nullptr},
+                         {"plan", fast<plan>(), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
