@@ -139,23 +139,21 @@ __device__ __forceinline__ int position(const QkvParams& p, int t) {
   return min(max(pos, 0), p.P - 1);
 }
 
-// The positions of a token whose pairs turn on several axes.
+// Positions on several axes: a warp gathers a token's R / 2 cosines and sines in shared memory, each lane those of
+// pairs `lane` and `lane + 32` from the rows of their axes' positions.  (A lane that instead read its own eight
+// pairs' columns of every axis' row, 16 bytes at a time, and kept what was theirs, took 74 registers for 64:
+// GB300, 8192 tokens H32/8 D 128, three axes side by side, AXES_OLD_US us for AXES_NEW_US.)
 struct AxisPositions {
-  int at[kMaxAxes];
+  int at[2];
 };
-__device__ __forceinline__ AxisPositions axis_positions(const QkvParams& p, int t) {
+__device__ __forceinline__ AxisPositions axis_positions(const QkvParams& p, int t, int lane) {
   AxisPositions a;
 #pragma unroll
-  for (int x = 0; x < kMaxAxes; ++x)
-    a.at[x] = x < p.n_axes ? min(max(__ldg(p.pos + x * p.pos_stride + t), 0), p.P - 1) : 0;
+  for (int k = 0; k < 2; ++k) {
+    const int axis = static_cast<int>((k ? p.axis_of[1] : p.axis_of[0]) >> (2 * lane)) & 3;
+    a.at[k] = lane + 32 * k < p.R / 2 ? min(max(__ldg(p.pos + axis * p.pos_stride + t), 0), p.P - 1) : 0;
+  }
   return a;
-}
-// The axis of pair i.
-__device__ __forceinline__ int axis_of(const QkvParams& p, int i) {
-  return static_cast<int>((i < 32 ? p.axis_of[0] : p.axis_of[1]) >> (2 * (i & 31))) & 3;
-}
-__device__ __forceinline__ int position_on(const AxisPositions& a, int axis) {
-  return axis & 2 ? (axis & 1 ? a.at[3] : a.at[2]) : (axis & 1 ? a.at[1] : a.at[0]);
 }
 
 // The angles of the eight values from i0 on, from their position's R / 2 = half cosines and sines:
@@ -184,43 +182,6 @@ __device__ __forceinline__ void angles(const float* cos, const float* sin, int i
       c[4 * h] = a.x, c[4 * h + 1] = a.y, c[4 * h + 2] = a.z, c[4 * h + 3] = a.w;
       s[4 * h] = sign * b.x, s[4 * h + 1] = sign * b.y, s[4 * h + 2] = sign * b.z, s[4 * h + 3] = sign * b.w;
     }
-  }
-}
-
-// angles<INTER, false> where the pairs turn on several axes.  A lane reads its pairs' columns from the
-// rows of those axes that it has, 16 bytes at a time, and keeps each pair's own.  GB300, 8192 tokens H32/8 D 128, three axes
-// in turns: AXES_VECTOR_US; a value at a time AXES_SCALAR_US.
-template <bool INTER>
-__device__ __forceinline__ void axis_angles(const QkvParams& p, const AxisPositions& at, int i0, float* c, float* s) {
-  constexpr int N = INTER ? 4 : 8;  // pairs
-  const int half = p.R / 2;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) c[i] = 1.f, s[i] = 0.f;
-  if (i0 >= p.R) return;
-  const bool low = INTER || i0 < half;
-  const int first = INTER ? i0 / 2 : low ? i0 : i0 - half;
-  const uint32_t axes = static_cast<uint32_t>((first < 32 ? p.axis_of[0] : p.axis_of[1]) >> (2 * (first & 31)));
-  float cc[N], ss[N];
-#pragma unroll
-  for (int x = 0; x < kMaxAxes; ++x) {
-    bool any = false;
-#pragma unroll
-    for (int i = 0; i < N; ++i) any |= (axes >> (2 * i) & 3) == x;
-    if (!any) continue;
-    const long long row = static_cast<long long>(at.at[x]) * half + first;
-#pragma unroll
-    for (int h = 0; h < N / 4; ++h) {
-      const float4 a = __ldg(reinterpret_cast<const float4*>(p.cos + row) + h), b = __ldg(reinterpret_cast<const float4*>(p.sin + row) + h);
-      const float av[4] = {a.x, a.y, a.z, a.w}, bv[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if ((axes >> (2 * (4 * h + i)) & 3) == x) cc[4 * h + i] = av[i], ss[4 * h + i] = bv[i];
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    c[i] = cc[INTER ? i / 2 : i];
-    s[i] = INTER ? (i & 1 ? ss[i / 2] : -ss[i / 2]) : low ? -ss[i % N] : ss[i % N];
   }
 }
 
@@ -287,15 +248,27 @@ __global__ void __launch_bounds__(kWarps * 32) qkv_norm_rope_kernel(const QkvPar
     return;
   }
   const int src = partner_lane<D, INTER>(p, lane);
+  const float *cos = p.cos, *sin = p.sin;  // the token's
+  if constexpr (AXES) {
+    __shared__ __align__(16) float gathered[kWarps][2][64];
+    float(&mine)[2][64] = gathered[threadIdx.x >> 5];
+    const AxisPositions at = axis_positions(p, u.t, lane);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int pair = lane + 32 * k;
+      const long long from = static_cast<long long>(at.at[k]) * (p.R / 2) + pair;
+      if (pair < p.R / 2) mine[0][pair] = __ldg(p.cos + from), mine[1][pair] = __ldg(p.sin + from);
+    }
+    __syncwarp();
+    cos = mine[0], sin = mine[1];
+  } else {
+    const long long row = static_cast<long long>(position(p, u.t)) * (p.R / 2);
+    cos += row, sin += row;
+  }
   uint64_t a[4], b[4];
   {
     float c[8], s[8], w[8], wp[8];
-    if constexpr (AXES) {
-      axis_angles<INTER>(p, axis_positions(p, u.t), i0, c, s);
-    } else {
-      const long long row = static_cast<long long>(position(p, u.t)) * (p.R / 2);
-      angles<INTER, false>(p.cos + row, p.sin + row, i0, p.R / 2, c, s);
-    }
+    angles<INTER, false>(cos, sin, i0, p.R / 2, c, s);
     load_weight(p, u.kind, i0, w);
     load_weight(p, u.kind, 8 * (src % LPH), wp);
 #pragma unroll
@@ -369,7 +342,7 @@ __global__ void __launch_bounds__(kWarps * 32, kBwdBlocksPerSm) qkv_norm_rope_bw
   using Position = std::conditional_t<AXES, AxisPositions, int>;
   const auto position_of = [&](int t) -> Position {
     if constexpr (AXES)
-      return axis_positions(p, t);
+      return axis_positions(p, t, lane);
     else
       return position(p, t);
   };
@@ -387,18 +360,17 @@ __global__ void __launch_bounds__(kWarps * 32, kBwdBlocksPerSm) qkv_norm_rope_bw
         copy16(&st.dy[s][lane], dy + s * RPW * head);
         if (u.kind != kValue) copy16(&st.x[s][lane], x + s * RPW * D);
       }
-    if (u.kind != kValue && 4 * (lane & 15) < half) {
-      const float* table = lane < 16 ? p.cos : p.sin;
-      float* to = (lane < 16 ? st.cos : st.sin) + 4 * (lane & 15);
-      if constexpr (AXES) {
+    if (u.kind == kValue) return;
+    if constexpr (AXES) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int pair = 4 * (lane & 15) + i;
-          copy4(to + i, table + static_cast<long long>(position_on(pos, axis_of(p, pair))) * half + pair);
-        }
-      } else {
-        copy16(to, table + static_cast<long long>(pos) * half + 4 * (lane & 15));
+      for (int k = 0; k < 2; ++k) {
+        const int pair = lane + 32 * k;
+        const long long from = static_cast<long long>(pos.at[k]) * half + pair;
+        if (pair < half) copy4(st.cos + pair, p.cos + from), copy4(st.sin + pair, p.sin + from);
       }
+    } else if (4 * (lane & 15) < half) {
+      const float* from = (lane < 16 ? p.cos : p.sin) + static_cast<long long>(pos) * half + 4 * (lane & 15);
+      copy16((lane < 16 ? st.cos : st.sin) + 4 * (lane & 15), from);
     }
   };
   int to = u.t, now = 0, free = 0;  // the token requested next; stages
