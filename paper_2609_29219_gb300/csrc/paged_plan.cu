@@ -49,7 +49,10 @@ __device__ __forceinline__ Sums scan(long long a, long long b, long long (*part)
           __shfl_sync(0xffffffffu, q, 31)};
 }
 
-__device__ __forceinline__ int pages_of(long long rows, int page) { return static_cast<int>((rows + page - 1) / page); }
+// (in 32 bits: rows and page - 1 are below 2^31; the 64-bit division took most of the kernel's instructions)
+__device__ __forceinline__ int pages_of(int rows, int page) {
+  return static_cast<int>((static_cast<unsigned>(rows) + static_cast<unsigned>(page) - 1u) / static_cast<unsigned>(page));
+}
 
 // The largest b with at[b] <= x, of n + 1 values that never decrease, at[0] <= x < at[n].
 __device__ __forceinline__ int holder(const int* at, int n, int x) {
@@ -82,35 +85,50 @@ __global__ void __launch_bounds__(kThreads) paged_plan_kernel(const PlanArgs p) 
   asm volatile("griddepcontrol.launch_dependents;");
 
   const int listed = min(max(*p.free_count, 0), p.num_pages);
-  long long tokens = 0, given = 0, asked = 0;
-  for (int b0 = 0; b0 < B; b0 += kThreads) {
-    const int b = b0 + static_cast<int>(threadIdx.x);
-    int n = 0, l = 0;
-    if (b < B) {
-      n = p.new_lens[b];
-      l = static_cast<int>(min(max(static_cast<long long>(p.lens[b]), 0ll), rows));
-    }
-    const Sums s = scan(max(n, 0), n < 0 ? pages_of(l, p.page) : 0, part);
-    const long long end = tokens + s.a + max(n, 0);
+  for (int b = threadIdx.x; b < B; b += kThreads) {
+    cu[b] = p.new_lens[b];
+    len[b] = static_cast<int>(min(max(static_cast<long long>(p.lens[b]), 0ll), rows));
+  }
+  __syncthreads();
+  // A thread has a few requests in a row, so that two scans of the block do for any number of them (a scan for every
+  // 1024 took 3 us each: 8192 requests 29.1 us for 16.8).
+  // An odd number, so that the threads of a warp meet in no bank.
+  const int each = (B + kThreads - 1) / kThreads | 1, b0 = min(B, each * static_cast<int>(threadIdx.x)), b1 = min(B, b0 + each);
+  long long n_sum = 0, rel_sum = 0;
+  for (int b = b0; b < b1; ++b) {
+    n_sum += max(cu[b], 0);
+    rel_sum += cu[b] < 0 ? pages_of(len[b], p.page) : 0;
+  }
+  const Sums s = scan(n_sum, rel_sum, part);
+  const long long given = s.all_b;
+  // (0 where the row or the step has no room; off holds it until the sums are known)
+  long long end = s.a, back = s.b, need_sum = 0;
+  for (int b = b0; b < b1; ++b) {
+    const int n = cu[b], l = len[b];
+    const long long begin = end;
+    end += max(n, 0);
     const bool fits = n >= 0 && l + static_cast<long long>(n) <= rows && end <= p.T;
-    const int need = fits && n > 0 ? pages_of(l + static_cast<long long>(n), p.page) - pages_of(l, p.page) : 0;
-    const Sums t = scan(need, 0, part);
-    if (b < B) {
-      cu[b] = static_cast<int>(min(tokens + s.a, static_cast<long long>(p.T)));
-      rel[b] = static_cast<int>(min(given + s.b, static_cast<long long>(p.num_pages)));
-      off[b] = static_cast<int>(min(asked + t.a, static_cast<long long>(p.num_pages) + 1));
-      len[b] = l;
-      // (whether the pages reach it is known when all that are given back are)
-      state[b] = n < 0 ? kOver : fits ? (need == 0 || asked + t.a + need <= p.num_pages ? kGranted : 0) : 0;
-    }
-    tokens += s.all_a;
-    given += s.all_b;
-    asked += t.all_a;
+    const int need = fits && n > 0 ? pages_of(l + n, p.page) - pages_of(l, p.page) : 0;
+    off[b] = need;
+    need_sum += need;
+    cu[b] = static_cast<int>(min(begin, static_cast<long long>(p.T)));
+    rel[b] = static_cast<int>(min(back, static_cast<long long>(p.num_pages)));
+    if (n < 0) back += pages_of(l, p.page);
+    state[b] = n < 0 ? kOver : fits ? kGranted : 0;
+  }
+  const Sums t = scan(need_sum, 0, part);
+  long long asked = t.a;
+  for (int b = b0; b < b1; ++b) {
+    const int need = off[b];
+    off[b] = static_cast<int>(min(asked, static_cast<long long>(p.num_pages) + 1));
+    asked += need;
+    // (past all pages there are: the sorted offsets do not tell these apart)
+    if (need && asked > p.num_pages) state[b] = 0;
   }
   if (threadIdx.x == 0) {
-    cu[B] = static_cast<int>(min(tokens, static_cast<long long>(p.T)));
+    cu[B] = static_cast<int>(min(s.all_a, static_cast<long long>(p.T)));
     rel[B] = static_cast<int>(min(given, static_cast<long long>(p.num_pages)));
-    off[B] = static_cast<int>(min(asked, static_cast<long long>(p.num_pages) + 1));
+    off[B] = static_cast<int>(min(t.all_a, static_cast<long long>(p.num_pages) + 1));
   }
   __syncthreads();
   const int total = static_cast<int>(min(listed + given, static_cast<long long>(p.num_pages)));
@@ -144,15 +162,27 @@ __global__ void __launch_bounds__(kThreads) paged_plan_kernel(const PlanArgs p) 
     p.block_table[static_cast<size_t>(b) * p.max_pages + pages_of(len[b], p.page) + (k - off[b])] = fresh_page(k);
   }
   for (int i = listed + first; i < total - taken; i += step) p.free_pages[i] = listed_page(i);
-  for (int t = first; t < p.T; t += step) {
+  // A warp takes as many tokens in a row as it has to, looks for its first and last one's request among all, and
+  // for the others between those (for each among all: 4096 requests of 15 tokens 18.3 us, here 16.6).
+  const int lane = static_cast<int>(threadIdx.x & 31), warps = step / 32;
+  const int mine = ((p.T + warps - 1) / warps + 31) / 32 * 32;
+  const long long t0 = static_cast<long long>(first / 32) * mine;
+  if (t0 >= p.T) return;
+  const int end_t = static_cast<int>(min(t0 + mine, static_cast<long long>(p.T))), real = min(end_t, cu[B]);  // (past real: padding)
+  int low = 0, high = 0;
+  if (t0 < real) low = holder(cu, B, static_cast<int>(t0)), high = holder(cu, B, real - 1);
+#pragma unroll 4
+  for (int i = 0; i < mine; i += 32) {
+    const long long t = t0 + i + lane;
+    if (t >= end_t) continue;
     int pos = 0, slot = -1;
-    if (t < cu[B]) {
-      const int b = holder(cu, B, t);
+    if (t < real) {
+      const int b = low + holder(cu + low, high + 1 - low, static_cast<int>(t));
       if (is_granted(b)) {
-        pos = len[b] + (t - cu[b]);
-        const int j = pos / p.page, held = pages_of(len[b], p.page);
+        pos = len[b] + (static_cast<int>(t) - cu[b]);
+        const int j = static_cast<int>(static_cast<unsigned>(pos) / static_cast<unsigned>(p.page)), held = pages_of(len[b], p.page);
         const int at = j < held ? p.block_table[static_cast<size_t>(b) * p.max_pages + j] : fresh_page(off[b] + j - held);
-        if (at >= 0 && at < p.num_pages) slot = at * p.page + pos % p.page;
+        if (at >= 0 && at < p.num_pages) slot = at * p.page + (pos - j * p.page);
       }
     }
     p.positions[t] = pos;

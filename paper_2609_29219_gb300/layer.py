@@ -1,10 +1,11 @@
-"""A decoder's attention layer on the library: trained with its gradients, then run token by token
-over a paged cache with the same weights.
+"""A decoder's attention layer on the library: trained with its gradients, then run over a paged cache
+with the same weights, token by token, or with whatever tokens each request brings to a step.
 
     python -m paper_2609_29219_gb300.layer
 
 trains a small layer for some steps to imitate another one, prints the loss, and checks that
-decoding the sequence through the cache gives what the prefill gives.
+decoding the sequence through the cache gives what the prefill gives, and that serving requests of
+unlike lengths in chunks does.
 """
 from __future__ import annotations
 
@@ -45,6 +46,27 @@ class PagedCache:
         return pos.reshape(-1), slots.reshape(-1)
 
 
+class RequestCache:
+    """K and V pages [num_pages, page, Hkv, D] shared by up to `requests` requests of `capacity` tokens, which
+    take pages as they grow and give them back when they end.  All of it is on the device: a step that
+    was captured can be replayed."""
+
+    def __init__(self, requests, num_pages, capacity, Hkv, D, page=16, device="cuda"):
+        i32 = dict(dtype=torch.int32, device=device)
+        self.page = page
+        self.k, self.v = (torch.zeros((num_pages, page, Hkv, D), dtype=torch.bfloat16, device=device) for _ in range(2))
+        self.table = torch.full((requests, -(-capacity // page)), -1, **i32)
+        self.lens = torch.zeros(requests, **i32)
+        self.free_pages, self.free_count = torch.arange(num_pages, **i32), torch.full((1,), num_pages, **i32)
+
+    def plan(self, new_lens, num_tokens):
+        """Takes `new_lens` more tokens of each request (negative: it is over) into a step of num_tokens:
+        (cu_seqlens, positions, slots, granted)."""
+        cu, _, positions, slots, granted = loom.loom_paged_plan(new_lens, self.lens, self.table, self.free_pages, self.free_count,
+                                                                num_tokens, self.page, seqlens_k=self.lens)
+        return cu, positions, slots, granted
+
+
 class AttentionLayer:
     """y = attention(rotated norms of x W_qkv^T) W_o^T with grouped queries; weights in bf16."""
 
@@ -76,6 +98,17 @@ class AttentionLayer:
         qkv = loom.loom_gemm_bf16(x, self.w_qkv, b_transposed=True)
         q = loom.loom_qkv_norm_rope_cache(qkv, self.q_norm, self.k_norm, self.cos, self.sin, pos, slots, cache.k, cache.v, self.Hq)
         o = loom.loom_attn_decode_paged(q.unsqueeze(2), cache.k, cache.v, cache.table, cache.lens)
+        return loom.loom_gemm_bf16(o.view(x.shape[0], -1), self.w_o, b_transposed=True)
+
+    @torch.no_grad()
+    def serve(self, x, cache, new_lens):
+        """The new tokens of a RequestCache's requests, packed, x [T, model]: prompts, chunks of them, single tokens.
+        Rows past the last request's (and those of requests that the cache had no room for) mean nothing.  The
+        rotation tables must reach the cache's capacity."""
+        cu, positions, slots, _ = cache.plan(new_lens, x.shape[0])
+        qkv = loom.loom_gemm_bf16(x, self.w_qkv, b_transposed=True)
+        q = loom.loom_qkv_norm_rope_cache(qkv, self.q_norm, self.k_norm, self.cos, self.sin, positions, slots, cache.k, cache.v, self.Hq)
+        o = loom.loom_attn_chunk_paged(q, cache.k, cache.v, cache.table, cu, cache.lens)
         return loom.loom_gemm_bf16(o.view(x.shape[0], -1), self.w_o, b_transposed=True)
 
 
@@ -114,6 +147,17 @@ def main():
     cache = PagedCache(B, S, shape["Hkv"], shape["D"])
     got = torch.stack([layer.step(x[:, i].contiguous(), cache) for i in range(S)], 1)
     loom.loom_attn_check_error()
+    requests = RequestCache(B, 16, 64, shape["Hkv"], shape["D"])
+    parts, done = [[] for _ in range(B)], [0] * B
+    for new in ((17, 3), (1, 30), (22, 7)):
+        y = layer.serve(torch.cat([x[b, done[b]:done[b] + n] for b, n in enumerate(new)]), requests,
+                        torch.tensor(new, dtype=torch.int32, device="cuda"))
+        for b, (n, part) in enumerate(zip(new, y.split(new))):
+            parts[b].append(part)
+            done[b] += n
+    served = torch.stack([torch.cat(p) for p in parts])
+    loom.loom_attn_check_error()
+    print(f"serving in chunks against prefill: largest difference {float((served.float() - want.float()).abs().max()):.2e}")
     print(f"decoding token by token against prefill: largest difference {float((got.float() - want.float()).abs().max()):.2e} "
           f"of {float(want.float().abs().max()):.2f}")
 
