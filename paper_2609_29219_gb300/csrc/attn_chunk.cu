@@ -16,7 +16,7 @@
 // TMEM, m and l through shared memory), so that its steps overlap too.
 //
 // Dealing.  All units lie on one line, in order, each as long as its modelled cost: kUnitCost and a
-// weight per key.  CTA c of G takes the stretch [W c / G, W (c + 1) / G) of the line's W, cut to
+// weight per key.  CTA c of G takes the c-th of G equal stretches of the line's W, cut to
 // whole key tiles of the units it starts and ends in.  So the CTAs finish together for any mixture of
 // prompts and single tokens, no list of items is made in memory, and nothing depends on timing: the
 // sequences' prefix sum and a binary search give each CTA its first unit, and one warp walks on from there,
@@ -44,7 +44,7 @@ constexpr float kRescaleThreshold = 8.0f;  // base-2 units; P <= 2^8 between res
 // The line's units: a key of a pair of tiles costs 1 << kKeyLg2, of a single tile 1 << kKeyLg1; a unit kUnitCost more.
 constexpr int kKeyLg2 = 3, kKeyLg1 = 2, kUnitCost = 3072;
 // The least that a CTA is given of units that are longer: they are not cut into shorter pieces.
-constexpr int kLeastStretch = 4608;
+constexpr int kLeastStretch = 3072;
 
 template <int D>
 struct ChunkCfg {
@@ -143,14 +143,16 @@ struct Line {
   __device__ __forceinline__ void set(long long length, int units, int ctas, int cta) {
     W = length;
     G = ctas;
-    if (units < ctas && W < static_cast<long long>(ctas) * kLeastStretch) G = max(max(1, units), static_cast<int>(W) / kLeastStretch);
+    // (as many for each unit, so that equal ones are not cut where they need not be)
+    if (units < ctas && W < static_cast<long long>(ctas) * kLeastStretch)
+      G = max(1, min(ctas, units * max(1, static_cast<int>(W) / (max(units, 1) * kLeastStretch))));
     each = quotient(W, G);
     rest = static_cast<int>(W - each * G);
     x0 = cta < G ? bound(cta) : W;
     x1 = cta + 1 < G ? bound(cta + 1) : W;
   }
   // Where CTA c's stretch begins.
-  __device__ __forceinline__ long long bound(int c) const { return each * c + static_cast<unsigned>(rest * c) / static_cast<unsigned>(G); }
+  __device__ __forceinline__ long long bound(int c) const { return each * c + min(c, rest); }
 };
 // Key tiles of a unit that lie before the place d > 0 behind its beginning.
 __device__ __forceinline__ int tiles_before(long long d, int key_lg, int tiles) {
@@ -172,7 +174,7 @@ struct Item {
   int tiles;                      // all its key tiles
   int two;                        // it has two query tiles
   int key_lg;                     // a key's cost
-  int first, pieces;              // cut: the first CTA that has a piece, and how many have
+  int first, pieces;              // cut: the first CTA that has a piece, and how many have (written before the next record)
   long long at, cost;             // its place on the line
   __device__ __forceinline__ bool cut() const { return n < tiles; }
 };
@@ -415,15 +417,21 @@ __device__ __forceinline__ float row_lse(float m, float l) { return l == 0.f ? -
 // Counts one more piece of a 32-row group: how many have come.  A count without the tag (see ChunkParams) is
 // whatever the workspace held before, and begins anew; a launch leaves its counts at zero.
 __device__ __forceinline__ int count_piece(unsigned long long* at, unsigned long long tag) {
-  unsigned long long was = atomicAdd(at, 1ull);
+  // (released: the warp's pieces before it; acquired: the others' behind it)
+  const auto add = [&]() {
+    unsigned long long was;
+    asm volatile("atom.acq_rel.gpu.global.add.u64 %0, [%1], 1;" : "=l"(was) : "l"(at) : "memory");
+    return was;
+  };
+  unsigned long long was = add();
   while ((was ^ tag) >> 16) {
     const unsigned long long seen = was + 1;
-    was = atomicCAS(at, seen, tag + 1);
+    asm volatile("atom.acq_rel.gpu.global.cas.b64 %0, [%1], %2, %3;" : "=l"(was) : "l"(at), "l"(seen), "l"(tag + 1) : "memory");
     if (was == seen) return 1;
     if ((was ^ tag) >> 16)
       --was;  // (another's count on top of what there was)
     else
-      was = atomicAdd(at, 1ull);
+      was = add();
   }
   return static_cast<int>(was & 0xffff) + 1;
 }
@@ -437,7 +445,6 @@ struct RowSums {
   float m, l, w0, w1;
   bool has, both;  // key tiles were walked here
   bool any;        // the warp has a row
-  bool alive;      // no wait has given up
 };
 
 // 32 columns of a row's O from column c on, weighted and summed.
@@ -594,7 +601,7 @@ __device__ __noinline__ void finish_piece(const ChunkParams& p, const Line& ln, 
   const int lane = threadIdx.x & 31, group = it.two ? warp : warp & 3;
   const bool row = r.at >= 0;
   const int slot = it.lo == 0 ? 2 * static_cast<int>(blockIdx.x) + 1 : 2 * static_cast<int>(blockIdx.x);
-  if (r.alive && r.any) {
+  if (r.any) {
     float4* mine = reinterpret_cast<float4*>(p.part) + (static_cast<size_t>(slot) * p.groups + group) * (D / 4) * 32 + lane;
     if (r.has) {
 #pragma unroll 1
@@ -610,13 +617,12 @@ __device__ __noinline__ void finish_piece(const ChunkParams& p, const Line& ln, 
     }
     if (row) p.part_ml[(static_cast<size_t>(slot) * p.groups + group) * 32 + lane] = make_float2(r.m, r.has ? r.l : -1.f);
   }
-  if (r.alive && r.has) release_o(r, bar_oe, bar_oe1);
+  if (r.has) release_o(r, bar_oe, bar_oe1);
   if (!r.any) return;
-  __threadfence();
   __syncwarp();
-  if (!last_piece(p, it.pieces, it.first, warp) || !r.alive) return;
+  if (!last_piece(p, it.pieces, it.first, warp)) return;
+  __syncwarp();
   list_pieces(ln, it, it.first, stg);
-  __threadfence();
   // The warp's rows (its first lanes') are spread over all lanes: 1 << lg of them side by side, each lane with
   // every (32 >> lg)-th 16 bytes of its row.
   const int rows = __popc(__ballot_sync(0xffffffffu, row));
@@ -804,17 +810,18 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
       Item it;
       more = next_item(p, l, walk, it);
       if (!more) it.n = -1;
-      if (more && it.cut()) {
-        it.first = first_cta(l, it);
-        it.pieces = count_pieces(l, it, it.first);
-      }
       const int i = k % C::NREC;
       if (k >= C::NREC && !wait_warp(bar_rece + 8 * i, (k / C::NREC - 1) & 1, p.ctl, ab)) break;
+      Item& rec = *reinterpret_cast<Item*>(smem + C::REC_OFF + i * 80);
       if (lane == 0) {
-        *reinterpret_cast<Item*>(smem + C::REC_OFF + i * 80) = it;
+        rec = it;
         mbar_arrive(bar_rec + 8 * i);
       }
       __syncwarp();
+      if (more && it.cut()) {
+        const int first = first_cta(l, it), pieces = count_pieces(l, it, first);
+        if (lane == 0) rec.first = first, rec.pieces = pieces;
+      }
     }
   } else if (warp == 8 || warp == 10) {
     // ------------------------------------------------------------------ loaders (whole warps): Q and K, and V
@@ -1063,7 +1070,7 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
         }
       } else {
         alive = alive && (n == 0 || wait_warp(my_o, items & 1, p.ctl, ab));
-        RowSums r{-1, nullptr, m_run, l_run, 1.f, 0.f, n > 0, both, any, alive};
+        RowSums r{-1, nullptr, m_run, l_run, 1.f, 0.f, n > 0, both, any};
         if (both) {
           alive = alive && wait_warp(bar_o + 8, items1 & 1, p.ctl, ab) && wait_warp(bar_ml, shared & 1, p.ctl, ab);
           if (alive) {
@@ -1075,7 +1082,6 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
             r.w1 = ex2(other.x - base);
             r.l = r.w0 * l_run + r.w1 * other.y;
           }
-          r.alive = alive;
         }
         tc_fence_after();
         const long long unit_at = static_cast<long long>(it.qb + it.t0) * p.Hq * D;  // its first token's place in O
@@ -1085,6 +1091,9 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
           if (p.lse) r.lse_at = p.lse + static_cast<size_t>(head) * p.total_q + it.qb + token;
         }
         if (it.cut()) {
+          // (the next record: behind it the numbers of the pieces are there; where a wait gave up, see count_rest)
+          alive = alive && wait_warp(bar_rec + 8 * ((rec_n + 1) % C::NREC), ((rec_n + 1) / C::NREC) & 1, p.ctl, ab);
+          if (!alive) break;
           finish_piece<D>(p, ln, it, r, unit_at, o_tm, my_oe, bar_oe + 8, stg, warp);
           counted += any;
         } else if (alive && any) {
