@@ -165,7 +165,7 @@ __global__ void __launch_bounds__(kThreads) paged_plan_kernel(const PlanArgs p) 
   // A warp takes as many tokens in a row as it has to, looks for its first and last one's request among all, and
   // for the others between those (for each among all: 4096 requests of 15 tokens 18.3 us, here 16.6).
   const int lane = static_cast<int>(threadIdx.x & 31), warps = step / 32;
-  const int mine = ((p.T + warps - 1) / warps + 31) / 32 * 32;
+  const int mine = static_cast<int>(((static_cast<unsigned>(p.T) + warps - 1) / warps + 31) / 32 * 32);
   const long long t0 = static_cast<long long>(first / 32) * mine;
   if (t0 >= p.T) return;
   const int end_t = static_cast<int>(min(t0 + mine, static_cast<long long>(p.T))), real = min(end_t, cu[B]);  // (past real: padding)

@@ -81,6 +81,16 @@ def test_refused_for_the_table_and_for_the_tokens(loom):
     _check(loom, [3, 32, 2, 9], [30, 0, 30, 5], table, free, 10, 0, 16, num)
 
 
+def test_as_many_tokens_as_there_may_be(loom):
+    T = (1 << 31) - 1
+    table, free = _ints([[0] * 4]), _ints(range(4))
+    cu, _, positions, slots, granted = loom.loom_paged_plan(_ints([20]), _ints([0]), table, free, _ints([4]), T, 16)
+    assert cu.tolist() == [0, 20] and granted.tolist() == [20] and positions[:20].tolist() == list(range(20))
+    assert slots[:20].tolist() == [3 * 16 + i for i in range(16)] + [2 * 16 + i for i in range(4)]
+    for at in (20, 1 << 30, T - 70000):  # (the largest step's ends and one in its middle)
+        assert (slots[at:at + 70000] == -1).all() and (positions[at:at + 70000] == 0).all()
+
+
 def test_every_page_is_given_back(loom):
     lens = [40, 0, 17, 64]
     table, free, num = _tables(random.Random(4), lens, 6, 16, 3)
