@@ -18,6 +18,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import operator
 import os
 import threading
 
@@ -924,7 +925,7 @@ def _axes_operands(qkv, cos, positions, pair_axis):
     _dev_ptr(positions, "positions", _i32, 2, qkv.get_device())
     if positions.shape[1] != qkv.shape[0]:
         raise ValueError("positions must be [axes, T] with pair_axis")
-    axes = _axis_array(pair_axis if type(pair_axis) is tuple else tuple(map(int, pair_axis)))
+    axes = _axis_array(tuple(map(operator.index, pair_axis)))  # (a copy: what it was given may change)
     if len(axes) != cos.shape[1]:
         raise ValueError(f"pair_axis must name an axis for each of the {cos.shape[1]} pairs that the tables have")
     if not all(0 <= a < positions.shape[0] for a in axes):
@@ -1008,8 +1009,9 @@ def loom_qkv_norm_rope(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_head
     if v is None:
         v = new(ks, kst, _bf16)
     lib = _lib or capi()
-    st = (lib.loom_qkv_norm_rope if pair_axis is None else lib.loom_qkv_norm_rope_axes)(qkv.data_ptr(), row, *norm, q.data_ptr(), k.data_ptr(), v.data_ptr(), T, S, num_heads,
-                                             num_kv_heads, D, float(eps), _stream_of(stream, qkv))
+    st = (lib.loom_qkv_norm_rope if pair_axis is None else lib.loom_qkv_norm_rope_axes)(
+        qkv.data_ptr(), row, *norm, q.data_ptr(), k.data_ptr(), v.data_ptr(), T, S, num_heads, num_kv_heads, D, float(eps),
+        _stream_of(stream, qkv))
     if st:
         raise LoomError(st, "loom_qkv_norm_rope")
     return q, k, v

@@ -9,6 +9,8 @@ The kernels have first gradients only: differentiating a gradient raises.
 """
 from __future__ import annotations
 
+import operator
+
 import torch
 from torch.autograd.function import once_differentiable
 
@@ -89,7 +91,7 @@ def qkv_norm_rope(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, po
         if t.requires_grad and torch.is_grad_enabled():
             raise ValueError(f"{name} requires a gradient, which qkv_norm_rope does not have: detach it")
     return _QkvNormRope.apply(qkv, q_weight, k_weight, cos, sin, num_heads, num_kv_heads, positions, seq_len, eps, interleaved,
-                              None if pair_axis is None else tuple(pair_axis))
+                              None if pair_axis is None else tuple(map(operator.index, pair_axis)))
 
 
 class _Linear(torch.autograd.Function):

@@ -130,6 +130,20 @@ def test_gradients_through_autograd(loom):  # noqa: F811
         assert abs((got * d).sum() - change) <= (bound * d.abs()).sum() + 1e-6 * abs(change) + 1e-6
 
 
+def test_axes_in_a_list_that_changes(loom):  # noqa: F811
+    """What pair_axis was is read at the call: a list or a tensor's numbers changed since are other axes."""
+    import torch
+    c = AxesCase(10, 4, 2, 64, 32, 0)
+    call = lambda axis: loom.loom_qkv_norm_rope(c.qkv, *c.args(), 4, 2, c.pos.cuda(), pair_axis=axis)[0]  # noqa: E731
+    one, other = [0] * 16, [1] * 16
+    for kind in (list, torch.tensor, lambda x: tuple(torch.tensor(x))):
+        axis = kind(one)
+        assert torch.equal(call(axis), call(tuple(one)))
+        for i in range(16):
+            axis[i].fill_(1) if isinstance(axis, tuple) else axis.__setitem__(i, 1)
+        assert torch.equal(call(axis), call(tuple(other))) and not torch.equal(call(axis), call(tuple(one)))
+
+
 def test_refusals(loom):  # noqa: F811
     c = AxesCase(10, 4, 2, 64, 32, 0)
     call = lambda pos, axis, **kw: loom.loom_qkv_norm_rope(c.qkv, *c.args(), 4, 2, pos, pair_axis=axis, **kw)  # noqa: E731
@@ -150,6 +164,8 @@ def test_refusals(loom):  # noqa: F811
         call(pos, [3] * 16)
     with pytest.raises(ValueError, match="do not have"):
         call(pos, [-1] * 16)
+    with pytest.raises(TypeError, match="integer"):
+        call(pos, [0.5] * 16)
     with pytest.raises(loom.LoomError, match="UNSUPPORTED"):
         call(pos[:1].expand(5, -1).contiguous(), c.axis)
     with pytest.raises(ValueError, match="1 dims"):
