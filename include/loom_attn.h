@@ -210,8 +210,9 @@ loom_status loom_attn_decode_paged(const void* q, const void* k_cache, const voi
  * reaches no output, whatever it is; a NaN or infinity in the value of one of a sequence's keys may
  * reach all its queries.  Sums have a fixed order: the same inputs give the same bits.
  * Errors: INVALID_ARG (NULL pointer, a size <= 0, total_q < 0, Hq % Hkv, scale, kv_layout, causal),
- * UNSUPPORTED (as loom_attn_decode_paged; more than 2^31 - 1 query rows total_q Hq), MISALIGNED (q,
- * caches, o, workspace: 16 bytes; the others 4), WORKSPACE, CUDA.  total_q = 0 returns LOOM_OK at once.
+ * UNSUPPORTED (as loom_attn_decode_paged; Hq > 65536; more than 2^31 - 1 query rows total_q Hq),
+ * MISALIGNED (q, caches, o, workspace: 16 bytes; the others 4), WORKSPACE, CUDA.  total_q = 0 returns
+ * LOOM_OK at once.
  */
 loom_status loom_attn_chunk_paged(const void* q, const void* k_cache, const void* v_cache,
                                   const int32_t* block_table, const int32_t* cu_seqlens_q,

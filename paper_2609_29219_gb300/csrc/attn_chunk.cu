@@ -46,7 +46,7 @@ constexpr int kKeyLg2 = 3, kKeyLg1 = 2, kUnitCost = 3000;
 // The least that a CTA is given of units that are longer: they are not cut into shorter pieces.
 constexpr int kLeastStretch = 3000;
 // A cut that would leave less than this of a unit's tiles on one side falls on its end: joining a piece costs more
-// than the unevenness.  One token after 4095: 22.0 us with every cut, 19.2 so, 21.9 with twice this; 128 tokens, 64
+// than the unevenness.  One token after 4095: 22.0 us with every cut, 19.2 to 21.2 so, 21.9 with twice this; 128 tokens, 64
 // wide, after 10 to 500: 47.2, 44.5, 44.3; 16 tokens after 4K to 8K: 75.0, 75.5, 77.3.
 constexpr int kSnap = 1024;
 
@@ -118,6 +118,7 @@ __device__ __forceinline__ int keys_until(const ChunkParams& p, const Seq& s, lo
   if (!p.causal) return s.skv;
   return static_cast<int>(max(0ll, min(end, static_cast<long long>(s.sq)) + s.skv - s.sq));
 }
+__device__ __forceinline__ int key_tiles(int keys) { return static_cast<int>((static_cast<unsigned>(keys) + 127u) / 128u); }
 __device__ __forceinline__ int key_lg(const ChunkParams& p, const Seq& s, int pair) {
   return s.sq - 2ll * p.tq * pair > p.tq ? kKeyLg2 : kKeyLg1;
 }
@@ -162,7 +163,7 @@ struct Line {
 __device__ __forceinline__ int tiles_before(long long d, int key_lg, int tiles) {
   const long long t = (d - kUnitCost + (128 << key_lg) - 1) >> (key_lg + 7);
   const int n = t < 0 ? 0 : t < tiles ? static_cast<int>(t) : tiles;
-  return (min(n, tiles - n) << (key_lg + 7)) < kSnap ? (2 * n < tiles ? 0 : tiles) : n;
+  return min(n, tiles - n) < (kSnap + (128 << key_lg) - 1) >> (key_lg + 7) ? (2 * n < tiles ? 0 : tiles) : n;
 }
 
 // A place on the line: unit `pair` of a plane of sequence b, which begins at `at`.
@@ -199,13 +200,13 @@ __device__ __forceinline__ bool next_item(const ChunkParams& p, const Line& ln, 
     it.two = w.s.sq - it.t0 > p.tq;
     it.key_lg = it.two ? kKeyLg2 : kKeyLg1;
     const int keys = keys_until(p, w.s, step * (w.pair + 1));
-    it.tiles = (keys + 127) / 128;
+    it.tiles = key_tiles(keys);
     it.at = w.at;
     it.cost = kUnitCost + (static_cast<long long>(keys) << it.key_lg);
     it.lo = ln.x0 > it.at ? tiles_before(ln.x0 - it.at, it.key_lg, it.tiles) : 0;
     const int hi = ln.x1 < it.at + it.cost ? tiles_before(ln.x1 - it.at, it.key_lg, it.tiles) : it.tiles;
     it.n = hi - it.lo;
-    it.n0 = it.two ? max(0, min(hi, (keys_until(p, w.s, it.t0 + p.tq) + 127) / 128) - it.lo) : (it.n + 1) / 2;
+    it.n0 = it.two ? max(0, min(hi, key_tiles(keys_until(p, w.s, it.t0 + p.tq))) - it.lo) : (it.n + 1) / 2;
     it.n1 = it.two ? it.n : it.n / 2;
     w.at += it.cost;
     if (++w.pair == w.s.pairs) {
@@ -865,8 +866,8 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
       if (lo == end) continue;  // no keys: nothing to load
       // the page of this lane's piece of key tile j (none past the sequence's keys)
       const auto page_of = [&](int j) {
-        const int key = j * C::BN + lane * rows;
-        return lane * rows < C::BN && key < skv ? table[static_cast<unsigned>(key) / static_cast<unsigned>(p.page)] : -1;
+        if (lane * rows >= C::BN || j * C::BN + lane * rows >= skv) return -1;
+        return table[static_cast<unsigned>(j * C::BN + lane * rows) / static_cast<unsigned>(p.page)];
       };
       int page = page_of(lo);
       if (!is_v && n0 > 0 && !(ok = load_q(two ? 0 : q_single, plane, token))) break;
@@ -1032,7 +1033,7 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
       const bool row = row_token < p.tq && token < it.sq;
       const bool any = __any_sync(0xffffffffu, row);
       const int query = min(token, it.sq - 1);  // (a row that is none: masked like the last)
-      const int limit = (p.causal ? max(0, query + it.skv - it.sq + 1) : it.skv) - it.lo * C::BN;
+      const int limit = (p.causal ? max(0, query - it.sq + 1 + it.skv) : it.skv) - it.lo * C::BN;
       // The unit's last tile here, where it reaches past the sequence's keys: what V's rows hold there (other
       // keys, or nothing that was ever written) must not meet P = 0, so they are cleared, by the
       // warps whose P.V comes first.

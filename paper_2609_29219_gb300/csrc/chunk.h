@@ -24,6 +24,8 @@ struct ChunkArgs {
   PagedKV pages;
 };
 
+constexpr int kMaxChunkHeads = 65536;  // query heads: what a unit's places in O leave room for in 32 bits
+
 size_t chunk_workspace_bytes(int Hq, int Hkv, int total_q, int D, int sms);
 cudaError_t launch_chunk_paged(const ChunkArgs& a, const KernelCtl& ctl, cudaStream_t stream);
 

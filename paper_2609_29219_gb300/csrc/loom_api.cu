@@ -424,7 +424,7 @@ loom_status loom_attn_bwd_varlen(const void* dout, const void* q, const void* k,
 namespace {
 // Sizes of a chunk call that there is a kernel for.
 bool chunk_sizes_ok(int B, int Hq, int Hkv, int total_q, int D) {
-  return (D == 64 || D == 128) && static_cast<long long>(total_q) * Hq <= 0x7fffffffLL;
+  return (D == 64 || D == 128) && Hq <= kMaxChunkHeads && static_cast<long long>(total_q) * Hq <= 0x7fffffffLL;
 }
 }  // namespace
 
@@ -614,74 +614,79 @@ loom_status norm_rope_bwd_call(QkvArgs& a, const void* dq, const void* dk, const
 }  // namespace
 
 loom_status loom_qkv_norm_rope(const void* qkv, int64_t qkv_stride, const void* q_weight, const void* k_weight,
-                               int weight_type, const float* cos, const float* sin, int table_rows, int rotary_dim, int interleaved,
-                               const int32_t* positions,
-                               void* q, void* k, void* v, int T, int seq_len, int Hq, int Hkv, int D, float eps, void* stream) {
+                               int weight_type, const float* cos, const float* sin, int table_rows, int rotary_dim,
+                               int interleaved, const int32_t* positions, void* q, void* k, void* v, int T,
+                               int seq_len, int Hq, int Hkv, int D, float eps, void* stream) {
   QkvArgs a{};
-  const loom_status st = qkv_common(&a, qkv, qkv_stride, q_weight, k_weight, weight_type, cos, sin, table_rows, rotary_dim, interleaved,
-                              positions, T, Hq, Hkv, D, eps);
+  const loom_status st = qkv_common(&a, qkv, qkv_stride, q_weight, k_weight, weight_type, cos, sin, table_rows, rotary_dim,
+                                    interleaved, positions, T, Hq, Hkv, D, eps);
   return st != LOOM_OK ? st : norm_rope_call(a, q, k, v, seq_len, stream);
 }
 
 loom_status loom_qkv_norm_rope_cache(const void* qkv, int64_t qkv_stride, const void* q_weight, const void* k_weight,
-                                     int weight_type, const float* cos, const float* sin, int table_rows, int rotary_dim, int interleaved,
-                                     const int32_t* positions,
-                                     const int32_t* slots, void* q, void* k_cache, void* v_cache, int num_pages, int page_size,
+                                     int weight_type, const float* cos, const float* sin, int table_rows,
+                                     int rotary_dim, int interleaved, const int32_t* positions, const int32_t* slots,
+                                     void* q, void* k_cache, void* v_cache, int num_pages, int page_size,
                                      int kv_layout, int T, int Hq, int Hkv, int D, float eps, void* stream) {
   QkvArgs a{};
-  const loom_status st = qkv_common(&a, qkv, qkv_stride, q_weight, k_weight, weight_type, cos, sin, table_rows, rotary_dim, interleaved,
-                              positions, T, Hq, Hkv, D, eps);
+  const loom_status st = qkv_common(&a, qkv, qkv_stride, q_weight, k_weight, weight_type, cos, sin, table_rows, rotary_dim,
+                                    interleaved, positions, T, Hq, Hkv, D, eps);
   return st != LOOM_OK ? st : norm_rope_cache_call(a, slots, q, k_cache, v_cache, num_pages, page_size, kv_layout, stream);
 }
 
 size_t loom_qkv_norm_rope_bwd_workspace_bytes(int D) { return D == 64 || D == 128 ? qkv_bwd_workspace_bytes(D) : 0; }
 
 loom_status loom_qkv_norm_rope_bwd(const void* dq, const void* dk, const void* dv, const void* qkv, int64_t qkv_stride,
-                                   const void* q_weight, const void* k_weight,
-                                   int weight_type, const float* cos, const float* sin, int table_rows, int rotary_dim, int interleaved,
-                                   const int32_t* positions,
-                                   void* dqkv, int64_t dqkv_stride, float* dq_weight, float* dk_weight, void* workspace,
-                                   size_t workspace_bytes, int T, int seq_len, int Hq, int Hkv, int D, float eps, void* stream) {
+                                   const void* q_weight, const void* k_weight, int weight_type, const float* cos,
+                                   const float* sin, int table_rows, int rotary_dim, int interleaved,
+                                   const int32_t* positions, void* dqkv, int64_t dqkv_stride, float* dq_weight,
+                                   float* dk_weight, void* workspace, size_t workspace_bytes, int T, int seq_len,
+                                   int Hq, int Hkv, int D, float eps, void* stream) {
   QkvArgs a{};
-  const loom_status st = qkv_common(&a, qkv, qkv_stride, q_weight, k_weight, weight_type, cos, sin, table_rows, rotary_dim, interleaved,
-                              positions, T, Hq, Hkv, D, eps);
+  const loom_status st = qkv_common(&a, qkv, qkv_stride, q_weight, k_weight, weight_type, cos, sin, table_rows, rotary_dim,
+                                    interleaved, positions, T, Hq, Hkv, D, eps);
   return st != LOOM_OK ? st
                        : norm_rope_bwd_call(a, dq, dk, dv, dqkv, dqkv_stride, dq_weight, dk_weight, workspace, workspace_bytes,
                                             seq_len, stream);
 }
 
 loom_status loom_qkv_norm_rope_axes(const void* qkv, int64_t qkv_stride, const void* q_weight, const void* k_weight,
-                                    int weight_type, const float* cos, const float* sin, int table_rows, int rotary_dim, int interleaved,
-                                    const int32_t* positions, int64_t positions_stride, int n_axes, const int* pair_axis,
-                                    void* q, void* k, void* v, int T, int seq_len, int Hq, int Hkv, int D, float eps, void* stream) {
+                                    int weight_type, const float* cos, const float* sin, int table_rows,
+                                    int rotary_dim, int interleaved, const int32_t* positions,
+                                    int64_t positions_stride, int n_axes, const int* pair_axis, void* q, void* k,
+                                    void* v, int T, int seq_len, int Hq, int Hkv, int D, float eps, void* stream) {
   QkvArgs a{};
-  loom_status st = qkv_common(&a, qkv, qkv_stride, q_weight, k_weight, weight_type, cos, sin, table_rows, rotary_dim, interleaved,
-                              positions, T, Hq, Hkv, D, eps);
+  loom_status st = qkv_common(&a, qkv, qkv_stride, q_weight, k_weight, weight_type, cos, sin, table_rows, rotary_dim,
+                              interleaved, positions, T, Hq, Hkv, D, eps);
   if (st == LOOM_OK) st = axes_args(&a, positions_stride, n_axes, pair_axis);
   return st != LOOM_OK ? st : norm_rope_call(a, q, k, v, seq_len, stream);
 }
 
-loom_status loom_qkv_norm_rope_axes_cache(const void* qkv, int64_t qkv_stride, const void* q_weight, const void* k_weight,
-                                          int weight_type, const float* cos, const float* sin, int table_rows, int rotary_dim,
-                                          int interleaved, const int32_t* positions, int64_t positions_stride, int n_axes, const int* pair_axis,
-                                          const int32_t* slots, void* q, void* k_cache, void* v_cache, int num_pages, int page_size,
-                                          int kv_layout, int T, int Hq, int Hkv, int D, float eps, void* stream) {
+loom_status loom_qkv_norm_rope_axes_cache(const void* qkv, int64_t qkv_stride, const void* q_weight,
+                                          const void* k_weight, int weight_type, const float* cos, const float* sin,
+                                          int table_rows, int rotary_dim, int interleaved, const int32_t* positions,
+                                          int64_t positions_stride, int n_axes, const int* pair_axis,
+                                          const int32_t* slots, void* q, void* k_cache, void* v_cache, int num_pages,
+                                          int page_size, int kv_layout, int T, int Hq, int Hkv, int D, float eps,
+                                          void* stream) {
   QkvArgs a{};
-  loom_status st = qkv_common(&a, qkv, qkv_stride, q_weight, k_weight, weight_type, cos, sin, table_rows, rotary_dim, interleaved,
-                              positions, T, Hq, Hkv, D, eps);
+  loom_status st = qkv_common(&a, qkv, qkv_stride, q_weight, k_weight, weight_type, cos, sin, table_rows, rotary_dim,
+                              interleaved, positions, T, Hq, Hkv, D, eps);
   if (st == LOOM_OK) st = axes_args(&a, positions_stride, n_axes, pair_axis);
   return st != LOOM_OK ? st : norm_rope_cache_call(a, slots, q, k_cache, v_cache, num_pages, page_size, kv_layout, stream);
 }
 
-loom_status loom_qkv_norm_rope_axes_bwd(const void* dq, const void* dk, const void* dv, const void* qkv, int64_t qkv_stride,
-                                        const void* q_weight, const void* k_weight,
-                                        int weight_type, const float* cos, const float* sin, int table_rows, int rotary_dim, int interleaved,
-                                        const int32_t* positions, int64_t positions_stride, int n_axes, const int* pair_axis,
-                                        void* dqkv, int64_t dqkv_stride, float* dq_weight, float* dk_weight, void* workspace,
-                                        size_t workspace_bytes, int T, int seq_len, int Hq, int Hkv, int D, float eps, void* stream) {
+loom_status loom_qkv_norm_rope_axes_bwd(const void* dq, const void* dk, const void* dv, const void* qkv,
+                                        int64_t qkv_stride, const void* q_weight, const void* k_weight,
+                                        int weight_type, const float* cos, const float* sin, int table_rows,
+                                        int rotary_dim, int interleaved, const int32_t* positions,
+                                        int64_t positions_stride, int n_axes, const int* pair_axis, void* dqkv,
+                                        int64_t dqkv_stride, float* dq_weight, float* dk_weight, void* workspace,
+                                        size_t workspace_bytes, int T, int seq_len, int Hq, int Hkv, int D, float eps,
+                                        void* stream) {
   QkvArgs a{};
-  loom_status st = qkv_common(&a, qkv, qkv_stride, q_weight, k_weight, weight_type, cos, sin, table_rows, rotary_dim, interleaved,
-                              positions, T, Hq, Hkv, D, eps);
+  loom_status st = qkv_common(&a, qkv, qkv_stride, q_weight, k_weight, weight_type, cos, sin, table_rows, rotary_dim,
+                              interleaved, positions, T, Hq, Hkv, D, eps);
   if (st == LOOM_OK) st = axes_args(&a, positions_stride, n_axes, pair_axis);
   return st != LOOM_OK ? st
                        : norm_rope_bwd_call(a, dq, dk, dv, dqkv, dqkv_stride, dq_weight, dk_weight, workspace, workspace_bytes,

@@ -53,7 +53,6 @@ struct QkvParams {
   int w_f32;
   const float *cos, *sin;
   const int32_t* pos;
-  int n_axes;
   long long pos_stride;
   unsigned long long axis_of[2];
   int T, Hq, Hkv, R, P;
@@ -507,7 +506,6 @@ QkvParams params_of(const QkvArgs& a, int unroll) {
   p.cos = a.cos;
   p.sin = a.sin;
   p.pos = a.positions;
-  p.n_axes = a.n_axes;
   p.pos_stride = a.pos_stride;
   p.axis_of[0] = a.axis_of[0];
   p.axis_of[1] = a.axis_of[1];

@@ -34,7 +34,7 @@ CHUNK = dict(q=FAKE, k=FAKE, v=FAKE, table=FAKE, cu=FAKE, lens=FAKE, o=FAKE, lse
     ({"B": 0}, 1), ({"Hq": 7}, 1), ({"Hkv": 0}, 1), ({"T": -1}, 1), ({"pages": 0}, 1), ({"page": 0}, 1), ({"most": 0}, 1),
     ({"layout": 2}, 1), ({"causal": 2}, 1), ({"scale": 0.0}, 1), ({"scale": float("nan")}, 1), ({"scale": float("inf")}, 1),
     ({"D": 96}, 2), ({"page": 24}, 2), ({"page": 4}, 2), ({"page": 65}, 2), ({"pages": HUGE}, 2), ({"most": HUGE}, 2),
-    ({"T": HUGE}, 2), ({"q": FAKE + 8}, 3), ({"v": FAKE + 2}, 3), ({"o": FAKE + 4}, 3), ({"lse": FAKE + 2}, 3),
+    ({"T": HUGE}, 2), ({"T": 1, "Hq": 1 << 17}, 2), ({"q": FAKE + 8}, 3), ({"v": FAKE + 2}, 3), ({"o": FAKE + 4}, 3), ({"lse": FAKE + 2}, 3),
     ({"table": FAKE + 1}, 3), ({"cu": FAKE + 2}, 3), ({"lens": FAKE + 2}, 3), ({"ws": None}, 4), ({"wsb": 100}, 4),
     ({"ws": FAKE + 8}, 3)])
 def test_chunk_rejects(lib, change, expect):

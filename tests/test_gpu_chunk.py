@@ -154,6 +154,44 @@ def test_a_sequence_reaches_no_other(loom):
     assert torch.equal(got[:70], clean[:70]) and torch.equal(got[140:], clean[140:]) and torch.isnan(got[70:140]).all()
 
 
+def test_caches_past_32_bits(loom):
+    """Pages whose values lie past 2^32 elements from the cache's beginning."""
+    import torch
+    page, Hkv, D = 64, 8, 128
+    num = (1 << 32) // (page * Hkv * D) + 40
+    c = Case([40, 1], [300, 2000], 16, Hkv, D, page)
+    d = list(c.device())
+    for i in (1, 2):
+        big = torch.empty((num, page, Hkv, D), dtype=torch.bfloat16, device="cuda")
+        big[-d[i].shape[0]:] = d[i]
+        d[i] = big
+    d[3] = torch.where(d[3] < c.k.shape[0], d[3] + num - c.k.shape[0], d[3])
+    o, lse = loom.loom_attn_chunk_paged(*d, return_lse=True)
+    _check(o, lse, c.exact(True))
+
+
+def test_as_many_keys_as_there_may_be(loom):
+    """2^31 - 64 keys, all of them one page's: its attention, and LSE that much larger.
+
+    A CTA of at least 120 adds up to 2^31 / 128 / 120 = 139811 tiles: l in one addition each, off by half a step, o in
+    eight, off by a step at most."""
+    import torch
+    most = (1 << 31) // 64 - 1
+    c = Case([1], [64], 4, 1, 64, 64)
+    d = list(c.device())
+    d[3] = torch.full((1, most), int(c.table[0, 0]), dtype=torch.int32, device="cuda")
+    d[5] = torch.full((1,), most * 64, dtype=torch.int32, device="cuda")
+    o, lse = loom.loom_attn_chunk_paged(*d, return_lse=True)
+    loom.loom_attn_check_error()
+    eo, bo, el, bl = c.exact(True)
+    rows = c.table[0, :1].tolist()
+    p = torch.exp(torch.einsum("thd,kd->thk", c.q.double(), ref.gathered(c.k, rows, 64, "nhd")[:, 0]) / 8 - el.T[..., None])
+    sizes = torch.einsum("thk,kd->thd", p, ref.gathered(c.v, rows, 64, "nhd")[:, 0].abs())
+    tiles = 139811
+    assert ((o.double().cpu() - eo).abs() <= bo + tiles * (8 * 2.0 ** -23 + 2.0 ** -24) * (sizes + eo.abs())).all()
+    assert ((lse.double().cpu() - el - math.log(most)).abs() <= 2 * bl + tiles * 2.0 ** -24 * 1.1).all()
+
+
 SPLIT = [([1, 1, 1], [9000, 5000, 70], 32, 8, 128), ([300], [4000], 16, 2, 64), ([3, 400, 1], [3000, 400, 2000], 28, 4, 128)]
 
 
