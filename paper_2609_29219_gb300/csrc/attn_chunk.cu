@@ -26,9 +26,9 @@
 //
 // What bounds it: many queries, the tensor cores, as the prefill kernel, whose step this one repeats
 // (two query tiles alternate on the tensor pipe, P in TMEM); few queries, the cache's bandwidth; small calls,
-// latencies.  GB300, H32/8 D 128: 2048 tokens after 30000 in 650 to 662 us, 1573 to 1600 TFLOP/s; 16 single
+// latencies.  GB300, H32/8 D 128: 2048 tokens after 30000 in 650 to 666 us, 1563 to 1600 TFLOP/s; 16 single
 // tokens of 4K to 8K keys in 75 us, 5.35 TB/s; 31 of 100 to 12K and 481 tokens of a prompt in 140 us,
-// 5.6 TB/s; one of 500 keys in 11.2 us.  Two tiles' alternation and 128 keys a tile: a step of both
+// 5.6 TB/s; one of 500 keys in 10.8 us.  Two tiles' alternation and 128 keys a tile: a step of both
 // takes 2900 clocks for 2048 of the tensor pipe, and TMEM has room for no third S and O.
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -58,9 +58,11 @@ constexpr int kSnap = 1024;
 template <int D>
 struct ChunkCfg {
   static constexpr int BM = 128, BN = 128;
-  static constexpr int NR = D == 128 ? 2 : 5;       // slots of the K ring, and of the V ring
+  static constexpr int NR = D == 128 ? 2 : 4;       // slots of the K ring, and of the V ring
   static constexpr int THREADS = 384;               // 8 softmax warps, K loader, MMA, V loader, scheduler
-  static constexpr int NREC = 4;                    // units that the scheduler is ahead
+  // Units that the scheduler is ahead: at D = 128 what shared memory has room for.  (D = 64, 128 tokens after 10 to 500:
+  // 4 and five slots a ring 44.7 us, 8 and four 41.4; longer units the same.)
+  static constexpr int NREC = D == 128 ? 4 : 8;
   static constexpr int NBOX = D / 64;               // 128-byte swizzled boxes per row of a tile
   static constexpr uint32_t BOX_BYTES = BM * 128;
   static constexpr uint32_t TILE_BYTES = NBOX * BOX_BYTES;
@@ -836,7 +838,7 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
     }
   } else if (warp == 8 || warp == 10) {
     // ------------------------------------------------------------------ loaders (whole warps): Q and K, and V
-    // Lane 0 waits and expects; a tile's pieces of min(page, 64) keys are looked up and copied by one lane each.
+    // Lane 0 waits and expects; a tile's pieces of min(page, 64) keys are copied by one lane each.
     const bool is_v = warp == 10;
     const CUtensorMap* map = is_v ? &tm_v : &tm_k;
     if (lane == 0) {
@@ -869,12 +871,15 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
       const int32_t* table = p.table + static_cast<size_t>(rec->b) * p.max_pages;
       give_item();
       if (lo == end) continue;  // no keys: nothing to load
-      // the page of this lane's piece of key tile j (none past the sequence's keys)
-      const auto page_of = [&](int j) {
-        if (lane * rows >= C::BN || j * C::BN + lane * rows >= skv) return -1;
-        return table[static_cast<unsigned>(j * C::BN + lane * rows) / static_cast<unsigned>(p.page)];
+      // the pages of the 32 pieces from key tile j on, this lane's (none past the sequence's keys)
+      const auto pages_from = [&](int j) {
+        const unsigned key = static_cast<unsigned>(j) * C::BN + lane * rows;
+        if (key >= static_cast<unsigned>(skv)) return -1;
+        return table[p.page > 64 ? key / static_cast<unsigned>(p.page) : key >> rows_lg];
       };
-      int page = page_of(lo);
+      // (32 pieces are `ahead` tiles; the next ones are looked up while these are loaded)
+      const int ahead = 1 << (rows_lg - 2);
+      int window = pages_from(lo), next_window = -1;
       if (!is_v && n0 > 0 && !(ok = load_q(two ? 0 : q_single, plane, token))) break;
       q_single ^= !two;
       const int hk = plane / p.planes_per_kv;
@@ -887,13 +892,18 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
           skipped = pos;
           continue;
         }
+        if (((j - lo) & (ahead - 1)) == 0) {
+          if (j > lo) window = next_window;
+          next_window = j + ahead < end ? pages_from(j + ahead) : -1;
+        }
+        const int page = __shfl_sync(0xffffffffu, window, ((j - lo) << (7 - rows_lg)) + lane);  // (of a width of 32)
         const int pieces = (min(C::BN, skv - j * C::BN) + rows - 1) >> rows_lg;
         if (lane == 0) mbar_expect_tx(full + 8 * slot, static_cast<uint32_t>(C::NBOX * pieces * rows * 128));
         __syncwarp();
         if (lane < pieces) {
           // NHD view [keys of all pages, Hkv, D]: (dim, kv head, key); HND view [pages x Hkv, page, D]:
           // (dim, row in page, page x Hkv + kv head).  A page that there is not: past the end, which reads as zeros.
-          const int in = static_cast<int>(static_cast<unsigned>(j * C::BN + lane * rows) % static_cast<unsigned>(p.page));
+          const int in = p.page > 64 ? static_cast<int>(static_cast<unsigned>(j * C::BN + lane * rows) % static_cast<unsigned>(p.page)) : 0;
           const bool bad = page < 0 || page >= p.num_pages;
           const int y = p.hnd ? in : hk;
           const int z = p.hnd ? (bad ? p.num_pages * p.Hkv : page * p.Hkv + hk) : (bad ? p.num_pages * p.page : page * p.page + in);
@@ -902,7 +912,6 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
             tma_load_3d(ring + slot * C::TILE_BYTES + x * C::BOX_BYTES + lane * rows * 128, map, x * 64, y, z, full + 8 * slot);
         }
         if (j == lo && !is_v && two && !(ok = load_q(1, plane, token + p.tq))) break;
-        if (j + 1 < end) page = page_of(j + 1);
       }
     }
     // drain copies still in flight before the CTA may exit
