@@ -1063,11 +1063,11 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
           // could be two phases behind, which a wait by parity takes for done)
           alive = wait_warp(my_s, (cnt + i) & 1, p.ctl, ab) && wait_warp(bar_full + 8 * (C::NR + slot), (vn / C::NR) & 1, p.ctl, ab);
           if (!alive) break;
-          const uint32_t v = sbase + C::RING_OFF + (C::NR + slot) * C::TILE_BYTES;
-          const int chunks = (C::BN - over) * 8;
-#pragma unroll 1
-          for (int x = row_in_tile; x < C::NBOX * chunks; x += C::BM)
-            st_shared_v4(v + x / chunks * C::BOX_BYTES + over * 128 + x % chunks * 16, 0, 0, 0, 0);
+          // (a thread clears its row, from a chunk of its own on: no two lanes of eight meet in a bank)
+          const uint32_t v = sbase + C::RING_OFF + (C::NR + slot) * C::TILE_BYTES + row_in_tile * 128;
+          if (row_in_tile >= over)
+#pragma unroll
+            for (int x = 0; x < C::NBOX * 8; ++x) st_shared_v4(v + x / 8 * C::BOX_BYTES + (((x + lane) & 7) << 4), 0, 0, 0, 0);
           fence_proxy_async_smem();
         }
         if (any) {
