@@ -493,49 +493,57 @@ __device__ __forceinline__ void release_o(const RowSums& r, uint32_t bar_oe, uin
   if (r.both) mbar_arrive(bar_oe1);
 }
 
-// Joins the pieces of a warp's rows, N of them and U chunks of 16 bytes of a row at a time, all of whose loads are
-// on their way together: a round takes an access' latency, whatever it loads.
-template <int D, int U, int N>
+// Joins the pieces of a warp's rows, 1 << lg of which lie side by side in the lanes, each lane with U chunks of 16
+// bytes of a row at a time, of two pieces, whose loads are on their way together.  (What runs once a unit is fetched
+// anew each time, at 100 clocks for eight instructions, so that code weighs more than rounds.)
+template <int D>
 __device__ __forceinline__ void join_pieces(const ChunkParams& p, uint32_t list, int pieces, const float2* ml, const float4* part,
                                             int rows, int lg, const RowSums& r, long long unit_at) {
-  const int lane = threadIdx.x & 31, my = lane & ((1 << lg) - 1), parts = 32 >> lg;
-  const bool mine = my < rows;
+  constexpr int U = 8;
+  const int lane = threadIdx.x & 31, my = min(lane & ((1 << lg) - 1), rows - 1), parts = 32 >> lg;
   const size_t ml_slot = static_cast<size_t>(p.groups) * 32, part_slot = ml_slot * (D / 4);
+  ml += my;
+  part += my + (lane >> lg) * 32;
+  float M = -INFINITY, l = 0.f;
+#pragma unroll 1
+  for (int k0 = 0; k0 < pieces; k0 += 4) {
+    float2 x[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = __ldcg(ml + ld_shared_i32(list + 4 * min(k0 + k, pieces - 1)) * ml_slot);
+    float M_new = M;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) M_new = fmaxf(M_new, x[k].x);
+    const float base = M_new == -INFINITY ? 0.f : M_new;
+    l *= ex2(M - base);
+    M = M_new;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (k0 + k < pieces && x[k].y >= 0.f) l = fmaf(ex2(x[k].x - base), x[k].y, l);
+  }
+  const float base = M == -INFINITY ? 0.f : M, inv = l == 0.f ? 0.f : 1.f / l;
   const int at = __shfl_sync(0xffffffffu, r.at, my);
-  __nv_bfloat16* o = p.o + unit_at + static_cast<long long>(at) * 8;
+  __nv_bfloat16* o = p.o + unit_at + static_cast<long long>(at) * 8 + (lane >> lg) * 4;
 #pragma unroll 1
   for (int block = 0; block < D / 4; block += U * parts) {  // (of all lanes alike)
-    const int c0 = block + (lane >> lg);
-    float acc[4 * U], M = -INFINITY, l = 0.f;
+    float acc[4 * U];
 #pragma unroll
     for (int i = 0; i < 4 * U; ++i) acc[i] = 0.f;
 #pragma unroll 1
-    for (int k0 = 0; k0 < pieces; k0 += N) {
-      float2 x[N];
-      float4 v[N][U];
+    for (int k0 = 0; k0 < pieces; k0 += 2) {
+      float2 x[2];
+      float4 v[2][U];
 #pragma unroll
-      for (int k = 0; k < N; ++k) {
-        const bool there = mine && k0 + k < pieces;
-        const size_t slot = there ? ld_shared_i32(list + 4 * (k0 + k)) : 0;
-        x[k] = there ? __ldcg(ml + slot * ml_slot + my) : make_float2(-INFINITY, -1.f);
-        const float4* from = part + slot * part_slot + my;
+      for (int k = 0; k < 2; ++k) {
+        const size_t slot = ld_shared_i32(list + 4 * min(k0 + k, pieces - 1));
+        x[k] = __ldcg(ml + slot * ml_slot);
+        const float4* from = part + slot * part_slot + block * 32;
 #pragma unroll
-        for (int i = 0; i < U; ++i)
-          v[k][i] = there && c0 + i * parts < D / 4 ? __ldcg(from + (c0 + i * parts) * 32) : make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int i = 0; i < U; ++i) v[k][i] = __ldcg(from + i * parts * 32);
       }
-      float M_new = M;
 #pragma unroll
-      for (int k = 0; k < N; ++k) M_new = fmaxf(M_new, x[k].x);
-      const float base = M_new == -INFINITY ? 0.f : M_new, alpha = ex2(M - base);
-      l *= alpha;
-#pragma unroll
-      for (int i = 0; i < 4 * U; ++i) acc[i] *= alpha;
-      M = M_new;
-#pragma unroll
-      for (int k = 0; k < N; ++k) {
-        if (x[k].y < 0.f) continue;  // (no keys of the row's tile: nothing was written there)
-        const float w = ex2(x[k].x - base);
-        l = fmaf(w, x[k].y, l);
+      for (int k = 0; k < 2; ++k) {
+        if (k0 + k >= pieces || x[k].y < 0.f) continue;  // (no keys of the row's tile: nothing was written there)
+        const float w = ex2(x[k].x - base) * inv;
 #pragma unroll
         for (int i = 0; i < U; ++i) {
           acc[4 * i] = fmaf(w, v[k][i].x, acc[4 * i]);
@@ -545,16 +553,14 @@ __device__ __forceinline__ void join_pieces(const ChunkParams& p, uint32_t list,
         }
       }
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    if (mine)
+    if ((lane & ((1 << lg) - 1)) < rows)
 #pragma unroll
       for (int i = 0; i < U; ++i)
-        if (c0 + i * parts < D / 4)
-          *reinterpret_cast<uint2*>(o + (c0 + i * parts) * 4) =
-              make_uint2(pack_bf16x2(acc[4 * i] * inv, acc[4 * i + 1] * inv), pack_bf16x2(acc[4 * i + 2] * inv, acc[4 * i + 3] * inv));
-    // (every lane below `rows` has its own row)
-    if (block == 0 && r.lse_at) *r.lse_at = row_lse(M, l);
+        *reinterpret_cast<uint2*>(o + (block + i * parts) * 4) =
+            make_uint2(pack_bf16x2(acc[4 * i], acc[4 * i + 1]), pack_bf16x2(acc[4 * i + 2], acc[4 * i + 3]));
   }
+  // (every lane below `rows` has its own row)
+  if (r.lse_at) *r.lse_at = row_lse(M, l);
 }
 
 // Counts one of the pieces of this warp's rows of a cut unit; true for the last to come.
@@ -639,10 +645,11 @@ __device__ __noinline__ void finish_piece(const ChunkParams& p, const Line& ln, 
   // The warp's rows (its first lanes') are spread over all lanes: 1 << lg of them side by side, each lane with
   // every (32 >> lg)-th 16 bytes of its row.
   const int rows = __popc(__ballot_sync(0xffffffffu, row));
-  const int lg = rows > 1 ? 32 - __clz(rows - 1) : 0;
+  // (at least 8, or 16 at D = 64: a row's chunks are as many as its lanes take at a time)
+  const int lg = max(D == 128 ? 3 : 4, 32 - __clz(rows - 1));
   const float2* ml = p.part_ml + group * 32;
   const float4* part = reinterpret_cast<const float4*>(p.part) + static_cast<size_t>(group) * (D / 4) * 32;
-  join_pieces<D, 8, 3>(p, stg, it.pieces, ml, part, rows, lg, r, unit_at);
+  join_pieces<D>(p, stg, it.pieces, ml, part, rows, lg, r, unit_at);
   __syncwarp();  // the list has been read
 }
 
