@@ -518,7 +518,7 @@ __device__ __forceinline__ void join_pieces(const ChunkParams& p, uint32_t list,
     M = M_new;
 #pragma unroll
     for (int k = 0; k < 4; ++k)
-      if (k0 + k < pieces && x[k].y >= 0.f) l = fmaf(ex2(x[k].x - base), x[k].y, l);
+      if (k0 + k < pieces && !(x[k].y < 0.f)) l = fmaf(ex2(x[k].x - base), x[k].y, l);
   }
   const float base = M == -INFINITY ? 0.f : M, inv = l == 0.f ? 0.f : 1.f / l;
   const int at = __shfl_sync(0xffffffffu, r.at, my);

@@ -192,6 +192,17 @@ def test_as_many_keys_as_there_may_be(loom):
     assert ((lse.double().cpu() - el - math.log(most)).abs() <= 2 * bl + tiles * 2.0 ** -24 * 1.1).all()
 
 
+def test_a_key_that_is_nan_in_a_sequence_of_many_pieces(loom):
+    """It is in one of the pieces that are joined, and in the row's LSE as in its output."""
+    import torch
+    c = Case([1, 1], [40000, 40000], 4, 1, 128)
+    d = list(c.device())
+    d[1][c.table[0, 1200].long().cuda(), 5] = math.nan
+    o, lse = loom.loom_attn_chunk_paged(*d, return_lse=True)
+    assert torch.isnan(o[0]).all() and torch.isnan(lse[:, 0]).all()
+    assert torch.isfinite(o[1]).all() and torch.isfinite(lse[:, 1]).all()
+
+
 SPLIT = [([1, 1, 1], [9000, 5000, 70], 32, 8, 128), ([300], [4000], 16, 2, 64), ([3, 400, 1], [3000, 400, 2000], 28, 4, 128)]
 
 
