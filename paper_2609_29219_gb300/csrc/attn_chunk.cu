@@ -26,9 +26,9 @@
 //
 // What bounds it: many queries, the tensor cores, as the prefill kernel, whose step this one repeats
 // (two query tiles alternate on the tensor pipe, P in TMEM); few queries, the cache's bandwidth; small calls,
-// latencies.  GB300, H32/8 D 128: 2048 tokens after 30000 in 650 to 666 us, 1563 to 1600 TFLOP/s; 16 single
-// tokens of 4K to 8K keys in 75 us, 5.35 TB/s; 31 of 100 to 12K and 481 tokens of a prompt in 140 us,
-// 5.6 TB/s; one of 500 keys in 10.8 us.  Two tiles' alternation and 128 keys a tile: a step of both
+// latencies.  GB300, H32/8 D 128: 2048 tokens after 30000 in 641 to 656 us, 1590 to 1625 TFLOP/s; 16 single
+// tokens of 4K to 8K keys in 73.5 us, 5.5 TB/s; 31 of 100 to 12K and 481 tokens of a prompt in 137 us,
+// 5.75 TB/s; one of 500 keys in 10.3 us.  Two tiles' alternation and 128 keys a tile: a step of both
 // takes 2900 clocks for 2048 of the tensor pipe, and TMEM has room for no third S and O.
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -47,7 +47,9 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kRescaleThreshold = 8.0f;  // base-2 units; P <= 2^8 between rescales
 
 // The line's units: a key of a pair of tiles costs 1 << kKeyLg2, of a single tile 1 << kKeyLg1; a unit kUnitCost more.
-constexpr int kKeyLg2 = 3, kKeyLg1 = 2, kUnitCost = 3000;
+// (1400, 2000, 3000 and 4200: 8192 tokens alone 357, 358, 361 and 365 us, 16 tokens of 4K to 8K keys 73.7, 73.8, 74.7 and
+// 76.5; 800: 8192 tokens 384.)
+constexpr int kKeyLg2 = 3, kKeyLg1 = 2, kUnitCost = 2000;
 // The least that a CTA is given of units that are longer: they are not cut into shorter pieces.
 constexpr int kLeastStretch = 3000;
 // A cut that would leave less than this of a unit's tiles on one side falls on its end: joining a piece costs more
