@@ -27,8 +27,8 @@
 // What bounds it: many queries, the tensor cores, as the prefill kernel, whose step this one repeats
 // (two query tiles alternate on the tensor pipe, P in TMEM); few queries, the cache's bandwidth; small calls,
 // latencies.  GB300, H32/8 D 128: 2048 tokens after 30000 in 641 to 656 us, 1590 to 1625 TFLOP/s; 16 single
-// tokens of 4K to 8K keys in 73.5 us, 5.5 TB/s; 31 of 100 to 12K and 481 tokens of a prompt in 137 us,
-// 5.75 TB/s; one of 500 keys in 10.3 us.  Two tiles' alternation and 128 keys a tile: a step of both
+// tokens of 4K to 8K keys in 73.7 us, 5.5 TB/s; 31 of 100 to 12K and 481 tokens of a prompt in 138 us,
+// 5.7 TB/s; one of 500 keys in 10.3 us.  Two tiles' alternation and 128 keys a tile: a step of both
 // takes 2900 clocks for 2048 of the tensor pipe, and TMEM has room for no third S and O.
 #include <cuda.h>
 #include <cuda_bf16.h>
