@@ -53,10 +53,14 @@ __device__ __forceinline__ Sums scan(long long a, long long b, long long (*part)
           __shfl_sync(0xffffffffu, q, 31)};
 }
 
-// (in 32 bits: rows and page - 1 are below 2^31; the 64-bit division took most of the kernel's instructions)
-__device__ __forceinline__ int pages_of(int rows, int page) {
-  return static_cast<int>((static_cast<unsigned>(rows) + static_cast<unsigned>(page) - 1u) / static_cast<unsigned>(page));
-}
+// Rows in pages, in 32 bits (rows and page - 1 are below 2^31), by a shift where it does: divisions of 64 bits took
+// most of the kernel's instructions, and of 32 a third (4096 requests with 130000 tokens 18.6 us, so 17.0).
+struct Pages {
+  unsigned page;
+  int lg;  // of a power of two; else -1
+  __device__ __forceinline__ int whole(unsigned rows) const { return static_cast<int>(lg >= 0 ? rows >> lg : rows / page); }
+  __device__ __forceinline__ int of(int rows) const { return whole(static_cast<unsigned>(rows) + page - 1u); }
+};
 
 // The largest b with at[b] <= x, of n + 1 values that never decrease, at[0] <= x < at[n].
 __device__ __forceinline__ int holder(const int* at, int n, int x) {
@@ -77,6 +81,7 @@ __global__ void __launch_bounds__(kThreads) paged_plan_kernel(const PlanArgs p) 
   extern __shared__ int plan_smem[];
   __shared__ long long part[32][2];
   const int B = p.B;
+  const Pages pages{static_cast<unsigned>(p.page), (p.page & (p.page - 1)) ? -1 : 31 - __clz(p.page)};
   int* cu = plan_smem;        // [B + 1] first token, p.T at most
   int* off = cu + B + 1;      // [B + 1] pages that the requests before ask for (one more than there are, at most)
   int* rel = off + B + 1;     // [B + 1] pages that the requests before give back, as many as there are at most
@@ -101,7 +106,7 @@ __global__ void __launch_bounds__(kThreads) paged_plan_kernel(const PlanArgs p) 
   long long n_sum = 0, rel_sum = 0;
   for (int b = b0; b < b1; ++b) {
     n_sum += max(cu[b], 0);
-    rel_sum += cu[b] < 0 ? pages_of(len[b], p.page) : 0;
+    rel_sum += cu[b] < 0 ? pages.of(len[b]) : 0;
   }
   const Sums s = scan(n_sum, rel_sum, part);
   const long long given = s.all_b;
@@ -112,12 +117,12 @@ __global__ void __launch_bounds__(kThreads) paged_plan_kernel(const PlanArgs p) 
     const long long begin = end;
     end += max(n, 0);
     const bool fits = n >= 0 && l + static_cast<long long>(n) <= rows && end <= p.T;
-    const int need = fits && n > 0 ? pages_of(l + n, p.page) - pages_of(l, p.page) : 0;
+    const int need = fits && n > 0 ? pages.of(l + n) - pages.of(l) : 0;
     off[b] = need;
     need_sum += need;
     cu[b] = static_cast<int>(min(begin, static_cast<long long>(p.T)));
     rel[b] = static_cast<int>(min(back, static_cast<long long>(p.num_pages)));
-    if (n < 0) back += pages_of(l, p.page);
+    if (n < 0) back += pages.of(l);
     state[b] = n < 0 ? kOver : fits ? kGranted : 0;
   }
   const Sums t = scan(need_sum, 0, part);
@@ -163,7 +168,7 @@ __global__ void __launch_bounds__(kThreads) paged_plan_kernel(const PlanArgs p) 
   }
   for (int k = first; k < taken; k += step) {
     const int b = holder(off, B, k);
-    p.block_table[static_cast<size_t>(b) * p.max_pages + pages_of(len[b], p.page) + (k - off[b])] = fresh_page(k);
+    p.block_table[static_cast<size_t>(b) * p.max_pages + pages.of(len[b]) + (k - off[b])] = fresh_page(k);
   }
   for (int i = listed + first; i < total - taken; i += step) p.free_pages[i] = listed_page(i);
   // A warp takes as many tokens in a row as it has to, looks for its first and last one's request among all, and
@@ -184,7 +189,7 @@ __global__ void __launch_bounds__(kThreads) paged_plan_kernel(const PlanArgs p) 
       const int b = low + holder(cu + low, high + 1 - low, static_cast<int>(t));
       if (is_granted(b)) {
         pos = len[b] + (static_cast<int>(t) - cu[b]);
-        const int j = static_cast<int>(static_cast<unsigned>(pos) / static_cast<unsigned>(p.page)), held = pages_of(len[b], p.page);
+        const int j = pages.whole(static_cast<unsigned>(pos)), held = pages.of(len[b]);
         const int at = j < held ? p.block_table[static_cast<size_t>(b) * p.max_pages + j] : fresh_page(off[b] + j - held);
         if (at >= 0 && at < p.num_pages) slot = at * p.page + (pos - j * p.page);
       }
