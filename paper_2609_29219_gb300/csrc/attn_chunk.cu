@@ -912,7 +912,8 @@ __global__ void __launch_bounds__(ChunkCfg<D>::THREADS, 1)
         if (lane < pieces) {
           // NHD view [keys of all pages, Hkv, D]: (dim, kv head, key); HND view [pages x Hkv, page, D]:
           // (dim, row in page, page x Hkv + kv head).  A page that there is not: past the end, which reads as zeros.
-          const int in = p.page > 64 ? static_cast<int>(static_cast<unsigned>(j * C::BN + lane * rows) % static_cast<unsigned>(p.page)) : 0;
+          const unsigned key = static_cast<unsigned>(j * C::BN + lane * rows);
+          const int in = p.page > 64 ? static_cast<int>(key % static_cast<unsigned>(p.page)) : 0;
           const bool bad = page < 0 || page >= p.num_pages;
           const int y = p.hnd ? in : hk;
           const int z = p.hnd ? (bad ? p.num_pages * p.Hkv : page * p.Hkv + hk) : (bad ? p.num_pages * p.page : page * p.page + in);
