@@ -195,10 +195,45 @@ struct Item {
 };
 static_assert(sizeof(Item) == 80, "fits its record");
 
-// The CTA's next piece, and the walk behind it; false past the stretch's end.
+// The first sequence from b on that brings tokens (B: none does), found by a whole warp, 256 sequences at a time.
+// (GB300, one token of 500 keys as the first of 4096 sequences: 309 us where idle ones were walked one at a time, and ahead of
+// the unit that was at hand; 24.9 so, of which 14 are the prefix sum over them all; a million idle ones outlasted the other roles'
+// waits.)
+__device__ __noinline__ int next_sequence(const ChunkParams& p, int b) {
+  const unsigned B = static_cast<unsigned>(p.B), lane = threadIdx.x & 31;
+#pragma unroll 1
+  for (unsigned from = static_cast<unsigned>(b); from < B; from += 256) {  // (of all lanes alike)
+    unsigned found = B;
+#pragma unroll
+    for (int i = 7; i >= 0; --i) {
+      const unsigned r = from + 32 * i + lane;
+      if (r < B && min(max(p.cu_q[r + 1], 0), p.total_q) > min(max(p.cu_q[r], 0), p.total_q)) found = r;  // (as load_seq has it)
+    }
+    found = __reduce_min_sync(0xffffffffu, found);
+    if (found < B) return static_cast<int>(found);
+  }
+  return p.B;
+}
+
+// The CTA's next piece, and the walk to it; false past the stretch's end.  (All lanes of a warp alike.)
 __device__ __forceinline__ bool next_item(const ChunkParams& p, const Line& ln, Walk& w, Item& it) {
 #pragma unroll 1
   while (w.b < p.B && w.at < ln.x1) {
+    // (past a sequence's end only here: the last unit of a stretch waits for no other sequence)
+    if (w.pair == w.s.pairs) {
+      w.pair = 0;
+      if (++w.plane == p.planes) {
+        w.plane = 0;
+        ++w.b;
+#pragma unroll 1
+        while (w.b < p.B) {
+          w.s = load_seq(p, w.b);
+          if (w.s.pairs) break;
+          w.b = next_sequence(p, w.b + 1);
+        }
+        if (w.b >= p.B) break;
+      }
+    }
     const long long step = 2ll * p.tq;
     it.b = w.b;
     it.plane = w.plane;
@@ -218,17 +253,7 @@ __device__ __forceinline__ bool next_item(const ChunkParams& p, const Line& ln, 
     it.n0 = it.two ? max(0, min(hi, key_tiles(keys_until(p, w.s, it.t0 + p.tq))) - it.lo) : (it.n + 1) / 2;
     it.n1 = it.two ? it.n : it.n / 2;
     w.at += it.cost;
-    if (++w.pair == w.s.pairs) {
-      w.pair = 0;
-      if (++w.plane == p.planes) {
-        w.plane = 0;
-#pragma unroll 1
-        while (++w.b < p.B) {
-          w.s = load_seq(p, w.b);
-          if (w.s.pairs) break;
-        }
-      }
-    }
+    ++w.pair;
     // (a unit without keys belongs to the CTA in whose stretch it begins)
     if (it.n > 0 || (it.tiles == 0 && ln.x0 <= it.at)) return true;
   }
