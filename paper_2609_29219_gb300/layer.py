@@ -47,15 +47,16 @@ class PagedCache:
 
 
 class RequestCache:
-    """K and V pages [num_pages, page, Hkv, D] shared by up to `requests` requests of `capacity` tokens, which
-    take pages as they grow and give them back when they end.  All of it is on the device: a step that
-    was captured can be replayed."""
+    """K and V pages [num_pages, page, Hkv, D] shared by up to `requests` requests of `capacity` tokens (whole
+    pages), which take pages as they grow and give them back when they end.  All of it is on the device: a step
+    that was captured can be replayed."""
 
     def __init__(self, requests, num_pages, capacity, Hkv, D, page=16, device="cuda"):
         i32 = dict(dtype=torch.int32, device=device)
-        self.page = page
+        self.page, per = page, -(-capacity // page)
+        self.capacity = per * page
         self.k, self.v = (torch.zeros((num_pages, page, Hkv, D), dtype=torch.bfloat16, device=device) for _ in range(2))
-        self.table = torch.full((requests, -(-capacity // page)), -1, **i32)
+        self.table = torch.full((requests, per), -1, **i32)
         self.lens = torch.zeros(requests, **i32)
         self.free_pages, self.free_count = torch.arange(num_pages, **i32), torch.full((1,), num_pages, **i32)
 
@@ -105,6 +106,8 @@ class AttentionLayer:
         """The new tokens of a RequestCache's requests, packed, x [T, model]: prompts, chunks of them, single tokens.
         Rows past the last request's (and those of requests that the cache had no room for) mean nothing.  The
         rotation tables must reach the cache's capacity."""
+        if cache.capacity > self.cos.shape[0]:
+            raise ValueError(f"the rotation tables have {self.cos.shape[0]} positions, the cache's requests up to {cache.capacity} tokens")
         cu, positions, slots, _ = cache.plan(new_lens, x.shape[0])
         qkv = loom.loom_gemm_bf16(x, self.w_qkv, b_transposed=True)
         q = loom.loom_qkv_norm_rope_cache(qkv, self.q_norm, self.k_norm, self.cos, self.sin, positions, slots, cache.k, cache.v, self.Hq)
