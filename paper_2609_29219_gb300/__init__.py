@@ -678,9 +678,9 @@ def loom_paged_plan(new_lens, lens, block_table, free_pages, free_count, num_tok
     [num_tokens] and ``granted`` [B] (allocated if None); the free pages that are left go to
     ``free_count_out`` (None: to free_count)."""
     _torch()
-    if _fast is not None and cu_seqlens is None and positions is None and slots is None and granted is None and stream is None:
+    if _fast is not None and cu_seqlens is None and positions is None and slots is None and stream is None:
         r = _fast.plan(new_lens, lens, block_table, free_pages, free_count, free_count if free_count_out is None else free_count_out,
-                       seqlens_k, num_tokens, page_size)
+                       seqlens_k, granted, num_tokens, page_size)
         if r is not None:
             return _fast_result(r, "loom_paged_plan")
     np_ = _ptr(new_lens, "new_lens", _i32, 1)

@@ -403,34 +403,37 @@ PyObject* chunk(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return with_lse ? PyTuple_Pack(2, o.p, lse.p) : PyTuple_Pack(1, o.p);
 }
 
-// plan(new_lens, lens, block_table, free_pages, free_count, free_count_out, seqlens_k or None, num_tokens, page_size):
-// (cu_seqlens, seqlens_k, positions, slots, granted)
+// plan(new_lens, lens, block_table, free_pages, free_count, free_count_out, seqlens_k or None, granted or None, num_tokens,
+// page_size): (cu_seqlens, seqlens_k, positions, slots, granted)
 PyObject* plan(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  Tensor news, lens, table, list, count, out, seqlens;
+  Tensor news, lens, table, list, count, out, seqlens, grants;
   long long T, page;
-  if (n != 9 || !view(a[0], kI32, &news) || news.dims != 1 || !view(a[1], kI32, &lens) || !same(lens, news) ||
+  if (n != 10 || !view(a[0], kI32, &news) || news.dims != 1 || !view(a[1], kI32, &lens) || !same(lens, news) ||
       !view(a[2], kI32, &table) || table.dims != 2 || table.size[0] != news.size[0] || !view(a[3], kI32, &list) || list.dims != 1 ||
       !view(a[4], kI32, &count) || count.dims != 1 || count.size[0] != 1 || !view(a[5], kI32, &out) || !same(out, count) ||
-      (a[6] != Py_None && (!view(a[6], kI32, &seqlens) || !same(seqlens, news))) || !as_int(a[7], &T) || !as_int(a[8], &page) ||
+      (a[6] != Py_None && (!view(a[6], kI32, &seqlens) || !same(seqlens, news))) ||
+      (a[7] != Py_None && (!view(a[7], kI32, &grants) || !same(grants, news))) || !as_int(a[8], &T) || !as_int(a[9], &page) ||
       !small(table) || !small(list))
     Py_RETURN_NONE;
   const long long dev = device_of(news), B = news.size[0], B1 = B + 1;
-  if (dev < 0 || !together(news, {&lens, &table, &list, &count, &out, &seqlens})) Py_RETURN_NONE;
-  void *cp, *sp = seqlens.ptr, *pp, *lp, *gp;
-  Ref cu(make(dev, 1, &B1, kI32, &cp)), lengths;
+  if (dev < 0 || !together(news, {&lens, &table, &list, &count, &out, &seqlens, &grants})) Py_RETURN_NONE;
+  // an output of one number a request: the one given, or a new one
+  const auto given_or_new = [&](const Tensor& given, void** ptr) {
+    if (!given.t) return make(dev, 1, &B, kI32, ptr);
+    Py_INCREF(given.obj);
+    *ptr = given.ptr;
+    return given.obj;
+  };
+  void *cp, *sp, *pp, *lp, *gp;
+  Ref cu(make(dev, 1, &B1, kI32, &cp));
   if (!cu.p) return nullptr;
-  if (a[6] == Py_None) {
-    lengths.p = make(dev, 1, &B, kI32, &sp);
-    if (!lengths.p) return nullptr;
-  } else {
-    Py_INCREF(a[6]);
-    lengths.p = a[6];
-  }
+  Ref lengths(given_or_new(seqlens, &sp));
+  if (!lengths.p) return nullptr;
   Ref positions(make(dev, 1, &T, kI32, &pp));
   if (!positions.p) return nullptr;
   Ref slots(make(dev, 1, &T, kI32, &lp));
   if (!slots.p) return nullptr;
-  Ref granted(make(dev, 1, &B, kI32, &gp));
+  Ref granted(given_or_new(grants, &gp));
   if (!granted.p) return nullptr;
   const auto i32 = [](void* x) { return static_cast<int32_t*>(x); };
   const loom_status st = F.plan(i32(news.ptr), i32(lens.ptr), i32(table.ptr), i32(list.ptr), i32(count.ptr), i32(out.ptr), i32(cp),

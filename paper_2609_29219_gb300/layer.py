@@ -49,7 +49,8 @@ class PagedCache:
 class RequestCache:
     """K and V pages [num_pages, page, Hkv, D] shared by up to `requests` requests of `capacity` tokens (whole
     pages), which take pages as they grow and give them back when they end.  All of it is on the device: a step
-    that was captured can be replayed."""
+    that was captured can be replayed.  `granted`: the tokens of each request that the last step had room
+    for (all that it brought, or none)."""
 
     def __init__(self, requests, num_pages, capacity, Hkv, D, page=16, device="cuda"):
         i32 = dict(dtype=torch.int32, device=device)
@@ -57,14 +58,14 @@ class RequestCache:
         self.capacity = per * page
         self.k, self.v = (torch.zeros((num_pages, page, Hkv, D), dtype=torch.bfloat16, device=device) for _ in range(2))
         self.table = torch.full((requests, per), -1, **i32)
-        self.lens = torch.zeros(requests, **i32)
+        self.lens, self.granted = (torch.zeros(requests, **i32) for _ in range(2))
         self.free_pages, self.free_count = torch.arange(num_pages, **i32), torch.full((1,), num_pages, **i32)
 
     def plan(self, new_lens, num_tokens):
         """Takes `new_lens` more tokens of each request (negative: it is over) into a step of num_tokens:
         (cu_seqlens, positions, slots, granted)."""
         cu, _, positions, slots, granted = loom.loom_paged_plan(new_lens, self.lens, self.table, self.free_pages, self.free_count,
-                                                                num_tokens, self.page, seqlens_k=self.lens)
+                                                                num_tokens, self.page, seqlens_k=self.lens, granted=self.granted)
         return cu, positions, slots, granted
 
 
@@ -104,8 +105,8 @@ class AttentionLayer:
     @torch.no_grad()
     def serve(self, x, cache, new_lens):
         """The new tokens of a RequestCache's requests, packed, x [T, model]: prompts, chunks of them, single tokens.
-        Rows past the last request's (and those of requests that the cache had no room for) mean nothing.  The
-        rotation tables must reach the cache's capacity."""
+        Rows past the last request's (and those of requests that the cache had no room for: cache.granted) mean
+        nothing.  The rotation tables must reach the cache's capacity."""
         if cache.capacity > self.cos.shape[0]:
             raise ValueError(f"the rotation tables have {self.cos.shape[0]} positions, the cache's requests up to {cache.capacity} tokens")
         cu, positions, slots, _ = cache.plan(new_lens, x.shape[0])
