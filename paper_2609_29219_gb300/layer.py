@@ -106,11 +106,19 @@ class AttentionLayer:
     def serve(self, x, cache, new_lens):
         """The new tokens of a RequestCache's requests, packed, x [T, model]: prompts, chunks of them, single tokens.
         Rows past the last request's (and those of requests that the cache had no room for: cache.granted) mean
-        nothing.  The rotation tables must reach the cache's capacity."""
+        nothing.  The rotation tables must reach the cache's capacity.  An x or a cache that is refused leaves the
+        cache as it was."""
+        if x.dim() != 2 or x.shape[1] != self.w_qkv.shape[1]:
+            raise ValueError(f"x must be [T, model] with a model of {self.w_qkv.shape[1]}, got shape {tuple(x.shape)}")
+        if tuple(cache.k.shape[2:]) != (self.Hkv, self.D):
+            raise ValueError(f"the cache's heads are {tuple(cache.k.shape[2:])}, the layer's {(self.Hkv, self.D)}")
         if cache.capacity > self.cos.shape[0]:
             raise ValueError(f"the rotation tables have {self.cos.shape[0]} positions, the cache's requests up to {cache.capacity} tokens")
+        if not x.shape[0]:
+            cache.plan(new_lens, 0)
+            return torch.empty_like(x)
+        qkv = loom.loom_gemm_bf16(x, self.w_qkv, b_transposed=True)  # (it refuses what else x may be, before anything is taken)
         cu, positions, slots, _ = cache.plan(new_lens, x.shape[0])
-        qkv = loom.loom_gemm_bf16(x, self.w_qkv, b_transposed=True)
         q = loom.loom_qkv_norm_rope_cache(qkv, self.q_norm, self.k_norm, self.cos, self.sin, positions, slots, cache.k, cache.v, self.Hq)
         o = loom.loom_attn_chunk_paged(q, cache.k, cache.v, cache.table, cu, cache.lens)
         return loom.loom_gemm_bf16(o.view(x.shape[0], -1), self.w_o, b_transposed=True)

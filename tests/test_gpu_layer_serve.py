@@ -71,3 +71,40 @@ def test_a_plan_with_granted_given(loom, monkeypatch):  # noqa: F811
             run(_ints(7, 7))
         with pytest.raises(TypeError, match="granted must be"):
             run(out.long())
+
+
+REFUSED = {  # what serve is given -> what it says
+    "width": (lambda x, c: (x[:, :64].contiguous(), c), "model"), "rank": (lambda x, c: (x[0], c), "model"),
+    "type": (lambda x, c: (x.float(), c), "bfloat16"), "rows": (lambda x, c: (x[::2], c), "contiguous"),
+    "empty and of another width": (lambda x, c: (x[:0, :64], c), "model"),
+    "cache of other heads": (lambda x, c: (x, _other(c, 1, 64)), "heads"), "cache of wider heads": (lambda x, c: (x, _other(c, 2, 128)), "heads")}
+
+
+def _other(cache, Hkv, D):
+    cache.k, cache.v = (t.new_zeros((*t.shape[:2], Hkv, D)) for t in (cache.k, cache.v))
+    return cache
+
+
+@pytest.mark.parametrize("name", REFUSED)
+def test_a_call_that_is_refused_leaves_the_cache_alone(loom, name):  # noqa: F811
+    import torch
+    mod, layer = _layer()
+    x, cache = torch.randn((20, 128), device="cuda").bfloat16(), mod.RequestCache(2, 8, 64, 2, 64)
+    layer.serve(x, cache, _ints(9, 4))
+    before = _held(cache)
+    change, says = REFUSED[name]
+    with pytest.raises((ValueError, TypeError), match=says):
+        layer.serve(*change(x, cache), _ints(9, 4))
+    assert _held(cache) == before
+
+
+def test_a_step_without_tokens(loom):  # noqa: F811
+    """Requests may end in a step that brings nothing else."""
+    import torch
+    mod, layer = _layer()
+    x, cache = torch.randn((20, 128), device="cuda").bfloat16(), mod.RequestCache(2, 8, 64, 2, 64)
+    layer.serve(x, cache, _ints(16, 4))
+    y = layer.serve(x[:0], cache, _ints(-1, 0))
+    loom.loom_attn_check_error()
+    assert y.shape == (0, 128) and y.dtype == x.dtype and y.is_cuda
+    assert cache.lens.tolist() == [0, 4] and int(cache.free_count) == 7
