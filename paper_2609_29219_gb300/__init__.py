@@ -683,15 +683,18 @@ def loom_paged_plan(new_lens, lens, block_table, free_pages, free_count, num_tok
                        seqlens_k, granted, num_tokens, page_size)
         if r is not None:
             return _fast_result(r, "loom_paged_plan")
+    T, page_size = operator.index(num_tokens), operator.index(page_size)  # (no fraction is cut off)
+    if T < 0:
+        raise ValueError("num_tokens must not be negative")
+    if max(T, abs(page_size)) > 0x7fffffff:  # (the C call's numbers have 32 bits)
+        raise ValueError("num_tokens and page_size must be below 2^31")
     np_ = _ptr(new_lens, "new_lens", _i32, 1)
     dev = _on_current(new_lens, "new_lens") if _several else None
-    B, T = new_lens.shape[0], int(num_tokens)
+    B = new_lens.shape[0]
     lp, tp = _ptr(lens, "lens", _i32, 1, dev), _ptr(block_table, "block_table", _i32, 2, dev)
     fp, cp = _ptr(free_pages, "free_pages", _i32, 1, dev), _ptr(free_count, "free_count", _i32, 1, dev)
     if lens.shape[0] != B or block_table.shape[0] != B or free_count.shape[0] != 1:
         raise ValueError("new_lens, lens, block_table and free_count must be [B], [B], [B, max_pages] and [1]")
-    if T < 0:
-        raise ValueError("num_tokens must not be negative")
     if free_count_out is None:
         free_count_out = free_count
     outs = []
@@ -703,7 +706,7 @@ def loom_paged_plan(new_lens, lens, block_table, free_pages, free_count, num_tok
             raise ValueError(f"{name} must be [{n}]")
         outs.append(t)
     st = (_lib or capi()).loom_paged_plan(
-        np_, lp, tp, fp, cp, *(t.data_ptr() for t in outs), B, T, free_pages.shape[0], int(page_size), block_table.shape[1],
+        np_, lp, tp, fp, cp, *(t.data_ptr() for t in outs), B, T, free_pages.shape[0], page_size, block_table.shape[1],
         _stream_of(stream, new_lens))
     _check(st, "loom_paged_plan")
     return tuple(outs[1:])
