@@ -638,6 +638,8 @@ def loom_attn_chunk_paged(q, k_cache, v_cache, block_table, cu_seqlens_q, seqlen
     B, max_pages = block_table.shape
     if cu_seqlens_q.shape[0] != B + 1 or seqlens_k.shape[0] != B:
         raise ValueError("block_table, cu_seqlens_q and seqlens_k must be [B, max_pages], [B + 1] and [B]")
+    if max(B, max_pages) > 0x7fffffff:  # (the C call's numbers have 32 bits)
+        raise LoomError(2, "loom_attn_chunk_paged")
     if o is None:
         o = _new((total_q, Hq, D), (Hq * D, D, 1), _bf16, q, True, stream)
     elif o.shape != q.shape:
@@ -695,6 +697,8 @@ def loom_paged_plan(new_lens, lens, block_table, free_pages, free_count, num_tok
     fp, cp = _ptr(free_pages, "free_pages", _i32, 1, dev), _ptr(free_count, "free_count", _i32, 1, dev)
     if lens.shape[0] != B or block_table.shape[0] != B or free_count.shape[0] != 1:
         raise ValueError("new_lens, lens, block_table and free_count must be [B], [B], [B, max_pages] and [1]")
+    if max(*block_table.shape, free_pages.shape[0]) > 0x7fffffff:
+        raise LoomError(2, "loom_paged_plan")
     if free_count_out is None:
         free_count_out = free_count
     outs = []
