@@ -26,8 +26,9 @@
 //
 // What bounds it: many queries, the tensor cores, as the prefill kernel, whose step this one repeats
 // (two query tiles alternate on the tensor pipe, P in TMEM); few queries, the cache's bandwidth; small calls,
-// latencies.  GB300, H32/8 D 128: 2048 tokens after 30000 in 641 to 656 us, 1590 to 1625 TFLOP/s; 16 single
-// tokens of 4K to 8K keys in 73.7 us, 5.5 TB/s; 31 of 100 to 12K and 481 tokens of a prompt in 138 us,
+// latencies.  GB300, H32/8 D 128, on the device alone: 2048 tokens after 30000 in 637 to 651 us, 1599 to 1634 TFLOP/s (call
+// after call from Python, under the power cap, 718 to 732 us, 1422 to 1450 TFLOP/s); 16 single
+// tokens of 4K to 8K keys in 73.8 us, 5.5 TB/s; 31 of 100 to 12K and 481 tokens of a prompt in 138 us,
 // 5.7 TB/s; one of 500 keys in 10.3 us.  Two tiles' alternation and 128 keys a tile: a step of both
 // takes 2900 clocks for 2048 of the tensor pipe, and TMEM has room for no third S and O.
 #include <cuda.h>
@@ -47,14 +48,17 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kRescaleThreshold = 8.0f;  // base-2 units; P <= 2^8 between rescales
 
 // The line's units: a key of a pair of tiles costs 1 << kKeyLg2, of a single tile 1 << kKeyLg1; a unit kUnitCost more.
-// (1400, 2000, 3000 and 4200: 8192 tokens alone 357, 358, 361 and 365 us, 16 tokens of 4K to 8K keys 73.7, 73.8, 74.7 and
-// 76.5; 800: 8192 tokens 384.)
+// (1000, 1400, 2000 and 3000: 8192 tokens alone 377, 354, 357 and 359 us, 2048 alone 50.0, 50.0, 48.9 and 49.9, 512 after 3584
+// 45.8, 46.0, 44.7 and 44.3, 48 drafts 23.9, 23.6, 23.3 and 23.2, 16 tokens of 4K to 8K keys 74.0, 73.8, 73.8 and 74.9.)
 constexpr int kKeyLg2 = 3, kKeyLg1 = 2, kUnitCost = 2000;
-// The least that a CTA is given of units that are longer: they are not cut into shorter pieces.
+// The least that a CTA is given of units that are longer: they are not cut into shorter pieces.  (1000, 2000, 3000, 6000 and
+// 12000: one token of 500 keys 11.4, 10.5, 10.3, 10.3 and 10.3 us, of 1024 15.0, 16.7, 16.5, 16.0 and 15.8, of 4096 21.6, 19.6,
+// 19.8, 24.3 and 41.4, four of 4096 25.5, 23.3, 25.7, 27.3 and 43.9, 48 drafts 23.4, 23.3, 23.3, 23.3 and 27.2.)
 constexpr int kLeastStretch = 3000;
 // A cut that would leave less than this of a unit's tiles on one side falls on its end: joining a piece costs more
-// than the unevenness.  One token after 4095: 22.0 us with every cut, 19.2 to 21.2 so, 21.9 with twice this; 128 tokens, 64
-// wide, after 10 to 500: 47.2, 44.5, 44.3; 16 tokens after 4K to 8K: 75.0, 75.5, 77.3.
+// than the unevenness.  It concerns single tiles: a pair's key tile costs as much by itself, so a pair is cut where the line says.
+// With every cut, so, and with twice this: 128 tokens, 64 wide, after 10 to 500 39.5, 37.5 and 36.8 us; 48 drafts 23.5, 23.3
+// and 23.9; one token of 4096 keys 19.3, 19.8 and 22.6; 16 of 4K to 8K 73.8, 73.8 and 74.2.
 constexpr int kSnap = 1024;
 
 template <int D>
@@ -350,7 +354,9 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, const K
 // s_tm: mask keys >= limit, move the running max lazily, write P = 2^(S c - m) as bf16 over the first
 // half of S's columns in two halves (arriving on bar_p and bar_p + 8 after each), rescale O at o_tm where
 // the max moved, and add to the row's sum.  S is only ready after the tile's previous P.V (issued before it by
-// the same warp), so the rescale needs no wait.
+// the same warp), so the rescale needs no wait.  P is rounded to bf16 because the product takes one type for P and V, and V is
+// the cache's; l sums the weights before that, in 32 bits.  A weight is off by half a step at most, to either side, which
+// puts an output's error at 0.0023 of the norm where its own rounding to bf16 is 0.0017; LSE has nothing of it.
 template <int D>
 __device__ __forceinline__ bool chunk_step(uint32_t s_tm, uint32_t o_tm, uint32_t bar_s, uint32_t par_s, uint32_t bar_p,
                                            bool first, int limit, float c, float& m_run, float& l_run, const KernelCtl& ctl,

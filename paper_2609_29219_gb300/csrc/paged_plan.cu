@@ -21,10 +21,13 @@
 namespace loom {
 namespace {
 
-// Blocks of the cluster: 16 where the device has room for one of them, else 8 (which any has).  (4096 requests with 130000
-// tokens, 256 with 65000: 4 blocks 34.0 and 14.6 us, 8 23.6 and 10.9, 16 18.6 and 9.9.)
+// Blocks of the cluster: 16 where the device has room for one of them, else 8 (which any has).  (4096 requests with 68648
+// tokens, 256 with 22883: 4 blocks 31.2 and 13.5 us, 8 21.6 and 10.3, 16 17.2 and 9.3.)
 constexpr int kThreads = 1024, kClusterBlocks = 16, kPortableBlocks = 8;
-// Requests and tokens that one block deals with alone.
+// Requests and tokens that one block deals with alone: it needs no 16 SMs of one GPC free at the same time.  On a device with
+// nothing else to do a cluster is sooner all the same (alone and in a cluster: 4 requests with 4 tokens 5.0 and 4.8 us, 64
+// with 64 6.2 and 5.8, 256 with 256 6.4 and 6.2, 512 with 1866 8.3 and 7.0, 1000 with 1450 8.6 and 7.6), and past these bounds
+// by more (64 with 2846 8.0 and 6.1, 2000 with 2000 10.0 and 8.5, 4096 with 4096 13.6 and 9.6).
 constexpr int kAloneTokens = 2048, kAloneRequests = 1024;
 
 // Exclusive prefix sums of a and b over the block, and their totals.
@@ -54,7 +57,7 @@ __device__ __forceinline__ Sums scan(long long a, long long b, long long (*part)
 }
 
 // Rows in pages, in 32 bits (rows and page - 1 are below 2^31), by a shift where it does: divisions of 64 bits took
-// most of the kernel's instructions, and of 32 a third (4096 requests with 130000 tokens 18.6 us, so 17.0).
+// most of the kernel's instructions, and of 32 a third (4096 requests with 68648 tokens 18.9 us, so 17.2).
 struct Pages {
   unsigned page;
   int lg;  // of a power of two; else -1

@@ -107,7 +107,8 @@ class AttentionLayer:
         """The new tokens of a RequestCache's requests, packed, x [T, model]: prompts, chunks of them, single tokens.
         Rows past the last request's (and those of requests that the cache had no room for: cache.granted) mean
         nothing.  The rotation tables must reach the cache's capacity.  An x or a cache that is refused leaves the
-        cache as it was."""
+        cache as it was.  (The step is planned here: a model of several layers plans once and makes the calls after
+        that a layer.  Where each request brings one token the paged decode is mostly the faster call: see step.)"""
         if x.dim() != 2 or x.shape[1] != self.w_qkv.shape[1]:
             raise ValueError(f"x must be [T, model] with a model of {self.w_qkv.shape[1]}, got shape {tuple(x.shape)}")
         if tuple(cache.k.shape[2:]) != (self.Hkv, self.D):
