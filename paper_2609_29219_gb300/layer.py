@@ -49,8 +49,8 @@ class PagedCache:
 class RequestCache:
     """K and V pages [num_pages, page, Hkv, D] shared by up to `requests` requests of `capacity` tokens (whole
     pages), which take pages as they grow and give them back when they end.  All of it is on the device: a step
-    that was captured can be replayed.  `granted`: the tokens of each request that the last step had room
-    for (all that it brought, or none)."""
+    that was captured can be replayed.  `granted`: the tokens of each request that the last step that a
+    layer served had room for (all that it brought, or none)."""
 
     def __init__(self, requests, num_pages, capacity, Hkv, D, page=16, device="cuda"):
         i32 = dict(dtype=torch.int32, device=device)
@@ -61,11 +61,11 @@ class RequestCache:
         self.lens, self.granted = (torch.zeros(requests, **i32) for _ in range(2))
         self.free_pages, self.free_count = torch.arange(num_pages, **i32), torch.full((1,), num_pages, **i32)
 
-    def plan(self, new_lens, num_tokens):
+    def plan(self, new_lens, num_tokens, granted=None):
         """Takes `new_lens` more tokens of each request (negative: it is over) into a step of num_tokens:
-        (cu_seqlens, positions, slots, granted)."""
+        (cu_seqlens, positions, slots, granted), the last one written to the tensor given or a new one."""
         cu, _, positions, slots, granted = loom.loom_paged_plan(new_lens, self.lens, self.table, self.free_pages, self.free_count,
-                                                                num_tokens, self.page, seqlens_k=self.lens, granted=self.granted)
+                                                                num_tokens, self.page, seqlens_k=self.lens, granted=granted)
         return cu, positions, slots, granted
 
 
@@ -116,10 +116,10 @@ class AttentionLayer:
         if cache.capacity > self.cos.shape[0]:
             raise ValueError(f"the rotation tables have {self.cos.shape[0]} positions, the cache's requests up to {cache.capacity} tokens")
         if not x.shape[0]:
-            cache.plan(new_lens, 0)
+            cache.plan(new_lens, 0, cache.granted)
             return torch.empty_like(x)
         qkv = loom.loom_gemm_bf16(x, self.w_qkv, b_transposed=True)  # (it refuses what else x may be, before anything is taken)
-        cu, positions, slots, _ = cache.plan(new_lens, x.shape[0])
+        cu, positions, slots, _ = cache.plan(new_lens, x.shape[0], cache.granted)
         q = loom.loom_qkv_norm_rope_cache(qkv, self.q_norm, self.k_norm, self.cos, self.sin, positions, slots, cache.k, cache.v, self.Hq)
         o = loom.loom_attn_chunk_paged(q, cache.k, cache.v, cache.table, cu, cache.lens)
         return loom.loom_gemm_bf16(o.view(x.shape[0], -1), self.w_o, b_transposed=True)

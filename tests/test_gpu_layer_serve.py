@@ -55,6 +55,17 @@ def test_what_was_granted_after_a_replay(loom):  # noqa: F811
     assert cache.granted.tolist() == [0, 5] and cache.lens.tolist() == [0, 5]
 
 
+def test_a_plan_of_its_own_keeps_its_grants(loom):  # noqa: F811
+    """What `plan` returns is that call's, whatever comes after; `granted` is the layer's."""
+    import torch
+    mod, layer = _layer()
+    cache = mod.RequestCache(2, 4, 64, 2, 64)
+    first, second = cache.plan(_ints(5, 6), 11)[3], cache.plan(_ints(1, 0), 1)[3]
+    layer.serve(torch.randn((8, 128), device="cuda").bfloat16(), cache, _ints(0, 8))
+    third = cache.plan(_ints(2, 2), 4)[3]
+    assert [t.tolist() for t in (first, second, third, cache.granted)] == [[5, 6], [1, 0], [2, 2], [0, 8]]
+
+
 def test_a_plan_with_granted_given(loom, monkeypatch):  # noqa: F811
     """The compiled binding writes into it, as the Python code does, and takes no other shape or type."""
     import torch
